@@ -18,9 +18,10 @@
  * one it came from (same pointer and strides).
  *
  * Values on the device that the host cannot check (slots, page numbers,
- * lengths) are checked by the kernels: an index outside its range reads and
- * writes nothing, and GTS_ERR_INVALID_PARAMS is stored to *d_status where that
- * is given.  *d_status is never cleared by the library.
+ * lengths) are checked by the kernels: an index outside its range is never
+ * followed, and GTS_ERR_INVALID_PARAMS is stored to *d_status where that is
+ * given; what it would have contributed to a result is then unspecified.
+ * *d_status is never cleared by the library.
  */
 #ifndef GTS_SERVING_H
 #define GTS_SERVING_H
