@@ -4,13 +4,14 @@
 // Mathematics.  With s_j = scale * q . k_j over the keys a query sees, m = max s_j, p_j = exp(s_j - m):
 // out = sum p_j v_j / sum p_j, lse = m + log sum p_j.  The keys are taken tile by tile with the maximum and the sum so
 // far: when a tile raises the maximum from m to m', what was summed is multiplied by exp(m - m').
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include <algorithm>
 #include <atomic>
 #include <cstring>
-#include <string>
+#include <type_traits>
 
 #include "internal.h"
 
@@ -91,7 +92,8 @@ constexpr int WARPS = 4, THREADS = 32 * WARPS;
 
 struct Line {           // the units of one launch
   int has_prefix, has_own;
-  int rows;             // of a pair's tile
+  int rows, keys;       // of a pair's tile, of a unit
+  int64_t per;          // units per block, where the host knows them
   int prefix_tiles, own_tiles;   // row tiles of the prefix's rows, of a sequence's rows
   int blocks;
   int64_t *starts;      // [n_seqs + 2]: first unit of each sequence, the units of all, units per block
@@ -101,7 +103,7 @@ struct Line {           // the units of one launch
   float2 *whole_ml[2];
 };
 
-__device__ __forceinline__ int tiles_of(int keys) { return (keys + KEYS - 1) / KEYS; }
+__host__ __device__ __forceinline__ int tiles_of(int keys, int tile = KEYS) { return (keys + tile - 1) / tile; }
 
 __device__ __forceinline__ int own_len(const Args &a, int b) {
   const int len = a.lens[b], most = a.max_pages * a.page_size;
@@ -447,6 +449,381 @@ __global__ void __launch_bounds__(THREADS) k_stream(const Args a, const Line w) 
   }
 }
 
+// ---------------------------------------------------------------- the prefix on the tensor cores
+__device__ __forceinline__ void bar_init(uint32_t bar, int count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("{\n.reg .b64 t;\nmbarrier.arrive.shared::cta.b64 t, [%0];\n}" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("{\n.reg .b64 t;\nmbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1;\n}" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
+// Every wait ends: after two seconds, or when another warp has given up, the block winds down with an error status.
+__device__ __forceinline__ uint64_t now_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+constexpr uint64_t LIMIT_NS = 2000000000ull;
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *dead) {
+  if (bar_try(bar, parity)) return true;
+  const uint64_t from = now_ns();
+  while (!*dead) {
+    for (int n = 0; n < 16; n++)
+      if (bar_try(bar, parity)) return true;
+    if (now_ns() - from > LIMIT_NS) *dead = 1;
+  }
+  return false;
+}
+__device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int page, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(page), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+// d [128 rows][N] (+)= a [128][16] b [16][N]; a from shared memory, or from tensor memory
+__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+               ::"r"(d), "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ void tc_mma_t(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add) {
+  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
+               ::"r"(d), "r"(a), "l"(b), "r"(shape), "r"((uint32_t)add) : "memory");
+}
+#define R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
+#define W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
+// 32 columns of the warp's 32 rows, one row a lane
+__device__ __forceinline__ void tc_ld(uint32_t *r, uint32_t at) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+               "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+               : R8(r, 0), R8(r, 8), R8(r, 16), R8(r, 24) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tc_st(uint32_t at, const uint32_t *r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+               "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+               ::W8(r, 0), W8(r, 8), W8(r, 16), W8(r, 24), "r"(at) : "memory");
+}
+#undef R8
+#undef W8
+__device__ __forceinline__ void tc_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// Operand in shared memory as rows of 128 bytes, eight rows to a swizzled group of 1024 bytes, groups one after the other;
+// `blocks`: bytes from one 128-byte column of groups to the next, for operands that are wider and not summed over.
+__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t blocks) {
+  return (uint64_t)((at & 0x3FFFF) >> 4) | (uint64_t)(blocks >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+
+// The rows of all sequences against the prefix.  A block holds 2 x 128 rows of one key head and passes along its stretch of
+// the keys in tiles of 128, each read once for all rows:
+//   warp 9 brings tiles of keys and values from their pages by TMA into a ring;
+//   warp 8 issues the products: scores S = Q K^T to tensor memory, O += P V with P from tensor memory;
+//   warps 0..3 and 4..7 take one half of the rows each, one row a thread: maximum, weights, sum.  P overwrites S.
+// The halves alternate: while one turns scores into weights, the tensor cores work for the other.  The maximum that scores
+// are taken against is raised, and what was summed rescaled, only when it has grown by more than 8 (in log 2): weights stay
+// below 2^8, sums are exact in the same way, and the result is the same up to rounding.
+// Weights are rounded to the values' type for their product; the sum is of the unrounded ones, all else is in 32 bits.
+constexpr int TC_KEYS = 128, TC_THREADS = 384;  // warps 10 and 11 fill up the third warpgroup
+constexpr float RAISE = 8.f;
+template <int D> struct Tc {
+  static constexpr int TILE = TC_KEYS * D * 2, STAGES = D == 64 ? 8 : 5, Q = 2 * 128 * D * 2;
+  static constexpr int SMEM = Q + STAGES * TILE + 1024 /* alignment */ + 256 /* barriers */;
+};
+
+// 384 threads start with 168 registers each (64512): the row threads go on with 216 (55296), the rest with 56 (7168).
+#define MORE_REGISTERS() asm volatile("setmaxnreg.inc.sync.aligned.u32 216;")
+#define FEWER_REGISTERS() asm volatile("setmaxnreg.dec.sync.aligned.u32 56;")
+
+struct Pages {
+  CUtensorMap k, v;    // pages x heads x tokens (or tokens x heads) x D, boxes of `box` tokens of a head x 64 values
+  int box, k_heads_first, v_heads_first;
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Line w, const __grid_constant__ Pages maps, const uint32_t flip) {
+  constexpr int TILE = Tc<D>::TILE, STAGES = Tc<D>::STAGES, HALF = TC_KEYS * 128;   // 64 columns of a tile
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char *const smem = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  unsigned char *const qs = smem, *const ring = smem + Tc<D>::Q;
+  uint64_t *const bars = (uint64_t *)(ring + STAGES * TILE);
+  uint32_t *const tmem_at = (uint32_t *)(bars + 2 * STAGES + 7);
+  volatile int *const dead = (volatile int *)(tmem_at + 1);
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const uint32_t bar0 = smem_u32(bars), q_at = smem_u32(qs), ring_at = smem_u32(ring);
+  auto full = [&](int s) { return bar0 + s * 8; };
+  auto empty = [&](int s) { return bar0 + (STAGES + s) * 8; };
+  auto q_full = [&](int h) { return bar0 + (2 * STAGES + h) * 8; };
+  auto s_full = [&](int h) { return bar0 + (2 * STAGES + 2 + h) * 8; };
+  auto p_full = [&](int h) { return bar0 + (2 * STAGES + 4 + h) * 8; };
+  const uint32_t ended = bar0 + (2 * STAGES + 6) * 8;
+  if (tid == 0) {
+    bar_init(ended, 1);
+    for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(empty(s), 1);
+    for (int h = 0; h < 2; h++) bar_init(q_full(h), 128), bar_init(s_full(h), 1), bar_init(p_full(h), 128);
+    *dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_at)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  tc_before();
+  __syncthreads();
+  tc_after();
+  const uint32_t tmem = *tmem_at;
+  auto scores = [&](int h) { return tmem + h * 128; };
+  auto sums = [&](int h) { return tmem + 256 + h * 128; };
+
+  const int n = tiles_of(a.prefix_len, TC_KEYS);
+  const int64_t u0 = w.per * blockIdx.x, u1 = min((int64_t)n * a.kv_heads * w.prefix_tiles, u0 + w.per);
+  const int all = a.n_seqs * a.n_new * a.group;
+
+  if (warp >= 8) {
+    FEWER_REGISTERS();
+    if (warp == 9) {
+      // ---- keys and values: lane x brings the x-th box of tokens of a tile, both of its 64-value halves
+      const int boxes = TC_KEYS / maps.box;
+      int it = 0;
+      bool alive = true;
+      for (int64_t u = u0; u < u1 && alive; u++) {
+        const int pair = (int)(u / n), tile = (int)(u - (int64_t)pair * n), kh = pair / w.prefix_tiles;
+        const int key = tile * TC_KEYS + lane * maps.box;
+        const bool live = lane < boxes && key < a.prefix_len;
+        int page = 0;
+        if (live) {
+          page = a.prefix_pages[key / a.page_size];
+          if (page < 0 || page >= a.n_pages) {             // outside the map: the box is filled with zeros
+            page = a.n_pages;
+            if (a.status) *a.status = GTS_ERR_INVALID_PARAMS;
+          }
+        }
+        const uint32_t bytes = __popc(__ballot_sync(~0u, live)) * maps.box * D * 2;
+        for (int kv = 0; kv < 2; kv++, it++) {
+          const int s = it % STAGES;
+          if (it >= STAGES && !bar_wait(empty(s), (it / STAGES - 1) & 1, dead)) alive = false;
+          alive = __all_sync(~0u, alive);
+          if (!alive) break;
+          if (lane == 0) bar_expect(full(s), bytes);
+          __syncwarp();
+          if (live) {
+            const bool heads_first = kv ? maps.v_heads_first : maps.k_heads_first;
+            const int token = key % a.page_size;
+#pragma unroll
+            for (int x = 0; x < D / 64; x++)
+              tile_load(ring_at + s * TILE + x * HALF + lane * maps.box * 128, kv ? &maps.v : &maps.k, x * 64, heads_first ? kh : token,
+                        heads_first ? token : kh, page, full(s));
+          }
+        }
+      }
+      if (!alive) {                                        // copies in flight end before the block does
+        const int first = max(0, it - STAGES);
+        const uint64_t from = now_ns();
+        for (int x = first; x < it; x++)
+          while (!bar_try(full(x % STAGES), (x / STAGES) & 1) && now_ns() - from < LIMIT_NS) {}
+      }
+    } else if (warp == 8) {
+      // ---- products; every lane follows, lane 0 issues
+      constexpr uint32_t TYPE = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+      constexpr uint32_t COMMON = 1u << 4 | TYPE << 7 | TYPE << 10 | (128u >> 4) << 24;
+      constexpr uint32_t QK = COMMON | (TC_KEYS >> 3) << 17, PV = COMMON | 1u << 16 | (D >> 3) << 17;
+      int it = 0;                                          // ring position
+      uint32_t seg[2] = {0, 0}, turn[2] = {0, 0};          // each half's pairs and tiles so far: the phases of its barriers
+      bool alive = true;
+      auto need = [&](uint32_t bar, uint32_t parity) { alive = __all_sync(~0u, alive && bar_wait(bar, parity, dead)); };
+      auto qk = [&](int h, int s) {
+        if (lane == 0) {
+#pragma unroll
+          for (int k = 0; k < D / 16; k++)
+            tc_mma(scores(h), operand(q_at + h * (Tc<D>::Q / 2) + k / 4 * HALF + k % 4 * 32, 16),
+                   operand(ring_at + s * TILE + k / 4 * HALF + k % 4 * 32, 16), QK, k > 0);
+          tc_commit(s_full(h));
+        }
+      };
+      for (int64_t u = u0; u < u1 && alive;) {
+        const int pair = (int)(u / n), tile0 = (int)(u - (int64_t)pair * n), count = (int)min((int64_t)(n - tile0), u1 - u);
+        const int halves = all - pair % w.prefix_tiles * 256 > 128 ? 2 : 1;
+        for (int h = 0; h < halves && alive; h++) need(q_full(h), seg[h]++ & 1);
+        if (alive) need(full(it % STAGES), (it / STAGES) & 1);
+        if (!alive) break;
+        tc_after();
+        for (int h = 0; h < halves; h++) qk(h, it % STAGES);
+        if (lane == 0) tc_commit(empty(it % STAGES));
+        it++;
+        for (int j = 0; j < count && alive; j++) {
+          const int sv = it % STAGES, nv = min(TC_KEYS, a.prefix_len - (tile0 + j) * TC_KEYS);
+          need(full(sv), (it / STAGES) & 1);
+          it++;
+          const int sk = it % STAGES, sk_phase = (it / STAGES) & 1;
+          if (j + 1 < count) it++;
+          if (nv % 16) {                                   // value rows past the end, in the last 16 that count: zeros
+            for (int x = lane; x < (16 - nv % 16) * (D / 8); x += 32) {
+              const int r = nv + x / (D / 8), c = x % (D / 8);
+              *(uint4 *)(ring + sv * TILE + c / 8 * HALF + r * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+          }
+          for (int h = 0; h < halves && alive; h++) {
+            need(p_full(h), turn[h]++ & 1);
+            if (!alive) break;
+            tc_after();
+            if (lane == 0) {
+              for (int k = 0; k * 16 < nv; k++)
+                tc_mma_t(sums(h), scores(h) + k * 8, operand(ring_at + sv * TILE + k * 2048, HALF), PV, j > 0 || k > 0);
+              if (h == halves - 1) tc_commit(empty(sv));
+            }
+            if (j + 1 < count) {
+              if (h == 0) {
+                need(full(sk), sk_phase);
+                if (!alive) break;
+              }
+              qk(h, sk);
+              if (h == halves - 1 && lane == 0) tc_commit(empty(sk));
+            } else if (lane == 0) {
+              tc_commit(s_full(h));                        // the pair's sums are complete
+            }
+          }
+        }
+        u += count;
+      }
+      if (!alive) {                                        // as do products in flight
+        if (lane == 0) tc_commit(ended);
+        const uint64_t from = now_ns();
+        while (!bar_try(ended, 0) && now_ns() - from < LIMIT_NS) {}
+      }
+    }
+  } else {
+    // ---- one row a thread
+    MORE_REGISTERS();
+    const int h = warp / 4, r = tid % 128;
+    const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+    const float sl2 = fabsf(a.scale) * 1.4426950408889634f;
+    const bool q_aligned = (((uintptr_t)a.q >> 1 | a.q_seq | a.q_tok | a.q_head) & 7) == 0;
+    uint32_t turn = 0;                                   // phases of s_full: a pair's tiles, then its sums
+    bool alive = true;
+    for (int64_t u = u0; u < u1 && alive;) {
+      const int pair = (int)(u / n), tile0 = (int)(u - (int64_t)pair * n), count = (int)min((int64_t)(n - tile0), u1 - u);
+      const int kh = pair / w.prefix_tiles, row = pair % w.prefix_tiles * 256 + h * 128 + r;
+      if (all - pair % w.prefix_tiles * 256 <= h * 128) {  // no rows for this half: the phases of its barriers stand still
+        u += count;
+        continue;
+      }
+      const Row p = row_of(a, -1, kh, row);
+      const T *src = (const T *)a.q + p.b * a.q_seq + p.i * a.q_tok + p.h * a.q_head;
+#pragma unroll
+      for (int c = 0; c < D / 8; c++) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < all) {
+          if (q_aligned) {
+            v = *(const uint4 *)(src + c * 8);
+          } else {
+            T e[8];
+#pragma unroll
+            for (int x = 0; x < 8; x++) e[x] = src[c * 8 + x];
+            memcpy(&v, e, 16);
+          }
+          v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;   // a negative scale: its sign goes to the queries
+        }
+        *(uint4 *)(qs + h * (Tc<D>::Q / 2) + c / 8 * HALF + r * 128 + ((c % 8) ^ (r & 7)) * 16) = v;
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      bar_arrive(q_full(h));
+
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < count; j++, turn++) {
+        alive = __all_sync(~0u, bar_wait(s_full(h), turn & 1, dead));
+        if (!alive) break;
+        tc_after();
+        uint32_t s[TC_KEYS];
+#pragma unroll
+        for (int c = 0; c < 4; c++) tc_ld(s + c * 32, scores(h) + lanes + c * 32);
+        tc_ld_wait();
+        const int nv = a.prefix_len - (tile0 + j) * TC_KEYS;
+        if (nv < TC_KEYS) {
+#pragma unroll
+          for (int c = 0; c < TC_KEYS; c++)
+            if (c >= nv) s[c] = 0xFF800000u;             // -infinity
+        }
+        float top[4];
+#pragma unroll
+        for (int c = 0; c < 4; c++) top[c] = __uint_as_float(s[c]);
+#pragma unroll
+        for (int c = 4; c < TC_KEYS; c++) top[c & 3] = fmaxf(top[c & 3], __uint_as_float(s[c]));
+        const float big = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sl2;
+        const bool raise = big > m + RAISE || (m == -INFINITY && big > m);
+        if (j == 0) {
+          m = big;
+        } else if (__any_sync(~0u, raise)) {
+          const float to = raise ? big : m, f = raise ? exp2_fast(m - to) : 1.f;
+          uint32_t o[32];
+#pragma unroll 1
+          for (int c = 0; c < D / 32; c++) {
+            tc_ld(o, sums(h) + lanes + c * 32);
+            tc_ld_wait();
+#pragma unroll
+            for (int x = 0; x < 32; x++) o[x] = __float_as_uint(__uint_as_float(o[x]) * f);
+            tc_st(sums(h) + lanes + c * 32, o);
+          }
+          l *= f;
+          m = to;
+        }
+        const float from = m == -INFINITY ? 0.f : m;
+        uint32_t pk[TC_KEYS / 2];
+        float part[4] = {};
+#pragma unroll
+        for (int c = 0; c < TC_KEYS; c += 2) {
+          const float x = exp2_fast(fmaf(__uint_as_float(s[c]), sl2, -from));
+          const float y = exp2_fast(fmaf(__uint_as_float(s[c + 1]), sl2, -from));
+          part[c & 2] += x, part[(c & 2) + 1] += y;
+          pk[c / 2] = pack<T>(x, y);
+        }
+        tc_st(scores(h) + lanes, pk);
+        tc_st(scores(h) + lanes + 32, pk + 32);
+        tc_st_wait();
+        tc_before();
+        bar_arrive(p_full(h));
+        l += (part[0] + part[1]) + (part[2] + part[3]);
+      }
+      if (!alive) break;
+      alive = __all_sync(~0u, bar_wait(s_full(h), turn & 1, dead));
+      turn++;
+      if (!alive) break;
+      tc_after();
+      const bool whole = count == n;
+      const int64_t at = whole ? ((int64_t)p.b * a.n_new + p.i) * a.q_heads + p.h
+                               : ((int64_t)blockIdx.x * 2 + (u > u0)) * 256 + h * 128 + r;
+      float *to = (whole ? w.whole_o[0] : w.cut_o) + at * D;
+#pragma unroll 1
+      for (int c = 0; c < D / 32; c++) {
+        uint32_t o[32];
+        tc_ld(o, sums(h) + lanes + c * 32);
+        tc_ld_wait();
+        if (row < all) {
+#pragma unroll
+          for (int x = 0; x < 32; x += 4) *(uint4 *)(to + c * 32 + x) = make_uint4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+        }
+      }
+      if (row < all) (whole ? w.whole_ml[0] : w.cut_ml)[at] = make_float2(m, l);
+      tc_before();
+      u += count;
+    }
+  }
+  tc_before();
+  __syncthreads();
+  if (*dead && tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+
 // Joins what a row's pairs left, prefix first, then the sequence's own keys, each in the order of its blocks: one warp a
 // row.  A row whose one pair was written whole, with no prefix, is done already.
 template <typename T, int D>
@@ -468,7 +845,7 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
   };
   auto gather = [&](const Line &w, bool own, int r, int tiles, int64_t start, int64_t n) {
     const int pair = kh * tiles + r / w.rows;
-    const int64_t u0 = start + pair * n, per = w.starts[a.n_seqs + 1], c0 = u0 / per, c1 = (u0 + n - 1) / per;
+    const int64_t u0 = start + pair * n, per = w.per ? w.per : w.starts[a.n_seqs + 1], c0 = u0 / per, c1 = (u0 + n - 1) / per;
     if (c0 == c1) {
       if (own && a.prefix_len == 0) return true;
       add(w.whole_o[own] + row * D, w.whole_ml[own][row]);
@@ -480,7 +857,7 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
     }
     return false;
   };
-  if (a.prefix_len) gather(lp, false, (b * a.n_new + i) * a.group + h - kh * a.group, lp.prefix_tiles, 0, tiles_of(a.prefix_len));
+  if (a.prefix_len) gather(lp, false, (b * a.n_new + i) * a.group + h - kh * a.group, lp.prefix_tiles, 0, tiles_of(a.prefix_len, lp.keys));
   const int n = tiles_of(own_len(a, b));
   if (n && gather(lo, true, i * a.group + h - kh * a.group, lo.own_tiles, lo.starts[b], n)) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -505,43 +882,108 @@ template <typename K> cudaError_t grant(K kernel, int bytes, std::atomic<uint64_
 
 size_t up(size_t x) { return (x + 255) / 256 * 256; }
 
+// How a call is run.  The prefix's rows (of all sequences) go to the tensor cores' kernel where its boxes fit the pages and
+// there are rows enough to fill its tiles; else to the streaming kernel, in the launch of the sequences' own keys or, with
+// many rows, in one of its own with tiles of 64 rows.
+enum Way { TOGETHER, APART, TENSOR };
 struct Plan {
-  int wm;              // warps along the rows
-  int blocks;
-  Line line;
+  Way way;
+  Line prefix, own;
   size_t bytes;
 };
 
-// rows of a sequence's own pairs decide the shape: 16, 32 or 64 of them to a tile
-Plan make_plan(const gts_attention_desc &d, char *at) {
+constexpr int64_t TENSOR_ROWS = 48, APART_ROWS = 64;
+
+int box_of(int page_size) {  // tokens of a TMA box: the largest power of two that divides both the page and a tile
+  int box = 1;
+  while (box < TC_KEYS && page_size % (box * 2) == 0) box *= 2;
+  return box;
+}
+
+int stream_blocks(int D) { return SMS * (D == 64 ? 3 : D == 128 ? 2 : 1); }
+
+Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
   const int D = (int)d.cache.head_dim, group = (int)(d.q_heads / d.cache.kv_heads);
   const int64_t own_rows = (int64_t)d.n_new * group, all = own_rows * d.n_seqs;
   Plan p = {};
-  p.wm = own_rows <= 16 ? 1 : own_rows <= 32 ? 2 : 4;
-  const int rows = 16 * p.wm;
-  p.blocks = SMS * (D == 64 ? 3 : D == 128 ? 2 : 1);
-  Line &w = p.line;
-  w.has_prefix = d.prefix_len > 0, w.has_own = 1, w.rows = rows;
-  w.prefix_tiles = (int)((all + rows - 1) / rows), w.own_tiles = (int)((own_rows + rows - 1) / rows);
-  w.blocks = p.blocks;
+  p.way = !d.prefix_len || all <= (tensor ? TENSOR_ROWS : APART_ROWS) || (!tensor && own_rows > 32) ? TOGETHER : tensor ? TENSOR : APART;
   size_t n = 0;
   auto take = [&](size_t bytes) {
     char *x = at ? at + n : nullptr;
     n += up(bytes);
     return x;
   };
-  const size_t total_rows = (size_t)d.n_seqs * d.n_new * d.q_heads, cut = (size_t)p.blocks * 2 * rows;
-  w.starts = (int64_t *)take(((size_t)d.n_seqs + 2) * 8);
-  w.cut_ml = (float2 *)take(cut * 8);
-  w.cut_o = (float *)take(cut * D * 4);
+  auto line = [&](Line &w, int rows, int keys, int blocks, bool has_prefix, bool has_own) {
+    w.has_prefix = has_prefix, w.has_own = has_own, w.rows = rows, w.keys = keys, w.blocks = blocks;
+    w.prefix_tiles = (int)((all + rows - 1) / rows), w.own_tiles = (int)((own_rows + rows - 1) / rows);
+    w.starts = (int64_t *)take(((size_t)d.n_seqs + 2) * 8);
+    w.cut_ml = (float2 *)take((size_t)blocks * 2 * rows * 8);
+    w.cut_o = (float *)take((size_t)blocks * 2 * rows * D * 4);
+  };
+  const int own_tile = own_rows <= 16 ? 16 : own_rows <= 32 ? 32 : 64;
+  line(p.own, own_tile, KEYS, stream_blocks(D), p.way == TOGETHER && d.prefix_len, true);
+  if (p.way == APART) line(p.prefix, 64, KEYS, stream_blocks(D), true, false);
+  if (p.way == TENSOR) {
+    line(p.prefix, 256, TC_KEYS, SMS, true, false);
+    const int64_t units = (int64_t)tiles_of((int)d.prefix_len, TC_KEYS) * d.cache.kv_heads * p.prefix.prefix_tiles;
+    p.prefix.per = (units + SMS - 1) / SMS;
+  }
+  if (p.way == TOGETHER) p.prefix = p.own;
   if (d.prefix_len) {
+    const size_t rows = (size_t)d.n_seqs * d.n_new * d.q_heads;
     for (int k = 0; k < 2; k++) {
-      w.whole_ml[k] = (float2 *)take(total_rows * 8);
-      w.whole_o[k] = (float *)take(total_rows * D * 4);
+      p.prefix.whole_ml[k] = p.own.whole_ml[k] = (float2 *)take(rows * 8);
+      p.prefix.whole_o[k] = p.own.whole_o[k] = (float *)take(rows * D * 4);
     }
   }
   p.bytes = n;
   return p;
+}
+
+// The shape's part of the rule for the tensor cores' kernel; tile_maps has the pointers' and strides' part.
+bool tensor_shape(const gts_attention_desc &d) { return d.cache.head_dim <= 128 && box_of((int)d.cache.page_size) >= 8; }
+
+typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiled encode_tiled() {
+  static std::atomic<void *> found{nullptr};
+  void *f = found.load(std::memory_order_relaxed);
+  if (!f) {
+    cudaDriverEntryPointQueryResult got;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &got) != cudaSuccess ||
+        got != cudaDriverEntryPointSuccess)
+      return nullptr;
+    found.store(f, std::memory_order_relaxed);
+  }
+  return (EncodeTiled)f;
+}
+
+// A map of the cache's pages for the tensor cores' kernel.  False where strides or alignment do not fit one: each dimension's
+// stride has to be a multiple of 16 bytes and of the one before it.
+bool tile_map(CUtensorMap &map, int &heads_first, int box, const gts_cache &c, void *base, int64_t page, int64_t token, int64_t head) {
+  const int64_t D = c.head_dim;
+  heads_first = c.page_size > 1 && (c.kv_heads == 1 || head < token);
+  if (c.kv_heads == 1) head = heads_first ? D : token * c.page_size;
+  if (c.page_size == 1) token = D;
+  const int64_t lo = heads_first ? head : token, hi = heads_first ? token : head;
+  if (c.n_pages == 1) page = hi * (heads_first ? c.page_size : c.kv_heads);
+  if ((uintptr_t)base % 16 || lo % 8 || lo < D || hi < lo || hi % lo || page < hi || page % hi || page >= 1ll << 38) return false;
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)D, heads_first ? c.kv_heads : c.page_size, heads_first ? c.page_size : c.kv_heads, c.n_pages};
+  const cuuint64_t strides[3] = {(cuuint64_t)lo * 2, (cuuint64_t)hi * 2, (cuuint64_t)page * 2};
+  const cuuint32_t boxes[4] = {64, heads_first ? 1u : (cuuint32_t)box, heads_first ? (cuuint32_t)box : 1u, 1}, ones[4] = {1, 1, 1, 1};
+  return encode(&map, c.dtype == GTS_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, base, dims, strides,
+                boxes, ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+bool tile_maps(Pages &p, const gts_cache &c) {
+  p.box = box_of((int)c.page_size);
+  return c.n_pages && tile_map(p.k, p.k_heads_first, p.box, c, c.k, c.k_page_stride, c.k_token_stride, c.k_head_stride) &&
+         tile_map(p.v, p.v_heads_first, p.box, c, c.v, c.v_page_stride, c.v_token_stride, c.v_head_stride);
 }
 
 template <typename T, int D, int WM>
@@ -555,17 +997,36 @@ cudaError_t stream(const Args &a, const Line &w, cudaStream_t s) {
 }
 
 template <typename T, int D>
-cudaError_t run(const Args &a, const Plan &p, cudaStream_t s) {
-  cudaError_t e = p.wm == 1 ? stream<T, D, 1>(a, p.line, s) : p.wm == 2 ? stream<T, D, 2>(a, p.line, s) : stream<T, D, 4>(a, p.line, s);
+cudaError_t stream(const Args &a, const Line &w, cudaStream_t s) {
+  return w.rows == 16 ? stream<T, D, 1>(a, w, s) : w.rows == 32 ? stream<T, D, 2>(a, w, s) : stream<T, D, 4>(a, w, s);
+}
+
+template <typename T, int D>
+cudaError_t tensor(const Args &a, const Line &w, const Pages &maps, cudaStream_t s) {
+  static std::atomic<uint64_t> granted{0};
+  const cudaError_t e = grant(k_prefix<T, D>, Tc<D>::SMEM, granted);
+  if (e != cudaSuccess) return e;
+  k_prefix<T, D><<<w.blocks, TC_THREADS, Tc<D>::SMEM, s>>>(a, w, maps, a.scale < 0 ? 0x80008000u : 0u);
+  return cudaGetLastError();
+}
+
+template <typename T, int D>
+cudaError_t run(const Args &a, const Plan &p, const Pages &maps, cudaStream_t s) {
+  cudaError_t e = cudaSuccess;
+  if (p.way == APART) e = stream<T, D, 4>(a, p.prefix, s);
+  if constexpr (D <= 128) {
+    if (p.way == TENSOR) e = tensor<T, D>(a, p.prefix, maps, s);
+  }
+  if (e == cudaSuccess) e = stream<T, D>(a, p.own, s);
   if (e != cudaSuccess) return e;
   const int64_t rows = (int64_t)a.n_seqs * a.n_new * a.q_heads;
-  k_join<T, D><<<(unsigned)((rows + WARPS - 1) / WARPS), THREADS, 0, s>>>(a, p.line, p.line);
+  k_join<T, D><<<(unsigned)((rows + WARPS - 1) / WARPS), THREADS, 0, s>>>(a, p.prefix, p.own);
   return cudaGetLastError();
 }
 
 template <typename T>
-cudaError_t launch(const Args &a, const Plan &p, int head_dim, cudaStream_t s) {
-  return head_dim == 64 ? run<T, 64>(a, p, s) : head_dim == 128 ? run<T, 128>(a, p, s) : run<T, 256>(a, p, s);
+cudaError_t launch(const Args &a, const Plan &p, const Pages &maps, int head_dim, cudaStream_t s) {
+  return head_dim == 64 ? run<T, 64>(a, p, maps, s) : head_dim == 128 ? run<T, 128>(a, p, maps, s) : run<T, 256>(a, p, maps, s);
 }
 
 const char *refuse_shape(const gts_attention_desc &d) {
@@ -587,7 +1048,7 @@ const char *refuse_shape(const gts_attention_desc &d) {
 
 extern "C" size_t gts_attention_workspace_bytes(const gts_attention_desc *d) {
   if (!d || refuse_shape(*d)) return 0;
-  return make_plan(*d, nullptr).bytes;
+  return std::max(make_plan(*d, false, nullptr).bytes, make_plan(*d, tensor_shape(*d), nullptr).bytes);
 }
 
 extern "C" gts_status gts_prefix_attention(const gts_attention_desc *d, void *stream) {
@@ -618,10 +1079,13 @@ extern "C" gts_status gts_prefix_attention(const gts_attention_desc *d, void *st
   a.scale = d->scale;
   a.prefix_pages = d->prefix_pages, a.table = d->page_table, a.lens = d->lens;
   a.status = d->d_status;
-  const Plan p = make_plan(*d, (char *)d->workspace);
-  if (d->workspace_bytes < p.bytes)
-    return gts::fail(GTS_ERR_NOMEM, ("attention: workspace too small: need " + std::to_string(p.bytes) + " bytes").c_str());
-  const cudaError_t e = c.dtype == GTS_BF16 ? launch<__nv_bfloat16>(a, p, c.head_dim, (cudaStream_t)stream)
-                                            : launch<__half>(a, p, c.head_dim, (cudaStream_t)stream);
+  if (d->workspace_bytes < gts_attention_workspace_bytes(d))
+    return gts::fail(GTS_ERR_NOMEM, "attention: workspace smaller than gts_attention_workspace_bytes");
+  Pages maps = {};
+  Plan p = make_plan(*d, tensor_shape(*d), (char *)d->workspace);
+  // (a scale of 0 would turn the -infinity of masked scores into NaN there)
+  if (p.way == TENSOR && (d->scale == 0.f || !tile_maps(maps, c))) p = make_plan(*d, false, (char *)d->workspace);
+  const cudaError_t e = c.dtype == GTS_BF16 ? launch<__nv_bfloat16>(a, p, maps, c.head_dim, (cudaStream_t)stream)
+                                            : launch<__half>(a, p, maps, c.head_dim, (cudaStream_t)stream);
   return e == cudaSuccess ? GTS_OK : gts::cuda_fail(e, "attention: launch");
 }
