@@ -473,10 +473,11 @@ __device__ __forceinline__ uint64_t now_ns() {
 }
 constexpr uint64_t LIMIT_NS = 2000000000ull;
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *dead) {
-  if (bar_try(bar, parity)) return true;
+  for (int n = 0; n < 1024; n++)  // reading the timer takes longer than most waits
+    if (bar_try(bar, parity)) return true;
   const uint64_t from = now_ns();
   while (!*dead) {
-    for (int n = 0; n < 16; n++)
+    for (int n = 0; n < 64; n++)
       if (bar_try(bar, parity)) return true;
     if (now_ns() - from > LIMIT_NS) *dead = 1;
   }
@@ -491,14 +492,22 @@ __device__ __forceinline__ void tc_commit(uint32_t bar) {
 }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-// d [128 rows][N] (+)= a [128][16] b [16][N]; a from shared memory, or from tensor memory
-__device__ __forceinline__ void tc_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t shape, bool add) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-               ::"r"(d), "l"(a), "l"(b), "r"(shape), "r"((uint32_t)add) : "memory");
+// d [128 rows][N] (+)= a [128][16] b [16][N]; a from shared memory, or from tensor memory.  Operands in shared memory are
+// described by two words; the upper one is the same for all of them here.
+__device__ __forceinline__ void tc_mma(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t shape, bool add) {
+  asm volatile("{\n.reg .pred p;\n.reg .b64 x, y;\nmov.b64 x, {%1, %3};\nmov.b64 y, {%2, %3};\nsetp.ne.u32 p, %5, 0;\n"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %4, p;\n}"
+               ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(shape), "r"((uint32_t)add) : "memory");
 }
-__device__ __forceinline__ void tc_mma_t(uint32_t d, uint32_t a, uint64_t b, uint32_t shape, bool add) {
-  asm volatile("{\n.reg .pred p;\nsetp.ne.u32 p, %4, 0;\ntcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}"
-               ::"r"(d), "r"(a), "l"(b), "r"(shape), "r"((uint32_t)add) : "memory");
+__device__ __forceinline__ void tc_mma_t(uint32_t d, uint32_t a, uint32_t b, uint32_t hi, uint32_t shape, bool add) {
+  asm volatile("{\n.reg .pred p;\n.reg .b64 y;\nmov.b64 y, {%2, %3};\nsetp.ne.u32 p, %5, 0;\n"
+               "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %4, p;\n}"
+               ::"r"(d), "r"(a), "r"(b), "r"(hi), "r"(shape), "r"((uint32_t)add) : "memory");
+}
+__device__ __forceinline__ bool elected() {  // one lane of a converged warp
+  uint32_t is;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(is));
+  return is;
 }
 #define R8(r, i) "=r"(r[i]), "=r"(r[i + 1]), "=r"(r[i + 2]), "=r"(r[i + 3]), "=r"(r[i + 4]), "=r"(r[i + 5]), "=r"(r[i + 6]), "=r"(r[i + 7])
 #define W8(r, i) "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]), "r"(r[i + 4]), "r"(r[i + 5]), "r"(r[i + 6]), "r"(r[i + 7])
@@ -518,11 +527,11 @@ __device__ __forceinline__ void tc_st(uint32_t at, const uint32_t *r) {
 __device__ __forceinline__ void tc_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// Operand in shared memory as rows of 128 bytes, eight rows to a swizzled group of 1024 bytes, groups one after the other;
-// `blocks`: bytes from one 128-byte column of groups to the next, for operands that are wider and not summed over.
-__device__ __forceinline__ uint64_t operand(uint32_t at, uint32_t blocks) {
-  return (uint64_t)((at & 0x3FFFF) >> 4) | (uint64_t)(blocks >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 | 2ull << 61;
-}
+// Operands in shared memory are rows of 128 bytes, eight rows to a swizzled group of 1024 bytes, groups one after the other.
+// Lower word: address, and the bytes from one 128-byte column of groups to the next (for operands that are wider and not
+// summed over); upper word: bytes from group to group, version, swizzle.
+__device__ __forceinline__ uint32_t operand(uint32_t at, uint32_t blocks) { return at >> 4 | (blocks >> 4) << 16; }
+constexpr uint32_t OPERAND_HI = 1024 >> 4 | 1u << 14 | 2u << 29;
 
 // The rows of all sequences against the prefix.  A block holds 2 x 128 rows of one key head and passes along its stretch of
 // the keys in tiles of 128, each read once for all rows:
@@ -558,7 +567,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   uint64_t *const bars = (uint64_t *)(ring + STAGES * TILE);
   uint32_t *const tmem_at = (uint32_t *)(bars + 2 * STAGES + 7);
   volatile int *const dead = (volatile int *)(tmem_at + 1);
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), q_at = smem_u32(qs), ring_at = smem_u32(ring);
   auto full = [&](int s) { return bar0 + s * 8; };
   auto empty = [&](int s) { return bar0 + (STAGES + s) * 8; };
@@ -580,7 +589,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   tc_before();
   __syncthreads();
   tc_after();
-  const uint32_t tmem = *tmem_at;
+  const uint32_t tmem = __shfl_sync(~0u, *tmem_at, 0);
   auto scores = [&](int h) { return tmem + h * 128; };
   auto sums = [&](int h) { return tmem + 256 + h * 128; };
 
@@ -631,73 +640,83 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
         for (int x = first; x < it; x++)
           while (!bar_try(full(x % STAGES), (x / STAGES) & 1) && now_ns() - from < LIMIT_NS) {}
       }
-    } else if (warp == 8) {
-      // ---- products; every lane follows, lane 0 issues
+    } else if (warp == 8 && elected()) {
+      // ---- products, from one thread
       constexpr uint32_t TYPE = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
       constexpr uint32_t COMMON = 1u << 4 | TYPE << 7 | TYPE << 10 | (128u >> 4) << 24;
       constexpr uint32_t QK = COMMON | (TC_KEYS >> 3) << 17, PV = COMMON | 1u << 16 | (D >> 3) << 17;
-      int it = 0;                                          // ring position
-      uint32_t seg[2] = {0, 0}, turn[2] = {0, 0};          // each half's pairs and tiles so far: the phases of its barriers
+      const uint32_t q_op = operand(q_at, 16), k_op = operand(ring_at, 16), v_op = operand(ring_at, HALF);
+      int stage = 0;                                       // of the ring
+      uint32_t lap = 0, seg[2] = {0, 0}, turn[2] = {0, 0}; // laps of the ring; each half's pairs and tiles so far
       bool alive = true;
-      auto need = [&](uint32_t bar, uint32_t parity) { alive = __all_sync(~0u, alive && bar_wait(bar, parity, dead)); };
+      auto need = [&](uint32_t bar, uint32_t parity) { alive = alive && bar_wait(bar, parity & 1, dead); };
+      auto next = [&] {
+        if (++stage == STAGES) stage = 0, lap++;
+      };
       auto qk = [&](int h, int s) {
-        if (lane == 0) {
 #pragma unroll
-          for (int k = 0; k < D / 16; k++)
-            tc_mma(scores(h), operand(q_at + h * (Tc<D>::Q / 2) + k / 4 * HALF + k % 4 * 32, 16),
-                   operand(ring_at + s * TILE + k / 4 * HALF + k % 4 * 32, 16), QK, k > 0);
-          tc_commit(s_full(h));
-        }
+        for (int k = 0; k < D / 16; k++)
+          tc_mma(scores(h), q_op + ((h * (Tc<D>::Q / 2) + k / 4 * HALF + k % 4 * 32) >> 4),
+                 k_op + ((s * TILE + k / 4 * HALF + k % 4 * 32) >> 4), OPERAND_HI, QK, k > 0);
+        tc_commit(s_full(h));
       };
       for (int64_t u = u0; u < u1 && alive;) {
         const int pair = (int)(u / n), tile0 = (int)(u - (int64_t)pair * n), count = (int)min((int64_t)(n - tile0), u1 - u);
         const int halves = all - pair % w.prefix_tiles * 256 > 128 ? 2 : 1;
-        for (int h = 0; h < halves && alive; h++) need(q_full(h), seg[h]++ & 1);
-        if (alive) need(full(it % STAGES), (it / STAGES) & 1);
+        for (int h = 0; h < halves; h++) need(q_full(h), seg[h]++);
+        need(full(stage), lap);
         if (!alive) break;
         tc_after();
-        for (int h = 0; h < halves; h++) qk(h, it % STAGES);
-        if (lane == 0) tc_commit(empty(it % STAGES));
-        it++;
-        for (int j = 0; j < count && alive; j++) {
-          const int sv = it % STAGES, nv = min(TC_KEYS, a.prefix_len - (tile0 + j) * TC_KEYS);
-          need(full(sv), (it / STAGES) & 1);
-          it++;
-          const int sk = it % STAGES, sk_phase = (it / STAGES) & 1;
-          if (j + 1 < count) it++;
-          if (nv % 16) {                                   // value rows past the end, in the last 16 that count: zeros
-            for (int x = lane; x < (16 - nv % 16) * (D / 8); x += 32) {
+        for (int h = 0; h < halves; h++) qk(h, stage);
+        tc_commit(empty(stage));
+        next();
+        for (int j = 0; j < count; j++) {
+          // this tile's values and the next one's keys, while the rows make their weights
+          const int sv = stage, nv = a.prefix_len - (tile0 + j) * TC_KEYS;
+          need(full(sv), lap);
+          next();
+          const int sk = stage;
+          if (j + 1 < count) {
+            need(full(sk), lap);
+            next();
+          }
+          if (nv < TC_KEYS && nv % 16 && alive) {          // value rows past the end, in the last 16 that count: zeros
+            for (int x = 0; x < (16 - nv % 16) * (D / 8); x++) {
               const int r = nv + x / (D / 8), c = x % (D / 8);
               *(uint4 *)(ring + sv * TILE + c / 8 * HALF + r * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
           }
-          for (int h = 0; h < halves && alive; h++) {
-            need(p_full(h), turn[h]++ & 1);
-            if (!alive) break;
-            tc_after();
-            if (lane == 0) {
-              for (int k = 0; k * 16 < nv; k++)
-                tc_mma_t(sums(h), scores(h) + k * 8, operand(ring_at + sv * TILE + k * 2048, HALF), PV, j > 0 || k > 0);
-              if (h == halves - 1) tc_commit(empty(sv));
-            }
-            if (j + 1 < count) {
-              if (h == 0) {
-                need(full(sk), sk_phase);
-                if (!alive) break;
+#pragma unroll
+          for (int h = 0; h < 2; h++) {
+            if (h < halves) {
+              need(p_full(h), turn[h]++);
+              if (!alive) break;
+              tc_after();
+              if (nv >= TC_KEYS) {
+#pragma unroll
+                for (int k = 0; k < TC_KEYS / 16; k++)
+                  tc_mma_t(sums(h), scores(h) + k * 8, v_op + ((sv * TILE + k * 2048) >> 4), OPERAND_HI, PV, j > 0 || k > 0);
+              } else {
+#pragma unroll 1
+                for (int k = 0; k * 16 < nv; k++)
+                  tc_mma_t(sums(h), scores(h) + k * 8, v_op + ((sv * TILE + k * 2048) >> 4), OPERAND_HI, PV, j > 0 || k > 0);
               }
-              qk(h, sk);
-              if (h == halves - 1 && lane == 0) tc_commit(empty(sk));
-            } else if (lane == 0) {
-              tc_commit(s_full(h));                        // the pair's sums are complete
+              if (h == halves - 1) tc_commit(empty(sv));
+              if (j + 1 < count) {
+                qk(h, sk);
+                if (h == halves - 1) tc_commit(empty(sk));
+              } else {
+                tc_commit(s_full(h));                      // the pair's sums are complete
+              }
             }
           }
+          if (!alive) break;
         }
         u += count;
       }
-      if (!alive) {                                        // as do products in flight
-        if (lane == 0) tc_commit(ended);
+      if (!alive) {                                        // products in flight end before the block does
+        tc_commit(ended);
         const uint64_t from = now_ns();
         while (!bar_try(ended, 0) && now_ns() - from < LIMIT_NS) {}
       }
