@@ -124,29 +124,33 @@ __device__ __forceinline__ Row row_of(const Args &a, int b, int kh, int r) {
   return x;
 }
 
+// A place in the line of units: a tile of keys of a pair of a sequence (b = -1: the prefix).
+struct Place { int b, len, n, pairs, pair, tile; };
+
 // One block of 4 warps: WM of them along the rows (16 each), 4 / WM along a tile's keys.  Keys and values stream through
-// a ring of tiles in shared memory by 16-byte asynchronous copies, gathered row by row from their pages.  Scores and
-// weights stay in the fragments of m16n8k16 products; each warp keeps its own running maximum and sum, and the warps
-// along the keys are joined at the end of a pair.  Weights are rounded to the type of the values for their product with
-// them (the sum is of the unrounded ones); everything else is in 32 bits.
-template <int D> struct Ring {
-  static constexpr int STAGES = D == 64 ? 4 : 3;
+// a ring of tiles in shared memory by 16-byte asynchronous copies, gathered row by row from their pages; the copies run
+// STAGES - 1 tiles ahead across the ends of pairs, so that a short sequence does not stop them, and a pair's queries come
+// with its first tile.  Scores and weights stay in the fragments of m16n8k16 products; each warp keeps its own running
+// maximum and sum, and the warps along the keys are joined at the end of a pair, in the stage just read.  Weights are
+// rounded to the type of the values for their product with them (the sum is of the unrounded ones); everything else is in
+// 32 bits.
+template <int D, int WM> struct Ring {
+  static constexpr int STAGES = (D == 64 ? 4 : 3) - (WM > 1);   // 3, 2 or 1 blocks to an SM for D of 64, 128, 256
   static constexpr int TILE = KEYS * D * 2;            // bytes of a tile of keys or of values
+  static constexpr int QUERIES = 16 * WM * D * 2;
+  static constexpr int SMEM = STAGES * (2 * TILE + QUERIES) + 2 * KEYS * 2 * 8 + 64 * 8 + 64;
 };
-template <int D, int WM> constexpr int stream_smem() {
-  return Ring<D>::STAGES * 2 * Ring<D>::TILE + 16 * WM * D * 2 + 2 * KEYS * 2 * 8 + 64 * 8 + 64;
-}
 
 template <typename T, int D, int WM>
 __global__ void __launch_bounds__(THREADS) k_stream(const Args a, const Line w) {
-  constexpr int WK = WARPS / WM, ROWS = 16 * WM, KW = KEYS / WK, STAGES = Ring<D>::STAGES, TILE = Ring<D>::TILE;
-  constexpr int CH = D / 8, PITCH = D * 2, OPITCH = D + 8;
-  static_assert(64 * OPITCH * 4 <= STAGES * 2 * TILE, "the joined result fits the ring");
+  using R = Ring<D, WM>;
+  constexpr int WK = WARPS / WM, ROWS = 16 * WM, KW = KEYS / WK, STAGES = R::STAGES, TILE = R::TILE;
+  constexpr int CH = D / 8, PITCH = D * 2;
   extern __shared__ __align__(128) unsigned char smem[];
   unsigned char *ring = smem, *qs = smem + STAGES * 2 * TILE;
-  int64_t *offs = (int64_t *)(qs + ROWS * PITCH);      // [2][KEYS][2]: where the rows of the next tile to load start
-  float2 *stat = (float2 *)(offs + 2 * KEYS * 2);      // [64]: maximum and sum of each warp's rows
-  int64_t *found = (int64_t *)(stat + 64);             // [4]
+  int64_t *offs = (int64_t *)(qs + STAGES * R::QUERIES);  // [2][KEYS][2]: where the rows of the next tile to load start
+  float2 *stat = (float2 *)(offs + 2 * KEYS * 2);         // [64]: maximum and sum of each warp's rows
+  int64_t *found = (int64_t *)(stat + 64);                // [4]
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const int wm = warp % WM, wk = warp / WM, quad = lane / 4, t4 = lane % 4;
   const uint32_t ring_at = smem_u32(ring), q_at = smem_u32(qs);
@@ -177,8 +181,7 @@ __global__ void __launch_bounds__(THREADS) k_stream(const Args a, const Line w) 
   }
   base += upto - mine;                                 // first unit of sequence b_first
   const int64_t per = (total + w.blocks - 1) / w.blocks;
-  int64_t u = per * blockIdx.x;
-  const int64_t u_end = min(total, u + per);
+  const int64_t u0 = per * blockIdx.x, u1 = min(total, u0 + per);
   __syncthreads();
   if (blockIdx.x == 0) {
     int64_t at = base;
@@ -188,264 +191,286 @@ __global__ void __launch_bounds__(THREADS) k_stream(const Args a, const Line w) 
     }
     if (tid == 0) w.starts[a.n_seqs] = total, w.starts[a.n_seqs + 1] = per;
   }
-  if (u >= u_end) return;
-  if (u >= prefix_units && u >= base && u < base + mine) {
+  if (u0 >= u1) return;
+  if (u0 >= prefix_units && u0 >= base && u0 < base + mine) {
     int64_t at = base;
     int b = b_first;
     for (;; b++) {
       const int64_t n = (int64_t)tiles_of(own_len(a, b)) * own_pairs;
-      if (u < at + n) break;
+      if (u0 < at + n) break;
       at += n;
     }
-    found[0] = b, found[1] = at;
+    found[0] = b, found[1] = u0 - at;
   }
   __syncthreads();
-  int b = u >= prefix_units ? (int)found[0] : -1;
-  int64_t b_start = u >= prefix_units ? found[1] : 0;
-  int len = b < 0 ? a.prefix_len : own_len(a, b);
-  __syncthreads();
+  Place now;                                           // the tile whose turn it is
+  {
+    const bool in_prefix = u0 < prefix_units;
+    const int64_t in = in_prefix ? u0 : found[1];
+    now.b = in_prefix ? -1 : (int)found[0];
+    now.len = in_prefix ? a.prefix_len : own_len(a, now.b);
+    now.n = tiles_of(now.len);
+    now.pairs = in_prefix ? a.kv_heads * w.prefix_tiles : own_pairs;
+    now.pair = (int)(in / now.n);
+    now.tile = (int)(in - (int64_t)now.pair * now.n);
+  }
+  const int count = (int)(u1 - u0);
+  auto advance = [&](Place &p) {                       // only ever to units of this block
+    if (++p.tile < p.n) return;
+    p.tile = 0;
+    if (++p.pair < p.pairs) return;
+    p.pair = 0, p.pairs = own_pairs;
+    do {
+      p.len = own_len(a, ++p.b);
+      p.n = tiles_of(p.len);
+    } while (p.n == 0);
+  };
+  auto row_tiles = [&](const Place &p) { return p.b < 0 ? w.prefix_tiles : w.own_tiles; };
 
-  while (u < u_end) {
-    int64_t n = tiles_of(len), units = n * (b < 0 ? (int64_t)a.kv_heads * w.prefix_tiles : own_pairs);
-    while (u >= b_start + units) {                     // the next sequence that has keys of its own
-      b_start += units;
-      len = own_len(a, ++b);
-      n = tiles_of(len);
-      units = n * own_pairs;
+  // page numbers are fetched two tiles ahead of the copies, places one tile ahead
+  Place ahead = now, placed = now, fetched = now;
+  int page_next = 0, n_fetched = 0, n_placed = 0, n_loaded = 0, load_stage = 0, load_seg = -1;
+  auto fetch = [&] {
+    if (n_fetched < count) {
+      if (n_fetched) advance(ahead);
+      fetched = ahead;
+      const int j = ahead.tile * KEYS + tid;
+      const int32_t *pages = ahead.b < 0 ? a.prefix_pages : a.table + (int64_t)ahead.b * a.max_pages;
+      if (tid < KEYS && j < ahead.len) page_next = pages[j / a.page_size];
     }
-    const int pair = (int)((u - b_start) / n), tiles = b < 0 ? w.prefix_tiles : w.own_tiles;
-    const int tile0 = (int)((u - b_start) - pair * n), tile1 = (int)min((int64_t)n, tile0 + (u_end - u));
-    const int kh = pair / tiles, row0 = (pair - kh * tiles) * ROWS;
-    const int rows = min(ROWS, (b < 0 ? a.n_seqs : 1) * a.n_new * a.group - row0);
-    const bool whole = tile0 == 0 && tile1 == n;
-    const int32_t *pages = b < 0 ? a.prefix_pages : a.table + (int64_t)b * a.max_pages;
-
-    // queries: rows beyond the last are zeros
-    for (int x = tid; x < ROWS * CH; x += THREADS) {
-      const int r = x / CH, c = x % CH;
-      const uint32_t at = r * PITCH + ((c ^ (r & 7)) * 16);
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (r < rows) {
-        const Row p = row_of(a, b, kh, row0 + r);
-        const T *src = (const T *)a.q + p.b * a.q_seq + p.i * a.q_tok + p.h * a.q_head + c * 8;
-        if (q_aligned) {
-          v = *(const uint4 *)src;
-        } else {
-          T e[8];
-#pragma unroll
-          for (int j = 0; j < 8; j++) e[j] = src[j];
-          memcpy(&v, e, 16);
-        }
-      }
-      *(uint4 *)(qs + at) = v;
-    }
-    // own keys that the rows of this thread's fragments see
-    int limit[2];
-#pragma unroll
-    for (int x = 0; x < 2; x++) {
-      const int r = row0 + wm * 16 + quad + 8 * x;
-      limit[x] = b < 0 ? len : len - (a.n_new - 1 - min(r / a.group, a.n_new - 1));
-    }
-    const int seen_by_all = b < 0 ? len : len - (a.n_new - 1);
-
-    // page numbers are fetched two tiles ahead, places one tile ahead of the copies
-    int page_next = 0;
-    auto fetch = [&](int tile) {
-      const int j = tile * KEYS + tid;
-      if (tid < KEYS && tile < tile1 && j < len) page_next = pages[j / a.page_size];
-    };
-    auto place = [&](int tile) {
-      if (tid >= KEYS || tile >= tile1) return;
-      const int j = tile * KEYS + tid;
-      int64_t k_off = -1, v_off = 0;
-      if (j < len) {
-        if (page_next < 0 || page_next >= a.n_pages) {
-          if (a.status) *a.status = GTS_ERR_INVALID_PARAMS;
-        } else {
-          const int in = j % a.page_size;
-          k_off = page_next * a.k_page + in * a.k_tok + kh * a.k_head;
-          v_off = page_next * a.v_page + in * a.v_tok + kh * a.v_head;
-        }
-      }
-      int64_t *to = offs + ((tile & 1) * KEYS + tid) * 2;
-      to[0] = k_off, to[1] = v_off;
-    };
-    auto load = [&](int tile) {
-      if (tile < tile1) {
-        const uint32_t at = ring_at + (tile % STAGES) * 2 * TILE;
-        for (int x = tid; x < KEYS * CH; x += THREADS) {
-          const int r = x / CH, c = x % CH;
-          const int64_t *from = offs + ((tile & 1) * KEYS + r) * 2;
-          const bool live = from[0] >= 0;
-          const T *k = (const T *)a.k + (live ? from[0] + c * 8 : 0), *v = (const T *)a.v + (live ? from[1] + c * 8 : 0);
-          const uint32_t to = at + r * PITCH + ((c ^ (r & 7)) * 16);
-          if (aligned) {
-            copy16(to, k, live);
-            copy16(to + TILE, v, live);
+    n_fetched++;
+  };
+  auto place = [&] {
+    if (n_placed < count) {
+      placed = fetched;
+      if (tid < KEYS) {
+        const int j = placed.tile * KEYS + tid, kh = placed.pair / row_tiles(placed);
+        int64_t k_off = -1, v_off = 0;
+        if (j < placed.len) {
+          if (page_next < 0 || page_next >= a.n_pages) {
+            if (a.status) *a.status = GTS_ERR_INVALID_PARAMS;
           } else {
-            T e[8], f[8];
+            const int in = j % a.page_size;
+            k_off = page_next * a.k_page + in * a.k_tok + kh * a.k_head;
+            v_off = page_next * a.v_page + in * a.v_tok + kh * a.v_head;
+          }
+        }
+        int64_t *to = offs + ((n_placed & 1) * KEYS + tid) * 2;
+        to[0] = k_off, to[1] = v_off;
+      }
+    }
+    n_placed++;
+  };
+  auto load = [&] {
+    if (n_loaded < count) {
+      const uint32_t at = ring_at + load_stage * 2 * TILE;
+      for (int x = tid; x < KEYS * CH; x += THREADS) {
+        const int r = x / CH, c = x % CH;
+        const int64_t *from = offs + ((n_loaded & 1) * KEYS + r) * 2;
+        const bool live = from[0] >= 0;
+        const T *k = (const T *)a.k + (live ? from[0] + c * 8 : 0), *v = (const T *)a.v + (live ? from[1] + c * 8 : 0);
+        const uint32_t to = at + r * PITCH + ((c ^ (r & 7)) * 16);
+        if (aligned) {
+          copy16(to, k, live);
+          copy16(to + TILE, v, live);
+        } else {
+          T e[8], f[8];
 #pragma unroll
-            for (int j = 0; j < 8; j++) e[j] = live ? k[j] : narrow<T>(0.f), f[j] = live ? v[j] : narrow<T>(0.f);
-            memcpy(ring + (to - ring_at), e, 16);
-            memcpy(ring + (to - ring_at) + TILE, f, 16);
+          for (int j = 0; j < 8; j++) e[j] = live ? k[j] : narrow<T>(0.f), f[j] = live ? v[j] : narrow<T>(0.f);
+          memcpy(ring + (to - ring_at), e, 16);
+          memcpy(ring + (to - ring_at) + TILE, f, 16);
+        }
+      }
+      if (n_loaded == 0 || placed.tile == 0) {         // a pair begins: its queries, zeros beyond the last row
+        load_seg = load_seg + 1 == STAGES ? 0 : load_seg + 1;
+        const int tiles = row_tiles(placed), kh = placed.pair / tiles, row0 = (placed.pair - kh * tiles) * ROWS;
+        const int rows = (placed.b < 0 ? a.n_seqs : 1) * a.n_new * a.group - row0;
+        for (int x = tid; x < ROWS * CH; x += THREADS) {
+          const int r = x / CH, c = x % CH;
+          const uint32_t to = load_seg * R::QUERIES + r * PITCH + ((c ^ (r & 7)) * 16);
+          const Row p = row_of(a, placed.b, kh, row0 + min(r, rows - 1));
+          const T *src = (const T *)a.q + p.b * a.q_seq + p.i * a.q_tok + p.h * a.q_head + c * 8;
+          if (q_aligned) {
+            copy16(q_at + to, src, r < rows);
+          } else {
+            T e[8];
+#pragma unroll
+            for (int j = 0; j < 8; j++) e[j] = r < rows ? src[j] : narrow<T>(0.f);
+            memcpy(qs + to, e, 16);
           }
         }
       }
-      copies_commit();
-    };
-    fetch(tile0);
-    place(tile0);
-    fetch(tile0 + 1);
-    __syncthreads();
-#pragma unroll
-    for (int x = 0; x < STAGES - 1; x++) {
-      load(tile0 + x);
-      place(tile0 + x + 1);
-      fetch(tile0 + x + 2);
-      __syncthreads();
+      if (++load_stage == STAGES) load_stage = 0;
     }
+    n_loaded++;
+    copies_commit();
+  };
+  fetch();
+  place();
+  fetch();
+  __syncthreads();
+#pragma unroll 1
+  for (int x = 0; x < STAGES - 1; x++) {
+    load();
+    place();
+    fetch();
+    __syncthreads();
+  }
 
-    float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+  int stage = 0, seg = -1, tile0 = 0, kh = 0, row0 = 0, rows = 0, limit[2] = {0, 0}, seen_by_all = 0;
+  bool first_pair = true;
+  float o[D / 8][4], m[2], l[2];
+  for (int unit = 0; unit < count; unit++) {
+    copies_wait<STAGES - 2>();
+    __syncthreads();
+    load();
+    place();
+    fetch();
+    if (unit == 0 || now.tile == 0) {                  // a pair begins
+      const int tiles = row_tiles(now);
+      seg = seg + 1 == STAGES ? 0 : seg + 1;
+      tile0 = now.tile;
+      kh = now.pair / tiles, row0 = (now.pair - kh * tiles) * ROWS;
+      rows = min(ROWS, (now.b < 0 ? a.n_seqs : 1) * a.n_new * a.group - row0);
+      seen_by_all = now.b < 0 ? now.len : now.len - (a.n_new - 1);
 #pragma unroll
-    for (int x = 0; x < D / 8; x++) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
-
-    for (int tile = tile0; tile < tile1; tile++) {
-      copies_wait<STAGES - 2>();
-      __syncthreads();
-      load(tile + STAGES - 1);
-      place(tile + STAGES);
-      fetch(tile + STAGES + 1);
-      const uint32_t k_at = ring_at + (tile % STAGES) * 2 * TILE, v_at = k_at + TILE;
-      const int mi = lane / 8, mr = lane % 8;
-      float s[KW / 8][4];
-#pragma unroll
-      for (int x = 0; x < KW / 8; x++) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
-#pragma unroll
-      for (int d = 0; d < D / 16; d++) {
-        uint32_t qf[4];
-        const int r = wm * 16 + (mi & 1) * 8 + mr;
-        ldsm(qf, q_at + r * PITCH + (((d * 2 + (mi >> 1)) ^ (r & 7)) * 16));
-#pragma unroll
-        for (int x = 0; x < KW / 16; x++) {
-          uint32_t kf[4];
-          const int key = wk * KW + x * 16 + (mi >> 1) * 8 + mr;
-          ldsm(kf, k_at + key * PITCH + (((d * 2 + (mi & 1)) ^ (key & 7)) * 16));
-          mma<T>(s[2 * x], qf, kf[0], kf[1]);
-          mma<T>(s[2 * x + 1], qf, kf[2], kf[3]);
-        }
+      for (int x = 0; x < 2; x++) {                    // keys that the rows of this thread's fragments see
+        const int r = row0 + wm * 16 + quad + 8 * x;
+        limit[x] = now.b < 0 ? now.len : now.len - (a.n_new - 1 - min(r / a.group, a.n_new - 1));
+        m[x] = -INFINITY, l[x] = 0.f;
       }
-      const int key0 = tile * KEYS + wk * KW;
-      const bool masked = key0 + KW > seen_by_all;
-      float top[2] = {m[0], m[1]};
 #pragma unroll
-      for (int x = 0; x < KW / 8; x++) {
+      for (int x = 0; x < D / 8; x++) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
+    }
+    const uint32_t k_at = ring_at + stage * 2 * TILE, v_at = k_at + TILE, qf_at = q_at + seg * R::QUERIES;
+    const int mi = lane / 8, mr = lane % 8;
+    float s[KW / 8][4];
 #pragma unroll
-        for (int c = 0; c < 4; c++) {
-          s[x][c] *= sl2;
-          if (masked && key0 + x * 8 + t4 * 2 + (c & 1) >= limit[c >> 1]) s[x][c] = -INFINITY;
-          top[c >> 1] = fmaxf(top[c >> 1], s[x][c]);
-        }
-      }
-      float keep[2], from[2];
+    for (int x = 0; x < KW / 8; x++) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
 #pragma unroll
-      for (int x = 0; x < 2; x++) {
-        top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 1));
-        top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 2));
-        from[x] = top[x] == -INFINITY ? 0.f : top[x];  // nothing seen so far
-        keep[x] = exp2_fast(m[x] - from[x]);
-        m[x] = top[x];
-        l[x] *= keep[x];
-      }
-      if (__any_sync(~0u, keep[0] != 1.f || keep[1] != 1.f)) {
-#pragma unroll
-        for (int x = 0; x < D / 8; x++) {
-          o[x][0] *= keep[0], o[x][1] *= keep[0];
-          o[x][2] *= keep[1], o[x][3] *= keep[1];
-        }
-      }
-      uint32_t pf[KW / 16][4];
-#pragma unroll
-      for (int x = 0; x < KW / 8; x++) {
-#pragma unroll
-        for (int c = 0; c < 4; c++) {
-          s[x][c] = exp2_fast(s[x][c] - from[c >> 1]);
-          l[c >> 1] += s[x][c];
-        }
-        pf[x / 2][(x & 1) * 2] = pack<T>(s[x][0], s[x][1]);
-        pf[x / 2][(x & 1) * 2 + 1] = pack<T>(s[x][2], s[x][3]);
-      }
+    for (int d = 0; d < D / 16; d++) {
+      uint32_t qf[4];
+      const int r = wm * 16 + (mi & 1) * 8 + mr;
+      ldsm(qf, qf_at + r * PITCH + (((d * 2 + (mi >> 1)) ^ (r & 7)) * 16));
 #pragma unroll
       for (int x = 0; x < KW / 16; x++) {
-        const int key = wk * KW + x * 16 + (mi & 1) * 8 + mr;
+        uint32_t kf[4];
+        const int key = wk * KW + x * 16 + (mi >> 1) * 8 + mr;
+        ldsm(kf, k_at + key * PITCH + (((d * 2 + (mi & 1)) ^ (key & 7)) * 16));
+        mma<T>(s[2 * x], qf, kf[0], kf[1]);
+        mma<T>(s[2 * x + 1], qf, kf[2], kf[3]);
+      }
+    }
+    const int key0 = now.tile * KEYS + wk * KW;
+    const bool masked = key0 + KW > seen_by_all;
+    float top[2] = {m[0], m[1]};
 #pragma unroll
-        for (int d = 0; d < D / 16; d++) {
-          uint32_t vf[4];
-          ldsm_t(vf, v_at + key * PITCH + (((d * 2 + (mi >> 1)) ^ (key & 7)) * 16));
-          mma<T>(o[2 * d], pf[x], vf[0], vf[1]);
-          mma<T>(o[2 * d + 1], pf[x], vf[2], vf[3]);
-        }
+    for (int x = 0; x < KW / 8; x++) {
+#pragma unroll
+      for (int c = 0; c < 4; c++) {
+        s[x][c] *= sl2;
+        if (masked && key0 + x * 8 + t4 * 2 + (c & 1) >= limit[c >> 1]) s[x][c] = -INFINITY;
+        top[c >> 1] = fmaxf(top[c >> 1], s[x][c]);
+      }
+    }
+    float keep[2], from[2];
+#pragma unroll
+    for (int x = 0; x < 2; x++) {
+      top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 1));
+      top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 2));
+      from[x] = top[x] == -INFINITY ? 0.f : top[x];    // nothing seen so far
+      keep[x] = exp2_fast(m[x] - from[x]);
+      m[x] = top[x];
+      l[x] *= keep[x];
+    }
+    if (__any_sync(~0u, keep[0] != 1.f || keep[1] != 1.f)) {
+#pragma unroll
+      for (int x = 0; x < D / 8; x++) {
+        o[x][0] *= keep[0], o[x][1] *= keep[0];
+        o[x][2] *= keep[1], o[x][3] *= keep[1];
+      }
+    }
+    uint32_t pf[KW / 16][4];
+#pragma unroll
+    for (int x = 0; x < KW / 8; x++) {
+#pragma unroll
+      for (int c = 0; c < 4; c++) {
+        s[x][c] = exp2_fast(s[x][c] - from[c >> 1]);
+        l[c >> 1] += s[x][c];
+      }
+      pf[x / 2][(x & 1) * 2] = pack<T>(s[x][0], s[x][1]);
+      pf[x / 2][(x & 1) * 2 + 1] = pack<T>(s[x][2], s[x][3]);
+    }
+#pragma unroll
+    for (int x = 0; x < KW / 16; x++) {
+      const int key = wk * KW + x * 16 + (mi & 1) * 8 + mr;
+#pragma unroll
+      for (int d = 0; d < D / 16; d++) {
+        uint32_t vf[4];
+        ldsm_t(vf, v_at + key * PITCH + (((d * 2 + (mi >> 1)) ^ (key & 7)) * 16));
+        mma<T>(o[2 * d], pf[x], vf[0], vf[1]);
+        mma<T>(o[2 * d + 1], pf[x], vf[2], vf[3]);
       }
     }
 
-    // join the warps along the keys, in shared memory, and write the pair's rows
-    copies_wait<0>();
-    __syncthreads();
-    float *acc = (float *)ring;                        // [4 warps][16][OPITCH]
+    if (now.tile == now.n - 1 || unit == count - 1) {
+      // a pair ends here: the warps along the keys are joined in the stage just read, and its rows written
+      __syncthreads();
+      float *acc = (float *)(ring + stage * 2 * TILE); // [4 warps][16][D], columns of row r turned by 8 (r mod 4)
 #pragma unroll
-    for (int x = 0; x < 2; x++) {
-      l[x] += __shfl_xor_sync(~0u, l[x], 1);
-      l[x] += __shfl_xor_sync(~0u, l[x], 2);
-      const int r = warp * 16 + quad + 8 * x;
-      if (t4 == 0) stat[r] = make_float2(m[x], l[x]);
+      for (int x = 0; x < 2; x++) {
+        l[x] += __shfl_xor_sync(~0u, l[x], 1);
+        l[x] += __shfl_xor_sync(~0u, l[x], 2);
+        const int r = warp * 16 + quad + 8 * x;
+        if (t4 == 0) stat[r] = make_float2(m[x], l[x]);
 #pragma unroll
-      for (int d = 0; d < D / 8; d++) *(float2 *)(acc + r * OPITCH + d * 8 + t4 * 2) = make_float2(o[d][2 * x], o[d][2 * x + 1]);
-    }
-    __syncthreads();
-    const bool final = whole && b >= 0 && a.prefix_len == 0;
-    const int side = u > per * blockIdx.x;             // 0: the block's first pair
-    for (int x = tid; x < rows * (D / 4); x += THREADS) {
-      const int r = x / (D / 4), c = x % (D / 4) * 4;
-      float top = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < WK; k++) top = fmaxf(top, stat[(k * WM + r / 16) * 16 + r % 16].x);
-      const float from = top == -INFINITY ? 0.f : top;
-      float sum = 0.f;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-      for (int k = 0; k < WK; k++) {
-        const int at = (k * WM + r / 16) * 16 + r % 16;
-        const float f = exp2_fast(stat[at].x - from);
-        const float4 y = *(const float4 *)(acc + at * OPITCH + c);
-        sum += f * stat[at].y;
-        v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
+        for (int d = 0; d < D / 8; d++)
+          *(float2 *)(acc + r * D + ((d * 8 + t4 * 2) ^ (r & 3) * 8)) = make_float2(o[d][2 * x], o[d][2 * x + 1]);
       }
-      if (final) {
-        const Row p = row_of(a, b, kh, row0 + r);
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-        T *dst = (T *)a.out + p.b * a.o_seq + p.i * a.o_tok + p.h * a.o_head + c;
-        const uint32_t lo = pack<T>(v.x * inv, v.y * inv), hi = pack<T>(v.z * inv, v.w * inv);
-        if (o_aligned) {
-          *(uint2 *)dst = make_uint2(lo, hi);
-        } else {
-          T e[4];
-          memcpy(e, &lo, 4), memcpy(e + 2, &hi, 4);
-          for (int j = 0; j < 4; j++) dst[j] = e[j];
+      __syncthreads();
+      const bool whole = tile0 == 0 && now.tile == now.n - 1;
+      const bool final = whole && now.b >= 0 && a.prefix_len == 0;
+      for (int x = tid; x < rows * (D / 4); x += THREADS) {
+        const int r = x / (D / 4), c = x % (D / 4) * 4;
+        float best = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < WK; k++) best = fmaxf(best, stat[(k * WM + r / 16) * 16 + r % 16].x);
+        const float against = best == -INFINITY ? 0.f : best;
+        float sum = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < WK; k++) {
+          const int at = (k * WM + r / 16) * 16 + r % 16;
+          const float f = exp2_fast(stat[at].x - against);
+          const float4 y = *(const float4 *)(acc + at * D + (c ^ (at & 3) * 8));
+          sum += f * stat[at].y;
+          v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
         }
-        if (c == 0 && a.lse)
-          a.lse[((int64_t)p.b * a.n_new + p.i) * a.q_heads + p.h] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * 0.6931471805599453f;
-      } else if (whole) {
-        const Row p = row_of(a, b, kh, row0 + r);
-        const int64_t at = ((int64_t)p.b * a.n_new + p.i) * a.q_heads + p.h;
-        *(float4 *)(w.whole_o[b >= 0] + at * D + c) = v;
-        if (c == 0) w.whole_ml[b >= 0][at] = make_float2(top, sum);
-      } else {
-        const int64_t at = ((int64_t)blockIdx.x * 2 + side) * ROWS + r;
-        *(float4 *)(w.cut_o + at * D + c) = v;
-        if (c == 0) w.cut_ml[at] = make_float2(top, sum);
+        const Row p = row_of(a, now.b, kh, row0 + r);
+        const int64_t row = ((int64_t)p.b * a.n_new + p.i) * a.q_heads + p.h;
+        if (final) {
+          const float inv = sum == 0.f ? 0.f : 1.f / sum;
+          T *dst = (T *)a.out + p.b * a.o_seq + p.i * a.o_tok + p.h * a.o_head + c;
+          const uint32_t lo = pack<T>(v.x * inv, v.y * inv), hi = pack<T>(v.z * inv, v.w * inv);
+          if (o_aligned) {
+            *(uint2 *)dst = make_uint2(lo, hi);
+          } else {
+            T e[4];
+            memcpy(e, &lo, 4), memcpy(e + 2, &hi, 4);
+            for (int j = 0; j < 4; j++) dst[j] = e[j];
+          }
+          if (c == 0 && a.lse) a.lse[row] = sum == 0.f ? -INFINITY : (best + log2f(sum)) * 0.6931471805599453f;
+        } else {
+          // whole pairs by row, cut ones by block: its first (0) or its last (1)
+          const int64_t at = whole ? row : ((int64_t)blockIdx.x * 2 + !first_pair) * ROWS + r;
+          *(float4 *)((whole ? w.whole_o[now.b >= 0] : w.cut_o) + at * D + c) = v;
+          if (c == 0) (whole ? w.whole_ml[now.b >= 0] : w.cut_ml)[at] = make_float2(best, sum);
+        }
       }
+      first_pair = false;
     }
-    __syncthreads();
-    u += tile1 - tile0;
+    if (unit + 1 < count) advance(now);
+    if (++stage == STAGES) stage = 0;
   }
 }
 
@@ -843,46 +868,106 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+  return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
 // Joins what a row's pairs left, prefix first, then the sequence's own keys, each in the order of its blocks: one warp a
-// row.  A row whose one pair was written whole, with no prefix, is done already.
+// row.  A row whose one pair was written whole, with no prefix, is done already.  Up to 32 parts at a time, a lane takes the
+// maximum and sum of one; then all lanes add up the parts' values, several loads in flight.
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, const Line lo) {
   constexpr int E = D / 32;
+  using V = typename std::conditional<E == 2, float2, float4>::type;
+  constexpr int NV = E * 4 / sizeof(V);
   const int lane = threadIdx.x % 32;
   const int64_t row = (int64_t)blockIdx.x * WARPS + threadIdx.x / 32;
   if (row >= (int64_t)a.n_seqs * a.n_new * a.q_heads) return;
-  const int h = (int)(row % a.q_heads), i = (int)(row / a.q_heads % a.n_new), b = (int)(row / a.q_heads / a.n_new);
+  const int64_t token = quotient(row, a.q_heads), seq = quotient(token, a.n_new);
+  const int h = (int)(row - token * a.q_heads), i = (int)(token - seq * a.n_new), b = (int)seq;
   const int kh = h / a.group;
-  float m = -INFINITY, l = 0.f, acc[E] = {};
-  auto add = [&](const float *o, float2 ml) {
-    const float top = fmaxf(m, ml.x), from = top == -INFINITY ? 0.f : top;
-    const float f = exp2_fast(m - from), g = exp2_fast(ml.x - from);
-#pragma unroll
-    for (int e = 0; e < E; e++) acc[e] = acc[e] * f + o[lane * E + e] * g;
-    l = l * f + ml.y * g;
-    m = top;
+  // a pair's parts: its blocks c0 .. c0 + count - 1, or one result of its own
+  struct Parts { int64_t u0, c0, per; int count, r; bool whole; };
+  auto parts = [&](const Line &w, int r, int tiles, int64_t start, int n) {
+    Parts p = {0, 0, 0, 0, 0, false};
+    if (n) {
+      p.per = w.per ? w.per : w.starts[a.n_seqs + 1];
+      p.u0 = start + (int64_t)(kh * tiles + r / w.rows) * n;
+      p.r = r % w.rows;
+      p.c0 = quotient(p.u0, p.per);
+      p.count = (int)(quotient(p.u0 + n - 1, p.per) - p.c0) + 1;
+      p.whole = p.count == 1;
+    }
+    return p;
   };
-  auto gather = [&](const Line &w, bool own, int r, int tiles, int64_t start, int64_t n) {
-    const int pair = kh * tiles + r / w.rows;
-    const int64_t u0 = start + pair * n, per = w.per ? w.per : w.starts[a.n_seqs + 1], c0 = u0 / per, c1 = (u0 + n - 1) / per;
-    if (c0 == c1) {
-      if (own && a.prefix_len == 0) return true;
-      add(w.whole_o[own] + row * D, w.whole_ml[own][row]);
-    } else {
-      for (int64_t c = c0; c <= c1; c++) {
-        const int64_t at = (c * 2 + (u0 > c * per)) * w.rows + r % w.rows;
-        add(w.cut_o + at * D, w.cut_ml[at]);
+  const int in = h - kh * a.group, n = tiles_of(own_len(a, b));
+  const Parts pre = parts(lp, (b * a.n_new + i) * a.group + in, lp.prefix_tiles, 0, tiles_of(a.prefix_len, lp.keys));
+  const Parts own = parts(lo, i * a.group + in, lo.own_tiles, n ? lo.starts[b] : 0, n);
+  if (a.prefix_len == 0 && own.whole) return;
+  const int total = pre.count + own.count;
+  float m = -INFINITY, l = 0.f, acc[E] = {};
+  for (int first = 0; first < total; first += 32) {
+    const int x = first + lane;
+    const float *o = nullptr;
+    float2 ml = make_float2(-INFINITY, 0.f);
+    if (x < total) {
+      const bool mine = x >= pre.count;
+      const bool whole = mine ? own.whole : pre.whole;
+      const int64_t c = mine ? own.c0 + x - pre.count : pre.c0 + x;
+      const bool last = mine ? own.u0 > c * own.per : pre.u0 > c * pre.per;
+      const int64_t at = whole ? row : (c * 2 + last) * (mine ? lo.rows : lp.rows) + (mine ? own.r : pre.r);
+      o = (whole ? mine ? lo.whole_o[1] : lp.whole_o[0] : mine ? lo.cut_o : lp.cut_o) + at * D;
+      ml = (whole ? mine ? lo.whole_ml[1] : lp.whole_ml[0] : mine ? lo.cut_ml : lp.cut_ml)[at];
+    }
+    float top = fmaxf(m, ml.x);
+#pragma unroll
+    for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
+    const float from = top == -INFINITY ? 0.f : top, keep = exp2_fast(m - from);
+    const float f = exp2_fast(ml.x - from);
+    float sum = f * ml.y;
+#pragma unroll
+    for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(~0u, sum, k);
+    l = l * keep + sum;
+    m = top;
+#pragma unroll
+    for (int e = 0; e < E; e++) acc[e] *= keep;
+    const int count = min(32, total - first);
+    for (int y = 0; y < count; y += 4) {
+      V v[4][NV];
+      float g[4];
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        const float *from_o = (const float *)__shfl_sync(~0u, (unsigned long long)o, y + k);
+        g[k] = __shfl_sync(~0u, f, y + k);
+        if (y + k < count) {
+#pragma unroll
+          for (int e = 0; e < NV; e++) v[k][e] = ((const V *)from_o)[lane * NV + e];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        if (y + k < count) {
+#pragma unroll
+          for (int e = 0; e < E; e++) acc[e] += g[k] * ((const float *)v[k])[e];
+        }
       }
     }
-    return false;
-  };
-  if (a.prefix_len) gather(lp, false, (b * a.n_new + i) * a.group + h - kh * a.group, lp.prefix_tiles, 0, tiles_of(a.prefix_len, lp.keys));
-  const int n = tiles_of(own_len(a, b));
-  if (n && gather(lo, true, i * a.group + h - kh * a.group, lo.own_tiles, lo.starts[b], n)) return;
+  }
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T *dst = (T *)a.out + b * a.o_seq + i * a.o_tok + h * a.o_head + lane * E;
+  uint32_t packed[E / 2];
 #pragma unroll
-  for (int e = 0; e < E; e++) dst[e] = narrow<T>(acc[e] * inv);
+  for (int e = 0; e < E; e += 2) packed[e / 2] = pack<T>(acc[e] * inv, acc[e + 1] * inv);
+  if ((((uintptr_t)a.out >> 1 | a.o_seq | a.o_tok | a.o_head) & (E - 1)) == 0) {
+    if constexpr (E == 2) *(uint32_t *)dst = packed[0];
+    else if constexpr (E == 4) *(uint2 *)dst = make_uint2(packed[0], packed[1]);
+    else *(uint4 *)dst = make_uint4(packed[0], packed[1], packed[2], packed[3]);
+  } else {
+    T e[E];
+    memcpy(e, packed, sizeof(e));
+#pragma unroll
+    for (int k = 0; k < E; k++) dst[k] = e[k];
+  }
   if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
@@ -1007,7 +1092,7 @@ bool tile_maps(Pages &p, const gts_cache &c) {
 
 template <typename T, int D, int WM>
 cudaError_t stream(const Args &a, const Line &w, cudaStream_t s) {
-  constexpr int bytes = stream_smem<D, WM>();
+  constexpr int bytes = Ring<D, WM>::SMEM;
   static std::atomic<uint64_t> granted{0};
   const cudaError_t e = grant(k_stream<T, D, WM>, bytes, granted);
   if (e != cudaSuccess) return e;

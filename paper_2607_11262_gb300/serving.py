@@ -17,6 +17,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
 import numpy as np
 import torch
@@ -71,6 +72,13 @@ class AttentionDesc(ctypes.Structure):
                 ("max_pages", _u32), ("lens", _vp), ("workspace", _vp), ("workspace_bytes", _sz), ("d_status", _vp)]
 
 
+# The same layouts as format strings: the torch entry points pack a descriptor in one go, which takes a fifth of the time of
+# filling the structures above (about 2 against 10 us a call).
+_HEADS_FORMAT, _ROTARY_FORMAT, _CACHE_FORMAT = "Pqq", "PIifI", "PPqqqqqqIIIIi4x"
+_ROPE = struct.Struct("@IIIIiP" + _ROTARY_FORMAT + 4 * _HEADS_FORMAT)
+_APPEND = struct.Struct("@IIPP" + _ROTARY_FORMAT + 4 * _HEADS_FORMAT + _CACHE_FORMAT + "P")
+_ATTENTION = struct.Struct("@IIIf" + 2 * "Pqqq" + "P" + _CACHE_FORMAT + "PI4xPI4xPPNP")
+
 _lib = None
 
 
@@ -108,52 +116,67 @@ def _refuse(msg):
     raise GtsError(gts.GTS_ERR_INVALID_ARG, msg)
 
 
-def _tensor(t, name, dims, dtype=None, like=None):
-    if t.dim() != dims:
-        _refuse(f"{name}: {dims} dimensions wanted, got {t.dim()}")
-    if not t.is_cuda:
-        _refuse(f"{name} is not on a CUDA device")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+def _tensor(t, name, dims, like=None):
+    """Shape and strides of a tensor with a contiguous innermost dimension on the current device (or like another)."""
+    shape = t.shape
+    if len(shape) != dims:
+        _refuse(f"{name}: {dims} dimensions wanted, got {len(shape)}")
+    if like is None:
+        if not t.is_cuda:
+            _refuse(f"{name} is not on a CUDA device")
+    elif t.dtype != like.dtype or t.device != like.device:
         _refuse(f"{name}: {like.dtype} on {like.device} wanted, got {t.dtype} on {t.device}")
-    if dtype is not None and t.dtype != dtype:
-        _refuse(f"{name}: {dtype} wanted, got {t.dtype}")
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
+    strides = t.stride()
+    if strides[-1] != 1 and shape[-1] > 1:
         _refuse(f"{name}: the innermost dimension must be contiguous")
-    return t
+    return shape, strides
 
 
 def _index(t, name, shape, dtype, device):
-    """A contiguous index tensor of the given shape (None: any extent)."""
+    """The address of a contiguous index tensor of the given shape (None: any extent)."""
     if t.dtype != dtype or t.device != device:
         _refuse(f"{name}: {dtype} on {device} wanted, got {t.dtype} on {t.device}")
-    if t.dim() != len(shape) or any(w is not None and w != n for w, n in zip(shape, t.shape)) or not t.is_contiguous():
-        _refuse(f"{name}: contiguous {list(shape)} wanted, got {list(t.shape)}")
-    return t
+    got = t.shape
+    if got != shape and (len(got) != len(shape) or any(w is not None and w != n for w, n in zip(shape, got))) or \
+            not t.is_contiguous():
+        _refuse(f"{name}: contiguous {list(shape)} wanted, got {list(got)}")
+    return t.data_ptr()
 
 
 def _status(t, device):
-    if t is None:
-        return None
-    return _index(t, "status", (1,), torch.int32, device).data_ptr()
+    return 0 if t is None else _index(t, "status", (1,), torch.int32, device)
 
 
-def _on(stream):
-    """(context in which outputs are allocated, stream handle)"""
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _handle(stream, device):
+    """The stream's handle, for tensors that have to be on the current device."""
+    index = device.index
+    if index != torch.cuda.current_device():
+        _refuse(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    if stream is not None:
+        return stream.cuda_stream
+    return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+
+
+def _empty(shape, dtype, device, stream):
+    """Memory that belongs to the stream the call runs on."""
     if stream is None:
-        return gts._null(), torch.cuda.current_stream().cuda_stream
-    return torch.cuda.stream(stream), stream.cuda_stream
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _check_device(t):
-    if t.device.index != torch.cuda.current_device():
-        _refuse(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-
-
-def _heads(t):
-    if t is None:
-        return HeadsDesc()
-    s = t.stride()
-    return HeadsDesc(t.data_ptr(), s[0], s[1])
+def _output(out, name, shape, like, stream):
+    """(tensor, strides)"""
+    if out is None:
+        out = _empty(shape, like.dtype, like.device, stream)
+        return out, out.stride()
+    got, strides = _tensor(out, name, len(shape), like)
+    if got != shape:
+        _refuse(f"{name}: {list(shape)} wanted, got {list(got)}")
+    return out, strides
 
 
 class Rotary:
@@ -183,8 +206,7 @@ class Rotary:
         self.theta, self.factor = self._frequencies(rot_dim, base, scaling)
         units = [round(float(t) / (2 * math.pi) * 2.0 ** 64) % 2 ** 64 for t in self.theta]
         self.units = torch.from_numpy(np.array(units, np.uint64).view(np.int64)).to(device)
-        self._descs = [RotaryDesc(self.units.data_ptr() if units else None, rot_dim, _LAYOUTS[layout], self.factor, t)
-                       for t in (0, 1)]
+        self._values = [(self.units.data_ptr() if units else 0, rot_dim, _LAYOUTS[layout], self.factor, t) for t in (0, 1)]
 
     @staticmethod
     def _frequencies(rot_dim, base, scaling):
@@ -221,7 +243,7 @@ class PagedCache:
 
     def __init__(self, k, v):
         _tensor(k, "k cache", 4)
-        _tensor(v, "v cache", 4, like=k)
+        _tensor(v, "v cache", 4, k)
         if k.shape != v.shape:
             _refuse(f"k and v caches differ: {list(k.shape)}, {list(v.shape)}")
         if k.dtype not in _DTYPES:
@@ -230,7 +252,7 @@ class PagedCache:
         self.n_pages, self.page_size, self.kv_heads, self.head_dim = k.shape
         if self.page_size < 1:
             _refuse("page_size must be positive")
-        self.desc = CacheDesc(k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3], *k.shape, _DTYPES[k.dtype])
+        self._values = (k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3], *k.shape, _DTYPES[k.dtype])
 
     @classmethod
     def empty(cls, n_pages, page_size, kv_heads, head_dim, dtype, order="tokens", device="cuda"):
@@ -246,38 +268,33 @@ class PagedCache:
 
 
 def _rope_call(q, k, positions, rotary, transposed, out_q, out_k, stream):
-    _tensor(q, "q", 3)
-    _check_device(q)
+    shape, qs = _tensor(q, "q", 3)
+    device = q.device
+    handle = _handle(stream, device)
     dt = _DTYPES.get(q.dtype)
     if dt is None:
         _refuse(f"q: bfloat16, float16 or float32 wanted, got {q.dtype}")
-    T, heads, dim = q.shape
+    T, heads, dim = shape
     if dim != rotary.head_dim:
         _refuse(f"q has heads of {dim}, the rotary of {rotary.head_dim}")
-    _index(positions, "positions", (T,), torch.int32, q.device)
+    pos = _index(positions, "positions", (T,), torch.int32, device)
+    kh, kp, kop, ks, kos = 0, 0, 0, (0, 0), (0, 0)
     if k is not None:
-        _tensor(k, "k", 3, like=q)
-        if k.shape[0] != T or k.shape[2] != dim:
-            _refuse(f"k: [{T}, kv_heads, {dim}] wanted, got {list(k.shape)}")
-    ctx, handle = _on(stream)
-    with ctx:
-        out_q = torch.empty((T, heads, dim), dtype=q.dtype, device=q.device) if out_q is None else \
-            _same_shape(out_q, q, "out_q")
-        if k is not None:
-            out_k = torch.empty(k.shape, dtype=q.dtype, device=q.device) if out_k is None else \
-                _same_shape(out_k, k, "out_k")
-    kh = 0 if k is None else k.shape[1]
+        kshape, ks = _tensor(k, "k", 3, q)
+        kh = kshape[1]
+        if kshape[0] != T or kshape[2] != dim:
+            _refuse(f"k: [{T}, kv_heads, {dim}] wanted, got {list(kshape)}")
+        out_k, kos = _output(out_k, "out_k", kshape, q, stream)
+        if kh:
+            kp, kop = k.data_ptr(), out_k.data_ptr()
+    else:
+        out_k = None
+    out_q, qos = _output(out_q, "out_q", shape, q, stream)
     if T and (heads or kh):
-        gts_rope(RopeDesc(T, heads, kh, dim, dt, positions.data_ptr(), rotary._descs[transposed], _heads(q),
-                          _heads(k if kh else None), _heads(out_q), _heads(out_k if kh else None)), handle)
-    return out_q, out_k if k is not None else None
-
-
-def _same_shape(out, t, name):
-    _tensor(out, name, t.dim(), like=t)
-    if out.shape != t.shape:
-        _refuse(f"{name}: {list(t.shape)} wanted, got {list(out.shape)}")
-    return out
+        gts._check(_load().gts_rope(_ROPE.pack(
+            T, heads, kh, dim, dt, pos, *rotary._values[transposed], q.data_ptr(), qs[0], qs[1], kp, ks[0], ks[1],
+            out_q.data_ptr(), qos[0], qos[1], kop, kos[0], kos[1]), handle))
+    return out_q, out_k
 
 
 class _Rope(torch.autograd.Function):
@@ -320,41 +337,35 @@ def append_kv(q, k, v, positions, slots, rotary, cache, out_q=None, status=None,
     page * page_size + index within the page, no two alike; a negative one is a padding row, of which nothing is
     written to the cache.  A slot beyond the cache writes nothing and stores GTS_ERR_INVALID_PARAMS to ``status``
     (int32 [1] on the device), where given."""
-    _tensor(q, "q", 3, like=cache.k)
-    _check_device(q)
-    T, heads, dim = q.shape
+    shape, qs = _tensor(q, "q", 3, cache.k)
+    device = q.device
+    handle = _handle(stream, device)
+    T, heads, dim = shape
     if dim != cache.head_dim or dim != rotary.head_dim:
         _refuse(f"heads of {dim} (q), {cache.head_dim} (cache) and {rotary.head_dim} (rotary)")
-    for t, name in ((k, "k"), (v, "v")):
-        _tensor(t, name, 3, like=q)
-        if t.shape != (T, cache.kv_heads, dim):
-            _refuse(f"{name}: {[T, cache.kv_heads, dim]} wanted, got {list(t.shape)}")
-    _index(positions, "positions", (T,), torch.int32, q.device)
-    _index(slots, "slots", (T,), torch.int64, q.device)
-    ctx, handle = _on(stream)
-    with ctx:
-        out_q = torch.empty((T, heads, dim), dtype=q.dtype, device=q.device) if out_q is None else \
-            _same_shape(out_q, q, "out_q")
-    st = _status(status, q.device)
+    (kshape, ks), (vshape, vs) = _tensor(k, "k", 3, q), _tensor(v, "v", 3, q)
+    if kshape != (T, cache.kv_heads, dim) or vshape != kshape:
+        _refuse(f"k and v: {[T, cache.kv_heads, dim]} wanted, got {list(kshape)} and {list(vshape)}")
+    pos = _index(positions, "positions", (T,), torch.int32, device)
+    at = _index(slots, "slots", (T,), torch.int64, device)
+    st = _status(status, device)
+    out_q, qos = _output(out_q, "out_q", shape, q, stream)
     if T:
-        gts_append_kv(AppendDesc(T, heads, positions.data_ptr(), slots.data_ptr(), rotary._descs[0], _heads(q),
-                                 _heads(k), _heads(v), _heads(out_q), cache.desc, st), handle)
+        gts._check(_load().gts_append_kv(_APPEND.pack(
+            T, heads, pos, at, *rotary._values[0], q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(),
+            vs[0], vs[1], out_q.data_ptr(), qos[0], qos[1], *cache._values, st), handle))
     return out_q
 
 
-def _attention_shape(q, cache, prefix_len, max_pages, scale=1.0):
-    B, new, heads, _ = q.shape
-    d = AttentionDesc(B, new, heads, scale)
-    d.cache, d.prefix_len, d.max_pages = cache.desc, prefix_len, max_pages
-    return d
+def _workspace_bytes(shape, cache, prefix_len, max_pages):
+    return int(_load().gts_attention_workspace_bytes(_ATTENTION.pack(
+        *shape[:3], 1.0, 0, 0, 0, 0, 0, 0, 0, 0, 0, *cache._values, 0, prefix_len, 0, max_pages, 0, 0, 0, 0)))
 
 
 def attention_workspace(cache, q, prefix_len, page_table, stream=None):
-    """A workspace for ``prefix_attention`` calls of this shape (and of this prefix or a shorter one); calls that may
-    run at the same time need one each."""
-    need = gts_attention_workspace_bytes(_attention_shape(q, cache, prefix_len, page_table.shape[1]))
-    with _on(stream)[0]:
-        return torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+    """A workspace for ``prefix_attention`` calls of this shape; calls that may run at the same time need one each."""
+    need = _workspace_bytes(q.shape, cache, prefix_len, page_table.shape[1])
+    return _empty(max(need, 16), torch.uint8, q.device, stream)
 
 
 def prefix_attention(q, cache, prefix_pages, prefix_len, page_table, lens, scale=None, out=None, lse=None,
@@ -367,36 +378,34 @@ def prefix_attention(q, cache, prefix_pages, prefix_len, page_table, lens, scale
     prefix and its sequence's tokens up to its own.  ``scale``: of the products (default 1 / sqrt(head_dim)).  A query
     that sees nothing gets zeros and lse = -inf (float32 [seqs, new, heads]).  A page number or a length out of range
     is not followed and stores GTS_ERR_INVALID_PARAMS to ``status`` (int32 [1] on the device), where given."""
-    _tensor(q, "q", 4, like=cache.k)
-    _check_device(q)
-    B, new, heads, dim = q.shape
+    shape, qs = _tensor(q, "q", 4, cache.k)
+    device = q.device
+    handle = _handle(stream, device)
+    B, new, heads, dim = shape
     if dim != cache.head_dim:
         _refuse(f"heads of {dim} (q) and {cache.head_dim} (cache)")
     if not 0 <= prefix_len <= 1 << 30:
         _refuse(f"prefix_len out of range: {prefix_len}")
-    dev = q.device
-    _index(prefix_pages, "prefix_pages", (None,), torch.int32, dev)
+    prefix_at = _index(prefix_pages, "prefix_pages", (None,), torch.int32, device)
     if prefix_pages.shape[0] * cache.page_size < prefix_len:
         _refuse(f"{prefix_pages.shape[0]} prefix pages of {cache.page_size} hold no {prefix_len} tokens")
-    _index(page_table, "page_table", (B, None), torch.int32, dev)
-    _index(lens, "lens", (B,), torch.int32, dev)
-    d = _attention_shape(q, cache, prefix_len, page_table.shape[1], 1.0 / math.sqrt(dim) if scale is None else scale)
-    ctx, handle = _on(stream)
-    with ctx:
-        out = torch.empty((B, new, heads, dim), dtype=q.dtype, device=dev) if out is None else _same_shape(out, q, "out")
-        if lse is None:
-            lse = torch.empty((B, new, heads), dtype=torch.float32, device=dev)
-        else:
-            _index(lse, "lse", (B, new, heads), torch.float32, dev)
-        if workspace is None:
-            workspace = torch.empty(max(gts_attention_workspace_bytes(d), 16), dtype=torch.uint8, device=dev)
-    s, o = q.stride(), out.stride()
-    d.q, d.q_seq_stride, d.q_token_stride, d.q_head_stride = q.data_ptr(), s[0], s[1], s[2]
-    d.out, d.out_seq_stride, d.out_token_stride, d.out_head_stride = out.data_ptr(), o[0], o[1], o[2]
-    d.lse, d.prefix_pages, d.page_table, d.lens = (lse.data_ptr(), prefix_pages.data_ptr(), page_table.data_ptr(),
-                                                   lens.data_ptr())
-    d.workspace, d.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    d.d_status = _status(status, dev)
+    table_at = _index(page_table, "page_table", (B, None), torch.int32, device)
+    max_pages = page_table.shape[1]
+    lens_at = _index(lens, "lens", (B,), torch.int32, device)
+    st = _status(status, device)
+    out, os = _output(out, "out", shape, q, stream)
+    if lse is None:
+        lse = _empty((B, new, heads), torch.float32, device, stream)
+        lse_at = lse.data_ptr()
+    else:
+        lse_at = _index(lse, "lse", (B, new, heads), torch.float32, device)
+    if workspace is None:
+        workspace = _empty(max(_workspace_bytes(shape, cache, prefix_len, max_pages), 16), torch.uint8, device, stream)
+    elif workspace.device != device or not workspace.is_contiguous():
+        _refuse(f"workspace: contiguous on {device} wanted")
     if B and new:
-        gts_prefix_attention(d, handle)
+        gts._check(_load().gts_prefix_attention(_ATTENTION.pack(
+            B, new, heads, 1.0 / math.sqrt(dim) if scale is None else scale, q.data_ptr(), qs[0], qs[1], qs[2],
+            out.data_ptr(), os[0], os[1], os[2], lse_at, *cache._values, prefix_at, prefix_len, table_at, max_pages, lens_at,
+            workspace.data_ptr(), workspace.nbytes, st), handle))
     return out, lse

@@ -50,6 +50,24 @@ def test_descriptors_have_the_headers_layout():
     assert got == want
 
 
+def test_packed_descriptors_are_the_structures():
+    """Each field's value comes back from its place in the structure."""
+    for packed, struct in ((serving._ROPE, serving.RopeDesc), (serving._APPEND, serving.AppendDesc),
+                           (serving._ATTENTION, serving.AttentionDesc)):
+        flat = []
+
+        def leaves(s, at):
+            for name, kind in s._fields_:
+                if issubclass(kind, ctypes.Structure):
+                    leaves(kind, at + getattr(s, name).offset)
+                else:
+                    flat.append((at + getattr(s, name).offset, kind))
+        leaves(struct, 0)
+        assert packed.size == ctypes.sizeof(struct)
+        raw = packed.pack(*range(1, len(flat) + 1))
+        assert [int(kind.from_buffer_copy(raw, at).value) for at, kind in flat] == list(range(1, len(flat) + 1))
+
+
 @pytest.mark.parametrize("scaling", SCALINGS)
 @pytest.mark.parametrize("rot", [2, 16, 96, 128])
 def test_frequencies(rot, scaling):
