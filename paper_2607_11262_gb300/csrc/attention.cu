@@ -31,6 +31,9 @@ struct Args {
   int32_t *status;
 };
 
+template <typename T> __device__ __forceinline__ float widen(T x);
+template <> __device__ __forceinline__ float widen(__half x) { return __half2float(x); }
+template <> __device__ __forceinline__ float widen(__nv_bfloat16 x) { return __bfloat162float(x); }
 template <typename T> __device__ __forceinline__ T narrow(float x);
 template <> __device__ __forceinline__ __half narrow(float x) { return __float2half_rn(x); }
 template <> __device__ __forceinline__ __nv_bfloat16 narrow(float x) { return __float2bfloat16_rn(x); }
@@ -39,10 +42,6 @@ template <> __device__ __forceinline__ __nv_bfloat16 narrow(float x) { return __
 __device__ __forceinline__ uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void copy16(uint32_t dst, const void *src, bool live) {  // zeros where not live
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(live ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 __device__ __forceinline__ void ldsm(uint32_t (&r)[4], uint32_t at) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -68,6 +67,48 @@ __device__ __forceinline__ float exp2_fast(float x) {  // ex2.approx: 2 ulp, 0 f
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+__device__ __forceinline__ void bar_init(uint32_t bar, int count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("{\n.reg .b64 t;\nmbarrier.arrive.shared::cta.b64 t, [%0];\n}" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("{\n.reg .b64 t;\nmbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1;\n}" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
+// Every wait ends: after two seconds, or when another warp has given up, the block winds down with an error status.
+__device__ __forceinline__ uint64_t now_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+constexpr uint64_t LIMIT_NS = 2000000000ull;
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *dead) {
+  for (int n = 0; n < 1024; n++)  // reading the timer takes longer than most waits
+    if (bar_try(bar, parity)) return true;
+  const uint64_t from = now_ns();
+  while (!*dead) {
+    for (int n = 0; n < 64; n++)
+      if (bar_try(bar, parity)) return true;
+    if (now_ns() - from > LIMIT_NS) *dead = 1;
+  }
+  return false;
+}
+__device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int page, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(page), "r"(bar) : "memory");
+}
+// the barrier's next arrival comes when this thread's copies so far have landed
+__device__ __forceinline__ void bar_arrive_copies(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 template <typename T> __device__ __forceinline__ uint32_t pack(float lo, float hi);
 template <> __device__ __forceinline__ uint32_t pack<__nv_bfloat16>(float lo, float hi) {
   uint32_t r;
@@ -111,6 +152,10 @@ __device__ __forceinline__ int own_len(const Args &a, int b) {
   return max(0, min(len, most));
 }
 
+__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
+  return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
+}
+
 struct Row { int b, i, h; };
 
 // Row r of a pair's rows: prefix rows run over all sequences (b = -1), own rows over one.
@@ -124,46 +169,59 @@ __device__ __forceinline__ Row row_of(const Args &a, int b, int kh, int r) {
   return x;
 }
 
+struct Pages {
+  CUtensorMap k, v;    // pages x heads x tokens (or tokens x heads) x D, boxes of `box` tokens of a head x 64 values (0: no maps)
+  int box, k_heads_first, v_heads_first;
+};
+
 // A place in the line of units: a tile of keys of a pair of a sequence (b = -1: the prefix).
 struct Place { int b, len, n, pairs, pair, tile; };
 
-// One block of 4 warps: WM of them along the rows (16 each), 4 / WM along a tile's keys.  Keys and values stream through
-// a ring of tiles in shared memory by 16-byte asynchronous copies, gathered row by row from their pages; the copies run
-// STAGES - 1 tiles ahead across the ends of pairs, so that a short sequence does not stop them, and a pair's queries come
-// with its first tile.  Scores and weights stay in the fragments of m16n8k16 products; each warp keeps its own running
-// maximum and sum, and the warps along the keys are joined at the end of a pair, in the stage just read.  Weights are
-// rounded to the type of the values for their product with them (the sum is of the unrounded ones); everything else is in
-// 32 bits.
+// A block is 4 warps that compute and one that brings the data.  The fifth warp runs ahead along the block's stretch of the
+// line, across the ends of pairs, and fills a ring of tiles: boxes of tokens by TMA where the pages allow it (see tile_map),
+// else rows gathered by 16-byte copies, else (caches off the 16-byte grid) by plain loads.  A pair's queries come with its
+// first tile.  Of the others, WM stand along the rows (16 each) and 4 / WM along a tile's keys; they meet only where a pair
+// ends, to be joined in the stage just read.  Scores and weights stay in the fragments of m16n8k16 products, each warp with
+// its own running maximum and sum.  Weights are rounded to the type of the values for their product with them (the sum is of
+// the unrounded ones); everything else is in 32 bits.
 template <int D, int WM> struct Ring {
-  static constexpr int STAGES = (D == 64 ? 4 : 3) - (WM > 1);   // 3, 2 or 1 blocks to an SM for D of 64, 128, 256
-  static constexpr int TILE = KEYS * D * 2;            // bytes of a tile of keys or of values
+  static constexpr int STAGES = (D == 64 ? 4 : 3) - (WM > 1);   // as many as stream_per_sm blocks find room for
+  static constexpr int TILE = KEYS * D * 2;                     // bytes of a tile of keys or of values
   static constexpr int QUERIES = 16 * WM * D * 2;
-  static constexpr int SMEM = STAGES * (2 * TILE + QUERIES) + 2 * KEYS * 2 * 8 + 64 * 8 + 64;
+  static constexpr int SMEM = 1024 /* alignment */ + STAGES * (2 * TILE + QUERIES) + 64 * 8 + (2 * STAGES + 1) * 8 + 48;
 };
+constexpr int STREAM_THREADS = THREADS + 32;
+constexpr int stream_per_sm(int D) { return D == 64 ? 3 : D == 128 ? 2 : 1; }
 
 template <typename T, int D, int WM>
-__global__ void __launch_bounds__(THREADS) k_stream(const Args a, const Line w) {
+__global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(const Args a, const Line w, const __grid_constant__ Pages maps) {
   using R = Ring<D, WM>;
   constexpr int WK = WARPS / WM, ROWS = 16 * WM, KW = KEYS / WK, STAGES = R::STAGES, TILE = R::TILE;
-  constexpr int CH = D / 8, PITCH = D * 2;
-  extern __shared__ __align__(128) unsigned char smem[];
-  unsigned char *ring = smem, *qs = smem + STAGES * 2 * TILE;
-  int64_t *offs = (int64_t *)(qs + STAGES * R::QUERIES);  // [2][KEYS][2]: where the rows of the next tile to load start
-  float2 *stat = (float2 *)(offs + 2 * KEYS * 2);         // [64]: maximum and sum of each warp's rows
-  int64_t *found = (int64_t *)(stat + 64);                // [4]
-  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
-  const int wm = warp % WM, wk = warp / WM, quad = lane / 4, t4 = lane % 4;
-  const uint32_t ring_at = smem_u32(ring), q_at = smem_u32(qs);
-  const bool aligned = ((((uintptr_t)a.k | (uintptr_t)a.v) >> 1 | a.k_page | a.k_tok | a.k_head | a.v_page | a.v_tok | a.v_head) & 7) == 0;
-  const bool q_aligned = (((uintptr_t)a.q >> 1 | a.q_seq | a.q_tok | a.q_head) & 7) == 0;
-  const bool o_aligned = (((uintptr_t)a.out >> 1 | a.o_seq | a.o_tok | a.o_head) & 3) == 0;
-  const float sl2 = a.scale * 1.4426950408889634f;     // scores in units of log 2
+  constexpr int CH = D / 8, HALF = KEYS * 128, QHALF = ROWS * 128;  // a tile's and the queries' 64 columns: rows of 128 bytes
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char *const ring = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+  unsigned char *const qs = ring + STAGES * 2 * TILE;
+  float2 *const stat = (float2 *)(qs + STAGES * R::QUERIES);        // [64]: maximum and sum of each warp's rows
+  uint64_t *const bars = (uint64_t *)(stat + 64);
+  int64_t *const found = (int64_t *)(bars + 2 * STAGES + 1);        // [5]; the last is the flag
+  volatile int *const dead = (volatile int *)(found + 5);
+  const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
+  const uint32_t ring_at = smem_u32(ring), q_at = smem_u32(qs), bar0 = smem_u32(bars);
+  auto full = [&](int s) { return bar0 + s * 8; };
+  auto empty = [&](int s) { return bar0 + (STAGES + s) * 8; };
+  const uint32_t together = bar0 + 2 * STAGES * 8;
+  if (tid == 0) {
+    for (int s = 0; s < STAGES; s++) bar_init(full(s), 33), bar_init(empty(s), WARPS);
+    bar_init(together, WARPS);
+    *dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
 
   // the line of units, and this block's stretch of it
   const int n_prefix = w.has_prefix ? tiles_of(a.prefix_len) : 0;
   const int64_t prefix_units = (int64_t)n_prefix * a.kv_heads * w.prefix_tiles;
   const int own_pairs = a.kv_heads * w.own_tiles;
-  const int each = w.has_own ? (a.n_seqs + THREADS - 1) / THREADS : 0;
+  const int each = w.has_own && tid < THREADS ? (a.n_seqs + THREADS - 1) / THREADS : 0;
   const int b_first = min(a.n_seqs, tid * each), b_last = min(a.n_seqs, (tid + 1) * each);
   int64_t mine = 0;
   for (int b = b_first; b < b_last; b++) mine += (int64_t)tiles_of(own_len(a, b)) * own_pairs;
@@ -172,7 +230,7 @@ __global__ void __launch_bounds__(THREADS) k_stream(const Args a, const Line w) 
     const int64_t x = __shfl_up_sync(~0u, upto, o);
     if (lane >= o) upto += x;
   }
-  if (lane == 31) found[warp] = upto;
+  if (lane == 31 && warp < WARPS) found[warp] = upto;
   __syncthreads();
   int64_t base = prefix_units, total = prefix_units;
   for (int x = 0; x < WARPS; x++) {
@@ -180,10 +238,10 @@ __global__ void __launch_bounds__(THREADS) k_stream(const Args a, const Line w) 
     total += found[x];
   }
   base += upto - mine;                                 // first unit of sequence b_first
-  const int64_t per = (total + w.blocks - 1) / w.blocks;
+  const int64_t per = quotient(total + w.blocks - 1, w.blocks);
   const int64_t u0 = per * blockIdx.x, u1 = min(total, u0 + per);
   __syncthreads();
-  if (blockIdx.x == 0) {
+  if (blockIdx.x == 0 && tid < THREADS) {
     int64_t at = base;
     for (int b = b_first; b < b_last; b++) {
       w.starts[b] = at;
@@ -211,7 +269,7 @@ __global__ void __launch_bounds__(THREADS) k_stream(const Args a, const Line w) 
     now.len = in_prefix ? a.prefix_len : own_len(a, now.b);
     now.n = tiles_of(now.len);
     now.pairs = in_prefix ? a.kv_heads * w.prefix_tiles : own_pairs;
-    now.pair = (int)(in / now.n);
+    now.pair = (int)quotient(in, now.n);
     now.tile = (int)(in - (int64_t)now.pair * now.n);
   }
   const int count = (int)(u1 - u0);
@@ -226,292 +284,381 @@ __global__ void __launch_bounds__(THREADS) k_stream(const Args a, const Line w) 
     } while (p.n == 0);
   };
   auto row_tiles = [&](const Place &p) { return p.b < 0 ? w.prefix_tiles : w.own_tiles; };
-
-  // page numbers are fetched two tiles ahead of the copies, places one tile ahead
-  Place ahead = now, placed = now, fetched = now;
-  int page_next = 0, n_fetched = 0, n_placed = 0, n_loaded = 0, load_stage = 0, load_seg = -1;
-  auto fetch = [&] {
-    if (n_fetched < count) {
-      if (n_fetched) advance(ahead);
-      fetched = ahead;
-      const int j = ahead.tile * KEYS + tid;
-      const int32_t *pages = ahead.b < 0 ? a.prefix_pages : a.table + (int64_t)ahead.b * a.max_pages;
-      if (tid < KEYS && j < ahead.len) page_next = pages[j / a.page_size];
-    }
-    n_fetched++;
+  bool alive = true;
+  int stage = 0;
+  uint32_t lap = 0;
+  auto next = [&] {
+    if (++stage == STAGES) stage = 0, lap++;
   };
-  auto place = [&] {
-    if (n_placed < count) {
-      placed = fetched;
-      if (tid < KEYS) {
-        const int j = placed.tile * KEYS + tid, kh = placed.pair / row_tiles(placed);
-        int64_t k_off = -1, v_off = 0;
-        if (j < placed.len) {
-          if (page_next < 0 || page_next >= a.n_pages) {
-            if (a.status) *a.status = GTS_ERR_INVALID_PARAMS;
-          } else {
-            const int in = j % a.page_size;
-            k_off = page_next * a.k_page + in * a.k_tok + kh * a.k_head;
-            v_off = page_next * a.v_page + in * a.v_tok + kh * a.v_head;
+
+  if (warp == WARPS) {
+    // ---- the warp that brings the data
+    const bool aligned = ((((uintptr_t)a.k | (uintptr_t)a.v) >> 1 | a.k_page | a.k_tok | a.k_head | a.v_page | a.v_tok | a.v_head) & 7) == 0;
+    const bool q_aligned = (((uintptr_t)a.q >> 1 | a.q_seq | a.q_tok | a.q_head) & 7) == 0;
+    const int box = maps.box, boxes = box ? KEYS / box : 0;
+    int page[2];                                       // of this lane's box, or of its two rows; -1: none
+    auto look_up = [&](const Place &p) {
+      const int32_t *pages = p.b < 0 ? a.prefix_pages : a.table + (int64_t)p.b * a.max_pages;
+#pragma unroll
+      for (int x = 0; x < 2; x++) {
+        const int j = p.tile * KEYS + (box ? lane * box : lane + 32 * x);
+        page[x] = -1;
+        if (box ? x == 0 && lane < boxes && j < p.len : j < p.len) page[x] = pages[j / a.page_size] & 0x7FFFFFFF;
+      }
+    };
+    Place ahead = now;
+    look_up(ahead);
+    int seg = -1;
+    for (int unit = 0; unit < count; unit++) {
+      const Place at = ahead;
+      int to_load[2] = {page[0], page[1]};
+      if (unit + 1 < count) {                          // the next tile's page numbers are fetched while this one waits
+        advance(ahead);
+        look_up(ahead);
+      }
+      if (unit >= STAGES) alive = __all_sync(~0u, bar_wait(empty(stage), (lap - 1) & 1, dead));
+      if (!alive) break;
+      const int tiles = row_tiles(at), kh = at.pair / tiles;
+#pragma unroll
+      for (int x = 0; x < 2; x++) {
+        if (to_load[x] >= a.n_pages) {                 // (a negative number has become a large one)
+          to_load[x] = box ? a.n_pages : -1;           // outside the map: the box is filled with zeros
+          if (a.status) *a.status = GTS_ERR_INVALID_PARAMS;
+        }
+      }
+      const uint32_t to = ring_at + stage * 2 * TILE;
+      uint32_t bytes = 0;
+      if (box) {
+        const bool live = to_load[0] >= 0;
+        bytes = __popc(__ballot_sync(~0u, live)) * box * D * 4;
+        if (lane == 0) bar_expect(full(stage), bytes);
+        __syncwarp();
+        if (live) {
+          const int token = (at.tile * KEYS + lane * box) % a.page_size;
+#pragma unroll
+          for (int x = 0; x < D / 64; x++) {
+            tile_load(to + x * HALF + lane * box * 128, &maps.k, x * 64, maps.k_heads_first ? kh : token,
+                      maps.k_heads_first ? token : kh, to_load[0], full(stage));
+            tile_load(to + TILE + x * HALF + lane * box * 128, &maps.v, x * 64, maps.v_heads_first ? kh : token,
+                      maps.v_heads_first ? token : kh, to_load[0], full(stage));
           }
         }
-        int64_t *to = offs + ((n_placed & 1) * KEYS + tid) * 2;
-        to[0] = k_off, to[1] = v_off;
-      }
-    }
-    n_placed++;
-  };
-  auto load = [&] {
-    if (n_loaded < count) {
-      const uint32_t at = ring_at + load_stage * 2 * TILE;
-      for (int x = tid; x < KEYS * CH; x += THREADS) {
-        const int r = x / CH, c = x % CH;
-        const int64_t *from = offs + ((n_loaded & 1) * KEYS + r) * 2;
-        const bool live = from[0] >= 0;
-        const T *k = (const T *)a.k + (live ? from[0] + c * 8 : 0), *v = (const T *)a.v + (live ? from[1] + c * 8 : 0);
-        const uint32_t to = at + r * PITCH + ((c ^ (r & 7)) * 16);
-        if (aligned) {
-          copy16(to, k, live);
-          copy16(to + TILE, v, live);
-        } else {
-          T e[8], f[8];
+      } else {
+        if (lane == 0) bar_expect(full(stage), 0);
+        int64_t k_off[2], v_off[2];                    // this lane's two rows
 #pragma unroll
-          for (int j = 0; j < 8; j++) e[j] = live ? k[j] : narrow<T>(0.f), f[j] = live ? v[j] : narrow<T>(0.f);
-          memcpy(ring + (to - ring_at), e, 16);
-          memcpy(ring + (to - ring_at) + TILE, f, 16);
+        for (int x = 0; x < 2; x++) {
+          const int in = (at.tile * KEYS + lane + 32 * x) % a.page_size;
+          k_off[x] = to_load[x] < 0 ? -1 : to_load[x] * a.k_page + in * a.k_tok + kh * a.k_head;
+          v_off[x] = to_load[x] < 0 ? -1 : to_load[x] * a.v_page + in * a.v_tok + kh * a.v_head;
+        }
+#pragma unroll
+        for (int x = 0; x < 2; x++) {
+#pragma unroll 4
+          for (int y = 0; y < 32; y++) {               // lanes along the row: D / 8 pieces of keys, then of values
+            const int r = x * 32 + y;
+            const int64_t k = __shfl_sync(~0u, k_off[x], y), v = __shfl_sync(~0u, v_off[x], y);
+#pragma unroll
+            for (int z = 0; z < 2 * CH; z += 32) {
+              const int c = (z + lane) % CH;
+              const bool is_k = z + lane < CH, live = k >= 0;
+              if (z + lane >= 2 * CH) continue;
+              const T *src = (const T *)(is_k ? a.k : a.v) + (live ? (is_k ? k : v) + c * 8 : 0);
+              const uint32_t dst = stage * 2 * TILE + (is_k ? 0 : TILE) + c / 8 * HALF + r * 128 + ((c % 8) ^ (r & 7)) * 16;
+              if (aligned) {
+                copy16(ring_at + dst, src, live);
+              } else {
+                T e[8];
+#pragma unroll
+                for (int j = 0; j < 8; j++) e[j] = live ? src[j] : narrow<T>(0.f);
+                memcpy(ring + dst, e, 16);
+              }
+            }
+          }
         }
       }
-      if (n_loaded == 0 || placed.tile == 0) {         // a pair begins: its queries, zeros beyond the last row
-        load_seg = load_seg + 1 == STAGES ? 0 : load_seg + 1;
-        const int tiles = row_tiles(placed), kh = placed.pair / tiles, row0 = (placed.pair - kh * tiles) * ROWS;
-        const int rows = (placed.b < 0 ? a.n_seqs : 1) * a.n_new * a.group - row0;
-        for (int x = tid; x < ROWS * CH; x += THREADS) {
+      if (unit == 0 || at.tile == 0) {                 // a pair begins: its queries, zeros beyond the last row
+        seg = seg + 1 == STAGES ? 0 : seg + 1;
+        const int row0 = (at.pair - kh * tiles) * ROWS, rows = (at.b < 0 ? a.n_seqs : 1) * a.n_new * a.group - row0;
+        for (int x = lane; x < ROWS * CH; x += 32) {
           const int r = x / CH, c = x % CH;
-          const uint32_t to = load_seg * R::QUERIES + r * PITCH + ((c ^ (r & 7)) * 16);
-          const Row p = row_of(a, placed.b, kh, row0 + min(r, rows - 1));
+          const uint32_t dst = seg * R::QUERIES + c / 8 * QHALF + r * 128 + ((c % 8) ^ (r & 7)) * 16;
+          const Row p = row_of(a, at.b, kh, row0 + min(r, rows - 1));
           const T *src = (const T *)a.q + p.b * a.q_seq + p.i * a.q_tok + p.h * a.q_head + c * 8;
           if (q_aligned) {
-            copy16(q_at + to, src, r < rows);
+            copy16(q_at + dst, src, r < rows);
           } else {
             T e[8];
 #pragma unroll
             for (int j = 0; j < 8; j++) e[j] = r < rows ? src[j] : narrow<T>(0.f);
-            memcpy(qs + to, e, 16);
+            memcpy(qs + dst, e, 16);
           }
         }
       }
-      if (++load_stage == STAGES) load_stage = 0;
+      // every lane's arrival: when its copies have landed; plain stores are ordered by a plain one after them
+      if (!q_aligned || (!box && !aligned)) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        bar_arrive(full(stage));
+      } else {
+        bar_arrive_copies(full(stage));
+      }
+      next();
     }
-    n_loaded++;
-    copies_commit();
-  };
-  fetch();
-  place();
-  fetch();
-  __syncthreads();
+    if (!alive) {                                      // copies in flight end before the block does
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      const uint64_t from = now_ns();
+      for (int s = 0; s < STAGES; s++)
+        while (!bar_try(full(s), (s < stage ? lap : lap - 1) & 1) && now_ns() - from < LIMIT_NS) {}
+    }
+  } else {
+    // ---- the warps that compute
+    const int wm = warp % WM, wk = warp / WM, quad = lane / 4, t4 = lane % 4, mi = lane / 8, mr = lane % 8;
+    const bool o_aligned = (((uintptr_t)a.out >> 1 | a.o_seq | a.o_tok | a.o_head) & 3) == 0;
+    const float sl2 = a.scale * 1.4426950408889634f;   // scores in units of log 2
+    constexpr bool KEEP_Q = D <= 128 && WM == 1;       // the queries' fragments stay in registers
+    // where this lane's rows of a fragment start; column d * 16 of the 64 is reached by turning bits 5 and 6
+    const uint32_t k_lane = (wk * KW + (mi >> 1) * 8 + mr) * 128 + ((mi & 1) ^ mr) * 16;
+    const uint32_t v_lane = (wk * KW + (mi & 1) * 8 + mr) * 128 + ((mi >> 1) ^ mr) * 16;
+    const uint32_t q_lane = (wm * 16 + (mi & 1) * 8 + mr) * 128 + ((mi >> 1) ^ mr) * 16;
+    uint32_t meetings = 0;
+    auto meet = [&] {
+      __syncwarp();
+      if (lane == 0) bar_arrive(together);
+      alive = __all_sync(~0u, bar_wait(together, meetings++ & 1, dead));
+    };
+    int seg = -1, tile0 = 0, kh = 0, row0 = 0, rows = 0, limit[2] = {0, 0}, seen_by_all = 0;
+    bool first_pair = true;
+    float o[D / 8][4], m[2], l[2];
+    uint32_t qf[KEEP_Q ? D / 16 : 1][4];
+    for (int unit = 0; unit < count; unit++) {
+      alive = __all_sync(~0u, bar_wait(full(stage), lap & 1, dead));
+      if (!alive) break;
+      if (unit == 0 || now.tile == 0) {                // a pair begins
+        const int tiles = row_tiles(now);
+        seg = seg + 1 == STAGES ? 0 : seg + 1;
+        tile0 = now.tile;
+        kh = now.pair / tiles, row0 = (now.pair - kh * tiles) * ROWS;
+        rows = min(ROWS, (now.b < 0 ? a.n_seqs : 1) * a.n_new * a.group - row0);
+        seen_by_all = now.b < 0 ? now.len : now.len - (a.n_new - 1);
+#pragma unroll
+        for (int x = 0; x < 2; x++) {                  // keys that the rows of this thread's fragments see
+          const int r = row0 + wm * 16 + quad + 8 * x;
+          limit[x] = now.b < 0 ? now.len : now.len - (a.n_new - 1 - min(r / a.group, a.n_new - 1));
+          m[x] = -INFINITY, l[x] = 0.f;
+        }
+#pragma unroll
+        for (int x = 0; x < D / 8; x++) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
+        if constexpr (KEEP_Q) {
+#pragma unroll
+          for (int d = 0; d < D / 16; d++) ldsm(qf[d], q_at + seg * R::QUERIES + (q_lane ^ d % 4 * 32) + d / 4 * QHALF);
+        }
+      }
+      uint32_t k_at[4], v_at[4], q_from[4];
+#pragma unroll
+      for (int x = 0; x < 4; x++) {
+        k_at[x] = ring_at + stage * 2 * TILE + (k_lane ^ x * 32);
+        v_at[x] = ring_at + stage * 2 * TILE + (v_lane ^ x * 32);
+        q_from[x] = q_at + seg * R::QUERIES + (q_lane ^ x * 32);
+      }
+      const int key0 = now.tile * KEYS + wk * KW;
+      const bool mask = key0 + KW > seen_by_all;       // some row does not see some key of this warp's
+      auto attend = [&](auto is_masked) {
+        constexpr bool masked = decltype(is_masked)::value;
+        uint64_t bad = 0;                                // keys of this warp with values that are not finite, see below
+        if constexpr (masked) {
+          // value rows past the end are zeros: what the pages hold there may be NaN, and 0 * NaN is not 0
+          const int end = now.len - key0;
+          for (int x = lane; x < (KW - max(0, min(KW, end))) * CH; x += 32) {
+            const int r = KW - 1 - x / CH, c = x % CH;
+            *(uint4 *)(ring + stage * 2 * TILE + TILE + c / 8 * HALF + (wk * KW + r) * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+          }
+          // and so for a value that some rows see and others do not: not finite, it is kept out of the products
+          for (int r = max(0, seen_by_all - key0); r < min(KW, end); r++) {
+            bool odd = false;
+            for (int x = lane; x < D / 2; x += 32) {
+              const uint32_t both = *(const uint32_t *)(ring + stage * 2 * TILE + TILE + x / 32 * HALF + (wk * KW + r) * 128 + x % 32 * 4);
+              const uint32_t e = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
+              odd |= (both & e) == e || (both >> 16 & e) == e;
+            }
+            if (__any_sync(~0u, odd)) bad |= 1ull << r;
+          }
+          __syncwarp();
+        }
+        float s[KW / 8][4];
+#pragma unroll
+        for (int x = 0; x < KW / 8; x++) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
+#pragma unroll
+        for (int d = 0; d < D / 16; d++) {
+          if constexpr (!KEEP_Q) ldsm(qf[0], q_from[d % 4] + d / 4 * QHALF);
+#pragma unroll
+          for (int x = 0; x < KW / 16; x++) {
+            uint32_t kf[4];
+            ldsm(kf, k_at[d % 4] + d / 4 * HALF + x * 16 * 128);
+            mma<T>(s[2 * x], qf[KEEP_Q ? d : 0], kf[0], kf[1]);
+            mma<T>(s[2 * x + 1], qf[KEEP_Q ? d : 0], kf[2], kf[3]);
+          }
+        }
+        float top[2] = {m[0], m[1]};
+#pragma unroll
+        for (int x = 0; x < KW / 8; x++) {
+#pragma unroll
+          for (int c = 0; c < 4; c++) {
+            s[x][c] *= sl2;
+            if (masked && key0 + x * 8 + t4 * 2 + (c & 1) >= limit[c >> 1]) s[x][c] = -INFINITY;
+            top[c >> 1] = fmaxf(top[c >> 1], s[x][c]);
+          }
+        }
+        float keep[2], from[2];
+#pragma unroll
+        for (int x = 0; x < 2; x++) {
+          top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 1));
+          top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 2));
+          from[x] = top[x] == -INFINITY ? 0.f : top[x];  // nothing seen so far
+          keep[x] = exp2_fast(m[x] - from[x]);
+          m[x] = top[x];
+          l[x] *= keep[x];
+        }
+        if (__any_sync(~0u, keep[0] != 1.f || keep[1] != 1.f)) {
+#pragma unroll
+          for (int x = 0; x < D / 8; x++) {
+            o[x][0] *= keep[0], o[x][1] *= keep[0];
+            o[x][2] *= keep[1], o[x][3] *= keep[1];
+          }
+        }
+        uint32_t pf[KW / 16][4];
+#pragma unroll
+        for (int x = 0; x < KW / 8; x++) {
+#pragma unroll
+          for (int c = 0; c < 4; c++) {
+            s[x][c] = exp2_fast(s[x][c] - from[c >> 1]);
+            l[c >> 1] += s[x][c];
+          }
+          pf[x / 2][(x & 1) * 2] = pack<T>(s[x][0], s[x][1]);
+          pf[x / 2][(x & 1) * 2 + 1] = pack<T>(s[x][2], s[x][3]);
+        }
+#pragma unroll
+        for (int x = 0; x < KW / 16; x++) {
+          uint32_t stay[2] = {~0u, ~0u};                 // of the fragment's keys 2 t4, 2 t4 + 1 and the same + 8
+          if (masked && bad) {
+#pragma unroll
+            for (int y = 0; y < 2; y++) {
+              const uint32_t two = (uint32_t)(bad >> (x * 16 + y * 8 + t4 * 2)) & 3;
+              stay[y] = (two & 1 ? 0 : 0xFFFFu) | (two & 2 ? 0 : 0xFFFF0000u);
+            }
+          }
+#pragma unroll
+          for (int d = 0; d < D / 16; d++) {
+            uint32_t vf[4];
+            ldsm_t(vf, v_at[d % 4] + TILE + d / 4 * HALF + x * 16 * 128);
+            mma<T>(o[2 * d], pf[x], vf[0] & stay[0], vf[1] & stay[1]);
+            mma<T>(o[2 * d + 1], pf[x], vf[2] & stay[0], vf[3] & stay[1]);
+          }
+        }
+        if (masked && bad) {
+          // each such key alone, for the rows that see it
+#pragma unroll
+          for (int x = 0; x < KW / 8; x++) {
 #pragma unroll 1
-  for (int x = 0; x < STAGES - 1; x++) {
-    load();
-    place();
-    fetch();
-    __syncthreads();
-  }
-
-  int stage = 0, seg = -1, tile0 = 0, kh = 0, row0 = 0, rows = 0, limit[2] = {0, 0}, seen_by_all = 0;
-  bool first_pair = true;
-  float o[D / 8][4], m[2], l[2];
-  for (int unit = 0; unit < count; unit++) {
-    copies_wait<STAGES - 2>();
-    __syncthreads();
-    load();
-    place();
-    fetch();
-    if (unit == 0 || now.tile == 0) {                  // a pair begins
-      const int tiles = row_tiles(now);
-      seg = seg + 1 == STAGES ? 0 : seg + 1;
-      tile0 = now.tile;
-      kh = now.pair / tiles, row0 = (now.pair - kh * tiles) * ROWS;
-      rows = min(ROWS, (now.b < 0 ? a.n_seqs : 1) * a.n_new * a.group - row0);
-      seen_by_all = now.b < 0 ? now.len : now.len - (a.n_new - 1);
+            for (int k = 0; k < 8; k++) {
+              if (!(bad >> (x * 8 + k) & 1)) continue;
+              const int r = wk * KW + x * 8 + k, key = key0 + x * 8 + k;
+              const unsigned char *row = ring + stage * 2 * TILE + TILE + r * 128;
+              T two[2];
+              float weight[2];
 #pragma unroll
-      for (int x = 0; x < 2; x++) {                    // keys that the rows of this thread's fragments see
-        const int r = row0 + wm * 16 + quad + 8 * x;
-        limit[x] = now.b < 0 ? now.len : now.len - (a.n_new - 1 - min(r / a.group, a.n_new - 1));
-        m[x] = -INFINITY, l[x] = 0.f;
-      }
+              for (int y = 0; y < 2; y++) {
+                const uint32_t both = __shfl_sync(~0u, pf[x / 2][(x & 1) * 2 + y], quad * 4 + k / 2);
+                memcpy(two, &both, 4);
+                weight[y] = widen(k & 1 ? two[1] : two[0]);
+              }
 #pragma unroll
-      for (int x = 0; x < D / 8; x++) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
-    }
-    const uint32_t k_at = ring_at + stage * 2 * TILE, v_at = k_at + TILE, qf_at = q_at + seg * R::QUERIES;
-    const int mi = lane / 8, mr = lane % 8;
-    float s[KW / 8][4];
+              for (int d = 0; d < D / 8; d++) {
+                memcpy(two, row + d / 8 * HALF + ((d % 8) ^ (r & 7)) * 16 + t4 * 4, 4);
 #pragma unroll
-    for (int x = 0; x < KW / 8; x++) s[x][0] = s[x][1] = s[x][2] = s[x][3] = 0.f;
-#pragma unroll
-    for (int d = 0; d < D / 16; d++) {
-      uint32_t qf[4];
-      const int r = wm * 16 + (mi & 1) * 8 + mr;
-      ldsm(qf, qf_at + r * PITCH + (((d * 2 + (mi >> 1)) ^ (r & 7)) * 16));
-#pragma unroll
-      for (int x = 0; x < KW / 16; x++) {
-        uint32_t kf[4];
-        const int key = wk * KW + x * 16 + (mi >> 1) * 8 + mr;
-        ldsm(kf, k_at + key * PITCH + (((d * 2 + (mi & 1)) ^ (key & 7)) * 16));
-        mma<T>(s[2 * x], qf, kf[0], kf[1]);
-        mma<T>(s[2 * x + 1], qf, kf[2], kf[3]);
-      }
-    }
-    const int key0 = now.tile * KEYS + wk * KW;
-    const bool masked = key0 + KW > seen_by_all;
-    float top[2] = {m[0], m[1]};
-#pragma unroll
-    for (int x = 0; x < KW / 8; x++) {
-#pragma unroll
-      for (int c = 0; c < 4; c++) {
-        s[x][c] *= sl2;
-        if (masked && key0 + x * 8 + t4 * 2 + (c & 1) >= limit[c >> 1]) s[x][c] = -INFINITY;
-        top[c >> 1] = fmaxf(top[c >> 1], s[x][c]);
-      }
-    }
-    float keep[2], from[2];
-#pragma unroll
-    for (int x = 0; x < 2; x++) {
-      top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 1));
-      top[x] = fmaxf(top[x], __shfl_xor_sync(~0u, top[x], 2));
-      from[x] = top[x] == -INFINITY ? 0.f : top[x];    // nothing seen so far
-      keep[x] = exp2_fast(m[x] - from[x]);
-      m[x] = top[x];
-      l[x] *= keep[x];
-    }
-    if (__any_sync(~0u, keep[0] != 1.f || keep[1] != 1.f)) {
-#pragma unroll
-      for (int x = 0; x < D / 8; x++) {
-        o[x][0] *= keep[0], o[x][1] *= keep[0];
-        o[x][2] *= keep[1], o[x][3] *= keep[1];
-      }
-    }
-    uint32_t pf[KW / 16][4];
-#pragma unroll
-    for (int x = 0; x < KW / 8; x++) {
-#pragma unroll
-      for (int c = 0; c < 4; c++) {
-        s[x][c] = exp2_fast(s[x][c] - from[c >> 1]);
-        l[c >> 1] += s[x][c];
-      }
-      pf[x / 2][(x & 1) * 2] = pack<T>(s[x][0], s[x][1]);
-      pf[x / 2][(x & 1) * 2 + 1] = pack<T>(s[x][2], s[x][3]);
-    }
-#pragma unroll
-    for (int x = 0; x < KW / 16; x++) {
-      const int key = wk * KW + x * 16 + (mi & 1) * 8 + mr;
-#pragma unroll
-      for (int d = 0; d < D / 16; d++) {
-        uint32_t vf[4];
-        ldsm_t(vf, v_at + key * PITCH + (((d * 2 + (mi >> 1)) ^ (key & 7)) * 16));
-        mma<T>(o[2 * d], pf[x], vf[0], vf[1]);
-        mma<T>(o[2 * d + 1], pf[x], vf[2], vf[3]);
-      }
-    }
-
-    if (now.tile == now.n - 1 || unit == count - 1) {
-      // a pair ends here: the warps along the keys are joined in the stage just read, and its rows written
-      __syncthreads();
-      float *acc = (float *)(ring + stage * 2 * TILE); // [4 warps][16][D], columns of row r turned by 8 (r mod 4)
-#pragma unroll
-      for (int x = 0; x < 2; x++) {
-        l[x] += __shfl_xor_sync(~0u, l[x], 1);
-        l[x] += __shfl_xor_sync(~0u, l[x], 2);
-        const int r = warp * 16 + quad + 8 * x;
-        if (t4 == 0) stat[r] = make_float2(m[x], l[x]);
-#pragma unroll
-        for (int d = 0; d < D / 8; d++)
-          *(float2 *)(acc + r * D + ((d * 8 + t4 * 2) ^ (r & 3) * 8)) = make_float2(o[d][2 * x], o[d][2 * x + 1]);
-      }
-      __syncthreads();
-      const bool whole = tile0 == 0 && now.tile == now.n - 1;
-      const bool final = whole && now.b >= 0 && a.prefix_len == 0;
-      for (int x = tid; x < rows * (D / 4); x += THREADS) {
-        const int r = x / (D / 4), c = x % (D / 4) * 4;
-        float best = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < WK; k++) best = fmaxf(best, stat[(k * WM + r / 16) * 16 + r % 16].x);
-        const float against = best == -INFINITY ? 0.f : best;
-        float sum = 0.f;
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int k = 0; k < WK; k++) {
-          const int at = (k * WM + r / 16) * 16 + r % 16;
-          const float f = exp2_fast(stat[at].x - against);
-          const float4 y = *(const float4 *)(acc + at * D + (c ^ (at & 3) * 8));
-          sum += f * stat[at].y;
-          v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
-        }
-        const Row p = row_of(a, now.b, kh, row0 + r);
-        const int64_t row = ((int64_t)p.b * a.n_new + p.i) * a.q_heads + p.h;
-        if (final) {
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;
-          T *dst = (T *)a.out + p.b * a.o_seq + p.i * a.o_tok + p.h * a.o_head + c;
-          const uint32_t lo = pack<T>(v.x * inv, v.y * inv), hi = pack<T>(v.z * inv, v.w * inv);
-          if (o_aligned) {
-            *(uint2 *)dst = make_uint2(lo, hi);
-          } else {
-            T e[4];
-            memcpy(e, &lo, 4), memcpy(e + 2, &hi, 4);
-            for (int j = 0; j < 4; j++) dst[j] = e[j];
+                for (int c = 0; c < 2; c++) {
+                  if (key < limit[0]) o[d][c] += weight[0] * widen(two[c]);
+                  if (key < limit[1]) o[d][2 + c] += weight[1] * widen(two[c]);
+                }
+              }
+            }
           }
-          if (c == 0 && a.lse) a.lse[row] = sum == 0.f ? -INFINITY : (best + log2f(sum)) * 0.6931471805599453f;
-        } else {
-          // whole pairs by row, cut ones by block: its first (0) or its last (1)
-          const int64_t at = whole ? row : ((int64_t)blockIdx.x * 2 + !first_pair) * ROWS + r;
-          *(float4 *)((whole ? w.whole_o[now.b >= 0] : w.cut_o) + at * D + c) = v;
-          if (c == 0) (whole ? w.whole_ml[now.b >= 0] : w.cut_ml)[at] = make_float2(best, sum);
         }
+      };
+      if (mask) attend(std::true_type());
+      else attend(std::false_type());
+
+      if (now.tile == now.n - 1 || unit == count - 1) {
+        // a pair ends here: the warps along the keys are joined in the stage just read, and its rows written
+        meet();
+        if (!alive) break;
+        float *acc = (float *)(ring + stage * 2 * TILE);   // [4 warps][16][D], columns of row r turned by 8 (r mod 4)
+#pragma unroll
+        for (int x = 0; x < 2; x++) {
+          l[x] += __shfl_xor_sync(~0u, l[x], 1);
+          l[x] += __shfl_xor_sync(~0u, l[x], 2);
+          const int r = warp * 16 + quad + 8 * x;
+          if (t4 == 0) stat[r] = make_float2(m[x], l[x]);
+#pragma unroll
+          for (int d = 0; d < D / 8; d++)
+            *(float2 *)(acc + r * D + ((d * 8 + t4 * 2) ^ (r & 3) * 8)) = make_float2(o[d][2 * x], o[d][2 * x + 1]);
+        }
+        meet();
+        if (!alive) break;
+        const bool whole = tile0 == 0 && now.tile == now.n - 1;
+        const bool final = whole && now.b >= 0 && a.prefix_len == 0;
+        for (int x = tid; x < rows * (D / 4); x += THREADS) {
+          const int r = x / (D / 4), c = x % (D / 4) * 4;
+          float best = -INFINITY;
+#pragma unroll
+          for (int k = 0; k < WK; k++) best = fmaxf(best, stat[(k * WM + r / 16) * 16 + r % 16].x);
+          const float against = best == -INFINITY ? 0.f : best;
+          float sum = 0.f;
+          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+          for (int k = 0; k < WK; k++) {
+            const int at = (k * WM + r / 16) * 16 + r % 16;
+            const float f = exp2_fast(stat[at].x - against);
+            const float4 y = *(const float4 *)(acc + at * D + (c ^ (at & 3) * 8));
+            sum += f * stat[at].y;
+            v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
+          }
+          const Row p = row_of(a, now.b, kh, row0 + r);
+          const int64_t row = ((int64_t)p.b * a.n_new + p.i) * a.q_heads + p.h;
+          if (final) {
+            const float inv = sum == 0.f ? 0.f : 1.f / sum;
+            T *dst = (T *)a.out + p.b * a.o_seq + p.i * a.o_tok + p.h * a.o_head + c;
+            const uint32_t lo = pack<T>(v.x * inv, v.y * inv), hi = pack<T>(v.z * inv, v.w * inv);
+            if (o_aligned) {
+              *(uint2 *)dst = make_uint2(lo, hi);
+            } else {
+              T e[4];
+              memcpy(e, &lo, 4), memcpy(e + 2, &hi, 4);
+              for (int j = 0; j < 4; j++) dst[j] = e[j];
+            }
+            if (c == 0 && a.lse) a.lse[row] = sum == 0.f ? -INFINITY : (best + log2f(sum)) * 0.6931471805599453f;
+          } else {
+            // whole pairs by row, cut ones by block: its first (0) or its last (1)
+            const int64_t at = whole ? row : ((int64_t)blockIdx.x * 2 + !first_pair) * ROWS + r;
+            *(float4 *)((whole ? w.whole_o[now.b >= 0] : w.cut_o) + at * D + c) = v;
+            if (c == 0) (whole ? w.whole_ml[now.b >= 0] : w.cut_ml)[at] = make_float2(best, sum);
+          }
+        }
+        first_pair = false;
+        fence_async();                                 // the stage was written here and is next written by TMA
+      } else if (mask) {
+        fence_async();
       }
-      first_pair = false;
+      __syncwarp();
+      if (lane == 0) bar_arrive(empty(stage));
+      if (unit + 1 < count) advance(now);
+      next();
     }
-    if (unit + 1 < count) advance(now);
-    if (++stage == STAGES) stage = 0;
   }
+  __syncthreads();
+  if (*dead && tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
 }
 
 // ---------------------------------------------------------------- the prefix on the tensor cores
-__device__ __forceinline__ void bar_init(uint32_t bar, int count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint32_t bar) {
-  asm volatile("{\n.reg .b64 t;\nmbarrier.arrive.shared::cta.b64 t, [%0];\n}" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
-  asm volatile("{\n.reg .b64 t;\nmbarrier.arrive.expect_tx.shared::cta.b64 t, [%0], %1;\n}" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
-               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-  return ok;
-}
-// Every wait ends: after two seconds, or when another warp has given up, the block winds down with an error status.
-__device__ __forceinline__ uint64_t now_ns() {
-  uint64_t t;
-  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-  return t;
-}
-constexpr uint64_t LIMIT_NS = 2000000000ull;
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *dead) {
-  for (int n = 0; n < 1024; n++)  // reading the timer takes longer than most waits
-    if (bar_try(bar, parity)) return true;
-  const uint64_t from = now_ns();
-  while (!*dead) {
-    for (int n = 0; n < 64; n++)
-      if (bar_try(bar, parity)) return true;
-    if (now_ns() - from > LIMIT_NS) *dead = 1;
-  }
-  return false;
-}
-__device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap *map, int x, int y, int z, int page, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-               ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(page), "r"(bar) : "memory");
-}
 __device__ __forceinline__ void tc_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -577,11 +724,6 @@ template <int D> struct Tc {
 // 384 threads start with 168 registers each (64512): the row threads go on with 216 (55296), the rest with 56 (7168).
 #define MORE_REGISTERS() asm volatile("setmaxnreg.inc.sync.aligned.u32 216;")
 #define FEWER_REGISTERS() asm volatile("setmaxnreg.dec.sync.aligned.u32 56;")
-
-struct Pages {
-  CUtensorMap k, v;    // pages x heads x tokens (or tokens x heads) x D, boxes of `box` tokens of a head x 64 values
-  int box, k_heads_first, v_heads_first;
-};
 
 template <typename T, int D>
 __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Line w, const __grid_constant__ Pages maps, const uint32_t flip) {
@@ -710,7 +852,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
               const int r = nv + x / (D / 8), c = x % (D / 8);
               *(uint4 *)(ring + sv * TILE + c / 8 * HALF + r * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
             }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            fence_async();
           }
 #pragma unroll
           for (int h = 0; h < 2; h++) {
@@ -780,7 +922,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
         }
         *(uint4 *)(qs + h * (Tc<D>::Q / 2) + c / 8 * HALF + r * 128 + ((c % 8) ^ (r & 7)) * 16) = v;
       }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      fence_async();
       bar_arrive(q_full(h));
 
       float m = -INFINITY, l = 0.f;
@@ -866,10 +1008,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   __syncthreads();
   if (*dead && tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
-}
-
-__device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
-  return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
 }
 
 // Joins what a row's pairs left, prefix first, then the sequence's own keys, each in the order of its blocks: one warp a
@@ -1000,11 +1138,11 @@ constexpr int64_t TENSOR_ROWS = 48, APART_ROWS = 64;
 
 int box_of(int page_size) {  // tokens of a TMA box: the largest power of two that divides both the page and a tile
   int box = 1;
-  while (box < TC_KEYS && page_size % (box * 2) == 0) box *= 2;
+  while (box < KEYS && page_size % (box * 2) == 0) box *= 2;
   return box;
 }
 
-int stream_blocks(int D) { return SMS * (D == 64 ? 3 : D == 128 ? 2 : 1); }
+int stream_blocks(int D) { return SMS * stream_per_sm(D); }
 
 Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
   const int D = (int)d.cache.head_dim, group = (int)(d.q_heads / d.cache.kv_heads);
@@ -1045,7 +1183,7 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
 }
 
 // The shape's part of the rule for the tensor cores' kernel; tile_maps has the pointers' and strides' part.
-bool tensor_shape(const gts_attention_desc &d) { return d.cache.head_dim <= 128 && box_of((int)d.cache.page_size) >= 8; }
+bool tensor_shape(const gts_attention_desc &d) { return d.cache.head_dim <= 128; }
 
 typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -1085,24 +1223,28 @@ bool tile_map(CUtensorMap &map, int &heads_first, int box, const gts_cache &c, v
 }
 
 bool tile_maps(Pages &p, const gts_cache &c) {
-  p.box = box_of((int)c.page_size);
-  return c.n_pages && tile_map(p.k, p.k_heads_first, p.box, c, c.k, c.k_page_stride, c.k_token_stride, c.k_head_stride) &&
-         tile_map(p.v, p.v_heads_first, p.box, c, c.v, c.v_page_stride, c.v_token_stride, c.v_head_stride);
+  const int box = box_of((int)c.page_size);
+  if (box < 8 || !c.n_pages) return false;   // a box is whole groups of eight rows
+  p.box = box;
+  const bool ok = tile_map(p.k, p.k_heads_first, p.box, c, c.k, c.k_page_stride, c.k_token_stride, c.k_head_stride) &&
+                  tile_map(p.v, p.v_heads_first, p.box, c, c.v, c.v_page_stride, c.v_token_stride, c.v_head_stride);
+  if (!ok) p.box = 0;
+  return ok;
 }
 
 template <typename T, int D, int WM>
-cudaError_t stream(const Args &a, const Line &w, cudaStream_t s) {
+cudaError_t stream(const Args &a, const Line &w, const Pages &maps, cudaStream_t s) {
   constexpr int bytes = Ring<D, WM>::SMEM;
   static std::atomic<uint64_t> granted{0};
   const cudaError_t e = grant(k_stream<T, D, WM>, bytes, granted);
   if (e != cudaSuccess) return e;
-  k_stream<T, D, WM><<<w.blocks, THREADS, bytes, s>>>(a, w);
+  k_stream<T, D, WM><<<w.blocks, STREAM_THREADS, bytes, s>>>(a, w, maps);
   return cudaGetLastError();
 }
 
 template <typename T, int D>
-cudaError_t stream(const Args &a, const Line &w, cudaStream_t s) {
-  return w.rows == 16 ? stream<T, D, 1>(a, w, s) : w.rows == 32 ? stream<T, D, 2>(a, w, s) : stream<T, D, 4>(a, w, s);
+cudaError_t stream(const Args &a, const Line &w, const Pages &maps, cudaStream_t s) {
+  return w.rows == 16 ? stream<T, D, 1>(a, w, maps, s) : w.rows == 32 ? stream<T, D, 2>(a, w, maps, s) : stream<T, D, 4>(a, w, maps, s);
 }
 
 template <typename T, int D>
@@ -1117,11 +1259,11 @@ cudaError_t tensor(const Args &a, const Line &w, const Pages &maps, cudaStream_t
 template <typename T, int D>
 cudaError_t run(const Args &a, const Plan &p, const Pages &maps, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
-  if (p.way == APART) e = stream<T, D, 4>(a, p.prefix, s);
+  if (p.way == APART) e = stream<T, D, 4>(a, p.prefix, maps, s);
   if constexpr (D <= 128) {
     if (p.way == TENSOR) e = tensor<T, D>(a, p.prefix, maps, s);
   }
-  if (e == cudaSuccess) e = stream<T, D>(a, p.own, s);
+  if (e == cudaSuccess) e = stream<T, D>(a, p.own, maps, s);
   if (e != cudaSuccess) return e;
   const int64_t rows = (int64_t)a.n_seqs * a.n_new * a.q_heads;
   k_join<T, D><<<(unsigned)((rows + WARPS - 1) / WARPS), THREADS, 0, s>>>(a, p.prefix, p.own);
@@ -1186,9 +1328,9 @@ extern "C" gts_status gts_prefix_attention(const gts_attention_desc *d, void *st
   if (d->workspace_bytes < gts_attention_workspace_bytes(d))
     return gts::fail(GTS_ERR_NOMEM, "attention: workspace smaller than gts_attention_workspace_bytes");
   Pages maps = {};
-  Plan p = make_plan(*d, tensor_shape(*d), (char *)d->workspace);
-  // (a scale of 0 would turn the -infinity of masked scores into NaN there)
-  if (p.way == TENSOR && (d->scale == 0.f || !tile_maps(maps, c))) p = make_plan(*d, false, (char *)d->workspace);
+  const bool mapped = tile_maps(maps, c);
+  // (a scale of 0 would turn the -infinity of masked scores into NaN on the tensor cores)
+  const Plan p = make_plan(*d, mapped && d->scale != 0.f && tensor_shape(*d), (char *)d->workspace);
   const cudaError_t e = c.dtype == GTS_BF16 ? launch<__nv_bfloat16>(a, p, maps, c.head_dim, (cudaStream_t)stream)
                                             : launch<__half>(a, p, maps, c.head_dim, (cudaStream_t)stream);
   return e == cudaSuccess ? GTS_OK : gts::cuda_fail(e, "attention: launch");
