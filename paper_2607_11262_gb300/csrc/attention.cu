@@ -90,10 +90,14 @@ __device__ __forceinline__ uint64_t now_ns() {
 }
 constexpr uint64_t LIMIT_NS = 2000000000ull;
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *dead) {
-  for (int n = 0; n < 1024; n++)  // reading the timer takes longer than most waits
+  if (bar_try(bar, parity)) return true;   // (an unrolled loop around it would try several times before it looks)
+#pragma unroll 1
+  for (int n = 0; n < 1024; n++)           // reading the timer takes longer than most waits
     if (bar_try(bar, parity)) return true;
   const uint64_t from = now_ns();
+#pragma unroll 1
   while (!*dead) {
+#pragma unroll 1
     for (int n = 0; n < 64; n++)
       if (bar_try(bar, parity)) return true;
     if (now_ns() - from > LIMIT_NS) *dead = 1;
@@ -109,6 +113,24 @@ __device__ __forceinline__ void bar_arrive_copies(uint32_t bar) {
   asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float y;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+  return y;
+}
+// two 32-bit values in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 y;
+  asm("{\n.reg .b64 a, b, c;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmov.b64 c, {%6, %7};\nfma.rn.f32x2 a, a, b, c;\nmov.b64 {%0, %1}, a;\n}"
+      : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+  return y;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 y;
+  asm("{\n.reg .b64 a, b;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nadd.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}"
+      : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return y;
+}
 template <typename T> __device__ __forceinline__ uint32_t pack(float lo, float hi);
 template <> __device__ __forceinline__ uint32_t pack<__nv_bfloat16>(float lo, float hi) {
   uint32_t r;
@@ -128,13 +150,14 @@ template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi)
 // and each block takes an equal stretch of it, so ragged lengths cost nothing and the cut needs no plan from the host.
 // A pair that lies within one block's stretch leaves one result per row; one that is cut leaves a partial result per block,
 // which k_join adds up in the order of the keys.
+constexpr int SMS = 152;
 constexpr int KEYS = 64;
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 
 struct Line {           // the units of one launch
   int has_prefix, has_own;
   int rows, keys;       // of a pair's tile, of a unit
-  int64_t per;          // units per block, where the host knows them
+  int beside_prefix;    // the tensor cores' kernel runs at the same time
   int prefix_tiles, own_tiles;   // row tiles of the prefix's rows, of a sequence's rows
   int blocks;
   int64_t *starts;      // [n_seqs + 2]: first unit of each sequence, the units of all, units per block
@@ -155,6 +178,20 @@ __device__ __forceinline__ int own_len(const Args &a, int b) {
 __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
   return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
 }
+
+// The prefix's kernel is bound by the tensor cores and holds whole SMs, the sequences' own keys are bound by memory: both run
+// at the same time, on SMs dealt out by the time each needs.  In units of an own tile's time on an SM (0.55 us measured at a
+// head of 128): a tile of the prefix for 256 rows takes 4 (2.3 us), the end of a pair 1.3; and own tiles alone cannot go
+// faster than memory brings them, 104 to that time.  Both kernels come to the same numbers from the lengths.
+__device__ __forceinline__ int prefix_sms(const Args &a, const Line &prefix, int64_t own_tiles, int64_t own_pairs) {
+  const float p = 4.f * tiles_of(a.prefix_len, 128) * a.kv_heads * prefix.prefix_tiles, o = own_tiles + 1.3f * own_pairs;
+  if (own_tiles == 0) return SMS;
+  const float each = fmaxf((p + o) / SMS, own_tiles / 104.f);
+  return max(1, min(SMS - 1, (int)(p / each + 0.5f)));
+}
+
+__device__ __forceinline__ void dependents_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_kernels_before() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 struct Row { int b, i, h; };
 
@@ -188,13 +225,13 @@ template <int D, int WM> struct Ring {
   static constexpr int STAGES = (D == 64 ? 4 : 3) - (WM > 1);   // as many as stream_per_sm blocks find room for
   static constexpr int TILE = KEYS * D * 2;                     // bytes of a tile of keys or of values
   static constexpr int QUERIES = 16 * WM * D * 2;
-  static constexpr int SMEM = 1024 /* alignment */ + STAGES * (2 * TILE + QUERIES) + 64 * 8 + (2 * STAGES + 1) * 8 + 48;
+  static constexpr int SMEM = 1024 /* alignment */ + STAGES * (2 * TILE + QUERIES) + 64 * 8 + (2 * STAGES + 1) * 8 + 56;
 };
 constexpr int STREAM_THREADS = THREADS + 32;
-constexpr int stream_per_sm(int D) { return D == 64 ? 3 : D == 128 ? 2 : 1; }
+__host__ __device__ constexpr int stream_per_sm(int D) { return D == 64 ? 3 : D == 128 ? 2 : 1; }
 
 template <typename T, int D, int WM>
-__global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(const Args a, const Line w, const __grid_constant__ Pages maps) {
+__global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(const Args a, const Line w, const Line prefix, const __grid_constant__ Pages maps) {
   using R = Ring<D, WM>;
   constexpr int WK = WARPS / WM, ROWS = 16 * WM, KW = KEYS / WK, STAGES = R::STAGES, TILE = R::TILE;
   constexpr int CH = D / 8, HALF = KEYS * 128, QHALF = ROWS * 128;  // a tile's and the queries' 64 columns: rows of 128 bytes
@@ -203,8 +240,9 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
   unsigned char *const qs = ring + STAGES * 2 * TILE;
   float2 *const stat = (float2 *)(qs + STAGES * R::QUERIES);        // [64]: maximum and sum of each warp's rows
   uint64_t *const bars = (uint64_t *)(stat + 64);
-  int64_t *const found = (int64_t *)(bars + 2 * STAGES + 1);        // [5]; the last is the flag
-  volatile int *const dead = (volatile int *)(found + 5);
+  int64_t *const found = (int64_t *)(bars + 2 * STAGES + 1);        // [4]
+  int *const nonempty = (int *)(found + 4);                         // [4]
+  volatile int *const dead = (volatile int *)(nonempty + 4);
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t ring_at = smem_u32(ring), q_at = smem_u32(qs), bar0 = smem_u32(bars);
   auto full = [&](int s) { return bar0 + s * 8; };
@@ -224,13 +262,20 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
   const int each = w.has_own && tid < THREADS ? (a.n_seqs + THREADS - 1) / THREADS : 0;
   const int b_first = min(a.n_seqs, tid * each), b_last = min(a.n_seqs, (tid + 1) * each);
   int64_t mine = 0;
-  for (int b = b_first; b < b_last; b++) mine += (int64_t)tiles_of(own_len(a, b)) * own_pairs;
+  int some = 0;                                        // sequences with keys of their own
+  for (int b = b_first; b < b_last; b++) {
+    const int n = tiles_of(own_len(a, b));
+    mine += (int64_t)n * own_pairs;
+    some += n > 0;
+  }
   int64_t upto = mine;
   for (int o = 1; o < 32; o *= 2) {
     const int64_t x = __shfl_up_sync(~0u, upto, o);
     if (lane >= o) upto += x;
   }
   if (lane == 31 && warp < WARPS) found[warp] = upto;
+  some = __reduce_add_sync(~0u, some);
+  if (lane == 0 && warp < WARPS) nonempty[warp] = some;
   __syncthreads();
   int64_t base = prefix_units, total = prefix_units;
   for (int x = 0; x < WARPS; x++) {
@@ -238,7 +283,12 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
     total += found[x];
   }
   base += upto - mine;                                 // first unit of sequence b_first
-  const int64_t per = quotient(total + w.blocks - 1, w.blocks);
+  int blocks = w.blocks;
+  if (w.beside_prefix) {
+    const int64_t pairs = (int64_t)(nonempty[0] + nonempty[1] + nonempty[2] + nonempty[3]) * own_pairs;
+    blocks = min(blocks, stream_per_sm(D) * (SMS - prefix_sms(a, prefix, total, pairs)));
+  }
+  const int64_t per = quotient(total + blocks - 1, max(blocks, 1));
   const int64_t u0 = per * blockIdx.x, u1 = min(total, u0 + per);
   __syncthreads();
   if (blockIdx.x == 0 && tid < THREADS) {
@@ -249,7 +299,11 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
     }
     if (tid == 0) w.starts[a.n_seqs] = total, w.starts[a.n_seqs + 1] = per;
   }
-  if (u0 >= u1) return;
+  if (u0 >= u1) {
+    // the kernel after this one waits for this one alone: so this one ends after the one before it
+    if (blockIdx.x == 0) wait_for_kernels_before();
+    return;
+  }
   if (u0 >= prefix_units && u0 >= base && u0 < base + mine) {
     int64_t at = base;
     int b = b_first;
@@ -654,8 +708,10 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
       next();
     }
   }
+  dependents_may_start();
   __syncthreads();
   if (*dead && tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
+  if (blockIdx.x == 0) wait_for_kernels_before();
 }
 
 // ---------------------------------------------------------------- the prefix on the tensor cores
@@ -708,31 +764,28 @@ constexpr uint32_t OPERAND_HI = 1024 >> 4 | 1u << 14 | 2u << 29;
 // The rows of all sequences against the prefix.  A block holds 2 x 128 rows of one key head and passes along its stretch of
 // the keys in tiles of 128, each read once for all rows:
 //   warp 9 brings tiles of keys and values from their pages by TMA into a ring;
-//   warp 8 issues the products: scores S = Q K^T to tensor memory, O += P V with P from tensor memory;
+//   warps 8 and 10 issue the products, each for one half of the rows: scores S = Q K^T to tensor memory, O += P V with P
+//   from tensor memory;
 //   warps 0..3 and 4..7 take one half of the rows each, one row a thread: maximum, weights, sum.  P overwrites S.
 // The halves alternate: while one turns scores into weights, the tensor cores work for the other.  The maximum that scores
 // are taken against is raised, and what was summed rescaled, only when it has grown by more than 8 (in log 2): weights stay
 // below 2^8, sums are exact in the same way, and the result is the same up to rounding.
 // Weights are rounded to the values' type for their product; the sum is of the unrounded ones, all else is in 32 bits.
-constexpr int TC_KEYS = 128, TC_THREADS = 384;  // warps 10 and 11 fill up the third warpgroup
+constexpr int TC_KEYS = 128, TC_THREADS = 352;
 constexpr float RAISE = 8.f;
 template <int D> struct Tc {
   static constexpr int TILE = TC_KEYS * D * 2, STAGES = D == 64 ? 8 : 5, Q = 2 * 128 * D * 2;
   static constexpr int SMEM = Q + STAGES * TILE + 1024 /* alignment */ + 256 /* barriers */;
 };
 
-// 384 threads start with 168 registers each (64512): the row threads go on with 216 (55296), the rest with 56 (7168).
-#define MORE_REGISTERS() asm volatile("setmaxnreg.inc.sync.aligned.u32 216;")
-#define FEWER_REGISTERS() asm volatile("setmaxnreg.dec.sync.aligned.u32 56;")
-
 template <typename T, int D>
-__global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Line w, const __grid_constant__ Pages maps, const uint32_t flip) {
+__global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Line w, const int own_rows, const __grid_constant__ Pages maps, const uint32_t flip) {
   constexpr int TILE = Tc<D>::TILE, STAGES = Tc<D>::STAGES, HALF = TC_KEYS * 128;   // 64 columns of a tile
   extern __shared__ unsigned char smem_raw[];
   unsigned char *const smem = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   unsigned char *const qs = smem, *const ring = smem + Tc<D>::Q;
   uint64_t *const bars = (uint64_t *)(ring + STAGES * TILE);
-  uint32_t *const tmem_at = (uint32_t *)(bars + 2 * STAGES + 7);
+  uint32_t *const tmem_at = (uint32_t *)(bars + 2 * STAGES + 10);
   volatile int *const dead = (volatile int *)(tmem_at + 1);
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), q_at = smem_u32(qs), ring_at = smem_u32(ring);
@@ -740,12 +793,30 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   auto empty = [&](int s) { return bar0 + (STAGES + s) * 8; };
   auto q_full = [&](int h) { return bar0 + (2 * STAGES + h) * 8; };
   auto s_full = [&](int h) { return bar0 + (2 * STAGES + 2 + h) * 8; };
-  auto p_full = [&](int h) { return bar0 + (2 * STAGES + 4 + h) * 8; };
-  const uint32_t ended = bar0 + (2 * STAGES + 6) * 8;
+  auto p_full = [&](int h, int q) { return bar0 + (2 * STAGES + 4 + h * 2 + q) * 8; };  // of half the keys
+  const uint32_t ended = bar0 + (2 * STAGES + 8) * 8;
+  dependents_may_start();                              // the sequences' own keys need nothing from here
+  __shared__ unsigned long long own[2];                // tiles, sequences that have any
+  if (tid < 2) own[tid] = 0;
+  __syncthreads();
+  const int own_pairs = a.kv_heads * ((a.n_new * a.group + own_rows - 1) / own_rows);
+  int64_t tiles = 0, some = 0;
+  for (int b = tid; b < a.n_seqs; b += TC_THREADS) {
+    const int x = tiles_of(own_len(a, b));
+    tiles += (int64_t)x * own_pairs;
+    some += x > 0;
+  }
+  if (tiles) atomicAdd(&own[0], (unsigned long long)tiles), atomicAdd(&own[1], (unsigned long long)some * own_pairs);
+  __syncthreads();
+  const int blocks = prefix_sms(a, w, own[0], own[1]);
+  const int n = tiles_of(a.prefix_len, TC_KEYS);
+  const int64_t units = (int64_t)n * a.kv_heads * w.prefix_tiles, per = quotient(units + blocks - 1, blocks);
+  const int64_t u0 = per * blockIdx.x, u1 = min(units, u0 + per);
+  if (blockIdx.x == 0 && tid == 0) w.starts[a.n_seqs + 1] = per;
+  if (u0 >= u1) return;
   if (tid == 0) {
-    bar_init(ended, 1);
-    for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(empty(s), 1);
-    for (int h = 0; h < 2; h++) bar_init(q_full(h), 128), bar_init(s_full(h), 1), bar_init(p_full(h), 128);
+    for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(empty(s), 2);
+    for (int h = 0; h < 2; h++) bar_init(ended + 8 * h, 1), bar_init(q_full(h), 128), bar_init(s_full(h), 1), bar_init(p_full(h, 0), 128), bar_init(p_full(h, 1), 128);
     *dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -760,12 +831,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   auto scores = [&](int h) { return tmem + h * 128; };
   auto sums = [&](int h) { return tmem + 256 + h * 128; };
 
-  const int n = tiles_of(a.prefix_len, TC_KEYS);
-  const int64_t u0 = w.per * blockIdx.x, u1 = min((int64_t)n * a.kv_heads * w.prefix_tiles, u0 + w.per);
   const int all = a.n_seqs * a.n_new * a.group;
 
   if (warp >= 8) {
-    FEWER_REGISTERS();
     if (warp == 9) {
       // ---- keys and values: lane x brings the x-th box of tokens of a tile, both of its 64-value halves
       const int boxes = TC_KEYS / maps.box;
@@ -807,35 +875,46 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
         for (int x = first; x < it; x++)
           while (!bar_try(full(x % STAGES), (x / STAGES) & 1) && now_ns() - from < LIMIT_NS) {}
       }
-    } else if (warp == 8 && elected()) {
-      // ---- products, from one thread
+    } else if (warp != 9 && elected()) {
+      // ---- products, from one thread for each half of the rows (one thread for both would set the time)
       constexpr uint32_t TYPE = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
       constexpr uint32_t COMMON = 1u << 4 | TYPE << 7 | TYPE << 10 | (128u >> 4) << 24;
       constexpr uint32_t QK = COMMON | (TC_KEYS >> 3) << 17, PV = COMMON | 1u << 16 | (D >> 3) << 17;
-      const uint32_t q_op = operand(q_at, 16), k_op = operand(ring_at, 16), v_op = operand(ring_at, HALF);
+      const int h = warp == 10;
+      const uint32_t k_op = operand(ring_at, 16), v_op = operand(ring_at, HALF), q_op = operand(q_at + h * (Tc<D>::Q / 2), 16);
+      const uint32_t s_at = scores(h), o_at = sums(h);
       int stage = 0;                                       // of the ring
-      uint32_t lap = 0, seg[2] = {0, 0}, turn[2] = {0, 0}; // laps of the ring; each half's pairs and tiles so far
+      uint32_t lap = 0, seg = 0, turn = 0;                 // laps of the ring; this half's pairs and tiles so far
       bool alive = true;
       auto need = [&](uint32_t bar, uint32_t parity) { alive = alive && bar_wait(bar, parity & 1, dead); };
       auto next = [&] {
         if (++stage == STAGES) stage = 0, lap++;
       };
-      auto qk = [&](int h, int s) {
+      auto qk = [&](int s) {
+        uint32_t q = q_op, k = k_op + ((s * TILE) >> 4);
 #pragma unroll
-        for (int k = 0; k < D / 16; k++)
-          tc_mma(scores(h), q_op + ((h * (Tc<D>::Q / 2) + k / 4 * HALF + k % 4 * 32) >> 4),
-                 k_op + ((s * TILE + k / 4 * HALF + k % 4 * 32) >> 4), OPERAND_HI, QK, k > 0);
+        for (int x = 0; x < D / 64; x++, q += HALF >> 4, k += HALF >> 4) {
+#pragma unroll
+          for (int y = 0; y < 4; y++) tc_mma(s_at, q + 2 * y, k + 2 * y, OPERAND_HI, QK, x + y > 0);
+        }
         tc_commit(s_full(h));
+        tc_commit(empty(s));
       };
       for (int64_t u = u0; u < u1 && alive;) {
         const int pair = (int)(u / n), tile0 = (int)(u - (int64_t)pair * n), count = (int)min((int64_t)(n - tile0), u1 - u);
-        const int halves = all - pair % w.prefix_tiles * 256 > 128 ? 2 : 1;
-        for (int h = 0; h < halves; h++) need(q_full(h), seg[h]++);
+        u += count;
+        if (all - pair % w.prefix_tiles * 256 <= h * 128) {  // no rows for this half: the tiles pass by
+          for (int x = 0; x < 2 * count && alive; x++, next()) {
+            need(full(stage), lap);
+            bar_arrive(empty(stage));
+          }
+          continue;
+        }
+        need(q_full(h), seg++);
         need(full(stage), lap);
         if (!alive) break;
         tc_after();
-        for (int h = 0; h < halves; h++) qk(h, stage);
-        tc_commit(empty(stage));
+        qk(stage);
         next();
         for (int j = 0; j < count; j++) {
           // this tile's values and the next one's keys, while the rows make their weights
@@ -854,43 +933,31 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
             }
             fence_async();
           }
+          const uint32_t v = v_op + ((sv * TILE) >> 4);
 #pragma unroll
-          for (int h = 0; h < 2; h++) {
-            if (h < halves) {
-              need(p_full(h), turn[h]++);
-              if (!alive) break;
-              tc_after();
-              if (nv >= TC_KEYS) {
+          for (int q = 0; q < 2; q++) {
+            need(p_full(h, q), turn);
+            if (!alive) break;
+            tc_after();
 #pragma unroll
-                for (int k = 0; k < TC_KEYS / 16; k++)
-                  tc_mma_t(sums(h), scores(h) + k * 8, v_op + ((sv * TILE + k * 2048) >> 4), OPERAND_HI, PV, j > 0 || k > 0);
-              } else {
-#pragma unroll 1
-                for (int k = 0; k * 16 < nv; k++)
-                  tc_mma_t(sums(h), scores(h) + k * 8, v_op + ((sv * TILE + k * 2048) >> 4), OPERAND_HI, PV, j > 0 || k > 0);
-              }
-              if (h == halves - 1) tc_commit(empty(sv));
-              if (j + 1 < count) {
-                qk(h, sk);
-                if (h == halves - 1) tc_commit(empty(sk));
-              } else {
-                tc_commit(s_full(h));                      // the pair's sums are complete
-              }
-            }
+            for (int k = 4 * q; k < 4 * q + 4; k++)
+              if (k * 16 < nv) tc_mma_t(o_at, s_at + k * 8, v + k * (2048 >> 4), OPERAND_HI, PV, j + k > 0);
           }
+          turn++;
           if (!alive) break;
+          tc_commit(empty(sv));
+          if (j + 1 < count) qk(sk);
+          else tc_commit(s_full(h));                       // the pair's sums are complete
         }
-        u += count;
       }
       if (!alive) {                                        // products in flight end before the block does
-        tc_commit(ended);
+        tc_commit(ended + 8 * h);
         const uint64_t from = now_ns();
-        while (!bar_try(ended, 0) && now_ns() - from < LIMIT_NS) {}
+        while (!bar_try(ended + 8 * h, 0) && now_ns() - from < LIMIT_NS) {}
       }
     }
   } else {
     // ---- one row a thread
-    MORE_REGISTERS();
     const int h = warp / 4, r = tid % 128;
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
     const float sl2 = fabsf(a.scale) * 1.4426950408889634f;
@@ -930,22 +997,31 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
         alive = __all_sync(~0u, bar_wait(s_full(h), turn & 1, dead));
         if (!alive) break;
         tc_after();
-        uint32_t s[TC_KEYS];
-#pragma unroll
-        for (int c = 0; c < 4; c++) tc_ld(s + c * 32, scores(h) + lanes + c * 32);
-        tc_ld_wait();
         const int nv = a.prefix_len - (tile0 + j) * TC_KEYS;
-        if (nv < TC_KEYS) {
+        // Half of the scores at a time, and tensor memory read again for the weights: all 128 in registers would spill, and
+        // shorter pieces add their latencies.
+        uint32_t s[64];
+        auto fetch = [&](int c) {
+          tc_ld(s, scores(h) + lanes + c);
+          tc_ld(s + 32, scores(h) + lanes + c + 32);
+          tc_ld_wait();
+          if (c + 64 > nv) {
 #pragma unroll
-          for (int c = 0; c < TC_KEYS; c++)
-            if (c >= nv) s[c] = 0xFF800000u;             // -infinity
+            for (int x = 0; x < 64; x++)
+              if (c + x >= nv) s[x] = 0xFF800000u;       // -infinity
+          }
+        };
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int q = 0; q < 2; q++) {
+          fetch(q * 64);
+#pragma unroll
+          for (int c = 0; c < 64; c += 8) {
+#pragma unroll
+            for (int x = 0; x < 4; x++) top[x] = max3(top[x], __uint_as_float(s[c + 2 * x]), __uint_as_float(s[c + 2 * x + 1]));
+          }
         }
-        float top[4];
-#pragma unroll
-        for (int c = 0; c < 4; c++) top[c] = __uint_as_float(s[c]);
-#pragma unroll
-        for (int c = 4; c < TC_KEYS; c++) top[c & 3] = fmaxf(top[c & 3], __uint_as_float(s[c]));
-        const float big = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * sl2;
+        const float big = fmaxf(max3(top[0], top[1], top[2]), top[3]) * sl2;
         const bool raise = big > m + RAISE || (m == -INFINITY && big > m);
         if (j == 0) {
           m = big;
@@ -964,21 +1040,26 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
           m = to;
         }
         const float from = m == -INFINITY ? 0.f : m;
-        uint32_t pk[TC_KEYS / 2];
-        float part[4] = {};
+        const float2 scale2 = make_float2(sl2, sl2), from2 = make_float2(-from, -from);
+        float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-        for (int c = 0; c < TC_KEYS; c += 2) {
-          const float x = exp2_fast(fmaf(__uint_as_float(s[c]), sl2, -from));
-          const float y = exp2_fast(fmaf(__uint_as_float(s[c + 1]), sl2, -from));
-          part[c & 2] += x, part[(c & 2) + 1] += y;
-          pk[c / 2] = pack<T>(x, y);
+        for (int q = 0; q < 2; q++) {                    // the products with the first 64 weights start under the others
+          uint32_t pk[32];
+          fetch(q * 64);
+#pragma unroll
+          for (int c = 0; c < 64; c += 2) {
+            float2 x = fma2(make_float2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), scale2, from2);
+            x.x = exp2_fast(x.x), x.y = exp2_fast(x.y);
+            part[c / 2 & 1] = add2(part[c / 2 & 1], x);
+            pk[c / 2] = pack<T>(x.x, x.y);
+          }
+          tc_st(scores(h) + lanes + q * 32, pk);
+          tc_st_wait();
+          tc_before();
+          bar_arrive(p_full(h, q));
         }
-        tc_st(scores(h) + lanes, pk);
-        tc_st(scores(h) + lanes + 32, pk + 32);
-        tc_st_wait();
-        tc_before();
-        bar_arrive(p_full(h));
-        l += (part[0] + part[1]) + (part[2] + part[3]);
+        const float2 both = add2(part[0], part[1]);
+        l += both.x + both.y;
       }
       if (!alive) break;
       alive = __all_sync(~0u, bar_wait(s_full(h), turn & 1, dead));
@@ -1021,6 +1102,7 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
   const int lane = threadIdx.x % 32;
   const int64_t row = (int64_t)blockIdx.x * WARPS + threadIdx.x / 32;
   if (row >= (int64_t)a.n_seqs * a.n_new * a.q_heads) return;
+  wait_for_kernels_before();
   const int64_t token = quotient(row, a.q_heads), seq = quotient(token, a.n_new);
   const int h = (int)(row - token * a.q_heads), i = (int)(token - seq * a.n_new), b = (int)seq;
   const int kh = h / a.group;
@@ -1029,7 +1111,7 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
   auto parts = [&](const Line &w, int r, int tiles, int64_t start, int n) {
     Parts p = {0, 0, 0, 0, 0, false};
     if (n) {
-      p.per = w.per ? w.per : w.starts[a.n_seqs + 1];
+      p.per = w.starts[a.n_seqs + 1];
       p.u0 = start + (int64_t)(kh * tiles + r / w.rows) * n;
       p.r = r % w.rows;
       p.c0 = quotient(p.u0, p.per);
@@ -1110,8 +1192,6 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
 }
 
 // ---------------------------------------------------------------- host side
-constexpr int SMS = 152;
-
 // A kernel's shared memory above 48 KB is granted once per device.
 template <typename K> cudaError_t grant(K kernel, int bytes, std::atomic<uint64_t> &granted) {
   int dev = 0;
@@ -1167,8 +1247,7 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
   if (p.way == APART) line(p.prefix, 64, KEYS, stream_blocks(D), true, false);
   if (p.way == TENSOR) {
     line(p.prefix, 256, TC_KEYS, SMS, true, false);
-    const int64_t units = (int64_t)tiles_of((int)d.prefix_len, TC_KEYS) * d.cache.kv_heads * p.prefix.prefix_tiles;
-    p.prefix.per = (units + SMS - 1) / SMS;
+    p.own.beside_prefix = 1;
   }
   if (p.way == TOGETHER) p.prefix = p.own;
   if (d.prefix_len) {
@@ -1232,42 +1311,47 @@ bool tile_maps(Pages &p, const gts_cache &c) {
   return ok;
 }
 
+// A launch that may start as soon as the kernel before it allows (`early`): the kernels above wait for each other themselves.
+template <typename... P, typename... A>
+cudaError_t launch_kernel(void (*kernel)(P...), unsigned blocks, unsigned threads, int shared, cudaStream_t s, bool early, const A &...args) {
+  cudaLaunchAttribute attr = {};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t c = {};
+  c.gridDim = dim3(blocks), c.blockDim = dim3(threads), c.dynamicSmemBytes = (size_t)shared, c.stream = s;
+  c.attrs = &attr, c.numAttrs = early ? 1 : 0;
+  return cudaLaunchKernelEx(&c, kernel, args...);
+}
+
 template <typename T, int D, int WM>
-cudaError_t stream(const Args &a, const Line &w, const Pages &maps, cudaStream_t s) {
-  constexpr int bytes = Ring<D, WM>::SMEM;
+cudaError_t stream(const Args &a, const Line &w, const Line &prefix, const Pages &maps, bool early, cudaStream_t s) {
   static std::atomic<uint64_t> granted{0};
-  const cudaError_t e = grant(k_stream<T, D, WM>, bytes, granted);
-  if (e != cudaSuccess) return e;
-  k_stream<T, D, WM><<<w.blocks, STREAM_THREADS, bytes, s>>>(a, w, maps);
-  return cudaGetLastError();
+  const cudaError_t e = grant(k_stream<T, D, WM>, Ring<D, WM>::SMEM, granted);
+  return e != cudaSuccess ? e : launch_kernel(k_stream<T, D, WM>, w.blocks, STREAM_THREADS, Ring<D, WM>::SMEM, s, early, a, w, prefix, maps);
 }
 
 template <typename T, int D>
-cudaError_t stream(const Args &a, const Line &w, const Pages &maps, cudaStream_t s) {
-  return w.rows == 16 ? stream<T, D, 1>(a, w, maps, s) : w.rows == 32 ? stream<T, D, 2>(a, w, maps, s) : stream<T, D, 4>(a, w, maps, s);
-}
-
-template <typename T, int D>
-cudaError_t tensor(const Args &a, const Line &w, const Pages &maps, cudaStream_t s) {
+cudaError_t tensor(const Args &a, const Line &w, int own_rows, const Pages &maps, cudaStream_t s) {
   static std::atomic<uint64_t> granted{0};
   const cudaError_t e = grant(k_prefix<T, D>, Tc<D>::SMEM, granted);
-  if (e != cudaSuccess) return e;
-  k_prefix<T, D><<<w.blocks, TC_THREADS, Tc<D>::SMEM, s>>>(a, w, maps, a.scale < 0 ? 0x80008000u : 0u);
-  return cudaGetLastError();
+  return e != cudaSuccess ? e : launch_kernel(k_prefix<T, D>, w.blocks, TC_THREADS, Tc<D>::SMEM, s, false, a, w, own_rows, maps, a.scale < 0 ? 0x80008000u : 0u);
 }
 
 template <typename T, int D>
 cudaError_t run(const Args &a, const Plan &p, const Pages &maps, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
-  if (p.way == APART) e = stream<T, D, 4>(a, p.prefix, maps, s);
+  if (p.way == APART) e = stream<T, D, 4>(a, p.prefix, p.prefix, maps, false, s);
   if constexpr (D <= 128) {
-    if (p.way == TENSOR) e = tensor<T, D>(a, p.prefix, maps, s);
+    if (p.way == TENSOR) e = tensor<T, D>(a, p.prefix, p.own.rows, maps, s);
   }
-  if (e == cudaSuccess) e = stream<T, D>(a, p.own, maps, s);
+  if (e != cudaSuccess) return e;
+  const bool early = p.way != TOGETHER;
+  e = p.own.rows == 16   ? stream<T, D, 1>(a, p.own, p.prefix, maps, early, s)
+      : p.own.rows == 32 ? stream<T, D, 2>(a, p.own, p.prefix, maps, early, s)
+                         : stream<T, D, 4>(a, p.own, p.prefix, maps, early, s);
   if (e != cudaSuccess) return e;
   const int64_t rows = (int64_t)a.n_seqs * a.n_new * a.q_heads;
-  k_join<T, D><<<(unsigned)((rows + WARPS - 1) / WARPS), THREADS, 0, s>>>(a, p.prefix, p.own);
-  return cudaGetLastError();
+  return launch_kernel(k_join<T, D>, (unsigned)((rows + WARPS - 1) / WARPS), THREADS, 0, s, true, a, p.prefix, p.own);
 }
 
 template <typename T>
