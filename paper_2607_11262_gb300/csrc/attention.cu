@@ -181,10 +181,10 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
 
 // The prefix's kernel is bound by the tensor cores and holds whole SMs, the sequences' own keys are bound by memory: both run
 // at the same time, on SMs dealt out by the time each needs.  In units of an own tile's time on an SM (0.55 us measured at a
-// head of 128): a tile of the prefix for 256 rows takes 4 (2.3 us), the end of a pair 1.3; and own tiles alone cannot go
+// head of 128): a tile of the prefix for 256 rows takes 3.2 (1.75 us), the end of a pair 2.5; and own tiles alone cannot go
 // faster than memory brings them, 104 to that time.  Both kernels come to the same numbers from the lengths.
 __device__ __forceinline__ int prefix_sms(const Args &a, const Line &prefix, int64_t own_tiles, int64_t own_pairs) {
-  const float p = 4.f * tiles_of(a.prefix_len, 128) * a.kv_heads * prefix.prefix_tiles, o = own_tiles + 1.3f * own_pairs;
+  const float p = 3.2f * tiles_of(a.prefix_len, 128) * a.kv_heads * prefix.prefix_tiles, o = own_tiles + 2.5f * own_pairs;
   if (own_tiles == 0) return SMS;
   const float each = fmaxf((p + o) / SMS, own_tiles / 104.f);
   return max(1, min(SMS - 1, (int)(p / each + 0.5f)));
@@ -785,7 +785,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   unsigned char *const smem = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   unsigned char *const qs = smem, *const ring = smem + Tc<D>::Q;
   uint64_t *const bars = (uint64_t *)(ring + STAGES * TILE);
-  uint32_t *const tmem_at = (uint32_t *)(bars + 2 * STAGES + 10);
+  uint32_t *const tmem_at = (uint32_t *)(bars + 2 * STAGES + 12);
   volatile int *const dead = (volatile int *)(tmem_at + 1);
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), q_at = smem_u32(qs), ring_at = smem_u32(ring);
@@ -795,20 +795,22 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   auto s_full = [&](int h) { return bar0 + (2 * STAGES + 2 + h) * 8; };
   auto p_full = [&](int h, int q) { return bar0 + (2 * STAGES + 4 + h * 2 + q) * 8; };  // of half the keys
   const uint32_t ended = bar0 + (2 * STAGES + 8) * 8;
+  auto my_turn = [&](int h) { return bar0 + (2 * STAGES + 10 + h) * 8; };
   dependents_may_start();                              // the sequences' own keys need nothing from here
-  __shared__ unsigned long long own[2];                // tiles, sequences that have any
-  if (tid < 2) own[tid] = 0;
-  __syncthreads();
-  const int own_pairs = a.kv_heads * ((a.n_new * a.group + own_rows - 1) / own_rows);
-  int64_t tiles = 0, some = 0;
+  __shared__ int own[TC_THREADS / 32][2];              // of each warp: sequences' tiles, sequences that have any
+  int tiles = 0, some = 0;
   for (int b = tid; b < a.n_seqs; b += TC_THREADS) {
     const int x = tiles_of(own_len(a, b));
-    tiles += (int64_t)x * own_pairs;
+    tiles += x;
     some += x > 0;
   }
-  if (tiles) atomicAdd(&own[0], (unsigned long long)tiles), atomicAdd(&own[1], (unsigned long long)some * own_pairs);
+  tiles = __reduce_add_sync(~0u, tiles), some = __reduce_add_sync(~0u, some);
+  if (lane == 0) own[warp][0] = tiles, own[warp][1] = some;
   __syncthreads();
-  const int blocks = prefix_sms(a, w, own[0], own[1]);
+  int64_t own_tiles = 0, own_pairs = 0;
+  for (int x = 0; x < TC_THREADS / 32; x++) own_tiles += own[x][0], own_pairs += own[x][1];
+  const int pairs_each = a.kv_heads * ((a.n_new * a.group + own_rows - 1) / own_rows);
+  const int blocks = prefix_sms(a, w, own_tiles * pairs_each, own_pairs * pairs_each);
   const int n = tiles_of(a.prefix_len, TC_KEYS);
   const int64_t units = (int64_t)n * a.kv_heads * w.prefix_tiles, per = quotient(units + blocks - 1, blocks);
   const int64_t u0 = per * blockIdx.x, u1 = min(units, u0 + per);
@@ -816,7 +818,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   if (u0 >= u1) return;
   if (tid == 0) {
     for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(empty(s), 2);
-    for (int h = 0; h < 2; h++) bar_init(ended + 8 * h, 1), bar_init(q_full(h), 128), bar_init(s_full(h), 1), bar_init(p_full(h, 0), 128), bar_init(p_full(h, 1), 128);
+    for (int h = 0; h < 2; h++) bar_init(ended + 8 * h, 1), bar_init(my_turn(h), 1), bar_init(q_full(h), 128), bar_init(s_full(h), 1), bar_init(p_full(h, 0), 128), bar_init(p_full(h, 1), 128);
     *dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -839,17 +841,21 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
       const int boxes = TC_KEYS / maps.box;
       int it = 0;
       bool alive = true;
+      int pair = (int)quotient(u0, n), tile = (int)(u0 - (int64_t)pair * n), kh = pair / w.prefix_tiles;
+      auto look_up = [&](int t) {                          // this lane's page of tile t; -1: none
+        const int key = t * TC_KEYS + lane * maps.box;
+        return lane < boxes && key < a.prefix_len ? a.prefix_pages[key / a.page_size] & 0x7FFFFFFF : -1;
+      };
+      int page_next = look_up(tile);
       for (int64_t u = u0; u < u1 && alive; u++) {
-        const int pair = (int)(u / n), tile = (int)(u - (int64_t)pair * n), kh = pair / w.prefix_tiles;
-        const int key = tile * TC_KEYS + lane * maps.box;
-        const bool live = lane < boxes && key < a.prefix_len;
-        int page = 0;
-        if (live) {
-          page = a.prefix_pages[key / a.page_size];
-          if (page < 0 || page >= a.n_pages) {             // outside the map: the box is filled with zeros
-            page = a.n_pages;
-            if (a.status) *a.status = GTS_ERR_INVALID_PARAMS;
-          }
+        const int key = tile * TC_KEYS + lane * maps.box, head = kh;
+        int page = page_next;
+        const bool live = page >= 0;
+        if (++tile == n) tile = 0, kh = ++pair / w.prefix_tiles;
+        if (u + 1 < u1) page_next = look_up(tile);         // arrives while this tile waits for room
+        if (page >= a.n_pages) {                           // (a negative number has become a large one)
+          page = a.n_pages;                                // outside the map: the box is filled with zeros
+          if (a.status) *a.status = GTS_ERR_INVALID_PARAMS;
         }
         const uint32_t bytes = __popc(__ballot_sync(~0u, live)) * maps.box * D * 2;
         for (int kv = 0; kv < 2; kv++, it++) {
@@ -864,8 +870,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
             const int token = key % a.page_size;
 #pragma unroll
             for (int x = 0; x < D / 64; x++)
-              tile_load(ring_at + s * TILE + x * HALF + lane * maps.box * 128, kv ? &maps.v : &maps.k, x * 64, heads_first ? kh : token,
-                        heads_first ? token : kh, page, full(s));
+              tile_load(ring_at + s * TILE + x * HALF + lane * maps.box * 128, kv ? &maps.v : &maps.k, x * 64, heads_first ? head : token,
+                        heads_first ? token : head, page, full(s));
           }
         }
       }
@@ -884,7 +890,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
       const uint32_t k_op = operand(ring_at, 16), v_op = operand(ring_at, HALF), q_op = operand(q_at + h * (Tc<D>::Q / 2), 16);
       const uint32_t s_at = scores(h), o_at = sums(h);
       int stage = 0;                                       // of the ring
-      uint32_t lap = 0, seg = 0, turn = 0;                 // laps of the ring; this half's pairs and tiles so far
+      uint32_t lap = 0, seg = 0, turn = 0, turns = 0;      // laps of the ring; this half's pairs and tiles so far, and turns
       bool alive = true;
       auto need = [&](uint32_t bar, uint32_t parity) { alive = alive && bar_wait(bar, parity & 1, dead); };
       auto next = [&] {
@@ -910,6 +916,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
           }
           continue;
         }
+        const bool both = all - pair % w.prefix_tiles * 256 > 128;
         need(q_full(h), seg++);
         need(full(stage), lap);
         if (!alive) break;
@@ -937,6 +944,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
 #pragma unroll
           for (int q = 0; q < 2; q++) {
             need(p_full(h, q), turn);
+            // The halves take turns, each with all its products for a tile: left alone they fall into step, and the tensor
+            // cores wait while both make weights (3300 against 2600 cycles a tile)
+            if (q == 0 && both) need(my_turn(h), h ? turns : turns - 1), turns++;
             if (!alive) break;
             tc_after();
 #pragma unroll
@@ -948,6 +958,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
           tc_commit(empty(sv));
           if (j + 1 < count) qk(sk);
           else tc_commit(s_full(h));                       // the pair's sums are complete
+          if (both) bar_arrive(my_turn(!h));
         }
       }
       if (!alive) {                                        // products in flight end before the block does
@@ -972,22 +983,26 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
         continue;
       }
       const Row p = row_of(a, -1, kh, row);
-      const T *src = (const T *)a.q + p.b * a.q_seq + p.i * a.q_tok + p.h * a.q_head;
-#pragma unroll
-      for (int c = 0; c < D / 8; c++) {
+      // queries: the warp takes its 32 rows together, lanes along them
+      const unsigned long long src = row < all ? (unsigned long long)((const T *)a.q + p.b * a.q_seq + p.i * a.q_tok + p.h * a.q_head) : 0;
+#pragma unroll 8
+      for (int x = lane; x < 32 * (D / 8); x += 32) {
+        const int y = x / (D / 8), c = x % (D / 8), at = warp % 4 * 32 + y;
+        const T *from = (const T *)__shfl_sync(~0u, src, y);
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (row < all) {
+        if (from) {
+          from += c * 8;
           if (q_aligned) {
-            v = *(const uint4 *)(src + c * 8);
+            v = *(const uint4 *)from;
           } else {
             T e[8];
 #pragma unroll
-            for (int x = 0; x < 8; x++) e[x] = src[c * 8 + x];
+            for (int z = 0; z < 8; z++) e[z] = from[z];
             memcpy(&v, e, 16);
           }
           v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;   // a negative scale: its sign goes to the queries
         }
-        *(uint4 *)(qs + h * (Tc<D>::Q / 2) + c / 8 * HALF + r * 128 + ((c % 8) ^ (r & 7)) * 16) = v;
+        *(uint4 *)(qs + h * (Tc<D>::Q / 2) + c / 8 * HALF + at * 128 + ((c % 8) ^ (at & 7)) * 16) = v;
       }
       fence_async();
       bar_arrive(q_full(h));
@@ -1069,16 +1084,27 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
       const bool whole = count == n;
       const int64_t at = whole ? ((int64_t)p.b * a.n_new + p.i) * a.q_heads + p.h
                                : ((int64_t)blockIdx.x * 2 + (u > u0)) * 256 + h * 128 + r;
-      float *to = (whole ? w.whole_o[0] : w.cut_o) + at * D;
+      // the sums, 32 columns at a time, through the warp's part of the queries' room (all products with them are done), so
+      // that a store covers whole lines
+      const unsigned long long to = row < all ? (unsigned long long)((whole ? w.whole_o[0] : w.cut_o) + at * D) : 0;
+      unsigned char *const room = qs + h * (Tc<D>::Q / 2) + warp % 4 * 4096;
 #pragma unroll 1
       for (int c = 0; c < D / 32; c++) {
         uint32_t o[32];
         tc_ld(o, sums(h) + lanes + c * 32);
         tc_ld_wait();
-        if (row < all) {
 #pragma unroll
-          for (int x = 0; x < 32; x += 4) *(uint4 *)(to + c * 32 + x) = make_uint4(o[x], o[x + 1], o[x + 2], o[x + 3]);
+        for (int x = 0; x < 8; x++)
+          *(uint4 *)(room + lane * 128 + (x ^ (lane & 7)) * 16) = make_uint4(o[4 * x], o[4 * x + 1], o[4 * x + 2], o[4 * x + 3]);
+        __syncwarp();
+#pragma unroll
+        for (int x = 0; x < 8; x++) {
+          const int y = x * 4 + lane / 8;
+          float *dst = (float *)__shfl_sync(~0u, to, y);
+          const uint4 v = *(const uint4 *)(room + y * 128 + ((lane % 8) ^ (y & 7)) * 16);
+          if (dst) *(uint4 *)(dst + c * 32 + lane % 8 * 4) = v;
         }
+        __syncwarp();
       }
       if (row < all) (whole ? w.whole_ml[0] : w.cut_ml)[at] = make_float2(m, l);
       tc_before();
