@@ -144,7 +144,7 @@ template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi)
 }
 
 // ---------------------------------------------------------------- how the work is cut
-// A "pair" is a key head with a tile of up to ROWS query rows that see the same keys: of the prefix, rows of all
+// A "pair" is a key head (or four of them) with a tile of up to ROWS query rows that see the same keys: of the prefix, rows of all
 // sequences (row (b * n_new + i) * group + h of n_seqs * n_new * group); of a sequence's own keys, its n_new * group rows.
 // A pair's keys come in tiles of KEYS, the unit of work.  All units stand in one line (prefix pairs, then the sequences'),
 // and each block takes an equal stretch of it, so ragged lengths cost nothing and the cut needs no plan from the host.
@@ -156,13 +156,13 @@ constexpr int WARPS = 4, THREADS = 32 * WARPS;
 
 struct Line {           // the units of one launch
   int has_prefix, has_own;
-  int rows, keys;       // of a pair's tile, of a unit
+  int heads, rows, keys;  // key heads of a pair, rows of its tile (for each head), keys of a unit
   int beside_prefix;    // the tensor cores' kernel runs at the same time
   int prefix_tiles, own_tiles;   // row tiles of the prefix's rows, of a sequence's rows
   int blocks;
   int64_t *starts;      // [n_seqs + 2]: first unit of each sequence, the units of all, units per block
-  float *cut_o;         // [blocks][2][rows][D]: results of the first and last pair of a block that are cut
-  float2 *cut_ml;       // [blocks][2][rows]: maximum (of log2 scores) and sum
+  float *cut_o;         // [blocks][2][heads][rows][D]: results of the first and last pair of a block that are cut
+  float2 *cut_ml;       // [blocks][2][heads][rows]: maximum (of log2 scores) and sum
   float *whole_o[2];    // [rows of all][D], prefix and own: results of pairs that are not cut
   float2 *whole_ml[2];
 };
@@ -180,11 +180,11 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
 }
 
 // The prefix's kernel is bound by the tensor cores and holds whole SMs, the sequences' own keys are bound by memory: both run
-// at the same time, on SMs dealt out by the time each needs.  In units of an own tile's time on an SM (0.55 us measured at a
-// head of 128): a tile of the prefix for 256 rows takes 3.2 (1.75 us), the end of a pair 2.5; and own tiles alone cannot go
+// at the same time, on SMs dealt out by the time each needs.  In units of an own tile's time on an SM (0.77 us measured at a
+// head of 128): a tile of the prefix for 256 rows takes 2.2 (1.7 us), the end of a pair 2; and own tiles alone cannot go
 // faster than memory brings them, 104 to that time.  Both kernels come to the same numbers from the lengths.
 __device__ __forceinline__ int prefix_sms(const Args &a, const Line &prefix, int64_t own_tiles, int64_t own_pairs) {
-  const float p = 3.2f * tiles_of(a.prefix_len, 128) * a.kv_heads * prefix.prefix_tiles, o = own_tiles + 2.5f * own_pairs;
+  const float p = 2.2f * tiles_of(a.prefix_len, 128) * a.kv_heads * prefix.prefix_tiles, o = own_tiles + 2.f * own_pairs;
   if (own_tiles == 0) return SMS;
   const float each = fmaxf((p + o) / SMS, own_tiles / 104.f);
   return max(1, min(SMS - 1, (int)(p / each + 0.5f)));
@@ -221,19 +221,20 @@ struct Place { int b, len, n, pairs, pair, tile; };
 // ends, to be joined in the stage just read.  Scores and weights stay in the fragments of m16n8k16 products, each warp with
 // its own running maximum and sum.  Weights are rounded to the type of the values for their product with them (the sum is of
 // the unrounded ones); everything else is in 32 bits.
-template <int D, int WM> struct Ring {
+template <int D, int WM, int WH> struct Ring {
   static constexpr int STAGES = (D == 64 ? 4 : 3) - (WM > 1);   // as many as stream_per_sm blocks find room for
   static constexpr int TILE = KEYS * D * 2;                     // bytes of a tile of keys or of values
-  static constexpr int QUERIES = 16 * WM * D * 2;
+  static constexpr int QUERIES = WH > 1 ? 0 : 16 * WM * D * 2;  // with four heads they go straight to registers
   static constexpr int SMEM = 1024 /* alignment */ + STAGES * (2 * TILE + QUERIES) + 64 * 8 + (2 * STAGES + 1) * 8 + 56;
 };
 constexpr int STREAM_THREADS = THREADS + 32;
 __host__ __device__ constexpr int stream_per_sm(int D) { return D == 64 ? 3 : D == 128 ? 2 : 1; }
 
-template <typename T, int D, int WM>
+template <typename T, int D, int WM, int WH>
 __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(const Args a, const Line w, const Line prefix, const __grid_constant__ Pages maps) {
-  using R = Ring<D, WM>;
-  constexpr int WK = WARPS / WM, ROWS = 16 * WM, KW = KEYS / WK, STAGES = R::STAGES, TILE = R::TILE;
+  using R = Ring<D, WM, WH>;
+  static_assert(WH == 1 || (WH == WARPS && WM == 1), "a warp for each head, or all for one");
+  constexpr int WK = WARPS / WM / WH, ROWS = 16 * WM, KU = KEYS / WH, KW = KU / WK, STAGES = R::STAGES, TILE = R::TILE;
   constexpr int CH = D / 8, HALF = KEYS * 128, QHALF = ROWS * 128;  // a tile's and the queries' 64 columns: rows of 128 bytes
   extern __shared__ unsigned char smem_raw[];
   unsigned char *const ring = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -256,15 +257,15 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
   }
 
   // the line of units, and this block's stretch of it
-  const int n_prefix = w.has_prefix ? tiles_of(a.prefix_len) : 0;
-  const int64_t prefix_units = (int64_t)n_prefix * a.kv_heads * w.prefix_tiles;
-  const int own_pairs = a.kv_heads * w.own_tiles;
+  const int n_prefix = w.has_prefix ? tiles_of(a.prefix_len, KU) : 0, head_groups = a.kv_heads / WH;
+  const int64_t prefix_units = (int64_t)n_prefix * head_groups * w.prefix_tiles;
+  const int own_pairs = head_groups * w.own_tiles;
   const int each = w.has_own && tid < THREADS ? (a.n_seqs + THREADS - 1) / THREADS : 0;
   const int b_first = min(a.n_seqs, tid * each), b_last = min(a.n_seqs, (tid + 1) * each);
   int64_t mine = 0;
   int some = 0;                                        // sequences with keys of their own
   for (int b = b_first; b < b_last; b++) {
-    const int n = tiles_of(own_len(a, b));
+    const int n = tiles_of(own_len(a, b), KU);
     mine += (int64_t)n * own_pairs;
     some += n > 0;
   }
@@ -295,7 +296,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
     int64_t at = base;
     for (int b = b_first; b < b_last; b++) {
       w.starts[b] = at;
-      at += (int64_t)tiles_of(own_len(a, b)) * own_pairs;
+      at += (int64_t)tiles_of(own_len(a, b), KU) * own_pairs;
     }
     if (tid == 0) w.starts[a.n_seqs] = total, w.starts[a.n_seqs + 1] = per;
   }
@@ -308,7 +309,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
     int64_t at = base;
     int b = b_first;
     for (;; b++) {
-      const int64_t n = (int64_t)tiles_of(own_len(a, b)) * own_pairs;
+      const int64_t n = (int64_t)tiles_of(own_len(a, b), KU) * own_pairs;
       if (u0 < at + n) break;
       at += n;
     }
@@ -321,8 +322,8 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
     const int64_t in = in_prefix ? u0 : found[1];
     now.b = in_prefix ? -1 : (int)found[0];
     now.len = in_prefix ? a.prefix_len : own_len(a, now.b);
-    now.n = tiles_of(now.len);
-    now.pairs = in_prefix ? a.kv_heads * w.prefix_tiles : own_pairs;
+    now.n = tiles_of(now.len, KU);
+    now.pairs = in_prefix ? head_groups * w.prefix_tiles : own_pairs;
     now.pair = (int)quotient(in, now.n);
     now.tile = (int)(in - (int64_t)now.pair * now.n);
   }
@@ -334,7 +335,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
     p.pair = 0, p.pairs = own_pairs;
     do {
       p.len = own_len(a, ++p.b);
-      p.n = tiles_of(p.len);
+      p.n = tiles_of(p.len, KU);
     } while (p.n == 0);
   };
   auto row_tiles = [&](const Place &p) { return p.b < 0 ? w.prefix_tiles : w.own_tiles; };
@@ -349,15 +350,16 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
     // ---- the warp that brings the data
     const bool aligned = ((((uintptr_t)a.k | (uintptr_t)a.v) >> 1 | a.k_page | a.k_tok | a.k_head | a.v_page | a.v_tok | a.v_head) & 7) == 0;
     const bool q_aligned = (((uintptr_t)a.q >> 1 | a.q_seq | a.q_tok | a.q_head) & 7) == 0;
-    const int box = maps.box, boxes = box ? KEYS / box : 0;
+    // (a box lies within a head's part of a tile; lane x has box x % boxes of head x / boxes)
+    const int box = maps.box, boxes = box ? KU / box : 0;
     int page[2];                                       // of this lane's box, or of its two rows; -1: none
     auto look_up = [&](const Place &p) {
       const int32_t *pages = p.b < 0 ? a.prefix_pages : a.table + (int64_t)p.b * a.max_pages;
 #pragma unroll
       for (int x = 0; x < 2; x++) {
-        const int j = p.tile * KEYS + (box ? lane * box : lane + 32 * x);
+        const int j = p.tile * KU + (box ? lane % boxes * box : (lane + 32 * x) % KU);
         page[x] = -1;
-        if (box ? x == 0 && lane < boxes && j < p.len : j < p.len) page[x] = pages[j / a.page_size] & 0x7FFFFFFF;
+        if (box ? x == 0 && lane < boxes * WH && j < p.len : j < p.len) page[x] = pages[j / a.page_size] & 0x7FFFFFFF;
       }
     };
     Place ahead = now;
@@ -372,7 +374,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
       }
       if (unit >= STAGES) alive = __all_sync(~0u, bar_wait(empty(stage), (lap - 1) & 1, dead));
       if (!alive) break;
-      const int tiles = row_tiles(at), kh = at.pair / tiles;
+      const int tiles = row_tiles(at), group = at.pair / tiles;
 #pragma unroll
       for (int x = 0; x < 2; x++) {
         if (to_load[x] >= a.n_pages) {                 // (a negative number has become a large one)
@@ -388,7 +390,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
         if (lane == 0) bar_expect(full(stage), bytes);
         __syncwarp();
         if (live) {
-          const int token = (at.tile * KEYS + lane * box) % a.page_size;
+          const int token = (at.tile * KU + lane % boxes * box) % a.page_size, kh = group * WH + lane / boxes;
 #pragma unroll
           for (int x = 0; x < D / 64; x++) {
             tile_load(to + x * HALF + lane * box * 128, &maps.k, x * 64, maps.k_heads_first ? kh : token,
@@ -402,7 +404,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
         int64_t k_off[2], v_off[2];                    // this lane's two rows
 #pragma unroll
         for (int x = 0; x < 2; x++) {
-          const int in = (at.tile * KEYS + lane + 32 * x) % a.page_size;
+          const int in = (at.tile * KU + (lane + 32 * x) % KU) % a.page_size, kh = group * WH + (lane + 32 * x) / KU;
           k_off[x] = to_load[x] < 0 ? -1 : to_load[x] * a.k_page + in * a.k_tok + kh * a.k_head;
           v_off[x] = to_load[x] < 0 ? -1 : to_load[x] * a.v_page + in * a.v_tok + kh * a.v_head;
         }
@@ -431,9 +433,9 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
           }
         }
       }
-      if (unit == 0 || at.tile == 0) {                 // a pair begins: its queries, zeros beyond the last row
+      if (WH == 1 && (unit == 0 || at.tile == 0)) {    // a pair begins: its queries, zeros beyond the last row
         seg = seg + 1 == STAGES ? 0 : seg + 1;
-        const int row0 = (at.pair - kh * tiles) * ROWS, rows = (at.b < 0 ? a.n_seqs : 1) * a.n_new * a.group - row0;
+        const int kh = group, row0 = (at.pair - kh * tiles) * ROWS, rows = (at.b < 0 ? a.n_seqs : 1) * a.n_new * a.group - row0;
         for (int x = lane; x < ROWS * CH; x += 32) {
           const int r = x / CH, c = x % CH;
           const uint32_t dst = seg * R::QUERIES + c / 8 * QHALF + r * 128 + ((c % 8) ^ (r & 7)) * 16;
@@ -450,7 +452,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
         }
       }
       // every lane's arrival: when its copies have landed; plain stores are ordered by a plain one after them
-      if (!q_aligned || (!box && !aligned)) {
+      if ((WH == 1 && !q_aligned) || (!box && !aligned)) {
         asm volatile("cp.async.wait_all;" ::: "memory");
         bar_arrive(full(stage));
       } else {
@@ -466,10 +468,10 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
     }
   } else {
     // ---- the warps that compute
-    const int wm = warp % WM, wk = warp / WM, quad = lane / 4, t4 = lane % 4, mi = lane / 8, mr = lane % 8;
+    const int wm = warp % WM, wk = warp / WM, wh = WH > 1 ? warp : 0, quad = lane / 4, t4 = lane % 4, mi = lane / 8, mr = lane % 8;
     const bool o_aligned = (((uintptr_t)a.out >> 1 | a.o_seq | a.o_tok | a.o_head) & 3) == 0;
     const float sl2 = a.scale * 1.4426950408889634f;   // scores in units of log 2
-    constexpr bool KEEP_Q = D <= 128 && WM == 1;       // the queries' fragments stay in registers
+    constexpr bool KEEP_Q = WH > 1 || (D <= 128 && WM == 1);       // the queries' fragments stay in registers
     // where this lane's rows of a fragment start; column d * 16 of the 64 is reached by turning bits 5 and 6
     const uint32_t k_lane = (wk * KW + (mi >> 1) * 8 + mr) * 128 + ((mi & 1) ^ mr) * 16;
     const uint32_t v_lane = (wk * KW + (mi & 1) * 8 + mr) * 128 + ((mi >> 1) ^ mr) * 16;
@@ -492,6 +494,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
         seg = seg + 1 == STAGES ? 0 : seg + 1;
         tile0 = now.tile;
         kh = now.pair / tiles, row0 = (now.pair - kh * tiles) * ROWS;
+        kh = kh * WH + wh;
         rows = min(ROWS, (now.b < 0 ? a.n_seqs : 1) * a.n_new * a.group - row0);
         seen_by_all = now.b < 0 ? now.len : now.len - (a.n_new - 1);
 #pragma unroll
@@ -502,7 +505,30 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
         }
 #pragma unroll
         for (int x = 0; x < D / 8; x++) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
-        if constexpr (KEEP_Q) {
+        if constexpr (WH > 1) {                        // straight to the fragments' places
+          const bool q_aligned = (((uintptr_t)a.q >> 1 | a.q_seq | a.q_tok | a.q_head) & 1) == 0;
+#pragma unroll
+          for (int x = 0; x < 2; x++) {
+            const Row p = row_of(a, now.b, kh, row0 + min(quad + 8 * x, rows - 1));
+            const T *src = (const T *)a.q + p.b * a.q_seq + p.i * a.q_tok + p.h * a.q_head + t4 * 2;
+#pragma unroll
+            for (int d = 0; d < D / 16; d++) {
+#pragma unroll
+              for (int y = 0; y < 2; y++) {
+                uint32_t v = 0;
+                if (quad + 8 * x < rows) {
+                  if (q_aligned) {
+                    v = *(const uint32_t *)(src + d * 16 + y * 8);
+                  } else {
+                    const T e[2] = {src[d * 16 + y * 8], src[d * 16 + y * 8 + 1]};
+                    memcpy(&v, e, 4);
+                  }
+                }
+                qf[d][x + 2 * y] = v;
+              }
+            }
+          }
+        } else if constexpr (KEEP_Q) {
 #pragma unroll
           for (int d = 0; d < D / 16; d++) ldsm(qf[d], q_at + seg * R::QUERIES + (q_lane ^ d % 4 * 32) + d / 4 * QHALF);
         }
@@ -514,7 +540,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
         v_at[x] = ring_at + stage * 2 * TILE + (v_lane ^ x * 32);
         q_from[x] = q_at + seg * R::QUERIES + (q_lane ^ x * 32);
       }
-      const int key0 = now.tile * KEYS + wk * KW;
+      const int key0 = now.tile * KU + (WH > 1 ? 0 : wk * KW);
       const bool mask = key0 + KW > seen_by_all;       // some row does not see some key of this warp's
       auto attend = [&](auto is_masked) {
         constexpr bool masked = decltype(is_masked)::value;
@@ -642,63 +668,99 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
       else attend(std::false_type());
 
       if (now.tile == now.n - 1 || unit == count - 1) {
-        // a pair ends here: the warps along the keys are joined in the stage just read, and its rows written
-        meet();
-        if (!alive) break;
-        float *acc = (float *)(ring + stage * 2 * TILE);   // [4 warps][16][D], columns of row r turned by 8 (r mod 4)
-#pragma unroll
-        for (int x = 0; x < 2; x++) {
-          l[x] += __shfl_xor_sync(~0u, l[x], 1);
-          l[x] += __shfl_xor_sync(~0u, l[x], 2);
-          const int r = warp * 16 + quad + 8 * x;
-          if (t4 == 0) stat[r] = make_float2(m[x], l[x]);
-#pragma unroll
-          for (int d = 0; d < D / 8; d++)
-            *(float2 *)(acc + r * D + ((d * 8 + t4 * 2) ^ (r & 3) * 8)) = make_float2(o[d][2 * x], o[d][2 * x + 1]);
-        }
-        meet();
-        if (!alive) break;
         const bool whole = tile0 == 0 && now.tile == now.n - 1;
         const bool final = whole && now.b >= 0 && a.prefix_len == 0;
-        for (int x = tid; x < rows * (D / 4); x += THREADS) {
-          const int r = x / (D / 4), c = x % (D / 4) * 4;
-          float best = -INFINITY;
+        if constexpr (WH > 1) {
+          // a pair ends here, and each warp has its head's rows
 #pragma unroll
-          for (int k = 0; k < WK; k++) best = fmaxf(best, stat[(k * WM + r / 16) * 16 + r % 16].x);
-          const float against = best == -INFINITY ? 0.f : best;
-          float sum = 0.f;
-          float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+          for (int x = 0; x < 2; x++) {
+            l[x] += __shfl_xor_sync(~0u, l[x], 1);
+            l[x] += __shfl_xor_sync(~0u, l[x], 2);
+            const int r = quad + 8 * x;
+            if (r >= rows) continue;
+            const Row p = row_of(a, now.b, kh, row0 + r);
+            const int64_t row = ((int64_t)p.b * a.n_new + p.i) * a.q_heads + p.h;
+            if (final) {
+              const float inv = l[x] == 0.f ? 0.f : 1.f / l[x];
+              T *dst = (T *)a.out + p.b * a.o_seq + p.i * a.o_tok + p.h * a.o_head + t4 * 2;
 #pragma unroll
-          for (int k = 0; k < WK; k++) {
-            const int at = (k * WM + r / 16) * 16 + r % 16;
-            const float f = exp2_fast(stat[at].x - against);
-            const float4 y = *(const float4 *)(acc + at * D + (c ^ (at & 3) * 8));
-            sum += f * stat[at].y;
-            v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
-          }
-          const Row p = row_of(a, now.b, kh, row0 + r);
-          const int64_t row = ((int64_t)p.b * a.n_new + p.i) * a.q_heads + p.h;
-          if (final) {
-            const float inv = sum == 0.f ? 0.f : 1.f / sum;
-            T *dst = (T *)a.out + p.b * a.o_seq + p.i * a.o_tok + p.h * a.o_head + c;
-            const uint32_t lo = pack<T>(v.x * inv, v.y * inv), hi = pack<T>(v.z * inv, v.w * inv);
-            if (o_aligned) {
-              *(uint2 *)dst = make_uint2(lo, hi);
+              for (int d = 0; d < D / 8; d++) {
+                const uint32_t v = pack<T>(o[d][2 * x] * inv, o[d][2 * x + 1] * inv);
+                if (o_aligned) {
+                  *(uint32_t *)(dst + d * 8) = v;
+                } else {
+                  T e[2];
+                  memcpy(e, &v, 4);
+                  dst[d * 8] = e[0], dst[d * 8 + 1] = e[1];
+                }
+              }
+              if (t4 == 0 && a.lse) a.lse[row] = l[x] == 0.f ? -INFINITY : (m[x] + log2f(l[x])) * 0.6931471805599453f;
             } else {
-              T e[4];
-              memcpy(e, &lo, 4), memcpy(e + 2, &hi, 4);
-              for (int j = 0; j < 4; j++) dst[j] = e[j];
+              const int64_t at = whole ? row : (((int64_t)blockIdx.x * 2 + !first_pair) * WH + wh) * ROWS + r;
+              float *dst = (whole ? w.whole_o[now.b >= 0] : w.cut_o) + at * D + t4 * 2;
+#pragma unroll
+              for (int d = 0; d < D / 8; d++) *(float2 *)(dst + d * 8) = make_float2(o[d][2 * x], o[d][2 * x + 1]);
+              if (t4 == 0) (whole ? w.whole_ml[now.b >= 0] : w.cut_ml)[at] = make_float2(m[x], l[x]);
             }
-            if (c == 0 && a.lse) a.lse[row] = sum == 0.f ? -INFINITY : (best + log2f(sum)) * 0.6931471805599453f;
-          } else {
-            // whole pairs by row, cut ones by block: its first (0) or its last (1)
-            const int64_t at = whole ? row : ((int64_t)blockIdx.x * 2 + !first_pair) * ROWS + r;
-            *(float4 *)((whole ? w.whole_o[now.b >= 0] : w.cut_o) + at * D + c) = v;
-            if (c == 0) (whole ? w.whole_ml[now.b >= 0] : w.cut_ml)[at] = make_float2(best, sum);
           }
+          if (mask) fence_async();
+        } else {
+          // a pair ends here: the warps along the keys are joined in the stage just read, and its rows written
+          meet();
+          if (!alive) break;
+          float *acc = (float *)(ring + stage * 2 * TILE);   // [4 warps][16][D], columns of row r turned by 8 (r mod 4)
+#pragma unroll
+          for (int x = 0; x < 2; x++) {
+            l[x] += __shfl_xor_sync(~0u, l[x], 1);
+            l[x] += __shfl_xor_sync(~0u, l[x], 2);
+            const int r = warp * 16 + quad + 8 * x;
+            if (t4 == 0) stat[r] = make_float2(m[x], l[x]);
+#pragma unroll
+            for (int d = 0; d < D / 8; d++)
+              *(float2 *)(acc + r * D + ((d * 8 + t4 * 2) ^ (r & 3) * 8)) = make_float2(o[d][2 * x], o[d][2 * x + 1]);
+          }
+          meet();
+          if (!alive) break;
+          for (int x = tid; x < rows * (D / 4); x += THREADS) {
+            const int r = x / (D / 4), c = x % (D / 4) * 4;
+            float best = -INFINITY;
+#pragma unroll
+            for (int k = 0; k < WK; k++) best = fmaxf(best, stat[(k * WM + r / 16) * 16 + r % 16].x);
+            const float against = best == -INFINITY ? 0.f : best;
+            float sum = 0.f;
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < WK; k++) {
+              const int at = (k * WM + r / 16) * 16 + r % 16;
+              const float f = exp2_fast(stat[at].x - against);
+              const float4 y = *(const float4 *)(acc + at * D + (c ^ (at & 3) * 8));
+              sum += f * stat[at].y;
+              v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
+            }
+            const Row p = row_of(a, now.b, kh, row0 + r);
+            const int64_t row = ((int64_t)p.b * a.n_new + p.i) * a.q_heads + p.h;
+            if (final) {
+              const float inv = sum == 0.f ? 0.f : 1.f / sum;
+              T *dst = (T *)a.out + p.b * a.o_seq + p.i * a.o_tok + p.h * a.o_head + c;
+              const uint32_t lo = pack<T>(v.x * inv, v.y * inv), hi = pack<T>(v.z * inv, v.w * inv);
+              if (o_aligned) {
+                *(uint2 *)dst = make_uint2(lo, hi);
+              } else {
+                T e[4];
+                memcpy(e, &lo, 4), memcpy(e + 2, &hi, 4);
+                for (int j = 0; j < 4; j++) dst[j] = e[j];
+              }
+              if (c == 0 && a.lse) a.lse[row] = sum == 0.f ? -INFINITY : (best + log2f(sum)) * 0.6931471805599453f;
+            } else {
+              // whole pairs by row, cut ones by block: its first (0) or its last (1)
+              const int64_t at = whole ? row : ((int64_t)blockIdx.x * 2 + !first_pair) * ROWS + r;
+              *(float4 *)((whole ? w.whole_o[now.b >= 0] : w.cut_o) + at * D + c) = v;
+              if (c == 0) (whole ? w.whole_ml[now.b >= 0] : w.cut_ml)[at] = make_float2(best, sum);
+            }
+          }
+          fence_async();                               // the stage was written here and is next written by TMA
         }
         first_pair = false;
-        fence_async();                                 // the stage was written here and is next written by TMA
       } else if (mask) {
         fence_async();
       }
@@ -779,7 +841,7 @@ template <int D> struct Tc {
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Line w, const int own_rows, const __grid_constant__ Pages maps, const uint32_t flip) {
+__global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Line w, const Line own_line, const __grid_constant__ Pages maps, const uint32_t flip) {
   constexpr int TILE = Tc<D>::TILE, STAGES = Tc<D>::STAGES, HALF = TC_KEYS * 128;   // 64 columns of a tile
   extern __shared__ unsigned char smem_raw[];
   unsigned char *const smem = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -800,7 +862,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   __shared__ int own[TC_THREADS / 32][2];              // of each warp: sequences' tiles, sequences that have any
   int tiles = 0, some = 0;
   for (int b = tid; b < a.n_seqs; b += TC_THREADS) {
-    const int x = tiles_of(own_len(a, b));
+    const int x = tiles_of(own_len(a, b), own_line.keys);
     tiles += x;
     some += x > 0;
   }
@@ -809,7 +871,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   __syncthreads();
   int64_t own_tiles = 0, own_pairs = 0;
   for (int x = 0; x < TC_THREADS / 32; x++) own_tiles += own[x][0], own_pairs += own[x][1];
-  const int pairs_each = a.kv_heads * ((a.n_new * a.group + own_rows - 1) / own_rows);
+  const int pairs_each = a.kv_heads / own_line.heads * own_line.own_tiles;
   const int blocks = prefix_sms(a, w, own_tiles * pairs_each, own_pairs * pairs_each);
   const int n = tiles_of(a.prefix_len, TC_KEYS);
   const int64_t units = (int64_t)n * a.kv_heads * w.prefix_tiles, per = quotient(units + blocks - 1, blocks);
@@ -985,24 +1047,28 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
       const Row p = row_of(a, -1, kh, row);
       // queries: the warp takes its 32 rows together, lanes along them
       const unsigned long long src = row < all ? (unsigned long long)((const T *)a.q + p.b * a.q_seq + p.i * a.q_tok + p.h * a.q_head) : 0;
-#pragma unroll 8
-      for (int x = lane; x < 32 * (D / 8); x += 32) {
-        const int y = x / (D / 8), c = x % (D / 8), at = warp % 4 * 32 + y;
-        const T *from = (const T *)__shfl_sync(~0u, src, y);
-        uint4 v = make_uint4(0, 0, 0, 0);
+      uint4 v[D / 8];
+#pragma unroll
+      for (int x = 0; x < D / 8; x++) {                  // all loads first
+        const T *from = (const T *)__shfl_sync(~0u, src, (x * 32 + lane) / (D / 8));
+        v[x] = make_uint4(0, 0, 0, 0);
         if (from) {
-          from += c * 8;
+          from += lane % (D / 8) * 8;
           if (q_aligned) {
-            v = *(const uint4 *)from;
+            v[x] = *(const uint4 *)from;
           } else {
             T e[8];
 #pragma unroll
             for (int z = 0; z < 8; z++) e[z] = from[z];
-            memcpy(&v, e, 16);
+            memcpy(&v[x], e, 16);
           }
-          v.x ^= flip, v.y ^= flip, v.z ^= flip, v.w ^= flip;   // a negative scale: its sign goes to the queries
         }
-        *(uint4 *)(qs + h * (Tc<D>::Q / 2) + c / 8 * HALF + at * 128 + ((c % 8) ^ (at & 7)) * 16) = v;
+      }
+#pragma unroll
+      for (int x = 0; x < D / 8; x++) {
+        const int c = lane % (D / 8), at = warp % 4 * 32 + (x * 32 + lane) / (D / 8);
+        v[x].x ^= flip, v[x].y ^= flip, v[x].z ^= flip, v[x].w ^= flip;   // a negative scale: its sign goes to the queries
+        *(uint4 *)(qs + h * (Tc<D>::Q / 2) + c / 8 * HALF + at * 128 + ((c % 8) ^ (at & 7)) * 16) = v[x];
       }
       fence_async();
       bar_arrive(q_full(h));
@@ -1138,15 +1204,15 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
     Parts p = {0, 0, 0, 0, 0, false};
     if (n) {
       p.per = w.starts[a.n_seqs + 1];
-      p.u0 = start + (int64_t)(kh * tiles + r / w.rows) * n;
-      p.r = r % w.rows;
+      p.u0 = start + (int64_t)(kh / w.heads * tiles + r / w.rows) * n;
+      p.r = kh % w.heads * w.rows + r % w.rows;
       p.c0 = quotient(p.u0, p.per);
       p.count = (int)(quotient(p.u0 + n - 1, p.per) - p.c0) + 1;
       p.whole = p.count == 1;
     }
     return p;
   };
-  const int in = h - kh * a.group, n = tiles_of(own_len(a, b));
+  const int in = h - kh * a.group, n = tiles_of(own_len(a, b), lo.keys);
   const Parts pre = parts(lp, (b * a.n_new + i) * a.group + in, lp.prefix_tiles, 0, tiles_of(a.prefix_len, lp.keys));
   const Parts own = parts(lo, i * a.group + in, lo.own_tiles, n ? lo.starts[b] : 0, n);
   if (a.prefix_len == 0 && own.whole) return;
@@ -1161,7 +1227,7 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
       const bool whole = mine ? own.whole : pre.whole;
       const int64_t c = mine ? own.c0 + x - pre.count : pre.c0 + x;
       const bool last = mine ? own.u0 > c * own.per : pre.u0 > c * pre.per;
-      const int64_t at = whole ? row : (c * 2 + last) * (mine ? lo.rows : lp.rows) + (mine ? own.r : pre.r);
+      const int64_t at = whole ? row : (c * 2 + last) * (mine ? lo.heads * lo.rows : lp.heads * lp.rows) + (mine ? own.r : pre.r);
       o = (whole ? mine ? lo.whole_o[1] : lp.whole_o[0] : mine ? lo.cut_o : lp.cut_o) + at * D;
       ml = (whole ? mine ? lo.whole_ml[1] : lp.whole_ml[0] : mine ? lo.cut_ml : lp.cut_ml)[at];
     }
@@ -1242,9 +1308,9 @@ struct Plan {
 
 constexpr int64_t TENSOR_ROWS = 48, APART_ROWS = 64;
 
-int box_of(int page_size) {  // tokens of a TMA box: the largest power of two that divides both the page and a tile
+int box_of(int page_size, int most) {  // tokens of a TMA box: the largest power of two that divides both the page and a tile
   int box = 1;
-  while (box < KEYS && page_size % (box * 2) == 0) box *= 2;
+  while (box < most && page_size % (box * 2) == 0) box *= 2;
   return box;
 }
 
@@ -1261,18 +1327,20 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
     n += up(bytes);
     return x;
   };
-  auto line = [&](Line &w, int rows, int keys, int blocks, bool has_prefix, bool has_own) {
-    w.has_prefix = has_prefix, w.has_own = has_own, w.rows = rows, w.keys = keys, w.blocks = blocks;
+  auto line = [&](Line &w, int heads, int rows, int keys, int blocks, bool has_prefix, bool has_own) {
+    w.has_prefix = has_prefix, w.has_own = has_own, w.heads = heads, w.rows = rows, w.keys = keys, w.blocks = blocks;
     w.prefix_tiles = (int)((all + rows - 1) / rows), w.own_tiles = (int)((own_rows + rows - 1) / rows);
     w.starts = (int64_t *)take(((size_t)d.n_seqs + 2) * 8);
-    w.cut_ml = (float2 *)take((size_t)blocks * 2 * rows * 8);
-    w.cut_o = (float *)take((size_t)blocks * 2 * rows * D * 4);
+    w.cut_ml = (float2 *)take((size_t)blocks * 2 * heads * rows * 8);
+    w.cut_o = (float *)take((size_t)blocks * 2 * heads * rows * D * 4);
   };
   const int own_tile = own_rows <= 16 ? 16 : own_rows <= 32 ? 32 : 64;
-  line(p.own, own_tile, KEYS, stream_blocks(D), p.way == TOGETHER && d.prefix_len, true);
-  if (p.way == APART) line(p.prefix, 64, KEYS, stream_blocks(D), true, false);
+  // few rows: a warp to each of four heads, which have nothing to join at the end, where the heads can be had by fours
+  const int heads = own_tile == 16 && D <= 128 && d.cache.kv_heads % WARPS == 0 ? WARPS : 1;
+  line(p.own, heads, own_tile, KEYS / heads, stream_blocks(D), p.way == TOGETHER && d.prefix_len, true);
+  if (p.way == APART) line(p.prefix, 1, 64, KEYS, stream_blocks(D), true, false);
   if (p.way == TENSOR) {
-    line(p.prefix, 256, TC_KEYS, SMS, true, false);
+    line(p.prefix, 1, 256, TC_KEYS, SMS, true, false);
     p.own.beside_prefix = 1;
   }
   if (p.way == TOGETHER) p.prefix = p.own;
@@ -1327,8 +1395,8 @@ bool tile_map(CUtensorMap &map, int &heads_first, int box, const gts_cache &c, v
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool tile_maps(Pages &p, const gts_cache &c) {
-  const int box = box_of((int)c.page_size);
+bool tile_maps(Pages &p, const gts_cache &c, int most) {
+  const int box = box_of((int)c.page_size, most);
   if (box < 8 || !c.n_pages) return false;   // a box is whole groups of eight rows
   p.box = box;
   const bool ok = tile_map(p.k, p.k_heads_first, p.box, c, c.k, c.k_page_stride, c.k_token_stride, c.k_head_stride) &&
@@ -1349,40 +1417,46 @@ cudaError_t launch_kernel(void (*kernel)(P...), unsigned blocks, unsigned thread
   return cudaLaunchKernelEx(&c, kernel, args...);
 }
 
-template <typename T, int D, int WM>
+template <typename T, int D, int WM, int WH>
 cudaError_t stream(const Args &a, const Line &w, const Line &prefix, const Pages &maps, bool early, cudaStream_t s) {
   static std::atomic<uint64_t> granted{0};
-  const cudaError_t e = grant(k_stream<T, D, WM>, Ring<D, WM>::SMEM, granted);
-  return e != cudaSuccess ? e : launch_kernel(k_stream<T, D, WM>, w.blocks, STREAM_THREADS, Ring<D, WM>::SMEM, s, early, a, w, prefix, maps);
+  const cudaError_t e = grant(k_stream<T, D, WM, WH>, Ring<D, WM, WH>::SMEM, granted);
+  return e != cudaSuccess ? e : launch_kernel(k_stream<T, D, WM, WH>, w.blocks, STREAM_THREADS, Ring<D, WM, WH>::SMEM, s, early, a, w, prefix, maps);
 }
 
 template <typename T, int D>
-cudaError_t tensor(const Args &a, const Line &w, int own_rows, const Pages &maps, cudaStream_t s) {
+cudaError_t tensor(const Args &a, const Line &w, const Line &own, const Pages &maps, cudaStream_t s) {
   static std::atomic<uint64_t> granted{0};
   const cudaError_t e = grant(k_prefix<T, D>, Tc<D>::SMEM, granted);
-  return e != cudaSuccess ? e : launch_kernel(k_prefix<T, D>, w.blocks, TC_THREADS, Tc<D>::SMEM, s, false, a, w, own_rows, maps, a.scale < 0 ? 0x80008000u : 0u);
+  return e != cudaSuccess ? e : launch_kernel(k_prefix<T, D>, w.blocks, TC_THREADS, Tc<D>::SMEM, s, false, a, w, own, maps, a.scale < 0 ? 0x80008000u : 0u);
 }
 
 template <typename T, int D>
-cudaError_t run(const Args &a, const Plan &p, const Pages &maps, cudaStream_t s) {
+cudaError_t run(const Args &a, const Plan &p, const Pages &maps, const Pages &own_maps, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
-  if (p.way == APART) e = stream<T, D, 4>(a, p.prefix, p.prefix, maps, false, s);
+  if (p.way == APART) e = stream<T, D, 4, 1>(a, p.prefix, p.prefix, own_maps, false, s);
   if constexpr (D <= 128) {
-    if (p.way == TENSOR) e = tensor<T, D>(a, p.prefix, p.own.rows, maps, s);
+    if (p.way == TENSOR) e = tensor<T, D>(a, p.prefix, p.own, maps, s);
   }
   if (e != cudaSuccess) return e;
   const bool early = p.way != TOGETHER;
-  e = p.own.rows == 16   ? stream<T, D, 1>(a, p.own, p.prefix, maps, early, s)
-      : p.own.rows == 32 ? stream<T, D, 2>(a, p.own, p.prefix, maps, early, s)
-                         : stream<T, D, 4>(a, p.own, p.prefix, maps, early, s);
+  if constexpr (D <= 128) {
+    if (p.own.heads > 1) e = stream<T, D, 1, WARPS>(a, p.own, p.prefix, own_maps, early, s);
+  }
+  if (p.own.heads == 1)
+    e = p.own.rows == 16 ? stream<T, D, 1, 1>(a, p.own, p.prefix, own_maps, early, s)
+        : p.own.rows == 32 ? stream<T, D, 2, 1>(a, p.own, p.prefix, own_maps, early, s)
+                           : stream<T, D, 4, 1>(a, p.own, p.prefix, own_maps, early, s);
   if (e != cudaSuccess) return e;
   const int64_t rows = (int64_t)a.n_seqs * a.n_new * a.q_heads;
   return launch_kernel(k_join<T, D>, (unsigned)((rows + WARPS - 1) / WARPS), THREADS, 0, s, true, a, p.prefix, p.own);
 }
 
 template <typename T>
-cudaError_t launch(const Args &a, const Plan &p, const Pages &maps, int head_dim, cudaStream_t s) {
-  return head_dim == 64 ? run<T, 64>(a, p, maps, s) : head_dim == 128 ? run<T, 128>(a, p, maps, s) : run<T, 256>(a, p, maps, s);
+cudaError_t launch(const Args &a, const Plan &p, const Pages &maps, const Pages &own_maps, int head_dim, cudaStream_t s) {
+  return head_dim == 64    ? run<T, 64>(a, p, maps, own_maps, s)
+         : head_dim == 128 ? run<T, 128>(a, p, maps, own_maps, s)
+                           : run<T, 256>(a, p, maps, own_maps, s);
 }
 
 const char *refuse_shape(const gts_attention_desc &d) {
@@ -1437,11 +1511,12 @@ extern "C" gts_status gts_prefix_attention(const gts_attention_desc *d, void *st
   a.status = d->d_status;
   if (d->workspace_bytes < gts_attention_workspace_bytes(d))
     return gts::fail(GTS_ERR_NOMEM, "attention: workspace smaller than gts_attention_workspace_bytes");
-  Pages maps = {};
-  const bool mapped = tile_maps(maps, c);
+  Pages maps = {}, own_maps = {};
   // (a scale of 0 would turn the -infinity of masked scores into NaN on the tensor cores)
+  const bool mapped = tile_maps(maps, c, TC_KEYS);
   const Plan p = make_plan(*d, mapped && d->scale != 0.f && tensor_shape(*d), (char *)d->workspace);
-  const cudaError_t e = c.dtype == GTS_BF16 ? launch<__nv_bfloat16>(a, p, maps, c.head_dim, (cudaStream_t)stream)
-                                            : launch<__half>(a, p, maps, c.head_dim, (cudaStream_t)stream);
+  if (mapped) tile_maps(own_maps, c, p.own.keys);
+  const cudaError_t e = c.dtype == GTS_BF16 ? launch<__nv_bfloat16>(a, p, maps, own_maps, c.head_dim, (cudaStream_t)stream)
+                                            : launch<__half>(a, p, maps, own_maps, c.head_dim, (cudaStream_t)stream);
   return e == cudaSuccess ? GTS_OK : gts::cuda_fail(e, "attention: launch");
 }
