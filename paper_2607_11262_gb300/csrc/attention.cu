@@ -17,6 +17,21 @@
 
 namespace {
 
+// x / d for 0 <= x < 2^31 by a multiplication: m = floor(2^(31 + l) / d) + 1 with 2^(l-1) < d <= 2^l, so m d exceeds 2^(31 + l) by
+// at most d <= 2^l, and x times that is below 2^(31 + l).
+struct Divisor {
+  uint32_t m;
+  int shift;           // l - 1; -1 for d = 1
+  int d;
+};
+Divisor divisor(int d) {
+  int l = 0;
+  while ((1ll << l) < d) l++;
+  return {l ? (uint32_t)(((1ull << (31 + l)) / (uint32_t)d) + 1) : 0u, l - 1, d};
+}
+__device__ __forceinline__ int operator/(int x, const Divisor &d) { return d.shift < 0 ? x : (int)(__umulhi((uint32_t)x, d.m) >> d.shift); }
+__device__ __forceinline__ int operator%(int x, const Divisor &d) { return x - x / d * d.d; }
+
 struct Args {
   const void *q;
   void *out;
@@ -26,6 +41,7 @@ struct Args {
   int64_t k_page, k_tok, k_head, v_page, v_tok, v_head;
   int n_seqs, n_new, q_heads, kv_heads, group;
   int n_pages, page_size, max_pages, prefix_len;
+  Divisor in_page, in_group;   // by page_size, by group
   float scale;
   const int32_t *prefix_pages, *table, *lens;
   int32_t *status;
@@ -201,7 +217,7 @@ __device__ __forceinline__ Row row_of(const Args &a, int b, int kh, int r) {
   Row x;
   x.b = b < 0 ? r / per : b;
   const int in = b < 0 ? r - x.b * per : r;
-  x.i = in / a.group;
+  x.i = in / a.in_group;
   x.h = kh * a.group + in - x.i * a.group;
   return x;
 }
@@ -217,7 +233,9 @@ struct Place { int b, len, n, pairs, pair, tile; };
 // A block is 4 warps that compute and one that brings the data.  The fifth warp runs ahead along the block's stretch of the
 // line, across the ends of pairs, and fills a ring of tiles: boxes of tokens by TMA where the pages allow it (see tile_map),
 // else rows gathered by 16-byte copies, else (caches off the 16-byte grid) by plain loads.  A pair's queries come with its
-// first tile.  Of the others, WM stand along the rows (16 each) and 4 / WM along a tile's keys; they meet only where a pair
+// first tile.  (With four heads there are four such warps: issuing a tile's copies takes one of them 1600 cycles, the
+// products 1000.  256 threads start with 65536 / 256 / blocks registers, 128 or 80, and go on with 200 and 56 or 112 and 48.)
+// Of the others, WM stand along the rows (16 each) and 4 / WM along a tile's keys; they meet only where a pair
 // ends, to be joined in the stage just read.  Scores and weights stay in the fragments of m16n8k16 products, each warp with
 // its own running maximum and sum.  Weights are rounded to the type of the values for their product with them (the sum is of
 // the unrounded ones); everything else is in 32 bits.
@@ -227,11 +245,11 @@ template <int D, int WM, int WH> struct Ring {
   static constexpr int QUERIES = WH > 1 ? 0 : 16 * WM * D * 2;  // with four heads they go straight to registers
   static constexpr int SMEM = 1024 /* alignment */ + STAGES * (2 * TILE + QUERIES) + 64 * 8 + (2 * STAGES + 1) * 8 + 56;
 };
-constexpr int STREAM_THREADS = THREADS + 32;
+__host__ __device__ constexpr int stream_threads(int WH) { return THREADS + 32 * WH; }
 __host__ __device__ constexpr int stream_per_sm(int D) { return D == 64 ? 3 : D == 128 ? 2 : 1; }
 
 template <typename T, int D, int WM, int WH>
-__global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(const Args a, const Line w, const Line prefix, const __grid_constant__ Pages maps) {
+__global__ void __launch_bounds__(stream_threads(WH), stream_per_sm(D)) k_stream(const Args a, const Line w, const Line prefix, const __grid_constant__ Pages maps) {
   using R = Ring<D, WM, WH>;
   static_assert(WH == 1 || (WH == WARPS && WM == 1), "a warp for each head, or all for one");
   constexpr int WK = WARPS / WM / WH, ROWS = 16 * WM, KU = KEYS / WH, KW = KU / WK, STAGES = R::STAGES, TILE = R::TILE;
@@ -250,7 +268,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
   auto empty = [&](int s) { return bar0 + (STAGES + s) * 8; };
   const uint32_t together = bar0 + 2 * STAGES * 8;
   if (tid == 0) {
-    for (int s = 0; s < STAGES; s++) bar_init(full(s), 33), bar_init(empty(s), WARPS);
+    for (int s = 0; s < STAGES; s++) bar_init(full(s), 33 * WH), bar_init(empty(s), WARPS);
     bar_init(together, WARPS);
     *dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -346,20 +364,25 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
     if (++stage == STAGES) stage = 0, lap++;
   };
 
-  if (warp == WARPS) {
-    // ---- the warp that brings the data
+  if (warp >= WARPS) {
+    // ---- the warp that brings the data (of one head: with four, there are four)
+    if constexpr (WH > 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(D == 64 ? 48 : 56));
     const bool aligned = ((((uintptr_t)a.k | (uintptr_t)a.v) >> 1 | a.k_page | a.k_tok | a.k_head | a.v_page | a.v_tok | a.v_head) & 7) == 0;
     const bool q_aligned = (((uintptr_t)a.q >> 1 | a.q_seq | a.q_tok | a.q_head) & 7) == 0;
-    // (a box lies within a head's part of a tile; lane x has box x % boxes of head x / boxes)
-    const int box = maps.box, boxes = box ? KU / box : 0;
+    const int hh = warp - WARPS, box = maps.box, boxes = box ? KU / box : 0;
     int page[2];                                       // of this lane's box, or of its two rows; -1: none
     auto look_up = [&](const Place &p) {
       const int32_t *pages = p.b < 0 ? a.prefix_pages : a.table + (int64_t)p.b * a.max_pages;
+      page[0] = page[1] = -1;
+      if (box) {
+        const int j = p.tile * KU + lane * box;
+        if (lane < boxes && j < p.len) page[0] = pages[j / a.in_page] & 0x7FFFFFFF;
+      } else {
 #pragma unroll
-      for (int x = 0; x < 2; x++) {
-        const int j = p.tile * KU + (box ? lane % boxes * box : (lane + 32 * x) % KU);
-        page[x] = -1;
-        if (box ? x == 0 && lane < boxes * WH && j < p.len : j < p.len) page[x] = pages[j / a.page_size] & 0x7FFFFFFF;
+        for (int x = 0; x < 2; x++) {
+          const int j = p.tile * KU + lane + 32 * x;
+          if (lane + 32 * x < KU && j < p.len) page[x] = pages[j / a.in_page] & 0x7FFFFFFF;
+        }
       }
     };
     Place ahead = now;
@@ -374,7 +397,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
       }
       if (unit >= STAGES) alive = __all_sync(~0u, bar_wait(empty(stage), (lap - 1) & 1, dead));
       if (!alive) break;
-      const int tiles = row_tiles(at), group = at.pair / tiles;
+      const int tiles = row_tiles(at), group = tiles == 1 ? at.pair : at.pair / tiles;
 #pragma unroll
       for (int x = 0; x < 2; x++) {
         if (to_load[x] >= a.n_pages) {                 // (a negative number has become a large one)
@@ -390,29 +413,31 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
         if (lane == 0) bar_expect(full(stage), bytes);
         __syncwarp();
         if (live) {
-          const int token = (at.tile * KU + lane % boxes * box) % a.page_size, kh = group * WH + lane / boxes;
+          const int token = (at.tile * KU + lane * box) % a.in_page, kh = group * WH + hh;
+          const int k_y = maps.k_heads_first ? kh : token, k_z = maps.k_heads_first ? token : kh;
+          const int v_y = maps.v_heads_first ? kh : token, v_z = maps.v_heads_first ? token : kh;
+          const uint32_t dst = to + (hh * KU + lane * box) * 128;
 #pragma unroll
           for (int x = 0; x < D / 64; x++) {
-            tile_load(to + x * HALF + lane * box * 128, &maps.k, x * 64, maps.k_heads_first ? kh : token,
-                      maps.k_heads_first ? token : kh, to_load[0], full(stage));
-            tile_load(to + TILE + x * HALF + lane * box * 128, &maps.v, x * 64, maps.v_heads_first ? kh : token,
-                      maps.v_heads_first ? token : kh, to_load[0], full(stage));
+            tile_load(dst + x * HALF, &maps.k, x * 64, k_y, k_z, to_load[0], full(stage));
+            tile_load(dst + TILE + x * HALF, &maps.v, x * 64, v_y, v_z, to_load[0], full(stage));
           }
         }
       } else {
         if (lane == 0) bar_expect(full(stage), 0);
+        const int kh = group * WH + hh;
         int64_t k_off[2], v_off[2];                    // this lane's two rows
 #pragma unroll
         for (int x = 0; x < 2; x++) {
-          const int in = (at.tile * KU + (lane + 32 * x) % KU) % a.page_size, kh = group * WH + (lane + 32 * x) / KU;
+          const int in = (at.tile * KU + lane + 32 * x) % a.in_page;
           k_off[x] = to_load[x] < 0 ? -1 : to_load[x] * a.k_page + in * a.k_tok + kh * a.k_head;
           v_off[x] = to_load[x] < 0 ? -1 : to_load[x] * a.v_page + in * a.v_tok + kh * a.v_head;
         }
 #pragma unroll
-        for (int x = 0; x < 2; x++) {
+        for (int x = 0; x < (KU + 31) / 32; x++) {
 #pragma unroll 4
-          for (int y = 0; y < 32; y++) {               // lanes along the row: D / 8 pieces of keys, then of values
-            const int r = x * 32 + y;
+          for (int y = 0; y < min(32, KU); y++) {      // lanes along the row: D / 8 pieces of keys, then of values
+            const int r = hh * KU + x * 32 + y;
             const int64_t k = __shfl_sync(~0u, k_off[x], y), v = __shfl_sync(~0u, v_off[x], y);
 #pragma unroll
             for (int z = 0; z < 2 * CH; z += 32) {
@@ -468,6 +493,7 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
     }
   } else {
     // ---- the warps that compute
+    if constexpr (WH > 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(D == 64 ? 112 : 200));
     const int wm = warp % WM, wk = warp / WM, wh = WH > 1 ? warp : 0, quad = lane / 4, t4 = lane % 4, mi = lane / 8, mr = lane % 8;
     const bool o_aligned = (((uintptr_t)a.out >> 1 | a.o_seq | a.o_tok | a.o_head) & 3) == 0;
     const float sl2 = a.scale * 1.4426950408889634f;   // scores in units of log 2
@@ -493,14 +519,14 @@ __global__ void __launch_bounds__(STREAM_THREADS, stream_per_sm(D)) k_stream(con
         const int tiles = row_tiles(now);
         seg = seg + 1 == STAGES ? 0 : seg + 1;
         tile0 = now.tile;
-        kh = now.pair / tiles, row0 = (now.pair - kh * tiles) * ROWS;
+        kh = tiles == 1 ? now.pair : now.pair / tiles, row0 = (now.pair - kh * tiles) * ROWS;
         kh = kh * WH + wh;
         rows = min(ROWS, (now.b < 0 ? a.n_seqs : 1) * a.n_new * a.group - row0);
         seen_by_all = now.b < 0 ? now.len : now.len - (a.n_new - 1);
 #pragma unroll
         for (int x = 0; x < 2; x++) {                  // keys that the rows of this thread's fragments see
           const int r = row0 + wm * 16 + quad + 8 * x;
-          limit[x] = now.b < 0 ? now.len : now.len - (a.n_new - 1 - min(r / a.group, a.n_new - 1));
+          limit[x] = now.b < 0 ? now.len : now.len - (a.n_new - 1 - min(r / a.in_group, a.n_new - 1));
           m[x] = -INFINITY, l[x] = 0.f;
         }
 #pragma unroll
@@ -906,7 +932,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
       int pair = (int)quotient(u0, n), tile = (int)(u0 - (int64_t)pair * n), kh = pair / w.prefix_tiles;
       auto look_up = [&](int t) {                          // this lane's page of tile t; -1: none
         const int key = t * TC_KEYS + lane * maps.box;
-        return lane < boxes && key < a.prefix_len ? a.prefix_pages[key / a.page_size] & 0x7FFFFFFF : -1;
+        return lane < boxes && key < a.prefix_len ? a.prefix_pages[key / a.in_page] & 0x7FFFFFFF : -1;
       };
       int page_next = look_up(tile);
       for (int64_t u = u0; u < u1 && alive; u++) {
@@ -929,7 +955,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
           __syncwarp();
           if (live) {
             const bool heads_first = kv ? maps.v_heads_first : maps.k_heads_first;
-            const int token = key % a.page_size;
+            const int token = key % a.in_page;
 #pragma unroll
             for (int x = 0; x < D / 64; x++)
               tile_load(ring_at + s * TILE + x * HALF + lane * maps.box * 128, kv ? &maps.v : &maps.k, x * 64, heads_first ? head : token,
@@ -1197,7 +1223,7 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
   wait_for_kernels_before();
   const int64_t token = quotient(row, a.q_heads), seq = quotient(token, a.n_new);
   const int h = (int)(row - token * a.q_heads), i = (int)(token - seq * a.n_new), b = (int)seq;
-  const int kh = h / a.group;
+  const int kh = h / a.in_group;
   // a pair's parts: its blocks c0 .. c0 + count - 1, or one result of its own
   struct Parts { int64_t u0, c0, per; int count, r; bool whole; };
   auto parts = [&](const Line &w, int r, int tiles, int64_t start, int n) {
@@ -1421,7 +1447,7 @@ template <typename T, int D, int WM, int WH>
 cudaError_t stream(const Args &a, const Line &w, const Line &prefix, const Pages &maps, bool early, cudaStream_t s) {
   static std::atomic<uint64_t> granted{0};
   const cudaError_t e = grant(k_stream<T, D, WM, WH>, Ring<D, WM, WH>::SMEM, granted);
-  return e != cudaSuccess ? e : launch_kernel(k_stream<T, D, WM, WH>, w.blocks, STREAM_THREADS, Ring<D, WM, WH>::SMEM, s, early, a, w, prefix, maps);
+  return e != cudaSuccess ? e : launch_kernel(k_stream<T, D, WM, WH>, w.blocks, stream_threads(WH), Ring<D, WM, WH>::SMEM, s, early, a, w, prefix, maps);
 }
 
 template <typename T, int D>
@@ -1506,6 +1532,7 @@ extern "C" gts_status gts_prefix_attention(const gts_attention_desc *d, void *st
   a.group = a.q_heads / a.kv_heads;
   a.n_pages = (int)c.n_pages, a.page_size = (int)c.page_size, a.max_pages = (int)d->max_pages;
   a.prefix_len = (int)d->prefix_len;
+  a.in_page = divisor(a.page_size), a.in_group = divisor(a.group);
   a.scale = d->scale;
   a.prefix_pages = d->prefix_pages, a.table = d->page_table, a.lens = d->lens;
   a.status = d->d_status;
