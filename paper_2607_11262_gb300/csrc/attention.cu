@@ -174,6 +174,7 @@ struct Line {           // the units of one launch
   int has_prefix, has_own;
   int heads, rows, keys;  // key heads of a pair, rows of its tile (for each head), keys of a unit
   int beside_prefix;    // the tensor cores' kernel runs at the same time
+  int side_by_side;     // that kernel's own: starts[n_seqs] row tiles at a time
   int prefix_tiles, own_tiles;   // row tiles of the prefix's rows, of a sequence's rows
   int blocks;
   int64_t *starts;      // [n_seqs + 2]: first unit of each sequence, the units of all, units per block
@@ -512,6 +513,17 @@ __global__ void __launch_bounds__(stream_threads(WH), stream_per_sm(D)) k_stream
     bool first_pair = true;
     float o[D / 8][4], m[2], l[2];
     uint32_t qf[KEEP_Q ? D / 16 : 1][4];
+    // Four heads: the next pair's queries are brought to L2 while this one's keys are worked on (from memory, while it is busy,
+    // a load takes up to 5 us)
+    auto ask_for_queries = [&](int b, int kh, int row0, int rows) {
+      constexpr int LINES = D / 64;                    // of a row
+      for (int x = lane; x < rows * LINES; x += 32) {
+        const Row p = row_of(a, b, kh, row0 + x / LINES);
+        const T *src = (const T *)a.q + p.b * a.q_seq + p.i * a.q_tok + p.h * a.q_head + x % LINES * 64;
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(src));
+      }
+    };
+    int after = WH > 1 && now.b + 1 < a.n_seqs ? a.lens[now.b + 1] : 0, after_b = now.b;   // the next sequence's length, ahead of time
     for (int unit = 0; unit < count; unit++) {
       alive = __all_sync(~0u, bar_wait(full(stage), lap & 1, dead));
       if (!alive) break;
@@ -531,7 +543,8 @@ __global__ void __launch_bounds__(stream_threads(WH), stream_per_sm(D)) k_stream
         }
 #pragma unroll
         for (int x = 0; x < D / 8; x++) o[x][0] = o[x][1] = o[x][2] = o[x][3] = 0.f;
-        if constexpr (WH > 1) {                        // straight to the fragments' places
+        if constexpr (WH > 1) {
+          // straight to the fragments' places
           const bool q_aligned = (((uintptr_t)a.q >> 1 | a.q_seq | a.q_tok | a.q_head) & 1) == 0;
 #pragma unroll
           for (int x = 0; x < 2; x++) {
@@ -693,6 +706,17 @@ __global__ void __launch_bounds__(stream_threads(WH), stream_per_sm(D)) k_stream
       if (mask) attend(std::true_type());
       else attend(std::false_type());
 
+      if constexpr (WH > 1) {
+        if (now.tile == tile0 && unit + (now.n - now.tile) < count) {
+          const int tiles = row_tiles(now), pair = now.pair + 1 < now.pairs ? now.pair + 1 : 0;
+          const bool same = now.pair + 1 < now.pairs;
+          if (same || after > 0) {                     // (with an empty sequence in between: no matter)
+            const int b = same ? now.b : now.b + 1, t = same ? tiles : w.own_tiles;
+            const int group = t == 1 ? pair : pair / t, first = (pair - group * t) * ROWS;
+            ask_for_queries(b, group * WH + wh, first, min(ROWS, (b < 0 ? a.n_seqs : 1) * a.n_new * a.group - first));
+          }
+        }
+      }
       if (now.tile == now.n - 1 || unit == count - 1) {
         const bool whole = tile0 == 0 && now.tile == now.n - 1;
         const bool final = whole && now.b >= 0 && a.prefix_len == 0;
@@ -793,6 +817,10 @@ __global__ void __launch_bounds__(stream_threads(WH), stream_per_sm(D)) k_stream
       __syncwarp();
       if (lane == 0) bar_arrive(empty(stage));
       if (unit + 1 < count) advance(now);
+      if (WH > 1 && now.b != after_b) {
+        after_b = now.b;
+        after = now.b + 1 < a.n_seqs ? a.lens[now.b + 1] : 0;
+      }
       next();
     }
   }
@@ -899,10 +927,16 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   for (int x = 0; x < TC_THREADS / 32; x++) own_tiles += own[x][0], own_pairs += own[x][1];
   const int pairs_each = a.kv_heads / own_line.heads * own_line.own_tiles;
   const int blocks = prefix_sms(a, w, own_tiles * pairs_each, own_pairs * pairs_each);
-  const int n = tiles_of(a.prefix_len, TC_KEYS);
-  const int64_t units = (int64_t)n * a.kv_heads * w.prefix_tiles, per = quotient(units + blocks - 1, blocks);
-  const int64_t u0 = per * blockIdx.x, u1 = min(units, u0 + per);
-  if (blockIdx.x == 0 && tid == 0) w.starts[a.n_seqs + 1] = per;
+  // Row tiles that see the same keys go side by side, in blocks next to each other: each stretch of the keys is then read from
+  // memory once and found in L2 by the others.  (With more row tiles than blocks, all of them follow each other instead.)
+  const int side = blocks >= w.prefix_tiles ? w.prefix_tiles : 1, behind = side == 1 ? w.prefix_tiles : 1;
+  const int n = tiles_of(a.prefix_len, TC_KEYS), stretches = blocks / side;
+  const int64_t units = (int64_t)n * a.kv_heads * behind, per = quotient(units + stretches - 1, stretches);
+  const int64_t u0 = per * (blockIdx.x / side), u1 = min(units, u0 + per);
+  const int my_tile = blockIdx.x % side;
+  auto head_of = [&](int pair) { return pair / behind; };
+  auto first_row = [&](int pair) { return (side == 1 ? pair % behind : my_tile) * 256; };
+  if (blockIdx.x == 0 && tid == 0) w.starts[a.n_seqs] = side, w.starts[a.n_seqs + 1] = per;
   if (u0 >= u1) return;
   if (tid == 0) {
     for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(empty(s), 2);
@@ -929,7 +963,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
       const int boxes = TC_KEYS / maps.box;
       int it = 0;
       bool alive = true;
-      int pair = (int)quotient(u0, n), tile = (int)(u0 - (int64_t)pair * n), kh = pair / w.prefix_tiles;
+      int pair = (int)quotient(u0, n), tile = (int)(u0 - (int64_t)pair * n), kh = head_of(pair);
       auto look_up = [&](int t) {                          // this lane's page of tile t; -1: none
         const int key = t * TC_KEYS + lane * maps.box;
         return lane < boxes && key < a.prefix_len ? a.prefix_pages[key / a.in_page] & 0x7FFFFFFF : -1;
@@ -939,7 +973,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
         const int key = tile * TC_KEYS + lane * maps.box, head = kh;
         int page = page_next;
         const bool live = page >= 0;
-        if (++tile == n) tile = 0, kh = ++pair / w.prefix_tiles;
+        if (++tile == n) tile = 0, kh = head_of(++pair);
         if (u + 1 < u1) page_next = look_up(tile);         // arrives while this tile waits for room
         if (page >= a.n_pages) {                           // (a negative number has become a large one)
           page = a.n_pages;                                // outside the map: the box is filled with zeros
@@ -997,14 +1031,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
       for (int64_t u = u0; u < u1 && alive;) {
         const int pair = (int)(u / n), tile0 = (int)(u - (int64_t)pair * n), count = (int)min((int64_t)(n - tile0), u1 - u);
         u += count;
-        if (all - pair % w.prefix_tiles * 256 <= h * 128) {  // no rows for this half: the tiles pass by
+        if (all - first_row(pair) <= h * 128) {              // no rows for this half: the tiles pass by
           for (int x = 0; x < 2 * count && alive; x++, next()) {
             need(full(stage), lap);
             bar_arrive(empty(stage));
           }
           continue;
         }
-        const bool both = all - pair % w.prefix_tiles * 256 > 128;
+        const bool both = all - first_row(pair) > 128;
         need(q_full(h), seg++);
         need(full(stage), lap);
         if (!alive) break;
@@ -1065,8 +1099,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
     bool alive = true;
     for (int64_t u = u0; u < u1 && alive;) {
       const int pair = (int)(u / n), tile0 = (int)(u - (int64_t)pair * n), count = (int)min((int64_t)(n - tile0), u1 - u);
-      const int kh = pair / w.prefix_tiles, row = pair % w.prefix_tiles * 256 + h * 128 + r;
-      if (all - pair % w.prefix_tiles * 256 <= h * 128) {  // no rows for this half: the phases of its barriers stand still
+      const int kh = head_of(pair), row = first_row(pair) + h * 128 + r;
+      if (all - first_row(pair) <= h * 128) {              // no rows for this half: the phases of its barriers stand still
         u += count;
         continue;
       }
@@ -1225,12 +1259,14 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
   const int h = (int)(row - token * a.q_heads), i = (int)(token - seq * a.n_new), b = (int)seq;
   const int kh = h / a.in_group;
   // a pair's parts: its blocks c0 .. c0 + count - 1, or one result of its own
-  struct Parts { int64_t u0, c0, per; int count, r; bool whole; };
-  auto parts = [&](const Line &w, int r, int tiles, int64_t start, int n) {
-    Parts p = {0, 0, 0, 0, 0, false};
+  struct Parts { int64_t u0, c0, per; int count, r, side, lane; bool whole; };
+  auto parts = [&](const Line &w, int r, int tiles, int64_t start, int n, int side) {
+    Parts p = {0, 0, 0, 0, 0, side, 0, false};
     if (n) {
+      const int tile = r / w.rows;
       p.per = w.starts[a.n_seqs + 1];
-      p.u0 = start + (int64_t)(kh / w.heads * tiles + r / w.rows) * n;
+      p.lane = side > 1 ? tile : 0;                    // of `side` row tiles side by side
+      p.u0 = start + (int64_t)(side > 1 ? kh : kh / w.heads * tiles + tile) * n;
       p.r = kh % w.heads * w.rows + r % w.rows;
       p.c0 = quotient(p.u0, p.per);
       p.count = (int)(quotient(p.u0 + n - 1, p.per) - p.c0) + 1;
@@ -1239,8 +1275,9 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
     return p;
   };
   const int in = h - kh * a.group, n = tiles_of(own_len(a, b), lo.keys);
-  const Parts pre = parts(lp, (b * a.n_new + i) * a.group + in, lp.prefix_tiles, 0, tiles_of(a.prefix_len, lp.keys));
-  const Parts own = parts(lo, i * a.group + in, lo.own_tiles, n ? lo.starts[b] : 0, n);
+  const Parts pre = parts(lp, (b * a.n_new + i) * a.group + in, lp.prefix_tiles, 0, tiles_of(a.prefix_len, lp.keys),
+                          lp.side_by_side ? (int)lp.starts[a.n_seqs] : 1);
+  const Parts own = parts(lo, i * a.group + in, lo.own_tiles, n ? lo.starts[b] : 0, n, 1);
   if (a.prefix_len == 0 && own.whole) return;
   const int total = pre.count + own.count;
   float m = -INFINITY, l = 0.f, acc[E] = {};
@@ -1253,7 +1290,8 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
       const bool whole = mine ? own.whole : pre.whole;
       const int64_t c = mine ? own.c0 + x - pre.count : pre.c0 + x;
       const bool last = mine ? own.u0 > c * own.per : pre.u0 > c * pre.per;
-      const int64_t at = whole ? row : (c * 2 + last) * (mine ? lo.heads * lo.rows : lp.heads * lp.rows) + (mine ? own.r : pre.r);
+      const int64_t block = mine ? c : c * pre.side + pre.lane;
+      const int64_t at = whole ? row : (block * 2 + last) * (mine ? lo.heads * lo.rows : lp.heads * lp.rows) + (mine ? own.r : pre.r);
       o = (whole ? mine ? lo.whole_o[1] : lp.whole_o[0] : mine ? lo.cut_o : lp.cut_o) + at * D;
       ml = (whole ? mine ? lo.whole_ml[1] : lp.whole_ml[0] : mine ? lo.cut_ml : lp.cut_ml)[at];
     }
@@ -1367,7 +1405,7 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
   if (p.way == APART) line(p.prefix, 1, 64, KEYS, stream_blocks(D), true, false);
   if (p.way == TENSOR) {
     line(p.prefix, 1, 256, TC_KEYS, SMS, true, false);
-    p.own.beside_prefix = 1;
+    p.own.beside_prefix = 1, p.prefix.side_by_side = 1;
   }
   if (p.way == TOGETHER) p.prefix = p.own;
   if (d.prefix_len) {
