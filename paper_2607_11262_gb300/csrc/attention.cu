@@ -180,6 +180,7 @@ struct Line {           // the units of one launch
   int64_t *starts;      // [n_seqs + 2]: first unit of each sequence, the units of all, units per block
   float *cut_o;         // [blocks][2][heads][rows][D]: results of the first and last pair of a block that are cut
   float2 *cut_ml;       // [blocks][2][heads][rows]: maximum (of log2 scores) and sum
+  int4 *ends;           // [blocks]: the pair that begins in a block and goes on in the next ones, see k_join_cut
   float *whole_o[2];    // [rows of all][D], prefix and own: results of pairs that are not cut
   float2 *whole_ml[2];
 };
@@ -235,7 +236,7 @@ struct Place { int b, len, n, pairs, pair, tile; };
 // line, across the ends of pairs, and fills a ring of tiles: boxes of tokens by TMA where the pages allow it (see tile_map),
 // else rows gathered by 16-byte copies, else (caches off the 16-byte grid) by plain loads.  A pair's queries come with its
 // first tile.  (With four heads there are four such warps: issuing a tile's copies takes one of them 1600 cycles, the
-// products 1000.  256 threads start with 65536 / 256 / blocks registers, 128 or 80, and go on with 200 and 56 or 112 and 48.)
+// products 1000.  256 threads start with 128 registers each, 32768, and go on with 200 and 56.)
 // Of the others, WM stand along the rows (16 each) and 4 / WM along a tile's keys; they meet only where a pair
 // ends, to be joined in the stage just read.  Scores and weights stay in the fragments of m16n8k16 products, each warp with
 // its own running maximum and sum.  Weights are rounded to the type of the values for their product with them (the sum is of
@@ -246,11 +247,12 @@ template <int D, int WM, int WH> struct Ring {
   static constexpr int QUERIES = WH > 1 ? 0 : 16 * WM * D * 2;  // with four heads they go straight to registers
   static constexpr int SMEM = 1024 /* alignment */ + STAGES * (2 * TILE + QUERIES) + 64 * 8 + (2 * STAGES + 1) * 8 + 56;
 };
-__host__ __device__ constexpr int stream_threads(int WH) { return THREADS + 32 * WH; }
+// (at a head of 64 one warp has half the copies to issue, and is enough)
+__host__ __device__ constexpr int bringers(int D, int WH) { return D > 64 ? WH : 1; }
 __host__ __device__ constexpr int stream_per_sm(int D) { return D == 64 ? 3 : D == 128 ? 2 : 1; }
 
 template <typename T, int D, int WM, int WH>
-__global__ void __launch_bounds__(stream_threads(WH), stream_per_sm(D)) k_stream(const Args a, const Line w, const Line prefix, const __grid_constant__ Pages maps) {
+__global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(D)) k_stream(const Args a, const Line w, const Line prefix, const __grid_constant__ Pages maps) {
   using R = Ring<D, WM, WH>;
   static_assert(WH == 1 || (WH == WARPS && WM == 1), "a warp for each head, or all for one");
   constexpr int WK = WARPS / WM / WH, ROWS = 16 * WM, KU = KEYS / WH, KW = KU / WK, STAGES = R::STAGES, TILE = R::TILE;
@@ -269,7 +271,7 @@ __global__ void __launch_bounds__(stream_threads(WH), stream_per_sm(D)) k_stream
   auto empty = [&](int s) { return bar0 + (STAGES + s) * 8; };
   const uint32_t together = bar0 + 2 * STAGES * 8;
   if (tid == 0) {
-    for (int s = 0; s < STAGES; s++) bar_init(full(s), 33 * WH), bar_init(empty(s), WARPS);
+    for (int s = 0; s < STAGES; s++) bar_init(full(s), 33 * bringers(D, WH)), bar_init(empty(s), WARPS);
     bar_init(together, WARPS);
     *dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -321,6 +323,7 @@ __global__ void __launch_bounds__(stream_threads(WH), stream_per_sm(D)) k_stream
   }
   if (u0 >= u1) {
     // the kernel after this one waits for this one alone: so this one ends after the one before it
+    if (tid == 0) w.ends[blockIdx.x] = make_int4(-1, 0, 0, 0);
     if (blockIdx.x == 0) wait_for_kernels_before();
     return;
   }
@@ -367,22 +370,24 @@ __global__ void __launch_bounds__(stream_threads(WH), stream_per_sm(D)) k_stream
 
   if (warp >= WARPS) {
     // ---- the warp that brings the data (of one head: with four, there are four)
-    if constexpr (WH > 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(D == 64 ? 48 : 56));
+    constexpr int HB = WH / bringers(D, WH), RB = HB * KU;   // its heads, and rows of a tile
+    if constexpr (bringers(D, WH) > 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     const bool aligned = ((((uintptr_t)a.k | (uintptr_t)a.v) >> 1 | a.k_page | a.k_tok | a.k_head | a.v_page | a.v_tok | a.v_head) & 7) == 0;
     const bool q_aligned = (((uintptr_t)a.q >> 1 | a.q_seq | a.q_tok | a.q_head) & 7) == 0;
-    const int hh = warp - WARPS, box = maps.box, boxes = box ? KU / box : 0;
+    const int box = maps.box, boxes = box ? KU / box : 0;
+    const int hh = (warp - WARPS) * HB + (box ? lane / boxes : 0), at_box = box ? lane % boxes : 0;  // this lane's box and its head
     int page[2];                                       // of this lane's box, or of its two rows; -1: none
     auto look_up = [&](const Place &p) {
       const int32_t *pages = p.b < 0 ? a.prefix_pages : a.table + (int64_t)p.b * a.max_pages;
       page[0] = page[1] = -1;
       if (box) {
-        const int j = p.tile * KU + lane * box;
-        if (lane < boxes && j < p.len) page[0] = pages[j / a.in_page] & 0x7FFFFFFF;
+        const int j = p.tile * KU + at_box * box;
+        if (lane < boxes * HB && j < p.len) page[0] = pages[j / a.in_page] & 0x7FFFFFFF;
       } else {
 #pragma unroll
         for (int x = 0; x < 2; x++) {
-          const int j = p.tile * KU + lane + 32 * x;
-          if (lane + 32 * x < KU && j < p.len) page[x] = pages[j / a.in_page] & 0x7FFFFFFF;
+          const int j = p.tile * KU + (lane + 32 * x) % KU;
+          if (lane + 32 * x < RB && j < p.len) page[x] = pages[j / a.in_page] & 0x7FFFFFFF;
         }
       }
     };
@@ -414,10 +419,10 @@ __global__ void __launch_bounds__(stream_threads(WH), stream_per_sm(D)) k_stream
         if (lane == 0) bar_expect(full(stage), bytes);
         __syncwarp();
         if (live) {
-          const int token = (at.tile * KU + lane * box) % a.in_page, kh = group * WH + hh;
+          const int token = (at.tile * KU + at_box * box) % a.in_page, kh = group * WH + hh;
           const int k_y = maps.k_heads_first ? kh : token, k_z = maps.k_heads_first ? token : kh;
           const int v_y = maps.v_heads_first ? kh : token, v_z = maps.v_heads_first ? token : kh;
-          const uint32_t dst = to + (hh * KU + lane * box) * 128;
+          const uint32_t dst = to + (hh * KU + at_box * box) * 128;
 #pragma unroll
           for (int x = 0; x < D / 64; x++) {
             tile_load(dst + x * HALF, &maps.k, x * 64, k_y, k_z, to_load[0], full(stage));
@@ -426,18 +431,17 @@ __global__ void __launch_bounds__(stream_threads(WH), stream_per_sm(D)) k_stream
         }
       } else {
         if (lane == 0) bar_expect(full(stage), 0);
-        const int kh = group * WH + hh;
         int64_t k_off[2], v_off[2];                    // this lane's two rows
 #pragma unroll
         for (int x = 0; x < 2; x++) {
-          const int in = (at.tile * KU + lane + 32 * x) % a.in_page;
+          const int in = (at.tile * KU + (lane + 32 * x) % KU) % a.in_page, kh = group * WH + hh + (lane + 32 * x) / KU;
           k_off[x] = to_load[x] < 0 ? -1 : to_load[x] * a.k_page + in * a.k_tok + kh * a.k_head;
           v_off[x] = to_load[x] < 0 ? -1 : to_load[x] * a.v_page + in * a.v_tok + kh * a.v_head;
         }
 #pragma unroll
-        for (int x = 0; x < (KU + 31) / 32; x++) {
+        for (int x = 0; x < (RB + 31) / 32; x++) {
 #pragma unroll 4
-          for (int y = 0; y < min(32, KU); y++) {      // lanes along the row: D / 8 pieces of keys, then of values
+          for (int y = 0; y < min(32, RB); y++) {      // lanes along the row: D / 8 pieces of keys, then of values
             const int r = hh * KU + x * 32 + y;
             const int64_t k = __shfl_sync(~0u, k_off[x], y), v = __shfl_sync(~0u, v_off[x], y);
 #pragma unroll
@@ -494,7 +498,7 @@ __global__ void __launch_bounds__(stream_threads(WH), stream_per_sm(D)) k_stream
     }
   } else {
     // ---- the warps that compute
-    if constexpr (WH > 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(D == 64 ? 112 : 200));
+    if constexpr (bringers(D, WH) > 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
     const int wm = warp % WM, wk = warp / WM, wh = WH > 1 ? warp : 0, quad = lane / 4, t4 = lane % 4, mi = lane / 8, mr = lane % 8;
     const bool o_aligned = (((uintptr_t)a.out >> 1 | a.o_seq | a.o_tok | a.o_head) & 3) == 0;
     const float sl2 = a.scale * 1.4426950408889634f;   // scores in units of log 2
@@ -719,6 +723,9 @@ __global__ void __launch_bounds__(stream_threads(WH), stream_per_sm(D)) k_stream
       }
       if (now.tile == now.n - 1 || unit == count - 1) {
         const bool whole = tile0 == 0 && now.tile == now.n - 1;
+        if (tid == 0 && unit == count - 1)
+          w.ends[blockIdx.x] = tile0 > 0 || whole ? make_int4(-1, 0, 0, 0)
+                                                  : make_int4(now.b, now.pair, (int)quotient(now.n - 2 - now.tile + per, per), !first_pair);
         const bool final = whole && now.b >= 0 && a.prefix_len == 0;
         if constexpr (WH > 1) {
           // a pair ends here, and each warp has its head's rows
@@ -1243,57 +1250,25 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
-// Joins what a row's pairs left, prefix first, then the sequence's own keys, each in the order of its blocks: one warp a
-// row.  A row whose one pair was written whole, with no prefix, is done already.  Up to 32 parts at a time, a lane takes the
-// maximum and sum of one; then all lanes add up the parts' values, several loads in flight.
-template <typename T, int D>
-__global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, const Line lo) {
+// The result of a row from its parts, in their order: one warp.  Up to 32 parts at a time, a lane takes the maximum and sum of
+// one; then all lanes add up the parts' values, several loads in flight.
+struct Part {
+  const float *o;
+  float2 ml;
+};
+template <typename T, int D, typename F>
+__device__ __forceinline__ void join_row(const Args &a, int lane, int b, int i, int h, int total, F part) {
   constexpr int E = D / 32;
   using V = typename std::conditional<E == 2, float2, float4>::type;
   constexpr int NV = E * 4 / sizeof(V);
-  const int lane = threadIdx.x % 32;
-  const int64_t row = (int64_t)blockIdx.x * WARPS + threadIdx.x / 32;
-  if (row >= (int64_t)a.n_seqs * a.n_new * a.q_heads) return;
-  wait_for_kernels_before();
-  const int64_t token = quotient(row, a.q_heads), seq = quotient(token, a.n_new);
-  const int h = (int)(row - token * a.q_heads), i = (int)(token - seq * a.n_new), b = (int)seq;
-  const int kh = h / a.in_group;
-  // a pair's parts: its blocks c0 .. c0 + count - 1, or one result of its own
-  struct Parts { int64_t u0, c0, per; int count, r, side, lane; bool whole; };
-  auto parts = [&](const Line &w, int r, int tiles, int64_t start, int n, int side) {
-    Parts p = {0, 0, 0, 0, 0, side, 0, false};
-    if (n) {
-      const int tile = r / w.rows;
-      p.per = w.starts[a.n_seqs + 1];
-      p.lane = side > 1 ? tile : 0;                    // of `side` row tiles side by side
-      p.u0 = start + (int64_t)(side > 1 ? kh : kh / w.heads * tiles + tile) * n;
-      p.r = kh % w.heads * w.rows + r % w.rows;
-      p.c0 = quotient(p.u0, p.per);
-      p.count = (int)(quotient(p.u0 + n - 1, p.per) - p.c0) + 1;
-      p.whole = p.count == 1;
-    }
-    return p;
-  };
-  const int in = h - kh * a.group, n = tiles_of(own_len(a, b), lo.keys);
-  const Parts pre = parts(lp, (b * a.n_new + i) * a.group + in, lp.prefix_tiles, 0, tiles_of(a.prefix_len, lp.keys),
-                          lp.side_by_side ? (int)lp.starts[a.n_seqs] : 1);
-  const Parts own = parts(lo, i * a.group + in, lo.own_tiles, n ? lo.starts[b] : 0, n, 1);
-  if (a.prefix_len == 0 && own.whole) return;
-  const int total = pre.count + own.count;
   float m = -INFINITY, l = 0.f, acc[E] = {};
   for (int first = 0; first < total; first += 32) {
     const int x = first + lane;
     const float *o = nullptr;
     float2 ml = make_float2(-INFINITY, 0.f);
     if (x < total) {
-      const bool mine = x >= pre.count;
-      const bool whole = mine ? own.whole : pre.whole;
-      const int64_t c = mine ? own.c0 + x - pre.count : pre.c0 + x;
-      const bool last = mine ? own.u0 > c * own.per : pre.u0 > c * pre.per;
-      const int64_t block = mine ? c : c * pre.side + pre.lane;
-      const int64_t at = whole ? row : (block * 2 + last) * (mine ? lo.heads * lo.rows : lp.heads * lp.rows) + (mine ? own.r : pre.r);
-      o = (whole ? mine ? lo.whole_o[1] : lp.whole_o[0] : mine ? lo.cut_o : lp.cut_o) + at * D;
-      ml = (whole ? mine ? lo.whole_ml[1] : lp.whole_ml[0] : mine ? lo.cut_ml : lp.cut_ml)[at];
+      const auto p = part(x);
+      o = p.o, ml = p.ml;
     }
     float top = fmaxf(m, ml.x);
 #pragma unroll
@@ -1344,7 +1319,75 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
 #pragma unroll
     for (int k = 0; k < E; k++) dst[k] = e[k];
   }
-  if (a.lse && lane == 0) a.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  if (a.lse && lane == 0) a.lse[((int64_t)b * a.n_new + i) * a.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+}
+
+// With a prefix: every row, from the parts of its prefix pair and then of its sequence's own.
+template <typename T, int D>
+__global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, const Line lo) {
+  const int lane = threadIdx.x % 32;
+  const int64_t row = (int64_t)blockIdx.x * WARPS + threadIdx.x / 32;
+  if (row >= (int64_t)a.n_seqs * a.n_new * a.q_heads) return;
+  wait_for_kernels_before();
+  const int64_t token = quotient(row, a.q_heads), seq = quotient(token, a.n_new);
+  const int h = (int)(row - token * a.q_heads), i = (int)(token - seq * a.n_new), b = (int)seq;
+  const int kh = h / a.in_group;
+  // a pair's parts: its blocks c0 .. c0 + count - 1, or one result of its own
+  struct Parts { int64_t u0, c0, per; int count, r, side, lane; bool whole; };
+  auto parts = [&](const Line &w, int r, int tiles, int64_t start, int n, int side) {
+    Parts p = {0, 0, 0, 0, 0, side, 0, false};
+    if (n) {
+      const int tile = r / w.rows;
+      p.per = w.starts[a.n_seqs + 1];
+      p.lane = side > 1 ? tile : 0;                    // of `side` row tiles side by side
+      p.u0 = start + (int64_t)(side > 1 ? kh : kh / w.heads * tiles + tile) * n;
+      p.r = kh % w.heads * w.rows + r % w.rows;
+      p.c0 = quotient(p.u0, p.per);
+      p.count = (int)(quotient(p.u0 + n - 1, p.per) - p.c0) + 1;
+      p.whole = p.count == 1;
+    }
+    return p;
+  };
+  const int in = h - kh * a.group, n = tiles_of(own_len(a, b), lo.keys);
+  const Parts pre = parts(lp, (b * a.n_new + i) * a.group + in, lp.prefix_tiles, 0, tiles_of(a.prefix_len, lp.keys),
+                          lp.side_by_side ? (int)lp.starts[a.n_seqs] : 1);
+  const Parts own = parts(lo, i * a.group + in, lo.own_tiles, n ? lo.starts[b] : 0, n, 1);
+  join_row<T, D>(a, lane, b, i, h, pre.count + own.count, [&](int x) {
+    const bool mine = x >= pre.count;
+    const bool whole = mine ? own.whole : pre.whole;
+    const int64_t c = mine ? own.c0 + x - pre.count : pre.c0 + x;
+    const bool last = mine ? own.u0 > c * own.per : pre.u0 > c * pre.per;
+    const int64_t block = mine ? c : c * pre.side + pre.lane;
+    const int64_t at = whole ? row : (block * 2 + last) * (mine ? lo.heads * lo.rows : lp.heads * lp.rows) + (mine ? own.r : pre.r);
+    const float *o = (whole ? mine ? lo.whole_o[1] : lp.whole_o[0] : mine ? lo.cut_o : lp.cut_o) + at * D;
+    return Part{o, (whole ? mine ? lo.whole_ml[1] : lp.whole_ml[0] : mine ? lo.cut_ml : lp.cut_ml)[at]};
+  });
+}
+
+// Without one: the rows of the pairs that are cut, each from the block where it begins (Line::ends) to that where it ends,
+// and the rows of sequences without keys; the others are done.
+template <typename T, int D>
+__global__ void __launch_bounds__(THREADS) k_join_cut(const Args a, const Line w, const int cut_blocks) {
+  const int lane = threadIdx.x % 32, rows = w.heads * w.rows;
+  wait_for_kernels_before();
+  if ((int)blockIdx.x >= cut_blocks) {
+    const int b = (blockIdx.x - cut_blocks) * WARPS + threadIdx.x / 32;
+    if (b >= a.n_seqs || own_len(a, b) > 0) return;
+    for (int x = 0; x < a.n_new * a.q_heads; x++)
+      join_row<T, D>(a, lane, b, x / a.q_heads, x % a.q_heads, 0, [](int) { return Part{nullptr, make_float2(0.f, 0.f)}; });
+    return;
+  }
+  const int x = blockIdx.x * WARPS + threadIdx.x / 32, c = x / rows, r = x % rows;
+  if (c >= w.blocks) return;
+  const int4 end = w.ends[c];                          // sequence, pair, blocks after this one, 1 if it is not this block's first
+  if (end.x < 0 || end.x >= a.n_seqs || end.z < 0 || end.z >= w.blocks - c) return;  // (a block that gave up wrote none)
+  const int group = end.y / w.own_tiles, row = (end.y - group * w.own_tiles) * w.rows + r % w.rows;
+  if (row >= a.n_new * a.group) return;
+  const Row p = row_of(a, end.x, group * w.heads + r / w.rows, row);
+  join_row<T, D>(a, lane, p.b, p.i, p.h, 1 + end.z, [&](int y) {
+    const int64_t at = ((int64_t)(c + y) * 2 + (y ? 0 : end.w)) * rows + r;
+    return Part{w.cut_o + at * D, w.cut_ml[at]};
+  });
 }
 
 // ---------------------------------------------------------------- host side
@@ -1395,12 +1438,16 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
     w.has_prefix = has_prefix, w.has_own = has_own, w.heads = heads, w.rows = rows, w.keys = keys, w.blocks = blocks;
     w.prefix_tiles = (int)((all + rows - 1) / rows), w.own_tiles = (int)((own_rows + rows - 1) / rows);
     w.starts = (int64_t *)take(((size_t)d.n_seqs + 2) * 8);
+    w.ends = (int4 *)take((size_t)blocks * 16);
     w.cut_ml = (float2 *)take((size_t)blocks * 2 * heads * rows * 8);
     w.cut_o = (float *)take((size_t)blocks * 2 * heads * rows * D * 4);
   };
   const int own_tile = own_rows <= 16 ? 16 : own_rows <= 32 ? 32 : 64;
-  // few rows: a warp to each of four heads, which have nothing to join at the end, where the heads can be had by fours
-  const int heads = own_tile == 16 && D <= 128 && d.cache.kv_heads % WARPS == 0 ? WARPS : 1;
+  // Few rows: a warp to each of four heads, which have nothing to join at a pair's end, where the heads can be had by fours.
+  // Long sequences seldom end, and their tiles of 64 keys of one head come in larger boxes: 256 of 1..1024 tokens take 102 us by
+  // fours and 108 by ones, 128 of 1..4096 take 182 and 175.
+  const bool fours = own_tile == 16 && D <= 128 && d.cache.kv_heads % WARPS == 0 && (uint64_t)d.max_pages * d.cache.page_size <= 2048;
+  const int heads = fours ? WARPS : 1;
   line(p.own, heads, own_tile, KEYS / heads, stream_blocks(D), p.way == TOGETHER && d.prefix_len, true);
   if (p.way == APART) line(p.prefix, 1, 64, KEYS, stream_blocks(D), true, false);
   if (p.way == TENSOR) {
@@ -1485,7 +1532,7 @@ template <typename T, int D, int WM, int WH>
 cudaError_t stream(const Args &a, const Line &w, const Line &prefix, const Pages &maps, bool early, cudaStream_t s) {
   static std::atomic<uint64_t> granted{0};
   const cudaError_t e = grant(k_stream<T, D, WM, WH>, Ring<D, WM, WH>::SMEM, granted);
-  return e != cudaSuccess ? e : launch_kernel(k_stream<T, D, WM, WH>, w.blocks, stream_threads(WH), Ring<D, WM, WH>::SMEM, s, early, a, w, prefix, maps);
+  return e != cudaSuccess ? e : launch_kernel(k_stream<T, D, WM, WH>, w.blocks, THREADS + 32 * bringers(D, WH), Ring<D, WM, WH>::SMEM, s, early, a, w, prefix, maps);
 }
 
 template <typename T, int D>
@@ -1512,6 +1559,10 @@ cudaError_t run(const Args &a, const Plan &p, const Pages &maps, const Pages &ow
         : p.own.rows == 32 ? stream<T, D, 2, 1>(a, p.own, p.prefix, own_maps, early, s)
                            : stream<T, D, 4, 1>(a, p.own, p.prefix, own_maps, early, s);
   if (e != cudaSuccess) return e;
+  if (a.prefix_len == 0) {
+    const int cut_blocks = (p.own.blocks * p.own.heads * p.own.rows + WARPS - 1) / WARPS, empty = (a.n_seqs + WARPS - 1) / WARPS;
+    return launch_kernel(k_join_cut<T, D>, (unsigned)(cut_blocks + empty), THREADS, 0, s, true, a, p.own, cut_blocks);
+  }
   const int64_t rows = (int64_t)a.n_seqs * a.n_new * a.q_heads;
   return launch_kernel(k_join<T, D>, (unsigned)((rows + WARPS - 1) / WARPS), THREADS, 0, s, true, a, p.prefix, p.own);
 }
