@@ -171,7 +171,8 @@ def _empty(shape, dtype, device, stream):
 def _output(out, name, shape, like, stream):
     """(tensor, strides)"""
     if out is None:
-        out = _empty(shape, like.dtype, like.device, stream)
+        out = torch.empty(shape, dtype=like.dtype, device=like.device) if stream is None else \
+            _empty(shape, like.dtype, like.device, stream)
         return out, out.stride()
     got, strides = _tensor(out, name, len(shape), like)
     if got != shape:
@@ -291,7 +292,7 @@ def _rope_call(q, k, positions, rotary, transposed, out_q, out_k, stream):
         out_k = None
     out_q, qos = _output(out_q, "out_q", shape, q, stream)
     if T and (heads or kh):
-        gts._check(_load().gts_rope(_ROPE.pack(
+        gts._check((_lib or _load()).gts_rope(_ROPE.pack(
             T, heads, kh, dim, dt, pos, *rotary._values[transposed], q.data_ptr(), qs[0], qs[1], kp, ks[0], ks[1],
             out_q.data_ptr(), qos[0], qos[1], kop, kos[0], kos[1]), handle))
     return out_q, out_k
@@ -351,7 +352,7 @@ def append_kv(q, k, v, positions, slots, rotary, cache, out_q=None, status=None,
     st = _status(status, device)
     out_q, qos = _output(out_q, "out_q", shape, q, stream)
     if T:
-        gts._check(_load().gts_append_kv(_APPEND.pack(
+        gts._check((_lib or _load()).gts_append_kv(_APPEND.pack(
             T, heads, pos, at, *rotary._values[0], q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(),
             vs[0], vs[1], out_q.data_ptr(), qos[0], qos[1], *cache._values, st), handle))
     return out_q
@@ -404,7 +405,7 @@ def prefix_attention(q, cache, prefix_pages, prefix_len, page_table, lens, scale
     elif workspace.device != device or not workspace.is_contiguous():
         _refuse(f"workspace: contiguous on {device} wanted")
     if B and new:
-        gts._check(_load().gts_prefix_attention(_ATTENTION.pack(
+        gts._check((_lib or _load()).gts_prefix_attention(_ATTENTION.pack(
             B, new, heads, 1.0 / math.sqrt(dim) if scale is None else scale, q.data_ptr(), qs[0], qs[1], qs[2],
             out.data_ptr(), os[0], os[1], os[2], lse_at, *cache._values, prefix_at, prefix_len, table_at, max_pages, lens_at,
             workspace.data_ptr(), workspace.nbytes, st), handle))
