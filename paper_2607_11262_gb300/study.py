@@ -21,7 +21,11 @@ The policy study reruns workloads' design points under the per-subpartition
 issue policies (greedy-then-oldest, round-robin; Section 5.3) with 1, 2 and 4
 schedulers per SM and compares each makespan with the lowest-id order.
 
-    python -m paper_2607_11262_gb300.study [--study pipelines|noc|l2|policies] [--points-per-graph 64] [--json out.json]
+The decode study runs a decode step on the GPU itself (append to a paged cache with rotary positions, attention over a
+shared prefix), times its attention and simulates the same kernels' tile graph with a GB300 row (Section 6.2 compares
+measured and simulated attention kernels).
+
+    python -m paper_2607_11262_gb300.study [--study pipelines|noc|l2|policies|decode] [--points-per-graph 64] [--json out.json]
 """
 from __future__ import annotations
 
@@ -30,7 +34,7 @@ import json
 
 import numpy as np
 
-from . import clusters, gts, l2gemm, pipelines, workloads
+from . import clusters, decode, gts, l2gemm, pipelines, workloads
 
 
 def run_study(points_per_graph=1, device="cuda"):
@@ -126,6 +130,40 @@ def run_l2_study(device="cuda"):
     return rows
 
 
+def run_decode_study(cases=decode.CASES):
+    """Measured and simulated time of a decode step's attention; one dict per case."""
+    import torch
+    gts.load()
+    rows = []
+    for case in cases:
+        step = decode.Step(**case)
+        off = step.check()
+        q = step.append()
+        append_us, attend_us = step.time_us(step.append), step.time_us(lambda: step.attend(q))
+        del step
+        dg = gts.DeviceGraph(decode.graph(**case))
+        dp = gts.DeviceParams(dg, decode.gb300_params()[None])
+        out = gts.simulate(dg, dp, flags=0)
+        torch.cuda.synchronize()
+        if int(out.status[0]) != gts.GTS_OK:
+            raise gts.GtsError(int(out.status[0]), "the decode step did not simulate")
+        cycles = int(out.makespan[0])
+        dp.close()
+        dg.close()
+        rows.append(dict(case, append_us=append_us, attend_us=attend_us, cycles=cycles, simulated_us=cycles / decode.GHZ / 1e3,
+                         difference=off))
+    return rows
+
+
+def format_decode_table(rows):
+    lines = [f"{'sequences':>10}{'prefix':>8}{'own':>6}{'append us':>11}{'attention us':>14}{'simulated us':>14}{'sim / meas':>12}"
+             f"{'off (of rms)':>14}"]
+    for r in rows:
+        lines.append(f"{r['seqs']:>10}{r['prefix']:>8}{r['own']:>6}{r['append_us']:>11.1f}{r['attend_us']:>14.1f}"
+                     f"{r['simulated_us']:>14.1f}{r['simulated_us'] / r['attend_us']:>12.2f}{r['difference']:>14.4f}")
+    return "\n".join(lines)
+
+
 POLICY_CASES = (("gto", 1), ("gto", 2), ("gto", 4), ("rr", 1), ("rr", 2), ("rr", 4))
 
 
@@ -204,7 +242,7 @@ def format_table(rows):
 
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("--study", default="pipelines", choices=["pipelines", "noc", "l2", "policies"])
+    ap.add_argument("--study", default="pipelines", choices=["pipelines", "noc", "l2", "policies", "decode"])
     ap.add_argument("--points-per-graph", type=int, default=1)
     ap.add_argument("--json", default=None)
     args = ap.parse_args()
@@ -214,6 +252,9 @@ def main():
     elif args.study == "l2":
         rows = run_l2_study()
         print(format_l2_table(rows))
+    elif args.study == "decode":
+        rows = run_decode_study()
+        print(format_decode_table(rows))
     elif args.study == "policies":
         rows = run_policy_study(points=args.points_per_graph)
         print(format_policy_table(rows))

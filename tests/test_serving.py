@@ -181,3 +181,19 @@ def test_null_descriptors():
     for f in (lib.gts_rope, lib.gts_append_kv, lib.gts_prefix_attention):
         assert f(None, None) == gts.GTS_ERR_INVALID_ARG and "null" in gts.gts_last_error()
     assert lib.gts_attention_workspace_bytes(None) == 0
+
+
+def test_divisor_method():
+    """attention.cu's division by a multiplication: m = floor(2^(31 + l) / d) + 1, x m >> (31 + l), for every 31-bit x."""
+    rng = np.random.default_rng(3)
+    ds = sorted({*range(1, 300), 65535, 65536, 1000, *(int(d) for d in rng.integers(1, 65537, 300))})
+    for d in ds:
+        bits = (d - 1).bit_length()
+        if bits == 0:
+            continue
+        m = (1 << (31 + bits)) // d + 1
+        assert m < 1 << 32
+        q = np.array([0, 1, d - 1, d, d + 1, 2 ** 31 - 1, *(k * d + e for k in (1, 7, (2 ** 31 - 1) // d) for e in (-1, 0) if k * d + e < 2 ** 31),
+                      *rng.integers(0, 2 ** 31, 50)], np.int64)
+        got = np.array([(int(x) * m) >> 32 >> (bits - 1) for x in q])
+        assert np.array_equal(got, q // d), d
