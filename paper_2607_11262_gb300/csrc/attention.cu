@@ -199,11 +199,12 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
 
 // The prefix's kernel is bound by the tensor cores and holds whole SMs, the sequences' own keys are bound by memory: both run
 // at the same time, on SMs dealt out by the time each needs.  In units of an own tile's time on an SM (0.77 us measured at a
-// head of 128, 0.42 at 64): a tile of the prefix for 256 rows takes 2.2 (1.7 us) or 3.3 (1.4 us), the end of a pair 2; and own
+// head of 128, 0.42 at 64): a tile of the prefix for 256 rows takes 2.2 (1.7 us) or 3.3 (1.4 us), the end of a pair 2, own work
+// with tiles of 32 or 64 rows 1.4 or 1.8 times as long; and own
 // tiles alone cannot go faster than memory brings them, 104 to that time.  Both kernels come to the same numbers from the lengths.
 template <int D>
-__device__ __forceinline__ int prefix_sms(const Args &a, const Line &prefix, int64_t own_tiles, int64_t own_pairs) {
-  const float p = (D == 64 ? 3.3f : 2.2f) * tiles_of(a.prefix_len, 128) * a.kv_heads * prefix.prefix_tiles, o = own_tiles + 2.f * own_pairs;
+__device__ __forceinline__ int prefix_sms(const Args &a, const Line &prefix, int own_rows, int64_t own_tiles, int64_t own_pairs) {
+  const float p = (D == 64 ? 3.3f : 2.2f) * tiles_of(a.prefix_len, 128) * a.kv_heads * prefix.prefix_tiles, o = (own_tiles + 2.f * own_pairs) * (own_rows == 16 ? 1.f : own_rows == 32 ? 1.4f : 1.8f);
   if (own_tiles == 0) return SMS;
   const float each = fmaxf((p + o) / SMS, own_tiles / 104.f);
   return max(1, min(SMS - 1, (int)(p / each + 0.5f)));
@@ -309,7 +310,7 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
   int blocks = w.blocks;
   if (w.beside_prefix) {
     const int64_t pairs = (int64_t)(nonempty[0] + nonempty[1] + nonempty[2] + nonempty[3]) * own_pairs;
-    blocks = min(blocks, stream_per_sm(D) * (SMS - prefix_sms<D>(a, prefix, total, pairs)));
+    blocks = min(blocks, stream_per_sm(D) * (SMS - prefix_sms<D>(a, prefix, ROWS, total, pairs)));
   }
   const int64_t per = quotient(total + blocks - 1, max(blocks, 1));
   const int64_t u0 = per * blockIdx.x, u1 = min(total, u0 + per);
@@ -938,7 +939,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   int64_t own_tiles = 0, own_pairs = 0;
   for (int x = 0; x < TC_THREADS / 32; x++) own_tiles += own[x][0], own_pairs += own[x][1];
   const int pairs_each = a.kv_heads / own_line.heads * own_line.own_tiles;
-  const int blocks = prefix_sms<D>(a, w, own_tiles * pairs_each, own_pairs * pairs_each);
+  const int blocks = prefix_sms<D>(a, w, own_line.rows, own_tiles * pairs_each, own_pairs * pairs_each);
   // Row tiles that see the same keys go side by side, in blocks next to each other: each stretch of the keys is then read from
   // memory once and found in L2 by the others.  (With more row tiles than blocks, all of them follow each other instead.)
   const int side = blocks >= w.prefix_tiles ? w.prefix_tiles : 1, behind = side == 1 ? w.prefix_tiles : 1;
