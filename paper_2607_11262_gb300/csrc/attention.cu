@@ -310,9 +310,9 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
   int blocks = w.blocks;
   if (w.beside_prefix) {
     const int64_t pairs = (int64_t)(nonempty[0] + nonempty[1] + nonempty[2] + nonempty[3]) * own_pairs;
-    blocks = min(blocks, stream_per_sm(D) * (SMS - prefix_sms<D>(a, prefix, ROWS, total, pairs)));
+    blocks = max(1, min(blocks, stream_per_sm(D) * (SMS - prefix_sms<D>(a, prefix, ROWS, total, pairs))));
   }
-  const int64_t per = quotient(total + blocks - 1, max(blocks, 1));
+  const int64_t per = quotient(total + blocks - 1, blocks);
   const int64_t u0 = per * blockIdx.x, u1 = min(total, u0 + per);
   __syncthreads();
   if (blockIdx.x == 0 && tid < THREADS) {
@@ -1590,6 +1590,7 @@ const char *refuse_shape(const gts_attention_desc &d) {
     return "attention: 1 <= page_size <= 65536, at most 2^30 pages";
   if ((uint64_t)d.n_seqs * d.n_new > 65535 || d.n_seqs > 65535 || d.n_new > 65535)
     return "attention: n_seqs * n_new must be at most 65535";
+  if ((uint64_t)d.n_seqs * d.n_new * d.q_heads > 1u << 30) return "attention: more than 2^30 rows of queries";
   if (d.prefix_len > 1u << 30 || (uint64_t)d.max_pages * c.page_size > 1u << 30)
     return "attention: a prefix or a sequence of more than 2^30 tokens";
   return nullptr;
@@ -1631,6 +1632,9 @@ extern "C" gts_status gts_prefix_attention(const gts_attention_desc *d, void *st
   a.scale = d->scale;
   a.prefix_pages = d->prefix_pages, a.table = d->page_table, a.lens = d->lens;
   a.status = d->d_status;
+  if (((uintptr_t)d->q | (uintptr_t)d->out | (uintptr_t)c.k | (uintptr_t)c.v) % 2 ||
+      ((uintptr_t)d->lse | (uintptr_t)d->prefix_pages | (uintptr_t)d->page_table | (uintptr_t)d->lens | (uintptr_t)d->d_status) % 4)
+    return gts::fail(GTS_ERR_INVALID_ARG, "attention: tensor misaligned for its type");
   if (d->workspace_bytes < gts_attention_workspace_bytes(d))
     return gts::fail(GTS_ERR_NOMEM, "attention: workspace smaller than gts_attention_workspace_bytes");
   Pages maps = {}, own_maps = {};

@@ -276,8 +276,8 @@ def _rope_call(q, k, positions, rotary, transposed, out_q, out_k, stream):
     if dt is None:
         _refuse(f"q: bfloat16, float16 or float32 wanted, got {q.dtype}")
     T, heads, dim = shape
-    if dim != rotary.head_dim:
-        _refuse(f"q has heads of {dim}, the rotary of {rotary.head_dim}")
+    if dim != rotary.head_dim or rotary.units.device != device:
+        _refuse(f"q has heads of {dim} on {device}, the rotary is of {rotary.head_dim} on {rotary.units.device}")
     pos = _index(positions, "positions", (T,), torch.int32, device)
     kh, kp, kop, ks, kos = 0, 0, 0, (0, 0), (0, 0)
     if k is not None:
@@ -342,8 +342,8 @@ def append_kv(q, k, v, positions, slots, rotary, cache, out_q=None, status=None,
     device = q.device
     handle = _handle(stream, device)
     T, heads, dim = shape
-    if dim != cache.head_dim or dim != rotary.head_dim:
-        _refuse(f"heads of {dim} (q), {cache.head_dim} (cache) and {rotary.head_dim} (rotary)")
+    if dim != cache.head_dim or dim != rotary.head_dim or rotary.units.device != device:
+        _refuse(f"heads of {dim} (q), {cache.head_dim} (cache) and {rotary.head_dim} (rotary, on {rotary.units.device})")
     (kshape, ks), (vshape, vs) = _tensor(k, "k", 3, q), _tensor(v, "v", 3, q)
     if kshape != (T, cache.kv_heads, dim) or vshape != kshape:
         _refuse(f"k and v: {[T, cache.kv_heads, dim]} wanted, got {list(kshape)} and {list(vshape)}")

@@ -122,3 +122,14 @@ def test_calls_in_a_row_share_a_workspace():
     got = [serving.prefix_attention(**ps[i % 3], workspace=ws) for i in range(9)]
     for i, (o, l) in enumerate(got):
         assert torch.equal(o, want[i % 3][0]) and torch.equal(l, want[i % 3][1])
+
+
+def test_what_is_on_another_device_is_refused():
+    q, pos = torch.zeros(3, 2, 64, device="cuda", dtype=torch.float16), torch.zeros(3, dtype=torch.int32, device="cuda")
+    elsewhere = serving.Rotary(64, device="cpu")
+    cache = serving.PagedCache.empty(2, 16, 2, 64, torch.float16)
+    for call in (lambda: serving.rope(q, None, pos, elsewhere), lambda: serving.rope_grad(q, None, pos, elsewhere),
+                 lambda: serving.append_kv(q, q, q, pos, torch.arange(3, device="cuda"), elsewhere, cache)):
+        with pytest.raises(gts.GtsError) as e:
+            call()
+        assert e.value.status == gts.GTS_ERR_INVALID_ARG

@@ -197,3 +197,12 @@ def test_divisor_method():
                       *rng.integers(0, 2 ** 31, 50)], np.int64)
         got = np.array([(int(x) * m) >> 32 >> (bits - 1) for x in q])
         assert np.array_equal(got, q // d), d
+
+
+@pytest.mark.parametrize("kw", [dict(q=PTR + 1), dict(out=PTR + 1), dict(lse=PTR + 2), dict(lens=PTR + 1), dict(page_table=PTR + 2),
+                                dict(prefix_pages=PTR + 2), dict(d_status=PTR + 2), dict(cache=dict(k=PTR + 1)),
+                                dict(n_seqs=60000, q_heads=32768, cache=dict(kv_heads=8))])
+def test_attention_refuses_misaligned_tensors_and_too_many_rows(kw):
+    with pytest.raises(gts.GtsError) as e:
+        serving.gts_prefix_attention(_attention(**kw))
+    assert e.value.status == gts.GTS_ERR_INVALID_ARG
