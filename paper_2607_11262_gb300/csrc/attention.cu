@@ -199,12 +199,13 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
 
 // The prefix's kernel is bound by the tensor cores and holds whole SMs, the sequences' own keys are bound by memory: both run
 // at the same time, on SMs dealt out by the time each needs.  In units of an own tile's time on an SM (0.77 us measured at a
-// head of 128, 0.42 at 64): a tile of the prefix for 256 rows takes 2.2 (1.7 us) or 3.3 (1.4 us), the end of a pair 2, own work
-// with tiles of 32 or 64 rows 1.4 or 1.8 times as long; and own
-// tiles alone cannot go faster than memory brings them, 104 to that time.  Both kernels come to the same numbers from the lengths.
+// head of 128, 0.42 at 64): a tile of the prefix for 256 rows takes 2.2 (1.7 us) or 3.3 (1.4 us), begin and end of its pair 8,
+// the end of an own pair 3; own work with tiles of 32 or 64 rows 1.4 or 1.8 times as long; and own tiles alone cannot go faster
+// than memory brings them, 104 to that time.  Both kernels come to the same numbers from the lengths.
 template <int D>
 __device__ __forceinline__ int prefix_sms(const Args &a, const Line &prefix, int own_rows, int64_t own_tiles, int64_t own_pairs) {
-  const float p = (D == 64 ? 3.3f : 2.2f) * tiles_of(a.prefix_len, 128) * a.kv_heads * prefix.prefix_tiles, o = (own_tiles + 2.f * own_pairs) * (own_rows == 16 ? 1.f : own_rows == 32 ? 1.4f : 1.8f);
+  const float p = ((D == 64 ? 3.3f : 2.2f) * tiles_of(a.prefix_len, 128) + 8.f) * a.kv_heads * prefix.prefix_tiles;
+  const float o = (own_tiles + 3.f * own_pairs) * (own_rows == 16 ? 1.f : own_rows == 32 ? 1.4f : 1.8f);
   if (own_tiles == 0) return SMS;
   const float each = fmaxf((p + o) / SMS, own_tiles / 104.f);
   return max(1, min(SMS - 1, (int)(p / each + 0.5f)));
@@ -1409,9 +1410,8 @@ template <typename K> cudaError_t grant(K kernel, int bytes, std::atomic<uint64_
 
 size_t up(size_t x) { return (x + 255) / 256 * 256; }
 
-// How a call is run.  The prefix's rows (of all sequences) go to the tensor cores' kernel where its boxes fit the pages and
-// there are rows enough to fill its tiles; else to the streaming kernel, in the launch of the sequences' own keys or, with
-// many rows, in one of its own with tiles of 64 rows.
+// How a call is run.  The prefix's rows (of all sequences) go to the tensor cores' kernel where its boxes fit the pages; else to
+// the streaming kernel, in the launch of the sequences' own keys or, with many rows, in one of its own with tiles of 64 rows.
 enum Way { TOGETHER, APART, TENSOR };
 struct Plan {
   Way way;
@@ -1419,7 +1419,7 @@ struct Plan {
   size_t bytes;
 };
 
-constexpr int64_t TENSOR_ROWS = 48, APART_ROWS = 64;
+constexpr int64_t APART_ROWS = 64;
 
 int box_of(int page_size, int most) {  // tokens of a TMA box: the largest power of two that divides both the page and a tile
   int box = 1;
@@ -1433,7 +1433,10 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
   const int D = (int)d.cache.head_dim, group = (int)(d.q_heads / d.cache.kv_heads);
   const int64_t own_rows = (int64_t)d.n_new * group, all = own_rows * d.n_seqs;
   Plan p = {};
-  p.way = !d.prefix_len || all <= (tensor ? TENSOR_ROWS : APART_ROWS) || (!tensor && own_rows > 32) ? TOGETHER : tensor ? TENSOR : APART;
+  // On the tensor cores even few rows of the prefix go faster (4 rows over 8192 keys 23 us, in the streaming kernel 35; 512 over
+  // 256 43 and 47), except over the shortest prefixes, where a launch more costs what it gains.
+  tensor &= d.prefix_len >= 256 && d.prefix_len * (uint64_t)std::max<int64_t>(all, 16) >= 16384;
+  p.way = tensor ? TENSOR : d.prefix_len && all > APART_ROWS && own_rows <= 32 ? APART : TOGETHER;
   size_t n = 0;
   auto take = [&](size_t bytes) {
     char *x = at ? at + n : nullptr;
