@@ -244,6 +244,10 @@ struct Place { int b, len, n, pairs, pair, tile; };
 // ends, to be joined in the stage just read.  Scores and weights stay in the fragments of m16n8k16 products, each warp with
 // its own running maximum and sum.  Weights are rounded to the type of the values for their product with them (the sum is of
 // the unrounded ones); everything else is in 32 bits.
+//
+// Bound by memory for long sequences: 128 of up to 4096 tokens, 1.08 GB, 169 us, 6.4 TB/s, 94% of the rate of a copy; 256 of up
+// to 1024, 537 MB, 102 us, 78%, where the ends of pairs and the first tiles' latencies count.  Tiles of 32 and 64 rows (5 and 16
+// new tokens) are bound by the latency of their products with two warps to a scheduler: the same 537 MB in 188 and 385 us.
 template <int D, int WM, int WH> struct Ring {
   static constexpr int STAGES = (D == 64 ? 4 : 3) - (WM > 1);   // as many as stream_per_sm blocks find room for
   static constexpr int TILE = KEYS * D * 2;                     // bytes of a tile of keys or of values
@@ -901,6 +905,12 @@ constexpr uint32_t OPERAND_HI = 1024 >> 4 | 1u << 14 | 2u << 29;
 // are taken against is raised, and what was summed rescaled, only when it has grown by more than 8 (in log 2): weights stay
 // below 2^8, sums are exact in the same way, and the result is the same up to rounding.
 // Weights are rounded to the values' type for their product; the sum is of the unrounded ones, all else is in 32 bits.
+//
+// Bound by the chain of a half: products 1024 cycles, scores to weights 1250, handing over 330, so 2600 cycles for a tile of
+// 256 x 128 x 128 whose products take 2048.  What was tried: scores in pieces of 32 (shorter code, but a longer chain: 3200),
+// all 128 scores in registers (spills), one issuing thread for both halves (3200), no turns (3300), turns from the second part
+// of the weights on (7% slower).  128 x 4 rows over 131072 keys on 140 SMs: 185 us, 1.47 PFLOP/s, 84% of what cuBLAS sustains on
+// as many; 256 x 4 rows over 32768 on 75, beside the own keys' kernel: 165 us, 0.83.
 constexpr int TC_KEYS = 128, TC_THREADS = 352;
 constexpr float RAISE = 8.f;
 template <int D> struct Tc {
@@ -1329,7 +1339,8 @@ __device__ __forceinline__ void join_row(const Args &a, int lane, int b, int i, 
   if (a.lse && lane == 0) a.lse[((int64_t)b * a.n_new + i) * a.q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
-// With a prefix: every row, from the parts of its prefix pair and then of its sequence's own.
+// With a prefix: every row, from the parts of its prefix pair and then of its sequence's own.  Bound by L2: 8192 rows of 128 with
+// about 4 parts each, 22 MB, 5 us.
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, const Line lo) {
   const int lane = threadIdx.x % 32;
