@@ -199,12 +199,12 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
 
 // The prefix's kernel is bound by the tensor cores and holds whole SMs, the sequences' own keys are bound by memory: both run
 // at the same time, on SMs dealt out by the time each needs.  In units of an own tile's time on an SM (0.77 us measured at a
-// head of 128, 0.42 at 64): a tile of the prefix for 256 rows takes 2.2 (1.7 us) or 3.3 (1.4 us), begin and end of its pair 8,
+// head of 128, 0.42 at 64, 1.7 at 256): a tile of the prefix takes 2.2 (1.7 us), 3.3 (1.4 us) or 0.4 (0.7 us), begin and end of its pair 8 or 4,
 // the end of an own pair 3; own work with tiles of 32 or 64 rows 1.4 or 1.8 times as long; and own tiles alone cannot go faster
 // than memory brings them, 104 to that time.  Both kernels come to the same numbers from the lengths.
 template <int D>
 __device__ __forceinline__ int prefix_sms(const Args &a, const Line &prefix, int own_rows, int64_t own_tiles, int64_t own_pairs) {
-  const float p = ((D == 64 ? 3.3f : 2.2f) * tiles_of(a.prefix_len, 128) + 8.f) * a.kv_heads * prefix.prefix_tiles;
+  const float p = ((D == 64 ? 3.3f : D == 128 ? 2.2f : 0.4f) * tiles_of(a.prefix_len, prefix.keys) + (D == 256 ? 4.f : 8.f)) * a.kv_heads * prefix.prefix_tiles;
   const float o = (own_tiles + 3.f * own_pairs) * (own_rows == 16 ? 1.f : own_rows == 32 ? 1.4f : 1.8f);
   if (own_tiles == 0) return SMS;
   const float each = fmaxf((p + o) / SMS, own_tiles / 104.f);
@@ -911,21 +911,28 @@ constexpr uint32_t OPERAND_HI = 1024 >> 4 | 1u << 14 | 2u << 29;
 // all 128 scores in registers (spills), one issuing thread for both halves (3200), no turns (3300), turns from the second part
 // of the weights on (7% slower).  128 x 4 rows over 131072 keys on 140 SMs: 185 us, 1.47 PFLOP/s, 84% of what cuBLAS sustains on
 // as many; 256 x 4 rows over 32768 on 75, beside the own keys' kernel: 165 us, 0.83.
-constexpr int TC_KEYS = 128, TC_THREADS = 352;
+//
+// A head of 256 has room for one half in tensor memory (256 columns of sums): 128 rows, tiles of 64 keys, and two buffers of
+// scores, so that the products of the next tile's scores run while the rows make their weights.
+constexpr int TC_THREADS = 352;
 constexpr float RAISE = 8.f;
 template <int D> struct Tc {
-  static constexpr int TILE = TC_KEYS * D * 2, STAGES = D == 64 ? 8 : 5, Q = 2 * 128 * D * 2;
+  static constexpr bool SINGLE = D == 256;
+  static constexpr int KEYS = SINGLE ? 64 : 128, ROWS = SINGLE ? 128 : 256;
+  static constexpr int TILE = KEYS * D * 2, STAGES = D == 64 ? 8 : 5, Q = ROWS * D * 2;
   static constexpr int SMEM = Q + STAGES * TILE + 1024 /* alignment */ + 256 /* barriers */;
 };
 
 template <typename T, int D>
 __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Line w, const Line own_line, const __grid_constant__ Pages maps, const uint32_t flip) {
-  constexpr int TILE = Tc<D>::TILE, STAGES = Tc<D>::STAGES, HALF = TC_KEYS * 128;   // 64 columns of a tile
+  constexpr bool SINGLE = Tc<D>::SINGLE;
+  constexpr int TC_KEYS = Tc<D>::KEYS, TILE = Tc<D>::TILE, STAGES = Tc<D>::STAGES;
+  constexpr int HALF = TC_KEYS * 128, QHALF = 128 * 128;       // 64 columns of a tile, of a half's queries
   extern __shared__ unsigned char smem_raw[];
   unsigned char *const smem = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   unsigned char *const qs = smem, *const ring = smem + Tc<D>::Q;
   uint64_t *const bars = (uint64_t *)(ring + STAGES * TILE);
-  uint32_t *const tmem_at = (uint32_t *)(bars + 2 * STAGES + 12);
+  uint32_t *const tmem_at = (uint32_t *)(bars + 2 * STAGES + 13);
   volatile int *const dead = (volatile int *)(tmem_at + 1);
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), q_at = smem_u32(qs), ring_at = smem_u32(ring);
@@ -936,6 +943,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   auto p_full = [&](int h, int q) { return bar0 + (2 * STAGES + 4 + h * 2 + q) * 8; };  // of half the keys
   const uint32_t ended = bar0 + (2 * STAGES + 8) * 8;
   auto my_turn = [&](int h) { return bar0 + (2 * STAGES + 10 + h) * 8; };
+  const uint32_t o_full = bar0 + (2 * STAGES + 12) * 8;
   dependents_may_start();                              // the sequences' own keys need nothing from here
   __shared__ int own[TC_THREADS / 32][2];              // of each warp: sequences' tiles, sequences that have any
   int tiles = 0, some = 0;
@@ -959,11 +967,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   const int64_t u0 = per * (blockIdx.x / side), u1 = min(units, u0 + per);
   const int my_tile = blockIdx.x % side;
   auto head_of = [&](int pair) { return pair / behind; };
-  auto first_row = [&](int pair) { return (side == 1 ? pair % behind : my_tile) * 256; };
+  auto first_row = [&](int pair) { return (side == 1 ? pair % behind : my_tile) * Tc<D>::ROWS; };
   if (blockIdx.x == 0 && tid == 0) w.starts[a.n_seqs] = side, w.starts[a.n_seqs + 1] = per;
   if (u0 >= u1) return;
   if (tid == 0) {
-    for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(empty(s), 2);
+    for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(empty(s), SINGLE ? 1 : 2);
+    bar_init(o_full, 1);
     for (int h = 0; h < 2; h++) bar_init(ended + 8 * h, 1), bar_init(my_turn(h), 1), bar_init(q_full(h), 128), bar_init(s_full(h), 1), bar_init(p_full(h, 0), 128), bar_init(p_full(h, 1), 128);
     *dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -976,7 +985,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   __syncthreads();
   tc_after();
   const uint32_t tmem = __shfl_sync(~0u, *tmem_at, 0);
-  auto scores = [&](int h) { return tmem + h * 128; };
+  auto scores = [&](int h) { return tmem + h * TC_KEYS; };       // of a half, or a buffer
   auto sums = [&](int h) { return tmem + 256 + h * 128; };
 
   const int all = a.n_seqs * a.n_new * a.group;
@@ -1027,7 +1036,69 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
         for (int x = first; x < it; x++)
           while (!bar_try(full(x % STAGES), (x / STAGES) & 1) && now_ns() - from < LIMIT_NS) {}
       }
-    } else if (warp != 9 && elected()) {
+    } else if (SINGLE && warp == 8 && elected()) {
+      // ---- products of the one half: scores a tile ahead, in two buffers
+      constexpr uint32_t TYPE = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+      constexpr uint32_t COMMON = 1u << 4 | TYPE << 7 | TYPE << 10 | (128u >> 4) << 24;
+      constexpr uint32_t QK = COMMON | (TC_KEYS >> 3) << 17, PV = COMMON | 1u << 16 | (D >> 3) << 17;
+      const uint32_t k_op = operand(ring_at, 16), v_op = operand(ring_at, HALF), q_op = operand(q_at, 16);
+      uint32_t seg = 0, turn = 0, made[2] = {0, 0};        // pairs, tiles (and ends of pairs), weights in each buffer so far
+      uint32_t at = 0;                                     // place in the ring: a tile's keys, then its values
+      bool alive = true;
+      auto need = [&](uint32_t bar, uint32_t parity) { alive = alive && bar_wait(bar, parity & 1, dead); };
+      auto qk = [&](uint32_t place, uint32_t t) {
+        const int s = place % STAGES;
+        need(full(s), place / STAGES);
+        if (!alive) return;
+        tc_after();
+        uint32_t q = q_op, k = k_op + ((s * TILE) >> 4);
+        const uint32_t to = scores(t & 1);
+#pragma unroll 1
+        for (int x = 0; x < D / 64; x++, q += QHALF >> 4, k += HALF >> 4) {
+#pragma unroll
+          for (int y = 0; y < 4; y++) tc_mma(to, q + 2 * y, k + 2 * y, OPERAND_HI, QK, x + y > 0);
+        }
+        tc_commit(s_full(t & 1));
+        tc_commit(empty(s));
+      };
+      for (int64_t u = u0; u < u1 && alive;) {
+        const int pair = (int)(u / n), tile0 = (int)(u - (int64_t)pair * n), count = (int)min((int64_t)(n - tile0), u1 - u);
+        u += count;
+        need(q_full(0), seg++);
+        if (!alive) break;
+        qk(at, turn);
+        if (count > 1 && alive) qk(at + 2, turn + 1);
+        for (int j = 0; j < count && alive; j++, turn++, at += 2) {
+          const int sv = (at + 1) % STAGES, b = turn & 1, nv = a.prefix_len - (tile0 + j) * TC_KEYS;
+          need(full(sv), (at + 1) / STAGES);
+          if (nv < TC_KEYS && nv % 16 && alive) {          // value rows past the end, in the last 16 that count: zeros
+            for (int x = 0; x < (16 - nv % 16) * (D / 8); x++) {
+              const int r = nv + x / (D / 8), c = x % (D / 8);
+              *(uint4 *)(ring + sv * TILE + c / 8 * HALF + r * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
+            }
+            fence_async();
+          }
+          need(p_full(b, 0), b ? made[1]++ : made[0]++);
+          if (!alive) break;
+          tc_after();
+          const uint32_t v = v_op + ((sv * TILE) >> 4), w_at = scores(b);
+#pragma unroll
+          for (int k = 0; k < TC_KEYS / 16; k++)
+            if (k * 16 < nv) tc_mma_t(sums(0), w_at + k * 8, v + k * (2048 >> 4), OPERAND_HI, PV, j + k > 0);
+          tc_commit(o_full);
+          tc_commit(empty(sv));
+          if (j + 2 < count) qk(at + 4, turn + 2);
+        }
+        if (!alive) break;
+        tc_commit(s_full(turn & 1));                       // the pair's sums are complete
+        turn++;
+      }
+      if (!alive) {                                        // products in flight end before the block does
+        tc_commit(ended);
+        const uint64_t from = now_ns();
+        while (!bar_try(ended, 0) && now_ns() - from < LIMIT_NS) {}
+      }
+    } else if (!SINGLE && warp != 9 && elected()) {
       // ---- products, from one thread for each half of the rows (one thread for both would set the time)
       constexpr uint32_t TYPE = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
       constexpr uint32_t COMMON = 1u << 4 | TYPE << 7 | TYPE << 10 | (128u >> 4) << 24;
@@ -1045,7 +1116,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
       auto qk = [&](int s) {
         uint32_t q = q_op, k = k_op + ((s * TILE) >> 4);
 #pragma unroll
-        for (int x = 0; x < D / 64; x++, q += HALF >> 4, k += HALF >> 4) {
+        for (int x = 0; x < D / 64; x++, q += QHALF >> 4, k += HALF >> 4) {
 #pragma unroll
           for (int y = 0; y < 4; y++) tc_mma(s_at, q + 2 * y, k + 2 * y, OPERAND_HI, QK, x + y > 0);
         }
@@ -1113,13 +1184,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
         while (!bar_try(ended + 8 * h, 0) && now_ns() - from < LIMIT_NS) {}
       }
     }
-  } else {
+  } else if (!SINGLE || warp < 4) {
     // ---- one row a thread
     const int h = warp / 4, r = tid % 128;
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
     const float sl2 = fabsf(a.scale) * 1.4426950408889634f;
     const bool q_aligned = (((uintptr_t)a.q >> 1 | a.q_seq | a.q_tok | a.q_head) & 7) == 0;
-    uint32_t turn = 0;                                   // phases of s_full: a pair's tiles, then its sums
+    uint32_t turn = 0, tiles_done = 0;                   // phases of s_full: a pair's tiles, then its sums
     bool alive = true;
     for (int64_t u = u0; u < u1 && alive;) {
       const int pair = (int)(u / n), tile0 = (int)(u - (int64_t)pair * n), count = (int)min((int64_t)(n - tile0), u1 - u);
@@ -1152,14 +1223,15 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
       for (int x = 0; x < D / 8; x++) {
         const int c = lane % (D / 8), at = warp % 4 * 32 + (x * 32 + lane) / (D / 8);
         v[x].x ^= flip, v[x].y ^= flip, v[x].z ^= flip, v[x].w ^= flip;   // a negative scale: its sign goes to the queries
-        *(uint4 *)(qs + h * (Tc<D>::Q / 2) + c / 8 * HALF + at * 128 + ((c % 8) ^ (at & 7)) * 16) = v[x];
+        *(uint4 *)(qs + h * (Tc<D>::Q / 2) + c / 8 * QHALF + at * 128 + ((c % 8) ^ (at & 7)) * 16) = v[x];
       }
       fence_async();
       bar_arrive(q_full(h));
 
       float m = -INFINITY, l = 0.f;
-      for (int j = 0; j < count; j++, turn++) {
-        alive = __all_sync(~0u, bar_wait(s_full(h), turn & 1, dead));
+      for (int j = 0; j < count; j++, turn++, tiles_done++) {
+        const int b = SINGLE ? turn & 1 : h;               // the buffer of scores
+        alive = __all_sync(~0u, bar_wait(s_full(b), (SINGLE ? turn >> 1 : turn) & 1, dead));
         if (!alive) break;
         tc_after();
         const int nv = a.prefix_len - (tile0 + j) * TC_KEYS;
@@ -1167,8 +1239,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
         // shorter pieces add their latencies.
         uint32_t s[64];
         auto fetch = [&](int c) {
-          tc_ld(s, scores(h) + lanes + c);
-          tc_ld(s + 32, scores(h) + lanes + c + 32);
+          tc_ld(s, scores(b) + lanes + c);
+          tc_ld(s + 32, scores(b) + lanes + c + 32);
           tc_ld_wait();
           if (c + 64 > nv) {
 #pragma unroll
@@ -1178,7 +1250,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
         };
         float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-        for (int q = 0; q < 2; q++) {
+        for (int q = 0; q < TC_KEYS / 64; q++) {
           fetch(q * 64);
 #pragma unroll
           for (int c = 0; c < 64; c += 8) {
@@ -1192,6 +1264,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
           m = big;
         } else if (__any_sync(~0u, raise)) {
           const float to = raise ? big : m, f = raise ? exp2_fast(m - to) : 1.f;
+          if (SINGLE) {                                    // the scores were ahead: the last product with values may not be done
+            alive = __all_sync(~0u, bar_wait(o_full, (tiles_done - 1) & 1, dead));
+            if (!alive) break;
+            tc_after();
+          }
           uint32_t o[32];
 #pragma unroll 1
           for (int c = 0; c < D / 32; c++) {
@@ -1208,9 +1285,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
         const float2 scale2 = make_float2(sl2, sl2), from2 = make_float2(-from, -from);
         float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-        for (int q = 0; q < 2; q++) {                    // the products with the first 64 weights start under the others
+        for (int q = 0; q < TC_KEYS / 64; q++) {         // the products with the first 64 weights start under the others
           uint32_t pk[32];
-          fetch(q * 64);
+          if (!SINGLE) fetch(q * 64);
 #pragma unroll
           for (int c = 0; c < 64; c += 2) {
             float2 x = fma2(make_float2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), scale2, from2);
@@ -1218,22 +1295,22 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
             part[c / 2 & 1] = add2(part[c / 2 & 1], x);
             pk[c / 2] = pack<T>(x.x, x.y);
           }
-          tc_st(scores(h) + lanes + q * 32, pk);
+          tc_st(scores(b) + lanes + q * 32, pk);
           tc_st_wait();
           tc_before();
-          bar_arrive(p_full(h, q));
+          bar_arrive(p_full(b, q));
         }
         const float2 both = add2(part[0], part[1]);
         l += both.x + both.y;
       }
       if (!alive) break;
-      alive = __all_sync(~0u, bar_wait(s_full(h), turn & 1, dead));
+      alive = __all_sync(~0u, SINGLE ? bar_wait(s_full(turn & 1), turn >> 1 & 1, dead) : bar_wait(s_full(h), turn & 1, dead));
       turn++;
       if (!alive) break;
       tc_after();
       const bool whole = count == n;
       const int64_t at = whole ? ((int64_t)p.b * a.n_new + p.i) * a.q_heads + p.h
-                               : ((int64_t)blockIdx.x * 2 + (u > u0)) * 256 + h * 128 + r;
+                               : ((int64_t)blockIdx.x * 2 + (u > u0)) * Tc<D>::ROWS + h * 128 + r;
       // the sums, 32 columns at a time, through the warp's part of the queries' room (all products with them are done), so
       // that a store covers whole lines
       const unsigned long long to = row < all ? (unsigned long long)((whole ? w.whole_o[0] : w.cut_o) + at * D) : 0;
@@ -1446,7 +1523,9 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
   Plan p = {};
   // On the tensor cores even few rows of the prefix go faster (4 rows over 8192 keys 23 us, in the streaming kernel 35; 512 over
   // 256 43 and 47), except over the shortest prefixes, where a launch more costs what it gains.
-  tensor &= d.prefix_len >= 256 && d.prefix_len * (uint64_t)std::max<int64_t>(all, 16) >= 16384;
+  // At a head of 256, with smaller tiles, from 32 rows on (16 over 8192 keys take 37 us here and 34 there, 256 over 512 70 and 77, 512
+  // over 32768 229 and 705).
+  tensor &= d.prefix_len >= 256 && d.prefix_len * (uint64_t)std::max<int64_t>(all, 16) >= 16384 && (D < 256 || all >= 32);
   p.way = tensor ? TENSOR : d.prefix_len && all > APART_ROWS && own_rows <= 32 ? APART : TOGETHER;
   size_t n = 0;
   auto take = [&](size_t bytes) {
@@ -1471,7 +1550,7 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
   line(p.own, heads, own_tile, KEYS / heads, stream_blocks(D), p.way == TOGETHER && d.prefix_len, true);
   if (p.way == APART) line(p.prefix, 1, 64, KEYS, stream_blocks(D), true, false);
   if (p.way == TENSOR) {
-    line(p.prefix, 1, 256, TC_KEYS, SMS, true, false);
+    line(p.prefix, 1, D == 256 ? Tc<256>::ROWS : Tc<128>::ROWS, D == 256 ? Tc<256>::KEYS : Tc<128>::KEYS, SMS, true, false);
     p.own.beside_prefix = 1, p.prefix.side_by_side = 1;
   }
   if (p.way == TOGETHER) p.prefix = p.own;
@@ -1486,8 +1565,6 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
   return p;
 }
 
-// The shape's part of the rule for the tensor cores' kernel; tile_maps has the pointers' and strides' part.
-bool tensor_shape(const gts_attention_desc &d) { return d.cache.head_dim <= 128; }
 
 typedef CUresult (*EncodeTiled)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                                 const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
@@ -1566,9 +1643,7 @@ template <typename T, int D>
 cudaError_t run(const Args &a, const Plan &p, const Pages &maps, const Pages &own_maps, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
   if (p.way == APART) e = stream<T, D, 4, 1>(a, p.prefix, p.prefix, own_maps, false, s);
-  if constexpr (D <= 128) {
-    if (p.way == TENSOR) e = tensor<T, D>(a, p.prefix, p.own, maps, s);
-  }
+  if (p.way == TENSOR) e = tensor<T, D>(a, p.prefix, p.own, maps, s);
   if (e != cudaSuccess) return e;
   const bool early = p.way != TOGETHER;
   if constexpr (D <= 128) {
@@ -1614,7 +1689,7 @@ const char *refuse_shape(const gts_attention_desc &d) {
 
 extern "C" size_t gts_attention_workspace_bytes(const gts_attention_desc *d) {
   if (!d || refuse_shape(*d)) return 0;
-  return std::max(make_plan(*d, false, nullptr).bytes, make_plan(*d, tensor_shape(*d), nullptr).bytes);
+  return std::max(make_plan(*d, false, nullptr).bytes, make_plan(*d, true, nullptr).bytes);
 }
 
 extern "C" gts_status gts_prefix_attention(const gts_attention_desc *d, void *stream) {
@@ -1653,8 +1728,8 @@ extern "C" gts_status gts_prefix_attention(const gts_attention_desc *d, void *st
     return gts::fail(GTS_ERR_NOMEM, "attention: workspace smaller than gts_attention_workspace_bytes");
   Pages maps = {}, own_maps = {};
   // (a scale of 0 would turn the -infinity of masked scores into NaN on the tensor cores)
-  const bool mapped = tile_maps(maps, c, TC_KEYS);
-  const Plan p = make_plan(*d, mapped && d->scale != 0.f && tensor_shape(*d), (char *)d->workspace);
+  const bool mapped = tile_maps(maps, c, c.head_dim == 256 ? Tc<256>::KEYS : Tc<128>::KEYS);
+  const Plan p = make_plan(*d, mapped && d->scale != 0.f, (char *)d->workspace);
   if (mapped) tile_maps(own_maps, c, p.own.keys);
   const cudaError_t e = c.dtype == GTS_BF16 ? launch<__nv_bfloat16>(a, p, maps, own_maps, c.head_dim, (cudaStream_t)stream)
                                             : launch<__half>(a, p, maps, own_maps, c.head_dim, (cudaStream_t)stream);

@@ -133,3 +133,21 @@ def test_what_is_on_another_device_is_refused():
         with pytest.raises(gts.GtsError) as e:
             call()
         assert e.value.status == gts.GTS_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("prefix", [256, 257, 272, 300, 383, 1000])
+@pytest.mark.parametrize("kw", [dict(), dict(spread=60.0), dict(rubbish=float("inf"))])
+def test_prefix_ends_anywhere_in_a_tile(D, prefix, kw):
+    """Many rows, so that the tensor cores' kernel takes the prefix; its last tile of any length, scores that keep raising the
+    maximum, rubbish in the rest of the pages."""
+    for scale in (None, -0.1):
+        check_attention(problem(prefix, 16, 4, D, 16, "tokens", "float16", prefix, [3 + b % 40 for b in range(70)], 1, **kw), "float16",
+                        scale=scale)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_few_key_heads_and_a_long_prefix(D):
+    """One pair of rows cut over all blocks, and pairs that begin and end inside a block."""
+    check_attention(problem(1, 33, 1, D, 32, "heads", "bfloat16", 9000, [5, 0, 17], 1), "bfloat16")
+    check_attention(problem(2, 40, 40, D, 32, "tokens", "bfloat16", 400, [5, 0, 17] * 14, 1), "bfloat16")
