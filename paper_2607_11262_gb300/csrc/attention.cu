@@ -909,7 +909,8 @@ constexpr uint32_t OPERAND_HI = 1024 >> 4 | 1u << 14 | 2u << 29;
 // Bound by the chain of a half: products 1024 cycles, scores to weights 1250, handing over 330, so 2600 cycles for a tile of
 // 256 x 128 x 128 whose products take 2048.  What was tried: scores in pieces of 32 (shorter code, but a longer chain: 3200),
 // all 128 scores in registers (spills), one issuing thread for both halves (3200), no turns (3300), turns from the second part
-// of the weights on (7% slower).  128 x 4 rows over 131072 keys on 140 SMs: 185 us, 1.47 PFLOP/s, 84% of what cuBLAS sustains on
+// of the weights on (7% slower), tiles of 64 keys with scores a tile ahead as at a head of 256 (8% slower: products of 64
+// columns wait for shared memory).  128 x 4 rows over 131072 keys on 140 SMs: 185 us, 1.47 PFLOP/s, 84% of what cuBLAS sustains on
 // as many; 256 x 4 rows over 32768 on 75, beside the own keys' kernel: 165 us, 0.83.
 //
 // A head of 256 has room for one half in tensor memory (256 columns of sums): 128 rows, tiles of 64 keys, and two buffers of
