@@ -116,16 +116,16 @@ def _refuse(msg):
     raise GtsError(gts.GTS_ERR_INVALID_ARG, msg)
 
 
-def _tensor(t, name, dims, like=None):
-    """Shape and strides of a tensor with a contiguous innermost dimension on the current device (or like another)."""
+def _tensor(t, name, dims, dtype=None, device=None):
+    """Shape and strides of a tensor with a contiguous innermost dimension on a CUDA device (or of a type, on a device)."""
     shape = t.shape
     if len(shape) != dims:
         _refuse(f"{name}: {dims} dimensions wanted, got {len(shape)}")
-    if like is None:
+    if device is None:
         if not t.is_cuda:
             _refuse(f"{name} is not on a CUDA device")
-    elif t.dtype != like.dtype or t.device != like.device:
-        _refuse(f"{name}: {like.dtype} on {like.device} wanted, got {t.dtype} on {t.device}")
+    elif t.device != device or t.dtype != dtype:
+        _refuse(f"{name}: {dtype} on {device} wanted, got {t.dtype} on {t.device}")
     strides = t.stride()
     if strides[-1] != 1 and shape[-1] > 1:
         _refuse(f"{name}: the innermost dimension must be contiguous")
@@ -147,14 +147,16 @@ def _status(t, device):
     return 0 if t is None else _index(t, "status", (1,), torch.int32, device)
 
 
+# (the same as torch.cuda's functions, without their checks for a first use of CUDA: a CUDA tensor exists here)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _handle(stream, device):
     """The stream's handle, for tensors that have to be on the current device."""
     index = device.index
-    if index != torch.cuda.current_device():
-        _refuse(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
+    if index != _current_device():
+        _refuse(f"tensors are on {device}, the current device is cuda:{_current_device()}")
     if stream is not None:
         return stream.cuda_stream
     return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
@@ -168,13 +170,12 @@ def _empty(shape, dtype, device, stream):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _output(out, name, shape, like, stream):
+def _output(out, name, shape, dtype, device, stream):
     """(tensor, strides)"""
     if out is None:
-        out = torch.empty(shape, dtype=like.dtype, device=like.device) if stream is None else \
-            _empty(shape, like.dtype, like.device, stream)
+        out = torch.empty(shape, dtype=dtype, device=device) if stream is None else _empty(shape, dtype, device, stream)
         return out, out.stride()
-    got, strides = _tensor(out, name, len(shape), like)
+    got, strides = _tensor(out, name, len(shape), dtype, device)
     if got != shape:
         _refuse(f"{name}: {list(shape)} wanted, got {list(got)}")
     return out, strides
@@ -207,6 +208,7 @@ class Rotary:
         self.theta, self.factor = self._frequencies(rot_dim, base, scaling)
         units = [round(float(t) / (2 * math.pi) * 2.0 ** 64) % 2 ** 64 for t in self.theta]
         self.units = torch.from_numpy(np.array(units, np.uint64).view(np.int64)).to(device)
+        self.device = self.units.device
         self._values = [(self.units.data_ptr() if units else 0, rot_dim, _LAYOUTS[layout], self.factor, t) for t in (0, 1)]
 
     @staticmethod
@@ -244,12 +246,12 @@ class PagedCache:
 
     def __init__(self, k, v):
         _tensor(k, "k cache", 4)
-        _tensor(v, "v cache", 4, k)
+        _tensor(v, "v cache", 4, k.dtype, k.device)
         if k.shape != v.shape:
             _refuse(f"k and v caches differ: {list(k.shape)}, {list(v.shape)}")
         if k.dtype not in _DTYPES:
             _refuse(f"cache: bfloat16, float16 or float32 wanted, got {k.dtype}")
-        self.k, self.v = k, v
+        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.device
         self.n_pages, self.page_size, self.kv_heads, self.head_dim = k.shape
         if self.page_size < 1:
             _refuse("page_size must be positive")
@@ -270,27 +272,27 @@ class PagedCache:
 
 def _rope_call(q, k, positions, rotary, transposed, out_q, out_k, stream):
     shape, qs = _tensor(q, "q", 3)
-    device = q.device
+    device, dtype = q.device, q.dtype
     handle = _handle(stream, device)
-    dt = _DTYPES.get(q.dtype)
+    dt = _DTYPES.get(dtype)
     if dt is None:
         _refuse(f"q: bfloat16, float16 or float32 wanted, got {q.dtype}")
     T, heads, dim = shape
-    if dim != rotary.head_dim or rotary.units.device != device:
-        _refuse(f"q has heads of {dim} on {device}, the rotary is of {rotary.head_dim} on {rotary.units.device}")
+    if dim != rotary.head_dim or rotary.device != device:
+        _refuse(f"q has heads of {dim} on {device}, the rotary is of {rotary.head_dim} on {rotary.device}")
     pos = _index(positions, "positions", (T,), torch.int32, device)
     kh, kp, kop, ks, kos = 0, 0, 0, (0, 0), (0, 0)
     if k is not None:
-        kshape, ks = _tensor(k, "k", 3, q)
+        kshape, ks = _tensor(k, "k", 3, dtype, device)
         kh = kshape[1]
         if kshape[0] != T or kshape[2] != dim:
             _refuse(f"k: [{T}, kv_heads, {dim}] wanted, got {list(kshape)}")
-        out_k, kos = _output(out_k, "out_k", kshape, q, stream)
+        out_k, kos = _output(out_k, "out_k", kshape, dtype, device, stream)
         if kh:
             kp, kop = k.data_ptr(), out_k.data_ptr()
     else:
         out_k = None
-    out_q, qos = _output(out_q, "out_q", shape, q, stream)
+    out_q, qos = _output(out_q, "out_q", shape, dtype, device, stream)
     if T and (heads or kh):
         gts._check((_lib or _load()).gts_rope(_ROPE.pack(
             T, heads, kh, dim, dt, pos, *rotary._values[transposed], q.data_ptr(), qs[0], qs[1], kp, ks[0], ks[1],
@@ -332,25 +334,25 @@ def rope_grad(dq, dk, positions, rotary, out_dq=None, out_dk=None, stream=None):
 
 
 def append_kv(q, k, v, positions, slots, rotary, cache, out_q=None, status=None, stream=None):
-    """Rotates q and k of every token to its position, writes k and v to the cache, returns the rotated q.
+    """Rotates q and k of every token to its position, writes k and v to the cache, returns the rotated q (no gradients).
 
     q [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim], positions [tokens] int32; slots [tokens] int64,
     page * page_size + index within the page, no two alike; a negative one is a padding row, of which nothing is
     written to the cache.  A slot beyond the cache writes nothing and stores GTS_ERR_INVALID_PARAMS to ``status``
     (int32 [1] on the device), where given."""
-    shape, qs = _tensor(q, "q", 3, cache.k)
-    device = q.device
+    dtype, device = cache.dtype, cache.device
+    shape, qs = _tensor(q, "q", 3, dtype, device)
     handle = _handle(stream, device)
     T, heads, dim = shape
-    if dim != cache.head_dim or dim != rotary.head_dim or rotary.units.device != device:
-        _refuse(f"heads of {dim} (q), {cache.head_dim} (cache) and {rotary.head_dim} (rotary, on {rotary.units.device})")
-    (kshape, ks), (vshape, vs) = _tensor(k, "k", 3, q), _tensor(v, "v", 3, q)
+    if dim != cache.head_dim or dim != rotary.head_dim or rotary.device != device:
+        _refuse(f"heads of {dim} (q), {cache.head_dim} (cache) and {rotary.head_dim} (rotary, on {rotary.device})")
+    (kshape, ks), (vshape, vs) = _tensor(k, "k", 3, dtype, device), _tensor(v, "v", 3, dtype, device)
     if kshape != (T, cache.kv_heads, dim) or vshape != kshape:
         _refuse(f"k and v: {[T, cache.kv_heads, dim]} wanted, got {list(kshape)} and {list(vshape)}")
     pos = _index(positions, "positions", (T,), torch.int32, device)
     at = _index(slots, "slots", (T,), torch.int64, device)
     st = _status(status, device)
-    out_q, qos = _output(out_q, "out_q", shape, q, stream)
+    out_q, qos = _output(out_q, "out_q", shape, dtype, device, stream)
     if T:
         gts._check((_lib or _load()).gts_append_kv(_APPEND.pack(
             T, heads, pos, at, *rotary._values[0], q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(),
@@ -371,7 +373,8 @@ def attention_workspace(cache, q, prefix_len, page_table, stream=None):
 
 def prefix_attention(q, cache, prefix_pages, prefix_len, page_table, lens, scale=None, out=None, lse=None,
                      workspace=None, status=None, stream=None):
-    """Attention of q [seqs, new, heads, head_dim] over a shared prefix and each sequence's own tokens: (out, lse).
+    """Attention of q [seqs, new, heads, head_dim] over a shared prefix and each sequence's own tokens: (out, lse), without
+    gradients.
 
     The prefix is the first ``prefix_len`` tokens of the pages in ``prefix_pages`` (int32); sequence b's own tokens are
     the first ``lens[b]`` (int32) of the pages in ``page_table[b]`` (int32 [seqs, max_pages]; entries past its length
@@ -379,8 +382,8 @@ def prefix_attention(q, cache, prefix_pages, prefix_len, page_table, lens, scale
     prefix and its sequence's tokens up to its own.  ``scale``: of the products (default 1 / sqrt(head_dim)).  A query
     that sees nothing gets zeros and lse = -inf (float32 [seqs, new, heads]).  A page number or a length out of range
     is not followed and stores GTS_ERR_INVALID_PARAMS to ``status`` (int32 [1] on the device), where given."""
-    shape, qs = _tensor(q, "q", 4, cache.k)
-    device = q.device
+    dtype, device = cache.dtype, cache.device
+    shape, qs = _tensor(q, "q", 4, dtype, device)
     handle = _handle(stream, device)
     B, new, heads, dim = shape
     if dim != cache.head_dim:
@@ -394,7 +397,7 @@ def prefix_attention(q, cache, prefix_pages, prefix_len, page_table, lens, scale
     max_pages = page_table.shape[1]
     lens_at = _index(lens, "lens", (B,), torch.int32, device)
     st = _status(status, device)
-    out, os = _output(out, "out", shape, q, stream)
+    out, os = _output(out, "out", shape, dtype, device, stream)
     if lse is None:
         lse = _empty((B, new, heads), torch.float32, device, stream)
         lse_at = lse.data_ptr()
