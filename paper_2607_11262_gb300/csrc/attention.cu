@@ -163,7 +163,8 @@ template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi)
 // A "pair" is a key head (or four of them) with a tile of up to ROWS query rows that see the same keys: of the prefix, rows of all
 // sequences (row (b * n_new + i) * group + h of n_seqs * n_new * group); of a sequence's own keys, its n_new * group rows.
 // A pair's keys come in tiles of KEYS, the unit of work.  All units stand in one line (prefix pairs, then the sequences'),
-// and each block takes an equal stretch of it, so ragged lengths cost nothing and the cut needs no plan from the host.
+// and each block takes an equal stretch of it, so ragged lengths cost nothing and the cut needs no plan from the host.  Before a
+// pair's first tile stand `lead` units for what it costs beside its tiles; a stretch that begins there begins with that tile.
 // A pair that lies within one block's stretch leaves one result per row; one that is cut leaves a partial result per block,
 // which k_join adds up in the order of the keys.
 constexpr int SMS = 152;
@@ -177,7 +178,8 @@ struct Line {           // the units of one launch
   int side_by_side;     // that kernel's own: starts[n_seqs] row tiles at a time
   int prefix_tiles, own_tiles;   // row tiles of the prefix's rows, of a sequence's rows
   int blocks;
-  int64_t *starts;      // [n_seqs + 2]: first unit of each sequence, the units of all, units per block
+  int lead;             // units that stand for what a pair costs beside its tiles
+  int64_t *starts;      // [n_seqs + 3]: first unit of each sequence, the units of all, units per block, before a pair's first tile
   float *cut_o;         // [blocks][2][heads][rows][D]: results of the first and last pair of a block that are cut
   float2 *cut_ml;       // [blocks][2][heads][rows]: maximum (of log2 scores) and sum
   int4 *ends;           // [blocks]: the pair that begins in a block and goes on in the next ones, see k_join_cut
@@ -199,16 +201,31 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
 
 // The prefix's kernel is bound by the tensor cores and holds whole SMs, the sequences' own keys are bound by memory: both run
 // at the same time, on SMs dealt out by the time each needs.  In units of an own tile's time on an SM (0.77 us measured at a
-// head of 128, 0.42 at 64, 1.7 at 256): a tile of the prefix takes 2.2 (1.7 us), 3.3 (1.4 us) or 0.4 (0.7 us), begin and end of its pair 8 or 4,
-// the end of an own pair 3; own work with tiles of 32 or 64 rows 1.4 or 1.8 times as long; and own tiles alone cannot go faster
-// than memory brings them, 104 to that time.  Both kernels come to the same numbers from the lengths.
+// head of 128, 0.42 at 64, 1.7 at 256, over all sizes of blocks): a tile of the prefix takes 2.2 (1.7 us), 3.3 (1.4 us) or 0.4
+// (0.7 us), begin and end of its pair 8 or 4, the end of an own pair 3; own work with tiles of 16, 32 or 64 rows 0.8, 1.1 or 2.1
+// times as long; and own tiles alone cannot go faster than memory brings them, 104 to that time.  Every block of the prefix takes
+// the same whole number of tiles: of that number, one fewer and one more, the one with which the slower kernel is the fastest
+// is taken, and no more SMs than it needs (64 sequences of 16 tokens over 8192 + 512 at a head of 256: 562 us without this
+// choice, 413 with it; 64 of 3 over 8192 + 4096 at 128: 173 and 137).  Both kernels come to the same numbers from the lengths.
 template <int D>
 __device__ __forceinline__ int prefix_sms(const Args &a, const Line &prefix, int own_rows, int64_t own_tiles, int64_t own_pairs) {
-  const float p = ((D == 64 ? 3.3f : D == 128 ? 2.2f : 0.4f) * tiles_of(a.prefix_len, prefix.keys) + (D == 256 ? 4.f : 8.f)) * a.kv_heads * prefix.prefix_tiles;
-  const float o = (own_tiles + 3.f * own_pairs) * (own_rows == 16 ? 1.f : own_rows == 32 ? 1.4f : 1.8f);
   if (own_tiles == 0) return SMS;
-  const float each = fmaxf((p + o) / SMS, own_tiles / 104.f);
-  return max(1, min(SMS - 1, (int)(p / each + 0.5f)));
+  const int n = tiles_of(a.prefix_len, prefix.keys);
+  const float tile = D == 64 ? 3.3f : D == 128 ? 2.2f : 0.4f, pair = D == 256 ? 4.f : 8.f;
+  const float p = (tile * n + pair) * a.kv_heads * prefix.prefix_tiles;
+  const float o = (own_tiles + 3.f * own_pairs) * (own_rows == 16 ? 0.8f : own_rows == 32 ? 1.1f : 2.1f), memory = own_tiles / 104.f;
+  const int even = max(1, min(SMS - 1, (int)(p / fmaxf((p + o) / SMS, memory) + 0.5f)));
+  const int side = even >= prefix.prefix_tiles ? prefix.prefix_tiles : 1;
+  const int64_t units = (int64_t)n * a.kv_heads * (side == 1 ? prefix.prefix_tiles : 1), per = quotient(units + even / side - 1, even / side);
+  int best = even;
+  float least = INFINITY;
+  for (int64_t x = max((int64_t)1, per - 1); x <= per + 1; x++) {
+    const int64_t sms = quotient(units + x - 1, x) * side;
+    if (sms >= SMS) continue;
+    const float time = fmaxf((tile + pair / n) * x, fmaxf(o / (SMS - sms), memory));
+    if (time < least) least = time, best = (int)sms;
+  }
+  return best;
 }
 
 __device__ __forceinline__ void dependents_may_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
@@ -252,7 +269,7 @@ template <int D, int WM, int WH> struct Ring {
   static constexpr int STAGES = (D == 64 ? 4 : 3) - (WM > 1);   // as many as stream_per_sm blocks find room for
   static constexpr int TILE = KEYS * D * 2;                     // bytes of a tile of keys or of values
   static constexpr int QUERIES = WH > 1 ? 0 : 16 * WM * D * 2;  // with four heads they go straight to registers
-  static constexpr int SMEM = 1024 /* alignment */ + STAGES * (2 * TILE + QUERIES) + 64 * 8 + (2 * STAGES + 1) * 8 + 56;
+  static constexpr int SMEM = 1024 /* alignment */ + STAGES * (2 * TILE + QUERIES) + 64 * (8 + 16) + (2 * STAGES + 1) * 8 + 56;
 };
 // (at a head of 64 one warp has half the copies to issue, and is enough)
 __host__ __device__ constexpr int bringers(int D, int WH) { return D > 64 ? WH : 1; }
@@ -268,7 +285,8 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
   unsigned char *const ring = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
   unsigned char *const qs = ring + STAGES * 2 * TILE;
   float2 *const stat = (float2 *)(qs + STAGES * R::QUERIES);        // [64]: maximum and sum of each warp's rows
-  uint64_t *const bars = (uint64_t *)(stat + 64);
+  longlong2 *const place = (longlong2 *)(stat + 64);                // [64]: of each row in the output, and its number
+  uint64_t *const bars = (uint64_t *)(place + 64);
   int64_t *const found = (int64_t *)(bars + 2 * STAGES + 1);        // [4]
   int *const nonempty = (int *)(found + 4);                         // [4]
   volatile int *const dead = (volatile int *)(nonempty + 4);
@@ -286,7 +304,7 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
 
   // the line of units, and this block's stretch of it
   const int n_prefix = w.has_prefix ? tiles_of(a.prefix_len, KU) : 0, head_groups = a.kv_heads / WH;
-  const int64_t prefix_units = (int64_t)n_prefix * head_groups * w.prefix_tiles;
+  const int prefix_pairs = n_prefix ? head_groups * w.prefix_tiles : 0;
   const int own_pairs = head_groups * w.own_tiles;
   const int each = w.has_own && tid < THREADS ? (a.n_seqs + THREADS - 1) / THREADS : 0;
   const int b_first = min(a.n_seqs, tid * each), b_last = min(a.n_seqs, (tid + 1) * each);
@@ -298,25 +316,31 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
     some += n > 0;
   }
   int64_t upto = mine;
+  int some_upto = some;
   for (int o = 1; o < 32; o *= 2) {
     const int64_t x = __shfl_up_sync(~0u, upto, o);
-    if (lane >= o) upto += x;
+    const int y = __shfl_up_sync(~0u, some_upto, o);
+    if (lane >= o) upto += x, some_upto += y;
   }
-  if (lane == 31 && warp < WARPS) found[warp] = upto;
-  some = __reduce_add_sync(~0u, some);
-  if (lane == 0 && warp < WARPS) nonempty[warp] = some;
+  if (lane == 31 && warp < WARPS) found[warp] = upto, nonempty[warp] = some_upto;
   __syncthreads();
-  int64_t base = prefix_units, total = prefix_units;
+  int64_t before = upto - mine, pairs_before = some_upto - some, own_tiles = 0, pairs = 0;
   for (int x = 0; x < WARPS; x++) {
-    if (x < warp) base += found[x];
-    total += found[x];
+    if (x < warp) before += found[x], pairs_before += nonempty[x];
+    own_tiles += found[x], pairs += nonempty[x];
   }
-  base += upto - mine;                                 // first unit of sequence b_first
+  pairs_before *= own_pairs, pairs *= own_pairs;
   int blocks = w.blocks;
-  if (w.beside_prefix) {
-    const int64_t pairs = (int64_t)(nonempty[0] + nonempty[1] + nonempty[2] + nonempty[3]) * own_pairs;
-    blocks = max(1, min(blocks, stream_per_sm(D) * (SMS - prefix_sms<D>(a, prefix, ROWS, total, pairs))));
-  }
+  if (w.beside_prefix) blocks = max(1, min(blocks, stream_per_sm(D) * (SMS - prefix_sms<D>(a, prefix, ROWS, own_tiles, pairs))));
+  // what a pair costs beside its tiles counts as units before its first (with few tiles to a block, each goes to its own)
+  const int lead = own_tiles + (int64_t)n_prefix * prefix_pairs >= 4 * blocks ? w.lead : 0;
+  auto own_units = [&](int b) {
+    const int n = tiles_of(own_len(a, b), KU);
+    return n ? (int64_t)(n + lead) * own_pairs : 0;
+  };
+  const int64_t prefix_units = (int64_t)(n_prefix + lead) * prefix_pairs, total = prefix_units + own_tiles + lead * pairs;
+  const int64_t base = prefix_units + before + lead * pairs_before;   // first unit of sequence b_first
+  mine += (int64_t)lead * some * own_pairs;
   const int64_t per = quotient(total + blocks - 1, blocks);
   const int64_t u0 = per * blockIdx.x, u1 = min(total, u0 + per);
   __syncthreads();
@@ -324,21 +348,24 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
     int64_t at = base;
     for (int b = b_first; b < b_last; b++) {
       w.starts[b] = at;
-      at += (int64_t)tiles_of(own_len(a, b), KU) * own_pairs;
+      at += own_units(b);
     }
-    if (tid == 0) w.starts[a.n_seqs] = total, w.starts[a.n_seqs + 1] = per;
+    if (tid == 0) w.starts[a.n_seqs] = total, w.starts[a.n_seqs + 1] = per, w.starts[a.n_seqs + 2] = lead;
   }
-  if (u0 >= u1) {
+  auto nothing_here = [&] {
     // the kernel after this one waits for this one alone: so this one ends after the one before it
     if (tid == 0) w.ends[blockIdx.x] = make_int4(-1, 0, 0, 0);
     if (blockIdx.x == 0) wait_for_kernels_before();
+  };
+  if (u0 >= u1) {
+    nothing_here();
     return;
   }
   if (u0 >= prefix_units && u0 >= base && u0 < base + mine) {
     int64_t at = base;
     int b = b_first;
     for (;; b++) {
-      const int64_t n = (int64_t)tiles_of(own_len(a, b), KU) * own_pairs;
+      const int64_t n = own_units(b);
       if (u0 < at + n) break;
       at += n;
     }
@@ -346,6 +373,8 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
   }
   __syncthreads();
   Place now;                                           // the tile whose turn it is
+  int left = (int)(u1 - u0);                           // units from it to the end of the stretch
+  bool inside;                                         // the stretch begins with a pair's first tile or a later one
   {
     const bool in_prefix = u0 < prefix_units;
     const int64_t in = in_prefix ? u0 : found[1];
@@ -353,10 +382,17 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
     now.len = in_prefix ? a.prefix_len : own_len(a, now.b);
     now.n = tiles_of(now.len, KU);
     now.pairs = in_prefix ? head_groups * w.prefix_tiles : own_pairs;
-    now.pair = (int)quotient(in, now.n);
-    now.tile = (int)(in - (int64_t)now.pair * now.n);
+    now.pair = (int)quotient(in, now.n + lead);
+    const int unit = (int)(in - (int64_t)now.pair * (now.n + lead));
+    inside = unit >= lead;
+    now.tile = max(0, unit - lead);
+    left -= max(0, lead - unit);
   }
-  const int count = (int)(u1 - u0);
+  if (left <= 0) {
+    nothing_here();
+    return;
+  }
+  auto units_to_next = [&](const Place &p) { return p.tile == p.n - 1 ? 1 + lead : 1; };
   auto advance = [&](Place &p) {                       // only ever to units of this block
     if (++p.tile < p.n) return;
     p.tile = 0;
@@ -401,10 +437,11 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
     Place ahead = now;
     look_up(ahead);
     int seg = -1;
-    for (int unit = 0; unit < count; unit++) {
+    for (int unit = 0; left > 0; unit++) {
       const Place at = ahead;
       int to_load[2] = {page[0], page[1]};
-      if (unit + 1 < count) {                          // the next tile's page numbers are fetched while this one waits
+      left -= units_to_next(at);
+      if (left > 0) {                                  // the next tile's page numbers are fetched while this one waits
         advance(ahead);
         look_up(ahead);
       }
@@ -473,18 +510,23 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
       if (WH == 1 && (unit == 0 || at.tile == 0)) {    // a pair begins: its queries, zeros beyond the last row
         seg = seg + 1 == STAGES ? 0 : seg + 1;
         const int kh = group, row0 = (at.pair - kh * tiles) * ROWS, rows = (at.b < 0 ? a.n_seqs : 1) * a.n_new * a.group - row0;
-        for (int x = lane; x < ROWS * CH; x += 32) {
-          const int r = x / CH, c = x % CH;
-          const uint32_t dst = seg * R::QUERIES + c / 8 * QHALF + r * 128 + ((c % 8) ^ (r & 7)) * 16;
-          const Row p = row_of(a, at.b, kh, row0 + min(r, rows - 1));
-          const T *src = (const T *)a.q + p.b * a.q_seq + p.i * a.q_tok + p.h * a.q_head + c * 8;
-          if (q_aligned) {
-            copy16(q_at + dst, src, r < rows);
-          } else {
-            T e[8];
 #pragma unroll
-            for (int j = 0; j < 8; j++) e[j] = r < rows ? src[j] : narrow<T>(0.f);
-            memcpy(qs + dst, e, 16);
+        for (int x = 0; x < (ROWS + 31) / 32; x++) {   // a lane finds where a row is, then lanes along the rows
+          const Row p = row_of(a, at.b, kh, row0 + min(x * 32 + lane, rows - 1));
+          const unsigned long long row = (unsigned long long)((const T *)a.q + p.b * a.q_seq + p.i * a.q_tok + p.h * a.q_head);
+#pragma unroll 4
+          for (int y = 0; y < min(32, ROWS) * CH; y += 32) {
+            const int in = (y + lane) / CH, r = x * 32 + in, c = lane % CH;
+            const uint32_t dst = seg * R::QUERIES + c / 8 * QHALF + r * 128 + ((c % 8) ^ (r & 7)) * 16;
+            const T *src = (const T *)__shfl_sync(~0u, row, in) + c * 8;
+            if (q_aligned) {
+              copy16(q_at + dst, src, r < rows);
+            } else {
+              T e[8];
+#pragma unroll
+              for (int j = 0; j < 8; j++) e[j] = r < rows ? src[j] : narrow<T>(0.f);
+              memcpy(qs + dst, e, 16);
+            }
           }
         }
       }
@@ -521,7 +563,7 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
       alive = __all_sync(~0u, bar_wait(together, meetings++ & 1, dead));
     };
     int seg = -1, tile0 = 0, kh = 0, row0 = 0, rows = 0, limit[2] = {0, 0}, seen_by_all = 0;
-    bool first_pair = true;
+    bool first_slot = inside;                          // where a cut pair's part goes: k_join works it out from the units
     float o[D / 8][4], m[2], l[2];
     uint32_t qf[KEEP_Q ? D / 16 : 1][4];
     // Four heads: the next pair's queries are brought to L2 while this one's keys are worked on (from memory, while it is busy,
@@ -535,7 +577,8 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
       }
     };
     int after = WH > 1 && now.b + 1 < a.n_seqs ? a.lens[now.b + 1] : 0, after_b = now.b;   // the next sequence's length, ahead of time
-    for (int unit = 0; unit < count; unit++) {
+    for (int unit = 0; left > 0; unit++) {
+      const int then = left - units_to_next(now);      // units left at the next tile
       const bool begins = unit == 0 || now.tile == 0;
       if (begins) {                                    // a pair begins
         const int tiles = row_tiles(now);
@@ -607,15 +650,15 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
             *(uint4 *)(ring + stage * 2 * TILE + TILE + c / 8 * HALF + (wk * KW + r) * 128 + c % 8 * 16) = make_uint4(0, 0, 0, 0);
           }
           // and so for a value that some rows see and others do not: not finite, it is kept out of the products
-          for (int r = max(0, seen_by_all - key0); r < min(KW, end); r++) {
-            bool odd = false;
-            for (int x = lane; x < D / 2; x += 32) {
-              const uint32_t both = *(const uint32_t *)(ring + stage * 2 * TILE + TILE + x / 32 * HALF + (wk * KW + r) * 128 + x % 32 * 4);
-              const uint32_t e = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u;
-              odd |= (both & e) == e || (both >> 16 & e) == e;
-            }
-            if (__any_sync(~0u, odd)) bad |= 1ull << r;
+          for (int r = max(0, seen_by_all - key0) + lane / CH; r < min(KW, end); r += 32 / CH) {
+            const int c = lane % CH;
+            const uint4 v = *(const uint4 *)(ring + stage * 2 * TILE + TILE + c / 8 * HALF + (wk * KW + r) * 128 + c % 8 * 16);
+            const uint32_t e = std::is_same<T, __half>::value ? 0x7C00u : 0x7F80u, w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int x = 0; x < 4; x++)
+              if ((w[x] & e) == e || (w[x] >> 16 & e) == e) bad |= 1ull << r;
           }
+          bad = (uint64_t)__reduce_or_sync(~0u, (uint32_t)(bad >> 32)) << 32 | __reduce_or_sync(~0u, (uint32_t)bad);
           __syncwarp();
         }
         float s[KW / 8][4];
@@ -722,7 +765,7 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
       else attend(std::false_type());
 
       if constexpr (WH > 1) {
-        if (now.tile == tile0 && unit + (now.n - now.tile) < count) {
+        if (now.tile == tile0 && now.n - now.tile + lead < left) {
           const int tiles = row_tiles(now), pair = now.pair + 1 < now.pairs ? now.pair + 1 : 0;
           const bool same = now.pair + 1 < now.pairs;
           if (same || after > 0) {                     // (with an empty sequence in between: no matter)
@@ -732,11 +775,11 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
           }
         }
       }
-      if (now.tile == now.n - 1 || unit == count - 1) {
+      if (now.tile == now.n - 1 || then <= 0) {
         const bool whole = tile0 == 0 && now.tile == now.n - 1;
-        if (tid == 0 && unit == count - 1)
+        if (tid == 0 && then <= 0)
           w.ends[blockIdx.x] = tile0 > 0 || whole ? make_int4(-1, 0, 0, 0)
-                                                  : make_int4(now.b, now.pair, (int)quotient(now.n - 2 - now.tile + per, per), !first_pair);
+                                                  : make_int4(now.b, now.pair, (int)quotient(now.n - 2 - now.tile + per, per), !first_slot);
         const bool final = whole && now.b >= 0 && a.prefix_len == 0;
         if constexpr (WH > 1) {
           // a pair ends here, and each warp has its head's rows
@@ -764,7 +807,7 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
               }
               if (t4 == 0 && a.lse) a.lse[row] = l[x] == 0.f ? -INFINITY : (m[x] + log2f(l[x])) * 0.6931471805599453f;
             } else {
-              const int64_t at = whole ? row : (((int64_t)blockIdx.x * 2 + !first_pair) * WH + wh) * ROWS + r;
+              const int64_t at = whole ? row : (((int64_t)blockIdx.x * 2 + !first_slot) * WH + wh) * ROWS + r;
               float *dst = (whole ? w.whole_o[now.b >= 0] : w.cut_o) + at * D + t4 * 2;
 #pragma unroll
               for (int d = 0; d < D / 8; d++) *(float2 *)(dst + d * 8) = make_float2(o[d][2 * x], o[d][2 * x + 1]);
@@ -774,8 +817,11 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
           if (mask) fence_async();
         } else {
           // a pair ends here: the warps along the keys are joined in the stage just read, and its rows written
-          meet();
+          const Row goes = row_of(a, now.b, kh, row0 + min(tid, rows - 1));
+          meet();                                      // (all are done with the rows of the pair before)
           if (!alive) break;
+          if (tid < rows)
+            place[tid] = make_longlong2(goes.b * a.o_seq + goes.i * a.o_tok + goes.h * a.o_head, ((int64_t)goes.b * a.n_new + goes.i) * a.q_heads + goes.h);
           float *acc = (float *)(ring + stage * 2 * TILE);   // [4 warps][16][D], columns of row r turned by 8 (r mod 4)
 #pragma unroll
           for (int x = 0; x < 2; x++) {
@@ -805,11 +851,10 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
               sum += f * stat[at].y;
               v.x += f * y.x, v.y += f * y.y, v.z += f * y.z, v.w += f * y.w;
             }
-            const Row p = row_of(a, now.b, kh, row0 + r);
-            const int64_t row = ((int64_t)p.b * a.n_new + p.i) * a.q_heads + p.h;
+            const int64_t row = place[r].y;
             if (final) {
               const float inv = sum == 0.f ? 0.f : 1.f / sum;
-              T *dst = (T *)a.out + p.b * a.o_seq + p.i * a.o_tok + p.h * a.o_head + c;
+              T *dst = (T *)a.out + place[r].x + c;
               const uint32_t lo = pack<T>(v.x * inv, v.y * inv), hi = pack<T>(v.z * inv, v.w * inv);
               if (o_aligned) {
                 *(uint2 *)dst = make_uint2(lo, hi);
@@ -821,20 +866,21 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
               if (c == 0 && a.lse) a.lse[row] = sum == 0.f ? -INFINITY : (best + log2f(sum)) * 0.6931471805599453f;
             } else {
               // whole pairs by row, cut ones by block: its first (0) or its last (1)
-              const int64_t at = whole ? row : ((int64_t)blockIdx.x * 2 + !first_pair) * ROWS + r;
+              const int64_t at = whole ? row : ((int64_t)blockIdx.x * 2 + !first_slot) * ROWS + r;
               *(float4 *)((whole ? w.whole_o[now.b >= 0] : w.cut_o) + at * D + c) = v;
               if (c == 0) (whole ? w.whole_ml[now.b >= 0] : w.cut_ml)[at] = make_float2(best, sum);
             }
           }
           fence_async();                               // the stage was written here and is next written by TMA
         }
-        first_pair = false;
+        first_slot = false;
       } else if (mask) {
         fence_async();
       }
       __syncwarp();
       if (lane == 0) bar_arrive(empty(stage));
-      if (unit + 1 < count) advance(now);
+      left = then;
+      if (left > 0) advance(now);
       if (WH > 1 && now.b != after_b) {
         after_b = now.b;
         after = now.b + 1 < a.n_seqs ? a.lens[now.b + 1] : 0;
@@ -969,7 +1015,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   const int my_tile = blockIdx.x % side;
   auto head_of = [&](int pair) { return pair / behind; };
   auto first_row = [&](int pair) { return (side == 1 ? pair % behind : my_tile) * Tc<D>::ROWS; };
-  if (blockIdx.x == 0 && tid == 0) w.starts[a.n_seqs] = side, w.starts[a.n_seqs + 1] = per;
+  if (blockIdx.x == 0 && tid == 0) w.starts[a.n_seqs] = side, w.starts[a.n_seqs + 1] = per, w.starts[a.n_seqs + 2] = 0;
   if (u0 >= u1) return;
   if (tid == 0) {
     for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(empty(s), SINGLE ? 1 : 2);
@@ -1436,7 +1482,8 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
       const int tile = r / w.rows;
       p.per = w.starts[a.n_seqs + 1];
       p.lane = side > 1 ? tile : 0;                    // of `side` row tiles side by side
-      p.u0 = start + (int64_t)(side > 1 ? kh : kh / w.heads * tiles + tile) * n;
+      const int lead = (int)w.starts[a.n_seqs + 2];
+      p.u0 = start + (int64_t)(side > 1 ? kh : kh / w.heads * tiles + tile) * (n + lead) + lead;
       p.r = kh % w.heads * w.rows + r % w.rows;
       p.c0 = quotient(p.u0, p.per);
       p.count = (int)(quotient(p.u0 + n - 1, p.per) - p.c0) + 1;
@@ -1534,10 +1581,13 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
     n += up(bytes);
     return x;
   };
+  // A pair's begin and end (first loads, queries, the join of its warps, its results) in units of its tiles.  Without them blocks
+  // with many short pairs end last: 128 sequences of 16 tokens over 1..2048 take 313 us without and 175 with 7 (4: 187, 12: 186);
+  // of 5, 161 and 113 with 5; 256 of one over 1..1024, by fours, 119 and 103 with 8; 128 of one over 1..4096 187 and 178 with 2.
   auto line = [&](Line &w, int heads, int rows, int keys, int blocks, bool has_prefix, bool has_own) {
-    w.has_prefix = has_prefix, w.has_own = has_own, w.heads = heads, w.rows = rows, w.keys = keys, w.blocks = blocks;
+    w.has_prefix = has_prefix, w.has_own = has_own, w.heads = heads, w.rows = rows, w.keys = keys, w.blocks = blocks, w.lead = heads > 1 ? 8 : rows == 16 ? 2 : rows == 32 ? 5 : 7;
     w.prefix_tiles = (int)((all + rows - 1) / rows), w.own_tiles = (int)((own_rows + rows - 1) / rows);
-    w.starts = (int64_t *)take(((size_t)d.n_seqs + 2) * 8);
+    w.starts = (int64_t *)take(((size_t)d.n_seqs + 3) * 8);
     w.ends = (int4 *)take((size_t)blocks * 16);
     w.cut_ml = (float2 *)take((size_t)blocks * 2 * heads * rows * 8);
     w.cut_o = (float *)take((size_t)blocks * 2 * heads * rows * D * 4);

@@ -151,3 +151,19 @@ def test_few_key_heads_and_a_long_prefix(D):
     """One pair of rows cut over all blocks, and pairs that begin and end inside a block."""
     check_attention(problem(1, 33, 1, D, 32, "heads", "bfloat16", 9000, [5, 0, 17], 1), "bfloat16")
     check_attention(problem(2, 40, 40, D, 32, "tokens", "bfloat16", 400, [5, 0, 17] * 14, 1), "bfloat16")
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("new", [1, 5, 16])
+@pytest.mark.parametrize("prefix", [0, 100])
+def test_many_short_pairs_to_a_block(D, new, prefix):
+    """Some 20 tiles to a block, most pairs of one to three: one pair's rows are written while the next one's keys arrive, and
+    stretches end between pairs as well as inside of them; a few long sequences among them."""
+    rng = np.random.default_rng(D + new)
+    lens = [new + int(x) for x in rng.integers(0, 150, 700)]
+    lens[::50] = [1500 + int(x) for x in rng.integers(0, 300, 14)]
+    lens[3] = lens[77] = 0
+    p = problem(D, 16, 4, D, 64, "heads", "bfloat16", prefix, lens, new)
+    check_attention(widen_table(p, 40), "bfloat16")
+    if new == 1:
+        check_attention(p, "bfloat16")
