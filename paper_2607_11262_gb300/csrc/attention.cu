@@ -219,6 +219,7 @@ __device__ __forceinline__ int prefix_sms(const Args &a, const Line &prefix, int
   const int64_t units = (int64_t)n * a.kv_heads * (side == 1 ? prefix.prefix_tiles : 1), per = quotient(units + even / side - 1, even / side);
   int best = even;
   float least = INFINITY;
+#pragma unroll 1
   for (int64_t x = max((int64_t)1, per - 1); x <= per + 1; x++) {
     const int64_t sms = quotient(units + x - 1, x) * side;
     if (sms >= SMS) continue;
@@ -262,9 +263,10 @@ struct Place { int b, len, n, pairs, pair, tile; };
 // its own running maximum and sum.  Weights are rounded to the type of the values for their product with them (the sum is of
 // the unrounded ones); everything else is in 32 bits.
 //
-// Bound by memory for long sequences: 128 of up to 4096 tokens, 1.08 GB, 169 us, 6.4 TB/s, 94% of the rate of a copy; 256 of up
-// to 1024, 537 MB, 102 us, 78%, where the ends of pairs and the first tiles' latencies count.  Tiles of 32 and 64 rows (5 and 16
-// new tokens) are bound by the latency of their products with two warps to a scheduler: the same 537 MB in 188 and 385 us.
+// Bound by memory for long sequences: 128 of up to 4096 tokens, 1.08 GB, 175 us, 6.2 TB/s, 91% of the rate of a copy; 256 of up
+// to 1024, 537 MB, 94 us, 84%, where the ends of pairs and the first tiles' latencies count.  Tiles of 32 and 64 rows (5 and 16
+// new tokens) are bound by the latency of their products with two warps to a scheduler: 128 of 1..2048, as many bytes, in 113 and
+// 175 us.
 template <int D, int WM, int WH> struct Ring {
   static constexpr int STAGES = (D == 64 ? 4 : 3) - (WM > 1);   // as many as stream_per_sm blocks find room for
   static constexpr int TILE = KEYS * D * 2;                     // bytes of a tile of keys or of values
@@ -1594,8 +1596,8 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
   };
   const int own_tile = own_rows <= 16 ? 16 : own_rows <= 32 ? 32 : 64;
   // Few rows: a warp to each of four heads, which have nothing to join at a pair's end, where the heads can be had by fours.
-  // Long sequences seldom end, and their tiles of 64 keys of one head come in larger boxes: 256 of 1..1024 tokens take 102 us by
-  // fours and 108 by ones, 128 of 1..4096 take 182 and 175.
+  // Long sequences seldom end, and their tiles of 64 keys of one head come in larger boxes: 256 of 1..1024 tokens take 103 us by
+  // fours and 107 by ones, 128 of 1..4096 take 183 and 178.
   const bool fours = own_tile == 16 && D <= 128 && d.cache.kv_heads % WARPS == 0 && (uint64_t)d.max_pages * d.cache.page_size <= 2048;
   const int heads = fours ? WARPS : 1;
   line(p.own, heads, own_tile, KEYS / heads, stream_blocks(D), p.way == TOGETHER && d.prefix_len, true);
