@@ -104,17 +104,18 @@ __device__ __forceinline__ uint64_t now_ns() {
   asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
   return t;
 }
-constexpr uint64_t LIMIT_NS = 2000000000ull;
+constexpr uint64_t LIMIT_NS = 2000000000ull, DRAIN_NS = 2000000000ull;   // of a wait; of what a block that winds down has in flight
+constexpr int TRIES = 1024, BETWEEN = 64;   // before the timer is read first, and from then on (reading it takes longer than most waits)
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *dead) {
   if (bar_try(bar, parity)) return true;   // (an unrolled loop around it would try several times before it looks)
 #pragma unroll 1
-  for (int n = 0; n < 1024; n++)           // reading the timer takes longer than most waits
+  for (int n = 0; n < TRIES; n++)
     if (bar_try(bar, parity)) return true;
   const uint64_t from = now_ns();
 #pragma unroll 1
   while (!*dead) {
 #pragma unroll 1
-    for (int n = 0; n < 64; n++)
+    for (int n = 0; n < BETWEEN; n++)
       if (bar_try(bar, parity)) return true;
     if (now_ns() - from > LIMIT_NS) *dead = 1;
   }
@@ -541,12 +542,6 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
       }
       next();
     }
-    if (!alive) {                                      // copies in flight end before the block does
-      asm volatile("cp.async.wait_all;" ::: "memory");
-      const uint64_t from = now_ns();
-      for (int s = 0; s < STAGES; s++)
-        while (!bar_try(full(s), (s < stage ? lap : lap - 1) & 1) && now_ns() - from < LIMIT_NS) {}
-    }
   } else {
     // ---- the warps that compute
     if constexpr (bringers(D, WH) > 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 200;");
@@ -892,7 +887,17 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
   }
   dependents_may_start();
   __syncthreads();
-  if (*dead && tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
+  if (*dead) {
+    // copies in flight end before the block does, whichever warp gave up
+    if (warp >= WARPS) {
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      const uint64_t from = now_ns();
+#pragma unroll 1
+      for (int s = 0; s < STAGES; s++)
+        while (!bar_try(full(s), (s < stage ? lap : lap - 1) & 1) && now_ns() - from < DRAIN_NS) {}
+    }
+    if (tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
+  }
   if (blockIdx.x == 0) wait_for_kernels_before();
 }
 
@@ -1038,12 +1043,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   auto sums = [&](int h) { return tmem + 256 + h * 128; };
 
   const int all = a.n_seqs * a.n_new * a.group;
+  int copies = 0;                                      // warp 9: tiles of keys or values asked for
+  bool issues = false;                                 // the threads that issue products
 
   if (warp >= 8) {
     if (warp == 9) {
       // ---- keys and values: lane x brings the x-th box of tokens of a tile, both of its 64-value halves
       const int boxes = TC_KEYS / maps.box;
-      int it = 0;
       bool alive = true;
       int pair = (int)quotient(u0, n), tile = (int)(u0 - (int64_t)pair * n), kh = head_of(pair);
       auto look_up = [&](int t) {                          // this lane's page of tile t; -1: none
@@ -1062,9 +1068,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
           if (a.status) *a.status = GTS_ERR_INVALID_PARAMS;
         }
         const uint32_t bytes = __popc(__ballot_sync(~0u, live)) * maps.box * D * 2;
-        for (int kv = 0; kv < 2; kv++, it++) {
-          const int s = it % STAGES;
-          if (it >= STAGES && !bar_wait(empty(s), (it / STAGES - 1) & 1, dead)) alive = false;
+        for (int kv = 0; kv < 2; kv++, copies++) {
+          const int s = copies % STAGES;
+          if (copies >= STAGES && !bar_wait(empty(s), (copies / STAGES - 1) & 1, dead)) alive = false;
           alive = __all_sync(~0u, alive);
           if (!alive) break;
           if (lane == 0) bar_expect(full(s), bytes);
@@ -1079,14 +1085,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
           }
         }
       }
-      if (!alive) {                                        // copies in flight end before the block does
-        const int first = max(0, it - STAGES);
-        const uint64_t from = now_ns();
-        for (int x = first; x < it; x++)
-          while (!bar_try(full(x % STAGES), (x / STAGES) & 1) && now_ns() - from < LIMIT_NS) {}
-      }
     } else if (SINGLE && warp == 8 && elected()) {
       // ---- products of the one half: scores a tile ahead, in two buffers
+      issues = true;
       constexpr uint32_t TYPE = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
       constexpr uint32_t COMMON = 1u << 4 | TYPE << 7 | TYPE << 10 | (128u >> 4) << 24;
       constexpr uint32_t QK = COMMON | (TC_KEYS >> 3) << 17, PV = COMMON | 1u << 16 | (D >> 3) << 17;
@@ -1142,13 +1143,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
         tc_commit(s_full(turn & 1));                       // the pair's sums are complete
         turn++;
       }
-      if (!alive) {                                        // products in flight end before the block does
-        tc_commit(ended);
-        const uint64_t from = now_ns();
-        while (!bar_try(ended, 0) && now_ns() - from < LIMIT_NS) {}
-      }
     } else if (!SINGLE && warp != 9 && elected()) {
       // ---- products, from one thread for each half of the rows (one thread for both would set the time)
+      issues = true;
       constexpr uint32_t TYPE = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
       constexpr uint32_t COMMON = 1u << 4 | TYPE << 7 | TYPE << 10 | (128u >> 4) << 24;
       constexpr uint32_t QK = COMMON | (TC_KEYS >> 3) << 17, PV = COMMON | 1u << 16 | (D >> 3) << 17;
@@ -1226,11 +1223,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
           else tc_commit(s_full(h));                       // the pair's sums are complete
           if (both) bar_arrive(my_turn(!h));
         }
-      }
-      if (!alive) {                                        // products in flight end before the block does
-        tc_commit(ended + 8 * h);
-        const uint64_t from = now_ns();
-        while (!bar_try(ended + 8 * h, 0) && now_ns() - from < LIMIT_NS) {}
       }
     }
   } else if (!SINGLE || warp < 4) {
@@ -1389,7 +1381,22 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   }
   tc_before();
   __syncthreads();
-  if (*dead && tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
+  if (*dead) {
+    // copies and products in flight end before the block does, whichever warp gave up
+    const uint64_t from = now_ns();
+    if (issues) {
+      const uint32_t bar = ended + (warp == 10 ? 8 : 0);
+      tc_commit(bar);
+      while (!bar_try(bar, 0) && now_ns() - from < DRAIN_NS) {}
+    }
+    if (warp == 9) {
+#pragma unroll 1
+      for (int x = max(0, copies - STAGES); x < copies; x++)
+        while (!bar_try(full(x % STAGES), (x / STAGES) & 1) && now_ns() - from < DRAIN_NS) {}
+    }
+    if (tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
+    __syncthreads();
+  }
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
