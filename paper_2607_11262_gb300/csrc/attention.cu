@@ -896,7 +896,10 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
       for (int s = 0; s < STAGES; s++)
         while (!bar_try(full(s), (s < stage ? lap : lap - 1) & 1) && now_ns() - from < DRAIN_NS) {}
     }
-    if (tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
+    if (tid == 0) {
+      w.ends[blockIdx.x] = make_int4(-1, 0, 0, 0);     // every block leaves a record, this one that nothing is to be joined
+      if (a.status) *a.status = GTS_ERR_STEP_LIMIT;
+    }
   }
   if (blockIdx.x == 0) wait_for_kernels_before();
 }
@@ -1532,7 +1535,7 @@ __global__ void __launch_bounds__(THREADS) k_join_cut(const Args a, const Line w
   const int x = blockIdx.x * WARPS + threadIdx.x / 32, c = x / rows, r = x % rows;
   if (c >= w.blocks) return;
   const int4 end = w.ends[c];                          // sequence, pair, blocks after this one, 1 if it is not this block's first
-  if (end.x < 0 || end.x >= a.n_seqs || end.z < 0 || end.z >= w.blocks - c) return;  // (a block that gave up wrote none)
+  if (end.x < 0) return;
   const int group = end.y / w.own_tiles, row = (end.y - group * w.own_tiles) * w.rows + r % w.rows;
   if (row >= a.n_new * a.group) return;
   const Row p = row_of(a, end.x, group * w.heads + r / w.rows, row);

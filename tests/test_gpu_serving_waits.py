@@ -41,6 +41,10 @@ def call(p, seed):
 WITH_PREFIX = [dict(lens=[40 + b % 90 for b in range(64)], prefix=3000), dict(lens=[300, 0, 77] * 10, prefix=100),
                dict(lens=[60 + b for b in range(40)], prefix=1500, new=5), dict(lens=[500] * 6, prefix=400, page=100),
                dict(lens=[0] * 200, prefix=2000), dict(lens=[200] * 30, prefix=700, kv=4, columns=40)]
+WITHOUT = [dict(lens=[300 + 11 * b for b in range(40)], prefix=0), dict(lens=[700] * 30, prefix=0, kv=4, columns=20),
+           dict(lens=[0, 400, 90, 0] * 20, prefix=0, new=5), dict(lens=[2000] * 3, prefix=0, page=100),
+           dict(lens=[900] * 20, prefix=0, new=16)]
+CASES = WITH_PREFIX + WITHOUT
 
 
 def make(D, lens, prefix, new=1, page=64, kv=2, columns=0):
@@ -50,9 +54,9 @@ def make(D, lens, prefix, new=1, page=64, kv=2, columns=0):
 
 @pytest.mark.parametrize("tries", [0, 30, 300])
 @pytest.mark.parametrize("D", [128, 256])
-@pytest.mark.parametrize("case", range(len(WITH_PREFIX)))
+@pytest.mark.parametrize("case", range(len(CASES)))
 def test_blocks_end_and_say_so(short, monkeypatch, case, D, tries):
-    p = make(D, **WITH_PREFIX[case])
+    p = make(D, **CASES[case])
     want = serving.prefix_attention(**p)
     assert short.set_tries(tries) == 0
     with monkeypatch.context() as m:
