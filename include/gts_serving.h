@@ -21,7 +21,9 @@
  * lengths) are checked by the kernels: an index outside its range is never
  * followed, and GTS_ERR_INVALID_PARAMS is stored to *d_status where that is
  * given; what it would have contributed to a result is then unspecified.
- * *d_status is never cleared by the library.
+ * *d_status is never cleared by the library.  Waits inside the attention
+ * kernels end after two seconds: GTS_ERR_STEP_LIMIT is then stored to *d_status
+ * where that is given, and rows of out and lse that miss a part are NaN.
  */
 #ifndef GTS_SERVING_H
 #define GTS_SERVING_H

@@ -169,6 +169,7 @@ template <> __device__ __forceinline__ uint32_t pack<__half>(float lo, float hi)
 // A pair that lies within one block's stretch leaves one result per row; one that is cut leaves a partial result per block,
 // which k_join adds up in the order of the keys.
 constexpr int SMS = 152;
+constexpr int NOTHING = -1, GAVE_UP = -2;   // a block's record: no pair to be joined from it; its waits ran out, results are missing
 constexpr int KEYS = 64;
 constexpr int WARPS = 4, THREADS = 32 * WARPS;
 
@@ -183,7 +184,8 @@ struct Line {           // the units of one launch
   int64_t *starts;      // [n_seqs + 3]: first unit of each sequence, the units of all, units per block, before a pair's first tile
   float *cut_o;         // [blocks][2][heads][rows][D]: results of the first and last pair of a block that are cut
   float2 *cut_ml;       // [blocks][2][heads][rows]: maximum (of log2 scores) and sum
-  int4 *ends;           // [blocks]: the pair that begins in a block and goes on in the next ones, see k_join_cut
+  int4 *ends;           // [blocks]: the pair that begins in a block and goes on in the next ones, see k_join_cut; x: its sequence,
+                        // NOTHING or GAVE_UP
   float *whole_o[2];    // [rows of all][D], prefix and own: results of pairs that are not cut
   float2 *whole_ml[2];
 };
@@ -357,7 +359,7 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
   }
   auto nothing_here = [&] {
     // the kernel after this one waits for this one alone: so this one ends after the one before it
-    if (tid == 0) w.ends[blockIdx.x] = make_int4(-1, 0, 0, 0);
+    if (tid == 0) w.ends[blockIdx.x] = make_int4(NOTHING, 0, 0, 0);
     if (blockIdx.x == 0) wait_for_kernels_before();
   };
   if (u0 >= u1) {
@@ -775,7 +777,7 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
       if (now.tile == now.n - 1 || then <= 0) {
         const bool whole = tile0 == 0 && now.tile == now.n - 1;
         if (tid == 0 && then <= 0)
-          w.ends[blockIdx.x] = tile0 > 0 || whole ? make_int4(-1, 0, 0, 0)
+          w.ends[blockIdx.x] = tile0 > 0 || whole ? make_int4(NOTHING, 0, 0, 0)
                                                   : make_int4(now.b, now.pair, (int)quotient(now.n - 2 - now.tile + per, per), !first_slot);
         const bool final = whole && now.b >= 0 && a.prefix_len == 0;
         if constexpr (WH > 1) {
@@ -897,7 +899,7 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
         while (!bar_try(full(s), (s < stage ? lap : lap - 1) & 1) && now_ns() - from < DRAIN_NS) {}
     }
     if (tid == 0) {
-      w.ends[blockIdx.x] = make_int4(-1, 0, 0, 0);     // every block leaves a record, this one that nothing is to be joined
+      w.ends[blockIdx.x] = make_int4(GAVE_UP, 0, 0, 0);
       if (a.status) *a.status = GTS_ERR_STEP_LIMIT;
     }
   }
@@ -1384,6 +1386,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   }
   tc_before();
   __syncthreads();
+  if (tid == 0) w.ends[blockIdx.x] = make_int4(*dead ? GAVE_UP : NOTHING, 0, 0, 0);
   if (*dead) {
     // copies and products in flight end before the block does, whichever warp gave up
     const uint64_t from = now_ns();
@@ -1402,6 +1405,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
   }
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
+
+// Every block with work leaves a record, so the joins know the parts that a block whose waits ran out has left unwritten: rows that
+// miss one are NaN, whether or not the caller looks at a status.
+__device__ __forceinline__ bool gave_up(const Line &w, int64_t block) { return w.ends[block].x == GAVE_UP; }
+__device__ __forceinline__ float2 missing() { return make_float2(NAN, NAN); }
 
 // The result of a row from its parts, in their order: one warp.  Up to 32 parts at a time, a lane takes the maximum and sum of
 // one; then all lanes add up the parts' values, several loads in flight.
@@ -1515,21 +1523,36 @@ __global__ void __launch_bounds__(THREADS) k_join(const Args a, const Line lp, c
     const int64_t block = mine ? c : c * pre.side + pre.lane;
     const int64_t at = whole ? row : (block * 2 + last) * (mine ? lo.heads * lo.rows : lp.heads * lp.rows) + (mine ? own.r : pre.r);
     const float *o = (whole ? mine ? lo.whole_o[1] : lp.whole_o[0] : mine ? lo.cut_o : lp.cut_o) + at * D;
-    return Part{o, (whole ? mine ? lo.whole_ml[1] : lp.whole_ml[0] : mine ? lo.cut_ml : lp.cut_ml)[at]};
+    const float2 ml = (whole ? mine ? lo.whole_ml[1] : lp.whole_ml[0] : mine ? lo.cut_ml : lp.cut_ml)[at];
+    return Part{o, gave_up(mine ? lo : lp, block) ? missing() : ml};
   });
 }
 
 // Without one: the rows of the pairs that are cut, each from the block where it begins (Line::ends) to that where it ends,
-// and the rows of sequences without keys; the others are done.
+// the rows of sequences without keys, and those of pairs that a block which gave up had a part of; the others are done.
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS) k_join_cut(const Args a, const Line w, const int cut_blocks) {
   const int lane = threadIdx.x % 32, rows = w.heads * w.rows;
   wait_for_kernels_before();
   if ((int)blockIdx.x >= cut_blocks) {
     const int b = (blockIdx.x - cut_blocks) * WARPS + threadIdx.x / 32;
-    if (b >= a.n_seqs || own_len(a, b) > 0) return;
-    for (int x = 0; x < a.n_new * a.q_heads; x++)
-      join_row<T, D>(a, lane, b, x / a.q_heads, x % a.q_heads, 0, [](int) { return Part{nullptr, make_float2(0.f, 0.f)}; });
+    if (b >= a.n_seqs) return;
+    const int n = tiles_of(own_len(a, b), w.keys);
+    const int64_t per = w.starts[a.n_seqs + 1], lead = w.starts[a.n_seqs + 2], start = n ? w.starts[b] : 0;
+    auto any_gave_up = [&](int64_t first, int64_t last) {  // of the blocks of these units
+      bool any = false;
+      for (int64_t c = quotient(first, per) + lane, end = quotient(last, per); c <= end; c += 32) any |= gave_up(w, c);
+      return __any_sync(~0u, any);
+    };
+    if (n && !any_gave_up(start, start + (n + lead) * (a.kv_heads / w.heads * w.own_tiles) - 1)) return;
+    for (int x = 0; x < a.n_new * a.q_heads; x++) {
+      const int i = x / a.q_heads, h = x % a.q_heads, kh = h / a.in_group;
+      if (n) {
+        const int64_t pair = kh / w.heads * w.own_tiles + (i * a.group + h - kh * a.group) / w.rows, u0 = start + pair * (n + lead) + lead;
+        if (!any_gave_up(u0, u0 + n - 1)) continue;
+      }
+      join_row<T, D>(a, lane, b, i, h, n ? 1 : 0, [&](int) { return Part{w.cut_o, missing()}; });
+    }
     return;
   }
   const int x = blockIdx.x * WARPS + threadIdx.x / 32, c = x / rows, r = x % rows;
@@ -1541,7 +1564,7 @@ __global__ void __launch_bounds__(THREADS) k_join_cut(const Args a, const Line w
   const Row p = row_of(a, end.x, group * w.heads + r / w.rows, row);
   join_row<T, D>(a, lane, p.b, p.i, p.h, 1 + end.z, [&](int y) {
     const int64_t at = ((int64_t)(c + y) * 2 + (y ? 0 : end.w)) * rows + r;
-    return Part{w.cut_o + at * D, w.cut_ml[at]};
+    return Part{w.cut_o + at * D, gave_up(w, c + y) ? missing() : w.cut_ml[at]};
   });
 }
 

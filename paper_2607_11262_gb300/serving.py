@@ -381,7 +381,8 @@ def prefix_attention(q, cache, prefix_pages, prefix_len, page_table, lens, scale
     are not looked at).  They include the ``new`` newest, whose keys are in the cache already: query i sees the whole
     prefix and its sequence's tokens up to its own.  ``scale``: of the products (default 1 / sqrt(head_dim)).  A query
     that sees nothing gets zeros and lse = -inf (float32 [seqs, new, heads]).  A page number or a length out of range
-    is not followed and stores GTS_ERR_INVALID_PARAMS to ``status`` (int32 [1] on the device), where given."""
+    is not followed and stores GTS_ERR_INVALID_PARAMS to ``status`` (int32 [1] on the device), where given.  A kernel whose
+    waits run out (after two seconds) stores GTS_ERR_STEP_LIMIT there, and rows that miss a part are NaN."""
     dtype, device = cache.dtype, cache.device
     shape, qs = _tensor(q, "q", 4, dtype, device)
     handle = _handle(stream, device)

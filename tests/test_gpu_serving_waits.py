@@ -1,5 +1,5 @@
 """Attention when its waits run out (tests/short_waits.py): every block ends, its copies and products with it, the status says
-so, nothing outside the results is written, and the calls after it are what they were."""
+so, rows that miss a part are NaN, nothing outside the results is written, and the calls after it are what they were."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -63,8 +63,12 @@ def test_blocks_end_and_say_so(short, monkeypatch, case, D, tries):
         m.setattr(serving, "_lib", short)
         for seed in range(3):
             out, lse, status = call(p, seed)
+            # a row is either what it should be or NaN throughout, lse and all
+            lost = torch.isnan(lse)
+            assert torch.equal(torch.isnan(out), lost[..., None].expand_as(out))
+            assert torch.equal(out[~lost], want[0][~lost]) and torch.equal(lse[~lost], want[1][~lost])
             if tries == 0:  # no tile arrives that soon
-                assert status == gts.GTS_ERR_STEP_LIMIT
+                assert status == gts.GTS_ERR_STEP_LIMIT and lost.any()
             if status == gts.GTS_OK:
                 assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
     again = call(p, 7)
