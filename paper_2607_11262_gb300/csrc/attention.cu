@@ -198,6 +198,9 @@ __device__ __forceinline__ int own_len(const Args &a, int b) {
   return max(0, min(len, most));
 }
 
+// A page number of a table: a negative one becomes the largest, which no cache has (-1 stands for "no page" in the kernels).
+__device__ __forceinline__ int page_number(int32_t x) { return (int)min((uint32_t)x, 0x7FFFFFFFu); }
+
 __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
   return ((x | y) >> 32) == 0 ? (int64_t)((uint32_t)x / (uint32_t)y) : x / y;
 }
@@ -430,12 +433,12 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
       page[0] = page[1] = -1;
       if (box) {
         const int j = p.tile * KU + at_box * box;
-        if (lane < boxes * HB && j < p.len) page[0] = pages[j / a.in_page] & 0x7FFFFFFF;
+        if (lane < boxes * HB && j < p.len) page[0] = page_number(pages[j / a.in_page]);
       } else {
 #pragma unroll
         for (int x = 0; x < 2; x++) {
           const int j = p.tile * KU + (lane + 32 * x) % KU;
-          if (lane + 32 * x < RB && j < p.len) page[x] = pages[j / a.in_page] & 0x7FFFFFFF;
+          if (lane + 32 * x < RB && j < p.len) page[x] = page_number(pages[j / a.in_page]);
         }
       }
     };
@@ -455,7 +458,7 @@ __global__ void __launch_bounds__(THREADS + 32 * bringers(D, WH), stream_per_sm(
       const int tiles = row_tiles(at), group = tiles == 1 ? at.pair : at.pair / tiles;
 #pragma unroll
       for (int x = 0; x < 2; x++) {
-        if (to_load[x] >= a.n_pages) {                 // (a negative number has become a large one)
+        if (to_load[x] >= a.n_pages) {                 // (a negative number among them, see page_number)
           to_load[x] = box ? a.n_pages : -1;           // outside the map: the box is filled with zeros
           if (a.status) *a.status = GTS_ERR_INVALID_PARAMS;
         }
@@ -1059,7 +1062,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
       int pair = (int)quotient(u0, n), tile = (int)(u0 - (int64_t)pair * n), kh = head_of(pair);
       auto look_up = [&](int t) {                          // this lane's page of tile t; -1: none
         const int key = t * TC_KEYS + lane * maps.box;
-        return lane < boxes && key < a.prefix_len ? a.prefix_pages[key / a.in_page] & 0x7FFFFFFF : -1;
+        return lane < boxes && key < a.prefix_len ? page_number(a.prefix_pages[key / a.in_page]) : -1;
       };
       int page_next = look_up(tile);
       for (int64_t u = u0; u < u1 && alive; u++) {
@@ -1068,7 +1071,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) k_prefix(const Args a, const Li
         const bool live = page >= 0;
         if (++tile == n) tile = 0, kh = head_of(++pair);
         if (u + 1 < u1) page_next = look_up(tile);         // arrives while this tile waits for room
-        if (page >= a.n_pages) {                           // (a negative number has become a large one)
+        if (page >= a.n_pages) {                           // (a negative number among them, see page_number)
           page = a.n_pages;                                // outside the map: the box is filled with zeros
           if (a.status) *a.status = GTS_ERR_INVALID_PARAMS;
         }
