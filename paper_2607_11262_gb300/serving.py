@@ -181,7 +181,17 @@ def _output(out, name, shape, dtype, device, stream):
     return out, strides
 
 
-class Rotary:
+class _Fixed:
+    """Attributes are set once, by the constructor: a descriptor made from them stays true."""
+
+    def __setattr__(self, name, value):
+        _refuse(f"{type(self).__name__}.{name} cannot be set: make a new {type(self).__name__}")
+
+    def __delattr__(self, name):
+        self.__setattr__(name, None)
+
+
+class Rotary(_Fixed):
     """The rotation of a model's heads: the frequencies of its pairs, held on the device in turns a position.
 
     Pair i of ``rot_dim / 2`` turns by ``base ** (-2 i / rot_dim)`` radians a position.  ``layout``: "half" pairs the
@@ -204,12 +214,22 @@ class Rotary:
             _refuse(f"unknown rotary layout {layout!r}")
         if not base > 0:
             _refuse("base must be positive")
-        self.head_dim, self.rot_dim, self.layout = head_dim, rot_dim, layout
-        self.theta, self.factor = self._frequencies(rot_dim, base, scaling)
-        units = [round(float(t) / (2 * math.pi) * 2.0 ** 64) % 2 ** 64 for t in self.theta]
-        self.units = torch.from_numpy(np.array(units, np.uint64).view(np.int64)).to(device)
-        self.device = self.units.device
-        self._values = [(self.units.data_ptr() if units else 0, rot_dim, _LAYOUTS[layout], self.factor, t) for t in (0, 1)]
+        theta, factor = self._frequencies(rot_dim, base, scaling)
+        units = [round(float(t) / (2 * math.pi) * 2.0 ** 64) % 2 ** 64 for t in theta]
+        units = torch.from_numpy(np.array(units, np.uint64).view(np.int64)).to(device)
+        vars(self).update(head_dim=head_dim, rot_dim=rot_dim, layout=layout, theta=theta, factor=factor, units=units,
+                          device=units.device)
+        self._describe()
+
+    def _describe(self):
+        at = _index(self.units, "units", (self.rot_dim // 2,), torch.int64, self.device)
+        vars(self).update(_at=at, _values=[(at, self.rot_dim, _LAYOUTS[self.layout], self.factor, t) for t in (0, 1)])
+
+    def _descriptor(self, transposed):
+        """The rotation's part of a call's descriptor; made again where the frequencies have moved (a copy of this object)."""
+        if self.units.data_ptr() != self._at:
+            self._describe()
+        return self._values[transposed]
 
     @staticmethod
     def _frequencies(rot_dim, base, scaling):
@@ -241,21 +261,34 @@ class Rotary:
         return theta, magnitude
 
 
-class PagedCache:
-    """Keys and values in pages: two [pages, page_size, kv_heads, head_dim] tensors of any outer strides."""
+class PagedCache(_Fixed):
+    """Keys and values in pages: two [pages, page_size, kv_heads, head_dim] tensors of any outer strides.  Other tensors (a
+    larger cache) take another PagedCache."""
 
     def __init__(self, k, v):
+        vars(self).update(k=k, v=v)
+        self._describe()
+
+    def _describe(self):
+        k, v = self.k, self.v
         _tensor(k, "k cache", 4)
         _tensor(v, "v cache", 4, k.dtype, k.device)
         if k.shape != v.shape:
             _refuse(f"k and v caches differ: {list(k.shape)}, {list(v.shape)}")
         if k.dtype not in _DTYPES:
             _refuse(f"cache: bfloat16, float16 or float32 wanted, got {k.dtype}")
-        self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.device
-        self.n_pages, self.page_size, self.kv_heads, self.head_dim = k.shape
-        if self.page_size < 1:
+        n_pages, page_size, kv_heads, head_dim = k.shape
+        if page_size < 1:
             _refuse("page_size must be positive")
-        self._values = (k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3], *k.shape, _DTYPES[k.dtype])
+        vars(self).update(dtype=k.dtype, device=k.device, n_pages=n_pages, page_size=page_size, kv_heads=kv_heads, head_dim=head_dim,
+                          _values=(k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3], *k.shape, _DTYPES[k.dtype]))
+
+    def _descriptor(self):
+        """The cache's part of a call's descriptor; made again where its tensors have moved (given other memory in place, or
+        copied with this object)."""
+        if self.k.data_ptr() != self._values[0] or self.v.data_ptr() != self._values[1]:
+            self._describe()
+        return self._values
 
     @classmethod
     def empty(cls, n_pages, page_size, kv_heads, head_dim, dtype, order="tokens", device="cuda"):
@@ -295,7 +328,7 @@ def _rope_call(q, k, positions, rotary, transposed, out_q, out_k, stream):
     out_q, qos = _output(out_q, "out_q", shape, dtype, device, stream)
     if T and (heads or kh):
         gts._check((_lib or _load()).gts_rope(_ROPE.pack(
-            T, heads, kh, dim, dt, pos, *rotary._values[transposed], q.data_ptr(), qs[0], qs[1], kp, ks[0], ks[1],
+            T, heads, kh, dim, dt, pos, *rotary._descriptor(transposed), q.data_ptr(), qs[0], qs[1], kp, ks[0], ks[1],
             out_q.data_ptr(), qos[0], qos[1], kop, kos[0], kos[1]), handle))
     return out_q, out_k
 
@@ -340,6 +373,7 @@ def append_kv(q, k, v, positions, slots, rotary, cache, out_q=None, status=None,
     page * page_size + index within the page, no two alike; a negative one is a padding row, of which nothing is
     written to the cache.  A slot beyond the cache writes nothing and stores GTS_ERR_INVALID_PARAMS to ``status``
     (int32 [1] on the device), where given."""
+    cache_values = cache._descriptor()
     dtype, device = cache.dtype, cache.device
     shape, qs = _tensor(q, "q", 3, dtype, device)
     handle = _handle(stream, device)
@@ -355,19 +389,19 @@ def append_kv(q, k, v, positions, slots, rotary, cache, out_q=None, status=None,
     out_q, qos = _output(out_q, "out_q", shape, dtype, device, stream)
     if T:
         gts._check((_lib or _load()).gts_append_kv(_APPEND.pack(
-            T, heads, pos, at, *rotary._values[0], q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(),
-            vs[0], vs[1], out_q.data_ptr(), qos[0], qos[1], *cache._values, st), handle))
+            T, heads, pos, at, *rotary._descriptor(0), q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(),
+            vs[0], vs[1], out_q.data_ptr(), qos[0], qos[1], *cache_values, st), handle))
     return out_q
 
 
-def _workspace_bytes(shape, cache, prefix_len, max_pages):
+def _workspace_bytes(shape, cache_values, prefix_len, max_pages):
     return int(_load().gts_attention_workspace_bytes(_ATTENTION.pack(
-        *shape[:3], 1.0, 0, 0, 0, 0, 0, 0, 0, 0, 0, *cache._values, 0, prefix_len, 0, max_pages, 0, 0, 0, 0)))
+        *shape[:3], 1.0, 0, 0, 0, 0, 0, 0, 0, 0, 0, *cache_values, 0, prefix_len, 0, max_pages, 0, 0, 0, 0)))
 
 
 def attention_workspace(cache, q, prefix_len, page_table, stream=None):
     """A workspace for ``prefix_attention`` calls of this shape; calls that may run at the same time need one each."""
-    need = _workspace_bytes(q.shape, cache, prefix_len, page_table.shape[1])
+    need = _workspace_bytes(q.shape, cache._descriptor(), prefix_len, page_table.shape[1])
     return _empty(max(need, 16), torch.uint8, q.device, stream)
 
 
@@ -383,6 +417,7 @@ def prefix_attention(q, cache, prefix_pages, prefix_len, page_table, lens, scale
     that sees nothing gets zeros and lse = -inf (float32 [seqs, new, heads]).  A page number or a length out of range
     is not followed and stores GTS_ERR_INVALID_PARAMS to ``status`` (int32 [1] on the device), where given.  A kernel whose
     waits run out (after two seconds) stores GTS_ERR_STEP_LIMIT there, and rows that miss a part are NaN."""
+    cache_values = cache._descriptor()
     dtype, device = cache.dtype, cache.device
     shape, qs = _tensor(q, "q", 4, dtype, device)
     handle = _handle(stream, device)
@@ -405,12 +440,12 @@ def prefix_attention(q, cache, prefix_pages, prefix_len, page_table, lens, scale
     else:
         lse_at = _index(lse, "lse", (B, new, heads), torch.float32, device)
     if workspace is None:
-        workspace = _empty(max(_workspace_bytes(shape, cache, prefix_len, max_pages), 16), torch.uint8, device, stream)
+        workspace = _empty(max(_workspace_bytes(shape, cache_values, prefix_len, max_pages), 16), torch.uint8, device, stream)
     elif workspace.device != device or not workspace.is_contiguous():
         _refuse(f"workspace: contiguous on {device} wanted")
     if B and new:
         gts._check((_lib or _load()).gts_prefix_attention(_ATTENTION.pack(
             B, new, heads, 1.0 / math.sqrt(dim) if scale is None else scale, q.data_ptr(), qs[0], qs[1], qs[2],
-            out.data_ptr(), os[0], os[1], os[2], lse_at, *cache._values, prefix_at, prefix_len, table_at, max_pages, lens_at,
+            out.data_ptr(), os[0], os[1], os[2], lse_at, *cache_values, prefix_at, prefix_len, table_at, max_pages, lens_at,
             workspace.data_ptr(), workspace.nbytes, st), handle))
     return out, lse
