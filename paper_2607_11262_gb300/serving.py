@@ -21,6 +21,7 @@ import struct
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 from . import gts
 from .gts import GtsError
@@ -334,36 +335,59 @@ def _rope_call(q, k, positions, rotary, transposed, out_q, out_k, stream):
 
 
 class _Rope(torch.autograd.Function):
+    """The rotation of each pair, or its transpose.  Either is linear, so its gradient is the other one and its tangent is itself,
+    through this function again: derivatives of any order are."""
+
     @staticmethod
-    def forward(ctx, q, k, positions, rotary):
+    def forward(q, k, positions, rotary, transposed):
+        return _rope_call(q, k, positions, rotary, transposed, None, None, None)
+
+    @staticmethod
+    def setup_context(ctx, inputs, output):
+        _, _, positions, ctx.rotary, ctx.transposed = inputs
         ctx.save_for_backward(positions)
-        ctx.rotary = rotary
-        return _rope_call(q, k, positions, rotary, 0, None, None, None)
+        ctx.save_for_forward(positions)
 
     @staticmethod
     def backward(ctx, dq, dk):
-        dq, dk = rope_grad(_inner(dq), _inner(dk), ctx.saved_tensors[0], ctx.rotary)
-        return dq, dk, None, None
+        want_q, want_k = ctx.needs_input_grad[:2]
+        x = [_inner(t) for t, want in ((dq, want_q), (dk, want_k)) if want]
+        got = list(_Rope.apply(x[0], x[1] if len(x) > 1 else None, ctx.saved_tensors[0], ctx.rotary, 1 - ctx.transposed))
+        return got.pop(0) if want_q else None, got.pop(0) if want_k else None, None, None, None
+
+    @staticmethod
+    def jvp(ctx, tq, tk, *_):
+        return _Rope.apply(_inner(tq), _inner(tk), ctx.saved_tensors[0], ctx.rotary, ctx.transposed)
 
 
 def _inner(t):
     return t if t is None or t.stride(-1) == 1 else t.contiguous()
 
 
-def rope(q, k, positions, rotary, out_q=None, out_k=None, stream=None):
-    """q [tokens, heads, head_dim] and k [tokens, kv_heads, head_dim] (or None) rotated to ``positions`` [tokens] int32:
-    (q', k').  ``out_q`` / ``out_k`` may be q and k themselves.  With outputs and stream left to the call, gradients
-    flow through it."""
-    if torch.is_grad_enabled() and (q.requires_grad or (k is not None and k.requires_grad)):
+def _differentiated(t):
+    """Whether a gradient or a tangent goes through t."""
+    return t is not None and (t.requires_grad and torch.is_grad_enabled() or
+                              getattr(forward_ad, "_current_level", 0) >= 0 and forward_ad.unpack_dual(t).tangent is not None)
+
+
+def _rope(q, k, positions, rotary, transposed, out_q, out_k, stream):
+    if _differentiated(q) or _differentiated(k):
         if out_q is not None or out_k is not None or stream is not None:
             _refuse("rope: gradients need the call's own outputs and the current stream")
-        return _Rope.apply(q, k, positions, rotary)
-    return _rope_call(q, k, positions, rotary, 0, out_q, out_k, stream)
+        return _Rope.apply(q, k, positions, rotary, transposed)
+    return _rope_call(q, k, positions, rotary, transposed, out_q, out_k, stream)
+
+
+def rope(q, k, positions, rotary, out_q=None, out_k=None, stream=None):
+    """q [tokens, heads, head_dim] and k [tokens, kv_heads, head_dim] (or None) rotated to ``positions`` [tokens] int32:
+    (q', k').  ``out_q`` / ``out_k`` may be q and k themselves.  With outputs and stream left to the call, gradients (of any
+    order) and tangents flow through it."""
+    return _rope(q, k, positions, rotary, 0, out_q, out_k, stream)
 
 
 def rope_grad(dq, dk, positions, rotary, out_dq=None, out_dk=None, stream=None):
-    """The gradients of q and k from those of ``rope``'s results: the transposed rotation."""
-    return _rope_call(dq, dk, positions, rotary, 1, out_dq, out_dk, stream)
+    """The gradients of q and k from those of ``rope``'s results: the transposed rotation.  Differentiable like ``rope``."""
+    return _rope(dq, dk, positions, rotary, 1, out_dq, out_dk, stream)
 
 
 def append_kv(q, k, v, positions, slots, rotary, cache, out_q=None, status=None, stream=None):
