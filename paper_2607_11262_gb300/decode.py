@@ -19,6 +19,7 @@ SMS = 152
 GHZ = 1.92                       # SM clock that measured times are compared at
 ROWS, PREFIX_KEYS = 256, 128     # query rows of a block and keys of its tiles, on the prefix
 OWN_TILE_KEYS = 64               # keys of a tile of a sequence's own (of one head, or 16 of each of four)
+PAGE = 64                        # tokens of a page in Step
 
 CASES = (dict(seqs=64, prefix=8192, own=256), dict(seqs=128, prefix=32768, own=128), dict(seqs=256, prefix=32768, own=512))
 
@@ -59,20 +60,52 @@ def own_cta(tiles, stages=3, tile_bytes=32768, fma=2 * 16 * 64 * 128, softmax_op
     return t
 
 
+def prefix_blocks(prefix_tiles, kv_heads, row_tiles, own_rows, own_tiles, own_pairs):
+    """SMs that the prefix gets at a head of 128, as the kernels work it out from the lengths (``prefix_sms`` in
+    csrc/attention.cu, which has the reasons and where the costs come from): in units of an own tile's time on an SM."""
+    if own_tiles == 0:
+        return SMS
+    f = np.float32                                     # in 32 bits, like the kernels
+    tile, pair = f(2.2), f(8)
+    p = (tile * f(prefix_tiles) + pair) * f(kv_heads) * f(row_tiles)
+    o = (f(own_tiles) + f(3) * f(own_pairs)) * f({16: 0.8, 32: 1.1}.get(own_rows, 2.1))
+    memory = f(own_tiles) / f(104)
+    even = max(1, min(SMS - 1, int(p / max((p + o) / f(SMS), memory) + f(0.5))))
+    side = row_tiles if even >= row_tiles else 1       # row tiles that pass along the keys side by side
+    units = prefix_tiles * kv_heads * (row_tiles if side == 1 else 1)
+    per = -(-units // (even // side))
+    best, least = even, f(np.inf)
+    for x in range(max(1, per - 1), per + 2):          # whole numbers of tiles to a block
+        sms = -(-units // x) * side
+        if sms < SMS:
+            time = max((tile + pair / f(prefix_tiles)) * f(x), o / f(SMS - sms), memory)
+            if time < least:
+                best, least = sms, time
+    return best
+
+
+def deal(seqs, prefix, own, heads=32, kv_heads=8):
+    """(tiles of each prefix block, SMs that stream own keys, own tiles of each of their two blocks) of a step at a head of 128."""
+    group = heads // kv_heads
+    row_tiles, tiles = -(-seqs * group // ROWS), -(-prefix // PREFIX_KEYS)
+    rows = 16 if group <= 16 else 32 if group <= 32 else 64
+    # by fours: a unit is 16 keys of four heads, else 64 of one
+    at_once = 4 if rows == 16 and kv_heads % 4 == 0 and -(-own // PAGE) * PAGE <= 2048 else 1
+    pairs = kv_heads // at_once * -(-group // rows)    # of a sequence
+    own_tiles = seqs * -(-own // (OWN_TILE_KEYS // at_once)) * pairs
+    blocks = prefix_blocks(tiles, kv_heads, row_tiles, rows, own_tiles, seqs * pairs)
+    side = row_tiles if blocks >= row_tiles else 1
+    units = tiles * kv_heads * (row_tiles if side == 1 else 1)
+    per = -(-units // (blocks // side))
+    counts = [min(per, units - at) for at in range(0, units, per) for _ in range(side)]
+    streams = max(1, SMS - blocks)
+    return counts, streams, -(-own_tiles // (2 * streams))
+
+
 def graph(seqs, prefix, own, heads=32, kv_heads=8):
     """The step's attention: blocks on the prefix (256 rows, tiles of 128 keys, two halves in turn) beside SMs that stream the
-    sequences' own keys, dealt out as the kernels do it."""
-    row_tiles = -(-seqs * (heads // kv_heads) // ROWS)
-    units = -(-prefix // PREFIX_KEYS) * kv_heads
-    own_tiles = seqs * -(-own // OWN_TILE_KEYS) * kv_heads
-    pairs = seqs * kv_heads // 4
-    p, o = 2.2 * units * row_tiles, own_tiles + 2.0 * pairs
-    each = max((p + o) / SMS, own_tiles / 104)
-    blocks = max(row_tiles, min(SMS - 1, int(p / each + 0.5)))
-    per = -(-units // (blocks // row_tiles))
-    counts = [min(per, units - s * per) for s in range(blocks // row_tiles) if s * per < units for _ in range(row_tiles)]
-    streams = SMS - len(counts)
-    rest = -(-own_tiles // (2 * streams))
+    sequences' own keys, dealt out as the kernels do it (``deal``)."""
+    counts, streams, rest = deal(seqs, prefix, own, heads, kv_heads)
     tpls, kind = [], {}
 
     def template(key, make):
@@ -91,7 +124,7 @@ class Step:
     """One decode step of ``seqs`` sequences with ``own`` tokens of their own (the newest included) after a shared prompt of
     ``prefix`` tokens."""
 
-    def __init__(self, seqs, prefix, own, heads=32, kv_heads=8, head_dim=128, page=64, dtype=None, seed=0, device="cuda"):
+    def __init__(self, seqs, prefix, own, heads=32, kv_heads=8, head_dim=128, page=PAGE, dtype=None, seed=0, device="cuda"):
         import torch
 
         from . import serving as S
