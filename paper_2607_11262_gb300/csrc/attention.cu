@@ -211,8 +211,8 @@ __device__ __forceinline__ int64_t quotient(int64_t x, int64_t y) {
 // (0.7 us), begin and end of its pair 8 or 4, the end of an own pair 3; own work with tiles of 16, 32 or 64 rows 0.8, 1.1 or 2.1
 // times as long; and own tiles alone cannot go faster than memory brings them, 104 to that time.  Every block of the prefix takes
 // the same whole number of tiles: of that number, one fewer and one more, the one with which the slower kernel is the fastest
-// is taken, and no more SMs than it needs (64 sequences of 16 tokens over 8192 + 512 at a head of 256: 562 us without this
-// choice, 413 with it; 64 of 3 over 8192 + 4096 at 128: 173 and 137).  Both kernels come to the same numbers from the lengths.
+// is taken, and no more SMs than it needs (64 sequences of 3 tokens over 8192 + 4096: 158 us without this choice, 139 with it; 64 of
+// 16 over 8192 + 512 at a head of 256: 407 and 410).  Both kernels come to the same numbers from the lengths.
 template <int D>
 __device__ __forceinline__ int prefix_sms(const Args &a, const Line &prefix, int own_rows, int64_t own_tiles, int64_t own_pairs) {
   if (own_tiles == 0) return SMS;
@@ -269,10 +269,11 @@ struct Place { int b, len, n, pairs, pair, tile; };
 // its own running maximum and sum.  Weights are rounded to the type of the values for their product with them (the sum is of
 // the unrounded ones); everything else is in 32 bits.
 //
-// Bound by memory for long sequences: 128 of up to 4096 tokens, 1.08 GB, 175 us, 6.2 TB/s, 91% of the rate of a copy; 256 of up
-// to 1024, 537 MB, 94 us, 84%, where the ends of pairs and the first tiles' latencies count.  Tiles of 32 and 64 rows (5 and 16
-// new tokens) are bound by the latency of their products with two warps to a scheduler: 128 of 1..2048, as many bytes, in 113 and
-// 175 us.
+// Bound by memory for long sequences: 128 of 1..4096 tokens, 1.08 GB, 178 us, 6.1 TB/s, 90% of the rate of a copy (187 us with the
+// join); 256 of 1..1024, 537 MB, 94 us, 84% (105), where the ends of pairs and the first tiles' latencies count.  Tiles of 32 and
+// 64 rows (5 and 16 new tokens) are bound by the latency of their products with two warps to a scheduler: 128 of 1..2048, 537 MB
+// too, in 102 and 170 us (111 and 183).  Bytes spilled at a head of 128, a thread: 100 with 16 rows of one head, 32 by fours, 8
+// and 96 with 32 and 64 rows; at 256, 0, 24 and 52; at 64, none, 8 and 60.
 template <int D, int WM, int WH> struct Ring {
   static constexpr int STAGES = (D == 64 ? 4 : 3) - (WM > 1);   // as many as stream_per_sm blocks find room for
   static constexpr int TILE = KEYS * D * 2;                     // bytes of a tile of keys or of values
@@ -971,8 +972,9 @@ constexpr uint32_t OPERAND_HI = 1024 >> 4 | 1u << 14 | 2u << 29;
 // 256 x 128 x 128 whose products take 2048.  What was tried: scores in pieces of 32 (shorter code, but a longer chain: 3200),
 // all 128 scores in registers (spills), one issuing thread for both halves (3200), no turns (3300), turns from the second part
 // of the weights on (7% slower), tiles of 64 keys with scores a tile ahead as at a head of 256 (8% slower: products of 64
-// columns wait for shared memory).  128 x 4 rows over 131072 keys on 140 SMs: 185 us, 1.47 PFLOP/s, 84% of what cuBLAS sustains on
-// as many; 256 x 4 rows over 32768 on 75, beside the own keys' kernel: 165 us, 0.83.
+// columns wait for shared memory).  128 x 4 rows over 131072 keys on 142 SMs: 187 us, 1.47 PFLOP/s, 82% of cuBLAS's burst rate on
+// as many; 256 x 4 rows over 32768 on 84, beside the own keys' kernel: 156 us, 0.88, 83%.  Bytes spilled a thread: 104 at a head of
+// 128, 56 at 64, 176 at 256.
 //
 // A head of 256 has room for one half in tensor memory (256 columns of sums): 128 rows, tiles of 64 keys, and two buffers of
 // scores, so that the products of the next tile's scores run while the rows make their weights.
@@ -1607,10 +1609,10 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
   const int D = (int)d.cache.head_dim, group = (int)(d.q_heads / d.cache.kv_heads);
   const int64_t own_rows = (int64_t)d.n_new * group, all = own_rows * d.n_seqs;
   Plan p = {};
-  // On the tensor cores even few rows of the prefix go faster (4 rows over 8192 keys 23 us, in the streaming kernel 35; 512 over
-  // 256 43 and 47), except over the shortest prefixes, where a launch more costs what it gains.
-  // At a head of 256, with smaller tiles, from 32 rows on (16 over 8192 keys take 37 us here and 34 there, 256 over 512 70 and 77, 512
-  // over 32768 229 and 705).
+  // On the tensor cores even few rows of the prefix go faster (4 rows of one key head over 8192 keys 28 us on the GPU, in the streaming
+  // kernel 34; of eight key heads 28 and 40; 512 over 256 29 and 33), except over the shortest prefixes, where a launch more costs what
+  // it gains.  At a head of 256, with smaller tiles, from 32 rows on (16 over 8192 keys take 43 us here and 31 there, 256 over 512 53
+  // and 48, 512 over 32768 198 and 459).
   tensor &= d.prefix_len >= 256 && d.prefix_len * (uint64_t)std::max<int64_t>(all, 16) >= 16384 && (D < 256 || all >= 32);
   p.way = tensor ? TENSOR : d.prefix_len && all > APART_ROWS && own_rows <= 32 ? APART : TOGETHER;
   size_t n = 0;
@@ -1620,8 +1622,9 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
     return x;
   };
   // A pair's begin and end (first loads, queries, the join of its warps, its results) in units of its tiles.  Without them blocks
-  // with many short pairs end last: 128 sequences of 16 tokens over 1..2048 take 313 us without and 175 with 7 (4: 187, 12: 186);
-  // of 5, 161 and 113 with 5; 256 of one over 1..1024, by fours, 119 and 103 with 8; 128 of one over 1..4096 187 and 178 with 2.
+  // with many short pairs end last: 128 sequences of 16 tokens over 1..2048 take 280 us without and 183 with 7 (4: 184, 12: 192);
+  // of 5, 150 and 111 with 5 (4: 110, 12: 117); 256 of one over 1..1024, by fours, 118 and 105 with 8 (4: 109, 12: 105); 128 of one
+  // over 1..4096 208 and 187 with 2 (4: 184, 12: 183).
   auto line = [&](Line &w, int heads, int rows, int keys, int blocks, bool has_prefix, bool has_own) {
     w.has_prefix = has_prefix, w.has_own = has_own, w.heads = heads, w.rows = rows, w.keys = keys, w.blocks = blocks, w.lead = heads > 1 ? 8 : rows == 16 ? 2 : rows == 32 ? 5 : 7;
     w.prefix_tiles = (int)((all + rows - 1) / rows), w.own_tiles = (int)((own_rows + rows - 1) / rows);
@@ -1632,8 +1635,9 @@ Plan make_plan(const gts_attention_desc &d, bool tensor, char *at) {
   };
   const int own_tile = own_rows <= 16 ? 16 : own_rows <= 32 ? 32 : 64;
   // Few rows: a warp to each of four heads, which have nothing to join at a pair's end, where the heads can be had by fours.
-  // Long sequences seldom end, and their tiles of 64 keys of one head come in larger boxes: 256 of 1..1024 tokens take 103 us by
-  // fours and 107 by ones, 128 of 1..4096 take 183 and 178.
+  // Long sequences seldom end, and their tiles of 64 keys of one head come in larger boxes.  The table's width stands for the lengths,
+  // which only the device knows: 256 of 1..1024 tokens take 105 us by fours and 114 by ones (which is what a wide table gets), 128 of
+  // 1..2048 103 and 109.  At 128 of 1..4096 the kernel of one head has lost its lead to its spills: 187, by fours 180.
   const bool fours = own_tile == 16 && D <= 128 && d.cache.kv_heads % WARPS == 0 && (uint64_t)d.max_pages * d.cache.page_size <= 2048;
   const int heads = fours ? WARPS : 1;
   line(p.own, heads, own_tile, KEYS / heads, stream_blocks(D), p.way == TOGETHER && d.prefix_len, true);

@@ -9,7 +9,8 @@
 // Bound by memory traffic: each value is read once and written once.  A block takes a few tokens and all their heads: the
 // angles are computed once per block into shared memory, and the values move as 16-byte vectors.  What counts beside that is
 // that many blocks stand on an SM (32 registers a thread): several vectors of a thread in flight, which take registers, and
-// angles kept in registers over the heads were slower by 5 to 60%, and the packed conversions gained 5%.
+// angles kept in registers over the heads were slower by 5 to 60%, and the packed conversions gained 5%.  Under that limit 8 of the 24
+// instances spill 4 to 24 bytes a thread.
 // Measured: 16384 tokens of 32 + 8 heads of 128 in 16 bits, 336 MB, 59 us, 85% of the rate of a copy; 8191 in 32 bits 54 us,
 // 92%; 16372 appended in 16 bits, 403 MB, 69 us, 87%.
 #include <cuda_bf16.h>

@@ -203,8 +203,9 @@ class Rotary(_Fixed):
     * ``{"kind": "ntk", "factor": s}``: the base times ``s ** (rot_dim / (rot_dim - 2))``, which divides the lowest
       frequency by s and keeps the highest;
     * ``{"kind": "by_parts", "factor": s, "original_len": L, "low": a, "high": b}``: frequencies of fewer than a
-      turns in L positions divided by s, those of more than b kept, a linear blend between; rotated values times
-      ``magnitude`` (default ``0.1 ln s + 1``).
+      turns in L positions divided by s, those of more than b kept, between them a blend that is linear in the turns
+      (a model whose blend is linear in the pair's index has other frequencies); rotated values times ``magnitude``
+      (default ``0.1 ln s + 1``).
     """
 
     def __init__(self, head_dim, rot_dim=None, base=10000.0, layout="half", scaling=None, device="cuda"):
