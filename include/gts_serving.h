@@ -2,7 +2,8 @@
  * gts_serving.h -- C ABI of libgts's operators of a decode step: rotary
  * positions, appending keys and values to a paged cache, and attention of a
  * batch over a prefix that all its sequences share and each sequence's own
- * tokens.
+ * tokens; and of prompts: attention of packed sequences with its gradient,
+ * attention of chunks of new tokens over a paged cache, and copies of pages.
  *
  * They are the work whose tile graphs the simulator takes (attention and the
  * kernels around it), as kernels that run on the machine itself, so that a
@@ -126,6 +127,80 @@ gts_status gts_prefix_attention(const gts_attention_desc *desc, void *stream);
 /* Bytes of workspace gts_prefix_attention wants for the shape in desc (its pointers are not looked at); 0 where the
  * shape is refused. */
 size_t gts_attention_workspace_bytes(const gts_attention_desc *desc);
+
+/* Attention of packed sequences over themselves.  Sequence b's tokens are the rows starts[b] .. starts[b + 1] - 1 of q, k, v and
+ * out; its query i sees its keys j <= i (causal) or all of them.  With s_j = scale * q_i . k_j over the keys seen and m = max s_j:
+ *   out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),   lse = m + log sum_j exp(s_j - m).
+ * Query head h uses key head h / (q_heads / kv_heads).  Rows of no sequence (before starts[0], from starts[n_seqs] on) are left as
+ * they are, or get out = 0 (zero_rest bit 0) and lse = -infinity (bit 1); what they hold in q, k and v is not looked at.  starts
+ * has to rise from 0 or more to n_tokens at most: other values are clamped to that (d_status, see above).
+ * Types: GTS_BF16 or GTS_F16; head_dim 64 or 128; q_heads a multiple of kv_heads, at most 128 times it; scale positive.  Products
+ * are summed in 32 bits. */
+typedef struct {
+  uint32_t n_seqs, n_tokens, q_heads, kv_heads, head_dim;
+  int32_t dtype;
+  uint32_t causal, zero_rest;   /* 0 or 1; bits */
+  float scale;
+  const int32_t *starts;        /* [n_seqs + 1] */
+  gts_heads q, k, v, out;
+  float *lse;                   /* [n_tokens][q_heads], contiguous; may be NULL */
+  void *workspace;              /* gts_prompt_workspace_bytes, 16-byte aligned; contents need not be kept */
+  size_t workspace_bytes;
+  int32_t *d_status;            /* optional */
+} gts_prompt_desc;
+gts_status gts_prompt_attention(const gts_prompt_desc *desc, void *stream);
+
+/* Bytes of workspace for the shape in desc (pointers and strides are not looked at); 0 where the shape is refused. */
+size_t gts_prompt_workspace_bytes(const gts_prompt_desc *desc);
+
+/* The gradients of gts_prompt_attention: forward is its desc, with out and lse as it left them (they are read; its workspace is
+ * this call's).  With p_ij = exp(s_ij - lse_i), e_i = sum_d dout_id out_id - dlse_i and ds_ij = p_ij (dout_i . v_j - e_i):
+ *   dv_j = sum_i p_ij dout_i,   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,
+ * those of a key head summed over its query heads.  Rows of no sequence are left as they are, or get 0: dq, dk, dv with
+ * bits 0, 1, 2 of forward.zero_rest.
+ * Every sum has one order: results repeat bit for bit. */
+typedef struct {
+  gts_prompt_desc forward;
+  gts_heads dout;
+  const float *dlse;            /* as lse; may be NULL: zero */
+  gts_heads dq, dk, dv;
+} gts_prompt_grad_desc;
+gts_status gts_prompt_attention_grad(const gts_prompt_grad_desc *desc, void *stream);
+size_t gts_prompt_grad_workspace_bytes(const gts_prompt_grad_desc *desc);
+
+/* Attention of chunks of new tokens over a paged cache that holds them already.  Sequence b's queries are the rows starts[b] ..
+ * starts[b + 1] - 1 of q, its keys the first lens[b] tokens of its pages (page_table row b); the last query sees all of them,
+ * and query i those j < lens[b] - (n - 1 - i), n its sequence's queries.  A query that sees no key gets out = 0 and lse =
+ * -infinity.  Otherwise as gts_prompt_attention; cache values that no query sees may be anything, NaN included. */
+typedef struct {
+  uint32_t n_seqs, n_tokens, q_heads, zero_rest;
+  float scale;
+  const int32_t *starts;        /* [n_seqs + 1] */
+  gts_heads q, out;
+  float *lse;                   /* [n_tokens][q_heads], contiguous; may be NULL */
+  gts_cache cache;
+  const int32_t *page_table;    /* [n_seqs][max_pages] */
+  uint32_t max_pages;
+  const int32_t *lens;          /* [n_seqs] */
+  void *workspace;
+  size_t workspace_bytes;
+  int32_t *d_status;
+} gts_chunk_desc;
+gts_status gts_chunk_attention(const gts_chunk_desc *desc, void *stream);
+size_t gts_chunk_workspace_bytes(const gts_chunk_desc *desc);
+
+/* The first tokens[i] tokens (NULL: all) of page src[i] of one cache, keys and values, go to page dst[i] of another one, or of the
+ * same.  The caches have the same page_size, kv_heads, head_dim and dtype, and strides of their own.  A negative src or dst
+ * copies nothing, nor does a page onto itself; tokens is clamped to 0 .. page_size.  A page may be copied to several others, but
+ * what a page holds that is written twice, or read and written, in one call is unspecified. */
+typedef struct {
+  uint32_t n_copies;
+  const int32_t *src, *dst;     /* [n_copies] */
+  const int32_t *tokens;        /* [n_copies] or NULL */
+  gts_cache cache, into;
+  int32_t *d_status;            /* optional */
+} gts_copy_pages_desc;
+gts_status gts_copy_pages(const gts_copy_pages_desc *desc, void *stream);
 
 #ifdef __cplusplus
 }

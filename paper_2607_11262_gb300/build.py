@@ -8,7 +8,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 SRC = os.path.join(CSRC, "gts.cu")                  # the simulator (compiled through libgts.cu)
-SOURCES = ("libgts.cu", "rotary.cu", "attention.cu")
+SOURCES = ("libgts.cu", "rotary.cu", "attention.cu", "prompt.cu", "pages.cu")
 HDR = os.path.join(ROOT, "include", "gts.h")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD_DIR, "libgts.so")

@@ -1,5 +1,6 @@
 """The operators of a decode step, on the GPU: rotary positions (and their gradient), appending keys and values to a
-paged cache, and attention of a batch over a shared prefix and each sequence's own tokens.
+paged cache, and attention of a batch over a shared prefix and each sequence's own tokens.  And those of prompts: attention
+of packed sequences (and its gradient), attention of chunks of new tokens over a paged cache, and copies of pages.
 
 They are the kernels whose tile graphs the simulator takes, run on the machine itself.  Functions named like the C ABI
 in include/gts_serving.h marshal its descriptors; the ones below them take torch tensors:
@@ -8,6 +9,10 @@ in include/gts_serving.h marshal its descriptors; the ones below them take torch
     cache = PagedCache.empty(n_pages, page_size, kv_heads, 128, torch.bfloat16)
     q = append_kv(q, k, v, positions, slots, rotary, cache)    # one step's new tokens
     out, lse = prefix_attention(q, cache, prefix_pages, prefix_len, page_table, lens)
+
+    out, lse = prompt_attention(q, k, v, starts)               # packed sequences, with gradients
+    out, lse = chunk_attention(q, starts, cache, page_table, lens)
+    copy_pages(cache, src, dst, tokens)
 
 Tensors are on one CUDA device, the current one, with a contiguous innermost dimension and any other strides.  Work is
 enqueued on ``stream`` (default: torch's current stream); outputs and workspaces that a call allocates belong to that
@@ -29,7 +34,9 @@ from .gts import GtsError
 GTS_BF16, GTS_F16, GTS_F32 = 0, 1, 2
 GTS_ROTARY_HALF, GTS_ROTARY_INTERLEAVED = 0, 1
 
-EXPORTS = ("gts_rope", "gts_append_kv", "gts_prefix_attention", "gts_attention_workspace_bytes")
+EXPORTS = ("gts_rope", "gts_append_kv", "gts_prefix_attention", "gts_prompt_attention", "gts_prompt_attention_grad",
+           "gts_chunk_attention", "gts_copy_pages", "gts_attention_workspace_bytes", "gts_prompt_workspace_bytes",
+           "gts_prompt_grad_workspace_bytes", "gts_chunk_workspace_bytes")
 
 _DTYPES = {torch.bfloat16: GTS_BF16, torch.float16: GTS_F16, torch.float32: GTS_F32}
 _LAYOUTS = {"half": GTS_ROTARY_HALF, "interleaved": GTS_ROTARY_INTERLEAVED}
@@ -73,12 +80,38 @@ class AttentionDesc(ctypes.Structure):
                 ("max_pages", _u32), ("lens", _vp), ("workspace", _vp), ("workspace_bytes", _sz), ("d_status", _vp)]
 
 
+class PromptDesc(ctypes.Structure):
+    _fields_ = [("n_seqs", _u32), ("n_tokens", _u32), ("q_heads", _u32), ("kv_heads", _u32), ("head_dim", _u32), ("dtype", _i32),
+                ("causal", _u32), ("zero_rest", _u32), ("scale", _f32), ("starts", _vp), ("q", HeadsDesc), ("k", HeadsDesc),
+                ("v", HeadsDesc), ("out", HeadsDesc), ("lse", _vp), ("workspace", _vp), ("workspace_bytes", _sz), ("d_status", _vp)]
+
+
+class PromptGradDesc(ctypes.Structure):
+    _fields_ = [("forward", PromptDesc), ("dout", HeadsDesc), ("dlse", _vp), ("dq", HeadsDesc), ("dk", HeadsDesc), ("dv", HeadsDesc)]
+
+
+class ChunkDesc(ctypes.Structure):
+    _fields_ = [("n_seqs", _u32), ("n_tokens", _u32), ("q_heads", _u32), ("zero_rest", _u32), ("scale", _f32), ("starts", _vp),
+                ("q", HeadsDesc), ("out", HeadsDesc), ("lse", _vp), ("cache", CacheDesc), ("page_table", _vp), ("max_pages", _u32),
+                ("lens", _vp), ("workspace", _vp), ("workspace_bytes", _sz), ("d_status", _vp)]
+
+
+class CopyPagesDesc(ctypes.Structure):
+    _fields_ = [("n_copies", _u32), ("src", _vp), ("dst", _vp), ("tokens", _vp), ("cache", CacheDesc), ("into", CacheDesc),
+                ("d_status", _vp)]
+
+
 # The same layouts as format strings: the torch entry points pack a descriptor in one go, which takes a fifth of the time of
 # filling the structures above (about 2 against 10 us a call).
 _HEADS_FORMAT, _ROTARY_FORMAT, _CACHE_FORMAT = "Pqq", "PIifI", "PPqqqqqqIIIIi4x"
 _ROPE = struct.Struct("@IIIIiP" + _ROTARY_FORMAT + 4 * _HEADS_FORMAT)
 _APPEND = struct.Struct("@IIPP" + _ROTARY_FORMAT + 4 * _HEADS_FORMAT + _CACHE_FORMAT + "P")
 _ATTENTION = struct.Struct("@IIIf" + 2 * "Pqqq" + "P" + _CACHE_FORMAT + "PI4xPI4xPPNP")
+_PROMPT_FORMAT = "IIIIIiIIf4xP" + 4 * _HEADS_FORMAT + "PPNP"
+_PROMPT = struct.Struct("@" + _PROMPT_FORMAT)
+_PROMPT_GRAD = struct.Struct("@" + _PROMPT_FORMAT + _HEADS_FORMAT + "P" + 3 * _HEADS_FORMAT)
+_CHUNK = struct.Struct("@IIIIf4xP" + 2 * _HEADS_FORMAT + "P" + _CACHE_FORMAT + "PI4xPPNP")
+_COPY_PAGES = struct.Struct("@I4xPPP" + 2 * _CACHE_FORMAT + "P")
 
 _lib = None
 
@@ -87,10 +120,9 @@ def _load():
     global _lib
     if _lib is None:
         lib = gts.load()
-        for name in EXPORTS[:3]:
+        for name in EXPORTS:
             f = getattr(lib, name)
-            f.argtypes, f.restype = [_vp, _vp], _i32
-        lib.gts_attention_workspace_bytes.argtypes, lib.gts_attention_workspace_bytes.restype = [_vp], _sz
+            f.argtypes, f.restype = ([_vp], _sz) if name.endswith("_bytes") else ([_vp, _vp], _i32)
         _lib = lib
     return _lib
 
@@ -110,6 +142,34 @@ def gts_prefix_attention(desc: AttentionDesc, stream: int = 0):
 
 def gts_attention_workspace_bytes(desc: AttentionDesc) -> int:
     return int(_load().gts_attention_workspace_bytes(ctypes.byref(desc)))
+
+
+def gts_prompt_attention(desc: PromptDesc, stream: int = 0):
+    gts._check(_load().gts_prompt_attention(ctypes.byref(desc), stream))
+
+
+def gts_prompt_workspace_bytes(desc: PromptDesc) -> int:
+    return int(_load().gts_prompt_workspace_bytes(ctypes.byref(desc)))
+
+
+def gts_prompt_attention_grad(desc: PromptGradDesc, stream: int = 0):
+    gts._check(_load().gts_prompt_attention_grad(ctypes.byref(desc), stream))
+
+
+def gts_prompt_grad_workspace_bytes(desc: PromptGradDesc) -> int:
+    return int(_load().gts_prompt_grad_workspace_bytes(ctypes.byref(desc)))
+
+
+def gts_chunk_attention(desc: ChunkDesc, stream: int = 0):
+    gts._check(_load().gts_chunk_attention(ctypes.byref(desc), stream))
+
+
+def gts_chunk_workspace_bytes(desc: ChunkDesc) -> int:
+    return int(_load().gts_chunk_workspace_bytes(ctypes.byref(desc)))
+
+
+def gts_copy_pages(desc: CopyPagesDesc, stream: int = 0):
+    gts._check(_load().gts_copy_pages(ctypes.byref(desc), stream))
 
 
 # ---------------------------------------------------------------- torch tensors
@@ -474,3 +534,223 @@ def prefix_attention(q, cache, prefix_pages, prefix_len, page_table, lens, scale
             out.data_ptr(), os[0], os[1], os[2], lse_at, *cache_values, prefix_at, prefix_len, table_at, max_pages, lens_at,
             workspace.data_ptr(), workspace.nbytes, st), handle))
     return out, lse
+
+
+# ---------------------------------------------------------------- prompts
+def _heads(t, strides):
+    return t.data_ptr(), strides[0], strides[1]
+
+
+def _workspace(workspace, need, device, stream):
+    if workspace is None:
+        return _empty(max(need, 16), torch.uint8, device, stream)
+    if workspace.device != device or not workspace.is_contiguous():
+        _refuse(f"workspace: contiguous on {device} wanted")
+    return workspace
+
+
+def _prompt_shape(q, k, v, starts):
+    """(values of the descriptor up to dtype, strides of q, k and v, device, address of starts)"""
+    shape, qs = _tensor(q, "q", 3)
+    device, dtype = q.device, q.dtype
+    dt = _DTYPES.get(dtype)
+    if dt is None or dt == GTS_F32:
+        _refuse(f"q: bfloat16 or float16 wanted, got {dtype}")
+    T, heads, dim = shape
+    (kshape, ks), (vshape, vs) = _tensor(k, "k", 3, dtype, device), _tensor(v, "v", 3, dtype, device)
+    if kshape[0] != T or kshape[2] != dim or vshape != kshape:
+        _refuse(f"k and v: [{T}, kv_heads, {dim}] wanted, got {list(kshape)} and {list(vshape)}")
+    return (_sequences(starts), T, heads, kshape[1], dim, dt), qs, ks, vs, device, _index(starts, "starts", (None,), torch.int32, device)
+
+
+def _sequences(starts):
+    if starts.dim() != 1 or starts.shape[0] < 1:
+        _refuse(f"starts: one dimension of sequences + 1 wanted, got {list(starts.shape)}")
+    return starts.shape[0] - 1
+
+
+def _scale(scale, dim):
+    if scale is None:
+        return 1.0 / math.sqrt(dim)
+    scale = float(scale)
+    if not 0.0 < scale < 3e38:
+        _refuse(f"scale must be positive, got {scale}")
+    return scale
+
+
+_NO_HEADS = (0, 0, 0)
+
+
+def prompt_workspace(q, k, starts, stream=None):
+    """A workspace for ``prompt_attention`` calls of this shape; calls that may run at the same time need one each."""
+    T, heads, dim = q.shape
+    need = _load().gts_prompt_workspace_bytes(_PROMPT.pack(
+        _sequences(starts), T, heads, k.shape[1], dim, _DTYPES.get(q.dtype, -1), 0, 0, 1.0, 0, *(4 * _NO_HEADS), 0, 0, 0, 0))
+    return _empty(max(int(need), 16), torch.uint8, q.device, stream)
+
+
+def _prompt_call(q, k, v, starts, causal, scale, out, lse, workspace, status, stream):
+    shape, qs, ks, vs, device, starts_at = _prompt_shape(q, k, v, starts)
+    handle = _handle(stream, device)
+    T, heads = shape[1:3]
+    scale, st, zero = _scale(scale, shape[4]), _status(status, device), (out is None) + 2 * (lse is None)
+    out, os = _output(out, "out", q.shape, q.dtype, device, stream)
+    if lse is None:
+        lse = _empty((T, heads), torch.float32, device, stream)
+    lse_at = _index(lse, "lse", (T, heads), torch.float32, device)
+    lib = _lib or _load()
+    if workspace is None:
+        workspace = _workspace(None, lib.gts_prompt_workspace_bytes(_PROMPT.pack(*shape, 0, 0, 1.0, 0, *(4 * _NO_HEADS), 0, 0, 0, 0)), device,
+                               stream)
+    else:
+        _workspace(workspace, 0, device, stream)
+    if T:
+        gts._check(lib.gts_prompt_attention(_PROMPT.pack(
+            *shape, bool(causal), zero, scale, starts_at, *_heads(q, qs), *_heads(k, ks), *_heads(v, vs), *_heads(out, os), lse_at,
+            workspace.data_ptr(), workspace.nbytes, st), handle))
+    return out, lse
+
+
+class _Prompt(torch.autograd.Function):
+    @staticmethod
+    def forward(q, k, v, starts, causal, scale, status):
+        return _prompt_call(q, k, v, starts, causal, scale, None, None, None, status, None)
+
+    @staticmethod
+    def setup_context(ctx, inputs, output):
+        q, k, v, starts, ctx.causal, ctx.scale, ctx.status = inputs
+        ctx.set_materialize_grads(False)
+        ctx.save_for_backward(q, k, v, starts, *output)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, dlse):
+        q, k, v, starts, out, lse = ctx.saved_tensors
+        if dout is None and dlse is None:
+            return (None,) * 7
+        dout = torch.zeros_like(out) if dout is None else _inner(dout)
+        dlse = None if dlse is None else dlse.contiguous()
+        got = prompt_attention_grad(dout, q, k, v, out, lse, starts, causal=ctx.causal, scale=ctx.scale, dlse=dlse, status=ctx.status)
+        return *(g if want else None for g, want in zip(got, ctx.needs_input_grad)), None, None, None, None
+
+
+def prompt_attention(q, k, v, starts, causal=True, scale=None, out=None, lse=None, workspace=None, status=None, stream=None):
+    """Attention of packed sequences over themselves: (out, lse).
+
+    q [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim], bfloat16 or float16, heads of 64 or 128; sequence b's tokens
+    are the rows ``starts[b]`` .. ``starts[b + 1] - 1`` (int32 [seqs + 1], rising, on the device).  A query sees its sequence's keys
+    up to its own (``causal``) or all of them; ``scale``: of the products, positive (default 1 / sqrt(head_dim)).  lse (float32
+    [tokens, heads]) is the logarithm of the sum of exponentials.  Rows of no sequence get zeros and lse = -inf; those
+    of a given ``out`` or ``lse`` are left as they are.  Starts out of range are clamped and store GTS_ERR_INVALID_PARAMS to ``status`` (int32 [1]
+    on the device), where given.  A kernel whose waits run out (after two seconds) stores GTS_ERR_STEP_LIMIT there, and its rows are NaN.
+
+    With outputs, workspace and stream left to the call, gradients flow from out and lse to q, k and v (once).  A backward pass that is
+    captured into a graph while another graph of the same leaves lives wants that one made on the capturing stream: torch ties
+    a leaf's gradient to the stream of its first use."""
+    if _differentiated(q) or _differentiated(k) or _differentiated(v):
+        if out is not None or lse is not None or workspace is not None or stream is not None:
+            _refuse("prompt_attention: gradients need the call's own outputs and workspace and the current stream")
+        return _Prompt.apply(q, k, v, starts, causal, scale, status)
+    return _prompt_call(q, k, v, starts, causal, scale, out, lse, workspace, status, stream)
+
+
+def prompt_attention_grad(dout, q, k, v, out, lse, starts, causal=True, scale=None, dlse=None, out_dq=None, out_dk=None, out_dv=None,
+                          workspace=None, status=None, stream=None):
+    """The gradients (dq, dk, dv) of ``prompt_attention`` from those of its results (``dlse`` [tokens, heads] float32, default none);
+    ``out`` and ``lse`` are what it gave.  Every sum has one order, so results repeat bit for bit.  Rows of no sequence get
+    zeros; those of a given output are left as they are."""
+    shape, qs, ks, vs, device, starts_at = _prompt_shape(q, k, v, starts)
+    handle = _handle(stream, device)
+    T, heads = shape[1:3]
+    scale, st = _scale(scale, shape[4]), _status(status, device)
+    (oshape, os), (dshape, ds) = _tensor(out, "out", 3, q.dtype, device), _tensor(dout, "dout", 3, q.dtype, device)
+    if oshape != q.shape or dshape != q.shape:
+        _refuse(f"out and dout: {list(q.shape)} wanted, got {list(oshape)} and {list(dshape)}")
+    lse_at = _index(lse, "lse", (T, heads), torch.float32, device)
+    dlse_at = 0 if dlse is None else _index(dlse, "dlse", (T, heads), torch.float32, device)
+    zero = (out_dq is None) + 2 * (out_dk is None) + 4 * (out_dv is None)
+    dq, dqs = _output(out_dq, "out_dq", q.shape, q.dtype, device, stream)
+    dk, dks = _output(out_dk, "out_dk", k.shape, q.dtype, device, stream)
+    dv, dvs = _output(out_dv, "out_dv", v.shape, q.dtype, device, stream)
+    lib = _lib or _load()
+
+    def pack(work_at, work_bytes):
+        return _PROMPT_GRAD.pack(
+            *shape, bool(causal), zero, scale, starts_at, *_heads(q, qs), *_heads(k, ks), *_heads(v, vs), *_heads(out, os), lse_at,
+            work_at, work_bytes, st, *_heads(dout, ds), dlse_at, *_heads(dq, dqs), *_heads(dk, dks), *_heads(dv, dvs))
+    if workspace is None:
+        workspace = _workspace(None, lib.gts_prompt_grad_workspace_bytes(pack(0, 0)), device, stream)
+    else:
+        _workspace(workspace, 0, device, stream)
+    if T:
+        gts._check(lib.gts_prompt_attention_grad(pack(workspace.data_ptr(), workspace.nbytes), handle))
+    return dq, dk, dv
+
+
+def _chunk_bytes(shape, cache_values, max_pages):
+    return int(_load().gts_chunk_workspace_bytes(_CHUNK.pack(*shape, 0, 1.0, 0, *(2 * _NO_HEADS), 0, *cache_values, 0, max_pages, 0, 0, 0, 0)))
+
+
+def chunk_workspace(q, starts, cache, page_table, stream=None):
+    """A workspace for ``chunk_attention`` calls of this shape; calls that may run at the same time need one each."""
+    need = _chunk_bytes((_sequences(starts), *q.shape[:2]), cache._descriptor(), page_table.shape[1])
+    return _empty(max(need, 16), torch.uint8, q.device, stream)
+
+
+def chunk_attention(q, starts, cache, page_table, lens, scale=None, out=None, lse=None, workspace=None, status=None, stream=None):
+    """Attention of chunks of new tokens over a paged cache: (out, lse), without gradients.
+
+    q [tokens, heads, head_dim] holds the new tokens of all sequences, packed: those of sequence b are the rows ``starts[b]`` ..
+    ``starts[b + 1] - 1`` (int32 [seqs + 1], rising).  Their keys and values are in the cache already, as the newest of the
+    sequence's first ``lens[b]`` tokens (int32) of the pages in ``page_table[b]`` (int32 [seqs, max_pages]; entries past its length
+    are not looked at): each query sees the tokens up to its own.  A query that sees nothing gets zeros and lse = -inf; so do rows
+    of no sequence, but those of a given ``out`` or ``lse`` are left as they are.  Types, scale, status and heads as in
+    ``prompt_attention``; a page number or length out of range is not followed.  ``prefix_attention`` does the same for a few tokens of each
+    sequence, and shares a prefix."""
+    cache_values = cache._descriptor()
+    dtype, device = cache.dtype, cache.device
+    shape, qs = _tensor(q, "q", 3, dtype, device)
+    handle = _handle(stream, device)
+    T, heads, dim = shape
+    if dim != cache.head_dim:
+        _refuse(f"heads of {dim} (q) and {cache.head_dim} (cache)")
+    n = _sequences(starts)
+    starts_at = _index(starts, "starts", (None,), torch.int32, device)
+    table_at = _index(page_table, "page_table", (n, None), torch.int32, device)
+    max_pages = page_table.shape[1]
+    lens_at = _index(lens, "lens", (n,), torch.int32, device)
+    scale, st, zero = _scale(scale, dim), _status(status, device), (out is None) + 2 * (lse is None)
+    out, os = _output(out, "out", shape, dtype, device, stream)
+    if lse is None:
+        lse = _empty((T, heads), torch.float32, device, stream)
+    lse_at = _index(lse, "lse", (T, heads), torch.float32, device)
+    if workspace is None:
+        workspace = _workspace(None, _chunk_bytes((n, T, heads), cache_values, max_pages), device, stream)
+    else:
+        _workspace(workspace, 0, device, stream)
+    if T:
+        gts._check((_lib or _load()).gts_chunk_attention(_CHUNK.pack(
+            n, T, heads, zero, scale, starts_at, *_heads(q, qs), *_heads(out, os), lse_at, *cache_values, table_at, max_pages,
+            lens_at, workspace.data_ptr(), workspace.nbytes, st), handle))
+    return out, lse
+
+
+def copy_pages(cache, src, dst, tokens=None, into=None, status=None, stream=None):
+    """Copies the pages ``src`` of a cache, keys and values, to its pages ``dst`` (int32, one of each a copy), or to those of the cache
+    ``into`` (of the same page size, heads and type, in any order).
+
+    ``tokens`` (int32): how many tokens of each page, from its first (default: all).  A negative page copies nothing.  So a sequence that
+    forks shares its full pages and copies the one that is being filled; a cache is compacted by moving pages to free ones.  A page may
+    be copied to several others, but one that is written twice, or read and written, in a call holds unspecified values.  A page
+    number beyond the cache copies nothing and stores GTS_ERR_INVALID_PARAMS to ``status`` (int32 [1] on the device), where given."""
+    into = cache if into is None else into
+    if into.dtype != cache.dtype or into.device != cache.device:
+        _refuse(f"into: a cache of {cache.dtype} on {cache.device} wanted, got {into.dtype} on {into.device}")
+    device = cache.device
+    handle = _handle(stream, device)
+    src_at = _index(src, "src", (None,), torch.int32, device)
+    n = src.shape[0]
+    dst_at = _index(dst, "dst", (n,), torch.int32, device)
+    tokens_at = 0 if tokens is None else _index(tokens, "tokens", (n,), torch.int32, device)
+    gts._check((_lib or _load()).gts_copy_pages(_COPY_PAGES.pack(
+        n, src_at, dst_at, tokens_at, *cache._descriptor(), *into._descriptor(), _status(status, device)), handle))
