@@ -166,6 +166,9 @@ typedef struct {
   gts_heads dq, dk, dv;
 } gts_prompt_grad_desc;
 gts_status gts_prompt_attention_grad(const gts_prompt_grad_desc *desc, void *stream);
+
+/* Bytes of workspace; addresses and strides of q, k, v and dout count: those off the 16-byte grid, or with heads further apart than
+ * tokens, are laid side by side there. */
 size_t gts_prompt_grad_workspace_bytes(const gts_prompt_grad_desc *desc);
 
 /* Attention of chunks of new tokens over a paged cache that holds them already.  Sequence b's queries are the rows starts[b] ..

@@ -5,19 +5,14 @@
 // q_i . k_j, out_i = sum_j exp(s_ij - max) v_j / sum_j exp(s_ij - max), taken with the maximum and the sum so far.  Backward: with
 // p_ij = exp(s_ij - lse_i), e_i = dout_i . out_i - dlse_i and ds_ij = p_ij (dout_i . v_j - e_i): dv_j = sum p_ij dout_i,
 // dq_i = scale sum ds_ij k_j, dk_j = scale sum ds_ij q_i.
-//
-// The simplest form: a warp for each row of a result, the head's values along its lanes, everything in 32 bits.
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
-
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "internal.h"
+#include "tensor.cuh"
 
 namespace {
-
-constexpr int WARPS = 8;
 
 struct Heads { const void *data; int64_t tok, head; };
 
@@ -29,18 +24,56 @@ struct Args {
   int64_t k_page, v_page;
   int n_seqs, n_tokens, q_heads, kv_heads, group, causal, zero_rest, paged;
   int n_pages, page_size, max_pages;
+  Divisor in_group, in_page;
   float scale;
   int32_t *status;
 };
 
-template <typename T> __device__ __forceinline__ float widen(T x);
-template <> __device__ __forceinline__ float widen(__half x) { return __half2float(x); }
-template <> __device__ __forceinline__ float widen(__nv_bfloat16 x) { return __bfloat162float(x); }
-template <typename T> __device__ __forceinline__ T narrow(float x);
-template <> __device__ __forceinline__ __half narrow(float x) { return __float2half_rn(x); }
-template <> __device__ __forceinline__ __nv_bfloat16 narrow(float x) { return __float2bfloat16_rn(x); }
+// Every wait ends: after two seconds, or when another warp has given up, the block winds down with an error status.
+constexpr uint64_t LIMIT_NS = 2000000000ull, DRAIN_NS = 2000000000ull;   // of a wait; of what a block that winds down has in flight
+constexpr int TRIES = 1024, BETWEEN = 64;   // before the timer is read first, and from then on (reading it takes longer than most waits)
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+               : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok;
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int *dead) {
+  if (bar_try(bar, parity)) return true;
+#pragma unroll 1
+  for (int n = 0; n < TRIES; n++)
+    if (bar_try(bar, parity)) return true;
+  const uint64_t from = now_ns();
+#pragma unroll 1
+  while (!*dead) {
+#pragma unroll 1
+    for (int n = 0; n < BETWEEN; n++)
+      if (bar_try(bar, parity)) return true;
+    if (now_ns() - from > LIMIT_NS) *dead = 1;
+  }
+  return false;
+}
 
-struct Seq { int first, n, keys; };  // rows of the queries, and keys
+// ---------------------------------------------------------------- how the work is cut
+// An item is a key head with a tile of rows of one sequence, or (the gradients of keys and values) a tile of 128 keys of it; it
+// passes along its tiles of the other side.  All items stand in one line, key head by key head, sequence by sequence, each with a
+// weight: what its tiles cost (one for each key or query seen) and what it costs beside them (LEAD of its tiles).  Each block takes an equal
+// stretch of the line, rounded to whole tiles, so sequences of any lengths share the SMs evenly, a few rows over many keys are
+// split along the keys, and the cut needs no plan from the host.  A sequence's weight up to an item is a sum of an arithmetic series, so a
+// block finds its stretch by a sum over the sequences and a bisection.  An item within one block's stretch is finished there; one
+// that is cut leaves partial results, which k_join adds up in their order.
+constexpr int SMS = 152, TILE = 128, LEAD = 2;
+constexpr int NOTHING = -1;
+
+struct Cut {
+  int blocks;
+  int queries;           // of an item of rows (two halves of them); of a tile of rows
+  int4 *ends;            // [blocks]: the item that begins in a block and goes on: sequence (or NOTHING), key head, item, further blocks
+  float *o;              // [blocks][2][rows of an item][D]: parts of the item that began before (0) and of the one that goes on (1)
+  float2 *ml;            // [blocks][2][rows]: maximum (of log2 scores) and sum
+};
+
+struct Seq { int first, n, keys; };  // first row and number of its queries, and keys
 
 __device__ __forceinline__ Seq sequence(const Args &a, int b) {
   const int from = a.starts[b], to = a.starts[b + 1];
@@ -50,153 +83,1797 @@ __device__ __forceinline__ Seq sequence(const Args &a, int b) {
   bool bad = from != s.first || to != s.first + s.n;
   s.keys = s.n;
   if (a.paged) {
-    const int most = a.max_pages * a.page_size;
-    s.keys = max(0, min(a.lens[b], most));
-    bad |= a.lens[b] > most;
+    const int len = a.lens[b], most = a.max_pages * a.page_size;
+    s.keys = max(0, min(len, most));
+    bad |= len > most;
   }
   if (bad && a.status) *a.status = GTS_ERR_INVALID_PARAMS;
   return s;
 }
 
-// The sequence of a row, -1: none.
-__device__ __forceinline__ int sequence_of(const Args &a, int row) {
-  for (int b = 0; b < a.n_seqs; b++)
-    if (a.starts[b] <= row && row < a.starts[b + 1]) return b;
-  return -1;
-}
+// Items of rows (BY_KEYS false) and of keys: how many a sequence has, the tiles of one, its weight and that of all before it.
+template <bool BY_KEYS> struct Items {
+  int q, causal;         // queries of an item (of a tile of rows, by keys)
+  __device__ __forceinline__ int lead() const { return LEAD * (BY_KEYS ? q : TILE); }
+  __device__ __forceinline__ int count(const Seq &s) const { return BY_KEYS ? (s.keys + TILE - 1) / TILE : (s.n + q - 1) / q; }
+  // keys that the item's last query sees, or queries that see the item's first key (rounded to whole items)
+  __device__ __forceinline__ int seen(const Seq &s, int t) const {
+    if (BY_KEYS) return causal ? s.n - t * TILE : s.n;
+    return causal ? max(0, s.keys - s.n + min(s.n, (t + 1) * q)) : s.keys;
+  }
+  __device__ __forceinline__ int first_tile(int t) const { return BY_KEYS && causal ? t * TILE / q : 0; }
+  __device__ __forceinline__ int tiles(const Seq &s, int t) const {
+    if (BY_KEYS) return (s.n + q - 1) / q - first_tile(t);
+    return max(1, (seen(s, t) + TILE - 1) / TILE);
+  }
+  __device__ __forceinline__ int64_t weight(const Seq &s, int t) const { return (int64_t)lead() + seen(s, t); }
+  __device__ __forceinline__ int64_t before(const Seq &s, int t) const {
+    const int64_t x = t;
+    if (!causal) return x * (lead() + (BY_KEYS ? s.n : s.keys));
+    if (BY_KEYS) return x * ((int64_t)lead() + s.n) - x * (x - 1) / 2 * TILE;
+    const int64_t off = (int64_t)s.keys - s.n, none = off < 0 ? min(x, -off / q) : 0;   // items that see nothing
+    int64_t sum = x * lead() + (x - none) * off + (x * (x + 1) - none * (none + 1)) / 2 * q;
+    if (x > none && x * q > s.n) sum -= x * q - s.n;
+    return sum;
+  }
+  // tiles of an item up to a place in its weight
+  __device__ __forceinline__ int tiles_before(int64_t y, int64_t weight, int tiles) const {
+    if (y >= weight) return tiles;
+    const int64_t in = y - lead() + (BY_KEYS ? q : TILE) / 2;
+    return in <= 0 ? 0 : (int)min((int64_t)tiles, in / (BY_KEYS ? q : TILE));
+  }
+};
 
-template <typename T, int E> __device__ __forceinline__ void load(float (&x)[E], const T *p) {
+// The line of a call, and a block's walk along its stretch of it.
+struct Stretch { int64_t head, all, per, x0, x1; int b, t; int64_t pos; int kh, rest_from, rest_to; };
+
+// Where a block begins: every thread of it takes part.  rest_from, rest_to: rows of sequences are between them.
+template <bool BY_KEYS, int THREADS>
+__device__ __forceinline__ Stretch find_stretch(const Args &a, const Items<BY_KEYS> &items, int blocks) {
+  __shared__ int64_t sums[THREADS / 32], places[2];
+  __shared__ int ends[THREADS / 32][2], found[2];
+  const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
+  const int each = (a.n_seqs + THREADS - 1) / THREADS, from = min(a.n_seqs, tid * each), to = min(a.n_seqs, from + each);
+  int64_t mine = 0;
+  int first = a.n_tokens, last = 0;
+  for (int b = from; b < to; b++) {
+    const Seq s = sequence(a, b);
+    if (s.n) first = min(first, s.first), last = max(last, s.first + s.n);
+    mine += items.before(s, items.count(s));
+  }
+  int64_t upto = mine;
 #pragma unroll
-  for (int e = 0; e < E; e++) x[e] = widen(p[e * 32]);
-}
-template <typename T, int E> __device__ __forceinline__ void store(T *p, const float (&x)[E], float f) {
+  for (int o = 1; o < 32; o *= 2) {
+    const int64_t x = __shfl_up_sync(~0u, upto, o);
+    if (lane >= o) upto += x;
+  }
+  first = __reduce_min_sync(~0u, first), last = __reduce_max_sync(~0u, last);
+  if (lane == 31) sums[warp] = upto;
+  if (lane == 0) ends[warp][0] = first, ends[warp][1] = last;
+  if (tid == 0) found[0] = -1;
+  __syncthreads();
+  Stretch s = {};
+  s.rest_from = a.n_tokens;
+  int64_t earlier = 0;
 #pragma unroll
-  for (int e = 0; e < E; e++) p[e * 32] = narrow<T>(x[e] * f);
-}
-template <int E> __device__ __forceinline__ float dot(const float (&x)[E], const float (&y)[E]) {
-  float s = 0.f;
-#pragma unroll
-  for (int e = 0; e < E; e++) s += x[e] * y[e];
-#pragma unroll
-  for (int o = 16; o; o /= 2) s += __shfl_xor_sync(~0u, s, o);
+  for (int w = 0; w < THREADS / 32; w++) {
+    if (w < warp) earlier += sums[w];
+    s.head += sums[w];
+    s.rest_from = min(s.rest_from, ends[w][0]), s.rest_to = max(s.rest_to, ends[w][1]);
+  }
+  if (s.rest_to == 0) s.rest_from = 0;
+  s.all = s.head * a.kv_heads;
+  s.per = max((int64_t)items.lead(), quotient(s.all + blocks - 1, blocks));
+  s.x0 = min(s.all, s.per * blockIdx.x), s.x1 = min(s.all, s.x0 + s.per);
+  if (s.x0 >= s.x1) return s;
+  s.kh = (int)quotient(s.x0, s.head);
+  const int64_t in = s.x0 - s.kh * s.head;
+  int64_t at = earlier + upto - mine;
+  if (in >= at && in < at + mine) {
+    for (int b = from; b < to; b++) {
+      const Seq q = sequence(a, b);
+      const int count = items.count(q);
+      const int64_t w = items.before(q, count);
+      if (in < at + w) {
+        int lo = 0, hi = count - 1;                    // the last item that begins at `in` or before
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) / 2;
+          if (at + items.before(q, mid) <= in) lo = mid; else hi = mid - 1;
+        }
+        found[0] = b, found[1] = lo, places[0] = s.kh * s.head + at + items.before(q, lo);
+        break;
+      }
+      at += w;
+    }
+  }
+  __syncthreads();
+  s.b = found[0], s.t = found[1], s.pos = places[0];
   return s;
 }
-template <typename T> __device__ __forceinline__ const T *at(const Heads &h, int64_t row, int head) { return (const T *)h.data + row * h.tok + head * h.head; }
 
-// The rows of a key and its value: false where the page table has no such page.
-template <typename T>
-__device__ __forceinline__ bool key_rows(const Args &a, int b, const Seq &s, int j, int kh, const T *&k, const T *&v) {
-  if (!a.paged) {
-    k = at<T>(a.k, s.first + j, kh), v = at<T>(a.v, s.first + j, kh);
-    return true;
+// What a block does with an item: its tiles from tile0 to tile1 of `tiles`.
+struct Item { int b, first, n, keys, kh, t, tile0, tile1, tiles; };
+
+// The next item of a stretch that has tiles in it; false at its end.  `ends`: where an item that goes on is recorded, by one thread.
+template <bool BY_KEYS>
+__device__ __forceinline__ bool next_item(const Args &a, const Items<BY_KEYS> &items, Stretch &s, Seq &q, Item &i, int4 *ends) {
+  while (s.pos < s.x1) {
+    if (s.t == 0 || i.b != s.b) q = sequence(a, s.b);
+    const int64_t w = items.weight(q, s.t), end = s.pos + w;
+    const int n = items.tiles(q, s.t);
+    i = {s.b, q.first, q.n, q.keys, s.kh, s.t, s.pos < s.x0 ? items.tiles_before(s.x0 - s.pos, w, n) : 0,
+         items.tiles_before(s.x1 - s.pos, w, n), n};
+    if (ends && i.tile0 == 0 && i.tile1 > 0 && i.tile1 < n) {
+      int64_t last = quotient(end - 1, s.per);
+      if (items.tiles_before(last * s.per - s.pos, w, n) == n) last--;
+      *ends = make_int4(s.b, s.kh, s.t, (int)(last - blockIdx.x));
+    }
+    s.pos = end;
+    if (++s.t == items.count(q)) {
+      s.t = 0;
+      do {
+        if (++s.b == a.n_seqs) s.b = 0, s.kh++;
+      } while (s.pos < s.x1 && sequence(a, s.b).n == 0);
+    }
+    if (i.tile1 > i.tile0) return true;
   }
-  const int page = a.table[(int64_t)b * a.max_pages + j / a.page_size];
+  return false;
+}
+
+template <typename T> __device__ __forceinline__ T *row_at(const Heads &h, int64_t row, int head) { return (T *)h.data + row * h.tok + head * h.head; }
+
+// Rows of no sequence (before `from`, from `to` on): all blocks together write them.
+template <typename T, typename F>
+__device__ __forceinline__ void fill_rest(const Heads &h, int heads, int dim, int n_tokens, int from, int to, T x, F store) {
+  const int64_t count = (int64_t)(from + n_tokens - to) * heads * dim;
+  for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < count; i += (int64_t)gridDim.x * blockDim.x) {
+    const int64_t row = i / (heads * dim);
+    const int in = (int)(i - row * heads * dim);
+    store(row < from ? row : row - from + to, in / dim, in % dim, x);
+  }
+}
+template <typename T> __device__ __forceinline__ void zero_rest(const Args &a, const Heads &h, int heads, int dim, const Stretch &s) {
+  fill_rest(h, heads, dim, a.n_tokens, s.rest_from, s.rest_to, narrow<T>(0.f), [&](int64_t row, int head, int d, T x) { row_at<T>(h, row, head)[d] = x; });
+}
+
+// The 16 bytes at a source off the 16-byte grid.
+template <typename T> __device__ __forceinline__ uint4 gather16(const T *from) {
+  T e[8];
+#pragma unroll
+  for (int z = 0; z < 8; z++) e[z] = from[z];
+  uint4 v;
+  memcpy(&v, e, 16);
+  return v;
+}
+
+// The row of a key, nullptr where its page is none of the cache's.
+template <typename T>
+__device__ __forceinline__ const T *key_row(const Args &a, const Heads &side, int64_t page_stride, int b, int first, int key, int kh) {
+  if (!a.paged) return row_at<T>(side, first + key, kh);
+  const int page = a.table[(int64_t)b * a.max_pages + key / a.in_page];
   if ((unsigned)page >= (unsigned)a.n_pages) {
     if (a.status) *a.status = GTS_ERR_INVALID_PARAMS;
-    return false;
+    return nullptr;
   }
-  k = at<T>(a.k, j % a.page_size, kh) + page * a.k_page;
-  v = at<T>(a.v, j % a.page_size, kh) + page * a.v_page;
-  return true;
+  return row_at<T>(side, key % a.in_page, kh) + page * page_stride;
 }
 
-template <typename T, int D>
-__global__ void __launch_bounds__(WARPS * 32) k_forward(const Args a) {
-  const int64_t w = (int64_t)blockIdx.x * WARPS + threadIdx.x / 32;
-  const int lane = threadIdx.x % 32;
-  if (blockIdx.x == 0)
-    for (int b = threadIdx.x; b < a.n_seqs; b += WARPS * 32) sequence(a, b);   // reports those out of range
-  if (w >= (int64_t)a.n_tokens * a.q_heads) return;
-  const int row = (int)(w / a.q_heads), h = (int)(w % a.q_heads), b = sequence_of(a, row);
-  float o[D / 32] = {}, q[D / 32], k[D / 32], v[D / 32], m = -INFINITY, l = 0.f;
-  if (b >= 0) {
-    const Seq s = sequence(a, b);
-    const int seen = a.causal ? min(s.keys, s.keys - s.n + (row - s.first) + 1) : s.keys;
-    load(q, at<T>(a.q, row, h) + lane);
-    for (int j = 0; j < seen; j++) {
-      const T *kp, *vp;
-      if (!key_rows(a, b, s, j, h / a.group, kp, vp)) continue;
-      load(k, kp + lane), load(v, vp + lane);
-      const float x = dot(q, k) * a.scale, top = fmaxf(m, x), keep = m == -INFINITY ? 0.f : __expf(m - top), p = __expf(x - top);
-      l = l * keep + p, m = top;
-#pragma unroll
-      for (int e = 0; e < D / 32; e++) o[e] = o[e] * keep + p * v[e];
-    }
-  }
-  if (b >= 0 || a.zero_rest & 1) store((T *)at<T>(a.out, row, h) + lane, o, l == 0.f ? 0.f : 1.f / l);
-  if ((b >= 0 || a.zero_rest & 2) && a.lse && lane == 0) a.lse[w] = l == 0.f ? -INFINITY : m + logf(l);
+// Tiles in shared memory: 64 columns after 64, each rows of 128 bytes, eight rows to a swizzled group.
+template <int ROWS> __device__ __forceinline__ int tile_at(int row, int c) { return c / 8 * (ROWS * 128) + row * 128 + ((c % 8) ^ (row & 7)) * 16; }
+
+// The top bit of each of two values that is infinite or NaN: all exponent bits are set.
+template <typename T> __device__ __forceinline__ uint32_t not_finite(uint32_t two) {
+  constexpr uint32_t ONES = std::is_same<T, __half>::value ? 0x7C007C00u : 0x7F807F80u, NEXT = std::is_same<T, __half>::value ? 0x04000400u : 0x00800080u;
+  return ((two & ONES) + NEXT) & 0x80008000u;
+}
+template <typename T> __device__ __forceinline__ uint32_t finite_part(uint32_t two) {   // zero in place of the others
+  const uint32_t x = not_finite<T>(two);
+  return two & ~((x >> 15) * 0xFFFFu);
 }
 
+// A tile's rows whose product is with weights of 0 where they are out of sight (one warp): 0 x infinity would be NaN.  Rows from
+// `live` on are zeroed; where some rows are hidden from some, so are values that are not finite, and the numbers of their rows
+// set in `bad`.
 template <typename T, int D>
-__global__ void __launch_bounds__(WARPS * 32) k_grad_q(const Args a) {
-  const int64_t w = (int64_t)blockIdx.x * WARPS + threadIdx.x / 32;
-  const int lane = threadIdx.x % 32;
-  if (blockIdx.x == 0)
-    for (int b = threadIdx.x; b < a.n_seqs; b += WARPS * 32) sequence(a, b);
-  if (w >= (int64_t)a.n_tokens * a.q_heads) return;
-  const int row = (int)(w / a.q_heads), h = (int)(w % a.q_heads), b = sequence_of(a, row);
-  float g[D / 32] = {}, q[D / 32], k[D / 32], v[D / 32], y[D / 32];
-  if (b >= 0) {
-    const Seq s = sequence(a, b);
-    const int seen = a.causal ? row - s.first + 1 : s.keys;
-    load(q, at<T>(a.q, row, h) + lane), load(y, at<T>(a.dout, row, h) + lane), load(v, at<T>(a.out, row, h) + lane);
-    const float delta = dot(y, v) - (a.dlse ? a.dlse[w] : 0.f), lse = a.lse[w];
-    if (lane == 0) a.delta[w] = delta;
-    for (int j = 0; j < seen; j++) {
-      const T *kp, *vp;
-      key_rows(a, b, s, j, h / a.group, kp, vp);
-      load(k, kp + lane), load(v, vp + lane);
-      const float ds = __expf(dot(q, k) * a.scale - lse) * (dot(y, v) - delta);
+__device__ __forceinline__ void clean_tile(unsigned char *tile, int lane, int live, bool look, uint32_t (&bad)[4]) {
+  constexpr int PER = D / 8, AT_ONCE = 32 / PER;       // 16-byte pieces of a row, rows at a time
+  const int c = lane % PER, sub = lane / PER;
 #pragma unroll
-      for (int e = 0; e < D / 32; e++) g[e] += ds * k[e];
-    }
-  }
-  if (b >= 0 || a.zero_rest & 1) store((T *)at<T>(a.dq, row, h) + lane, g, a.scale);
-}
-
-template <typename T, int D>
-__global__ void __launch_bounds__(WARPS * 32) k_grad_kv(const Args a) {
-  const int64_t w = (int64_t)blockIdx.x * WARPS + threadIdx.x / 32;
-  const int lane = threadIdx.x % 32;
-  if (w >= (int64_t)a.n_tokens * a.kv_heads) return;
-  const int row = (int)(w / a.kv_heads), kh = (int)(w % a.kv_heads), b = sequence_of(a, row);
-  float gk[D / 32] = {}, gv[D / 32] = {}, q[D / 32], k[D / 32], v[D / 32], y[D / 32];
-  if (b >= 0) {
-    const Seq s = sequence(a, b);
-    load(k, at<T>(a.k, row, kh) + lane), load(v, at<T>(a.v, row, kh) + lane);
-    for (int x = a.causal ? row : s.first; x < s.first + s.n; x++) {
-      for (int h = kh * a.group; h < (kh + 1) * a.group; h++) {
-        load(q, at<T>(a.q, x, h) + lane), load(y, at<T>(a.dout, x, h) + lane);
-        const int64_t r = (int64_t)x * a.q_heads + h;
-        const float p = __expf(dot(q, k) * a.scale - a.lse[r]), ds = p * (dot(y, v) - a.delta[r]);
+  for (int i = 0; i < 4; i++) bad[i] = 0;
+  if (look) {
 #pragma unroll
-        for (int e = 0; e < D / 32; e++) gk[e] += ds * q[e], gv[e] += p * y[e];
+    for (int word = 0; word < 4; word++) {
+#pragma unroll 8
+      for (int r0 = 0; r0 < 32; r0 += AT_ONCE) {
+        const int row = word * 32 + r0 + sub;
+        uint4 *const at = (uint4 *)(tile + tile_at<128>(row, c));
+        const uint4 v = *at;
+        const bool some = (not_finite<T>(v.x) | not_finite<T>(v.y) | not_finite<T>(v.z) | not_finite<T>(v.w)) && row < live;
+        const uint32_t hit = __ballot_sync(~0u, some);
+        if (hit) {
+#pragma unroll
+          for (int k = 0; k < AT_ONCE; k++)
+            if (hit >> (k * PER) & (uint32_t)((1ull << PER) - 1)) bad[word] |= 1u << (r0 + k);
+          if (some) *at = make_uint4(finite_part<T>(v.x), finite_part<T>(v.y), finite_part<T>(v.z), finite_part<T>(v.w));
+        }
       }
     }
   }
-  if (b >= 0 || a.zero_rest & 2) store((T *)at<T>(a.dk, row, kh) + lane, gk, a.scale);
-  if (b >= 0 || a.zero_rest & 4) store((T *)at<T>(a.dv, row, kh) + lane, gv, 1.f);
+  for (int i = max(0, live) * PER + lane; i < 128 * PER; i += 32) *(uint4 *)(tile + tile_at<128>(i / PER, i % PER)) = make_uint4(0, 0, 0, 0);
+}
+
+// ---------------------------------------------------------------- forward
+// A block holds 2 x 128 rows of one key head - `queries / 2` queries of a sequence with all their heads in each half - and passes along
+// its tiles of 128 keys:
+//   warp 9 walks along the block's stretch, hands its items on through a short queue, and brings tiles of keys and values
+//   (TMA where pages and strides allow it, else 16-byte copies or plain loads) into a ring;
+//   warp 11 brings an item's queries, and cleans tiles of values in which some rows are out of sight;
+//   warps 8 and 10 issue the products, each for one half: S = Q K^T to tensor memory, O += P V with P from tensor memory;
+//   warps 0..3 and 4..7 take one half each, one row a thread: maximum, weights, sum.  P overwrites S.
+// The halves alternate: while one turns scores into weights, the tensor cores work for the other.  An item's first scores are
+// worked out, and its queries brought, while the rows of the one before store their results.  The maximum that scores are taken against is
+// raised, and what was summed rescaled, only when it has grown by more than 8 (in log 2).  Weights are rounded to the values'
+// type for their product; the sum is of the unrounded ones, all else is in 32 bits.
+constexpr int FWD_THREADS = 384, QUEUE = 4;
+constexpr float RAISE = 8.f;
+template <int D> struct Fwd {
+  static constexpr int BYTES = TILE * D * 2, STAGES = D == 64 ? 8 : 5, Q = 2 * BYTES;
+  static constexpr int SMEM = Q + STAGES * BYTES + 1024 /* alignment */ + 768;
+};
+
+// An item as one half of its rows sees it.
+struct Half {
+  int q0, queries, count;                              // its first query (of the sequence), how many it has, tiles of the block's stretch
+  int seen;                                            // keys that its last query sees
+};
+__device__ __forceinline__ Half half_of(const Args &a, const Items<false> &items, const Item &i, int h) {
+  Half x;
+  const int per = items.q / 2;
+  x.q0 = i.t * items.q + h * per;
+  x.queries = max(0, min(per, i.n - x.q0));
+  x.seen = a.causal ? max(0, i.keys - i.n + x.q0 + x.queries) : i.keys;
+  x.count = x.queries ? max(0, min(i.tile1, max(1, (x.seen + TILE - 1) / TILE)) - i.tile0) : 0;
+  return x;
+}
+// keys that the first query of a half sees: tiles that end after them hide keys from some row
+__device__ __forceinline__ int seen_by_all(const Args &a, const Item &i, int q0) { return a.causal ? max(0, i.keys - i.n + q0 + 1) : i.keys; }
+
+template <typename T, int D>
+__global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const Items<false> items, const Cut cut, const __grid_constant__ Pages maps) {
+  constexpr int BYTES = Fwd<D>::BYTES, STAGES = Fwd<D>::STAGES, COLUMNS = TILE * 128;   // bytes of 64 columns of a tile
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char *const qs = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023), *const ring = qs + Fwd<D>::Q;
+  uint64_t *const bars = (uint64_t *)(ring + STAGES * BYTES);
+  constexpr int BARS = 2 * STAGES + 4 + 2 + 2 + 2 + 4 + 2 + 2 + 2 + 2 * QUEUE + 2;
+  Item *const queue = (Item *)(bars + BARS);
+  uint32_t *const bad_rows = (uint32_t *)(queue + QUEUE);                               // [4][4]: of the last tiles of values
+  uint32_t *const tmem_at = bad_rows + 16;
+  volatile int *const dead = (volatile int *)(tmem_at + 1);
+  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 16 * 4 + 8 <= 768, "room behind the ring");
+  const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
+  const uint32_t bar0 = smem_u32(bars), q_at = smem_u32(qs), ring_at = smem_u32(ring);
+  auto full = [&](int s) { return bar0 + s * 8; };
+  auto empty = [&](int s) { return bar0 + (STAGES + s) * 8; };
+  constexpr int B0 = 2 * STAGES;
+  auto ready = [&](uint32_t v) { return bar0 + (B0 + v % 4) * 8; };                     // the v-th tile of values is clean
+  auto q_full = [&](int h) { return bar0 + (B0 + 4 + h) * 8; };
+  auto q_empty = [&](int h) { return bar0 + (B0 + 6 + h) * 8; };
+  auto s_full = [&](int h) { return bar0 + (B0 + 8 + h) * 8; };
+  auto p_full = [&](int h, int x) { return bar0 + (B0 + 10 + h * 2 + x) * 8; };         // weights of half the keys
+  auto o_full = [&](int h) { return bar0 + (B0 + 14 + h) * 8; };
+  auto o_free = [&](int h) { return bar0 + (B0 + 16 + h) * 8; };
+  auto my_turn = [&](int h) { return bar0 + (B0 + 18 + h) * 8; };
+  auto given = [&](uint32_t i) { return bar0 + (B0 + 20 + i % QUEUE) * 8; };
+  auto taken = [&](uint32_t i) { return bar0 + (B0 + 20 + QUEUE + i % QUEUE) * 8; };
+  const uint32_t ended = bar0 + (B0 + 20 + 2 * QUEUE) * 8;
+
+  dependents_may_start();
+  Stretch line = find_stretch<false, FWD_THREADS>(a, items, cut.blocks);
+  if (line.rest_from + a.n_tokens - line.rest_to > 0) {
+    if (a.zero_rest & 1) zero_rest<T>(a, a.out, a.q_heads, D, line);
+    if (a.zero_rest & 2 && a.lse)
+      fill_rest(a.out, a.q_heads, 1, a.n_tokens, line.rest_from, line.rest_to, -INFINITY, [&](int64_t row, int head, int, float x) { a.lse[row * a.q_heads + head] = x; });
+  }
+  if (tid == 0) cut.ends[blockIdx.x] = make_int4(NOTHING, 0, 0, 0);
+  if (line.x0 >= line.x1) return;
+  if (tid == 0) {
+    for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(empty(s), 2);
+    for (int v = 0; v < 4; v++) bar_init(ready(v), 1);
+    for (int h = 0; h < 2; h++) {
+      bar_init(q_full(h), 32), bar_init(q_empty(h), 1), bar_init(s_full(h), 1), bar_init(p_full(h, 0), 128), bar_init(p_full(h, 1), 128);
+      bar_init(o_full(h), 1), bar_init(o_free(h), 128), bar_init(my_turn(h), 1), bar_init(ended + 8 * h, 1);
+    }
+    for (int i = 0; i < QUEUE; i++) bar_init(given(i), 1), bar_init(taken(i), 11);
+    *dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_at)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  tc_before();
+  __syncthreads();
+  tc_after();
+  const uint32_t tmem = __shfl_sync(~0u, *tmem_at, 0);
+  auto scores = [&](int h) { return tmem + h * TILE; };
+  auto sums = [&](int h) { return tmem + 256 + h * 128; };
+  int copies = 0;                                      // warp 9: tiles asked for by TMA
+  bool issues = false;                                 // the threads that issue products
+  bool alive = true;
+  auto need = [&](uint32_t bar, uint32_t parity) { alive = alive && bar_wait(bar, parity & 1, dead); };
+  // the next item of the queue; false at the end
+  uint32_t turn_of_queue = 0;
+  auto next = [&](Item &i) {                           // (of one thread)
+    need(given(turn_of_queue), turn_of_queue / QUEUE);
+    if (alive) i = queue[turn_of_queue % QUEUE];
+    return alive && i.tiles > 0;
+  };
+  auto need_all = [&](uint32_t bar, uint32_t parity) { alive = __all_sync(~0u, bar_wait(bar, parity & 1, dead)); };
+  auto next_all = [&](Item &i) {                       // of a warp
+    need_all(given(turn_of_queue), turn_of_queue / QUEUE);
+    if (alive) i = queue[turn_of_queue % QUEUE];
+    return alive && i.tiles > 0;
+  };
+  auto take = [&] { bar_arrive(taken(turn_of_queue++)); };
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp == 9) {
+      // ---- the walk, keys and values
+      const bool aligned = (((uintptr_t)a.k.data >> 1 | (uintptr_t)a.v.data >> 1 | a.k.tok | a.k.head | a.v.tok | a.v.head | (a.paged ? a.k_page | a.v_page : 0)) & 7) == 0;
+      Stretch s = line;
+      Seq q;
+      Item i;
+      i.b = -1;
+      int slot = 0;
+      for (uint32_t n = 0; alive; n++) {
+        if (!next_item(a, items, s, q, i, lane == 0 ? cut.ends + blockIdx.x : nullptr)) i.tiles = 0;
+        if (n >= QUEUE) need_all(taken(n), n / QUEUE - 1);
+        if (!alive) break;
+        if (lane == 0) queue[n % QUEUE] = i, bar_arrive(given(n));
+        if (i.tiles == 0) break;
+        if (maps.box) {
+          // lane x brings the x-th box of tokens of a tile, 64 values after 64
+          const int boxes = TILE / maps.box;
+          auto look_up = [&](int t) {                      // this lane's page of tile t; -1: none
+            const int key = t * TILE + lane * maps.box;
+            return lane < boxes && key < i.keys ? a.paged ? page_number(a.table[(int64_t)i.b * a.max_pages + key / a.in_page]) : 0 : -1;
+          };
+          int page_next = look_up(i.tile0);
+          for (int t = i.tile0; t < i.tile1 && alive; t++) {
+            int page = page_next;
+            const bool live = page >= 0;
+            if (t + 1 < i.tile1) page_next = look_up(t + 1);
+            if (page >= (a.paged ? a.n_pages : 1)) {
+              page = a.n_pages;                            // outside the map: zeros
+              if (a.status) *a.status = GTS_ERR_INVALID_PARAMS;
+            }
+            const int key = t * TILE + lane * maps.box, token = a.paged ? key % a.in_page : i.first + key;
+            const uint32_t bytes = __popc(__ballot_sync(~0u, live)) * maps.box * D * 2;
+            for (int kv = 0; kv < 2; kv++, copies++) {
+              const int st = copies % STAGES;
+              if (copies >= STAGES) need_all(empty(st), copies / STAGES - 1);
+              if (!alive) break;
+              if (lane == 0) bar_expect(full(st), bytes);
+              __syncwarp();
+              if (live) {
+                const bool heads_first = kv ? maps.v_heads_first : maps.k_heads_first;
+#pragma unroll
+                for (int x = 0; x < D / 64; x++)
+                  tile_load(ring_at + st * BYTES + x * COLUMNS + lane * maps.box * 128, kv ? &maps.v : &maps.k, x * 64, heads_first ? i.kh : token,
+                            heads_first ? token : i.kh, page, full(st));
+              }
+            }
+          }
+        } else {
+          // rows gathered: a tile's copies land while the next one's are asked for
+          int landing = -1;
+          auto landed = [&] {
+            fence_async();
+            __syncwarp();
+            if (lane == 0) bar_arrive(full(landing));
+          };
+          for (int t = i.tile0; t < i.tile1 && alive; t++) {
+            for (int kv = 0; kv < 2 && alive; kv++, slot++) {
+              const int st = slot % STAGES;
+              const T *rows[4];                            // of keys lane, lane + 32, ...
+#pragma unroll
+              for (int x = 0; x < 4; x++) {
+                const int key = t * TILE + x * 32 + lane;
+                rows[x] = key < i.keys ? key_row<T>(a, kv ? a.v : a.k, kv ? a.v_page : a.k_page, i.b, i.first, key, i.kh) : nullptr;
+              }
+              if (slot >= STAGES) need_all(empty(st), slot / STAGES - 1);
+              if (!alive) break;
+#pragma unroll
+              for (int x = 0; x < 4; x++) {
+#pragma unroll 4
+                for (int y = 0; y < 32 * (D / 8); y += 32) {
+                  const int r = (y + lane) / (D / 8), c = lane % (D / 8);
+                  const T *from = (const T *)__shfl_sync(~0u, (unsigned long long)rows[x], r);
+                  const int at = st * BYTES + tile_at<128>(x * 32 + r, c);
+                  if (aligned) copy16(ring_at + at, from ? from + c * 8 : (const T *)a.k.data, from);
+                  else *(uint4 *)(ring + at) = from ? gather16(from + c * 8) : make_uint4(0, 0, 0, 0);
+                }
+              }
+              asm volatile("cp.async.commit_group;" ::: "memory");
+              if (landing >= 0) {
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+                landed();
+              }
+              landing = st;
+            }
+          }
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          if (landing >= 0) landed();
+        }
+      }
+    } else if (warp == 11) {
+      // ---- queries, and tiles of values made clean
+      const bool aligned = (((uintptr_t)a.q.data >> 1 | a.q.tok | a.q.head) & 7) == 0;
+      Item i;
+      uint32_t tiles = 0, had[2] = {0, 0};
+      while (next_all(i)) {
+#pragma unroll 1
+        for (int h = 0; h < 2; h++) {
+          const Half x = half_of(a, items, i, h);
+          if (x.count == 0) continue;
+          if (had[h]) need_all(q_empty(h), had[h] - 1);
+          had[h]++;
+          if (!alive) break;
+          const int rows = x.queries * a.group;
+#pragma unroll 8
+          for (int y = lane; y < rows * (D / 8); y += 32) {
+            const int r = y / (D / 8), c = y % (D / 8), query = r / a.in_group;
+            const T *from = row_at<const T>(a.q, i.first + x.q0 + query, i.kh * a.group + r - query * a.group) + c * 8;
+            const int at = h * BYTES + tile_at<128>(r, c);
+            if (aligned) copy16(q_at + at, from, true);
+            else *(uint4 *)(qs + at) = gather16(from);
+          }
+          asm volatile("cp.async.wait_all;" ::: "memory");
+          fence_async();
+          bar_arrive(q_full(h));
+        }
+        const int clear = seen_by_all(a, i, i.t * items.q);
+        for (int t = i.tile0; t < i.tile1 && alive; t++, tiles++) {
+          const int slot = 2 * tiles + 1, st = slot % STAGES;
+          need_all(full(st), slot / STAGES);
+          if (!alive) break;
+          uint32_t bad[4] = {0, 0, 0, 0};
+          if ((t + 1) * TILE > clear) {
+            clean_tile<T, D>(ring + st * BYTES, lane, i.keys - t * TILE, a.causal, bad);
+            fence_async();
+          }
+          __syncwarp();
+          if (lane < 4) bad_rows[tiles % 4 * 4 + lane] = bad[lane];
+          __syncwarp();
+          if (lane == 0) bar_arrive(ready(tiles));
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(taken(turn_of_queue));
+        turn_of_queue++;
+      }
+    } else if (elected()) {
+      // ---- products, from one thread for each half of the rows (one thread for both would set the time)
+      issues = true;
+      constexpr uint32_t TYPE = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+      constexpr uint32_t COMMON = 1u << 4 | TYPE << 7 | TYPE << 10 | (128u >> 4) << 24;
+      constexpr uint32_t QK = COMMON | (TILE >> 3) << 17, PV = COMMON | 1u << 16 | (D >> 3) << 17;
+      const int h = warp == 10;
+      const uint32_t k_op = operand(ring_at, 16), v_op = operand(ring_at, COLUMNS), q_op = operand(q_at + h * BYTES, 16);
+      const uint32_t s_at = scores(h), o_at = sums(h);
+      uint32_t slot = 0, tiles = 0, items_done = 0, turn = 0, turns = 0;
+      auto qk = [&](uint32_t sl) {
+        const uint32_t st = sl % STAGES;
+        uint32_t q = q_op, k = k_op + ((st * BYTES) >> 4);
+#pragma unroll
+        for (int x = 0; x < D / 64; x++, q += COLUMNS >> 4, k += COLUMNS >> 4) {
+#pragma unroll
+          for (int y = 0; y < 4; y++) tc_mma(s_at, q + 2 * y, k + 2 * y, OPERAND_HI, QK, x + y > 0);
+        }
+        tc_commit(s_full(h));
+        tc_commit(empty(st));
+      };
+      Item i;
+      while (next(i)) {
+        const Half x = half_of(a, items, i, h);
+        const int both = min(x.count, half_of(a, items, i, !h).count), n = i.tile1 - i.tile0;
+        take();
+        if (x.count) {
+          need(q_full(h), items_done);
+          need(full(slot % STAGES), slot / STAGES);
+          if (!alive) break;
+          tc_after();
+          qk(slot++);
+          if (x.count == 1) tc_commit(q_empty(h));
+        }
+        for (int j = 0; j < x.count && alive; j++, tiles++) {
+          // this tile's values and the next one's keys, while the rows make their weights
+          const uint32_t sv = slot++, sk = slot;
+          const int seen = x.seen - (i.tile0 + j) * TILE;
+          need(ready(tiles), tiles / 4);
+          if (j + 1 < x.count) need(full(sk % STAGES), sk / STAGES), slot++;
+          if (j == 0 && items_done) need(o_free(h), items_done - 1);
+          if (!alive) break;
+          const uint32_t *const bad = bad_rows + tiles % 4 * 4;
+          const bool add = j > 0 || (bad[0] | bad[1] | bad[2] | bad[3]);
+          const uint32_t v = v_op + ((sv % STAGES * BYTES) >> 4);
+#pragma unroll
+          for (int y = 0; y < 2; y++) {
+            need(p_full(h, y), turn);
+            // The halves take turns, each with all its products for a tile: left alone they fall into step, and the tensor
+            // cores wait while both make weights
+            if (y == 0 && j < both) need(my_turn(h), h ? turns : turns - 1), turns++;
+            if (!alive) break;
+            tc_after();
+#pragma unroll
+            for (int k = 4 * y; k < 4 * y + 4; k++)
+              if (k == 0 || k * 16 < seen) tc_mma_t(o_at, s_at + k * 8, v + k * (2048 >> 4), OPERAND_HI, PV, add || k > 0);
+          }
+          turn++;
+          if (!alive) break;
+          tc_commit(empty(sv % STAGES));
+          if (j + 1 < x.count) {
+            qk(sk);
+            if (j + 2 == x.count) tc_commit(q_empty(h));
+          } else {
+            tc_commit(o_full(h));
+          }
+          if (j < both) bar_arrive(my_turn(!h));
+        }
+        if (x.count) items_done++;
+        for (int j = 2 * x.count; j < 2 * n && alive; j++, slot++) {   // tiles that are only the other half's pass by
+          need(full(slot % STAGES), slot / STAGES);
+          if (alive) bar_arrive(empty(slot % STAGES));
+        }
+        tiles += n - x.count;
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    // ---- one row a thread
+    const int h = warp / 4, r = tid % 128;
+    const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+    const float sl2 = a.scale * 1.4426950408889634f;
+    const bool aligned = (((uintptr_t)a.out.data >> 1 | a.out.tok | a.out.head) & 7) == 0;
+    const int in_half = r / a.in_group, head_in = r - in_half * a.group;
+    uint32_t turn = 0, items_done = 0, tiles = 0;
+    Item i;
+    while (next_all(i)) {
+      const Half x = half_of(a, items, i, h);
+      const int query = x.q0 + in_half, kh = i.kh;
+      const bool valid = in_half < x.queries;
+      const int64_t row = (int64_t)i.first + query;
+      const int limit = a.causal ? min(i.keys, i.keys - i.n + query + 1) : i.keys, clear = seen_by_all(a, i, x.q0), clear_of_all = seen_by_all(a, i, i.t * items.q);
+      const bool whole = i.tile0 == 0 && i.tile1 == i.tiles;
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < x.count; j++, turn++) {
+        alive = __all_sync(~0u, bar_wait(s_full(h), turn & 1, dead));
+        if (!alive) break;
+        tc_after();
+        const int t = i.tile0 + j, nv = limit - t * TILE;
+        const bool masked = (t + 1) * TILE > clear;
+        // Half of the scores at a time, and tensor memory read again for the weights: all 128 in registers would spill, and
+        // shorter pieces add their latencies.
+        uint32_t s[64];
+        auto fetch = [&](int c) {
+          tc_ld(s, scores(h) + lanes + c);
+          tc_ld(s + 32, scores(h) + lanes + c + 32);
+          tc_ld_wait();
+          if (masked) {
+#pragma unroll
+            for (int y = 0; y < 64; y++)
+              if (c + y >= nv) s[y] = 0xFF800000u;         // -infinity
+          }
+        };
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int y = 0; y < 2; y++) {
+          fetch(y * 64);
+#pragma unroll
+          for (int c = 0; c < 64; c += 8) {
+#pragma unroll
+            for (int z = 0; z < 4; z++) top[z] = max3(top[z], __uint_as_float(s[c + 2 * z]), __uint_as_float(s[c + 2 * z + 1]));
+          }
+        }
+        const float big = fmaxf(max3(top[0], top[1], top[2]), top[3]) * sl2;
+        const bool raise = big > m + RAISE || (m == -INFINITY && big > m);
+        if (j == 0) {
+          m = big;
+        } else if (__any_sync(~0u, raise)) {
+          const float to = raise ? big : m, f = raise ? exp2_fast(m - to) : 1.f;
+          uint32_t o[32];
+#pragma unroll 1
+          for (int c = 0; c < D / 32; c++) {
+            tc_ld(o, sums(h) + lanes + c * 32);
+            tc_ld_wait();
+#pragma unroll
+            for (int y = 0; y < 32; y++) o[y] = __float_as_uint(__uint_as_float(o[y]) * f);
+            tc_st(sums(h) + lanes + c * 32, o);
+          }
+          l *= f;
+          m = to;
+        }
+        const float from = m == -INFINITY ? 0.f : m;
+        if (a.causal && (t + 1) * TILE > clear_of_all) {
+          // values that are not finite: each for the rows that see it, before the products are added
+          alive = __all_sync(~0u, bar_wait(ready(tiles + j), (tiles + j) / 4 & 1, dead));
+          if (!alive) break;
+          const uint32_t *const bad = bad_rows + (tiles + j) % 4 * 4;
+          if (bad[0] | bad[1] | bad[2] | bad[3]) {
+#pragma unroll 1
+            for (int c = 0; c < D / 32; c++) {
+              uint32_t o[32];
+              if (j == 0) {
+#pragma unroll
+                for (int y = 0; y < 32; y++) o[y] = 0;
+              } else {
+                tc_ld(o, sums(h) + lanes + c * 32);
+                tc_ld_wait();
+              }
+#pragma unroll 1
+              for (int key = 0; key < TILE; key++) {
+                if (!(bad[key / 32] >> (key % 32) & 1)) continue;
+                uint32_t score;
+                asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(score) : "r"(scores(h) + lanes + key) : "memory");
+                tc_ld_wait();
+                const T *value = key_row<T>(a, a.v, a.v_page, i.b, i.first, t * TILE + key, kh);
+                if (key < nv && value) {
+                  const float p = widen(narrow<T>(exp2_fast(__uint_as_float(score) * sl2 - from)));
+#pragma unroll
+                  for (int y = 0; y < 32; y++) {
+                    const float v = widen(value[c * 32 + y]);
+                    if (!isfinite(v)) o[y] = __float_as_uint(__uint_as_float(o[y]) + p * v);
+                  }
+                }
+                __syncwarp();
+              }
+              tc_st(sums(h) + lanes + c * 32, o);
+            }
+          }
+        }
+        const float2 scale2 = make_float2(sl2, sl2), from2 = make_float2(-from, -from);
+        float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+        for (int y = 0; y < 2; y++) {                      // the products with the first 64 weights start under the others
+          uint32_t pk[32];
+          fetch(y * 64);
+#pragma unroll
+          for (int c = 0; c < 64; c += 2) {
+            float2 e = fma2(make_float2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), scale2, from2);
+            e.x = exp2_fast(e.x), e.y = exp2_fast(e.y);
+            part[c / 2 & 1] = add2(part[c / 2 & 1], e);
+            pk[c / 2] = pack<T>(e.x, e.y);
+          }
+          tc_st(scores(h) + lanes + y * 32, pk);
+          tc_st_wait();
+          tc_before();
+          bar_arrive(p_full(h, y));
+        }
+        const float2 sum = add2(part[0], part[1]);
+        l += sum.x + sum.y;
+      }
+      if (!alive) break;
+      tiles += i.tile1 - i.tile0;
+      const int64_t part = ((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 256 + h * 128 + r;
+      if (x.count) {
+        alive = __all_sync(~0u, bar_wait(o_full(h), items_done & 1, dead));
+        if (!alive) break;
+        items_done++;
+        tc_after();
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        T *const dst = row_at<T>(a.out, row, kh * a.group + head_in);
+        float *const mid = cut.o + part * D;
+#pragma unroll 1
+        for (int c = 0; c < D / 32; c++) {
+          uint32_t o[32];
+          tc_ld(o, sums(h) + lanes + c * 32);
+          tc_ld_wait();
+          if (valid && !whole) {
+#pragma unroll
+            for (int y = 0; y < 32; y += 4) *(uint4 *)(mid + c * 32 + y) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+          } else if (valid) {
+            uint32_t w[16];
+#pragma unroll
+            for (int y = 0; y < 16; y++) w[y] = pack<T>(__uint_as_float(o[2 * y]) * inv, __uint_as_float(o[2 * y + 1]) * inv);
+            if (aligned) {
+#pragma unroll
+              for (int y = 0; y < 16; y += 4) *(uint4 *)(dst + c * 32 + 2 * y) = make_uint4(w[y], w[y + 1], w[y + 2], w[y + 3]);
+            } else {
+#pragma unroll
+              for (int y = 0; y < 16; y++) {
+                T e[2];
+                memcpy(e, &w[y], 4);
+                dst[c * 32 + 2 * y] = e[0], dst[c * 32 + 2 * y + 1] = e[1];
+              }
+            }
+          }
+          __syncwarp();
+        }
+        tc_before();
+        bar_arrive(o_free(h));
+      }
+      if (valid) {
+        if (!whole) cut.ml[part] = make_float2(m, l);
+        else if (a.lse) a.lse[row * a.q_heads + kh * a.group + head_in] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+      }
+      __syncwarp();
+      if (lane == 0) bar_arrive(taken(turn_of_queue));
+      turn_of_queue++;
+    }
+  }
+  tc_before();
+  __syncthreads();
+  if (*dead) {
+    // copies and products in flight end before the block does, whichever warp gave up
+    const uint64_t from = now_ns();
+    if (issues) {
+      const uint32_t bar = ended + (warp == 10 ? 8 : 0);
+      tc_commit(bar);
+      while (!bar_try(bar, 0) && now_ns() - from < DRAIN_NS) {}
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    if (warp == 9) {
+#pragma unroll 1
+      for (int x = max(0, copies - STAGES); x < copies; x++)
+        while (!bar_try(full(x % STAGES), (x / STAGES) & 1) && now_ns() - from < DRAIN_NS) {}
+    }
+    if (tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
+    __syncthreads();
+    // every result of the block's stretch is NaN
+    Stretch s = line;
+    Seq q;
+    Item i;
+    i.b = -1;
+    while (next_item(a, items, s, q, i, tid == 0 ? cut.ends + blockIdx.x : nullptr)) {
+      const bool whole = i.tile0 == 0 && i.tile1 == i.tiles;
+      for (int r = tid; r < 256; r += FWD_THREADS) {
+        const int in_half = r % 128 / a.in_group, query = i.t * items.q + r / 128 * (items.q / 2) + in_half;
+        if (in_half >= items.q / 2 || query >= i.n) continue;
+        const int head = i.kh * a.group + r % 128 - in_half * a.group;
+        if (!whole) {
+          cut.ml[((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 256 + r] = make_float2(NAN, NAN);
+          for (int d = 0; d < D; d++) cut.o[(((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 256 + r) * D + d] = NAN;
+        } else {
+          for (int d = 0; d < D; d++) row_at<T>(a.out, i.first + query, head)[d] = narrow<T>(NAN);
+          if (a.lse) a.lse[((int64_t)i.first + query) * a.q_heads + head] = NAN;
+        }
+      }
+    }
+  }
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+
+// Rows of the items that were cut: a warp each, from the block where the item begins to that where it ends.  Up to 32 parts at a
+// time, a lane takes the maximum and sum of one; then all lanes add up the parts' values, four loads in flight.
+constexpr int JOIN_BLOCKS = 8, JOIN_WARPS = 8;           // thread blocks for an item
+template <typename T, int D>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) k_join(const Args a, const Items<false> items, const Cut cut) {
+  wait_for_kernels_before();
+  const int c = blockIdx.x / JOIN_BLOCKS, lane = threadIdx.x % 32;
+  const int4 end = cut.ends[c];
+  if (end.x < 0) return;
+  const Seq s = sequence(a, end.x);
+  constexpr int E = D / 32;
+  using V = typename std::conditional<E == 2, float2, float4>::type;
+#pragma unroll 1
+  for (int r = blockIdx.x % JOIN_BLOCKS * JOIN_WARPS + threadIdx.x / 32; r < 256; r += JOIN_BLOCKS * JOIN_WARPS) {
+    const int in_half = r % 128 / a.in_group, query = end.z * items.q + r / 128 * (items.q / 2) + in_half;
+    if (in_half >= items.q / 2 || query >= s.n) continue;
+    const int head = end.y * a.group + r % 128 - in_half * a.group;
+    auto place = [&](int x) { return ((int64_t)(c + x) * 2 + (x == 0)) * 256 + r; };
+    float m = -INFINITY, l = 0.f, acc[E] = {};
+    for (int first = 0; first <= end.w; first += 32) {
+      const int x = first + lane;
+      const float2 ml = x <= end.w ? cut.ml[place(x)] : make_float2(-INFINITY, 0.f);
+      float top = fmaxf(m, ml.x);
+#pragma unroll
+      for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
+      const float from = top == -INFINITY ? 0.f : top, keep = exp2_fast(m - from), f = exp2_fast(ml.x - from);
+      float sum = f * ml.y;
+#pragma unroll
+      for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(~0u, sum, k);
+      l = l * keep + sum, m = top;
+#pragma unroll
+      for (int e = 0; e < E; e++) acc[e] *= keep;
+      const uint32_t some = __ballot_sync(~0u, !(ml.x == -INFINITY));   // (a part of no tiles has no values)
+      const int count = min(32, end.w + 1 - first);
+      for (int y = 0; y < count; y += 4) {
+        V v[4];
+        float g[4];
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+          g[k] = __shfl_sync(~0u, f, (y + k) & 31);
+          if (y + k < count && some >> (y + k) & 1) v[k] = ((const V *)(cut.o + place(first + y + k) * D))[lane];
+        }
+#pragma unroll
+        for (int k = 0; k < 4; k++) {
+          if (y + k < count && some >> (y + k) & 1) {
+#pragma unroll
+            for (int e = 0; e < E; e++) acc[e] += g[k] * ((const float *)&v[k])[e];
+          }
+        }
+      }
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    T *const dst = row_at<T>(a.out, s.first + query, head) + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; e++) dst[e] = narrow<T>(acc[e] * inv);
+    if (a.lse && lane == 0) a.lse[((int64_t)s.first + query) * a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+  }
+}
+
+// ---------------------------------------------------------------- gradients
+// Two kernels, one for the gradients of keys and values (a block holds 128 keys and passes along the rows that see them) and one for
+// those of the queries (a block holds 128 rows and passes along the keys they see).  Each works scores and weights out again, so
+// there are seven products where one pass over both would have five, but every sum is taken in one order by one block, with
+// no atomic adds, and nothing of the size of the scores is ever stored.  Weights p and ds are rounded to the inputs' type for
+// their products; all else is in 32 bits.
+//
+// float16 is short of small numbers: weights are held times 2^10 and ds times the power of two that puts the largest |dout| of the
+// call between 1/2 and 1 (then |ds| stays below 256 times the largest |v|, and what is lost below 2^-24 of it does not
+// count beside the largest).  bfloat16 has the range of 32 bits and needs neither.
+constexpr int GRAD_THREADS = 384, DELTA_BLOCKS = 608, DELTA_THREADS = 256;
+template <typename T> constexpr float WEIGHT_SHIFT = std::is_same<T, __half>::value ? 10.f : 0.f;
+template <typename T> constexpr float WEIGHT_UNIT = std::is_same<T, __half>::value ? 0x1p-10f : 1.f;
+
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 y;
+  asm("{\n.reg .b64 a, b;\nmov.b64 a, {%2, %3};\nmov.b64 b, {%4, %5};\nmul.rn.f32x2 a, a, b;\nmov.b64 {%0, %1}, a;\n}"
+      : "=f"(y.x), "=f"(y.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return y;
+}
+
+// e_i = dout_i . out_i - dlse_i of the rows that belong to sequences, and each block's largest finite |dout|.  Bound by memory.
+template <typename T, int D>
+__global__ void __launch_bounds__(DELTA_THREADS) k_delta(const Args a, float *largest) {
+  constexpr int PER = D / 8;                           // lanes of a row
+  __shared__ int ends[2];
+  if (threadIdx.x == 0) ends[0] = a.n_tokens, ends[1] = 0;
+  __syncthreads();
+  for (int b = threadIdx.x; b < a.n_seqs; b += DELTA_THREADS) {
+    const Seq s = sequence(a, b);
+    if (s.n) atomicMin(&ends[0], s.first), atomicMax(&ends[1], s.first + s.n);
+  }
+  __syncthreads();
+  const int from = ends[0], to = max(from, ends[1]);
+  const bool aligned = (((uintptr_t)a.dout.data >> 1 | (uintptr_t)a.out.data >> 1 | a.dout.tok | a.dout.head | a.out.tok | a.out.head) & 7) == 0;
+  const int c = threadIdx.x % PER;
+  float most = 0.f;
+  const int64_t rows = (int64_t)(to - from) * a.q_heads;
+  for (int64_t first = (int64_t)blockIdx.x * (DELTA_THREADS / PER); first < rows; first += (int64_t)gridDim.x * (DELTA_THREADS / PER)) {
+    const int64_t r = first + threadIdx.x / PER;
+    float sum = 0.f;
+    if (r < rows) {
+      const int64_t token = quotient(r, a.q_heads) + from;
+      const int head = (int)(r - (token - from) * a.q_heads);
+      const T *x = row_at<const T>(a.dout, token, head) + c * 8, *y = row_at<const T>(a.out, token, head) + c * 8;
+      const uint4 u = aligned ? *(const uint4 *)x : gather16(x), v = aligned ? *(const uint4 *)y : gather16(y);
+      T e[8], f[8];
+      memcpy(e, &u, 16), memcpy(f, &v, 16);
+#pragma unroll
+      for (int i = 0; i < 8; i++) {
+        const float w = widen(e[i]);
+        sum += w * widen(f[i]);
+        if (isfinite(w)) most = fmaxf(most, fabsf(w));
+      }
+    }
+#pragma unroll
+    for (int o = PER / 2; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
+    if (r < rows && c == 0) {
+      const int64_t at = (int64_t)from * a.q_heads + r;
+      a.delta[at] = sum - (a.dlse ? a.dlse[at] : 0.f);
+    }
+  }
+  if (std::is_same<T, __half>::value) {
+    __shared__ float warps[DELTA_THREADS / 32];
+#pragma unroll
+    for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+    if (threadIdx.x % 32 == 0) warps[threadIdx.x / 32] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 0; w < DELTA_THREADS / 32; w++) most = fmaxf(most, warps[w]);
+      largest[blockIdx.x] = most;
+    }
+  }
+}
+
+// The power of two that ds is held times: of the largest |dout| all threads of the block look for.
+template <typename T> __device__ __forceinline__ float ds_factor(const float *largest) {
+  if (!std::is_same<T, __half>::value) return 1.f;
+  __shared__ float warps[GRAD_THREADS / 32];
+  float most = 0.f;
+  for (int i = threadIdx.x; i < DELTA_BLOCKS; i += GRAD_THREADS) most = fmaxf(most, largest[i]);
+#pragma unroll
+  for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+  if (threadIdx.x % 32 == 0) warps[threadIdx.x / 32] = most;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < GRAD_THREADS / 32; w++) most = fmaxf(most, warps[w]);
+  int e = 0;
+  if (most > 0.f) frexpf(most, &e);
+  return ldexpf(1.f, -e);
+}
+
+// Maps of the rows of queries (or of dout): a box is the `group` heads of a key head of `q` tokens; of keys and values.
+struct GradMaps { CUtensorMap q, dout; Pages kv; };
+
+// Columns of a row in tensor memory to a result, or as they are to a partial one.
+template <typename T, int COLUMNS>
+__device__ __forceinline__ void store_row(uint32_t at, T *dst, float *part, bool valid, bool aligned, float factor) {
+#pragma unroll 1
+  for (int c = 0; c < COLUMNS; c += 32) {
+    uint32_t o[32];
+    tc_ld(o, at + c);
+    tc_ld_wait();
+    if (valid && part) {
+#pragma unroll
+      for (int y = 0; y < 32; y += 4) *(uint4 *)(part + c + y) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+    } else if (valid) {
+      uint32_t w[16];
+#pragma unroll
+      for (int y = 0; y < 16; y++) w[y] = pack<T>(__uint_as_float(o[2 * y]) * factor, __uint_as_float(o[2 * y + 1]) * factor);
+      if (aligned) {
+#pragma unroll
+        for (int y = 0; y < 16; y += 4) *(uint4 *)(dst + c + 2 * y) = make_uint4(w[y], w[y + 1], w[y + 2], w[y + 3]);
+      } else {
+#pragma unroll
+        for (int y = 0; y < 16; y++) {
+          T e[2];
+          memcpy(e, &w[y], 4);
+          dst[c + 2 * y] = e[0], dst[c + 2 * y + 1] = e[1];
+        }
+      }
+    }
+    __syncwarp();
+  }
+}
+__device__ __forceinline__ bool rows_aligned(const Heads &h) { return (((uintptr_t)h.data >> 1 | h.tok | h.head) & 7) == 0; }
+
+// What the two kernels' threads that issue products need: shapes of S (or dP), 128 x 128 over a head, and of products with 128
+// weights to a row, from tensor memory.  Half w of the threads writes its 64 weights to a row 64 columns after the other's.
+template <typename T, int D> struct Products {
+  static constexpr uint32_t TYPE = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+  static constexpr uint32_t COMMON = 1u << 4 | TYPE << 7 | TYPE << 10 | (128u >> 4) << 24;
+  static constexpr uint32_t ROWS = COMMON | (TILE >> 3) << 17, SUMS = COMMON | 1u << 16 | (D >> 3) << 17;
+  static constexpr uint32_t COLUMNS = TILE * 128 >> 4;
+  static __device__ __forceinline__ void scores(uint32_t to, uint32_t x, uint32_t y) {
+#pragma unroll
+    for (int c = 0; c < D / 64; c++, x += COLUMNS, y += COLUMNS) {
+#pragma unroll
+      for (int k = 0; k < 4; k++) tc_mma(to, x + 2 * k, y + 2 * k, OPERAND_HI, ROWS, c + k > 0);
+    }
+  }
+  static __device__ __forceinline__ void sums(uint32_t to, uint32_t weights, uint32_t y, bool add) {
+#pragma unroll
+    for (int k = 0; k < 8; k++) tc_mma_t(to, weights + k / 4 * 64 + k % 4 * 8, y + k * (2048 >> 4), OPERAND_HI, SUMS, add || k > 0);
+  }
+};
+
+// Keys and values.  Warp 9 walks along the stretch and brings an item's keys and values and then its tiles of rows: queries and
+// dout by TMA.  Warps 10 and 11 clean queries and dout where some are out of sight, and bring the rows' lse and e.  Warp 8 issues the products:
+//   S^T = K Q^T, dP^T = V dout^T, dV += P^T dout, dK += dS^T Q
+// in the order S, dP, (dV, next S, dK, next dP), ..., so that the tensor cores have the next scores to work out while rows turn the
+// present ones into weights: nothing waits for a second buffer.  Warps 0..7: a thread for a key and half of a tile's rows.
+template <int D> struct GradKv {
+  static constexpr int BYTES = TILE * D * 2, STAGES = D == 64 ? 4 : 2;
+  static constexpr int SMEM = 2 * BYTES + STAGES * (2 * BYTES + 2 * TILE * 4) + 1024 + 512;
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const Items<true> items, const Cut cut, const float *largest, const __grid_constant__ GradMaps maps) {
+  constexpr int BYTES = GradKv<D>::BYTES, STAGES = GradKv<D>::STAGES, COLUMNS = TILE * 128;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char *const kv = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023), *const ring = kv + 2 * BYTES;
+  float *const stats = (float *)(ring + STAGES * 2 * BYTES);                            // [stage][2][128]: -lse (of log2 weights), -e
+  uint64_t *const bars = (uint64_t *)(stats + STAGES * 2 * TILE);
+  constexpr int BARS = 3 * STAGES + 2 * QUEUE + 9;
+  Item *const queue = (Item *)(bars + BARS);
+  uint32_t *const tmem_at = (uint32_t *)(queue + QUEUE);
+  volatile int *const dead = (volatile int *)(tmem_at + 1);
+  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 8 <= 512, "room behind the ring");
+  const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
+  const uint32_t bar0 = smem_u32(bars), kv_at = smem_u32(kv), ring_at = smem_u32(ring);
+  auto full = [&](int s) { return bar0 + s * 8; };
+  auto ready = [&](int s) { return bar0 + (STAGES + s) * 8; };
+  auto empty = [&](int s) { return bar0 + (2 * STAGES + s) * 8; };
+  auto given = [&](uint32_t i) { return bar0 + (3 * STAGES + i % QUEUE) * 8; };
+  auto taken = [&](uint32_t i) { return bar0 + (3 * STAGES + QUEUE + i % QUEUE) * 8; };
+  const uint32_t rest = bar0 + (3 * STAGES + 2 * QUEUE) * 8;
+  const uint32_t kv_full = rest, kv_empty = rest + 8, s_full = rest + 16, dp_full = rest + 24, p_full = rest + 32, ds_full = rest + 40,
+                 o_full = rest + 48, o_free = rest + 56, ended = rest + 64;
+
+  dependents_may_start();
+  Stretch line = find_stretch<true, GRAD_THREADS>(a, items, cut.blocks);
+  if (line.rest_from + a.n_tokens - line.rest_to > 0) {
+    if (a.zero_rest & 2) zero_rest<T>(a, a.dk, a.kv_heads, D, line);
+    if (a.zero_rest & 4) zero_rest<T>(a, a.dv, a.kv_heads, D, line);
+  }
+  if (tid == 0) cut.ends[blockIdx.x] = make_int4(NOTHING, 0, 0, 0);
+  if (line.x0 >= line.x1) return;
+  const float factor = ds_factor<T>(largest);
+  if (tid == 0) {
+    for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(ready(s), 2), bar_init(empty(s), 9);
+    bar_init(kv_full, 1), bar_init(kv_empty, 1), bar_init(s_full, 1), bar_init(dp_full, 1), bar_init(p_full, 256), bar_init(ds_full, 256);
+    bar_init(o_full, 1), bar_init(o_free, 256), bar_init(ended, 1);
+    for (int i = 0; i < QUEUE; i++) bar_init(given(i), 1), bar_init(taken(i), 11);
+    *dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_at)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  // rows that no box reaches (where the group does not divide 128) stay zero
+  const int box_rows = items.q * a.group;
+  for (int y = tid; y < STAGES * 2 * (TILE - box_rows) * (D / 8); y += GRAD_THREADS) {
+    const int c = y % (D / 8), r = y / (D / 8) % (TILE - box_rows) + box_rows, s = y / (D / 8) / (TILE - box_rows);
+    *(uint4 *)(ring + s * BYTES + tile_at<128>(r, c)) = make_uint4(0, 0, 0, 0);
+  }
+  fence_async();
+  tc_before();
+  __syncthreads();
+  tc_after();
+  const uint32_t tmem = __shfl_sync(~0u, *tmem_at, 0), s_at = tmem, dp_at = tmem + 128, dv_at = tmem + 256, dk_at = tmem + 384;
+  int copies = 0, kv_copies = 0;
+  bool issues = false, alive = true;
+  auto need = [&](uint32_t bar, uint32_t parity) { alive = alive && bar_wait(bar, parity & 1, dead); };
+  uint32_t turn_of_queue = 0;
+  auto next = [&](Item &i) {                           // (of one thread)
+    need(given(turn_of_queue), turn_of_queue / QUEUE);
+    if (alive) i = queue[turn_of_queue % QUEUE];
+    return alive && i.tiles > 0;
+  };
+  auto need_all = [&](uint32_t bar, uint32_t parity) { alive = __all_sync(~0u, bar_wait(bar, parity & 1, dead)); };
+  auto next_all = [&](Item &i) {                       // of a warp
+    need_all(given(turn_of_queue), turn_of_queue / QUEUE);
+    if (alive) i = queue[turn_of_queue % QUEUE];
+    return alive && i.tiles > 0;
+  };
+  // the first query of a tile, and whether it hides keys from some of its rows
+  auto first_query = [&](const Item &i, int tile) { return (items.first_tile(i.t) + tile) * items.q; };
+  auto hides = [&](const Item &i, int q0) { return a.causal && q0 < min(i.t * TILE + TILE, i.keys) - 1; };
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp == 9) {
+      Stretch s = line;
+      Seq q;
+      Item i;
+      i.b = -1;
+      for (uint32_t n = 0; alive; n++) {
+        if (!next_item(a, items, s, q, i, lane == 0 ? cut.ends + blockIdx.x : nullptr)) i.tiles = 0;
+        if (n >= QUEUE) need_all(taken(n), n / QUEUE - 1);
+        if (!alive) break;
+        if (lane == 0) queue[n % QUEUE] = i, bar_arrive(given(n));
+        if (i.tiles == 0) break;
+        if (n) need_all(kv_empty, n - 1);
+        if (!alive) break;
+        if (lane == 0) {
+          bar_expect(kv_full, 2 * BYTES);
+          const int token = i.first + i.t * TILE;
+#pragma unroll
+          for (int x = 0; x < D / 64; x++) {
+            tile_load(kv_at + x * COLUMNS, &maps.kv.k, x * 64, maps.kv.k_heads_first ? i.kh : token, maps.kv.k_heads_first ? token : i.kh, 0, kv_full);
+            tile_load(kv_at + BYTES + x * COLUMNS, &maps.kv.v, x * 64, maps.kv.v_heads_first ? i.kh : token, maps.kv.v_heads_first ? token : i.kh, 0, kv_full);
+          }
+        }
+        kv_copies++;
+        __syncwarp();
+        for (int t = i.tile0; t < i.tile1; t++, copies++) {
+          const int st = copies % STAGES;
+          if (copies >= STAGES) need_all(empty(st), copies / STAGES - 1);
+          if (!alive) break;
+          if (lane == 0) {
+            bar_expect(full(st), 2 * box_rows * D * 2);
+            const int token = i.first + first_query(i, t);
+#pragma unroll
+            for (int x = 0; x < D / 64; x++) {
+              tile_load(ring_at + st * 2 * BYTES + x * COLUMNS, &maps.q, x * 64, i.kh * a.group, token, 0, full(st));
+              tile_load(ring_at + st * 2 * BYTES + BYTES + x * COLUMNS, &maps.dout, x * 64, i.kh * a.group, token, 0, full(st));
+            }
+          }
+          __syncwarp();
+        }
+      }
+    } else if (warp >= 10) {
+      // ---- one cleans queries and brings lse, the other dout and e
+      const int which = warp - 10;
+      const float *const src = which ? a.delta : a.lse;
+      const float factor_of = which ? -factor * WEIGHT_UNIT<T> : -1.4426950408889634f, shift = which ? 0.f : WEIGHT_SHIFT<T>, none = which ? 0.f : -INFINITY;
+      Item i;
+      int tiles = 0;
+      while (next_all(i)) {
+        float x[4];
+        auto ask = [&](int t) {                        // of rows lane, lane + 32, ... of a tile
+          const int q0 = first_query(i, t), live = min(items.q, i.n - q0) * a.group;
+#pragma unroll
+          for (int k = 0; k < 4; k++) {
+            const int r = lane + k * 32, query = r / a.in_group;
+            x[k] = none;
+            if (r < live) x[k] = src[((int64_t)i.first + q0 + query) * a.q_heads + i.kh * a.group + r - query * a.group] * factor_of + shift;
+          }
+        };
+        ask(i.tile0);
+        for (int t = i.tile0; t < i.tile1 && alive; t++, tiles++) {
+          const int st = tiles % STAGES, q0 = first_query(i, t), live = min(items.q, i.n - q0) * a.group;
+          need_all(full(st), tiles / STAGES);
+          if (!alive) break;
+#pragma unroll
+          for (int k = 0; k < 4; k++) stats[(st * 2 + which) * TILE + lane + k * 32] = x[k];
+          if (t + 1 < i.tile1) ask(t + 1);
+          if (hides(i, q0) || live < box_rows) {
+            uint32_t bad[4];
+            clean_tile<T, D>(ring + (st * 2 + which) * BYTES, lane, live, hides(i, q0), bad);
+            fence_async();
+          }
+          __syncwarp();
+          if (lane == 0) bar_arrive(ready(st));
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(taken(turn_of_queue));
+        turn_of_queue++;
+      }
+    } else if (elected()) {
+      issues = true;
+      using P = Products<T, D>;
+      const uint32_t k_op = operand(kv_at, 16), v_op = operand(kv_at + BYTES, 16);
+      const uint32_t rows_op = operand(ring_at, 16), sums_op = operand(ring_at, COLUMNS);
+      auto stage = [&](int tile) { return (uint32_t)(tile % STAGES * 2 * BYTES) >> 4; };
+      int tiles = 0;
+      uint32_t done = 0;
+      Item i;
+      while (next(i)) {
+        const int n = i.tile1 - i.tile0;
+        bar_arrive(taken(turn_of_queue++));
+        need(kv_full, done);
+        need(ready(tiles % STAGES), tiles / STAGES);
+        if (!alive) break;
+        tc_after();
+        P::scores(s_at, k_op, rows_op + stage(tiles));
+        tc_commit(s_full);
+        P::scores(dp_at, v_op, rows_op + stage(tiles) + (BYTES >> 4));
+        tc_commit(dp_full);
+        if (n == 1) tc_commit(kv_empty);
+        for (int j = 0; j < n && alive; j++, tiles++) {
+          need(p_full, tiles);
+          if (j == 0 && done) need(o_free, done - 1);
+          if (!alive) break;
+          tc_after();
+          P::sums(dv_at, s_at, sums_op + stage(tiles) + (BYTES >> 4), j > 0);
+          if (j + 1 < n) {
+            need(ready((tiles + 1) % STAGES), (tiles + 1) / STAGES);
+            if (!alive) break;
+            tc_after();
+            P::scores(s_at, k_op, rows_op + stage(tiles + 1));
+            tc_commit(s_full);
+          }
+          need(ds_full, tiles);
+          if (!alive) break;
+          tc_after();
+          P::sums(dk_at, dp_at, sums_op + stage(tiles), j > 0);
+          tc_commit(empty(tiles % STAGES));
+          if (j + 1 < n) {
+            P::scores(dp_at, v_op, rows_op + stage(tiles + 1) + (BYTES >> 4));
+            tc_commit(dp_full);
+            if (j + 2 == n) tc_commit(kv_empty);
+          } else {
+            tc_commit(o_full);
+          }
+        }
+        done++;
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    const int w = warp / 4, r = tid % 128;
+    const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+    const float sl2 = a.scale * 1.4426950408889634f, dp_scale = factor * WEIGHT_UNIT<T>;
+    const Heads &to = w ? a.dk : a.dv;
+    const bool aligned = rows_aligned(to);
+    int tiles = 0;
+    uint32_t done = 0;
+    Item i;
+    while (next_all(i)) {
+      const int key = i.t * TILE + r;
+      for (int t = i.tile0; t < i.tile1; t++, tiles++) {
+        const int st = tiles % STAGES, q0 = first_query(i, t);
+        const bool masked = hides(i, q0);
+        const int first_seen = (key - q0) * a.group - w * 64;   // columns before it are rows that do not see this key
+        const float *const nl = stats + st * 2 * TILE + w * 64, *const ne = nl + TILE;
+        need(ready(st), tiles / STAGES);
+        need(s_full, tiles);
+        alive = __all_sync(~0u, alive);
+        if (!alive) break;
+        tc_after();
+        uint32_t p[64];
+        tc_ld(p, s_at + lanes + w * 64);
+        tc_ld(p + 32, s_at + lanes + w * 64 + 32);
+        tc_ld_wait();
+        const float2 scale2 = make_float2(sl2, sl2);
+        uint32_t pk[32];
+#pragma unroll
+        for (int c = 0; c < 64; c += 4) {
+          const float4 l = *(const float4 *)(nl + c);
+          const float2 x = fma2(make_float2(__uint_as_float(p[c]), __uint_as_float(p[c + 1])), scale2, make_float2(l.x, l.y));
+          const float2 y = fma2(make_float2(__uint_as_float(p[c + 2]), __uint_as_float(p[c + 3])), scale2, make_float2(l.z, l.w));
+          p[c] = __float_as_uint(exp2_fast(x.x)), p[c + 1] = __float_as_uint(exp2_fast(x.y));
+          p[c + 2] = __float_as_uint(exp2_fast(y.x)), p[c + 3] = __float_as_uint(exp2_fast(y.y));
+        }
+        if (masked) {
+          // (dout has lost its infinite and NaN values here: e has them, and makes NaN of the weights of rows that have some)
+#pragma unroll
+          for (int c = 0; c < 64; c++) p[c] = c < first_seen ? 0 : __float_as_uint(fmaf(0.f, ne[c], __uint_as_float(p[c])));
+        }
+#pragma unroll
+        for (int c = 0; c < 64; c += 2) pk[c / 2] = pack<T>(__uint_as_float(p[c]), __uint_as_float(p[c + 1]));
+        tc_st(s_at + lanes + w * 64, pk);
+        tc_st_wait();
+        tc_before();
+        bar_arrive(p_full);
+
+        alive = __all_sync(~0u, bar_wait(dp_full, tiles & 1, dead));
+        if (!alive) break;
+        tc_after();
+        const float2 dp2 = make_float2(dp_scale, dp_scale);
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+          uint32_t d[32];
+          tc_ld(d, dp_at + lanes + w * 64 + half * 32);
+          tc_ld_wait();
+#pragma unroll
+          for (int c = 0; c < 32; c += 4) {
+            const int z = half * 32 + c;
+            const float4 e = *(const float4 *)(ne + z);
+            const float2 x = fma2(make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1])), dp2, make_float2(e.x, e.y));
+            const float2 y = fma2(make_float2(__uint_as_float(d[c + 2]), __uint_as_float(d[c + 3])), dp2, make_float2(e.z, e.w));
+            float2 u = mul2(make_float2(__uint_as_float(p[z]), __uint_as_float(p[z + 1])), x);
+            float2 v = mul2(make_float2(__uint_as_float(p[z + 2]), __uint_as_float(p[z + 3])), y);
+            if (masked) {
+              u.x = z < first_seen ? 0.f : u.x, u.y = z + 1 < first_seen ? 0.f : u.y;
+              v.x = z + 2 < first_seen ? 0.f : v.x, v.y = z + 3 < first_seen ? 0.f : v.y;
+            }
+            pk[z / 2] = pack<T>(u.x, u.y), pk[z / 2 + 1] = pack<T>(v.x, v.y);
+          }
+        }
+        tc_st(dp_at + lanes + w * 64, pk);
+        tc_st_wait();
+        tc_before();
+        bar_arrive(ds_full);
+        __syncwarp();
+        if (lane == 0) bar_arrive(empty(st));
+      }
+      if (!alive) break;
+      alive = __all_sync(~0u, bar_wait(o_full, done & 1, dead));
+      if (!alive) break;
+      done++;
+      tc_after();
+      const bool whole = i.tile0 == 0 && i.tile1 == i.tiles;
+      float *const part = whole ? nullptr : cut.o + ((((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 2 + w) * TILE + r) * D;
+      store_row<T, D>((w ? dk_at : dv_at) + lanes, row_at<T>(to, (int64_t)i.first + key, i.kh), part, key < i.keys, aligned,
+                      w ? a.scale / factor : WEIGHT_UNIT<T>);
+      tc_before();
+      bar_arrive(o_free);
+      __syncwarp();
+      if (lane == 0) bar_arrive(taken(turn_of_queue));
+      turn_of_queue++;
+    }
+  }
+  tc_before();
+  __syncthreads();
+  if (*dead) {
+    const uint64_t from = now_ns();
+    if (issues) {
+      tc_commit(ended);
+      while (!bar_try(ended, 0) && now_ns() - from < DRAIN_NS) {}
+    }
+    if (warp == 9) {
+#pragma unroll 1
+      for (int x = max(0, copies - STAGES); x < copies; x++)
+        while (!bar_try(full(x % STAGES), (x / STAGES) & 1) && now_ns() - from < DRAIN_NS) {}
+      while (kv_copies && !bar_try(kv_full, (kv_copies - 1) & 1) && now_ns() - from < DRAIN_NS) {}
+    }
+    if (tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
+    __syncthreads();
+    Stretch s = line;
+    Seq q;
+    Item i;
+    i.b = -1;
+    while (next_item(a, items, s, q, i, tid == 0 ? cut.ends + blockIdx.x : nullptr)) {
+      const bool whole = i.tile0 == 0 && i.tile1 == i.tiles;
+      for (int x = tid; x < 2 * TILE * D; x += GRAD_THREADS) {
+        const int w = x / (TILE * D), r = x / D % TILE, d = x % D, key = i.t * TILE + r;
+        if (key >= i.keys) continue;
+        if (whole) row_at<T>(w ? a.dk : a.dv, (int64_t)i.first + key, i.kh)[d] = narrow<T>(NAN);
+        else cut.o[((((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 2 + w) * TILE + r) * D + d] = NAN;
+      }
+    }
+  }
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+
+// Queries.  Warp 9 walks along the stretch and brings an item's queries and dout and then its tiles of keys and values; warp 10 cleans
+// tiles of keys in which some are out of sight.  Warp 8 issues the products:
+//   S = Q K^T (in two buffers), dP = dout V^T, dQ += dS K
+// in the order (next dP, dQ, S of the tile after), so that the rows find their next scores and dP ready.  dS overwrites S.
+// Warps 0..7: a thread for a row and half of a tile's keys.
+template <int D> struct GradQ {
+  static constexpr int BYTES = TILE * D * 2, STAGES = D == 64 ? 8 : 5;
+  static constexpr int SMEM = (2 + STAGES) * BYTES + 1024 + 768;
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const Items<false> items, const Cut cut, const float *largest, const __grid_constant__ GradMaps maps) {
+  constexpr int BYTES = GradQ<D>::BYTES, STAGES = GradQ<D>::STAGES, COLUMNS = TILE * 128;
+  extern __shared__ unsigned char smem_raw[];
+  unsigned char *const rows = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023), *const ring = rows + 2 * BYTES;
+  uint64_t *const bars = (uint64_t *)(ring + STAGES * BYTES);
+  constexpr int BARS = 2 * STAGES + 2 * QUEUE + 14;
+  Item *const queue = (Item *)(bars + BARS);
+  uint32_t *const tmem_at = (uint32_t *)(queue + QUEUE);
+  volatile int *const dead = (volatile int *)(tmem_at + 1);
+  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 8 <= 768, "room behind the ring");
+  const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
+  const uint32_t bar0 = smem_u32(bars), rows_at = smem_u32(rows), ring_at = smem_u32(ring);
+  auto full = [&](int s) { return bar0 + s * 8; };
+  auto empty = [&](int s) { return bar0 + (STAGES + s) * 8; };
+  auto given = [&](uint32_t i) { return bar0 + (2 * STAGES + i % QUEUE) * 8; };
+  auto taken = [&](uint32_t i) { return bar0 + (2 * STAGES + QUEUE + i % QUEUE) * 8; };
+  const uint32_t rest = bar0 + (2 * STAGES + 2 * QUEUE) * 8;
+  const uint32_t q_full = rest, q_empty = rest + 8, dp_full = rest + 16, ds_full = rest + 24, o_full = rest + 32, o_free = rest + 40, ended = rest + 48;
+  auto s_full = [&](int tile) { return rest + 56 + tile % 2 * 8; };
+  auto ready = [&](int tile) { return rest + 72 + tile % 4 * 8; };                      // its keys are clean
+
+  dependents_may_start();
+  Stretch line = find_stretch<false, GRAD_THREADS>(a, items, cut.blocks);
+  if (line.rest_from + a.n_tokens - line.rest_to > 0 && a.zero_rest & 1) zero_rest<T>(a, a.dq, a.q_heads, D, line);
+  if (tid == 0) cut.ends[blockIdx.x] = make_int4(NOTHING, 0, 0, 0);
+  if (line.x0 >= line.x1) return;
+  const float factor = ds_factor<T>(largest);
+  if (tid == 0) {
+    for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(empty(s), 1);
+    bar_init(q_full, 1), bar_init(q_empty, 1), bar_init(dp_full, 1), bar_init(ds_full, 256), bar_init(o_full, 1), bar_init(o_free, 256), bar_init(ended, 1);
+    for (int s = 0; s < 2; s++) bar_init(s_full(s), 1);
+    for (int s = 0; s < 4; s++) bar_init(ready(s), 1);
+    for (int i = 0; i < QUEUE; i++) bar_init(given(i), 1), bar_init(taken(i), 10);
+    *dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 8) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_at)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  tc_before();
+  __syncthreads();
+  tc_after();
+  const uint32_t tmem = __shfl_sync(~0u, *tmem_at, 0), dp_at = tmem + 256, dq_at = tmem + 384;
+  auto s_at = [&](int tile) { return tmem + tile % 2 * 128; };
+  int copies = 0, q_copies = 0;
+  bool issues = false, alive = true;
+  auto need = [&](uint32_t bar, uint32_t parity) { alive = alive && bar_wait(bar, parity & 1, dead); };
+  uint32_t turn_of_queue = 0;
+  auto next = [&](Item &i) {                           // (of one thread)
+    need(given(turn_of_queue), turn_of_queue / QUEUE);
+    if (alive) i = queue[turn_of_queue % QUEUE];
+    return alive && i.tiles > 0;
+  };
+  auto need_all = [&](uint32_t bar, uint32_t parity) { alive = __all_sync(~0u, bar_wait(bar, parity & 1, dead)); };
+  auto next_all = [&](Item &i) {                       // of a warp
+    need_all(given(turn_of_queue), turn_of_queue / QUEUE);
+    if (alive) i = queue[turn_of_queue % QUEUE];
+    return alive && i.tiles > 0;
+  };
+
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    if (warp == 9) {
+      Stretch s = line;
+      Seq q;
+      Item i;
+      i.b = -1;
+      for (uint32_t n = 0; alive; n++) {
+        if (!next_item(a, items, s, q, i, lane == 0 ? cut.ends + blockIdx.x : nullptr)) i.tiles = 0;
+        if (n >= QUEUE) need_all(taken(n), n / QUEUE - 1);
+        if (!alive) break;
+        if (lane == 0) queue[n % QUEUE] = i, bar_arrive(given(n));
+        if (i.tiles == 0) break;
+        if (n) need_all(q_empty, n - 1);
+        if (!alive) break;
+        if (lane == 0) {
+          bar_expect(q_full, 2 * items.q * a.group * D * 2);
+          const int token = i.first + i.t * items.q;
+#pragma unroll
+          for (int x = 0; x < D / 64; x++) {
+            tile_load(rows_at + x * COLUMNS, &maps.q, x * 64, i.kh * a.group, token, 0, q_full);
+            tile_load(rows_at + BYTES + x * COLUMNS, &maps.dout, x * 64, i.kh * a.group, token, 0, q_full);
+          }
+        }
+        q_copies++;
+        __syncwarp();
+        for (int x = 2 * i.tile0; x < 2 * i.tile1; x++, copies++) {   // keys, values, keys, ...
+          const int st = copies % STAGES, token = i.first + x / 2 * TILE;
+          if (copies >= STAGES) need_all(empty(st), copies / STAGES - 1);
+          if (!alive) break;
+          const bool heads_first = x % 2 ? maps.kv.v_heads_first : maps.kv.k_heads_first;
+          if (lane == 0) {
+            bar_expect(full(st), BYTES);
+#pragma unroll
+            for (int c = 0; c < D / 64; c++)
+              tile_load(ring_at + st * BYTES + c * COLUMNS, x % 2 ? &maps.kv.v : &maps.kv.k, c * 64, heads_first ? i.kh : token, heads_first ? token : i.kh, 0, full(st));
+          }
+          __syncwarp();
+        }
+      }
+    } else if (warp == 10) {
+      Item i;
+      int tiles = 0;
+      while (next_all(i)) {
+        const int clear = seen_by_all(a, i, i.t * items.q);
+        for (int t = i.tile0; t < i.tile1 && alive; t++, tiles++) {
+          const int slot = 2 * tiles;
+          need_all(full(slot % STAGES), slot / STAGES);
+          if (!alive) break;
+          if ((t + 1) * TILE > clear) {
+            uint32_t bad[4];
+            clean_tile<T, D>(ring + slot % STAGES * BYTES, lane, i.keys - t * TILE, a.causal, bad);
+            fence_async();
+          }
+          __syncwarp();
+          if (lane == 0) bar_arrive(ready(tiles));
+        }
+        __syncwarp();
+        if (lane == 0) bar_arrive(taken(turn_of_queue));
+        turn_of_queue++;
+      }
+    } else if (warp == 8 && elected()) {
+      issues = true;
+      using P = Products<T, D>;
+      const uint32_t q_op = operand(rows_at, 16), do_op = operand(rows_at + BYTES, 16), rows_op = operand(ring_at, 16), sums_op = operand(ring_at, COLUMNS);
+      auto stage = [&](int slot) { return (uint32_t)(slot % STAGES * BYTES) >> 4; };
+      int tiles = 0;
+      uint32_t done = 0;
+      auto scores = [&](int tile) {
+        need(ready(tile), tile / 4);
+        if (!alive) return;
+        tc_after();
+        P::scores(s_at(tile), q_op, rows_op + stage(2 * tile));
+        tc_commit(s_full(tile));
+      };
+      auto dp = [&](int tile, bool last) {
+        need(full((2 * tile + 1) % STAGES), (2 * tile + 1) / STAGES);
+        if (!alive) return;
+        tc_after();
+        P::scores(dp_at, do_op, rows_op + stage(2 * tile + 1));
+        tc_commit(dp_full);
+        tc_commit(empty((2 * tile + 1) % STAGES));
+        if (last) tc_commit(q_empty);
+      };
+      Item i;
+      while (next(i)) {
+        const int n = i.tile1 - i.tile0;
+        bar_arrive(taken(turn_of_queue++));
+        need(q_full, done);
+        if (alive) scores(tiles);
+        if (alive) dp(tiles, n == 1);
+        if (alive && n > 1) scores(tiles + 1);
+        for (int j = 0; j < n && alive; j++, tiles++) {
+          need(ds_full, tiles);
+          if (j == 0 && done) need(o_free, done - 1);
+          if (!alive) break;
+          tc_after();
+          if (j + 1 < n) dp(tiles + 1, j + 2 == n);
+          if (!alive) break;
+          P::sums(dq_at, s_at(tiles), sums_op + stage(2 * tiles), j > 0);
+          tc_commit(empty(2 * tiles % STAGES));
+          if (j + 2 < n) scores(tiles + 2);
+          if (j + 1 == n) tc_commit(o_full);
+        }
+        done++;
+      }
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    const int w = warp / 4, r = tid % 128, in_tile = r / a.in_group, head_in = r - in_tile * a.group;
+    const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+    const float sl2 = a.scale * 1.4426950408889634f, dp_scale = factor * WEIGHT_UNIT<T>;
+    const bool aligned = rows_aligned(a.dq);
+    int tiles = 0;
+    uint32_t done = 0;
+    Item i;
+    while (next_all(i)) {
+      const int query = i.t * items.q + in_tile, limit = a.causal ? min(i.keys, query + 1) : i.keys, clear = seen_by_all(a, i, i.t * items.q);
+      const bool valid = in_tile < items.q && query < i.n;
+      const int64_t row = (int64_t)i.first + query;
+      float nl = 0.f, ne = 0.f;
+      if (valid) {
+        const int64_t at = row * a.q_heads + i.kh * a.group + head_in;
+        nl = WEIGHT_SHIFT<T> - a.lse[at] * 1.4426950408889634f, ne = -a.delta[at] * dp_scale;
+      }
+      for (int t = i.tile0; t < i.tile1; t++, tiles++) {
+        const bool masked = (t + 1) * TILE > clear;
+        const int seen = limit - t * TILE - w * 64;
+        alive = __all_sync(~0u, bar_wait(s_full(tiles), tiles / 2 & 1, dead));
+        if (!alive) break;
+        tc_after();
+        const uint32_t at = s_at(tiles) + lanes + w * 64;
+        uint32_t p[64];
+        tc_ld(p, at);
+        tc_ld(p + 32, at + 32);
+        tc_ld_wait();
+        const float2 scale2 = make_float2(sl2, sl2), nl2 = make_float2(nl, nl);
+#pragma unroll
+        for (int c = 0; c < 64; c += 2) {
+          const float2 x = fma2(make_float2(__uint_as_float(p[c]), __uint_as_float(p[c + 1])), scale2, nl2);
+          p[c] = __float_as_uint(exp2_fast(x.x)), p[c + 1] = __float_as_uint(exp2_fast(x.y));
+        }
+        alive = __all_sync(~0u, bar_wait(dp_full, tiles & 1, dead));
+        if (!alive) break;
+        tc_after();
+        const float2 dp2 = make_float2(dp_scale, dp_scale), ne2 = make_float2(ne, ne);
+        uint32_t pk[32];
+#pragma unroll
+        for (int half = 0; half < 2; half++) {
+          uint32_t d[32];
+          tc_ld(d, dp_at + lanes + w * 64 + half * 32);
+          tc_ld_wait();
+#pragma unroll
+          for (int c = 0; c < 32; c += 2) {
+            const int z = half * 32 + c;
+            const float2 x = fma2(make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1])), dp2, ne2);
+            float2 u = mul2(make_float2(__uint_as_float(p[z]), __uint_as_float(p[z + 1])), x);
+            if (masked) u.x = z < seen ? u.x : 0.f, u.y = z + 1 < seen ? u.y : 0.f;
+            pk[z / 2] = pack<T>(u.x, u.y);
+          }
+        }
+        tc_st(at, pk);
+        tc_st_wait();
+        tc_before();
+        bar_arrive(ds_full);
+      }
+      if (!alive) break;
+      alive = __all_sync(~0u, bar_wait(o_full, done & 1, dead));
+      if (!alive) break;
+      done++;
+      tc_after();
+      const bool whole = i.tile0 == 0 && i.tile1 == i.tiles;
+      float *const part = whole ? nullptr : cut.o + (((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * TILE + r) * D + w * (D / 2);
+      store_row<T, D / 2>(dq_at + lanes + w * (D / 2), row_at<T>(a.dq, row, i.kh * a.group + head_in) + w * (D / 2), part, valid, aligned, a.scale / factor);
+      tc_before();
+      bar_arrive(o_free);
+      __syncwarp();
+      if (lane == 0) bar_arrive(taken(turn_of_queue));
+      turn_of_queue++;
+    }
+  }
+  tc_before();
+  __syncthreads();
+  if (*dead) {
+    const uint64_t from = now_ns();
+    if (issues) {
+      tc_commit(ended);
+      while (!bar_try(ended, 0) && now_ns() - from < DRAIN_NS) {}
+    }
+    if (warp == 9) {
+#pragma unroll 1
+      for (int x = max(0, copies - STAGES); x < copies; x++)
+        while (!bar_try(full(x % STAGES), (x / STAGES) & 1) && now_ns() - from < DRAIN_NS) {}
+      while (q_copies && !bar_try(q_full, (q_copies - 1) & 1) && now_ns() - from < DRAIN_NS) {}
+    }
+    if (tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
+    __syncthreads();
+    Stretch s = line;
+    Seq q;
+    Item i;
+    i.b = -1;
+    while (next_item(a, items, s, q, i, tid == 0 ? cut.ends + blockIdx.x : nullptr)) {
+      const bool whole = i.tile0 == 0 && i.tile1 == i.tiles;
+      for (int x = tid; x < TILE * D; x += GRAD_THREADS) {
+        const int r = x / D, d = x % D, in_tile = r / a.in_group, query = i.t * items.q + in_tile;
+        if (in_tile >= items.q || query >= i.n) continue;
+        if (whole) row_at<T>(a.dq, (int64_t)i.first + query, i.kh * a.group + r - in_tile * a.group)[d] = narrow<T>(NAN);
+        else cut.o[(((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * TILE + r) * D + d] = NAN;
+      }
+    }
+  }
+  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+}
+
+// Sums of the parts of items that were cut, in their order: a warp for each row.
+template <typename T, int D, bool BY_KEYS>
+__global__ void __launch_bounds__(JOIN_WARPS * 32) k_join_grad(const Args a, const Items<BY_KEYS> items, const Cut cut, const float *largest) {
+  wait_for_kernels_before();
+  constexpr int ROWS = BY_KEYS ? 2 * TILE : TILE, E = D / 32;
+  using V = typename std::conditional<E == 2, float2, float4>::type;
+  const int c = blockIdx.x / JOIN_BLOCKS, lane = threadIdx.x % 32;
+  const int4 end = cut.ends[c];
+  if (end.x < 0) return;
+  float most = 0.f;
+  int e = 0;
+  if (std::is_same<T, __half>::value) {
+    for (int i = lane; i < DELTA_BLOCKS; i += 32) most = fmaxf(most, largest[i]);
+#pragma unroll
+    for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+    if (most > 0.f) frexpf(most, &e);
+  }
+  const Seq s = sequence(a, end.x);
+#pragma unroll 1
+  for (int r = blockIdx.x % JOIN_BLOCKS * JOIN_WARPS + threadIdx.x / 32; r < ROWS; r += JOIN_BLOCKS * JOIN_WARPS) {
+    T *dst;
+    float f = ldexpf(a.scale, e);
+    if (BY_KEYS) {
+      const int key = end.z * TILE + r % TILE;
+      if (key >= s.n) continue;
+      dst = row_at<T>(r < TILE ? a.dv : a.dk, (int64_t)s.first + key, end.y);
+      if (r < TILE) f = WEIGHT_UNIT<T>;
+    } else {
+      const int in_tile = r / a.in_group, query = end.z * items.q + in_tile;
+      if (in_tile >= items.q || query >= s.n) continue;
+      dst = row_at<T>(a.dq, (int64_t)s.first + query, end.y * a.group + r - in_tile * a.group);
+    }
+    float acc[E] = {};
+    for (int x = 0; x <= end.w; x += 4) {
+      V v[4];
+#pragma unroll
+      for (int k = 0; k < 4; k++)
+        if (x + k <= end.w) v[k] = ((const V *)(cut.o + (((int64_t)(c + x + k) * 2 + (x + k == 0)) * ROWS + r) * D))[lane];
+#pragma unroll
+      for (int k = 0; k < 4; k++) {
+        if (x + k <= end.w) {
+#pragma unroll
+          for (int y = 0; y < E; y++) acc[y] += ((const float *)&v[k])[y];
+        }
+      }
+    }
+#pragma unroll
+    for (int y = 0; y < E; y++) dst[lane * E + y] = narrow<T>(acc[y] * f);
+  }
+}
+
+// Rows that TMA cannot take as they lie, side by side.
+template <typename T>
+__global__ void __launch_bounds__(256) k_side_by_side(const Args a, const Heads from, T *to, int heads, int dim) {
+  const int64_t all = (int64_t)a.n_tokens * heads * dim;
+  for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < all; x += (int64_t)gridDim.x * 256) {
+    const int64_t row = x / (heads * dim);
+    const int in = (int)(x - row * heads * dim);
+    to[x] = row_at<const T>(from, row, in / dim)[in % dim];
+  }
 }
 
 // ---------------------------------------------------------------- host side
-unsigned blocks_for(int64_t rows) { return (unsigned)((rows + WARPS - 1) / WARPS); }
+// The forward pass's workspace.
+size_t plan(Cut &c, int dim, int queries, char *at) {
+  size_t n = 0;
+  auto take = [&](size_t bytes) {
+    char *x = at ? at + n : nullptr;
+    n += up(bytes);
+    return x;
+  };
+  c.blocks = SMS, c.queries = queries;
+  c.ends = (int4 *)take(SMS * sizeof(int4));
+  c.ml = (float2 *)take((size_t)SMS * 2 * 256 * sizeof(float2));
+  c.o = (float *)take((size_t)SMS * 2 * 256 * dim * sizeof(float));
+  return n;
+}
 
-template <typename T, int D> void forward(const Args &a, cudaStream_t s) {
-  k_forward<T, D><<<blocks_for((int64_t)a.n_tokens * a.q_heads), WARPS * 32, 0, s>>>(a);
+template <typename T, int D>
+cudaError_t forward(const Args &a, const Pages &maps, char *workspace, cudaStream_t s) {
+  static std::atomic<uint64_t> granted{0};
+  cudaError_t e = grant(k_forward<T, D>, Fwd<D>::SMEM, granted);
+  if (e != cudaSuccess) return e;
+  Cut cut;
+  const Items<false> items = {2 * (128 / a.group), a.causal};
+  plan(cut, D, items.q, workspace);
+  e = launch_kernel(k_forward<T, D>, cut.blocks, FWD_THREADS, Fwd<D>::SMEM, s, false, a, items, cut, maps);
+  return e != cudaSuccess ? e : launch_kernel(k_join<T, D>, cut.blocks * JOIN_BLOCKS, JOIN_WARPS * 32, 0, s, true, a, items, cut);
 }
-template <typename T, int D> void backward(const Args &a, cudaStream_t s) {
-  k_grad_q<T, D><<<blocks_for((int64_t)a.n_tokens * a.q_heads), WARPS * 32, 0, s>>>(a);
-  k_grad_kv<T, D><<<blocks_for((int64_t)a.n_tokens * a.kv_heads), WARPS * 32, 0, s>>>(a);
+cudaError_t run_forward(const Args &a, const Pages &maps, int32_t dtype, uint32_t dim, void *workspace, cudaStream_t s) {
+  char *const w = (char *)workspace;
+  if (dtype == GTS_BF16) return dim == 64 ? forward<__nv_bfloat16, 64>(a, maps, w, s) : forward<__nv_bfloat16, 128>(a, maps, w, s);
+  return dim == 64 ? forward<__half, 64>(a, maps, w, s) : forward<__half, 128>(a, maps, w, s);
 }
-cudaError_t run(const Args &a, int32_t dtype, uint32_t dim, bool grad, cudaStream_t s) {
-  if (dtype == GTS_BF16) {
-    if (dim == 64) grad ? backward<__nv_bfloat16, 64>(a, s) : forward<__nv_bfloat16, 64>(a, s);
-    else grad ? backward<__nv_bfloat16, 128>(a, s) : forward<__nv_bfloat16, 128>(a, s);
-  } else {
-    if (dim == 64) grad ? backward<__half, 64>(a, s) : forward<__half, 64>(a, s);
-    else grad ? backward<__half, 128>(a, s) : forward<__half, 128>(a, s);
+
+// Maps of rows of queries: boxes of a key head's `group` heads of `queries` tokens.
+bool rows_map(CUtensorMap &map, const Heads &h, int heads, int tokens, int dim, int group, int queries, bool bf16) {
+  int64_t head = heads == 1 ? h.tok : h.head, tok = tokens == 1 ? head * heads : h.tok;
+  if (heads == 1 && tokens == 1) head = tok = dim;
+  if ((uintptr_t)h.data % 16 || head % 8 || head < dim || tok < head || tok % head || tok >= 1ll << 38) return false;
+  const EncodeTiled encode = encode_tiled();
+  if (!encode) return false;
+  const cuuint64_t dims[4] = {(cuuint64_t)dim, (cuuint64_t)heads, (cuuint64_t)tokens, 1};
+  const cuuint64_t strides[3] = {(cuuint64_t)head * 2, (cuuint64_t)tok * 2, (cuuint64_t)tok * 2 * (cuuint64_t)tokens};
+  const cuuint32_t boxes[4] = {64, (cuuint32_t)group, (cuuint32_t)queries, 1}, ones[4] = {1, 1, 1, 1};
+  return strides[2] < 1ull << 40 && encode(&map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, (void *)h.data, dims, strides, boxes, ones,
+                                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The gradients' workspace: e of every row, each block's largest |dout|, partial results, and q, dout, k, v where TMA cannot take
+// them as they lie.
+struct GradPlan {
+  float *delta, *largest;
+  Cut cut;
+  char *copy[4];
+  size_t bytes;
+};
+GradPlan plan_grad(const gts_prompt_grad_desc &d, const bool (&copied)[4], char *at) {
+  const gts_prompt_desc &f = d.forward;
+  GradPlan p = {};
+  auto take = [&](size_t bytes) {
+    char *x = at ? at + p.bytes : nullptr;
+    p.bytes += up(bytes);
+    return x;
+  };
+  p.delta = (float *)take((size_t)f.n_tokens * f.q_heads * sizeof(float));
+  p.largest = (float *)take(DELTA_BLOCKS * sizeof(float));
+  p.cut.blocks = SMS;
+  p.cut.ends = (int4 *)take(SMS * sizeof(int4));
+  p.cut.o = (float *)take((size_t)SMS * 2 * 2 * TILE * f.head_dim * sizeof(float));
+  for (int i = 0; i < 4; i++)
+    if (copied[i]) p.copy[i] = take((size_t)f.n_tokens * (i < 2 ? f.q_heads : f.kv_heads) * f.head_dim * 2);
+  return p;
+}
+
+void packed_maps(Pages &p, const gts_prompt_desc &d);
+
+// The maps, and which of q, dout, k and v have to be copied for theirs.
+void grad_maps(GradMaps &m, const gts_prompt_grad_desc &d, bool (&copied)[4]) {
+  const gts_prompt_desc &f = d.forward;
+  const int group = (int)(f.q_heads / f.kv_heads);
+  const bool bf16 = f.dtype == GTS_BF16;
+  auto rows = [&](CUtensorMap &map, const gts_heads &h) {
+    return rows_map(map, {h.data, h.token_stride, h.head_stride}, (int)f.q_heads, (int)f.n_tokens, (int)f.head_dim, group, TILE / group, bf16);
+  };
+  copied[0] = !rows(m.q, f.q), copied[1] = !rows(m.dout, d.dout);
+  packed_maps(m.kv, f);
+  copied[2] = copied[3] = !m.kv.box;
+}
+
+template <typename T, int D>
+cudaError_t backward(const Args &a, const GradPlan &p, const GradMaps &maps, cudaStream_t s) {
+  static std::atomic<uint64_t> granted_kv{0}, granted_q{0};
+  cudaError_t e = grant(k_grad_kv<T, D>, GradKv<D>::SMEM, granted_kv);
+  if (e == cudaSuccess) e = grant(k_grad_q<T, D>, GradQ<D>::SMEM, granted_q);
+  if (e != cudaSuccess) return e;
+  const int queries = TILE / a.group;
+  const Items<true> by_keys = {queries, a.causal};
+  const Items<false> by_rows = {queries, a.causal};
+  const float *const largest = p.largest;
+  e = launch_kernel(k_delta<T, D>, DELTA_BLOCKS, DELTA_THREADS, 0, s, false, a, p.largest);
+  if (e == cudaSuccess) e = launch_kernel(k_grad_kv<T, D>, SMS, GRAD_THREADS, GradKv<D>::SMEM, s, false, a, by_keys, p.cut, largest, maps);
+  if (e == cudaSuccess) e = launch_kernel(k_join_grad<T, D, true>, SMS * JOIN_BLOCKS, JOIN_WARPS * 32, 0, s, true, a, by_keys, p.cut, largest);
+  if (e == cudaSuccess) e = launch_kernel(k_grad_q<T, D>, SMS, GRAD_THREADS, GradQ<D>::SMEM, s, false, a, by_rows, p.cut, largest, maps);
+  if (e == cudaSuccess) e = launch_kernel(k_join_grad<T, D, false>, SMS * JOIN_BLOCKS, JOIN_WARPS * 32, 0, s, true, a, by_rows, p.cut, largest);
+  return e;
+}
+
+template <typename T> cudaError_t side_by_side(const Args &a, Heads &h, int heads, int dim, char *to, cudaStream_t s) {
+  const Heads from = h;
+  const int64_t all = (int64_t)a.n_tokens * heads * dim;
+  const cudaError_t e = launch_kernel(k_side_by_side<T>, (unsigned)std::min<int64_t>(SMS * 8, (all + 255) / 256), 256, 0, s, false, a, from, (T *)to, heads, dim);
+  h = {to, (int64_t)heads * dim, dim};
+  return e;
+}
+
+template <typename T>
+cudaError_t run_grad(Args a, const GradPlan &p, GradMaps &maps, const gts_prompt_grad_desc &d, cudaStream_t s) {
+  const int dim = (int)d.forward.head_dim;
+  gts_prompt_grad_desc c = d;
+  Heads *const from[4] = {&a.q, &a.dout, &a.k, &a.v};
+  gts_heads *const to[4] = {&c.forward.q, &c.dout, &c.forward.k, &c.forward.v};
+  bool any = false;
+  for (int i = 0; i < 4; i++) {
+    if (!p.copy[i]) continue;
+    const cudaError_t e = side_by_side<T>(a, *from[i], i < 2 ? a.q_heads : a.kv_heads, dim, p.copy[i], s);
+    if (e != cudaSuccess) return e;
+    *to[i] = {(void *)from[i]->data, from[i]->tok, from[i]->head};
+    any = true;
   }
-  return cudaGetLastError();
+  if (any) {
+    bool copied[4];
+    grad_maps(maps, c, copied);
+    if (copied[0] || copied[1] || copied[2]) return cudaErrorInvalidValue;
+  }
+  return dim == 64 ? backward<T, 64>(a, p, maps, s) : backward<T, 128>(a, p, maps, s);
 }
 
 // What all of these calls refuse.
@@ -232,11 +1909,20 @@ Args args(const gts_prompt_desc &d) {
   a.q = heads(d.q), a.k = heads(d.k), a.v = heads(d.v), a.out = heads(d.out);
   a.lse = d.lse, a.starts = d.starts;
   a.n_seqs = (int)d.n_seqs, a.n_tokens = (int)d.n_tokens, a.q_heads = (int)d.q_heads, a.kv_heads = (int)d.kv_heads;
-  a.group = a.q_heads / a.kv_heads, a.causal = (int)d.causal, a.zero_rest = (int)d.zero_rest;
+  a.group = a.q_heads / a.kv_heads, a.in_group = divisor(a.group), a.causal = (int)d.causal, a.zero_rest = (int)d.zero_rest;
   a.scale = d.scale, a.status = d.d_status;
   return a;
 }
-size_t up(size_t x) { return (x + 255) / 256 * 256; }
+
+// Maps of packed keys and values: one page of all tokens.
+void packed_maps(Pages &p, const gts_prompt_desc &d) {
+  gts_cache c = {};
+  c.n_pages = 1, c.page_size = d.n_tokens, c.kv_heads = d.kv_heads, c.head_dim = d.head_dim, c.dtype = d.dtype;
+  p.box = TILE;
+  if (!tile_map(p.k, p.k_heads_first, TILE, c, d.k.data, 0, d.k.token_stride, d.k.head_stride) ||
+      !tile_map(p.v, p.v_heads_first, TILE, c, d.v.data, 0, d.v.token_stride, d.v.head_stride))
+    p.box = 0;
+}
 
 const char *refuse_shape(const gts_chunk_desc &d) {
   const gts_cache &c = d.cache;
@@ -250,7 +1936,10 @@ const char *refuse_shape(const gts_chunk_desc &d) {
 
 }  // namespace
 
-extern "C" size_t gts_prompt_workspace_bytes(const gts_prompt_desc *d) { return !d || refuse_shape(*d) ? 0 : 256; }
+extern "C" size_t gts_prompt_workspace_bytes(const gts_prompt_desc *d) { 
+  Cut c;
+  return !d || refuse_shape(*d) ? 0 : plan(c, (int)d->head_dim, 0, nullptr);
+}
 
 extern "C" gts_status gts_prompt_attention(const gts_prompt_desc *d, void *stream) {
   gts::clear_error();
@@ -260,12 +1949,18 @@ extern "C" gts_status gts_prompt_attention(const gts_prompt_desc *d, void *strea
   if (const char *why = refuse_call(*d, false)) return gts::fail(GTS_ERR_INVALID_ARG, why);
   if (d->workspace_bytes < gts_prompt_workspace_bytes(d))
     return gts::fail(GTS_ERR_NOMEM, "attention: workspace smaller than gts_prompt_workspace_bytes");
-  const cudaError_t e = run(args(*d), d->dtype, d->head_dim, false, (cudaStream_t)stream);
+  Pages maps = {};
+  packed_maps(maps, *d);
+  const cudaError_t e = run_forward(args(*d), maps, d->dtype, d->head_dim, d->workspace, (cudaStream_t)stream);
   return e == cudaSuccess ? GTS_OK : gts::cuda_fail(e, "attention: launch");
 }
 
 extern "C" size_t gts_prompt_grad_workspace_bytes(const gts_prompt_grad_desc *d) {
-  return !d || refuse_shape(d->forward) ? 0 : up((size_t)d->forward.n_tokens * d->forward.q_heads * 4) + 256;
+  if (!d || refuse_shape(d->forward)) return 0;
+  GradMaps maps = {};
+  bool copied[4];
+  grad_maps(maps, *d, copied);
+  return plan_grad(*d, copied, nullptr).bytes;
 }
 
 extern "C" gts_status gts_prompt_attention_grad(const gts_prompt_grad_desc *d, void *stream) {
@@ -279,16 +1974,22 @@ extern "C" gts_status gts_prompt_attention_grad(const gts_prompt_grad_desc *d, v
     return gts::fail(GTS_ERR_INVALID_ARG, "attention: null lse, dout, dq, dk or dv");
   if (misaligned(d->dout) || misaligned(d->dq) || misaligned(d->dk) || misaligned(d->dv) || (uintptr_t)d->dlse % 4)
     return gts::fail(GTS_ERR_INVALID_ARG, "attention: tensor misaligned for its type");
-  if (f.workspace_bytes < gts_prompt_grad_workspace_bytes(d))
-    return gts::fail(GTS_ERR_NOMEM, "attention: workspace smaller than gts_prompt_grad_workspace_bytes");
+  GradMaps maps = {};
+  bool copied[4];
+  grad_maps(maps, *d, copied);
+  const GradPlan p = plan_grad(*d, copied, (char *)f.workspace);
+  if (f.workspace_bytes < p.bytes) return gts::fail(GTS_ERR_NOMEM, "attention: workspace smaller than gts_prompt_grad_workspace_bytes");
   Args a = args(f);
   a.dout = heads(d->dout), a.dq = heads(d->dq), a.dk = heads(d->dk), a.dv = heads(d->dv);
-  a.dlse = d->dlse, a.delta = (float *)f.workspace;
-  const cudaError_t e = run(a, f.dtype, f.head_dim, true, (cudaStream_t)stream);
+  a.dlse = d->dlse, a.delta = p.delta;
+  const cudaError_t e = f.dtype == GTS_BF16 ? run_grad<__nv_bfloat16>(a, p, maps, *d, (cudaStream_t)stream) : run_grad<__half>(a, p, maps, *d, (cudaStream_t)stream);
   return e == cudaSuccess ? GTS_OK : gts::cuda_fail(e, "attention: launch");
 }
 
-extern "C" size_t gts_chunk_workspace_bytes(const gts_chunk_desc *d) { return !d || refuse_shape(*d) ? 0 : 256; }
+extern "C" size_t gts_chunk_workspace_bytes(const gts_chunk_desc *d) { 
+  Cut c;
+  return !d || refuse_shape(*d) ? 0 : plan(c, (int)d->cache.head_dim, 0, nullptr);
+}
 
 extern "C" gts_status gts_chunk_attention(const gts_chunk_desc *d, void *stream) {
   gts::clear_error();
@@ -312,9 +2013,11 @@ extern "C" gts_status gts_chunk_attention(const gts_chunk_desc *d, void *stream)
   a.k_page = c.k_page_stride, a.v_page = c.v_page_stride;
   a.lse = d->lse, a.starts = d->starts, a.lens = d->lens, a.table = d->page_table;
   a.n_seqs = (int)d->n_seqs, a.n_tokens = (int)d->n_tokens, a.q_heads = (int)d->q_heads, a.kv_heads = (int)c.kv_heads;
-  a.group = a.q_heads / a.kv_heads, a.causal = 1, a.zero_rest = (int)d->zero_rest, a.paged = 1;
-  a.n_pages = (int)c.n_pages, a.page_size = (int)c.page_size, a.max_pages = (int)d->max_pages;
+  a.group = a.q_heads / a.kv_heads, a.in_group = divisor(a.group), a.causal = 1, a.zero_rest = (int)d->zero_rest, a.paged = 1;
+  a.n_pages = (int)c.n_pages, a.page_size = (int)c.page_size, a.max_pages = (int)d->max_pages, a.in_page = divisor(a.page_size);
   a.scale = d->scale, a.status = d->d_status;
-  const cudaError_t e = run(a, c.dtype, c.head_dim, false, (cudaStream_t)stream);
+  Pages maps = {};
+  tile_maps(maps, c, TILE);
+  const cudaError_t e = run_forward(a, maps, c.dtype, c.head_dim, d->workspace, (cudaStream_t)stream);
   return e == cudaSuccess ? GTS_OK : gts::cuda_fail(e, "attention: launch");
 }
