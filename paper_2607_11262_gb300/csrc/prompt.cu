@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
   extern __shared__ unsigned char smem_raw[];
   unsigned char *const qs = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023), *const ring = qs + Fwd<D>::Q;
   uint64_t *const bars = (uint64_t *)(ring + STAGES * BYTES);
-  constexpr int BARS = 2 * STAGES + 4 + 2 + 2 + 2 + 4 + 2 + 2 + 2 + 2 * QUEUE + 2;
+  constexpr int BARS = 8 + STAGES + 4 + 2 + 2 + 2 + 4 + 2 + 2 + 2 + 2 * QUEUE + 2;
   Item *const queue = (Item *)(bars + BARS);
   uint32_t *const bad_rows = (uint32_t *)(queue + QUEUE);                               // [4][4]: of the last tiles of values
   uint32_t *const tmem_at = bad_rows + 16;
@@ -352,9 +352,10 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
   static_assert(BARS * 8 + QUEUE * sizeof(Item) + 16 * 4 + 8 <= 768, "room behind the ring");
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), q_at = smem_u32(qs), ring_at = smem_u32(ring);
-  auto full = [&](int s) { return bar0 + s * 8; };
-  auto empty = [&](int s) { return bar0 + (STAGES + s) * 8; };
-  constexpr int B0 = 2 * STAGES;
+  // a ring of barriers for keys and one for values: who waits for either sees each of its phases
+  auto full = [&](int slot) { return bar0 + (slot % 2 * 4 + slot / 2 % 4) * 8; };
+  auto empty = [&](int s) { return bar0 + (8 + s) * 8; };
+  constexpr int B0 = 8 + STAGES;
   auto ready = [&](uint32_t v) { return bar0 + (B0 + v % 4) * 8; };                     // the v-th tile of values is clean
   auto q_full = [&](int h) { return bar0 + (B0 + 4 + h) * 8; };
   auto q_empty = [&](int h) { return bar0 + (B0 + 6 + h) * 8; };
@@ -377,7 +378,8 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
   if (tid == 0) cut.ends[blockIdx.x] = make_int4(NOTHING, 0, 0, 0);
   if (line.x0 >= line.x1) return;
   if (tid == 0) {
-    for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(empty(s), 2);
+    for (int s = 0; s < 8; s++) bar_init(full(s), 1);
+    for (int s = 0; s < STAGES; s++) bar_init(empty(s), 2);
     for (int v = 0; v < 4; v++) bar_init(ready(v), 1);
     for (int h = 0; h < 2; h++) {
       bar_init(q_full(h), 32), bar_init(q_empty(h), 1), bar_init(s_full(h), 1), bar_init(p_full(h, 0), 128), bar_init(p_full(h, 1), 128);
@@ -454,14 +456,14 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
               const int st = copies % STAGES;
               if (copies >= STAGES) need_all(empty(st), copies / STAGES - 1);
               if (!alive) break;
-              if (lane == 0) bar_expect(full(st), bytes);
+              if (lane == 0) bar_expect(full(copies), bytes);
               __syncwarp();
               if (live) {
                 const bool heads_first = kv ? maps.v_heads_first : maps.k_heads_first;
 #pragma unroll
                 for (int x = 0; x < D / 64; x++)
                   tile_load(ring_at + st * BYTES + x * COLUMNS + lane * maps.box * 128, kv ? &maps.v : &maps.k, x * 64, heads_first ? i.kh : token,
-                            heads_first ? token : i.kh, page, full(st));
+                            heads_first ? token : i.kh, page, full(copies));
               }
             }
           }
@@ -500,7 +502,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
                 asm volatile("cp.async.wait_group 1;" ::: "memory");
                 landed();
               }
-              landing = st;
+              landing = slot;
             }
           }
           asm volatile("cp.async.wait_all;" ::: "memory");
@@ -536,7 +538,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
         const int clear = seen_by_all(a, i, i.t * items.q);
         for (int t = i.tile0; t < i.tile1 && alive; t++, tiles++) {
           const int slot = 2 * tiles + 1, st = slot % STAGES;
-          need_all(full(st), slot / STAGES);
+          need_all(full(slot), slot / 8);
           if (!alive) break;
           uint32_t bad[4] = {0, 0, 0, 0};
           if ((t + 1) * TILE > clear) {
@@ -580,7 +582,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
         take();
         if (x.count) {
           need(q_full(h), items_done);
-          need(full(slot % STAGES), slot / STAGES);
+          need(full(slot), slot / 8);
           if (!alive) break;
           tc_after();
           qk(slot++);
@@ -591,7 +593,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           const uint32_t sv = slot++, sk = slot;
           const int seen = x.seen - (i.tile0 + j) * TILE;
           need(ready(tiles), tiles / 4);
-          if (j + 1 < x.count) need(full(sk % STAGES), sk / STAGES), slot++;
+          if (j + 1 < x.count) need(full(sk), sk / 8), slot++;
           if (j == 0 && items_done) need(o_free(h), items_done - 1);
           if (!alive) break;
           const uint32_t *const bad = bad_rows + tiles % 4 * 4;
@@ -621,11 +623,12 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           if (j < both) bar_arrive(my_turn(!h));
         }
         if (x.count) items_done++;
-        for (int j = 2 * x.count; j < 2 * n && alive; j++, slot++) {   // tiles that are only the other half's pass by
-          need(full(slot % STAGES), slot / STAGES);
-          if (alive) bar_arrive(empty(slot % STAGES));
+        for (int j = x.count; j < n && alive; j++, tiles++) {          // tiles that are only the other half's pass by
+          need(full(slot), slot / 8);
+          if (alive) bar_arrive(empty(slot++ % STAGES));
+          need(ready(tiles), tiles / 4);
+          if (alive) bar_arrive(empty(slot++ % STAGES));
         }
-        tiles += n - x.count;
       }
     }
   } else {
@@ -815,7 +818,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
     if (warp == 9) {
 #pragma unroll 1
       for (int x = max(0, copies - STAGES); x < copies; x++)
-        while (!bar_try(full(x % STAGES), (x / STAGES) & 1) && now_ns() - from < DRAIN_NS) {}
+        while (!bar_try(full(x), (x / 8) & 1) && now_ns() - from < DRAIN_NS) {}
     }
     if (tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
     __syncthreads();
@@ -1407,18 +1410,19 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
   extern __shared__ unsigned char smem_raw[];
   unsigned char *const rows = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023), *const ring = rows + 2 * BYTES;
   uint64_t *const bars = (uint64_t *)(ring + STAGES * BYTES);
-  constexpr int BARS = 2 * STAGES + 2 * QUEUE + 14;
+  constexpr int BARS = 8 + STAGES + 2 * QUEUE + 14;
   Item *const queue = (Item *)(bars + BARS);
   uint32_t *const tmem_at = (uint32_t *)(queue + QUEUE);
   volatile int *const dead = (volatile int *)(tmem_at + 1);
   static_assert(BARS * 8 + QUEUE * sizeof(Item) + 8 <= 768, "room behind the ring");
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), rows_at = smem_u32(rows), ring_at = smem_u32(ring);
-  auto full = [&](int s) { return bar0 + s * 8; };
-  auto empty = [&](int s) { return bar0 + (STAGES + s) * 8; };
-  auto given = [&](uint32_t i) { return bar0 + (2 * STAGES + i % QUEUE) * 8; };
-  auto taken = [&](uint32_t i) { return bar0 + (2 * STAGES + QUEUE + i % QUEUE) * 8; };
-  const uint32_t rest = bar0 + (2 * STAGES + 2 * QUEUE) * 8;
+  // a ring of barriers for keys and one for values: who waits for either sees each of its phases
+  auto full = [&](int slot) { return bar0 + (slot % 2 * 4 + slot / 2 % 4) * 8; };
+  auto empty = [&](int s) { return bar0 + (8 + s) * 8; };
+  auto given = [&](uint32_t i) { return bar0 + (8 + STAGES + i % QUEUE) * 8; };
+  auto taken = [&](uint32_t i) { return bar0 + (8 + STAGES + QUEUE + i % QUEUE) * 8; };
+  const uint32_t rest = bar0 + (8 + STAGES + 2 * QUEUE) * 8;
   const uint32_t q_full = rest, q_empty = rest + 8, dp_full = rest + 16, ds_full = rest + 24, o_full = rest + 32, o_free = rest + 40, ended = rest + 48;
   auto s_full = [&](int tile) { return rest + 56 + tile % 2 * 8; };
   auto ready = [&](int tile) { return rest + 72 + tile % 4 * 8; };                      // its keys are clean
@@ -1430,7 +1434,8 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
   if (line.x0 >= line.x1) return;
   const float factor = ds_factor<T>(largest);
   if (tid == 0) {
-    for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(empty(s), 1);
+    for (int s = 0; s < 8; s++) bar_init(full(s), 1);
+    for (int s = 0; s < STAGES; s++) bar_init(empty(s), 1);
     bar_init(q_full, 1), bar_init(q_empty, 1), bar_init(dp_full, 1), bar_init(ds_full, 256), bar_init(o_full, 1), bar_init(o_free, 256), bar_init(ended, 1);
     for (int s = 0; s < 2; s++) bar_init(s_full(s), 1);
     for (int s = 0; s < 4; s++) bar_init(ready(s), 1);
@@ -1495,10 +1500,10 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
           if (!alive) break;
           const bool heads_first = x % 2 ? maps.kv.v_heads_first : maps.kv.k_heads_first;
           if (lane == 0) {
-            bar_expect(full(st), BYTES);
+            bar_expect(full(copies), BYTES);
 #pragma unroll
             for (int c = 0; c < D / 64; c++)
-              tile_load(ring_at + st * BYTES + c * COLUMNS, x % 2 ? &maps.kv.v : &maps.kv.k, c * 64, heads_first ? i.kh : token, heads_first ? token : i.kh, 0, full(st));
+              tile_load(ring_at + st * BYTES + c * COLUMNS, x % 2 ? &maps.kv.v : &maps.kv.k, c * 64, heads_first ? i.kh : token, heads_first ? token : i.kh, 0, full(copies));
           }
           __syncwarp();
         }
@@ -1510,7 +1515,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
         const int clear = seen_by_all(a, i, i.t * items.q);
         for (int t = i.tile0; t < i.tile1 && alive; t++, tiles++) {
           const int slot = 2 * tiles;
-          need_all(full(slot % STAGES), slot / STAGES);
+          need_all(full(slot), slot / 8);
           if (!alive) break;
           if ((t + 1) * TILE > clear) {
             uint32_t bad[4];
@@ -1539,7 +1544,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
         tc_commit(s_full(tile));
       };
       auto dp = [&](int tile, bool last) {
-        need(full((2 * tile + 1) % STAGES), (2 * tile + 1) / STAGES);
+        need(full(2 * tile + 1), (2 * tile + 1) / 8);
         if (!alive) return;
         tc_after();
         P::scores(dp_at, do_op, rows_op + stage(2 * tile + 1));
@@ -1655,7 +1660,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
     if (warp == 9) {
 #pragma unroll 1
       for (int x = max(0, copies - STAGES); x < copies; x++)
-        while (!bar_try(full(x % STAGES), (x / STAGES) & 1) && now_ns() - from < DRAIN_NS) {}
+        while (!bar_try(full(x), (x / 8) & 1) && now_ns() - from < DRAIN_NS) {}
       while (q_copies && !bar_try(q_full, (q_copies - 1) & 1) && now_ns() - from < DRAIN_NS) {}
     }
     if (tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;

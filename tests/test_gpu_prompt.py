@@ -521,6 +521,29 @@ def test_backward_in_a_graph():
     assert all(torch.equal(a, b) for a, b in zip(again, want))
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("lens,H,KV,D", [([4096], 32, 8, 128), ([1024] * 8, 16, 4, 64), ([512] * 48, 12, 12, 64), ([70] * 200, 8, 8, 128)])
+def test_many_calls_on_end(lens, H, KV, D, causal):
+    """Calls one after the other, with memory busy: copies that land out of order change nothing."""
+    q, k, v, starts = problem(3, lens, H, KV, D, "bfloat16")
+    at, status = ints(starts), ints([0])
+    out, lse = serving.prompt_attention(q, k, v, at, causal=causal)
+    want = serving.prompt_attention_grad(q, q, k, v, out, lse, at, causal=causal)
+    other = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    for i in range(150):
+        if i % 3 == 0:
+            with torch.cuda.stream(side):
+                other.add_(1)
+        o, l = serving.prompt_attention(q, k, v, at, causal=causal, status=status)
+        got = serving.prompt_attention_grad(q, q, k, v, out, lse, at, causal=causal, status=status)
+        for x, y in zip((o, l, *got), (out, lse, *want)):
+            wrong += (x != y).sum()
+    torch.cuda.synchronize()
+    assert int(status) == 0 and int(wrong) == 0
+
+
 def test_beyond_32_bit_offsets():
     """Rows past 2^31 values and pages past 2^31 values, the same numbers as near ones."""
     H, KV, D, n = 64, 8, 128, 150
