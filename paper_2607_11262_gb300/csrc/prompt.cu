@@ -69,7 +69,7 @@ struct Cut {
   int blocks;
   int queries;           // of an item of rows (two halves of them); of a tile of rows
   int4 *ends;            // [blocks]: the item that begins in a block and goes on: sequence (or NOTHING), key head, item, further blocks
-  float *o;              // [blocks][2][rows of an item][D]: parts of the item that began before (0) and of the one that goes on (1)
+  float4 *o;             // [blocks][2][D / 4][rows of an item]: parts of the item that began before (0) and of the one that goes on (1)
   float2 *ml;            // [blocks][2][rows]: maximum (of log2 scores) and sum
 };
 
@@ -246,6 +246,36 @@ template <typename T> __device__ __forceinline__ uint4 gather16(const T *from) {
   return v;
 }
 
+// 32 values of a row: in pieces of 32 bytes where rows stand on that grid (half the accesses of 16, and whole sectors).
+template <typename T> __device__ __forceinline__ void store64(T *to, const uint32_t (&w)[16], bool aligned) {
+  if (aligned) {
+#pragma unroll
+    for (int y = 0; y < 16; y += 8)
+      asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 2 * y), "r"(w[y]), "r"(w[y + 1]), "r"(w[y + 2]), "r"(w[y + 3]),
+                   "r"(w[y + 4]), "r"(w[y + 5]), "r"(w[y + 6]), "r"(w[y + 7]) : "memory");
+  } else {
+#pragma unroll
+    for (int y = 0; y < 16; y++) {
+      T e[2];
+      memcpy(e, &w[y], 4);
+      to[2 * y] = e[0], to[2 * y + 1] = e[1];
+    }
+  }
+}
+__device__ __forceinline__ bool rows_aligned(const Heads &h) { return (((uintptr_t)h.data >> 1 | h.tok | h.head) & 15) == 0; }   // to 32 bytes
+
+template <typename T> __device__ __forceinline__ void store4(T *to, const float4 &v, float f, bool aligned) {
+  const uint32_t lo = pack<T>(v.x * f, v.y * f), hi = pack<T>(v.z * f, v.w * f);
+  if (aligned) {
+    *(uint2 *)to = make_uint2(lo, hi);
+  } else {
+    T e[4];
+    memcpy(e, &lo, 4), memcpy(e + 2, &hi, 4);
+#pragma unroll
+    for (int i = 0; i < 4; i++) to[i] = e[i];
+  }
+}
+
 // The row of a key, nullptr where its page is none of the cache's.
 template <typename T>
 __device__ __forceinline__ const T *key_row(const Args &a, const Heads &side, int64_t page_stride, int b, int first, int key, int kh) {
@@ -276,30 +306,34 @@ template <typename T> __device__ __forceinline__ uint32_t finite_part(uint32_t t
 // set in `bad`.
 template <typename T, int D>
 __device__ __forceinline__ void clean_tile(unsigned char *tile, int lane, int live, bool look, uint32_t (&bad)[4]) {
-  constexpr int PER = D / 8, AT_ONCE = 32 / PER;       // 16-byte pieces of a row, rows at a time
-  const int c = lane % PER, sub = lane / PER;
+  constexpr int PER = D / 8;                           // 16-byte pieces of a row
 #pragma unroll
   for (int i = 0; i < 4; i++) bad[i] = 0;
-  if (look) {
-#pragma unroll
-    for (int word = 0; word < 4; word++) {
-#pragma unroll 8
-      for (int r0 = 0; r0 < 32; r0 += AT_ONCE) {
-        const int row = word * 32 + r0 + sub;
-        uint4 *const at = (uint4 *)(tile + tile_at<128>(row, c));
-        const uint4 v = *at;
-        const bool some = (not_finite<T>(v.x) | not_finite<T>(v.y) | not_finite<T>(v.z) | not_finite<T>(v.w)) && row < live;
-        const uint32_t hit = __ballot_sync(~0u, some);
-        if (hit) {
-#pragma unroll
-          for (int k = 0; k < AT_ONCE; k++)
-            if (hit >> (k * PER) & (uint32_t)((1ull << PER) - 1)) bad[word] |= 1u << (r0 + k);
-          if (some) *at = make_uint4(finite_part<T>(v.x), finite_part<T>(v.y), finite_part<T>(v.z), finite_part<T>(v.w));
-        }
-      }
-    }
+  for (int i = max(0, live) * PER + lane; i < TILE * PER; i += 32) *(uint4 *)(tile + tile_at<128>(i / PER, i % PER)) = make_uint4(0, 0, 0, 0);
+  if (!look) return;
+  // first whether there are any, in no order
+  uint32_t any = 0;
+  __syncwarp();
+#pragma unroll 16
+  for (int i = lane; i < TILE * PER; i += 32) {
+    const uint4 v = *(const uint4 *)(tile + i * 16);
+    any |= not_finite<T>(v.x) | not_finite<T>(v.y) | not_finite<T>(v.z) | not_finite<T>(v.w);
   }
-  for (int i = max(0, live) * PER + lane; i < 128 * PER; i += 32) *(uint4 *)(tile + tile_at<128>(i / PER, i % PER)) = make_uint4(0, 0, 0, 0);
+  if (!__any_sync(~0u, any)) return;
+#pragma unroll 1
+  for (int row = 0; row < TILE; row++) {
+    bool some = false;
+    if (lane < PER) {
+      uint4 *const at = (uint4 *)(tile + tile_at<128>(row, lane));
+      const uint4 v = *at;
+      some = not_finite<T>(v.x) | not_finite<T>(v.y) | not_finite<T>(v.z) | not_finite<T>(v.w);
+      if (some) *at = make_uint4(finite_part<T>(v.x), finite_part<T>(v.y), finite_part<T>(v.z), finite_part<T>(v.w));
+    }
+    const bool hit = __any_sync(~0u, some);
+#pragma unroll
+    for (int i = 0; i < 4; i++)
+      if (hit && row / 32 == i) bad[i] |= 1u << row % 32;
+  }
 }
 
 // ---------------------------------------------------------------- forward
@@ -321,6 +355,12 @@ template <int D> struct Fwd {
   static constexpr int SMEM = Q + STAGES * BYTES + 1024 /* alignment */ + 768;
 };
 
+struct FwdMaps {
+  Pages kv;
+  CUtensorMap q;       // boxes of a key head's heads of the queries of a half
+  int has_q;
+};
+
 // An item as one half of its rows sees it.
 struct Half {
   int q0, queries, count;                              // its first query (of the sequence), how many it has, tiles of the block's stretch
@@ -339,7 +379,7 @@ __device__ __forceinline__ Half half_of(const Args &a, const Items<false> &items
 __device__ __forceinline__ int seen_by_all(const Args &a, const Item &i, int q0) { return a.causal ? max(0, i.keys - i.n + q0 + 1) : i.keys; }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const Items<false> items, const Cut cut, const __grid_constant__ Pages maps) {
+__global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const Items<false> items, const Cut cut, const __grid_constant__ FwdMaps all_maps) {
   constexpr int BYTES = Fwd<D>::BYTES, STAGES = Fwd<D>::STAGES, COLUMNS = TILE * 128;   // bytes of 64 columns of a tile
   extern __shared__ unsigned char smem_raw[];
   unsigned char *const qs = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023), *const ring = qs + Fwd<D>::Q;
@@ -352,6 +392,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
   static_assert(BARS * 8 + QUEUE * sizeof(Item) + 16 * 4 + 8 <= 768, "room behind the ring");
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), q_at = smem_u32(qs), ring_at = smem_u32(ring);
+  const Pages &maps = all_maps.kv;
   // a ring of barriers for keys and one for values: who waits for either sees each of its phases
   auto full = [&](int slot) { return bar0 + (slot % 2 * 4 + slot / 2 % 4) * 8; };
   auto empty = [&](int s) { return bar0 + (8 + s) * 8; };
@@ -382,7 +423,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
     for (int s = 0; s < STAGES; s++) bar_init(empty(s), 2);
     for (int v = 0; v < 4; v++) bar_init(ready(v), 1);
     for (int h = 0; h < 2; h++) {
-      bar_init(q_full(h), 32), bar_init(q_empty(h), 1), bar_init(s_full(h), 1), bar_init(p_full(h, 0), 128), bar_init(p_full(h, 1), 128);
+      bar_init(q_full(h), 1), bar_init(q_empty(h), 1), bar_init(s_full(h), 1), bar_init(p_full(h, 0), 128), bar_init(p_full(h, 1), 128);
       bar_init(o_full(h), 1), bar_init(o_free(h), 128), bar_init(my_turn(h), 1), bar_init(ended + 8 * h, 1);
     }
     for (int i = 0; i < QUEUE; i++) bar_init(given(i), 1), bar_init(taken(i), 11);
@@ -399,7 +440,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
   const uint32_t tmem = __shfl_sync(~0u, *tmem_at, 0);
   auto scores = [&](int h) { return tmem + h * TILE; };
   auto sums = [&](int h) { return tmem + 256 + h * 128; };
-  int copies = 0;                                      // warp 9: tiles asked for by TMA
+  int copies = 0, asked[2] = {0, 0};                   // warp 9: tiles asked for by TMA; warp 11: halves of queries
   bool issues = false;                                 // the threads that issue products
   bool alive = true;
   auto need = [&](uint32_t bar, uint32_t parity) { alive = alive && bar_wait(bar, parity & 1, dead); };
@@ -522,6 +563,16 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           if (had[h]) need_all(q_empty(h), had[h] - 1);
           had[h]++;
           if (!alive) break;
+          if (all_maps.has_q) {
+            if (lane == 0) {
+              bar_expect(q_full(h), items.q / 2 * a.group * D * 2);
+#pragma unroll
+              for (int c = 0; c < D / 64; c++) tile_load(q_at + h * BYTES + c * COLUMNS, &all_maps.q, c * 64, i.kh * a.group, i.first + x.q0, 0, q_full(h));
+            }
+            asked[h]++;
+            __syncwarp();
+            continue;
+          }
           const int rows = x.queries * a.group;
 #pragma unroll 8
           for (int y = lane; y < rows * (D / 8); y += 32) {
@@ -533,7 +584,8 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           }
           asm volatile("cp.async.wait_all;" ::: "memory");
           fence_async();
-          bar_arrive(q_full(h));
+          __syncwarp();
+          if (lane == 0) bar_arrive(q_full(h));
         }
         const int clear = seen_by_all(a, i, i.t * items.q);
         for (int t = i.tile0; t < i.tile1 && alive; t++, tiles++) {
@@ -637,7 +689,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
     const int h = warp / 4, r = tid % 128;
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
     const float sl2 = a.scale * 1.4426950408889634f;
-    const bool aligned = (((uintptr_t)a.out.data >> 1 | a.out.tok | a.out.head) & 7) == 0;
+    const bool aligned = rows_aligned(a.out);
     const int in_half = r / a.in_group, head_in = r - in_half * a.group;
     uint32_t turn = 0, items_done = 0, tiles = 0;
     Item i;
@@ -765,7 +817,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
         tc_after();
         const float inv = l == 0.f ? 0.f : 1.f / l;
         T *const dst = row_at<T>(a.out, row, kh * a.group + head_in);
-        float *const mid = cut.o + part * D;
+        float4 *const mid = cut.o + part / 256 * (D / 4) * 256 + part % 256;
 #pragma unroll 1
         for (int c = 0; c < D / 32; c++) {
           uint32_t o[32];
@@ -773,22 +825,12 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           tc_ld_wait();
           if (valid && !whole) {
 #pragma unroll
-            for (int y = 0; y < 32; y += 4) *(uint4 *)(mid + c * 32 + y) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+            for (int y = 0; y < 32; y += 4) *(uint4 *)(mid + (c * 8 + y / 4) * 256) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
           } else if (valid) {
             uint32_t w[16];
 #pragma unroll
             for (int y = 0; y < 16; y++) w[y] = pack<T>(__uint_as_float(o[2 * y]) * inv, __uint_as_float(o[2 * y + 1]) * inv);
-            if (aligned) {
-#pragma unroll
-              for (int y = 0; y < 16; y += 4) *(uint4 *)(dst + c * 32 + 2 * y) = make_uint4(w[y], w[y + 1], w[y + 2], w[y + 3]);
-            } else {
-#pragma unroll
-              for (int y = 0; y < 16; y++) {
-                T e[2];
-                memcpy(e, &w[y], 4);
-                dst[c * 32 + 2 * y] = e[0], dst[c * 32 + 2 * y + 1] = e[1];
-              }
-            }
+            store64<T>(dst + c * 32, w, aligned);
           }
           __syncwarp();
         }
@@ -820,6 +862,11 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
       for (int x = max(0, copies - STAGES); x < copies; x++)
         while (!bar_try(full(x), (x / 8) & 1) && now_ns() - from < DRAIN_NS) {}
     }
+    if (warp == 11) {
+#pragma unroll 1
+      for (int h = 0; h < 2; h++)
+        while (asked[h] && !bar_try(q_full(h), (asked[h] - 1) & 1) && now_ns() - from < DRAIN_NS) {}
+    }
     if (tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
     __syncthreads();
     // every result of the block's stretch is NaN
@@ -835,7 +882,6 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
         const int head = i.kh * a.group + r % 128 - in_half * a.group;
         if (!whole) {
           cut.ml[((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 256 + r] = make_float2(NAN, NAN);
-          for (int d = 0; d < D; d++) cut.o[(((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 256 + r) * D + d] = NAN;
         } else {
           for (int d = 0; d < D; d++) row_at<T>(a.out, i.first + query, head)[d] = narrow<T>(NAN);
           if (a.lse) a.lse[((int64_t)i.first + query) * a.q_heads + head] = NAN;
@@ -846,63 +892,58 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
-// Rows of the items that were cut: a warp each, from the block where the item begins to that where it ends.  Up to 32 parts at a
-// time, a lane takes the maximum and sum of one; then all lanes add up the parts' values, four loads in flight.
-constexpr int JOIN_BLOCKS = 8, JOIN_WARPS = 8;           // thread blocks for an item
+// Rows of the items that were cut, from the block where the item begins to that where it ends: a thread for a row and an eighth
+// of its columns, so that loads of parts cover whole lines.
+constexpr int JOIN_BLOCKS = 8, JOIN_THREADS = 256;      // thread blocks for an item of 256 rows
 template <typename T, int D>
-__global__ void __launch_bounds__(JOIN_WARPS * 32) k_join(const Args a, const Items<false> items, const Cut cut) {
+__global__ void __launch_bounds__(JOIN_THREADS) k_join(const Args a, const Items<false> items, const Cut cut) {
   wait_for_kernels_before();
-  const int c = blockIdx.x / JOIN_BLOCKS, lane = threadIdx.x % 32;
+  const int c = blockIdx.x / JOIN_BLOCKS, lane = threadIdx.x % 32, column = threadIdx.x / 32;
   const int4 end = cut.ends[c];
   if (end.x < 0) return;
+  constexpr int E = D / 32;                             // fours of columns
+  const int r = blockIdx.x % JOIN_BLOCKS * 32 + lane;
+  const int in_half = r % 128 / a.in_group, query = end.z * items.q + r / 128 * (items.q / 2) + in_half;
   const Seq s = sequence(a, end.x);
-  constexpr int E = D / 32;
-  using V = typename std::conditional<E == 2, float2, float4>::type;
-#pragma unroll 1
-  for (int r = blockIdx.x % JOIN_BLOCKS * JOIN_WARPS + threadIdx.x / 32; r < 256; r += JOIN_BLOCKS * JOIN_WARPS) {
-    const int in_half = r % 128 / a.in_group, query = end.z * items.q + r / 128 * (items.q / 2) + in_half;
-    if (in_half >= items.q / 2 || query >= s.n) continue;
-    const int head = end.y * a.group + r % 128 - in_half * a.group;
-    auto place = [&](int x) { return ((int64_t)(c + x) * 2 + (x == 0)) * 256 + r; };
-    float m = -INFINITY, l = 0.f, acc[E] = {};
-    for (int first = 0; first <= end.w; first += 32) {
-      const int x = first + lane;
-      const float2 ml = x <= end.w ? cut.ml[place(x)] : make_float2(-INFINITY, 0.f);
-      float top = fmaxf(m, ml.x);
+  if (in_half >= items.q / 2 || query >= s.n) return;
+  float m = -INFINITY, l = 0.f;
+  float4 acc[E] = {};
+  for (int x = 0; x <= end.w; x += 4) {
+    float2 ml[4];
+    float4 v[4][E];
+    int64_t part[4];
 #pragma unroll
-      for (int k = 16; k; k >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, k));
-      const float from = top == -INFINITY ? 0.f : top, keep = exp2_fast(m - from), f = exp2_fast(ml.x - from);
-      float sum = f * ml.y;
+    for (int k = 0; k < 4; k++) {
+      part[k] = (int64_t)(c + x + k) * 2 + (x + k == 0);
+      ml[k] = x + k <= end.w ? cut.ml[part[k] * 256 + r] : make_float2(-INFINITY, 0.f);
+    }
 #pragma unroll
-      for (int k = 16; k; k >>= 1) sum += __shfl_xor_sync(~0u, sum, k);
-      l = l * keep + sum, m = top;
+    for (int k = 0; k < 4; k++) {
+      if (!(ml[k].x == -INFINITY)) {                    // (a part of no tiles has no values)
 #pragma unroll
-      for (int e = 0; e < E; e++) acc[e] *= keep;
-      const uint32_t some = __ballot_sync(~0u, !(ml.x == -INFINITY));   // (a part of no tiles has no values)
-      const int count = min(32, end.w + 1 - first);
-      for (int y = 0; y < count; y += 4) {
-        V v[4];
-        float g[4];
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-          g[k] = __shfl_sync(~0u, f, (y + k) & 31);
-          if (y + k < count && some >> (y + k) & 1) v[k] = ((const V *)(cut.o + place(first + y + k) * D))[lane];
-        }
-#pragma unroll
-        for (int k = 0; k < 4; k++) {
-          if (y + k < count && some >> (y + k) & 1) {
-#pragma unroll
-            for (int e = 0; e < E; e++) acc[e] += g[k] * ((const float *)&v[k])[e];
-          }
-        }
+        for (int e = 0; e < E; e++) v[k][e] = cut.o[(part[k] * (D / 4) + column * E + e) * 256 + r];
       }
     }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    T *const dst = row_at<T>(a.out, s.first + query, head) + lane * E;
+    const float top = fmaxf(fmaxf(fmaxf(m, ml[0].x), fmaxf(ml[1].x, ml[2].x)), ml[3].x), from = top == -INFINITY ? 0.f : top, keep = exp2_fast(m - from);
+    l *= keep, m = top;
 #pragma unroll
-    for (int e = 0; e < E; e++) dst[e] = narrow<T>(acc[e] * inv);
-    if (a.lse && lane == 0) a.lse[((int64_t)s.first + query) * a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+    for (int e = 0; e < E; e++) acc[e].x *= keep, acc[e].y *= keep, acc[e].z *= keep, acc[e].w *= keep;
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+      if (!(ml[k].x == -INFINITY)) {
+        const float f = exp2_fast(ml[k].x - from);
+        l += f * ml[k].y;
+#pragma unroll
+        for (int e = 0; e < E; e++) acc[e].x += f * v[k][e].x, acc[e].y += f * v[k][e].y, acc[e].z += f * v[k][e].z, acc[e].w += f * v[k][e].w;
+      }
+    }
   }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const int head = end.y * a.group + r % 128 - in_half * a.group;
+  T *const dst = row_at<T>(a.out, (int64_t)s.first + query, head) + column * E * 4;
+#pragma unroll
+  for (int e = 0; e < E; e++) store4(dst + 4 * e, acc[e], inv, rows_aligned(a.out));
+  if (a.lse && column == 0) a.lse[((int64_t)s.first + query) * a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
 // ---------------------------------------------------------------- gradients
@@ -1002,7 +1043,7 @@ struct GradMaps { CUtensorMap q, dout; Pages kv; };
 
 // Columns of a row in tensor memory to a result, or as they are to a partial one.
 template <typename T, int COLUMNS>
-__device__ __forceinline__ void store_row(uint32_t at, T *dst, float *part, bool valid, bool aligned, float factor) {
+__device__ __forceinline__ void store_row(uint32_t at, T *dst, float4 *part, bool valid, bool aligned, float factor) {
 #pragma unroll 1
   for (int c = 0; c < COLUMNS; c += 32) {
     uint32_t o[32];
@@ -1010,27 +1051,16 @@ __device__ __forceinline__ void store_row(uint32_t at, T *dst, float *part, bool
     tc_ld_wait();
     if (valid && part) {
 #pragma unroll
-      for (int y = 0; y < 32; y += 4) *(uint4 *)(part + c + y) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+      for (int y = 0; y < 32; y += 4) *(uint4 *)(part + (c + y) / 4 * TILE) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
     } else if (valid) {
       uint32_t w[16];
 #pragma unroll
       for (int y = 0; y < 16; y++) w[y] = pack<T>(__uint_as_float(o[2 * y]) * factor, __uint_as_float(o[2 * y + 1]) * factor);
-      if (aligned) {
-#pragma unroll
-        for (int y = 0; y < 16; y += 4) *(uint4 *)(dst + c + 2 * y) = make_uint4(w[y], w[y + 1], w[y + 2], w[y + 3]);
-      } else {
-#pragma unroll
-        for (int y = 0; y < 16; y++) {
-          T e[2];
-          memcpy(e, &w[y], 4);
-          dst[c + 2 * y] = e[0], dst[c + 2 * y + 1] = e[1];
-        }
-      }
+      store64<T>(dst + c, w, aligned);
     }
     __syncwarp();
   }
 }
-__device__ __forceinline__ bool rows_aligned(const Heads &h) { return (((uintptr_t)h.data >> 1 | h.tok | h.head) & 7) == 0; }
 
 // What the two kernels' threads that issue products need: shapes of S (or dP), 128 x 128 over a head, and of products with 128
 // weights to a row, from tensor memory.  Half w of the threads writes its 64 weights to a row 64 columns after the other's.
@@ -1351,7 +1381,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
       done++;
       tc_after();
       const bool whole = i.tile0 == 0 && i.tile1 == i.tiles;
-      float *const part = whole ? nullptr : cut.o + ((((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 2 + w) * TILE + r) * D;
+      float4 *const part = whole ? nullptr : cut.o + (((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 2 + w) * (D / 4) * TILE + r;
       store_row<T, D>((w ? dk_at : dv_at) + lanes, row_at<T>(to, (int64_t)i.first + key, i.kh), part, key < i.keys, aligned,
                       w ? a.scale / factor : WEIGHT_UNIT<T>);
       tc_before();
@@ -1387,7 +1417,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
         const int w = x / (TILE * D), r = x / D % TILE, d = x % D, key = i.t * TILE + r;
         if (key >= i.keys) continue;
         if (whole) row_at<T>(w ? a.dk : a.dv, (int64_t)i.first + key, i.kh)[d] = narrow<T>(NAN);
-        else cut.o[((((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 2 + w) * TILE + r) * D + d] = NAN;
+        else if (d % 4 == 0) cut.o[((((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 2 + w) * (D / 4) + d / 4) * TILE + r] = make_float4(NAN, NAN, NAN, NAN);
       }
     }
   }
@@ -1640,7 +1670,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
       done++;
       tc_after();
       const bool whole = i.tile0 == 0 && i.tile1 == i.tiles;
-      float *const part = whole ? nullptr : cut.o + (((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * TILE + r) * D + w * (D / 2);
+      float4 *const part = whole ? nullptr : cut.o + (((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * (D / 4) + w * (D / 8)) * TILE + r;
       store_row<T, D / 2>(dq_at + lanes + w * (D / 2), row_at<T>(a.dq, row, i.kh * a.group + head_in) + w * (D / 2), part, valid, aligned, a.scale / factor);
       tc_before();
       bar_arrive(o_free);
@@ -1675,62 +1705,59 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
         const int r = x / D, d = x % D, in_tile = r / a.in_group, query = i.t * items.q + in_tile;
         if (in_tile >= items.q || query >= i.n) continue;
         if (whole) row_at<T>(a.dq, (int64_t)i.first + query, i.kh * a.group + r - in_tile * a.group)[d] = narrow<T>(NAN);
-        else cut.o[(((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * TILE + r) * D + d] = NAN;
+        else if (d % 4 == 0) cut.o[(((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * (D / 4) + d / 4) * TILE + r] = make_float4(NAN, NAN, NAN, NAN);
       }
     }
   }
   if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
-// Sums of the parts of items that were cut, in their order: a warp for each row.
+// Sums of the parts of items that were cut, in their order: a thread for a row and an eighth of its columns.
 template <typename T, int D, bool BY_KEYS>
-__global__ void __launch_bounds__(JOIN_WARPS * 32) k_join_grad(const Args a, const Items<BY_KEYS> items, const Cut cut, const float *largest) {
+__global__ void __launch_bounds__(JOIN_THREADS) k_join_grad(const Args a, const Items<BY_KEYS> items, const Cut cut, const float *largest) {
   wait_for_kernels_before();
-  constexpr int ROWS = BY_KEYS ? 2 * TILE : TILE, E = D / 32;
-  using V = typename std::conditional<E == 2, float2, float4>::type;
-  const int c = blockIdx.x / JOIN_BLOCKS, lane = threadIdx.x % 32;
+  constexpr int ROWS = BY_KEYS ? 2 * TILE : TILE, E = D / 32;   // (keys' gradients after values')
+  const int c = blockIdx.x / (ROWS / 32), lane = threadIdx.x % 32, column = threadIdx.x / 32;
   const int4 end = cut.ends[c];
   if (end.x < 0) return;
-  float most = 0.f;
-  int e = 0;
-  if (std::is_same<T, __half>::value) {
+  const Seq s = sequence(a, end.x);
+  const int row = blockIdx.x % (ROWS / 32) * 32 + lane, which = row / TILE, r = row % TILE;
+  float f = a.scale;
+  if (BY_KEYS && which == 0) {
+    f = WEIGHT_UNIT<T>;
+  } else if (std::is_same<T, __half>::value) {
+    float most = 0.f;
     for (int i = lane; i < DELTA_BLOCKS; i += 32) most = fmaxf(most, largest[i]);
 #pragma unroll
     for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+    int e = 0;
     if (most > 0.f) frexpf(most, &e);
+    f = ldexpf(f, e);
   }
-  const Seq s = sequence(a, end.x);
-#pragma unroll 1
-  for (int r = blockIdx.x % JOIN_BLOCKS * JOIN_WARPS + threadIdx.x / 32; r < ROWS; r += JOIN_BLOCKS * JOIN_WARPS) {
-    T *dst;
-    float f = ldexpf(a.scale, e);
-    if (BY_KEYS) {
-      const int key = end.z * TILE + r % TILE;
-      if (key >= s.n) continue;
-      dst = row_at<T>(r < TILE ? a.dv : a.dk, (int64_t)s.first + key, end.y);
-      if (r < TILE) f = WEIGHT_UNIT<T>;
-    } else {
-      const int in_tile = r / a.in_group, query = end.z * items.q + in_tile;
-      if (in_tile >= items.q || query >= s.n) continue;
-      dst = row_at<T>(a.dq, (int64_t)s.first + query, end.y * a.group + r - in_tile * a.group);
-    }
-    float acc[E] = {};
-    for (int x = 0; x <= end.w; x += 4) {
-      V v[4];
+  const int in_tile = BY_KEYS ? 0 : r / a.in_group, at = BY_KEYS ? end.z * TILE + r : end.z * items.q + in_tile;
+  if (at >= s.n || (!BY_KEYS && in_tile >= items.q)) return;
+  const Heads &to = !BY_KEYS ? a.dq : which ? a.dk : a.dv;
+  float4 acc[E] = {};
+  for (int x = 0; x <= end.w; x += 4) {
+    float4 v[4][E];
 #pragma unroll
-      for (int k = 0; k < 4; k++)
-        if (x + k <= end.w) v[k] = ((const V *)(cut.o + (((int64_t)(c + x + k) * 2 + (x + k == 0)) * ROWS + r) * D))[lane];
+    for (int k = 0; k < 4; k++) {
+      if (x + k <= end.w) {
 #pragma unroll
-      for (int k = 0; k < 4; k++) {
-        if (x + k <= end.w) {
-#pragma unroll
-          for (int y = 0; y < E; y++) acc[y] += ((const float *)&v[k])[y];
-        }
+        for (int e = 0; e < E; e++) v[k][e] = cut.o[((((int64_t)(c + x + k) * 2 + (x + k == 0)) * (ROWS / TILE) + which) * (D / 4) + column * E + e) * TILE + r];
       }
     }
 #pragma unroll
-    for (int y = 0; y < E; y++) dst[lane * E + y] = narrow<T>(acc[y] * f);
+    for (int k = 0; k < 4; k++) {
+      if (x + k <= end.w) {
+#pragma unroll
+        for (int e = 0; e < E; e++) acc[e].x += v[k][e].x, acc[e].y += v[k][e].y, acc[e].z += v[k][e].z, acc[e].w += v[k][e].w;
+      }
+    }
   }
+  T *const dst = row_at<T>(to, (int64_t)s.first + at, BY_KEYS ? end.y : end.y * a.group + r - in_tile * a.group) + column * E * 4;
+#pragma unroll
+  for (int e = 0; e < E; e++) store4(dst + 4 * e, acc[e], f, rows_aligned(to));
 }
 
 // Rows that TMA cannot take as they lie, side by side.
@@ -1745,38 +1772,6 @@ __global__ void __launch_bounds__(256) k_side_by_side(const Args a, const Heads 
 }
 
 // ---------------------------------------------------------------- host side
-// The forward pass's workspace.
-size_t plan(Cut &c, int dim, int queries, char *at) {
-  size_t n = 0;
-  auto take = [&](size_t bytes) {
-    char *x = at ? at + n : nullptr;
-    n += up(bytes);
-    return x;
-  };
-  c.blocks = SMS, c.queries = queries;
-  c.ends = (int4 *)take(SMS * sizeof(int4));
-  c.ml = (float2 *)take((size_t)SMS * 2 * 256 * sizeof(float2));
-  c.o = (float *)take((size_t)SMS * 2 * 256 * dim * sizeof(float));
-  return n;
-}
-
-template <typename T, int D>
-cudaError_t forward(const Args &a, const Pages &maps, char *workspace, cudaStream_t s) {
-  static std::atomic<uint64_t> granted{0};
-  cudaError_t e = grant(k_forward<T, D>, Fwd<D>::SMEM, granted);
-  if (e != cudaSuccess) return e;
-  Cut cut;
-  const Items<false> items = {2 * (128 / a.group), a.causal};
-  plan(cut, D, items.q, workspace);
-  e = launch_kernel(k_forward<T, D>, cut.blocks, FWD_THREADS, Fwd<D>::SMEM, s, false, a, items, cut, maps);
-  return e != cudaSuccess ? e : launch_kernel(k_join<T, D>, cut.blocks * JOIN_BLOCKS, JOIN_WARPS * 32, 0, s, true, a, items, cut);
-}
-cudaError_t run_forward(const Args &a, const Pages &maps, int32_t dtype, uint32_t dim, void *workspace, cudaStream_t s) {
-  char *const w = (char *)workspace;
-  if (dtype == GTS_BF16) return dim == 64 ? forward<__nv_bfloat16, 64>(a, maps, w, s) : forward<__nv_bfloat16, 128>(a, maps, w, s);
-  return dim == 64 ? forward<__half, 64>(a, maps, w, s) : forward<__half, 128>(a, maps, w, s);
-}
-
 // Maps of rows of queries: boxes of a key head's `group` heads of `queries` tokens.
 bool rows_map(CUtensorMap &map, const Heads &h, int heads, int tokens, int dim, int group, int queries, bool bf16) {
   int64_t head = heads == 1 ? h.tok : h.head, tok = tokens == 1 ? head * heads : h.tok;
@@ -1790,6 +1785,39 @@ bool rows_map(CUtensorMap &map, const Heads &h, int heads, int tokens, int dim, 
   return strides[2] < 1ull << 40 && encode(&map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, (void *)h.data, dims, strides, boxes, ones,
                                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                                            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The forward pass's workspace.
+size_t plan(Cut &c, int dim, int queries, char *at) {
+  size_t n = 0;
+  auto take = [&](size_t bytes) {
+    char *x = at ? at + n : nullptr;
+    n += up(bytes);
+    return x;
+  };
+  c.blocks = SMS, c.queries = queries;
+  c.ends = (int4 *)take(SMS * sizeof(int4));
+  c.ml = (float2 *)take((size_t)SMS * 2 * 256 * sizeof(float2));
+  c.o = (float4 *)take((size_t)SMS * 2 * 256 * dim * sizeof(float));
+  return n;
+}
+
+template <typename T, int D>
+cudaError_t forward(const Args &a, const FwdMaps &maps, char *workspace, cudaStream_t s) {
+  static std::atomic<uint64_t> granted{0};
+  cudaError_t e = grant(k_forward<T, D>, Fwd<D>::SMEM, granted);
+  if (e != cudaSuccess) return e;
+  Cut cut;
+  const Items<false> items = {2 * (128 / a.group), a.causal};
+  plan(cut, D, items.q, workspace);
+  e = launch_kernel(k_forward<T, D>, cut.blocks, FWD_THREADS, Fwd<D>::SMEM, s, false, a, items, cut, maps);
+  return e != cudaSuccess ? e : launch_kernel(k_join<T, D>, cut.blocks * JOIN_BLOCKS, JOIN_THREADS, 0, s, true, a, items, cut);
+}
+cudaError_t run_forward(const Args &a, FwdMaps &maps, int32_t dtype, uint32_t dim, void *workspace, cudaStream_t s) {
+  char *const w = (char *)workspace;
+  maps.has_q = rows_map(maps.q, a.q, a.q_heads, a.n_tokens, (int)dim, a.group, TILE / a.group, dtype == GTS_BF16);
+  if (dtype == GTS_BF16) return dim == 64 ? forward<__nv_bfloat16, 64>(a, maps, w, s) : forward<__nv_bfloat16, 128>(a, maps, w, s);
+  return dim == 64 ? forward<__half, 64>(a, maps, w, s) : forward<__half, 128>(a, maps, w, s);
 }
 
 // The gradients' workspace: e of every row, each block's largest |dout|, partial results, and q, dout, k, v where TMA cannot take
@@ -1812,7 +1840,7 @@ GradPlan plan_grad(const gts_prompt_grad_desc &d, const bool (&copied)[4], char 
   p.largest = (float *)take(DELTA_BLOCKS * sizeof(float));
   p.cut.blocks = SMS;
   p.cut.ends = (int4 *)take(SMS * sizeof(int4));
-  p.cut.o = (float *)take((size_t)SMS * 2 * 2 * TILE * f.head_dim * sizeof(float));
+  p.cut.o = (float4 *)take((size_t)SMS * 2 * 2 * TILE * f.head_dim * sizeof(float));
   for (int i = 0; i < 4; i++)
     if (copied[i]) p.copy[i] = take((size_t)f.n_tokens * (i < 2 ? f.q_heads : f.kv_heads) * f.head_dim * 2);
   return p;
@@ -1845,9 +1873,9 @@ cudaError_t backward(const Args &a, const GradPlan &p, const GradMaps &maps, cud
   const float *const largest = p.largest;
   e = launch_kernel(k_delta<T, D>, DELTA_BLOCKS, DELTA_THREADS, 0, s, false, a, p.largest);
   if (e == cudaSuccess) e = launch_kernel(k_grad_kv<T, D>, SMS, GRAD_THREADS, GradKv<D>::SMEM, s, false, a, by_keys, p.cut, largest, maps);
-  if (e == cudaSuccess) e = launch_kernel(k_join_grad<T, D, true>, SMS * JOIN_BLOCKS, JOIN_WARPS * 32, 0, s, true, a, by_keys, p.cut, largest);
+  if (e == cudaSuccess) e = launch_kernel(k_join_grad<T, D, true>, SMS * (2 * TILE / 32), JOIN_THREADS, 0, s, true, a, by_keys, p.cut, largest);
   if (e == cudaSuccess) e = launch_kernel(k_grad_q<T, D>, SMS, GRAD_THREADS, GradQ<D>::SMEM, s, false, a, by_rows, p.cut, largest, maps);
-  if (e == cudaSuccess) e = launch_kernel(k_join_grad<T, D, false>, SMS * JOIN_BLOCKS, JOIN_WARPS * 32, 0, s, true, a, by_rows, p.cut, largest);
+  if (e == cudaSuccess) e = launch_kernel(k_join_grad<T, D, false>, SMS * (TILE / 32), JOIN_THREADS, 0, s, true, a, by_rows, p.cut, largest);
   return e;
 }
 
@@ -1954,8 +1982,8 @@ extern "C" gts_status gts_prompt_attention(const gts_prompt_desc *d, void *strea
   if (const char *why = refuse_call(*d, false)) return gts::fail(GTS_ERR_INVALID_ARG, why);
   if (d->workspace_bytes < gts_prompt_workspace_bytes(d))
     return gts::fail(GTS_ERR_NOMEM, "attention: workspace smaller than gts_prompt_workspace_bytes");
-  Pages maps = {};
-  packed_maps(maps, *d);
+  FwdMaps maps = {};
+  packed_maps(maps.kv, *d);
   const cudaError_t e = run_forward(args(*d), maps, d->dtype, d->head_dim, d->workspace, (cudaStream_t)stream);
   return e == cudaSuccess ? GTS_OK : gts::cuda_fail(e, "attention: launch");
 }
@@ -2021,8 +2049,8 @@ extern "C" gts_status gts_chunk_attention(const gts_chunk_desc *d, void *stream)
   a.group = a.q_heads / a.kv_heads, a.in_group = divisor(a.group), a.causal = 1, a.zero_rest = (int)d->zero_rest, a.paged = 1;
   a.n_pages = (int)c.n_pages, a.page_size = (int)c.page_size, a.max_pages = (int)d->max_pages, a.in_page = divisor(a.page_size);
   a.scale = d->scale, a.status = d->d_status;
-  Pages maps = {};
-  tile_maps(maps, c, TILE);
+  FwdMaps maps = {};
+  tile_maps(maps.kv, c, TILE);
   const cudaError_t e = run_forward(a, maps, c.dtype, c.head_dim, d->workspace, (cudaStream_t)stream);
   return e == cudaSuccess ? GTS_OK : gts::cuda_fail(e, "attention: launch");
 }
