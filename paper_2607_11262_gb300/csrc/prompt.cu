@@ -127,11 +127,15 @@ template <bool BY_KEYS> struct Items {
 // The line of a call, and a block's walk along its stretch of it.
 struct Stretch { int64_t head, all, per, x0, x1; int b, t; int64_t pos; int kh, rest_from, rest_to; };
 
-// Where a block begins: every thread of it takes part.  rest_from, rest_to: rows of sequences are between them.
+// Where a block begins: every thread of it takes part.  rest_from, rest_to: rows of sequences are between them.  (`scratch`: SCRATCH bytes of shared memory)
+constexpr int SCRATCH = 512;
 template <bool BY_KEYS, int THREADS>
-__device__ __forceinline__ Stretch find_stretch(const Args &a, const Items<BY_KEYS> &items, int blocks) {
-  __shared__ int64_t sums[THREADS / 32], places[2];
-  __shared__ int ends[THREADS / 32][2], found[2];
+__device__ __forceinline__ Stretch find_stretch(const Args &a, const Items<BY_KEYS> &items, int blocks, void *scratch) {
+  constexpr int WARPS = THREADS / 32;
+  int64_t *const sums = (int64_t *)scratch, *const places = sums + WARPS;
+  int (*const ends)[2] = (int (*)[2])(places + 1);
+  int *const found = (int *)(ends + WARPS);
+  static_assert(WARPS * 16 + 16 <= SCRATCH, "room for the sums");
   const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
   const int each = (a.n_seqs + THREADS - 1) / THREADS, from = min(a.n_seqs, tid * each), to = min(a.n_seqs, from + each);
   int64_t mine = 0;
@@ -352,7 +356,7 @@ constexpr int FWD_THREADS = 384, QUEUE = 4;
 constexpr float RAISE = 8.f;
 template <int D> struct Fwd {
   static constexpr int BYTES = TILE * D * 2, STAGES = D == 64 ? 8 : 5, Q = 2 * BYTES;
-  static constexpr int SMEM = Q + STAGES * BYTES + 1024 /* alignment */ + 768;
+  static constexpr int BEHIND = 1280, SMEM = Q + STAGES * BYTES + BEHIND;
 };
 
 struct FwdMaps {
@@ -381,15 +385,16 @@ __device__ __forceinline__ int seen_by_all(const Args &a, const Item &i, int q0)
 template <typename T, int D>
 __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const Items<false> items, const Cut cut, const __grid_constant__ FwdMaps all_maps) {
   constexpr int BYTES = Fwd<D>::BYTES, STAGES = Fwd<D>::STAGES, COLUMNS = TILE * 128;   // bytes of 64 columns of a tile
-  extern __shared__ unsigned char smem_raw[];
-  unsigned char *const qs = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023), *const ring = qs + Fwd<D>::Q;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char *const qs = smem, *const ring = qs + Fwd<D>::Q;
   uint64_t *const bars = (uint64_t *)(ring + STAGES * BYTES);
   constexpr int BARS = 8 + STAGES + 4 + 2 + 2 + 2 + 4 + 2 + 2 + 2 + 2 * QUEUE + 2;
   Item *const queue = (Item *)(bars + BARS);
   uint32_t *const bad_rows = (uint32_t *)(queue + QUEUE);                               // [4][4]: of the last tiles of values
   uint32_t *const tmem_at = bad_rows + 16;
   volatile int *const dead = (volatile int *)(tmem_at + 1);
-  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 16 * 4 + 8 <= 768, "room behind the ring");
+  void *const scratch = (void *)(tmem_at + 2);
+  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 16 * 4 + 8 + SCRATCH <= Fwd<D>::BEHIND, "room behind the ring");
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), q_at = smem_u32(qs), ring_at = smem_u32(ring);
   const Pages &maps = all_maps.kv;
@@ -410,7 +415,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
   const uint32_t ended = bar0 + (B0 + 20 + 2 * QUEUE) * 8;
 
   dependents_may_start();
-  Stretch line = find_stretch<false, FWD_THREADS>(a, items, cut.blocks);
+  Stretch line = find_stretch<false, FWD_THREADS>(a, items, cut.blocks, scratch);
   if (line.rest_from + a.n_tokens - line.rest_to > 0) {
     if (a.zero_rest & 1) zero_rest<T>(a, a.out, a.q_heads, D, line);
     if (a.zero_rest & 2 && a.lse)
@@ -956,7 +961,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join(const Args a, const Items
 // float16 is short of small numbers: weights are held times 2^10 and ds times the power of two that puts the largest |dout| of the
 // call between 1/2 and 1 (then |ds| stays below 256 times the largest |v|, and what is lost below 2^-24 of it does not
 // count beside the largest).  bfloat16 has the range of 32 bits and needs neither.
-constexpr int GRAD_THREADS = 384, DELTA_BLOCKS = 608, DELTA_THREADS = 256;
+constexpr int ROW_WARPS = 16, ROW_THREADS = ROW_WARPS * 32, GRAD_THREADS = ROW_THREADS + 128, DELTA_BLOCKS = 1216, DELTA_THREADS = 256;
 template <typename T> constexpr float WEIGHT_SHIFT = std::is_same<T, __half>::value ? 10.f : 0.f;
 template <typename T> constexpr float WEIGHT_UNIT = std::is_same<T, __half>::value ? 0x1p-10f : 1.f;
 
@@ -1022,9 +1027,10 @@ __global__ void __launch_bounds__(DELTA_THREADS) k_delta(const Args a, float *la
 }
 
 // The power of two that ds is held times: of the largest |dout| all threads of the block look for.
-template <typename T> __device__ __forceinline__ float ds_factor(const float *largest) {
+template <typename T> __device__ __forceinline__ float ds_factor(const float *largest, void *scratch) {
   if (!std::is_same<T, __half>::value) return 1.f;
-  __shared__ float warps[GRAD_THREADS / 32];
+  float *const warps = (float *)scratch;
+  __syncthreads();
   float most = 0.f;
   for (int i = threadIdx.x; i < DELTA_BLOCKS; i += GRAD_THREADS) most = fmaxf(most, largest[i]);
 #pragma unroll
@@ -1040,6 +1046,12 @@ template <typename T> __device__ __forceinline__ float ds_factor(const float *la
 
 // Maps of the rows of queries (or of dout): a box is the `group` heads of a key head of `q` tokens; of keys and values.
 struct GradMaps { CUtensorMap q, dout; Pages kv; };
+
+__device__ __forceinline__ void tc_st16(uint32_t at, const uint32_t *r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+               "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(at) : "memory");
+}
 
 // Columns of a row in tensor memory to a result, or as they are to a partial one.
 template <typename T, int COLUMNS>
@@ -1063,7 +1075,7 @@ __device__ __forceinline__ void store_row(uint32_t at, T *dst, float4 *part, boo
 }
 
 // What the two kernels' threads that issue products need: shapes of S (or dP), 128 x 128 over a head, and of products with 128
-// weights to a row, from tensor memory.  Half w of the threads writes its 64 weights to a row 64 columns after the other's.
+// weights to a row, from tensor memory.  Quarter w of the threads writes its 32 weights to a row where its 32 scores were.
 template <typename T, int D> struct Products {
   static constexpr uint32_t TYPE = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
   static constexpr uint32_t COMMON = 1u << 4 | TYPE << 7 | TYPE << 10 | (128u >> 4) << 24;
@@ -1078,67 +1090,73 @@ template <typename T, int D> struct Products {
   }
   static __device__ __forceinline__ void sums(uint32_t to, uint32_t weights, uint32_t y, bool add) {
 #pragma unroll
-    for (int k = 0; k < 8; k++) tc_mma_t(to, weights + k / 4 * 64 + k % 4 * 8, y + k * (2048 >> 4), OPERAND_HI, SUMS, add || k > 0);
+    for (int k = 0; k < 8; k++) tc_mma_t(to, weights + k / 2 * 32 + k % 2 * 8, y + k * (2048 >> 4), OPERAND_HI, SUMS, add || k > 0);
   }
 };
 
-// Keys and values.  Warp 9 walks along the stretch and brings an item's keys and values and then its tiles of rows: queries and
-// dout by TMA.  Warps 10 and 11 clean queries and dout where some are out of sight, and bring the rows' lse and e.  Warp 8 issues the products:
+// Keys and values.  Warp 17 walks along the stretch and brings an item's keys and values and then its tiles of rows: queries and
+// dout by TMA.  Warps 18 and 19 clean queries and dout where some are out of sight, and bring the rows' lse and e.  Warp 16 issues the products:
 //   S^T = K Q^T, dP^T = V dout^T, dV += P^T dout, dK += dS^T Q
 // in the order S, dP, (dV, next S, dK, next dP), ..., so that the tensor cores have the next scores to work out while rows turn the
-// present ones into weights: nothing waits for a second buffer.  Warps 0..7: a thread for a key and half of a tile's rows.
+// present ones into weights: nothing waits for a second buffer.  Warps 0..15: a thread for a key and a quarter of a tile's rows.
 template <int D> struct GradKv {
-  static constexpr int BYTES = TILE * D * 2, STAGES = D == 64 ? 4 : 2;
-  static constexpr int SMEM = 2 * BYTES + STAGES * (2 * BYTES + 2 * TILE * 4) + 1024 + 512;
+  static constexpr int BYTES = TILE * D * 2, STAGES = D == 64 ? 8 : 5, STATS = 2;       // tiles of queries or dout; of lse and e
+  static constexpr int BEHIND = 1024, SMEM = (2 + STAGES) * BYTES + STATS * 2 * TILE * 4 + BEHIND;
 };
 
 template <typename T, int D>
 __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const Items<true> items, const Cut cut, const float *largest, const __grid_constant__ GradMaps maps) {
-  constexpr int BYTES = GradKv<D>::BYTES, STAGES = GradKv<D>::STAGES, COLUMNS = TILE * 128;
-  extern __shared__ unsigned char smem_raw[];
-  unsigned char *const kv = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023), *const ring = kv + 2 * BYTES;
-  float *const stats = (float *)(ring + STAGES * 2 * BYTES);                            // [stage][2][128]: -lse (of log2 weights), -e
-  uint64_t *const bars = (uint64_t *)(stats + STAGES * 2 * TILE);
-  constexpr int BARS = 3 * STAGES + 2 * QUEUE + 9;
+  constexpr int BYTES = GradKv<D>::BYTES, STAGES = GradKv<D>::STAGES, STATS = GradKv<D>::STATS, COLUMNS = TILE * 128;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char *const kv = smem, *const ring = kv + 2 * BYTES;
+  float *const stats = (float *)(ring + STAGES * BYTES);                                // [STATS][2][128]: -lse (of log2 weights), -e
+  uint64_t *const bars = (uint64_t *)(stats + STATS * 2 * TILE);
+  constexpr int BARS = 16 + STAGES + STATS + 2 * QUEUE + 9;
   Item *const queue = (Item *)(bars + BARS);
   uint32_t *const tmem_at = (uint32_t *)(queue + QUEUE);
   volatile int *const dead = (volatile int *)(tmem_at + 1);
-  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 8 <= 512, "room behind the ring");
+  void *const scratch = (void *)(tmem_at + 2);
+  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 8 + SCRATCH <= GradKv<D>::BEHIND, "room behind the ring");
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), kv_at = smem_u32(kv), ring_at = smem_u32(ring);
-  auto full = [&](int s) { return bar0 + s * 8; };
-  auto ready = [&](int s) { return bar0 + (STAGES + s) * 8; };
-  auto empty = [&](int s) { return bar0 + (2 * STAGES + s) * 8; };
-  auto given = [&](uint32_t i) { return bar0 + (3 * STAGES + i % QUEUE) * 8; };
-  auto taken = [&](uint32_t i) { return bar0 + (3 * STAGES + QUEUE + i % QUEUE) * 8; };
-  const uint32_t rest = bar0 + (3 * STAGES + 2 * QUEUE) * 8;
+  // slots of the ring: a tile's queries, its dout, the next one's queries, ...  Barriers are a ring for each kind, so that who waits for
+  // one sees each of its phases
+  auto full = [&](int slot) { return bar0 + (slot % 2 * 4 + slot / 2 % 4) * 8; };
+  auto ready = [&](int slot) { return bar0 + (8 + slot % 2 * 4 + slot / 2 % 4) * 8; };
+  auto empty = [&](int s) { return bar0 + (16 + s) * 8; };
+  auto read = [&](int s) { return bar0 + (16 + STAGES + s) * 8; };                      // a tile's lse and e
+  auto given = [&](uint32_t i) { return bar0 + (16 + STAGES + STATS + i % QUEUE) * 8; };
+  auto taken = [&](uint32_t i) { return bar0 + (16 + STAGES + STATS + QUEUE + i % QUEUE) * 8; };
+  const uint32_t rest = bar0 + (16 + STAGES + STATS + 2 * QUEUE) * 8;
   const uint32_t kv_full = rest, kv_empty = rest + 8, s_full = rest + 16, dp_full = rest + 24, p_full = rest + 32, ds_full = rest + 40,
                  o_full = rest + 48, o_free = rest + 56, ended = rest + 64;
 
   dependents_may_start();
-  Stretch line = find_stretch<true, GRAD_THREADS>(a, items, cut.blocks);
+  Stretch line = find_stretch<true, GRAD_THREADS>(a, items, cut.blocks, scratch);
   if (line.rest_from + a.n_tokens - line.rest_to > 0) {
     if (a.zero_rest & 2) zero_rest<T>(a, a.dk, a.kv_heads, D, line);
     if (a.zero_rest & 4) zero_rest<T>(a, a.dv, a.kv_heads, D, line);
   }
   if (tid == 0) cut.ends[blockIdx.x] = make_int4(NOTHING, 0, 0, 0);
   if (line.x0 >= line.x1) return;
-  const float factor = ds_factor<T>(largest);
+  const float factor = ds_factor<T>(largest, scratch);
   if (tid == 0) {
-    for (int s = 0; s < STAGES; s++) bar_init(full(s), 1), bar_init(ready(s), 2), bar_init(empty(s), 9);
-    bar_init(kv_full, 1), bar_init(kv_empty, 1), bar_init(s_full, 1), bar_init(dp_full, 1), bar_init(p_full, 256), bar_init(ds_full, 256);
-    bar_init(o_full, 1), bar_init(o_free, 256), bar_init(ended, 1);
-    for (int i = 0; i < QUEUE; i++) bar_init(given(i), 1), bar_init(taken(i), 11);
+    for (int s = 0; s < 8; s++) bar_init(full(s), 1), bar_init(ready(s), 1);
+    for (int s = 0; s < STAGES; s++) bar_init(empty(s), 1);
+    for (int s = 0; s < STATS; s++) bar_init(read(s), ROW_WARPS);
+    bar_init(kv_full, 1), bar_init(kv_empty, 1), bar_init(s_full, 1), bar_init(dp_full, 1), bar_init(p_full, ROW_THREADS), bar_init(ds_full, ROW_THREADS);
+    bar_init(o_full, 1), bar_init(o_free, ROW_THREADS), bar_init(ended, 1);
+    for (int i = 0; i < QUEUE; i++) bar_init(given(i), 1), bar_init(taken(i), ROW_WARPS + 3);
     *dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 8) {
+  if (warp == ROW_WARPS) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_at)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
   // rows that no box reaches (where the group does not divide 128) stay zero
   const int box_rows = items.q * a.group;
-  for (int y = tid; y < STAGES * 2 * (TILE - box_rows) * (D / 8); y += GRAD_THREADS) {
+  for (int y = tid; y < STAGES * (TILE - box_rows) * (D / 8); y += GRAD_THREADS) {
     const int c = y % (D / 8), r = y / (D / 8) % (TILE - box_rows) + box_rows, s = y / (D / 8) / (TILE - box_rows);
     *(uint4 *)(ring + s * BYTES + tile_at<128>(r, c)) = make_uint4(0, 0, 0, 0);
   }
@@ -1166,9 +1184,9 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
   auto first_query = [&](const Item &i, int tile) { return (items.first_tile(i.t) + tile) * items.q; };
   auto hides = [&](const Item &i, int q0) { return a.causal && q0 < min(i.t * TILE + TILE, i.keys) - 1; };
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (warp == 9) {
+  if (warp >= ROW_WARPS) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == ROW_WARPS + 1) {
       Stretch s = line;
       Seq q;
       Item i;
@@ -1192,25 +1210,23 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
         }
         kv_copies++;
         __syncwarp();
-        for (int t = i.tile0; t < i.tile1; t++, copies++) {
+        for (int z = 2 * i.tile0; z < 2 * i.tile1; z++, copies++) {   // queries, dout, queries, ...
           const int st = copies % STAGES;
           if (copies >= STAGES) need_all(empty(st), copies / STAGES - 1);
           if (!alive) break;
           if (lane == 0) {
-            bar_expect(full(st), 2 * box_rows * D * 2);
-            const int token = i.first + first_query(i, t);
+            bar_expect(full(copies), box_rows * D * 2);
+            const int token = i.first + first_query(i, z / 2);
 #pragma unroll
-            for (int x = 0; x < D / 64; x++) {
-              tile_load(ring_at + st * 2 * BYTES + x * COLUMNS, &maps.q, x * 64, i.kh * a.group, token, 0, full(st));
-              tile_load(ring_at + st * 2 * BYTES + BYTES + x * COLUMNS, &maps.dout, x * 64, i.kh * a.group, token, 0, full(st));
-            }
+            for (int x = 0; x < D / 64; x++)
+              tile_load(ring_at + st * BYTES + x * COLUMNS, z % 2 ? &maps.dout : &maps.q, x * 64, i.kh * a.group, token, 0, full(copies));
           }
           __syncwarp();
         }
       }
-    } else if (warp >= 10) {
+    } else if (warp >= ROW_WARPS + 2) {
       // ---- one cleans queries and brings lse, the other dout and e
-      const int which = warp - 10;
+      const int which = warp - ROW_WARPS - 2;
       const float *const src = which ? a.delta : a.lse;
       const float factor_of = which ? -factor * WEIGHT_UNIT<T> : -1.4426950408889634f, shift = which ? 0.f : WEIGHT_SHIFT<T>, none = which ? 0.f : -INFINITY;
       Item i;
@@ -1228,19 +1244,21 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
         };
         ask(i.tile0);
         for (int t = i.tile0; t < i.tile1 && alive; t++, tiles++) {
-          const int st = tiles % STAGES, q0 = first_query(i, t), live = min(items.q, i.n - q0) * a.group;
-          need_all(full(st), tiles / STAGES);
+          const int slot = 2 * tiles + which, q0 = first_query(i, t), live = min(items.q, i.n - q0) * a.group;
+          if (tiles >= STATS) need_all(read(tiles % STATS), tiles / STATS - 1);
           if (!alive) break;
 #pragma unroll
-          for (int k = 0; k < 4; k++) stats[(st * 2 + which) * TILE + lane + k * 32] = x[k];
+          for (int k = 0; k < 4; k++) stats[(tiles % STATS * 2 + which) * TILE + lane + k * 32] = x[k];
           if (t + 1 < i.tile1) ask(t + 1);
+          need_all(full(slot), slot / 8);
+          if (!alive) break;
           if (hides(i, q0) || live < box_rows) {
             uint32_t bad[4];
-            clean_tile<T, D>(ring + (st * 2 + which) * BYTES, lane, live, hides(i, q0), bad);
+            clean_tile<T, D>(ring + slot % STAGES * BYTES, lane, live, hides(i, q0), bad);
             fence_async();
           }
           __syncwarp();
-          if (lane == 0) bar_arrive(ready(st));
+          if (lane == 0) bar_arrive(ready(slot));
         }
         __syncwarp();
         if (lane == 0) bar_arrive(taken(turn_of_queue));
@@ -1251,57 +1269,56 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
       using P = Products<T, D>;
       const uint32_t k_op = operand(kv_at, 16), v_op = operand(kv_at + BYTES, 16);
       const uint32_t rows_op = operand(ring_at, 16), sums_op = operand(ring_at, COLUMNS);
-      auto stage = [&](int tile) { return (uint32_t)(tile % STAGES * 2 * BYTES) >> 4; };
+      auto stage = [&](int slot) { return (uint32_t)(slot % STAGES * BYTES) >> 4; };
       int tiles = 0;
       uint32_t done = 0;
+      auto scores = [&](int tile) {
+        need(ready(2 * tile), tile / 4);
+        if (!alive) return;
+        tc_after();
+        P::scores(s_at, k_op, rows_op + stage(2 * tile));
+        tc_commit(s_full);
+      };
+      auto dp = [&](int tile, bool last) {
+        need(ready(2 * tile + 1), tile / 4);
+        if (!alive) return;
+        tc_after();
+        P::scores(dp_at, v_op, rows_op + stage(2 * tile + 1));
+        tc_commit(dp_full);
+        if (last) tc_commit(kv_empty);
+      };
       Item i;
       while (next(i)) {
         const int n = i.tile1 - i.tile0;
         bar_arrive(taken(turn_of_queue++));
         need(kv_full, done);
-        need(ready(tiles % STAGES), tiles / STAGES);
-        if (!alive) break;
-        tc_after();
-        P::scores(s_at, k_op, rows_op + stage(tiles));
-        tc_commit(s_full);
-        P::scores(dp_at, v_op, rows_op + stage(tiles) + (BYTES >> 4));
-        tc_commit(dp_full);
-        if (n == 1) tc_commit(kv_empty);
+        if (alive) scores(tiles);
+        if (alive) dp(tiles, n == 1);
         for (int j = 0; j < n && alive; j++, tiles++) {
           need(p_full, tiles);
           if (j == 0 && done) need(o_free, done - 1);
           if (!alive) break;
           tc_after();
-          P::sums(dv_at, s_at, sums_op + stage(tiles) + (BYTES >> 4), j > 0);
-          if (j + 1 < n) {
-            need(ready((tiles + 1) % STAGES), (tiles + 1) / STAGES);
-            if (!alive) break;
-            tc_after();
-            P::scores(s_at, k_op, rows_op + stage(tiles + 1));
-            tc_commit(s_full);
-          }
+          P::sums(dv_at, s_at, sums_op + stage(2 * tiles + 1), j > 0);
+          tc_commit(empty((2 * tiles + 1) % STAGES));
+          if (j + 1 < n) scores(tiles + 1);
           need(ds_full, tiles);
           if (!alive) break;
           tc_after();
-          P::sums(dk_at, dp_at, sums_op + stage(tiles), j > 0);
-          tc_commit(empty(tiles % STAGES));
-          if (j + 1 < n) {
-            P::scores(dp_at, v_op, rows_op + stage(tiles + 1) + (BYTES >> 4));
-            tc_commit(dp_full);
-            if (j + 2 == n) tc_commit(kv_empty);
-          } else {
-            tc_commit(o_full);
-          }
+          P::sums(dk_at, dp_at, sums_op + stage(2 * tiles), j > 0);
+          tc_commit(empty(2 * tiles % STAGES));
+          if (j + 1 < n) dp(tiles + 1, j + 2 == n);
+          else tc_commit(o_full);
         }
         done++;
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
     const int w = warp / 4, r = tid % 128;
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
     const float sl2 = a.scale * 1.4426950408889634f, dp_scale = factor * WEIGHT_UNIT<T>;
-    const Heads &to = w ? a.dk : a.dv;
+    const Heads &to = w < 2 ? a.dv : a.dk;
     const bool aligned = rows_aligned(to);
     int tiles = 0;
     uint32_t done = 0;
@@ -1309,81 +1326,78 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
     while (next_all(i)) {
       const int key = i.t * TILE + r;
       for (int t = i.tile0; t < i.tile1; t++, tiles++) {
-        const int st = tiles % STAGES, q0 = first_query(i, t);
+        const int q0 = first_query(i, t);
         const bool masked = hides(i, q0);
-        const int first_seen = (key - q0) * a.group - w * 64;   // columns before it are rows that do not see this key
-        const float *const nl = stats + st * 2 * TILE + w * 64, *const ne = nl + TILE;
-        need(ready(st), tiles / STAGES);
+        const int first_seen = (key - q0) * a.group - w * 32;   // columns before it are rows that do not see this key
+        const float *const nl = stats + tiles % STATS * 2 * TILE + w * 32, *const ne = nl + TILE;
+        need(ready(2 * tiles), tiles / 4);                      // (lse)
         need(s_full, tiles);
         alive = __all_sync(~0u, alive);
         if (!alive) break;
         tc_after();
-        uint32_t p[64];
-        tc_ld(p, s_at + lanes + w * 64);
-        tc_ld(p + 32, s_at + lanes + w * 64 + 32);
+        uint32_t p[32], pk[16];
+        tc_ld(p, s_at + lanes + w * 32);
         tc_ld_wait();
         const float2 scale2 = make_float2(sl2, sl2);
-        uint32_t pk[32];
 #pragma unroll
-        for (int c = 0; c < 64; c += 4) {
+        for (int c = 0; c < 32; c += 4) {
           const float4 l = *(const float4 *)(nl + c);
           const float2 x = fma2(make_float2(__uint_as_float(p[c]), __uint_as_float(p[c + 1])), scale2, make_float2(l.x, l.y));
           const float2 y = fma2(make_float2(__uint_as_float(p[c + 2]), __uint_as_float(p[c + 3])), scale2, make_float2(l.z, l.w));
           p[c] = __float_as_uint(exp2_fast(x.x)), p[c + 1] = __float_as_uint(exp2_fast(x.y));
           p[c + 2] = __float_as_uint(exp2_fast(y.x)), p[c + 3] = __float_as_uint(exp2_fast(y.y));
         }
+        need(ready(2 * tiles + 1), tiles / 4);                  // (e)
         if (masked) {
           // (dout has lost its infinite and NaN values here: e has them, and makes NaN of the weights of rows that have some)
 #pragma unroll
-          for (int c = 0; c < 64; c++) p[c] = c < first_seen ? 0 : __float_as_uint(fmaf(0.f, ne[c], __uint_as_float(p[c])));
+          for (int c = 0; c < 32; c++) p[c] = c < first_seen ? 0 : __float_as_uint(fmaf(0.f, ne[c], __uint_as_float(p[c])));
         }
 #pragma unroll
-        for (int c = 0; c < 64; c += 2) pk[c / 2] = pack<T>(__uint_as_float(p[c]), __uint_as_float(p[c + 1]));
-        tc_st(s_at + lanes + w * 64, pk);
+        for (int c = 0; c < 32; c += 2) pk[c / 2] = pack<T>(__uint_as_float(p[c]), __uint_as_float(p[c + 1]));
+        __syncwarp();
+        tc_st16(s_at + lanes + w * 32, pk);
         tc_st_wait();
         tc_before();
         bar_arrive(p_full);
 
-        alive = __all_sync(~0u, bar_wait(dp_full, tiles & 1, dead));
+        need(dp_full, tiles);
+        alive = __all_sync(~0u, alive);
         if (!alive) break;
         tc_after();
         const float2 dp2 = make_float2(dp_scale, dp_scale);
+        uint32_t d[32];
+        tc_ld(d, dp_at + lanes + w * 32);
+        tc_ld_wait();
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-          uint32_t d[32];
-          tc_ld(d, dp_at + lanes + w * 64 + half * 32);
-          tc_ld_wait();
-#pragma unroll
-          for (int c = 0; c < 32; c += 4) {
-            const int z = half * 32 + c;
-            const float4 e = *(const float4 *)(ne + z);
-            const float2 x = fma2(make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1])), dp2, make_float2(e.x, e.y));
-            const float2 y = fma2(make_float2(__uint_as_float(d[c + 2]), __uint_as_float(d[c + 3])), dp2, make_float2(e.z, e.w));
-            float2 u = mul2(make_float2(__uint_as_float(p[z]), __uint_as_float(p[z + 1])), x);
-            float2 v = mul2(make_float2(__uint_as_float(p[z + 2]), __uint_as_float(p[z + 3])), y);
-            if (masked) {
-              u.x = z < first_seen ? 0.f : u.x, u.y = z + 1 < first_seen ? 0.f : u.y;
-              v.x = z + 2 < first_seen ? 0.f : v.x, v.y = z + 3 < first_seen ? 0.f : v.y;
-            }
-            pk[z / 2] = pack<T>(u.x, u.y), pk[z / 2 + 1] = pack<T>(v.x, v.y);
+        for (int c = 0; c < 32; c += 4) {
+          const float4 e = *(const float4 *)(ne + c);
+          const float2 x = fma2(make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1])), dp2, make_float2(e.x, e.y));
+          const float2 y = fma2(make_float2(__uint_as_float(d[c + 2]), __uint_as_float(d[c + 3])), dp2, make_float2(e.z, e.w));
+          float2 u = mul2(make_float2(__uint_as_float(p[c]), __uint_as_float(p[c + 1])), x);
+          float2 v = mul2(make_float2(__uint_as_float(p[c + 2]), __uint_as_float(p[c + 3])), y);
+          if (masked) {
+            u.x = c < first_seen ? 0.f : u.x, u.y = c + 1 < first_seen ? 0.f : u.y;
+            v.x = c + 2 < first_seen ? 0.f : v.x, v.y = c + 3 < first_seen ? 0.f : v.y;
           }
+          pk[c / 2] = pack<T>(u.x, u.y), pk[c / 2 + 1] = pack<T>(v.x, v.y);
         }
-        tc_st(dp_at + lanes + w * 64, pk);
+        tc_st16(dp_at + lanes + w * 32, pk);
         tc_st_wait();
         tc_before();
         bar_arrive(ds_full);
         __syncwarp();
-        if (lane == 0) bar_arrive(empty(st));
+        if (lane == 0) bar_arrive(read(tiles % STATS));
       }
       if (!alive) break;
-      alive = __all_sync(~0u, bar_wait(o_full, done & 1, dead));
+      need_all(o_full, done);
       if (!alive) break;
       done++;
       tc_after();
       const bool whole = i.tile0 == 0 && i.tile1 == i.tiles;
-      float4 *const part = whole ? nullptr : cut.o + (((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 2 + w) * (D / 4) * TILE + r;
-      store_row<T, D>((w ? dk_at : dv_at) + lanes, row_at<T>(to, (int64_t)i.first + key, i.kh), part, key < i.keys, aligned,
-                      w ? a.scale / factor : WEIGHT_UNIT<T>);
+      float4 *const part = whole ? nullptr : cut.o + ((((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 2 + w / 2) * (D / 4) + w % 2 * (D / 8)) * TILE + r;
+      store_row<T, D / 2>((w < 2 ? dv_at : dk_at) + lanes + w % 2 * (D / 2), row_at<T>(to, (int64_t)i.first + key, i.kh) + w % 2 * (D / 2), part, key < i.keys,
+                          aligned, w < 2 ? WEIGHT_UNIT<T> : a.scale / factor);
       tc_before();
       bar_arrive(o_free);
       __syncwarp();
@@ -1399,10 +1413,10 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
       tc_commit(ended);
       while (!bar_try(ended, 0) && now_ns() - from < DRAIN_NS) {}
     }
-    if (warp == 9) {
+    if (warp == ROW_WARPS + 1) {
 #pragma unroll 1
       for (int x = max(0, copies - STAGES); x < copies; x++)
-        while (!bar_try(full(x % STAGES), (x / STAGES) & 1) && now_ns() - from < DRAIN_NS) {}
+        while (!bar_try(full(x), (x / 8) & 1) && now_ns() - from < DRAIN_NS) {}
       while (kv_copies && !bar_try(kv_full, (kv_copies - 1) & 1) && now_ns() - from < DRAIN_NS) {}
     }
     if (tid == 0 && a.status) *a.status = GTS_ERR_STEP_LIMIT;
@@ -1421,30 +1435,31 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
       }
     }
   }
-  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  if (warp == ROW_WARPS) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
-// Queries.  Warp 9 walks along the stretch and brings an item's queries and dout and then its tiles of keys and values; warp 10 cleans
-// tiles of keys in which some are out of sight.  Warp 8 issues the products:
+// Queries.  Warp 17 walks along the stretch and brings an item's queries and dout and then its tiles of keys and values; warp 18 cleans
+// tiles of keys in which some are out of sight.  Warp 16 issues the products:
 //   S = Q K^T (in two buffers), dP = dout V^T, dQ += dS K
 // in the order (next dP, dQ, S of the tile after), so that the rows find their next scores and dP ready.  dS overwrites S.
-// Warps 0..7: a thread for a row and half of a tile's keys.
+// Warps 0..15: a thread for a row and a quarter of a tile's keys.
 template <int D> struct GradQ {
   static constexpr int BYTES = TILE * D * 2, STAGES = D == 64 ? 8 : 5;
-  static constexpr int SMEM = (2 + STAGES) * BYTES + 1024 + 768;
+  static constexpr int BEHIND = 1152, SMEM = (2 + STAGES) * BYTES + BEHIND;
 };
 
 template <typename T, int D>
 __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const Items<false> items, const Cut cut, const float *largest, const __grid_constant__ GradMaps maps) {
   constexpr int BYTES = GradQ<D>::BYTES, STAGES = GradQ<D>::STAGES, COLUMNS = TILE * 128;
-  extern __shared__ unsigned char smem_raw[];
-  unsigned char *const rows = (unsigned char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023), *const ring = rows + 2 * BYTES;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  unsigned char *const rows = smem, *const ring = rows + 2 * BYTES;
   uint64_t *const bars = (uint64_t *)(ring + STAGES * BYTES);
   constexpr int BARS = 8 + STAGES + 2 * QUEUE + 14;
   Item *const queue = (Item *)(bars + BARS);
   uint32_t *const tmem_at = (uint32_t *)(queue + QUEUE);
   volatile int *const dead = (volatile int *)(tmem_at + 1);
-  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 8 <= 768, "room behind the ring");
+  void *const scratch = (void *)(tmem_at + 2);
+  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 8 + SCRATCH <= GradQ<D>::BEHIND, "room behind the ring");
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), rows_at = smem_u32(rows), ring_at = smem_u32(ring);
   // a ring of barriers for keys and one for values: who waits for either sees each of its phases
@@ -1458,22 +1473,22 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
   auto ready = [&](int tile) { return rest + 72 + tile % 4 * 8; };                      // its keys are clean
 
   dependents_may_start();
-  Stretch line = find_stretch<false, GRAD_THREADS>(a, items, cut.blocks);
+  Stretch line = find_stretch<false, GRAD_THREADS>(a, items, cut.blocks, scratch);
   if (line.rest_from + a.n_tokens - line.rest_to > 0 && a.zero_rest & 1) zero_rest<T>(a, a.dq, a.q_heads, D, line);
   if (tid == 0) cut.ends[blockIdx.x] = make_int4(NOTHING, 0, 0, 0);
   if (line.x0 >= line.x1) return;
-  const float factor = ds_factor<T>(largest);
+  const float factor = ds_factor<T>(largest, scratch);
   if (tid == 0) {
     for (int s = 0; s < 8; s++) bar_init(full(s), 1);
     for (int s = 0; s < STAGES; s++) bar_init(empty(s), 1);
-    bar_init(q_full, 1), bar_init(q_empty, 1), bar_init(dp_full, 1), bar_init(ds_full, 256), bar_init(o_full, 1), bar_init(o_free, 256), bar_init(ended, 1);
+    bar_init(q_full, 1), bar_init(q_empty, 1), bar_init(dp_full, 1), bar_init(ds_full, ROW_THREADS), bar_init(o_full, 1), bar_init(o_free, ROW_THREADS), bar_init(ended, 1);
     for (int s = 0; s < 2; s++) bar_init(s_full(s), 1);
     for (int s = 0; s < 4; s++) bar_init(ready(s), 1);
-    for (int i = 0; i < QUEUE; i++) bar_init(given(i), 1), bar_init(taken(i), 10);
+    for (int i = 0; i < QUEUE; i++) bar_init(given(i), 1), bar_init(taken(i), ROW_WARPS + 2);
     *dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 8) {
+  if (warp == ROW_WARPS) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_at)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
@@ -1498,9 +1513,9 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
     return alive && i.tiles > 0;
   };
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (warp == 9) {
+  if (warp >= ROW_WARPS) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == ROW_WARPS + 1) {
       Stretch s = line;
       Seq q;
       Item i;
@@ -1538,7 +1553,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
           __syncwarp();
         }
       }
-    } else if (warp == 10) {
+    } else if (warp == ROW_WARPS + 2) {
       Item i;
       int tiles = 0;
       while (next_all(i)) {
@@ -1559,7 +1574,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
         if (lane == 0) bar_arrive(taken(turn_of_queue));
         turn_of_queue++;
       }
-    } else if (warp == 8 && elected()) {
+    } else if (warp == ROW_WARPS && elected()) {
       issues = true;
       using P = Products<T, D>;
       const uint32_t q_op = operand(rows_at, 16), do_op = operand(rows_at + BYTES, 16), rows_op = operand(ring_at, 16), sums_op = operand(ring_at, COLUMNS);
@@ -1606,7 +1621,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
     const int w = warp / 4, r = tid % 128, in_tile = r / a.in_group, head_in = r - in_tile * a.group;
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
     const float sl2 = a.scale * 1.4426950408889634f, dp_scale = factor * WEIGHT_UNIT<T>;
@@ -1625,41 +1640,34 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
       }
       for (int t = i.tile0; t < i.tile1; t++, tiles++) {
         const bool masked = (t + 1) * TILE > clear;
-        const int seen = limit - t * TILE - w * 64;
-        alive = __all_sync(~0u, bar_wait(s_full(tiles), tiles / 2 & 1, dead));
+        const int seen = limit - t * TILE - w * 32;
+        need_all(s_full(tiles), tiles / 2);
         if (!alive) break;
         tc_after();
-        const uint32_t at = s_at(tiles) + lanes + w * 64;
-        uint32_t p[64];
+        const uint32_t at = s_at(tiles) + lanes + w * 32;
+        uint32_t p[32], d[32], pk[16];
         tc_ld(p, at);
-        tc_ld(p + 32, at + 32);
         tc_ld_wait();
         const float2 scale2 = make_float2(sl2, sl2), nl2 = make_float2(nl, nl);
 #pragma unroll
-        for (int c = 0; c < 64; c += 2) {
+        for (int c = 0; c < 32; c += 2) {
           const float2 x = fma2(make_float2(__uint_as_float(p[c]), __uint_as_float(p[c + 1])), scale2, nl2);
           p[c] = __float_as_uint(exp2_fast(x.x)), p[c + 1] = __float_as_uint(exp2_fast(x.y));
         }
-        alive = __all_sync(~0u, bar_wait(dp_full, tiles & 1, dead));
+        need_all(dp_full, tiles);
         if (!alive) break;
         tc_after();
         const float2 dp2 = make_float2(dp_scale, dp_scale), ne2 = make_float2(ne, ne);
-        uint32_t pk[32];
+        tc_ld(d, dp_at + lanes + w * 32);
+        tc_ld_wait();
 #pragma unroll
-        for (int half = 0; half < 2; half++) {
-          uint32_t d[32];
-          tc_ld(d, dp_at + lanes + w * 64 + half * 32);
-          tc_ld_wait();
-#pragma unroll
-          for (int c = 0; c < 32; c += 2) {
-            const int z = half * 32 + c;
-            const float2 x = fma2(make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1])), dp2, ne2);
-            float2 u = mul2(make_float2(__uint_as_float(p[z]), __uint_as_float(p[z + 1])), x);
-            if (masked) u.x = z < seen ? u.x : 0.f, u.y = z + 1 < seen ? u.y : 0.f;
-            pk[z / 2] = pack<T>(u.x, u.y);
-          }
+        for (int c = 0; c < 32; c += 2) {
+          const float2 x = fma2(make_float2(__uint_as_float(d[c]), __uint_as_float(d[c + 1])), dp2, ne2);
+          float2 u = mul2(make_float2(__uint_as_float(p[c]), __uint_as_float(p[c + 1])), x);
+          if (masked) u.x = c < seen ? u.x : 0.f, u.y = c + 1 < seen ? u.y : 0.f;
+          pk[c / 2] = pack<T>(u.x, u.y);
         }
-        tc_st(at, pk);
+        tc_st16(at, pk);
         tc_st_wait();
         tc_before();
         bar_arrive(ds_full);
@@ -1670,8 +1678,10 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
       done++;
       tc_after();
       const bool whole = i.tile0 == 0 && i.tile1 == i.tiles;
-      float4 *const part = whole ? nullptr : cut.o + (((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * (D / 4) + w * (D / 8)) * TILE + r;
-      store_row<T, D / 2>(dq_at + lanes + w * (D / 2), row_at<T>(a.dq, row, i.kh * a.group + head_in) + w * (D / 2), part, valid, aligned, a.scale / factor);
+      if (w < D / 32) {
+        float4 *const part = whole ? nullptr : cut.o + (((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * (D / 4) + w * 8) * TILE + r;
+        store_row<T, 32>(dq_at + lanes + w * 32, row_at<T>(a.dq, row, i.kh * a.group + head_in) + w * 32, part, valid, aligned, a.scale / factor);
+      }
       tc_before();
       bar_arrive(o_free);
       __syncwarp();
@@ -1687,7 +1697,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
       tc_commit(ended);
       while (!bar_try(ended, 0) && now_ns() - from < DRAIN_NS) {}
     }
-    if (warp == 9) {
+    if (warp == ROW_WARPS + 1) {
 #pragma unroll 1
       for (int x = max(0, copies - STAGES); x < copies; x++)
         while (!bar_try(full(x), (x / 8) & 1) && now_ns() - from < DRAIN_NS) {}
@@ -1709,7 +1719,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
       }
     }
   }
-  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  if (warp == ROW_WARPS) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
 // Sums of the parts of items that were cut, in their order: a thread for a row and an eighth of its columns.
