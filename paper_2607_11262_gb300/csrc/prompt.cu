@@ -17,7 +17,7 @@ namespace {
 struct Heads { const void *data; int64_t tok, head; };
 
 struct Args {
-  Heads q, k, v, out, dout, dq, dk, dv;
+  Heads q, k, v, out, low, dout, dq, dk, dv;   // low: what rounding took from out
   float *lse, *delta;
   const float *dlse;
   const int32_t *starts, *lens, *table;
@@ -267,6 +267,15 @@ template <typename T> __device__ __forceinline__ void store64(T *to, const uint3
   }
 }
 __device__ __forceinline__ bool rows_aligned(const Heads &h) { return (((uintptr_t)h.data >> 1 | h.tok | h.head) & 15) == 0; }   // to 32 bytes
+
+// Two values of a word, and what their rounding took from them.
+template <typename T> __device__ __forceinline__ float2 unpack(uint32_t two);
+template <> __device__ __forceinline__ float2 unpack<__half>(uint32_t two) { return __half22float2(*(const __half2 *)&two); }
+template <> __device__ __forceinline__ float2 unpack<__nv_bfloat16>(uint32_t two) { return make_float2(__uint_as_float(two << 16), __uint_as_float(two & 0xFFFF0000u)); }
+template <typename T> __device__ __forceinline__ uint32_t pack_low(float x, float y) {
+  const float2 z = unpack<T>(pack<T>(x, y));
+  return pack<T>(x - z.x, y - z.y);
+}
 
 template <typename T> __device__ __forceinline__ void store4(T *to, const float4 &v, float f, bool aligned) {
   const uint32_t lo = pack<T>(v.x * f, v.y * f), hi = pack<T>(v.z * f, v.w * f);
@@ -694,7 +703,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
     const int h = warp / 4, r = tid % 128;
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
     const float sl2 = a.scale * 1.4426950408889634f;
-    const bool aligned = rows_aligned(a.out);
+    const bool aligned = rows_aligned(a.out), low_aligned = rows_aligned(a.low);
     const int in_half = r / a.in_group, head_in = r - in_half * a.group;
     uint32_t turn = 0, items_done = 0, tiles = 0;
     Item i;
@@ -836,6 +845,11 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
 #pragma unroll
             for (int y = 0; y < 16; y++) w[y] = pack<T>(__uint_as_float(o[2 * y]) * inv, __uint_as_float(o[2 * y + 1]) * inv);
             store64<T>(dst + c * 32, w, aligned);
+            if (a.low.data) {
+#pragma unroll
+              for (int y = 0; y < 16; y++) w[y] = pack_low<T>(__uint_as_float(o[2 * y]) * inv, __uint_as_float(o[2 * y + 1]) * inv);
+              store64<T>(row_at<T>(a.low, row, kh * a.group + head_in) + c * 32, w, low_aligned);
+            }
           }
           __syncwarp();
         }
@@ -889,6 +903,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           cut.ml[((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 256 + r] = make_float2(NAN, NAN);
         } else {
           for (int d = 0; d < D; d++) row_at<T>(a.out, i.first + query, head)[d] = narrow<T>(NAN);
+          for (int d = 0; d < D && a.low.data; d++) row_at<T>(a.low, i.first + query, head)[d] = narrow<T>(NAN);
           if (a.lse) a.lse[((int64_t)i.first + query) * a.q_heads + head] = NAN;
         }
       }
@@ -947,7 +962,15 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join(const Args a, const Items
   const int head = end.y * a.group + r % 128 - in_half * a.group;
   T *const dst = row_at<T>(a.out, (int64_t)s.first + query, head) + column * E * 4;
 #pragma unroll
-  for (int e = 0; e < E; e++) store4(dst + 4 * e, acc[e], inv, rows_aligned(a.out));
+  for (int e = 0; e < E; e++) {
+    store4(dst + 4 * e, acc[e], inv, rows_aligned(a.out));
+    if (a.low.data) {
+      const float4 x = acc[e];
+      const float2 u = unpack<T>(pack<T>(x.x * inv, x.y * inv)), v = unpack<T>(pack<T>(x.z * inv, x.w * inv));
+      store4(row_at<T>(a.low, (int64_t)s.first + query, head) + (column * E + e) * 4, make_float4(x.x * inv - u.x, x.y * inv - u.y, x.z * inv - v.x, x.w * inv - v.y), 1.f,
+             rows_aligned(a.low));
+    }
+  }
   if (a.lse && column == 0) a.lse[((int64_t)s.first + query) * a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
 }
 
@@ -985,7 +1008,8 @@ __global__ void __launch_bounds__(DELTA_THREADS) k_delta(const Args a, float *la
   }
   __syncthreads();
   const int from = ends[0], to = max(from, ends[1]);
-  const bool aligned = (((uintptr_t)a.dout.data >> 1 | (uintptr_t)a.out.data >> 1 | a.dout.tok | a.dout.head | a.out.tok | a.out.head) & 7) == 0;
+  const bool aligned = (((uintptr_t)a.dout.data >> 1 | (uintptr_t)a.out.data >> 1 | (uintptr_t)a.low.data >> 1 | a.dout.tok | a.dout.head | a.out.tok | a.out.head |
+                         a.low.tok | a.low.head) & 7) == 0;
   const int c = threadIdx.x % PER;
   float most = 0.f;
   const int64_t rows = (int64_t)(to - from) * a.q_heads;
@@ -996,13 +1020,16 @@ __global__ void __launch_bounds__(DELTA_THREADS) k_delta(const Args a, float *la
       const int64_t token = quotient(r, a.q_heads) + from;
       const int head = (int)(r - (token - from) * a.q_heads);
       const T *x = row_at<const T>(a.dout, token, head) + c * 8, *y = row_at<const T>(a.out, token, head) + c * 8;
+      const T *const z = a.low.data ? row_at<const T>(a.low, token, head) + c * 8 : nullptr;
       const uint4 u = aligned ? *(const uint4 *)x : gather16(x), v = aligned ? *(const uint4 *)y : gather16(y);
-      T e[8], f[8];
-      memcpy(e, &u, 16), memcpy(f, &v, 16);
+      uint4 l = make_uint4(0, 0, 0, 0);
+      if (z) l = aligned ? *(const uint4 *)z : gather16(z);
+      T e[8], f[8], g[8];
+      memcpy(e, &u, 16), memcpy(f, &v, 16), memcpy(g, &l, 16);
 #pragma unroll
       for (int i = 0; i < 8; i++) {
         const float w = widen(e[i]);
-        sum += w * widen(f[i]);
+        sum += w * (widen(f[i]) + widen(g[i]));
         if (isfinite(w)) most = fmaxf(most, fabsf(w));
       }
     }
@@ -1813,7 +1840,7 @@ size_t plan(Cut &c, int dim, int queries, char *at) {
 }
 
 template <typename T, int D>
-cudaError_t forward(const Args &a, const FwdMaps &maps, char *workspace, cudaStream_t s) {
+cudaError_t forward(const Args &a, const FwdMaps &maps, int64_t most_keys, char *workspace, cudaStream_t s) {
   static std::atomic<uint64_t> granted{0};
   cudaError_t e = grant(k_forward<T, D>, Fwd<D>::SMEM, granted);
   if (e != cudaSuccess) return e;
@@ -1821,13 +1848,15 @@ cudaError_t forward(const Args &a, const FwdMaps &maps, char *workspace, cudaStr
   const Items<false> items = {2 * (128 / a.group), a.causal};
   plan(cut, D, items.q, workspace);
   e = launch_kernel(k_forward<T, D>, cut.blocks, FWD_THREADS, Fwd<D>::SMEM, s, false, a, items, cut, maps);
-  return e != cudaSuccess ? e : launch_kernel(k_join<T, D>, cut.blocks * JOIN_BLOCKS, JOIN_THREADS, 0, s, true, a, items, cut);
+  if (e != cudaSuccess || most_keys <= TILE) return e;   // (items of one tile are not cut)
+  return launch_kernel(k_join<T, D>, cut.blocks * JOIN_BLOCKS, JOIN_THREADS, 0, s, true, a, items, cut);
 }
 cudaError_t run_forward(const Args &a, FwdMaps &maps, int32_t dtype, uint32_t dim, void *workspace, cudaStream_t s) {
   char *const w = (char *)workspace;
   maps.has_q = rows_map(maps.q, a.q, a.q_heads, a.n_tokens, (int)dim, a.group, TILE / a.group, dtype == GTS_BF16);
-  if (dtype == GTS_BF16) return dim == 64 ? forward<__nv_bfloat16, 64>(a, maps, w, s) : forward<__nv_bfloat16, 128>(a, maps, w, s);
-  return dim == 64 ? forward<__half, 64>(a, maps, w, s) : forward<__half, 128>(a, maps, w, s);
+  const int64_t most = a.paged ? (int64_t)a.max_pages * a.page_size : a.n_tokens;   // keys of a sequence
+  if (dtype == GTS_BF16) return dim == 64 ? forward<__nv_bfloat16, 64>(a, maps, most, w, s) : forward<__nv_bfloat16, 128>(a, maps, most, w, s);
+  return dim == 64 ? forward<__half, 64>(a, maps, most, w, s) : forward<__half, 128>(a, maps, most, w, s);
 }
 
 // The gradients' workspace: e of every row, each block's largest |dout|, partial results, and q, dout, k, v where TMA cannot take
@@ -1883,9 +1912,9 @@ cudaError_t backward(const Args &a, const GradPlan &p, const GradMaps &maps, cud
   const float *const largest = p.largest;
   e = launch_kernel(k_delta<T, D>, DELTA_BLOCKS, DELTA_THREADS, 0, s, false, a, p.largest);
   if (e == cudaSuccess) e = launch_kernel(k_grad_kv<T, D>, SMS, GRAD_THREADS, GradKv<D>::SMEM, s, false, a, by_keys, p.cut, largest, maps);
-  if (e == cudaSuccess) e = launch_kernel(k_join_grad<T, D, true>, SMS * (2 * TILE / 32), JOIN_THREADS, 0, s, true, a, by_keys, p.cut, largest);
+  if (e == cudaSuccess && a.n_tokens > queries) e = launch_kernel(k_join_grad<T, D, true>, SMS * (2 * TILE / 32), JOIN_THREADS, 0, s, true, a, by_keys, p.cut, largest);
   if (e == cudaSuccess) e = launch_kernel(k_grad_q<T, D>, SMS, GRAD_THREADS, GradQ<D>::SMEM, s, false, a, by_rows, p.cut, largest, maps);
-  if (e == cudaSuccess) e = launch_kernel(k_join_grad<T, D, false>, SMS * (TILE / 32), JOIN_THREADS, 0, s, true, a, by_rows, p.cut, largest);
+  if (e == cudaSuccess && a.n_tokens > TILE) e = launch_kernel(k_join_grad<T, D, false>, SMS * (TILE / 32), JOIN_THREADS, 0, s, true, a, by_rows, p.cut, largest);
   return e;
 }
 
@@ -1941,7 +1970,7 @@ const char *refuse_call(const gts_prompt_desc &d, bool null_ok) {
   if (!(d.scale > 0.f) || std::isinf(d.scale)) return "attention: scale must be positive";
   if (!d.starts) return "attention: null starts";
   if (!null_ok && (!d.q.data || !d.k.data || !d.v.data || !d.out.data)) return "attention: null q, k, v or out";
-  if (misaligned(d.q) || misaligned(d.k) || misaligned(d.v) || misaligned(d.out) ||
+  if (misaligned(d.q) || misaligned(d.k) || misaligned(d.v) || misaligned(d.out) || misaligned(d.low) ||
       ((uintptr_t)d.starts | (uintptr_t)d.lse | (uintptr_t)d.d_status) % 4)
     return "attention: tensor misaligned for its type";
   if (!d.workspace || (uintptr_t)d.workspace % 16) return "attention: null or misaligned workspace";
@@ -1950,6 +1979,7 @@ const char *refuse_call(const gts_prompt_desc &d, bool null_ok) {
 Args args(const gts_prompt_desc &d) {
   Args a = {};
   a.q = heads(d.q), a.k = heads(d.k), a.v = heads(d.v), a.out = heads(d.out);
+  if (d.low.data) a.low = heads(d.low);
   a.lse = d.lse, a.starts = d.starts;
   a.n_seqs = (int)d.n_seqs, a.n_tokens = (int)d.n_tokens, a.q_heads = (int)d.q_heads, a.kv_heads = (int)d.kv_heads;
   a.group = a.q_heads / a.kv_heads, a.in_group = divisor(a.group), a.causal = (int)d.causal, a.zero_rest = (int)d.zero_rest;

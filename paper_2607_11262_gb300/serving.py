@@ -83,7 +83,7 @@ class AttentionDesc(ctypes.Structure):
 class PromptDesc(ctypes.Structure):
     _fields_ = [("n_seqs", _u32), ("n_tokens", _u32), ("q_heads", _u32), ("kv_heads", _u32), ("head_dim", _u32), ("dtype", _i32),
                 ("causal", _u32), ("zero_rest", _u32), ("scale", _f32), ("starts", _vp), ("q", HeadsDesc), ("k", HeadsDesc),
-                ("v", HeadsDesc), ("out", HeadsDesc), ("lse", _vp), ("workspace", _vp), ("workspace_bytes", _sz), ("d_status", _vp)]
+                ("v", HeadsDesc), ("out", HeadsDesc), ("low", HeadsDesc), ("lse", _vp), ("workspace", _vp), ("workspace_bytes", _sz), ("d_status", _vp)]
 
 
 class PromptGradDesc(ctypes.Structure):
@@ -107,7 +107,7 @@ _HEADS_FORMAT, _ROTARY_FORMAT, _CACHE_FORMAT = "Pqq", "PIifI", "PPqqqqqqIIIIi4x"
 _ROPE = struct.Struct("@IIIIiP" + _ROTARY_FORMAT + 4 * _HEADS_FORMAT)
 _APPEND = struct.Struct("@IIPP" + _ROTARY_FORMAT + 4 * _HEADS_FORMAT + _CACHE_FORMAT + "P")
 _ATTENTION = struct.Struct("@IIIf" + 2 * "Pqqq" + "P" + _CACHE_FORMAT + "PI4xPI4xPPNP")
-_PROMPT_FORMAT = "IIIIIiIIf4xP" + 4 * _HEADS_FORMAT + "PPNP"
+_PROMPT_FORMAT = "IIIIIiIIf4xP" + 5 * _HEADS_FORMAT + "PPNP"
 _PROMPT = struct.Struct("@" + _PROMPT_FORMAT)
 _PROMPT_GRAD = struct.Struct("@" + _PROMPT_FORMAT + _HEADS_FORMAT + "P" + 3 * _HEADS_FORMAT)
 _CHUNK = struct.Struct("@IIIIf4xP" + 2 * _HEADS_FORMAT + "P" + _CACHE_FORMAT + "PI4xPPNP")
@@ -585,11 +585,11 @@ def prompt_workspace(q, k, starts, stream=None):
     """A workspace for ``prompt_attention`` calls of this shape; calls that may run at the same time need one each."""
     T, heads, dim = q.shape
     need = _load().gts_prompt_workspace_bytes(_PROMPT.pack(
-        _sequences(starts), T, heads, k.shape[1], dim, _DTYPES.get(q.dtype, -1), 0, 0, 1.0, 0, *(4 * _NO_HEADS), 0, 0, 0, 0))
+        _sequences(starts), T, heads, k.shape[1], dim, _DTYPES.get(q.dtype, -1), 0, 0, 1.0, 0, *(5 * _NO_HEADS), 0, 0, 0, 0))
     return _empty(max(int(need), 16), torch.uint8, q.device, stream)
 
 
-def _prompt_call(q, k, v, starts, causal, scale, out, lse, workspace, status, stream):
+def _prompt_call(q, k, v, starts, causal, scale, out, lse, low, workspace, status, stream):
     shape, qs, ks, vs, device, starts_at = _prompt_shape(q, k, v, starts)
     handle = _handle(stream, device)
     T, heads = shape[1:3]
@@ -598,49 +598,60 @@ def _prompt_call(q, k, v, starts, causal, scale, out, lse, workspace, status, st
     if lse is None:
         lse = _empty((T, heads), torch.float32, device, stream)
     lse_at = _index(lse, "lse", (T, heads), torch.float32, device)
+    low_at = _low(low, q, device)
     lib = _lib or _load()
     if workspace is None:
-        workspace = _workspace(None, lib.gts_prompt_workspace_bytes(_PROMPT.pack(*shape, 0, 0, 1.0, 0, *(4 * _NO_HEADS), 0, 0, 0, 0)), device,
+        workspace = _workspace(None, lib.gts_prompt_workspace_bytes(_PROMPT.pack(*shape, 0, 0, 1.0, 0, *(5 * _NO_HEADS), 0, 0, 0, 0)), device,
                                stream)
     else:
         _workspace(workspace, 0, device, stream)
     if T:
         gts._check(lib.gts_prompt_attention(_PROMPT.pack(
-            *shape, bool(causal), zero, scale, starts_at, *_heads(q, qs), *_heads(k, ks), *_heads(v, vs), *_heads(out, os), lse_at,
-            workspace.data_ptr(), workspace.nbytes, st), handle))
+            *shape, bool(causal), zero, scale, starts_at, *_heads(q, qs), *_heads(k, ks), *_heads(v, vs), *_heads(out, os), *low_at,
+            lse_at, workspace.data_ptr(), workspace.nbytes, st), handle))
     return out, lse
 
 
-class _Prompt(torch.autograd.Function):
-    @staticmethod
-    def forward(q, k, v, starts, causal, scale, status):
-        return _prompt_call(q, k, v, starts, causal, scale, None, None, None, status, None)
+def _low(low, q, device):
+    if low is None:
+        return _NO_HEADS
+    shape, strides = _tensor(low, "low", 3, q.dtype, device)
+    if shape != q.shape:
+        _refuse(f"low: {list(q.shape)} wanted, got {list(shape)}")
+    return _heads(low, strides)
 
+
+class _Prompt(torch.autograd.Function):
+    # (forward with a context: the form with setup_context takes 25 us more of the host's time a call)
     @staticmethod
-    def setup_context(ctx, inputs, output):
-        q, k, v, starts, ctx.causal, ctx.scale, ctx.status = inputs
+    def forward(ctx, q, k, v, starts, causal, scale, status):
+        low = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out, lse = _prompt_call(q, k, v, starts, causal, scale, None, None, low, None, status, None)
+        ctx.causal, ctx.scale, ctx.status = causal, scale, status
         ctx.set_materialize_grads(False)
-        ctx.save_for_backward(q, k, v, starts, *output)
+        ctx.save_for_backward(q, k, v, starts, out, lse, low)
+        return out, lse
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dout, dlse):
-        q, k, v, starts, out, lse = ctx.saved_tensors
+        q, k, v, starts, out, lse, low = ctx.saved_tensors
         if dout is None and dlse is None:
             return (None,) * 7
         dout = torch.zeros_like(out) if dout is None else _inner(dout)
         dlse = None if dlse is None else dlse.contiguous()
-        got = prompt_attention_grad(dout, q, k, v, out, lse, starts, causal=ctx.causal, scale=ctx.scale, dlse=dlse, status=ctx.status)
+        got = prompt_attention_grad(dout, q, k, v, out, lse, starts, causal=ctx.causal, scale=ctx.scale, dlse=dlse, low=low, status=ctx.status)
         return *(g if want else None for g, want in zip(got, ctx.needs_input_grad)), None, None, None, None
 
 
-def prompt_attention(q, k, v, starts, causal=True, scale=None, out=None, lse=None, workspace=None, status=None, stream=None):
+def prompt_attention(q, k, v, starts, causal=True, scale=None, out=None, lse=None, low=None, workspace=None, status=None, stream=None):
     """Attention of packed sequences over themselves: (out, lse).
 
     q [tokens, heads, head_dim], k and v [tokens, kv_heads, head_dim], bfloat16 or float16, heads of 64 or 128; sequence b's tokens
     are the rows ``starts[b]`` .. ``starts[b + 1] - 1`` (int32 [seqs + 1], rising, on the device).  A query sees its sequence's keys
     up to its own (``causal``) or all of them; ``scale``: of the products, positive (default 1 / sqrt(head_dim)).  lse (float32
-    [tokens, heads]) is the logarithm of the sum of exponentials.  Rows of no sequence get zeros and lse = -inf; those
+    [tokens, heads]) is the logarithm of the sum of exponentials; ``low``, a tensor like out, gets what rounding took from out, for
+    ``prompt_attention_grad``.  Rows of no sequence get zeros and lse = -inf; those
     of a given ``out`` or ``lse`` are left as they are.  Starts out of range are clamped and store GTS_ERR_INVALID_PARAMS to ``status`` (int32 [1]
     on the device), where given.  A kernel whose waits run out (after two seconds) stores GTS_ERR_STEP_LIMIT there, and its rows are NaN.
 
@@ -648,16 +659,16 @@ def prompt_attention(q, k, v, starts, causal=True, scale=None, out=None, lse=Non
     captured into a graph while another graph of the same leaves lives wants that one made on the capturing stream: torch ties
     a leaf's gradient to the stream of its first use."""
     if _differentiated(q) or _differentiated(k) or _differentiated(v):
-        if out is not None or lse is not None or workspace is not None or stream is not None:
+        if out is not None or lse is not None or low is not None or workspace is not None or stream is not None:
             _refuse("prompt_attention: gradients need the call's own outputs and workspace and the current stream")
         return _Prompt.apply(q, k, v, starts, causal, scale, status)
-    return _prompt_call(q, k, v, starts, causal, scale, out, lse, workspace, status, stream)
+    return _prompt_call(q, k, v, starts, causal, scale, out, lse, low, workspace, status, stream)
 
 
-def prompt_attention_grad(dout, q, k, v, out, lse, starts, causal=True, scale=None, dlse=None, out_dq=None, out_dk=None, out_dv=None,
-                          workspace=None, status=None, stream=None):
+def prompt_attention_grad(dout, q, k, v, out, lse, starts, causal=True, scale=None, dlse=None, low=None, out_dq=None, out_dk=None,
+                          out_dv=None, workspace=None, status=None, stream=None):
     """The gradients (dq, dk, dv) of ``prompt_attention`` from those of its results (``dlse`` [tokens, heads] float32, default none);
-    ``out`` and ``lse`` are what it gave.  Every sum has one order, so results repeat bit for bit.  Rows of no sequence get
+    ``out``, ``lse`` and ``low`` are what it gave (without ``low`` dq and dk are 4 to 10% less exact).  Every sum has one order, so results repeat bit for bit.  Rows of no sequence get
     zeros; those of a given output are left as they are."""
     shape, qs, ks, vs, device, starts_at = _prompt_shape(q, k, v, starts)
     handle = _handle(stream, device)
@@ -668,6 +679,7 @@ def prompt_attention_grad(dout, q, k, v, out, lse, starts, causal=True, scale=No
         _refuse(f"out and dout: {list(q.shape)} wanted, got {list(oshape)} and {list(dshape)}")
     lse_at = _index(lse, "lse", (T, heads), torch.float32, device)
     dlse_at = 0 if dlse is None else _index(dlse, "dlse", (T, heads), torch.float32, device)
+    low_at = _low(low, q, device)
     zero = (out_dq is None) + 2 * (out_dk is None) + 4 * (out_dv is None)
     dq, dqs = _output(out_dq, "out_dq", q.shape, q.dtype, device, stream)
     dk, dks = _output(out_dk, "out_dk", k.shape, q.dtype, device, stream)
@@ -676,8 +688,8 @@ def prompt_attention_grad(dout, q, k, v, out, lse, starts, causal=True, scale=No
 
     def pack(work_at, work_bytes):
         return _PROMPT_GRAD.pack(
-            *shape, bool(causal), zero, scale, starts_at, *_heads(q, qs), *_heads(k, ks), *_heads(v, vs), *_heads(out, os), lse_at,
-            work_at, work_bytes, st, *_heads(dout, ds), dlse_at, *_heads(dq, dqs), *_heads(dk, dks), *_heads(dv, dvs))
+            *shape, bool(causal), zero, scale, starts_at, *_heads(q, qs), *_heads(k, ks), *_heads(v, vs), *_heads(out, os), *low_at,
+            lse_at, work_at, work_bytes, st, *_heads(dout, ds), dlse_at, *_heads(dq, dqs), *_heads(dk, dks), *_heads(dv, dvs))
     if workspace is None:
         workspace = _workspace(None, lib.gts_prompt_grad_workspace_bytes(pack(0, 0)), device, stream)
     else:

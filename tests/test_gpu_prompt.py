@@ -79,16 +79,31 @@ def test_prompt_gradient(shape, causal, dtype):
     rubbish(dout[:starts[0]]), rubbish(dout[starts[-1]:])
     dlse = rand(g, *q.shape[:2], dtype="float32") * size if shape % 2 else None
     at = ints(starts)
-    out, lse = serving.prompt_attention(q, k, v, at, causal=causal)
+    low = torch.empty_like(q) if shape % 3 else None
+    out, lse = serving.prompt_attention(q, k, v, at, causal=causal, low=low)
     status = ints([0])
-    got = serving.prompt_attention_grad(dout, q, k, v, out, lse, at, causal=causal, dlse=dlse, status=status)
+    got = serving.prompt_attention_grad(dout, q, k, v, out, lse, at, causal=causal, dlse=dlse, low=low, status=status)
     assert int(status) == 0
     _, _, want, bound = R.packed(f64(q), f64(k), f64(v), starts, D ** -0.5, causal, dtype, f64(dout), None if dlse is None else f64(dlse))
     for name, x, w, b in zip(("dq", "dk", "dv"), got, want, bound):
         check(x, w, b, name)
-    again = serving.prompt_attention_grad(dout, q, k, v, out, lse, at, causal=causal, dlse=dlse)
+    again = serving.prompt_attention_grad(dout, q, k, v, out, lse, at, causal=causal, dlse=dlse, low=low)
     for x, y in zip(again, got):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float16"])
+def test_what_rounding_took(dtype):
+    """out + low has the forward pass's own error alone: that of out without its rounding's half-step, and low's of half a step of it."""
+    lens, H, KV, D = [500, 3, 300], 4, 2, 128
+    q, k, v, starts = problem(2, lens, H, KV, D, dtype)
+    low = torch.full_like(q, 7.0)
+    out, _ = serving.prompt_attention(q, k, v, ints(starts), low=low)
+    (want, _), (bound, _), _, _ = R.packed(f64(q), f64(k), f64(v), starts, D ** -0.5, True, dtype)
+    u = R.HALF_STEP[dtype]
+    check(torch.from_numpy(f64(out) + f64(low)), want, bound - u * np.abs(want) + u * u * (np.abs(want) + bound) + (2.0 ** -24 if dtype == "float16" else 0.0), "out + low")
+    plain, _ = serving.prompt_attention(q, k, v, ints(starts))
+    assert torch.equal(plain, out)
 
 
 def test_gradient_against_differences():
@@ -125,9 +140,10 @@ def test_autograd():
     lens, H, KV, D = [40, 100], 6, 2, 128
     q, k, v, starts = problem(11, lens, H, KV, D, "bfloat16")
     at = ints(starts)
-    out, lse = serving.prompt_attention(q, k, v, at)
+    low = torch.empty_like(q)
+    out, lse = serving.prompt_attention(q, k, v, at, low=low)
     ones = torch.ones_like(out)
-    want = serving.prompt_attention_grad(ones, q, k, v, out, lse, at)
+    want = serving.prompt_attention_grad(ones, q, k, v, out, lse, at, low=low)
     for which in ([0], [1], [2], [0, 2], [0, 1, 2]):
         x = [t.detach().requires_grad_(i in which) for i, t in enumerate((q, k, v))]
         o, _ = serving.prompt_attention(*x, at)
@@ -139,17 +155,17 @@ def test_autograd():
     x = [t.detach().requires_grad_() for t in (q, k, v)]
     o, l = serving.prompt_attention(*x, at)
     l.sum().backward()
-    want = serving.prompt_attention_grad(ones * 0, q, k, v, out, lse, at, dlse=torch.ones_like(lse))
+    want = serving.prompt_attention_grad(ones * 0, q, k, v, out, lse, at, dlse=torch.ones_like(lse), low=low)
     assert all(torch.equal(t.grad, w) for t, w in zip(x, want))
     t = ones.transpose(0, 2).contiguous().transpose(0, 2)                       # the head's values are not contiguous
     x = [t.detach().requires_grad_() for t in (q, k, v)]
     got = torch.autograd.grad(serving.prompt_attention(*x, at)[0], x, t)
-    want = serving.prompt_attention_grad(ones, q, k, v, out, lse, at)
+    want = serving.prompt_attention_grad(ones, q, k, v, out, lse, at, low=low)
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     with pytest.raises(RuntimeError):
         g = torch.autograd.grad(serving.prompt_attention(*x, at)[0], x, ones, create_graph=True)
         g[0].sum().backward()
-    for kw in (dict(out=torch.empty_like(out)), dict(lse=torch.empty_like(lse)), dict(stream=torch.cuda.current_stream()),
+    for kw in (dict(out=torch.empty_like(out)), dict(lse=torch.empty_like(lse)), dict(low=torch.empty_like(out)), dict(stream=torch.cuda.current_stream()),
                dict(workspace=serving.prompt_workspace(q, k, at))):
         with pytest.raises(gts.GtsError):
             serving.prompt_attention(*x, at, **kw)
@@ -294,7 +310,7 @@ def test_refusals():
             serving.prompt_attention(**{**dict(q=q, k=k, v=v, starts=at), **kw})
         with pytest.raises(gts.GtsError):
             serving.prompt_attention_grad(**{**dict(dout=out, q=q, k=k, v=v, out=out, lse=lse, starts=at), **kw})
-    for kw in (dict(out=out[:5]), dict(lse=lse[:5]), dict(lse=lse.double())):
+    for kw in (dict(out=out[:5]), dict(lse=lse[:5]), dict(lse=lse.double()), dict(low=out[:5]), dict(low=lse)):
         with pytest.raises(gts.GtsError):
             serving.prompt_attention(q, k, v, at, **kw)
     for kw in (dict(dout=out[:5]), dict(dout=out.float()), dict(dlse=lse[:5]), dict(lse=lse[:4]), dict(out_dq=k), dict(out_dk=q)):
@@ -717,7 +733,8 @@ def test_a_training_step_through_the_rotation():
     dout = rand(g, *out.shape, dtype="bfloat16")
     out.backward(dout)
     d = [rq.detach(), rk.detach(), v.detach()]
-    o, l = serving.prompt_attention(*d, ints(rows_of(lens)))
-    dq, dk, dv = serving.prompt_attention_grad(dout, *d, o, l, ints(rows_of(lens)))
+    low = torch.empty_like(d[0])
+    o, l = serving.prompt_attention(*d, ints(rows_of(lens)), low=low)
+    dq, dk, dv = serving.prompt_attention_grad(dout, *d, o, l, ints(rows_of(lens)), low=low)
     dq, dk = serving.rope_grad(dq, dk, pos, rotary)
     assert torch.equal(rows.grad, torch.cat([dq, dk, dv], 1))

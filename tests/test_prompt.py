@@ -64,8 +64,8 @@ def _heads(at=PTR):
 
 
 def _prompt(**kw):
-    kw = {k: _heads(v) if k in ("q", "k", "v", "out") else v for k, v in kw.items()}
-    return _set(serving.PromptDesc(3, 100, 8, 2, 128, serving.GTS_BF16, 1, 0, 0.1, PTR, _heads(), _heads(), _heads(), _heads(), PTR, PTR,
+    kw = {k: _heads(v) if k in ("q", "k", "v", "out", "low") else v for k, v in kw.items()}
+    return _set(serving.PromptDesc(3, 100, 8, 2, 128, serving.GTS_BF16, 1, 0, 0.1, PTR, _heads(), _heads(), _heads(), _heads(), _heads(), PTR, PTR,
                                    1 << 40, None), kw)
 
 
@@ -73,7 +73,7 @@ PROMPT = [dict(dtype=serving.GTS_F32), dict(dtype=-1), dict(head_dim=80), dict(h
           dict(q_heads=0), dict(kv_heads=0), dict(q_heads=260, kv_heads=2), dict(kv_heads=2048, q_heads=2048), dict(causal=2),
           dict(zero_rest=8), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(starts=None),
           dict(starts=PTR + 2), dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(q=PTR + 1), dict(k=PTR + 1),
-          dict(v=PTR + 1), dict(out=PTR + 1), dict(lse=PTR + 2), dict(workspace=None), dict(workspace=PTR + 8), dict(d_status=PTR + 1),
+          dict(v=PTR + 1), dict(out=PTR + 1), dict(low=PTR + 1), dict(lse=PTR + 2), dict(workspace=None), dict(workspace=PTR + 8), dict(d_status=PTR + 1),
           dict(n_seqs=1 << 16), dict(n_tokens=(1 << 28) + 1), dict(n_tokens=1 << 28, q_heads=16)]
 
 
