@@ -6,6 +6,7 @@
 // p_ij = exp(s_ij - lse_i), e_i = dout_i . out_i - dlse_i and ds_ij = p_ij (dout_i . v_j - e_i): dv_j = sum p_ij dout_i,
 // dq_i = scale sum ds_ij k_j, dk_j = scale sum ds_ij q_i.
 #include <algorithm>
+#include <climits>
 #include <cmath>
 #include <type_traits>
 
@@ -250,6 +251,18 @@ template <typename T> __device__ __forceinline__ uint4 gather16(const T *from) {
   return v;
 }
 
+// 16 columns of the warp's 32 rows
+__device__ __forceinline__ void tc_ld16(uint32_t *r, uint32_t at) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
+                 "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void tc_st16(uint32_t at, const uint32_t *r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+               "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(at) : "memory");
+}
+
 // 32 values of a row: in pieces of 32 bytes where rows stand on that grid (half the accesses of 16, and whole sectors).
 template <typename T> __device__ __forceinline__ void store64(T *to, const uint32_t (&w)[16], bool aligned) {
   if (aligned) {
@@ -352,20 +365,22 @@ __device__ __forceinline__ void clean_tile(unsigned char *tile, int lane, int li
 // ---------------------------------------------------------------- forward
 // A block holds 2 x 128 rows of one key head - `queries / 2` queries of a sequence with all their heads in each half - and passes along
 // its tiles of 128 keys:
-//   warp 9 walks along the block's stretch, hands its items on through a short queue, and brings tiles of keys and values
+//   warp 17 walks along the block's stretch, hands its items on through a short queue, and brings tiles of keys and values
 //   (TMA where pages and strides allow it, else 16-byte copies or plain loads) into a ring;
-//   warp 11 brings an item's queries, and cleans tiles of values in which some rows are out of sight;
-//   warps 8 and 10 issue the products, each for one half: S = Q K^T to tensor memory, O += P V with P from tensor memory;
-//   warps 0..3 and 4..7 take one half each, one row a thread: maximum, weights, sum.  P overwrites S.
+//   warp 19 brings an item's queries, and cleans tiles of values in which some rows are out of sight;
+//   warps 16 and 18 issue the products, each for one half: S = Q K^T to tensor memory, O += P V with P from tensor memory;
+//   warps 0..7 and 8..15 take one half each, two threads to a row with 64 of a tile's keys each: maximum (of both, through shared
+//   memory), weights, sum.  P overwrites S.
 // The halves alternate: while one turns scores into weights, the tensor cores work for the other.  An item's first scores are
 // worked out, and its queries brought, while the rows of the one before store their results.  The maximum that scores are taken against is
 // raised, and what was summed rescaled, only when it has grown by more than 8 (in log 2).  Weights are rounded to the values'
 // type for their product; the sum is of the unrounded ones, all else is in 32 bits.
-constexpr int FWD_THREADS = 384, QUEUE = 4;
+constexpr int ROW_WARPS = 16, ROW_THREADS = ROW_WARPS * 32, BLOCK_THREADS = ROW_THREADS + 128, FWD_THREADS = BLOCK_THREADS, QUEUE = 4;
 constexpr float RAISE = 8.f;
 template <int D> struct Fwd {
+  static constexpr bool APART = D == 64;               // sums of their own for either half of a tile's keys
   static constexpr int BYTES = TILE * D * 2, STAGES = D == 64 ? 8 : 5, Q = 2 * BYTES;
-  static constexpr int BEHIND = 1280, SMEM = Q + STAGES * BYTES + BEHIND;
+  static constexpr int BEHIND = 2816, SMEM = Q + STAGES * BYTES + BEHIND;
 };
 
 struct FwdMaps {
@@ -393,17 +408,19 @@ __device__ __forceinline__ int seen_by_all(const Args &a, const Item &i, int q0)
 
 template <typename T, int D>
 __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const Items<false> items, const Cut cut, const __grid_constant__ FwdMaps all_maps) {
+  constexpr bool APART = Fwd<D>::APART;
   constexpr int BYTES = Fwd<D>::BYTES, STAGES = Fwd<D>::STAGES, COLUMNS = TILE * 128;   // bytes of 64 columns of a tile
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char *const qs = smem, *const ring = qs + Fwd<D>::Q;
   uint64_t *const bars = (uint64_t *)(ring + STAGES * BYTES);
-  constexpr int BARS = 8 + STAGES + 4 + 2 + 2 + 2 + 4 + 2 + 2 + 2 + 2 * QUEUE + 2;
+  constexpr int BARS = 8 + STAGES + 24 + 2 * QUEUE;
   Item *const queue = (Item *)(bars + BARS);
   uint32_t *const bad_rows = (uint32_t *)(queue + QUEUE);                               // [4][4]: of the last tiles of values
-  uint32_t *const tmem_at = bad_rows + 16;
+  float *const tops = (float *)(bad_rows + 16);                                         // [2][2][128]: each thread's maximum or sum
+  uint32_t *const tmem_at = (uint32_t *)(tops + 512);
   volatile int *const dead = (volatile int *)(tmem_at + 1);
-  void *const scratch = (void *)(tmem_at + 2);
-  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 16 * 4 + 8 + SCRATCH <= Fwd<D>::BEHIND, "room behind the ring");
+  void *const scratch = tops;                          // (done with before the first maximum)
+  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 16 * 4 + 2048 + 8 <= Fwd<D>::BEHIND && SCRATCH <= 2048, "room behind the ring");
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), q_at = smem_u32(qs), ring_at = smem_u32(ring);
   const Pages &maps = all_maps.kv;
@@ -414,14 +431,14 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
   auto ready = [&](uint32_t v) { return bar0 + (B0 + v % 4) * 8; };                     // the v-th tile of values is clean
   auto q_full = [&](int h) { return bar0 + (B0 + 4 + h) * 8; };
   auto q_empty = [&](int h) { return bar0 + (B0 + 6 + h) * 8; };
-  auto s_full = [&](int h) { return bar0 + (B0 + 8 + h) * 8; };
-  auto p_full = [&](int h, int x) { return bar0 + (B0 + 10 + h * 2 + x) * 8; };         // weights of half the keys
-  auto o_full = [&](int h) { return bar0 + (B0 + 14 + h) * 8; };
-  auto o_free = [&](int h) { return bar0 + (B0 + 16 + h) * 8; };
-  auto my_turn = [&](int h) { return bar0 + (B0 + 18 + h) * 8; };
-  auto given = [&](uint32_t i) { return bar0 + (B0 + 20 + i % QUEUE) * 8; };
-  auto taken = [&](uint32_t i) { return bar0 + (B0 + 20 + QUEUE + i % QUEUE) * 8; };
-  const uint32_t ended = bar0 + (B0 + 20 + 2 * QUEUE) * 8;
+  auto s_full = [&](int h, int y) { return bar0 + (B0 + 8 + (APART ? 2 * y : 0) + h) * 8; };   // (of half the keys, where those are apart)
+  auto p_full = [&](int h, int x) { return bar0 + (B0 + 12 + h * 2 + x) * 8; };         // weights of half the keys
+  auto o_full = [&](int h) { return bar0 + (B0 + 16 + h) * 8; };
+  auto o_free = [&](int h) { return bar0 + (B0 + 18 + h) * 8; };
+  auto my_turn = [&](int h) { return bar0 + (B0 + 20 + h) * 8; };
+  auto given = [&](uint32_t i) { return bar0 + (B0 + 22 + i % QUEUE) * 8; };
+  auto taken = [&](uint32_t i) { return bar0 + (B0 + 22 + QUEUE + i % QUEUE) * 8; };
+  const uint32_t ended = bar0 + (B0 + 22 + 2 * QUEUE) * 8;
 
   dependents_may_start();
   Stretch line = find_stretch<false, FWD_THREADS>(a, items, cut.blocks, scratch);
@@ -437,14 +454,14 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
     for (int s = 0; s < STAGES; s++) bar_init(empty(s), 2);
     for (int v = 0; v < 4; v++) bar_init(ready(v), 1);
     for (int h = 0; h < 2; h++) {
-      bar_init(q_full(h), 1), bar_init(q_empty(h), 1), bar_init(s_full(h), 1), bar_init(p_full(h, 0), 128), bar_init(p_full(h, 1), 128);
-      bar_init(o_full(h), 1), bar_init(o_free(h), 128), bar_init(my_turn(h), 1), bar_init(ended + 8 * h, 1);
+      bar_init(q_full(h), 1), bar_init(q_empty(h), 1), bar_init(s_full(h, 0), 1), bar_init(bar0 + (B0 + 10 + h) * 8, 1), bar_init(p_full(h, 0), 128), bar_init(p_full(h, 1), 128);
+      bar_init(o_full(h), 1), bar_init(o_free(h), ROW_THREADS / 2), bar_init(my_turn(h), 1), bar_init(ended + 8 * h, 1);
     }
-    for (int i = 0; i < QUEUE; i++) bar_init(given(i), 1), bar_init(taken(i), 11);
+    for (int i = 0; i < QUEUE; i++) bar_init(given(i), 1), bar_init(taken(i), ROW_WARPS + 3);
     *dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 8) {
+  if (warp == ROW_WARPS) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_at)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
   }
@@ -454,7 +471,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
   const uint32_t tmem = __shfl_sync(~0u, *tmem_at, 0);
   auto scores = [&](int h) { return tmem + h * TILE; };
   auto sums = [&](int h) { return tmem + 256 + h * 128; };
-  int copies = 0, asked[2] = {0, 0};                   // warp 9: tiles asked for by TMA; warp 11: halves of queries
+  int copies = 0, asked[2] = {0, 0};                   // warp 17: tiles asked for by TMA; warp 19: halves of queries
   bool issues = false;                                 // the threads that issue products
   bool alive = true;
   auto need = [&](uint32_t bar, uint32_t parity) { alive = alive && bar_wait(bar, parity & 1, dead); };
@@ -473,9 +490,9 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
   };
   auto take = [&] { bar_arrive(taken(turn_of_queue++)); };
 
-  if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    if (warp == 9) {
+  if (warp >= ROW_WARPS) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    if (warp == ROW_WARPS + 1) {
       // ---- the walk, keys and values
       const bool aligned = (((uintptr_t)a.k.data >> 1 | (uintptr_t)a.v.data >> 1 | a.k.tok | a.k.head | a.v.tok | a.v.head | (a.paged ? a.k_page | a.v_page : 0)) & 7) == 0;
       Stretch s = line;
@@ -564,7 +581,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           if (landing >= 0) landed();
         }
       }
-    } else if (warp == 11) {
+    } else if (warp == ROW_WARPS + 3) {
       // ---- queries, and tiles of values made clean
       const bool aligned = (((uintptr_t)a.q.data >> 1 | a.q.tok | a.q.head) & 7) == 0;
       Item i;
@@ -625,33 +642,37 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
       issues = true;
       constexpr uint32_t TYPE = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
       constexpr uint32_t COMMON = 1u << 4 | TYPE << 7 | TYPE << 10 | (128u >> 4) << 24;
-      constexpr uint32_t QK = COMMON | (TILE >> 3) << 17, PV = COMMON | 1u << 16 | (D >> 3) << 17;
-      const int h = warp == 10;
+      constexpr uint32_t QK = COMMON | ((APART ? TILE / 2 : TILE) >> 3) << 17, PV = COMMON | 1u << 16 | (D >> 3) << 17;
+      const int h = warp == ROW_WARPS + 2;
       const uint32_t k_op = operand(ring_at, 16), v_op = operand(ring_at, COLUMNS), q_op = operand(q_at + h * BYTES, 16);
       const uint32_t s_at = scores(h), o_at = sums(h);
       uint32_t slot = 0, tiles = 0, items_done = 0, turn = 0, turns = 0;
-      auto qk = [&](uint32_t sl) {
+      auto qk = [&](uint32_t sl, int y) {                // with all keys of a tile, or with those of half y
         const uint32_t st = sl % STAGES;
-        uint32_t q = q_op, k = k_op + ((st * BYTES) >> 4);
+        uint32_t q = q_op, k = k_op + ((st * BYTES + (APART ? y * 64 * 128 : 0)) >> 4);
 #pragma unroll
         for (int x = 0; x < D / 64; x++, q += COLUMNS >> 4, k += COLUMNS >> 4) {
 #pragma unroll
-          for (int y = 0; y < 4; y++) tc_mma(s_at, q + 2 * y, k + 2 * y, OPERAND_HI, QK, x + y > 0);
+          for (int z = 0; z < 4; z++) tc_mma(s_at + (APART ? y * 64 : 0), q + 2 * z, k + 2 * z, OPERAND_HI, QK, x + z > 0);
         }
-        tc_commit(s_full(h));
-        tc_commit(empty(st));
+        tc_commit(s_full(h, y));
+        if (!APART || y) tc_commit(empty(st));
       };
       Item i;
       while (next(i)) {
         const Half x = half_of(a, items, i, h);
         const int both = min(x.count, half_of(a, items, i, !h).count), n = i.tile1 - i.tile0;
         take();
+        const int clear = a.causal ? seen_by_all(a, i, i.t * items.q) : INT_MAX;   // tiles that end after it are cleaned of values: before their scores
         if (x.count) {
           need(q_full(h), items_done);
           need(full(slot), slot / 8);
+          if ((i.tile0 + 1) * TILE > clear) need(ready(tiles), tiles / 4);
           if (!alive) break;
           tc_after();
-          qk(slot++);
+          qk(slot, 0);
+          if (APART) qk(slot, 1);
+          slot++;
           if (x.count == 1) tc_commit(q_empty(h));
         }
         for (int j = 0; j < x.count && alive; j++, tiles++) {
@@ -659,7 +680,10 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           const uint32_t sv = slot++, sk = slot;
           const int seen = x.seen - (i.tile0 + j) * TILE;
           need(ready(tiles), tiles / 4);
-          if (j + 1 < x.count) need(full(sk), sk / 8), slot++;
+          if (j + 1 < x.count) {
+            need(full(sk), sk / 8), slot++;
+            if ((i.tile0 + j + 2) * TILE > clear) need(ready(tiles + 1), (tiles + 1) / 4);
+          }
           if (j == 0 && items_done) need(o_free(h), items_done - 1);
           if (!alive) break;
           const uint32_t *const bad = bad_rows + tiles % 4 * 4;
@@ -669,24 +693,26 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           for (int y = 0; y < 2; y++) {
             need(p_full(h, y), turn);
             // The halves take turns, each with all its products for a tile: left alone they fall into step, and the tensor
-            // cores wait while both make weights
-            if (y == 0 && j < both) need(my_turn(h), h ? turns : turns - 1), turns++;
+            // cores wait while both make weights (four parts of scores to work on cover each other)
+            if (!APART && y == 0 && j < both) need(my_turn(h), h ? turns : turns - 1), turns++;
             if (!alive) break;
             tc_after();
 #pragma unroll
             for (int k = 4 * y; k < 4 * y + 4; k++)
-              if (k == 0 || k * 16 < seen) tc_mma_t(o_at, s_at + k * 8, v + k * (2048 >> 4), OPERAND_HI, PV, add || k > 0);
+              if (k == 0 || (APART && k == 4) || k * 16 < seen)
+                tc_mma_t(o_at + (APART ? y * 64 : 0), s_at + k / 4 * 64 + k % 4 * 8, v + k * (2048 >> 4), OPERAND_HI, PV, add || (APART ? k % 4 : k) > 0);
+            if (APART && j + 1 < x.count) qk(sk, y);
           }
           turn++;
           if (!alive) break;
           tc_commit(empty(sv % STAGES));
           if (j + 1 < x.count) {
-            qk(sk);
+            if (!APART) qk(sk, 0);
             if (j + 2 == x.count) tc_commit(q_empty(h));
           } else {
             tc_commit(o_full(h));
           }
-          if (j < both) bar_arrive(my_turn(!h));
+          if (!APART && j < both) bar_arrive(my_turn(!h));
         }
         if (x.count) items_done++;
         for (int j = x.count; j < n && alive; j++, tiles++) {          // tiles that are only the other half's pass by
@@ -698,16 +724,30 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
       }
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-    // ---- one row a thread
-    const int h = warp / 4, r = tid % 128;
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
+    // ---- two threads to a row, y for the second 64 keys of a tile and the second half of the head's values
+    const int h = warp / 8, y = warp / 4 % 2, r = tid % 128;
     const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
     const float sl2 = a.scale * 1.4426950408889634f;
     const bool aligned = rows_aligned(a.out), low_aligned = rows_aligned(a.low);
     const int in_half = r / a.in_group, head_in = r - in_half * a.group;
+    float *const mine = tops + (h * 2 + y) * 128 + r, *const others = tops + (h * 2 + !y) * 128 + r;
+    // The two warps of the same rows exchange a value each; NaN says that a wait ran out, so that both go on or both leave: this
+    // barrier has no limit of its own.
+    auto meet = [&] { asm volatile("bar.sync %0, 64;" ::"r"(1 + h * 4 + warp % 4) : "memory"); };
+    auto exchange = [&](float x) {
+      meet();                                            // what was there has been read
+      *mine = alive ? x : NAN;
+      meet();
+      return *others;
+    };
+    auto wait = [&](uint32_t bar, uint32_t parity) { alive = __all_sync(~0u, bar_wait(bar, parity & 1, dead)) && alive; };
     uint32_t turn = 0, items_done = 0, tiles = 0;
     Item i;
-    while (next_all(i)) {
+    while (true) {
+      wait(given(turn_of_queue), turn_of_queue / QUEUE);
+      i = queue[turn_of_queue % QUEUE];
+      if (isnan(exchange(0.f)) || !alive || i.tiles == 0) break;
       const Half x = half_of(a, items, i, h);
       const int query = x.q0 + in_half, kh = i.kh;
       const bool valid = in_half < x.queries;
@@ -716,139 +756,204 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
       const bool whole = i.tile0 == 0 && i.tile1 == i.tiles;
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < x.count; j++, turn++) {
-        alive = __all_sync(~0u, bar_wait(s_full(h), turn & 1, dead));
-        if (!alive) break;
+        wait(s_full(h, y), turn);
         tc_after();
-        const int t = i.tile0 + j, nv = limit - t * TILE;
+        const int t = i.tile0 + j, nv = limit - t * TILE - y * 64;
         const bool masked = (t + 1) * TILE > clear;
-        // Half of the scores at a time, and tensor memory read again for the weights: all 128 in registers would spill, and
-        // shorter pieces add their latencies.
-        uint32_t s[64];
+        uint32_t s[32], pk[32];
         auto fetch = [&](int c) {
-          tc_ld(s, scores(h) + lanes + c);
-          tc_ld(s + 32, scores(h) + lanes + c + 32);
+          tc_ld(s, scores(h) + lanes + y * 64 + c);
           tc_ld_wait();
           if (masked) {
 #pragma unroll
-            for (int y = 0; y < 64; y++)
-              if (c + y >= nv) s[y] = 0xFF800000u;         // -infinity
+            for (int z = 0; z < 32; z++)
+              if (c + z >= nv) s[z] = 0xFF800000u;         // -infinity
           }
         };
-        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+        float top[2] = {-INFINITY, -INFINITY};
+        auto see = [&] {
 #pragma unroll
-        for (int y = 0; y < 2; y++) {
-          fetch(y * 64);
-#pragma unroll
-          for (int c = 0; c < 64; c += 8) {
-#pragma unroll
-            for (int z = 0; z < 4; z++) top[z] = max3(top[z], __uint_as_float(s[c + 2 * z]), __uint_as_float(s[c + 2 * z + 1]));
+          for (int z = 0; z < 32; z += 4) {
+            top[0] = max3(top[0], __uint_as_float(s[z]), __uint_as_float(s[z + 1]));
+            top[1] = max3(top[1], __uint_as_float(s[z + 2]), __uint_as_float(s[z + 3]));
           }
-        }
-        const float big = fmaxf(max3(top[0], top[1], top[2]), top[3]) * sl2;
-        const bool raise = big > m + RAISE || (m == -INFINITY && big > m);
-        if (j == 0) {
-          m = big;
-        } else if (__any_sync(~0u, raise)) {
-          const float to = raise ? big : m, f = raise ? exp2_fast(m - to) : 1.f;
-          uint32_t o[32];
+        };
+        float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+        auto weigh = [&](int c, float from) {
+          const float2 scale2 = make_float2(sl2, sl2), from2 = make_float2(-from, -from);
+#pragma unroll
+          for (int z = 0; z < 32; z += 2) {
+            float2 e = fma2(make_float2(__uint_as_float(s[z]), __uint_as_float(s[z + 1])), scale2, from2);
+            e.x = exp2_fast(e.x), e.y = exp2_fast(e.y);
+            part[z / 2 & 1] = add2(part[z / 2 & 1], e);
+            pk[(c + z) / 2] = pack<T>(e.x, e.y);
+          }
+        };
+        if (APART) {
+          // one thread's own: the maximum, then weights
+          if (!alive) break;
+          fetch(0), see();
+          if (j) weigh(0, m == -INFINITY ? 0.f : m);       // (by the maximum so far, which seldom turns out to be too low)
+          fetch(32), see();
+          const float big = fmaxf(top[0], top[1]) * sl2;
+          const bool raise = j == 0 || big > m + RAISE || (m == -INFINITY && big > m);
+          if (__any_sync(~0u, raise)) {
+            const float to = raise ? big : m, f = raise ? exp2_fast(m - to) : 1.f;
+            if (j) {
+              uint32_t o[16];
 #pragma unroll 1
-          for (int c = 0; c < D / 32; c++) {
-            tc_ld(o, sums(h) + lanes + c * 32);
-            tc_ld_wait();
+              for (int c = 0; c < D; c += 16) {
+                tc_ld16(o, sums(h) + y * 64 + lanes + c);
+                tc_ld_wait();
 #pragma unroll
-            for (int y = 0; y < 32; y++) o[y] = __float_as_uint(__uint_as_float(o[y]) * f);
-            tc_st(sums(h) + lanes + c * 32, o);
+                for (int z = 0; z < 16; z++) o[z] = __float_as_uint(__uint_as_float(o[z]) * f);
+                tc_st16(sums(h) + y * 64 + lanes + c, o);
+              }
+              l *= f;
+            }
+            m = to;
+            part[0] = part[1] = make_float2(0.f, 0.f);
+            weigh(32, m == -INFINITY ? 0.f : m), fetch(0), weigh(0, m == -INFINITY ? 0.f : m);
+          } else {
+            weigh(32, m == -INFINITY ? 0.f : m);
           }
-          l *= f;
-          m = to;
+        } else if (j == 0) {                               // the maximum first, then weights
+          fetch(0), see(), fetch(32), see();
+          const float theirs = exchange(fmaxf(top[0], top[1]));
+          alive = alive && !isnan(theirs);                 // (a maximum is none)
+          if (!alive) break;
+          m = fmaxf(fmaxf(top[0], top[1]), theirs) * sl2;
+          const float from = m == -INFINITY ? 0.f : m;
+          weigh(32, from), fetch(0), weigh(0, from);
+        } else {
+          // weights by the maximum so far, which seldom turns out to be too low; both threads know in the end.  (The other one has
+          // read what this one writes over: the scores were asked for after its weights.)
+          const float old = m == -INFINITY ? 0.f : m;
+          fetch(0), see(), weigh(0, old);
+          fetch(32), see();
+          *mine = alive ? fmaxf(top[0], top[1]) : NAN;
+          weigh(32, old);
+          meet();
+          const float theirs = *others;
+          alive = alive && !isnan(theirs);
+          if (!alive) break;
+          const float big = fmaxf(fmaxf(top[0], top[1]), theirs) * sl2;
+          const bool raise = big > m + RAISE || (m == -INFINITY && big > m);
+          if (__any_sync(~0u, raise)) {
+            const float to = raise ? big : m, f = raise ? exp2_fast(m - to) : 1.f;
+            uint32_t o[16];
+#pragma unroll 1
+            for (int c = y * (D / 2); c < (y + 1) * (D / 2); c += 16) {
+              tc_ld16(o, sums(h) + lanes + c);
+              tc_ld_wait();
+#pragma unroll
+              for (int z = 0; z < 16; z++) o[z] = __float_as_uint(__uint_as_float(o[z]) * f);
+              tc_st16(sums(h) + lanes + c, o);
+            }
+            l *= f;
+            m = to;
+            const float from = m == -INFINITY ? 0.f : m;
+            part[0] = part[1] = make_float2(0.f, 0.f);
+            fetch(0), weigh(0, from), fetch(32), weigh(32, from);
+          }
         }
         const float from = m == -INFINITY ? 0.f : m;
         if (a.causal && (t + 1) * TILE > clear_of_all) {
-          // values that are not finite: each for the rows that see it, before the products are added
-          alive = __all_sync(~0u, bar_wait(ready(tiles + j), (tiles + j) / 4 & 1, dead));
-          if (!alive) break;
+          // values that are not finite: each for the rows that see it, before the products are added (the tile was clean before its
+          // scores were asked for, so this wait is over)
+          bar_wait(ready(tiles + j), (tiles + j) / 4 & 1, dead);
           const uint32_t *const bad = bad_rows + (tiles + j) % 4 * 4;
           if (bad[0] | bad[1] | bad[2] | bad[3]) {
 #pragma unroll 1
-            for (int c = 0; c < D / 32; c++) {
-              uint32_t o[32];
+            for (int c = APART ? 0 : y * (D / 2); c < (APART ? D : (y + 1) * (D / 2)); c += 16) {
+              uint32_t o[16];
+              const uint32_t at = sums(h) + (APART ? y * 64 : 0) + lanes + c;
               if (j == 0) {
 #pragma unroll
-                for (int y = 0; y < 32; y++) o[y] = 0;
+                for (int z = 0; z < 16; z++) o[z] = 0;
               } else {
-                tc_ld(o, sums(h) + lanes + c * 32);
+                tc_ld16(o, at);
                 tc_ld_wait();
               }
 #pragma unroll 1
-              for (int key = 0; key < TILE; key++) {
+              for (int key = APART ? y * 64 : 0; key < (APART ? y * 64 + 64 : TILE); key++) {
                 if (!(bad[key / 32] >> (key % 32) & 1)) continue;
                 uint32_t score;
                 asm volatile("tcgen05.ld.sync.aligned.32x32b.x1.b32 {%0}, [%1];" : "=r"(score) : "r"(scores(h) + lanes + key) : "memory");
                 tc_ld_wait();
                 const T *value = key_row<T>(a, a.v, a.v_page, i.b, i.first, t * TILE + key, kh);
-                if (key < nv && value) {
+                if (key < limit - t * TILE && value) {
                   const float p = widen(narrow<T>(exp2_fast(__uint_as_float(score) * sl2 - from)));
 #pragma unroll
-                  for (int y = 0; y < 32; y++) {
-                    const float v = widen(value[c * 32 + y]);
-                    if (!isfinite(v)) o[y] = __float_as_uint(__uint_as_float(o[y]) + p * v);
+                  for (int z = 0; z < 16; z++) {
+                    const float v = widen(value[c + z]);
+                    if (!isfinite(v)) o[z] = __float_as_uint(__uint_as_float(o[z]) + p * v);
                   }
                 }
                 __syncwarp();
               }
-              tc_st(sums(h) + lanes + c * 32, o);
+              tc_st16(at, o);
             }
+            if (!APART) exchange(0.f);                     // both have read the scores before weights overwrite them
           }
         }
-        const float2 scale2 = make_float2(sl2, sl2), from2 = make_float2(-from, -from);
-        float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-#pragma unroll
-        for (int y = 0; y < 2; y++) {                      // the products with the first 64 weights start under the others
-          uint32_t pk[32];
-          fetch(y * 64);
-#pragma unroll
-          for (int c = 0; c < 64; c += 2) {
-            float2 e = fma2(make_float2(__uint_as_float(s[c]), __uint_as_float(s[c + 1])), scale2, from2);
-            e.x = exp2_fast(e.x), e.y = exp2_fast(e.y);
-            part[c / 2 & 1] = add2(part[c / 2 & 1], e);
-            pk[c / 2] = pack<T>(e.x, e.y);
-          }
-          tc_st(scores(h) + lanes + y * 32, pk);
-          tc_st_wait();
-          tc_before();
-          bar_arrive(p_full(h, y));
-        }
+        tc_st(scores(h) + lanes + y * 64, pk);
+        tc_st_wait();
+        tc_before();
+        bar_arrive(p_full(h, y));
         const float2 sum = add2(part[0], part[1]);
         l += sum.x + sum.y;
       }
-      if (!alive) break;
+      // the row's sum: both threads', against one maximum
+      float f0 = 1.f, f1 = 1.f;                            // of either half's sums
+      if (APART) {
+        const float m1 = exchange(m == -INFINITY ? -3e38f : m), l1 = exchange(l);
+        alive = alive && !isnan(m1);
+        if (!alive) break;                                 // (both: a maximum is no NaN)
+        const float to = fmaxf(m, m1), against = to == -INFINITY || to == -3e38f ? 0.f : to;
+        const float mine_f = exp2_fast(m - against), their_f = exp2_fast(m1 - against);
+        l = l * mine_f + l1 * their_f, m = to == -3e38f ? -INFINITY : to;
+        f0 = y ? their_f : mine_f, f1 = y ? mine_f : their_f;
+      } else {
+        if (!alive) break;                                 // (both)
+        l += exchange(l);
+      }
       tiles += i.tile1 - i.tile0;
       const int64_t part = ((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 256 + h * 128 + r;
       if (x.count) {
-        alive = __all_sync(~0u, bar_wait(o_full(h), items_done & 1, dead));
-        if (!alive) break;
+        wait(o_full(h), items_done);
         items_done++;
         tc_after();
         const float inv = l == 0.f ? 0.f : 1.f / l;
         T *const dst = row_at<T>(a.out, row, kh * a.group + head_in);
         float4 *const mid = cut.o + part / 256 * (D / 4) * 256 + part % 256;
 #pragma unroll 1
-        for (int c = 0; c < D / 32; c++) {
+        for (int c = y * (D / 2); c < (y + 1) * (D / 2) && alive; c += 32) {
           uint32_t o[32];
-          tc_ld(o, sums(h) + lanes + c * 32);
+          tc_ld(o, sums(h) + lanes + c);
           tc_ld_wait();
+          if (APART) {
+#pragma unroll
+            for (int part = 0; part < 32; part += 16) {
+              uint32_t o1[16];
+              tc_ld16(o1, sums(h) + 64 + lanes + c + part);
+              tc_ld_wait();
+#pragma unroll
+              for (int z = 0; z < 16; z++) o[part + z] = __float_as_uint(f0 * __uint_as_float(o[part + z]) + f1 * __uint_as_float(o1[z]));
+            }
+          }
           if (valid && !whole) {
 #pragma unroll
-            for (int y = 0; y < 32; y += 4) *(uint4 *)(mid + (c * 8 + y / 4) * 256) = make_uint4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+            for (int z = 0; z < 32; z += 4) *(uint4 *)(mid + (c + z) / 4 * 256) = make_uint4(o[z], o[z + 1], o[z + 2], o[z + 3]);
           } else if (valid) {
             uint32_t w[16];
 #pragma unroll
-            for (int y = 0; y < 16; y++) w[y] = pack<T>(__uint_as_float(o[2 * y]) * inv, __uint_as_float(o[2 * y + 1]) * inv);
-            store64<T>(dst + c * 32, w, aligned);
+            for (int z = 0; z < 16; z++) w[z] = pack<T>(__uint_as_float(o[2 * z]) * inv, __uint_as_float(o[2 * z + 1]) * inv);
+            store64<T>(dst + c, w, aligned);
             if (a.low.data) {
 #pragma unroll
-              for (int y = 0; y < 16; y++) w[y] = pack_low<T>(__uint_as_float(o[2 * y]) * inv, __uint_as_float(o[2 * y + 1]) * inv);
-              store64<T>(row_at<T>(a.low, row, kh * a.group + head_in) + c * 32, w, low_aligned);
+              for (int z = 0; z < 16; z++) w[z] = pack_low<T>(__uint_as_float(o[2 * z]) * inv, __uint_as_float(o[2 * z + 1]) * inv);
+              store64<T>(row_at<T>(a.low, row, kh * a.group + head_in) + c, w, low_aligned);
             }
           }
           __syncwarp();
@@ -856,7 +961,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
         tc_before();
         bar_arrive(o_free(h));
       }
-      if (valid) {
+      if (valid && y == 0) {
         if (!whole) cut.ml[part] = make_float2(m, l);
         else if (a.lse) a.lse[row * a.q_heads + kh * a.group + head_in] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
       }
@@ -871,17 +976,17 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
     // copies and products in flight end before the block does, whichever warp gave up
     const uint64_t from = now_ns();
     if (issues) {
-      const uint32_t bar = ended + (warp == 10 ? 8 : 0);
+      const uint32_t bar = ended + (warp == ROW_WARPS + 2 ? 8 : 0);
       tc_commit(bar);
       while (!bar_try(bar, 0) && now_ns() - from < DRAIN_NS) {}
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-    if (warp == 9) {
+    if (warp == ROW_WARPS + 1) {
 #pragma unroll 1
       for (int x = max(0, copies - STAGES); x < copies; x++)
         while (!bar_try(full(x), (x / 8) & 1) && now_ns() - from < DRAIN_NS) {}
     }
-    if (warp == 11) {
+    if (warp == ROW_WARPS + 3) {
 #pragma unroll 1
       for (int h = 0; h < 2; h++)
         while (asked[h] && !bar_try(q_full(h), (asked[h] - 1) & 1) && now_ns() - from < DRAIN_NS) {}
@@ -909,7 +1014,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
       }
     }
   }
-  if (warp == 8) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
+  if (warp == ROW_WARPS) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
 // Rows of the items that were cut, from the block where the item begins to that where it ends: a thread for a row and an eighth
@@ -928,29 +1033,27 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join(const Args a, const Items
   if (in_half >= items.q / 2 || query >= s.n) return;
   float m = -INFINITY, l = 0.f;
   float4 acc[E] = {};
-  for (int x = 0; x <= end.w; x += 4) {
-    float2 ml[4];
-    float4 v[4][E];
-    int64_t part[4];
+  for (int x = 0; x <= end.w; x += 2) {
+    float2 ml[2];
+    float4 v[2][E];
 #pragma unroll
-    for (int k = 0; k < 4; k++) {
-      part[k] = (int64_t)(c + x + k) * 2 + (x + k == 0);
-      ml[k] = x + k <= end.w ? cut.ml[part[k] * 256 + r] : make_float2(-INFINITY, 0.f);
-    }
+    for (int k = 0; k < 2; k++) {
+      if (x + k <= end.w) {
+        const int64_t part = (int64_t)(c + x + k) * 2 + (x + k == 0);
+        ml[k] = cut.ml[part * 256 + r];
 #pragma unroll
-    for (int k = 0; k < 4; k++) {
-      if (!(ml[k].x == -INFINITY)) {                    // (a part of no tiles has no values)
-#pragma unroll
-        for (int e = 0; e < E; e++) v[k][e] = cut.o[(part[k] * (D / 4) + column * E + e) * 256 + r];
+        for (int e = 0; e < E; e++) v[k][e] = cut.o[(part * (D / 4) + column * E + e) * 256 + r];
+      } else {
+        ml[k] = make_float2(-INFINITY, 0.f);
       }
     }
-    const float top = fmaxf(fmaxf(fmaxf(m, ml[0].x), fmaxf(ml[1].x, ml[2].x)), ml[3].x), from = top == -INFINITY ? 0.f : top, keep = exp2_fast(m - from);
+    const float top = fmaxf(m, fmaxf(ml[0].x, ml[1].x)), from = top == -INFINITY ? 0.f : top, keep = exp2_fast(m - from);
     l *= keep, m = top;
 #pragma unroll
     for (int e = 0; e < E; e++) acc[e].x *= keep, acc[e].y *= keep, acc[e].z *= keep, acc[e].w *= keep;
 #pragma unroll
-    for (int k = 0; k < 4; k++) {
-      if (!(ml[k].x == -INFINITY)) {
+    for (int k = 0; k < 2; k++) {
+      if (!(ml[k].x == -INFINITY)) {                    // (a part of no tiles has no values)
         const float f = exp2_fast(ml[k].x - from);
         l += f * ml[k].y;
 #pragma unroll
@@ -984,7 +1087,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join(const Args a, const Items
 // float16 is short of small numbers: weights are held times 2^10 and ds times the power of two that puts the largest |dout| of the
 // call between 1/2 and 1 (then |ds| stays below 256 times the largest |v|, and what is lost below 2^-24 of it does not
 // count beside the largest).  bfloat16 has the range of 32 bits and needs neither.
-constexpr int ROW_WARPS = 16, ROW_THREADS = ROW_WARPS * 32, GRAD_THREADS = ROW_THREADS + 128, DELTA_BLOCKS = 1216, DELTA_THREADS = 256;
+constexpr int GRAD_THREADS = BLOCK_THREADS, DELTA_BLOCKS = 1216, DELTA_THREADS = 256;
 template <typename T> constexpr float WEIGHT_SHIFT = std::is_same<T, __half>::value ? 10.f : 0.f;
 template <typename T> constexpr float WEIGHT_UNIT = std::is_same<T, __half>::value ? 0x1p-10f : 1.f;
 
@@ -1073,12 +1176,6 @@ template <typename T> __device__ __forceinline__ float ds_factor(const float *la
 
 // Maps of the rows of queries (or of dout): a box is the `group` heads of a key head of `q` tokens; of keys and values.
 struct GradMaps { CUtensorMap q, dout; Pages kv; };
-
-__device__ __forceinline__ void tc_st16(uint32_t at, const uint32_t *r) {
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
-               ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
-               "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(at) : "memory");
-}
 
 // Columns of a row in tensor memory to a result, or as they are to a partial one.
 template <typename T, int COLUMNS>
