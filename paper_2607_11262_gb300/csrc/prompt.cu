@@ -1103,6 +1103,7 @@ template <typename T, int D>
 __global__ void __launch_bounds__(DELTA_THREADS) k_delta(const Args a, float *largest) {
   constexpr int PER = D / 8;                           // lanes of a row
   __shared__ int ends[2];
+  dependents_may_start();
   if (threadIdx.x == 0) ends[0] = a.n_tokens, ends[1] = 0;
   __syncthreads();
   for (int b = threadIdx.x; b < a.n_seqs; b += DELTA_THREADS) {
@@ -1255,13 +1256,14 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
   const uint32_t kv_full = rest, kv_empty = rest + 8, s_full = rest + 16, dp_full = rest + 24, p_full = rest + 32, ds_full = rest + 40,
                  o_full = rest + 48, o_free = rest + 56, ended = rest + 64;
 
-  dependents_may_start();
   Stretch line = find_stretch<true, GRAD_THREADS>(a, items, cut.blocks, scratch);
   if (line.rest_from + a.n_tokens - line.rest_to > 0) {
     if (a.zero_rest & 2) zero_rest<T>(a, a.dk, a.kv_heads, D, line);
     if (a.zero_rest & 4) zero_rest<T>(a, a.dv, a.kv_heads, D, line);
   }
   if (tid == 0) cut.ends[blockIdx.x] = make_int4(NOTHING, 0, 0, 0);
+  wait_for_kernels_before();                             // e; only then may the next kernel start, which wants it too
+  dependents_may_start();
   if (line.x0 >= line.x1) return;
   const float factor = ds_factor<T>(largest, scratch);
   if (tid == 0) {
@@ -1600,7 +1602,10 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
   Stretch line = find_stretch<false, GRAD_THREADS>(a, items, cut.blocks, scratch);
   if (line.rest_from + a.n_tokens - line.rest_to > 0 && a.zero_rest & 1) zero_rest<T>(a, a.dq, a.q_heads, D, line);
   if (tid == 0) cut.ends[blockIdx.x] = make_int4(NOTHING, 0, 0, 0);
-  if (line.x0 >= line.x1) return;
+  if (line.x0 >= line.x1) {
+    if (blockIdx.x == 0) wait_for_kernels_before();
+    return;
+  }
   const float factor = ds_factor<T>(largest, scratch);
   if (tid == 0) {
     for (int s = 0; s < 8; s++) bar_init(full(s), 1);
@@ -1843,19 +1848,19 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
       }
     }
   }
+  if (blockIdx.x == 0) wait_for_kernels_before();        // so that the joining kernel needs to wait for one kernel only
   if (warp == ROW_WARPS) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
 // Sums of the parts of items that were cut, in their order: a thread for a row and an eighth of its columns.
 template <typename T, int D, bool BY_KEYS>
-__global__ void __launch_bounds__(JOIN_THREADS) k_join_grad(const Args a, const Items<BY_KEYS> items, const Cut cut, const float *largest) {
-  wait_for_kernels_before();
+__device__ __forceinline__ void join_grad(const Args &a, const Items<BY_KEYS> &items, const Cut &cut, const float *largest, int block) {
   constexpr int ROWS = BY_KEYS ? 2 * TILE : TILE, E = D / 32;   // (keys' gradients after values')
-  const int c = blockIdx.x / (ROWS / 32), lane = threadIdx.x % 32, column = threadIdx.x / 32;
+  const int c = block / (ROWS / 32), lane = threadIdx.x % 32, column = threadIdx.x / 32;
   const int4 end = cut.ends[c];
   if (end.x < 0) return;
   const Seq s = sequence(a, end.x);
-  const int row = blockIdx.x % (ROWS / 32) * 32 + lane, which = row / TILE, r = row % TILE;
+  const int row = block % (ROWS / 32) * 32 + lane, which = row / TILE, r = row % TILE;
   float f = a.scale;
   if (BY_KEYS && which == 0) {
     f = WEIGHT_UNIT<T>;
@@ -1872,17 +1877,17 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join_grad(const Args a, const 
   if (at >= s.n || (!BY_KEYS && in_tile >= items.q)) return;
   const Heads &to = !BY_KEYS ? a.dq : which ? a.dk : a.dv;
   float4 acc[E] = {};
-  for (int x = 0; x <= end.w; x += 4) {
-    float4 v[4][E];
+  for (int x = 0; x <= end.w; x += 2) {
+    float4 v[2][E];
 #pragma unroll
-    for (int k = 0; k < 4; k++) {
+    for (int k = 0; k < 2; k++) {
       if (x + k <= end.w) {
 #pragma unroll
         for (int e = 0; e < E; e++) v[k][e] = cut.o[((((int64_t)(c + x + k) * 2 + (x + k == 0)) * (ROWS / TILE) + which) * (D / 4) + column * E + e) * TILE + r];
       }
     }
 #pragma unroll
-    for (int k = 0; k < 4; k++) {
+    for (int k = 0; k < 2; k++) {
       if (x + k <= end.w) {
 #pragma unroll
         for (int e = 0; e < E; e++) acc[e].x += v[k][e].x, acc[e].y += v[k][e].y, acc[e].z += v[k][e].z, acc[e].w += v[k][e].w;
@@ -1892,6 +1897,14 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join_grad(const Args a, const 
   T *const dst = row_at<T>(to, (int64_t)s.first + at, BY_KEYS ? end.y : end.y * a.group + r - in_tile * a.group) + column * E * 4;
 #pragma unroll
   for (int e = 0; e < E; e++) store4(dst + 4 * e, acc[e], f, rows_aligned(to));
+}
+
+constexpr int JOIN_KV = SMS * (2 * TILE / 32), JOIN_Q = SMS * (TILE / 32);   // its blocks
+template <typename T, int D>
+__global__ void __launch_bounds__(JOIN_THREADS) k_join_grad(const Args a, const Items<true> by_keys, const Items<false> by_rows, const Cut kv, const Cut q, const float *largest) {
+  wait_for_kernels_before();
+  if (blockIdx.x < JOIN_KV) join_grad<T, D, true>(a, by_keys, kv, largest, blockIdx.x);
+  else join_grad<T, D, false>(a, by_rows, q, largest, blockIdx.x - JOIN_KV);
 }
 
 // Rows that TMA cannot take as they lie, side by side.
@@ -1960,7 +1973,7 @@ cudaError_t run_forward(const Args &a, FwdMaps &maps, int32_t dtype, uint32_t di
 // them as they lie.
 struct GradPlan {
   float *delta, *largest;
-  Cut cut;
+  Cut kv, q;
   char *copy[4];
   size_t bytes;
 };
@@ -1974,9 +1987,10 @@ GradPlan plan_grad(const gts_prompt_grad_desc &d, const bool (&copied)[4], char 
   };
   p.delta = (float *)take((size_t)f.n_tokens * f.q_heads * sizeof(float));
   p.largest = (float *)take(DELTA_BLOCKS * sizeof(float));
-  p.cut.blocks = SMS;
-  p.cut.ends = (int4 *)take(SMS * sizeof(int4));
-  p.cut.o = (float4 *)take((size_t)SMS * 2 * 2 * TILE * f.head_dim * sizeof(float));
+  p.kv.blocks = p.q.blocks = SMS;
+  p.kv.ends = (int4 *)take(SMS * sizeof(int4)), p.q.ends = (int4 *)take(SMS * sizeof(int4));
+  p.kv.o = (float4 *)take((size_t)SMS * 2 * 2 * TILE * f.head_dim * sizeof(float));
+  p.q.o = (float4 *)take((size_t)SMS * 2 * TILE * f.head_dim * sizeof(float));
   for (int i = 0; i < 4; i++)
     if (copied[i]) p.copy[i] = take((size_t)f.n_tokens * (i < 2 ? f.q_heads : f.kv_heads) * f.head_dim * 2);
   return p;
@@ -2008,10 +2022,11 @@ cudaError_t backward(const Args &a, const GradPlan &p, const GradMaps &maps, cud
   const Items<false> by_rows = {queries, a.causal};
   const float *const largest = p.largest;
   e = launch_kernel(k_delta<T, D>, DELTA_BLOCKS, DELTA_THREADS, 0, s, false, a, p.largest);
-  if (e == cudaSuccess) e = launch_kernel(k_grad_kv<T, D>, SMS, GRAD_THREADS, GradKv<D>::SMEM, s, false, a, by_keys, p.cut, largest, maps);
-  if (e == cudaSuccess && a.n_tokens > queries) e = launch_kernel(k_join_grad<T, D, true>, SMS * (2 * TILE / 32), JOIN_THREADS, 0, s, true, a, by_keys, p.cut, largest);
-  if (e == cudaSuccess) e = launch_kernel(k_grad_q<T, D>, SMS, GRAD_THREADS, GradQ<D>::SMEM, s, false, a, by_rows, p.cut, largest, maps);
-  if (e == cudaSuccess && a.n_tokens > TILE) e = launch_kernel(k_join_grad<T, D, false>, SMS * (TILE / 32), JOIN_THREADS, 0, s, true, a, by_rows, p.cut, largest);
+  // each may start while the one before it ends: the first waits for e, the second for nothing, the third for both
+  if (e == cudaSuccess) e = launch_kernel(k_grad_kv<T, D>, SMS, GRAD_THREADS, GradKv<D>::SMEM, s, true, a, by_keys, p.kv, largest, maps);
+  if (e == cudaSuccess) e = launch_kernel(k_grad_q<T, D>, SMS, GRAD_THREADS, GradQ<D>::SMEM, s, true, a, by_rows, p.q, largest, maps);
+  if (e == cudaSuccess && a.n_tokens > queries)          // (else no item has more than a tile)
+    e = launch_kernel(k_join_grad<T, D>, JOIN_KV + JOIN_Q, JOIN_THREADS, 0, s, true, a, by_keys, by_rows, p.kv, p.q, largest);
   return e;
 }
 
