@@ -327,6 +327,16 @@ template <typename T> __device__ __forceinline__ uint32_t finite_part(uint32_t t
   return two & ~((x >> 15) * 0xFFFFu);
 }
 
+template <typename T> __device__ __forceinline__ uint32_t zero_times(uint32_t x, uint32_t sum);
+template <> __device__ __forceinline__ uint32_t zero_times<__half>(uint32_t x, uint32_t sum) {
+  asm("fma.rn.f16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(x), "r"(0));
+  return sum;
+}
+template <> __device__ __forceinline__ uint32_t zero_times<__nv_bfloat16>(uint32_t x, uint32_t sum) {
+  asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(sum) : "r"(x), "r"(0));
+  return sum;
+}
+
 // A tile's rows whose product is with weights of 0 where they are out of sight (one warp): 0 x infinity would be NaN.  Rows from
 // `live` on are zeroed; where some rows are hidden from some, so are values that are not finite, and the numbers of their rows
 // set in `bad`.
@@ -337,15 +347,15 @@ __device__ __forceinline__ void clean_tile(unsigned char *tile, int lane, int li
   for (int i = 0; i < 4; i++) bad[i] = 0;
   for (int i = max(0, live) * PER + lane; i < TILE * PER; i += 32) *(uint4 *)(tile + tile_at<128>(i / PER, i % PER)) = make_uint4(0, 0, 0, 0);
   if (!look) return;
-  // first whether there are any, in no order
-  uint32_t any = 0;
+  // first whether there are any, in no order: 0 times each, added up, is NaN then
+  uint32_t sum[4] = {0, 0, 0, 0};
   __syncwarp();
 #pragma unroll 16
   for (int i = lane; i < TILE * PER; i += 32) {
     const uint4 v = *(const uint4 *)(tile + i * 16);
-    any |= not_finite<T>(v.x) | not_finite<T>(v.y) | not_finite<T>(v.z) | not_finite<T>(v.w);
+    sum[0] = zero_times<T>(v.x, sum[0]), sum[1] = zero_times<T>(v.y, sum[1]), sum[2] = zero_times<T>(v.z, sum[2]), sum[3] = zero_times<T>(v.w, sum[3]);
   }
-  if (!__any_sync(~0u, any)) return;
+  if (!__any_sync(~0u, not_finite<T>(sum[0]) | not_finite<T>(sum[1]) | not_finite<T>(sum[2]) | not_finite<T>(sum[3]))) return;
 #pragma unroll 1
   for (int row = 0; row < TILE; row++) {
     bool some = false;
@@ -420,7 +430,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
   uint32_t *const tmem_at = (uint32_t *)(tops + 512);
   volatile int *const dead = (volatile int *)(tmem_at + 1);
   void *const scratch = tops;                          // (done with before the first maximum)
-  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 16 * 4 + 2048 + 8 <= Fwd<D>::BEHIND && SCRATCH <= 2048, "room behind the ring");
+  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 16 * 4 + 2048 + 8 <= Fwd<D>::BEHIND && SCRATCH <= 2048 && QUEUE * sizeof(Item) % 8 == 0, "room behind the ring");
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), q_at = smem_u32(qs), ring_at = smem_u32(ring);
   const Pages &maps = all_maps.kv;
@@ -1053,7 +1063,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join(const Args a, const Items
     for (int e = 0; e < E; e++) acc[e].x *= keep, acc[e].y *= keep, acc[e].z *= keep, acc[e].w *= keep;
 #pragma unroll
     for (int k = 0; k < 2; k++) {
-      if (!(ml[k].x == -INFINITY)) {                    // (a part of no tiles has no values)
+      if (ml[k].x != -INFINITY || ml[k].y != 0.f) {     // (a part of no tiles has no values; one of NaN scores has a sum of NaN)
         const float f = exp2_fast(ml[k].x - from);
         l += f * ml[k].y;
 #pragma unroll
@@ -1226,7 +1236,7 @@ template <typename T, int D> struct Products {
 // present ones into weights: nothing waits for a second buffer.  Warps 0..15: a thread for a key and a quarter of a tile's rows.
 template <int D> struct GradKv {
   static constexpr int BYTES = TILE * D * 2, STAGES = D == 64 ? 8 : 5, STATS = 2;       // tiles of queries or dout; of lse and e
-  static constexpr int BEHIND = 1024, SMEM = (2 + STAGES) * BYTES + STATS * 2 * TILE * 4 + BEHIND;
+  static constexpr int BEHIND = D == 64 ? 1088 : 1024, SMEM = (2 + STAGES) * BYTES + STATS * 2 * TILE * 4 + BEHIND;
 };
 
 template <typename T, int D>
@@ -1238,10 +1248,11 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
   uint64_t *const bars = (uint64_t *)(stats + STATS * 2 * TILE);
   constexpr int BARS = 16 + STAGES + STATS + 2 * QUEUE + 9;
   Item *const queue = (Item *)(bars + BARS);
-  uint32_t *const tmem_at = (uint32_t *)(queue + QUEUE);
+  uint32_t *const bad_rows = (uint32_t *)(queue + QUEUE);                               // [STATS][4]: rows of dout with values that are not finite
+  uint32_t *const tmem_at = bad_rows + 4 * STATS;
   volatile int *const dead = (volatile int *)(tmem_at + 1);
   void *const scratch = (void *)(tmem_at + 2);
-  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 8 + SCRATCH <= GradKv<D>::BEHIND, "room behind the ring");
+  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 16 * STATS + 8 + SCRATCH <= GradKv<D>::BEHIND && QUEUE * sizeof(Item) % 8 == 0, "room behind the ring, and its alignment");
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), kv_at = smem_u32(kv), ring_at = smem_u32(ring);
   // slots of the ring: a tile's queries, its dout, the next one's queries, ...  Barriers are a ring for each kind, so that who waits for
@@ -1359,29 +1370,45 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
       int tiles = 0;
       while (next_all(i)) {
         float x[4];
+        bool odd = false;                              // the asked tile has rows with lse or e that is not finite
         auto ask = [&](int t) {                        // of rows lane, lane + 32, ... of a tile
           const int q0 = first_query(i, t), live = min(items.q, i.n - q0) * a.group;
 #pragma unroll
           for (int k = 0; k < 4; k++) {
             const int r = lane + k * 32, query = r / a.in_group;
             x[k] = none;
-            if (r < live) x[k] = src[((int64_t)i.first + q0 + query) * a.q_heads + i.kh * a.group + r - query * a.group] * factor_of + shift;
+            if (r < live) x[k] = src[((int64_t)i.first + q0 + query) * a.q_heads + i.kh * a.group + r - query * a.group];
           }
+        };
+        auto give = [&](int t, float *to) {            // to shared memory, in the units of the weights
+          const int live = min(items.q, i.n - first_query(i, t)) * a.group;
+          odd = false;
+#pragma unroll
+          for (int k = 0; k < 4; k++) {
+            const bool there = lane + k * 32 < live;
+            odd |= there && !isfinite(x[k]);
+            to[lane + k * 32] = there ? x[k] * factor_of + shift : none;
+          }
+          odd = __any_sync(~0u, odd);
         };
         ask(i.tile0);
         for (int t = i.tile0; t < i.tile1 && alive; t++, tiles++) {
           const int slot = 2 * tiles + which, q0 = first_query(i, t), live = min(items.q, i.n - q0) * a.group;
           if (tiles >= STATS) need_all(read(tiles % STATS), tiles / STATS - 1);
           if (!alive) break;
-#pragma unroll
-          for (int k = 0; k < 4; k++) stats[(tiles % STATS * 2 + which) * TILE + lane + k * 32] = x[k];
+          give(t, stats + (tiles % STATS * 2 + which) * TILE);
+          const bool look = odd && hides(i, q0);       // a row with values that are not finite has such an lse (queries) or e (dout)
           if (t + 1 < i.tile1) ask(t + 1);
           need_all(full(slot), slot / 8);
           if (!alive) break;
-          if (hides(i, q0) || live < box_rows) {
-            uint32_t bad[4];
-            clean_tile<T, D>(ring + slot % STAGES * BYTES, lane, live, hides(i, q0), bad);
+          uint32_t bad[4] = {0, 0, 0, 0};
+          if (look || live < box_rows) {
+            clean_tile<T, D>(ring + slot % STAGES * BYTES, lane, live, look, bad);
             fence_async();
+          }
+          if (which && lane == 0) {
+#pragma unroll
+            for (int k = 0; k < 4; k++) bad_rows[tiles % STATS * 4 + k] = bad[k];
           }
           __syncwarp();
           if (lane == 0) bar_arrive(ready(slot));
@@ -1475,9 +1502,10 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
         }
         need(ready(2 * tiles + 1), tiles / 4);                  // (e)
         if (masked) {
-          // (dout has lost its infinite and NaN values here: e has them, and makes NaN of the weights of rows that have some)
+          // (dout has lost its infinite and NaN values here: weights of rows that had some become NaN)
+          const uint32_t bad = bad_rows[tiles % STATS * 4 + w];
 #pragma unroll
-          for (int c = 0; c < 32; c++) p[c] = c < first_seen ? 0 : __float_as_uint(fmaf(0.f, ne[c], __uint_as_float(p[c])));
+          for (int c = 0; c < 32; c++) p[c] = c < first_seen ? 0 : bad >> c & 1 ? 0x7FFFFFFFu : p[c];
         }
 #pragma unroll
         for (int c = 0; c < 32; c += 2) pk[c / 2] = pack<T>(__uint_as_float(p[c]), __uint_as_float(p[c + 1]));
@@ -1585,7 +1613,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
   uint32_t *const tmem_at = (uint32_t *)(queue + QUEUE);
   volatile int *const dead = (volatile int *)(tmem_at + 1);
   void *const scratch = (void *)(tmem_at + 2);
-  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 8 + SCRATCH <= GradQ<D>::BEHIND, "room behind the ring");
+  static_assert(BARS * 8 + QUEUE * sizeof(Item) + 8 + SCRATCH <= GradQ<D>::BEHIND && QUEUE * sizeof(Item) % 8 == 0, "room behind the ring, and its alignment");
   const int tid = threadIdx.x, warp = __shfl_sync(~0u, tid / 32, 0), lane = tid % 32;
   const uint32_t bar0 = smem_u32(bars), rows_at = smem_u32(rows), ring_at = smem_u32(ring);
   // a ring of barriers for keys and one for values: who waits for either sees each of its phases
@@ -1757,16 +1785,23 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
     const bool aligned = rows_aligned(a.dq);
     int tiles = 0;
     uint32_t done = 0;
-    Item i;
-    while (next_all(i)) {
-      const int query = i.t * items.q + in_tile, limit = a.causal ? min(i.keys, query + 1) : i.keys, clear = seen_by_all(a, i, i.t * items.q);
-      const bool valid = in_tile < items.q && query < i.n;
-      const int64_t row = (int64_t)i.first + query;
-      float nl = 0.f, ne = 0.f;
-      if (valid) {
-        const int64_t at = row * a.q_heads + i.kh * a.group + head_in;
-        nl = WEIGHT_SHIFT<T> - a.lse[at] * 1.4426950408889634f, ne = -a.delta[at] * dp_scale;
+    Item i = {};
+    float nl = 0.f, ne = 0.f;
+    auto ask = [&] {                                     // the item's lse and e of this row
+      const int query = i.t * items.q + in_tile;
+      if (in_tile < items.q && query < i.n) {
+        const int64_t at = ((int64_t)i.first + query) * a.q_heads + i.kh * a.group + head_in;
+        nl = a.lse[at], ne = a.delta[at];
       }
+    };
+    bool more = next_all(i);
+    if (more) ask();
+    while (more) {
+      const int query = i.t * items.q + in_tile, limit = a.causal ? min(i.keys, query + 1) : i.keys, clear = seen_by_all(a, i, i.t * items.q);
+      const bool valid = in_tile < items.q && query < i.n, whole = i.tile0 == 0 && i.tile1 == i.tiles;
+      const int64_t row = (int64_t)i.first + query;
+      const int head = i.kh * a.group + head_in, first_part = i.tile0 == 0;
+      nl = WEIGHT_SHIFT<T> - nl * 1.4426950408889634f, ne = -ne * dp_scale;
       for (int t = i.tile0; t < i.tile1; t++, tiles++) {
         const bool masked = (t + 1) * TILE > clear;
         const int seen = limit - t * TILE - w * 32;
@@ -1802,20 +1837,22 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
         bar_arrive(ds_full);
       }
       if (!alive) break;
-      alive = __all_sync(~0u, bar_wait(o_full, done & 1, dead));
-      if (!alive) break;
-      done++;
-      tc_after();
-      const bool whole = i.tile0 == 0 && i.tile1 == i.tiles;
-      if (w < D / 32) {
-        float4 *const part = whole ? nullptr : cut.o + (((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * (D / 4) + w * 8) * TILE + r;
-        store_row<T, 32>(dq_at + lanes + w * 32, row_at<T>(a.dq, row, i.kh * a.group + head_in) + w * 32, part, valid, aligned, a.scale / factor);
-      }
-      tc_before();
-      bar_arrive(o_free);
       __syncwarp();
       if (lane == 0) bar_arrive(taken(turn_of_queue));
       turn_of_queue++;
+      more = next_all(i);                                // (given as soon as this item's tiles have been asked for)
+      if (!alive) break;
+      if (more) ask();                                   // arrives while the last products run and the results are stored
+      need_all(o_full, done);
+      if (!alive) break;
+      done++;
+      tc_after();
+      if (w < D / 32) {
+        float4 *const part = whole ? nullptr : cut.o + (((int64_t)blockIdx.x * 2 + first_part) * (D / 4) + w * 8) * TILE + r;
+        store_row<T, 32>(dq_at + lanes + w * 32, row_at<T>(a.dq, row, head) + w * 32, part, valid, aligned, a.scale / factor);
+      }
+      tc_before();
+      bar_arrive(o_free);
     }
   }
   tc_before();

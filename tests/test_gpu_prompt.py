@@ -270,6 +270,57 @@ def test_values_out_of_sight(D, bad):
                 assert torch.equal(seen[:, :5], was[:, :5]) and torch.equal(seen[:, 6:], was[:, 6:])
 
 
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("D,group", [(64, 4), (128, 4), (128, 3)])
+def test_gradients_out_of_sight(D, group, bad):
+    """One infinite or NaN value of a sequence: gradients that it has no part in are what they were."""
+    lens, KV = [100, 200, 300], 2
+    H = KV * group
+    q, k, v, starts = problem(D, lens, H, KV, D, "bfloat16")
+    at, dout = ints(starts), rand(gen(2), *q.shape, dtype="bfloat16")
+
+    def grads(q, k, v, dout):
+        out, lse = serving.prompt_attention(q, k, v, at)
+        return serving.prompt_attention_grad(dout, q, k, v, out, lse, at)
+    want = grads(q, k, v, dout)
+    for row in (300, 427, 428, 450, 511, 599):
+        for name in ("q", "k", "v", "dout"):
+            x = {"q": q, "k": k, "v": v, "dout": dout}
+            x[name] = x[name].clone()
+            x[name][row, 0, 5] = bad
+            got = grads(**x)
+            keep = [torch.ones(600, n, dtype=torch.bool, device="cuda") for n in (H, KV, KV)]
+            if name in ("q", "dout"):                            # that query's own, and those of the keys it sees
+                keep[0][row, 0] = keep[1][300:row + 1, 0] = keep[2][300:row + 1, 0] = False
+            else:                                                # those of the queries that see it, and of all their keys
+                keep[0][row:, :group] = keep[1][300:, 0] = False
+                if name == "k":
+                    keep[2][300:, 0] = False
+            for a, b, m in zip(got, want, keep):
+                assert torch.equal(a[m], b[m]), (name, row)
+            if name == "dout":
+                assert not torch.isfinite(got[2][300:row + 1, 0, 5]).any()
+            if bad != bad:                                       # (an infinite key may weigh nothing)
+                assert torch.isnan(got[0][row, 0]).all(), (name, row)
+
+
+@pytest.mark.parametrize("lens", [[100], [3000], [40, 2500, 7]])
+@pytest.mark.parametrize("D", [64, 128])
+def test_a_query_of_nan(D, lens):
+    """Its row is NaN, cut or whole, wherever it is; the others are what they were."""
+    q, k, v, starts = problem(D, lens, 4, 1, D, "bfloat16")
+    at = ints(starts)
+    out, lse = serving.prompt_attention(q, k, v, at)
+    rows = sorted({0, 1, 63, 64, starts[-1] // 2, starts[-1] - 1} & set(range(starts[-1])))
+    x = q.clone()
+    x[rows, 2, 7] = float("nan")
+    o, l = serving.prompt_attention(x, k, v, at)
+    keep = torch.ones(starts[-1], 4, dtype=torch.bool, device="cuda")
+    keep[rows, 2] = False
+    assert torch.isnan(o[~keep]).all() and torch.isnan(l[~keep]).all()
+    assert torch.equal(o[keep], out[keep]) and torch.equal(l[keep], lse[keep])
+
+
 def test_large_and_equal_scores():
     """Scores of thousands, and rows whose scores are all alike."""
     D, H, n = 128, 4, 300
