@@ -646,6 +646,35 @@ def test_beyond_32_bit_offsets():
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+def test_many_sequences():
+    """As many as a call takes, of one token: each is its own value."""
+    n = 65535
+    g = gen(1)
+    q, k, v = (rand(g, n, 2, 64, dtype="bfloat16") for _ in range(3))
+    at = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    out, lse = serving.prompt_attention(q, k, v, at)
+    assert torch.equal(out, v)
+    assert ((lse.double() - (q.double() * k.double()).sum(-1) / 8).abs() <= 1e-5).all()      # (of scores below 8, in 32 bits)
+    dq, dk, dv = serving.prompt_attention_grad(q, q, k, v, out, lse, at)
+    # p = 1 to 2^-20 (lse and the score are 32-bit sums of one magnitude), dp - e is 0 to 128 2^-24 of terms below 30
+    assert torch.equal(dv, q) and float(dq.abs().max()) < 1e-2 and float(dk.abs().max()) < 1e-2
+    cache = serving.PagedCache(k[:, None], v[:, None])                                         # a page for each
+    got = serving.chunk_attention(q, at, cache, at[:-1, None].contiguous(), torch.ones(n, dtype=torch.int32, device="cuda"))
+    assert torch.equal(got[0], v)
+
+
+def test_chunks_without_keys():
+    """No pages at all, no lengths, no tokens."""
+    cache = serving.PagedCache.empty(0, 16, 2, 64, torch.bfloat16)
+    q = rand(gen(1), 7, 4, 64, dtype="bfloat16")
+    out, lse = serving.chunk_attention(q, ints([0, 3, 7]), cache, torch.zeros(2, 0, dtype=torch.int32, device="cuda"), ints([0, 0]))
+    assert (out == 0).all() and (lse == float("-inf")).all()
+    out, lse = serving.chunk_attention(q[:0], ints([0]), cache, torch.zeros(0, 3, dtype=torch.int32, device="cuda"), ints([]))
+    assert out.shape == (0, 4, 64)
+    out, lse = serving.chunk_attention(q, ints([0]), cache, torch.zeros(0, 3, dtype=torch.int32, device="cuda"), ints([]))
+    assert (out == 0).all() and (lse == float("-inf")).all()
+
+
 def test_a_long_sequence():
     """Keys by the tens of thousands: the sums' own value (every value row is its token's number / 2^16), and a cut in every way."""
     n, H, KV, D = 40000, 4, 2, 64
