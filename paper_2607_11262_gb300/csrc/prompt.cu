@@ -6,7 +6,6 @@
 // p_ij = exp(s_ij - lse_i), e_i = dout_i . out_i - dlse_i and ds_ij = p_ij (dout_i . v_j - e_i): dv_j = sum p_ij dout_i,
 // dq_i = scale sum ds_ij k_j, dk_j = scale sum ds_ij q_i.
 #include <algorithm>
-#include <climits>
 #include <cmath>
 #include <type_traits>
 
@@ -673,11 +672,9 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
         const Half x = half_of(a, items, i, h);
         const int both = min(x.count, half_of(a, items, i, !h).count), n = i.tile1 - i.tile0;
         take();
-        const int clear = a.causal ? seen_by_all(a, i, i.t * items.q) : INT_MAX;   // tiles that end after it are cleaned of values: before their scores
         if (x.count) {
           need(q_full(h), items_done);
           need(full(slot), slot / 8);
-          if ((i.tile0 + 1) * TILE > clear) need(ready(tiles), tiles / 4);
           if (!alive) break;
           tc_after();
           qk(slot, 0);
@@ -690,10 +687,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           const uint32_t sv = slot++, sk = slot;
           const int seen = x.seen - (i.tile0 + j) * TILE;
           need(ready(tiles), tiles / 4);
-          if (j + 1 < x.count) {
-            need(full(sk), sk / 8), slot++;
-            if ((i.tile0 + j + 2) * TILE > clear) need(ready(tiles + 1), (tiles + 1) / 4);
-          }
+          if (j + 1 < x.count) need(full(sk), sk / 8), slot++;
           if (j == 0 && items_done) need(o_free(h), items_done - 1);
           if (!alive) break;
           const uint32_t *const bad = bad_rows + tiles % 4 * 4;
@@ -769,7 +763,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
         wait(s_full(h, y), turn);
         tc_after();
         const int t = i.tile0 + j, nv = limit - t * TILE - y * 64;
-        const bool masked = (t + 1) * TILE > clear;
+        const bool masked = (t + 1) * TILE > clear, cleaned = a.causal && (t + 1) * TILE > clear_of_all;
         uint32_t s[32], pk[32];
         auto fetch = [&](int c) {
           tc_ld(s, scores(h) + lanes + y * 64 + c);
@@ -805,6 +799,8 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           fetch(0), see();
           if (j) weigh(0, m == -INFINITY ? 0.f : m);       // (by the maximum so far, which seldom turns out to be too low)
           fetch(32), see();
+          if (cleaned) wait(ready(tiles + j), (tiles + j) / 4);
+          if (!alive) break;
           const float big = fmaxf(top[0], top[1]) * sl2;
           const bool raise = j == 0 || big > m + RAISE || (m == -INFINITY && big > m);
           if (__any_sync(~0u, raise)) {
@@ -829,6 +825,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           }
         } else if (j == 0) {                               // the maximum first, then weights
           fetch(0), see(), fetch(32), see();
+          if (cleaned) wait(ready(tiles + j), (tiles + j) / 4);
           const float theirs = exchange(fmaxf(top[0], top[1]));
           alive = alive && !isnan(theirs);                 // (a maximum is none)
           if (!alive) break;
@@ -841,6 +838,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           const float old = m == -INFINITY ? 0.f : m;
           fetch(0), see(), weigh(0, old);
           fetch(32), see();
+          if (cleaned) wait(ready(tiles + j), (tiles + j) / 4);
           *mine = alive ? fmaxf(top[0], top[1]) : NAN;
           weigh(32, old);
           meet();
@@ -868,10 +866,9 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           }
         }
         const float from = m == -INFINITY ? 0.f : m;
-        if (a.causal && (t + 1) * TILE > clear_of_all) {
-          // values that are not finite: each for the rows that see it, before the products are added (the tile was clean before its
-          // scores were asked for, so this wait is over)
-          bar_wait(ready(tiles + j), (tiles + j) / 4 & 1, dead);
+        if (cleaned) {
+          // values that are not finite: each for the rows that see it, before the products are added (the tile is clean: waited for
+          // above, before both threads of a row agree to go on)
           const uint32_t *const bad = bad_rows + (tiles + j) % 4 * 4;
           if (bad[0] | bad[1] | bad[2] | bad[3]) {
 #pragma unroll 1
