@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
   auto q_full = [&](int h) { return bar0 + (B0 + 4 + h) * 8; };
   auto q_empty = [&](int h) { return bar0 + (B0 + 6 + h) * 8; };
   auto s_full = [&](int h, int y) { return bar0 + (B0 + 8 + (APART ? 2 * y : 0) + h) * 8; };   // (of half the keys, where those are apart)
-  auto p_full = [&](int h, int x) { return bar0 + (B0 + 12 + h * 2 + x) * 8; };         // weights of half the keys
+  auto p_full = [&](int h, int x) { return bar0 + (B0 + 12 + h * 2 + x) * 8; };         // weights of half the keys of a tile
   auto o_full = [&](int h) { return bar0 + (B0 + 16 + h) * 8; };
   auto o_free = [&](int h) { return bar0 + (B0 + 18 + h) * 8; };
   auto my_turn = [&](int h) { return bar0 + (B0 + 20 + h) * 8; };
@@ -463,7 +463,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
     for (int s = 0; s < STAGES; s++) bar_init(empty(s), 2);
     for (int v = 0; v < 4; v++) bar_init(ready(v), 1);
     for (int h = 0; h < 2; h++) {
-      bar_init(q_full(h), 1), bar_init(q_empty(h), 1), bar_init(s_full(h, 0), 1), bar_init(bar0 + (B0 + 10 + h) * 8, 1), bar_init(p_full(h, 0), 128), bar_init(p_full(h, 1), 128);
+      bar_init(q_full(h), 1), bar_init(q_empty(h), 1), bar_init(s_full(h, 0), 1), bar_init(bar0 + (B0 + 10 + h) * 8, 1), bar_init(p_full(h, 0), APART ? 128 : 256), bar_init(p_full(h, 1), APART ? 128 : 256);
       bar_init(o_full(h), 1), bar_init(o_free(h), ROW_THREADS / 2), bar_init(my_turn(h), 1), bar_init(ended + 8 * h, 1);
     }
     for (int i = 0; i < QUEUE; i++) bar_init(given(i), 1), bar_init(taken(i), ROW_WARPS + 3);
@@ -702,9 +702,11 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
             if (!alive) break;
             tc_after();
 #pragma unroll
-            for (int k = 4 * y; k < 4 * y + 4; k++)
+            for (int x = 0; x < 4; x++) {
+              const int k = APART ? 4 * y + x : x / 2 * 4 + 2 * y + x % 2;   // the first or last 32 keys of either half, or a half's
               if (k == 0 || (APART && k == 4) || k * 16 < seen)
                 tc_mma_t(o_at + (APART ? y * 64 : 0), s_at + k / 4 * 64 + k % 4 * 8, v + k * (2048 >> 4), OPERAND_HI, PV, add || (APART ? k % 4 : k) > 0);
+            }
             if (APART && j + 1 < x.count) qk(sk, y);
           }
           turn++;
@@ -764,7 +766,8 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
         tc_after();
         const int t = i.tile0 + j, nv = limit - t * TILE - y * 64;
         const bool masked = (t + 1) * TILE > clear, cleaned = a.causal && (t + 1) * TILE > clear_of_all;
-        uint32_t s[32], pk[32];
+        // The maximum first, then weights, 32 scores at a time and read twice: more registers are not to be had.
+        uint32_t s[32];
         auto fetch = [&](int c) {
           tc_ld(s, scores(h) + lanes + y * 64 + c);
           tc_ld_wait();
@@ -775,95 +778,44 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           }
         };
         float top[2] = {-INFINITY, -INFINITY};
-        auto see = [&] {
+#pragma unroll
+        for (int c = 0; c < 64; c += 32) {
+          fetch(c);
 #pragma unroll
           for (int z = 0; z < 32; z += 4) {
             top[0] = max3(top[0], __uint_as_float(s[z]), __uint_as_float(s[z + 1]));
             top[1] = max3(top[1], __uint_as_float(s[z + 2]), __uint_as_float(s[z + 3]));
           }
-        };
-        float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-        auto weigh = [&](int c, float from) {
-          const float2 scale2 = make_float2(sl2, sl2), from2 = make_float2(-from, -from);
-#pragma unroll
-          for (int z = 0; z < 32; z += 2) {
-            float2 e = fma2(make_float2(__uint_as_float(s[z]), __uint_as_float(s[z + 1])), scale2, from2);
-            e.x = exp2_fast(e.x), e.y = exp2_fast(e.y);
-            part[z / 2 & 1] = add2(part[z / 2 & 1], e);
-            pk[(c + z) / 2] = pack<T>(e.x, e.y);
-          }
-        };
-        if (APART) {
-          // one thread's own: the maximum, then weights
-          if (!alive) break;
-          fetch(0), see();
-          if (j) weigh(0, m == -INFINITY ? 0.f : m);       // (by the maximum so far, which seldom turns out to be too low)
-          fetch(32), see();
-          if (cleaned) wait(ready(tiles + j), (tiles + j) / 4);
-          if (!alive) break;
-          const float big = fmaxf(top[0], top[1]) * sl2;
-          const bool raise = j == 0 || big > m + RAISE || (m == -INFINITY && big > m);
-          if (__any_sync(~0u, raise)) {
-            const float to = raise ? big : m, f = raise ? exp2_fast(m - to) : 1.f;
-            if (j) {
-              uint32_t o[16];
-#pragma unroll 1
-              for (int c = 0; c < D; c += 16) {
-                tc_ld16(o, sums(h) + y * 64 + lanes + c);
-                tc_ld_wait();
-#pragma unroll
-                for (int z = 0; z < 16; z++) o[z] = __float_as_uint(__uint_as_float(o[z]) * f);
-                tc_st16(sums(h) + y * 64 + lanes + c, o);
-              }
-              l *= f;
-            }
-            m = to;
-            part[0] = part[1] = make_float2(0.f, 0.f);
-            weigh(32, m == -INFINITY ? 0.f : m), fetch(0), weigh(0, m == -INFINITY ? 0.f : m);
-          } else {
-            weigh(32, m == -INFINITY ? 0.f : m);
-          }
-        } else if (j == 0) {                               // the maximum first, then weights
-          fetch(0), see(), fetch(32), see();
-          if (cleaned) wait(ready(tiles + j), (tiles + j) / 4);
-          const float theirs = exchange(fmaxf(top[0], top[1]));
-          alive = alive && !isnan(theirs);                 // (a maximum is none)
-          if (!alive) break;
-          m = fmaxf(fmaxf(top[0], top[1]), theirs) * sl2;
-          const float from = m == -INFINITY ? 0.f : m;
-          weigh(32, from), fetch(0), weigh(0, from);
-        } else {
-          // weights by the maximum so far, which seldom turns out to be too low; both threads know in the end.  (The other one has
-          // read what this one writes over: the scores were asked for after its weights.)
-          const float old = m == -INFINITY ? 0.f : m;
-          fetch(0), see(), weigh(0, old);
-          fetch(32), see();
-          if (cleaned) wait(ready(tiles + j), (tiles + j) / 4);
-          *mine = alive ? fmaxf(top[0], top[1]) : NAN;
-          weigh(32, old);
+        }
+        if (cleaned) wait(ready(tiles + j), (tiles + j) / 4);
+        float big = fmaxf(top[0], top[1]);
+        if (!APART) {
+          if (j == 0) meet();                              // (later on the other one has read what was there: the scores were asked for
+          *mine = alive ? big : NAN;                       // after its weights)
           meet();
           const float theirs = *others;
-          alive = alive && !isnan(theirs);
-          if (!alive) break;
-          const float big = fmaxf(fmaxf(top[0], top[1]), theirs) * sl2;
-          const bool raise = big > m + RAISE || (m == -INFINITY && big > m);
-          if (__any_sync(~0u, raise)) {
-            const float to = raise ? big : m, f = raise ? exp2_fast(m - to) : 1.f;
-            uint32_t o[16];
+          alive = alive && !isnan(theirs);                 // (a maximum is none)
+          big = fmaxf(big, theirs);
+        }
+        if (!alive) break;
+        big *= sl2;
+        const bool raise = big > m + RAISE || (m == -INFINITY && big > m);
+        if (j == 0) {
+          m = big;
+        } else if (__any_sync(~0u, raise)) {
+          const float to = raise ? big : m, f = raise ? exp2_fast(m - to) : 1.f;
+          uint32_t o[16];
 #pragma unroll 1
-            for (int c = y * (D / 2); c < (y + 1) * (D / 2); c += 16) {
-              tc_ld16(o, sums(h) + lanes + c);
-              tc_ld_wait();
+          for (int c = APART ? 0 : y * (D / 2); c < (APART ? D : (y + 1) * (D / 2)); c += 16) {
+            const uint32_t at = sums(h) + (APART ? y * 64 : 0) + lanes + c;
+            tc_ld16(o, at);
+            tc_ld_wait();
 #pragma unroll
-              for (int z = 0; z < 16; z++) o[z] = __float_as_uint(__uint_as_float(o[z]) * f);
-              tc_st16(sums(h) + lanes + c, o);
-            }
-            l *= f;
-            m = to;
-            const float from = m == -INFINITY ? 0.f : m;
-            part[0] = part[1] = make_float2(0.f, 0.f);
-            fetch(0), weigh(0, from), fetch(32), weigh(32, from);
+            for (int z = 0; z < 16; z++) o[z] = __float_as_uint(__uint_as_float(o[z]) * f);
+            tc_st16(at, o);
           }
+          l *= f;
+          m = to;
         }
         const float from = m == -INFINITY ? 0.f : m;
         if (cleaned) {
@@ -904,10 +856,25 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
             if (!APART) exchange(0.f);                     // both have read the scores before weights overwrite them
           }
         }
-        tc_st(scores(h) + lanes + y * 64, pk);
-        tc_st_wait();
-        tc_before();
-        bar_arrive(p_full(h, y));
+        const float2 scale2 = make_float2(sl2, sl2), from2 = make_float2(-from, -from);
+        float2 part[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+        for (int c = 0; c < 64; c += 32) {                 // the products with the first 32 of both start under the others
+          fetch(c);
+#pragma unroll
+          for (int z = 0; z < 32; z += 2) {
+            float2 e = fma2(make_float2(__uint_as_float(s[z]), __uint_as_float(s[z + 1])), scale2, from2);
+            e.x = exp2_fast(e.x), e.y = exp2_fast(e.y);
+            part[z / 2 & 1] = add2(part[z / 2 & 1], e);
+            s[z / 2] = pack<T>(e.x, e.y);
+          }
+          tc_st16(scores(h) + lanes + y * 64 + c / 2, s);
+          if (!APART || c) {
+            tc_st_wait();
+            tc_before();
+            bar_arrive(p_full(h, APART ? y : c / 32));
+          }
+        }
         const float2 sum = add2(part[0], part[1]);
         l += sum.x + sum.y;
       }
