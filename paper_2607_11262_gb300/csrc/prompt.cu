@@ -94,7 +94,8 @@ __device__ __forceinline__ Seq sequence(const Args &a, int b) {
 // Items of rows (BY_KEYS false) and of keys: how many a sequence has, the tiles of one, its weight and that of all before it.
 template <bool BY_KEYS> struct Items {
   int q, causal;         // queries of an item (of a tile of rows, by keys)
-  __device__ __forceinline__ int lead() const { return LEAD * (BY_KEYS ? q : TILE); }
+  int beside = LEAD;
+  __device__ __forceinline__ int lead() const { return beside * (BY_KEYS ? q : TILE); }
   __device__ __forceinline__ int count(const Seq &s) const { return BY_KEYS ? (s.keys + TILE - 1) / TILE : (s.n + q - 1) / q; }
   // keys that the item's last query sees, or queries that see the item's first key (rounded to whole items)
   __device__ __forceinline__ int seen(const Seq &s, int t) const {
@@ -262,16 +263,16 @@ __device__ __forceinline__ void tc_st16(uint32_t at, const uint32_t *r) {
                "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(at) : "memory");
 }
 
-// 32 values of a row: in pieces of 32 bytes where rows stand on that grid (half the accesses of 16, and whole sectors).
-template <typename T> __device__ __forceinline__ void store64(T *to, const uint32_t (&w)[16], bool aligned) {
+// Values of a row, two to a word: in pieces of 32 bytes where rows stand on that grid (half the accesses of 16, and whole sectors).
+template <typename T, int N> __device__ __forceinline__ void store_piece(T *to, const uint32_t (&w)[N], bool aligned) {
   if (aligned) {
 #pragma unroll
-    for (int y = 0; y < 16; y += 8)
+    for (int y = 0; y < N; y += 8)
       asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to + 2 * y), "r"(w[y]), "r"(w[y + 1]), "r"(w[y + 2]), "r"(w[y + 3]),
                    "r"(w[y + 4]), "r"(w[y + 5]), "r"(w[y + 6]), "r"(w[y + 7]) : "memory");
   } else {
 #pragma unroll
-    for (int y = 0; y < 16; y++) {
+    for (int y = 0; y < N; y++) {
       T e[2];
       memcpy(e, &w[y], 4);
       to[2 * y] = e[0], to[2 * y + 1] = e[1];
@@ -384,10 +385,25 @@ __device__ __forceinline__ void clean_tile(unsigned char *tile, int lane, int li
 // worked out, and its queries brought, while the rows of the one before store their results.  The maximum that scores are taken against is
 // raised, and what was summed rescaled, only when it has grown by more than 8 (in log 2).  Weights are rounded to the values'
 // type for their product; the sum is of the unrounded ones, all else is in 32 bits.
+//
+// A row's thread reads its scores twice, for the maximum and for the weights: 104 registers to a thread do not hold 64 scores.  The
+// weights of the first 32 keys of both threads are multiplied while those of the others are made (1441 against 1605 us for 16384 tokens,
+// causal, 32 heads on 8 of 128).  At a head of 64 each of the two threads has sums and a maximum of its own, joined at the end
+// (APART): no exchange for each tile, and four streams of scores for the tensor cores instead of two.  A thread with 128 keys of
+// its own takes 1510 us there, but loses on short sequences; weights against the last tile's maximum, mended where it has grown,
+// take 10% more at a head of 128.
+//
+// Bound by the chain of a tile from scores to weights to products, and on short sequences by the ends of items.  16384 tokens of 32
+// heads on 8 of 128 without a mask: 2815 us, 1.56 PFLOP/s, 82% of the rate of a large matrix product; 2300 cycles for a tile of both
+// halves against 2048 of products.  24 sequences of 1024: 288 us causal and 376 not, of which an item's begin and end take 6 of 19 us
+// (both halves are at their ends at the same time; the stores themselves are 5%).  A head of 64: 8192 tokens of 16 heads, causal, 166 us.
 constexpr int ROW_WARPS = 16, ROW_THREADS = ROW_WARPS * 32, BLOCK_THREADS = ROW_THREADS + 128, FWD_THREADS = BLOCK_THREADS, QUEUE = 4;
 constexpr float RAISE = 8.f;
 template <int D> struct Fwd {
   static constexpr bool APART = D == 64;               // sums of their own for either half of a tile's keys
+  static constexpr int PIECE = APART ? 16 : 32;        // columns that a row's results are stored by (the other way round: 2% and 4% more)
+  static constexpr int BESIDE = APART ? 3 : LEAD;      // what an item costs beside its tiles (2 at a head of 64: 184 against 166 us for
+                                                       // 8192 tokens; 3 and 1 at 128: 2 and 14% more for ragged sequences)
   static constexpr int BYTES = TILE * D * 2, STAGES = D == 64 ? 8 : 5, Q = 2 * BYTES;
   static constexpr int BEHIND = 2816, SMEM = Q + STAGES * BYTES + BEHIND;
 };
@@ -416,9 +432,10 @@ __device__ __forceinline__ Half half_of(const Args &a, const Items<false> &items
 __device__ __forceinline__ int seen_by_all(const Args &a, const Item &i, int q0) { return a.causal ? max(0, i.keys - i.n + q0 + 1) : i.keys; }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const Items<false> items, const Cut cut, const __grid_constant__ FwdMaps all_maps) {
+__global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const Items<false> of_call, const Cut cut, const __grid_constant__ FwdMaps all_maps) {
+  const Items<false> items = {of_call.q, of_call.causal, Fwd<D>::BESIDE};
   constexpr bool APART = Fwd<D>::APART;
-  constexpr int BYTES = Fwd<D>::BYTES, STAGES = Fwd<D>::STAGES, COLUMNS = TILE * 128;   // bytes of 64 columns of a tile
+  constexpr int PIECE = Fwd<D>::PIECE, BYTES = Fwd<D>::BYTES, STAGES = Fwd<D>::STAGES, COLUMNS = TILE * 128;   // bytes of 64 columns of a tile
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char *const qs = smem, *const ring = qs + Fwd<D>::Q;
   uint64_t *const bars = (uint64_t *)(ring + STAGES * BYTES);
@@ -902,32 +919,31 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
         T *const dst = row_at<T>(a.out, row, kh * a.group + head_in);
         float4 *const mid = cut.o + part / 256 * (D / 4) * 256 + part % 256;
 #pragma unroll 1
-        for (int c = y * (D / 2); c < (y + 1) * (D / 2) && alive; c += 32) {
-          uint32_t o[32];
-          tc_ld(o, sums(h) + lanes + c);
-          tc_ld_wait();
-          if (APART) {
+        for (int c = y * (D / 2); c < (y + 1) * (D / 2) && alive; c += PIECE) {
+          uint32_t o[PIECE];
+          if constexpr (APART) {
+            uint32_t o1[PIECE];
+            tc_ld16(o, sums(h) + lanes + c);
+            tc_ld16(o1, sums(h) + 64 + lanes + c);
+            tc_ld_wait();
 #pragma unroll
-            for (int part = 0; part < 32; part += 16) {
-              uint32_t o1[16];
-              tc_ld16(o1, sums(h) + 64 + lanes + c + part);
-              tc_ld_wait();
-#pragma unroll
-              for (int z = 0; z < 16; z++) o[part + z] = __float_as_uint(f0 * __uint_as_float(o[part + z]) + f1 * __uint_as_float(o1[z]));
-            }
+            for (int z = 0; z < PIECE; z++) o[z] = __float_as_uint(f0 * __uint_as_float(o[z]) + f1 * __uint_as_float(o1[z]));
+          } else {
+            tc_ld(o, sums(h) + lanes + c);
+            tc_ld_wait();
           }
           if (valid && !whole) {
 #pragma unroll
-            for (int z = 0; z < 32; z += 4) *(uint4 *)(mid + (c + z) / 4 * 256) = make_uint4(o[z], o[z + 1], o[z + 2], o[z + 3]);
+            for (int z = 0; z < PIECE; z += 4) *(uint4 *)(mid + (c + z) / 4 * 256) = make_uint4(o[z], o[z + 1], o[z + 2], o[z + 3]);
           } else if (valid) {
-            uint32_t w[16];
+            uint32_t w[PIECE / 2];
 #pragma unroll
-            for (int z = 0; z < 16; z++) w[z] = pack<T>(__uint_as_float(o[2 * z]) * inv, __uint_as_float(o[2 * z + 1]) * inv);
-            store64<T>(dst + c, w, aligned);
+            for (int z = 0; z < PIECE / 2; z++) w[z] = pack<T>(__uint_as_float(o[2 * z]) * inv, __uint_as_float(o[2 * z + 1]) * inv);
+            store_piece<T>(dst + c, w, aligned);
             if (a.low.data) {
 #pragma unroll
-              for (int z = 0; z < 16; z++) w[z] = pack_low<T>(__uint_as_float(o[2 * z]) * inv, __uint_as_float(o[2 * z + 1]) * inv);
-              store64<T>(row_at<T>(a.low, row, kh * a.group + head_in) + c, w, low_aligned);
+              for (int z = 0; z < PIECE / 2; z++) w[z] = pack_low<T>(__uint_as_float(o[2 * z]) * inv, __uint_as_float(o[2 * z + 1]) * inv);
+              store_piece<T>(row_at<T>(a.low, row, kh * a.group + head_in) + c, w, low_aligned);
             }
           }
           __syncwarp();
@@ -1058,6 +1074,11 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join(const Args a, const Items
 // no atomic adds, and nothing of the size of the scores is ever stored.  Weights p and ds are rounded to the inputs' type for
 // their products; all else is in 32 bits.
 //
+// Bound by the rows' threads and the products of 128 weights, which want as much of shared memory as of the tensor cores: a tile of
+// k_grad_kv takes 1.33 us against 1.07 of its four products, one of k_grad_q 1.15 against 0.8 of its three (0.93 of shared memory's time).
+// 32 heads on 8 of 128, causal: one sequence of 16384 tokens 5.45 ms (1.0 PFLOP/s of the five products, 1.4 of the seven that are done),
+// 24 of 1024 780 us, 8 of 512 to 4096 1.31 ms.  The three kernels start while the one before ends (1024 tokens: 67 us).
+//
 // float16 is short of small numbers: weights are held times 2^10 and ds times the power of two that puts the largest |dout| of the
 // call between 1/2 and 1 (then |ds| stays below 256 times the largest |v|, and what is lost below 2^-24 of it does not
 // count beside the largest).  bfloat16 has the range of 32 bits and needs neither.
@@ -1167,7 +1188,7 @@ __device__ __forceinline__ void store_row(uint32_t at, T *dst, float4 *part, boo
       uint32_t w[16];
 #pragma unroll
       for (int y = 0; y < 16; y++) w[y] = pack<T>(__uint_as_float(o[2 * y]) * factor, __uint_as_float(o[2 * y + 1]) * factor);
-      store64<T>(dst + c, w, aligned);
+      store_piece<T>(dst + c, w, aligned);
     }
     __syncwarp();
   }
