@@ -396,7 +396,7 @@ __device__ __forceinline__ void clean_tile(unsigned char *tile, int lane, int li
 // Bound by the chain of a tile from scores to weights to products, and on short sequences by the ends of items.  16384 tokens of 32
 // heads on 8 of 128 without a mask: 2815 us, 1.56 PFLOP/s, 82% of the rate of a large matrix product; 2300 cycles for a tile of both
 // halves against 2048 of products.  24 sequences of 1024: 288 us causal and 376 not, of which an item's begin and end take 6 of 19 us
-// (both halves are at their ends at the same time; the stores themselves are 5%).  A head of 64: 8192 tokens of 16 heads, causal, 166 us.
+// (both halves are at their ends at the same time; the stores themselves are 5%).  A head of 64: 8192 tokens of 16 heads, causal, 161 us.
 constexpr int ROW_WARPS = 16, ROW_THREADS = ROW_WARPS * 32, BLOCK_THREADS = ROW_THREADS + 128, FWD_THREADS = BLOCK_THREADS, QUEUE = 4;
 constexpr float RAISE = 8.f;
 template <int D> struct Fwd {
@@ -719,8 +719,8 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
             if (!alive) break;
             tc_after();
 #pragma unroll
-            for (int x = 0; x < 4; x++) {
-              const int k = APART ? 4 * y + x : x / 2 * 4 + 2 * y + x % 2;   // the first or last 32 keys of either half, or a half's
+            for (int z = 0; z < 4; z++) {
+              const int k = APART ? 4 * y + z : z / 2 * 4 + 2 * y + z % 2;   // the first or last 32 keys of either half, or a half's
               if (k == 0 || (APART && k == 4) || k * 16 < seen)
                 tc_mma_t(o_at + (APART ? y * 64 : 0), s_at + k / 4 * 64 + k % 4 * 8, v + k * (2048 >> 4), OPERAND_HI, PV, add || (APART ? k % 4 : k) > 0);
             }
@@ -767,10 +767,16 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
     auto wait = [&](uint32_t bar, uint32_t parity) { alive = __all_sync(~0u, bar_wait(bar, parity & 1, dead)) && alive; };
     uint32_t turn = 0, items_done = 0, tiles = 0;
     Item i;
-    while (true) {
+    auto take_item = [&] {                               // the next one; both threads of a row go on with it, or neither
       wait(given(turn_of_queue), turn_of_queue / QUEUE);
       i = queue[turn_of_queue % QUEUE];
-      if (isnan(exchange(0.f)) || !alive || i.tiles == 0) break;
+      const bool on = !isnan(exchange(0.f)) && alive && i.tiles > 0;
+      if (lane == 0) bar_arrive(taken(turn_of_queue));
+      turn_of_queue++;
+      return on;
+    };
+    bool on = take_item();
+    while (on) {
       const Half x = half_of(a, items, i, h);
       const int query = x.q0 + in_half, kh = i.kh;
       const bool valid = in_half < x.queries;
@@ -911,13 +917,18 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
       }
       tiles += i.tile1 - i.tile0;
       const int64_t part = ((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 256 + h * 128 + r;
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      T *const dst = row_at<T>(a.out, row, kh * a.group + head_in);
+      float4 *const mid = cut.o + part / 256 * (D / 4) * 256 + part % 256;
+      if (valid && y == 0) {
+        if (!whole) cut.ml[part] = make_float2(m, l);
+        else if (a.lse) a.lse[row * a.q_heads + kh * a.group + head_in] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+      }
+      on = take_item();                                  // (while the last products are worked out)
       if (x.count) {
         wait(o_full(h), items_done);
         items_done++;
         tc_after();
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        T *const dst = row_at<T>(a.out, row, kh * a.group + head_in);
-        float4 *const mid = cut.o + part / 256 * (D / 4) * 256 + part % 256;
 #pragma unroll 1
         for (int c = y * (D / 2); c < (y + 1) * (D / 2) && alive; c += PIECE) {
           uint32_t o[PIECE];
@@ -951,13 +962,6 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
         tc_before();
         bar_arrive(o_free(h));
       }
-      if (valid && y == 0) {
-        if (!whole) cut.ml[part] = make_float2(m, l);
-        else if (a.lse) a.lse[row * a.q_heads + kh * a.group + head_in] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
-      }
-      __syncwarp();
-      if (lane == 0) bar_arrive(taken(turn_of_queue));
-      turn_of_queue++;
     }
   }
   tc_before();
