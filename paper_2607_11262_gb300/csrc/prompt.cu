@@ -79,7 +79,7 @@ __device__ __forceinline__ Seq sequence(const Args &a, int b) {
   const int from = a.starts[b], to = a.starts[b + 1];
   Seq s;
   s.first = max(0, min(from, a.n_tokens));
-  s.n = max(0, min(to, a.n_tokens) - s.first);
+  s.n = max(s.first, min(to, a.n_tokens)) - s.first;     // (a difference of what lies within the call: starts may be any numbers)
   bool bad = from != s.first || to != s.first + s.n;
   s.keys = s.n;
   if (a.paged) {
@@ -193,6 +193,7 @@ __device__ __forceinline__ Stretch find_stretch(const Args &a, const Items<BY_KE
   }
   __syncthreads();
   s.b = found[0], s.t = found[1], s.pos = places[0];
+  if (s.b < 0) s.x0 = s.x1 = 0;                        // (sequences that overlap without end, from starts that fall: their sum may pass 64 bits)
   return s;
 }
 

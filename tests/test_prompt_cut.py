@@ -91,13 +91,13 @@ def cut(tmp_path_factory):
     f = ctypes.CDLL(lib).cut
     f.restype = ctypes.c_int64
 
-    def run(by_keys, starts, lens, kv_heads, causal, q, blocks=152):
+    def run(by_keys, starts, lens, kv_heads, causal, q, blocks=152, n_tokens=None):
         s = np.array(starts, np.int32)
         k = None if lens is None else np.array(lens, np.int32)
-        room = 4 * blocks + kv_heads * sum(int(n) // min(q, 128) + 2 for n in np.maximum(0, np.diff(s)))
+        room = 4 * blocks + kv_heads * sum(int(n) // min(q, 128) + 2 for n in np.clip(np.diff(s.astype(np.int64)), 0, s.max()))
         out, ends = np.zeros((room, 8), np.int32), np.zeros((blocks, 4), np.int32)
         p = [x.ctypes.data_as(ctypes.c_void_p) if x is not None else None for x in (s, k, out, ends)]
-        n = f(int(by_keys), p[0], p[1], len(s) - 1, int(s[-1]), kv_heads, int(lens is not None), 1 << 28, int(causal), q, blocks, p[2],
+        n = f(int(by_keys), p[0], p[1], len(s) - 1, int(s[-1]) if n_tokens is None else n_tokens, kv_heads, int(lens is not None), 1 << 28, int(causal), q, blocks, p[2],
               ctypes.c_int64(room), p[3])
         assert n <= room
         return out[:n], ends
@@ -157,3 +157,13 @@ def test_every_tile_is_one_blocks(cut):
         load = np.bincount(got[:, 0], got[:, 5] - got[:, 4], minlength=case[6])
         total = sum(want.values()) + 2 * len(want)
         assert load.max(initial=0) <= total / case[6] + 4, case
+
+
+def test_starts_at_the_ends_of_their_type(cut):
+    """What lies between starts that are far out of range has no rows beyond the call's."""
+    low, high = -2**31, 2**31 - 1
+    for by_keys in (False, True):
+        for starts, want in (([0, 30, low, 40], {0: 30, 2: 40}), ([low, 30, 80], {0: 30, 1: 50}), ([0, high, low, high], {0: 80, 2: 80}),
+                             ([high, low, 80], {1: 80}), ([30, low, low], {})):
+            got, _ = cut(by_keys, starts, None, 2, True, 64, n_tokens=80)
+            assert {int(b): int(n) for b, n in got[:, [1, 7]]} == want, starts
