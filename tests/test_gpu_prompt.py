@@ -334,6 +334,20 @@ def test_large_and_equal_scores():
         check(lse, w_lse, b_lse, ("lse", scale))
 
 
+def test_starts_at_the_ends_of_their_type():
+    """Sequences stay within the call whatever the numbers are; the ones whose starts are good are worked out as ever."""
+    low, high = -2**31, 2**31 - 1
+    q, k, v, _ = problem(2, [30, 50], 4, 2, 64, "bfloat16")
+    want = serving.prompt_attention(q, k, v, ints([0, 30, 80]))
+    for bad, rows in (([0, 30, low], slice(0, 30)), ([low, 30, 80], slice(30, 80)), ([high, low, low], slice(0, 0)), ([0, 30, high], slice(0, 80))):
+        status = ints([0])
+        out, lse = serving.prompt_attention(q, k, v, ints(bad), status=status)
+        assert int(status) == gts.GTS_ERR_INVALID_PARAMS, bad
+        assert torch.equal(out[rows], want[0][rows]) and torch.equal(lse[rows], want[1][rows]), bad
+        got = serving.prompt_attention_grad(out, q, k, v, out, lse, ints(bad))
+        assert all(torch.isfinite(x).all() for x in got), bad
+
+
 def test_starts_out_of_range_are_clamped():
     q, k, v, starts = problem(1, [30, 50], 4, 2, 64, "bfloat16")
     for bad, good in (([-5, 30, 80], [0, 30, 80]), ([0, 30, 1 << 30], [0, 30, 80]), ([0, 30, 20], [0, 30, 30])):
