@@ -582,7 +582,8 @@ _NO_HEADS = (0, 0, 0)
 
 
 def prompt_workspace(q, k, starts, stream=None):
-    """A workspace for ``prompt_attention`` calls of this shape; calls that may run at the same time need one each."""
+    """A workspace for ``prompt_attention`` calls of this shape; calls that may run at the same time need one each, and one that a
+    captured call was given lives as long as the graph."""
     T, heads, dim = q.shape
     need = _load().gts_prompt_workspace_bytes(_PROMPT.pack(
         _sequences(starts), T, heads, k.shape[1], dim, _DTYPES.get(q.dtype, -1), 0, 0, 1.0, 0, *(5 * _NO_HEADS), 0, 0, 0, 0))
@@ -704,7 +705,8 @@ def _chunk_bytes(shape, cache_values, max_pages):
 
 
 def chunk_workspace(q, starts, cache, page_table, stream=None):
-    """A workspace for ``chunk_attention`` calls of this shape; calls that may run at the same time need one each."""
+    """A workspace for ``chunk_attention`` calls of this shape; calls that may run at the same time need one each, and one that a
+    captured call was given lives as long as the graph."""
     need = _chunk_bytes((_sequences(starts), *q.shape[:2]), cache._descriptor(), page_table.shape[1])
     return _empty(max(need, 16), torch.uint8, q.device, stream)
 

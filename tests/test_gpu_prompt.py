@@ -557,7 +557,7 @@ def test_graphs_follow_starts_and_lengths():
         with torch.cuda.graph(g, stream=side):
             got = (serving.chunk_attention(**p, workspace=ws), serving.prompt_attention(q, k, v, at),
                    serving.prompt_attention_grad(q, q, k, v, out, lse, at))
-        graphs.append((g, got))
+        graphs.append((g, got, ws))                      # (a replay writes to the workspace: it lives as long as the graph)
     for step in (0, 1, 2):
         if step == 1:
             p["lens"].copy_(ints([800, 30, 100])), p["starts"].copy_(ints([0, 100, 110, 300])), at.copy_(ints([0, 10, 600, 900]))
@@ -568,11 +568,11 @@ def test_graphs_follow_starts_and_lengths():
             out.copy_(o), lse.copy_(l)
         want = serving.chunk_attention(**p), (o, l), serving.prompt_attention_grad(q, q, k, v, out, lse, at)
         torch.cuda.synchronize()
-        for (g, _), s in zip(graphs, (side, torch.cuda.current_stream())):
+        for (g, _, _), s in zip(graphs, (side, torch.cuda.current_stream())):
             with torch.cuda.stream(s):
                 g.replay()
         torch.cuda.synchronize()
-        for _, got in graphs:
+        for _, got, _ in graphs:
             for x, y in zip(got, want):
                 assert all(torch.equal(a, b) for a, b in zip(x, y))
 
