@@ -155,7 +155,8 @@ gts_status gts_prompt_attention(const gts_prompt_desc *desc, void *stream);
 size_t gts_prompt_workspace_bytes(const gts_prompt_desc *desc);
 
 /* The gradients of gts_prompt_attention: forward is its desc, with out, lse and, where given, low as it left them (they are read;
- * its workspace is this call's).  Without low, e_i below has the rounding of out in it, of all its errors the one that adds up.  With p_ij = exp(s_ij - lse_i), e_i = sum_d dout_id (out_id + low_id) - dlse_i and ds_ij = p_ij (dout_i . v_j - e_i):
+ * its workspace is this call's).  Without low, e_i below has the rounding of out in it, of all its errors the one that adds up.
+ * With p_ij = exp(s_ij - lse_i), e_i = sum_d dout_id (out_id + low_id) - dlse_i and ds_ij = p_ij (dout_i . v_j - e_i):
  *   dv_j = sum_i p_ij dout_i,   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,
  * those of a key head summed over its query heads.  Rows of no sequence are left as they are, or get 0: dq, dk, dv with
  * bits 0, 1, 2 of forward.zero_rest.

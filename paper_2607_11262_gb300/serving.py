@@ -669,8 +669,8 @@ def prompt_attention(q, k, v, starts, causal=True, scale=None, out=None, lse=Non
 def prompt_attention_grad(dout, q, k, v, out, lse, starts, causal=True, scale=None, dlse=None, low=None, out_dq=None, out_dk=None,
                           out_dv=None, workspace=None, status=None, stream=None):
     """The gradients (dq, dk, dv) of ``prompt_attention`` from those of its results (``dlse`` [tokens, heads] float32, default none);
-    ``out``, ``lse`` and ``low`` are what it gave (without ``low`` dq and dk are 4 to 10% less exact).  Every sum has one order, so results repeat bit for bit.  Rows of no sequence get
-    zeros; those of a given output are left as they are.  ``workspace``: of gts_prompt_grad_workspace_bytes, by default the call's own."""
+    ``out``, ``lse`` and ``low`` are what it gave (without ``low`` dq and dk are 4 to 10% less exact).  Every sum has one order, so
+    results repeat bit for bit.  Rows of no sequence get zeros; those of a given output are left as they are.  ``workspace``: of gts_prompt_grad_workspace_bytes, by default the call's own."""
     shape, qs, ks, vs, device, starts_at = _prompt_shape(q, k, v, starts)
     handle = _handle(stream, device)
     T, heads = shape[1:3]
