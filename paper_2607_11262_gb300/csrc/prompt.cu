@@ -847,6 +847,11 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           // above, before both threads of a row agree to go on)
           const uint32_t *const bad = bad_rows + (tiles + j) % 4 * 4;
           if (bad[0] | bad[1] | bad[2] | bad[3]) {
+            if (APART && j == 0 && items_done) {           // the other warp of these rows may still read sums of the item before
+              wait(o_free(h), items_done - 1);
+              if (!alive) break;
+              tc_after();
+            }
 #pragma unroll 1
             for (int c = APART ? 0 : y * (D / 2); c < (APART ? D : (y + 1) * (D / 2)); c += 16) {
               uint32_t o[16];
