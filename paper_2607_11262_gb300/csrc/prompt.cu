@@ -756,12 +756,13 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
     const bool aligned = rows_aligned(a.out), low_aligned = rows_aligned(a.low);
     const int in_half = r / a.in_group, head_in = r - in_half * a.group;
     float *const mine = tops + (h * 2 + y) * 128 + r, *const others = tops + (h * 2 + !y) * 128 + r;
-    // The two warps of the same rows exchange a value each; NaN says that a wait ran out, so that both go on or both leave: this
-    // barrier has no limit of its own.
+    // The two warps of the same rows exchange a value each.  Their barrier has no limit of its own, so each also says whether a wait of
+    // its ran out, and both go on or both leave: neither leaves on what it alone knows.  (A tile's exchange without its first barrier, as
+    // scores come only after both have read the last one's, takes 1 to 2% less for 16384 tokens, but scores may also be given up.)
     auto meet = [&] { asm volatile("bar.sync %0, 64;" ::"r"(1 + h * 4 + warp % 4) : "memory"); };
-    auto exchange = [&](float x) {
+    auto exchange = [&](float x, float ran_out = NAN) {  // (a value that x never has)
       meet();                                            // what was there has been read
-      *mine = alive ? x : NAN;
+      *mine = alive ? x : ran_out;
       meet();
       return *others;
     };
@@ -814,10 +815,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
         if (cleaned) wait(ready(tiles + j), (tiles + j) / 4);
         float big = fmaxf(top[0], top[1]);
         if (!APART) {
-          if (j == 0) meet();                              // (later on the other one has read what was there: the scores were asked for
-          *mine = alive ? big : NAN;                       // after its weights)
-          meet();
-          const float theirs = *others;
+          const float theirs = exchange(big);
           alive = alive && !isnan(theirs);                 // (a maximum is none)
           big = fmaxf(big, theirs);
         }
@@ -918,8 +916,10 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
         l = l * mine_f + l1 * their_f, m = to == -3e38f ? -INFINITY : to;
         f0 = y ? their_f : mine_f, f1 = y ? mine_f : their_f;
       } else {
+        const float l1 = exchange(l, -1.f);                // (a sum is not negative; it may be NaN)
+        alive = alive && !(l1 < 0.f);
         if (!alive) break;                                 // (both)
-        l += exchange(l);
+        l += l1;
       }
       tiles += i.tile1 - i.tile0;
       const int64_t part = ((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 256 + h * 128 + r;
