@@ -1625,10 +1625,11 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
   Stretch line = find_stretch<false, GRAD_THREADS>(a, items, cut.blocks, scratch);
   if (line.rest_from + a.n_tokens - line.rest_to > 0 && a.zero_rest & 1) zero_rest<T>(a, a.dq, a.q_heads, D, line);
   if (tid == 0) cut.ends[blockIdx.x] = make_int4(NOTHING, 0, 0, 0);
-  if (line.x0 >= line.x1) {
-    if (blockIdx.x == 0) wait_for_kernels_before();
-    return;
-  }
+  // k_grad_kv has waited for e, but what lets this grid see it is a wait of its own.  Every thread waits here, before any wait that has a
+  // limit (a block of k_grad_kv may take longer than another one by more than that), and every block does, so that the joining kernel
+  // needs to wait for one kernel only.
+  wait_for_kernels_before();
+  if (line.x0 >= line.x1) return;
   const float factor = ds_factor<T>(largest, scratch);
   if (tid == 0) {
     for (int s = 0; s < 8; s++) bar_init(full(s), 1);
@@ -1880,7 +1881,6 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
       }
     }
   }
-  if (blockIdx.x == 0) wait_for_kernels_before();        // so that the joining kernel needs to wait for one kernel only
   if (warp == ROW_WARPS) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
 }
 
@@ -2054,7 +2054,7 @@ cudaError_t backward(const Args &a, const GradPlan &p, const GradMaps &maps, cud
   const Items<false> by_rows = {queries, a.causal};
   const float *const largest = p.largest;
   e = launch_kernel(k_delta<T, D>, DELTA_BLOCKS, DELTA_THREADS, 0, s, false, a, p.largest);
-  // each may start while the one before it ends: the first waits for e, the second for nothing, the third for both
+  // each may start while the one before it ends, and waits for all of it before it reads what that, or one before, has written
   if (e == cudaSuccess) e = launch_kernel(k_grad_kv<T, D>, SMS, GRAD_THREADS, GradKv<D>::SMEM, s, true, a, by_keys, p.kv, largest, maps);
   if (e == cudaSuccess) e = launch_kernel(k_grad_q<T, D>, SMS, GRAD_THREADS, GradQ<D>::SMEM, s, true, a, by_rows, p.q, largest, maps);
   if (e == cudaSuccess && a.n_tokens > queries)          // (else no item has more than a tile)
