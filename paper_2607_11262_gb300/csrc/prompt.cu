@@ -1089,9 +1089,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join(const Args a, const Items
 // 32 heads on 8 of 128, causal: one sequence of 16384 tokens 5.45 ms (1.0 PFLOP/s of the five products, 1.4 of the seven that are done),
 // 24 of 1024 780 us, 8 of 512 to 4096 1.31 ms.  The three kernels start while the one before ends (1024 tokens: 67 us).
 //
-// float16 is short of small numbers: weights are held times 2^10 and ds times the power of two that puts the largest |dout| of the
-// call between 1/2 and 1 (then |ds| stays below 256 times the largest |v|, and what is lost below 2^-24 of it does not
-// count beside the largest).  bfloat16 has the range of 32 bits and needs neither.
+// float16 is short of numbers: weights are held times 2^10, and ds times the power of two that puts a bound of the call's |ds| between
+// 2^14 and 2^15, below its largest number by a factor of two.  As p <= 1 and out is a mean of values, |ds_ij| = p_ij |dout_i . v_j - dout_i .
+// out_i + dlse_i| <= 2 max |dout_i| max |v_j| + max |dlse_i|, with Euclidean norms of rows, over the rows of all sequences; what
+// is lost is 2^-39 of that at most, below 2^-14.  bfloat16 has the range of 32 bits and needs neither.
 constexpr int GRAD_THREADS = BLOCK_THREADS, DELTA_BLOCKS = 1216, DELTA_THREADS = 256;
 template <typename T> constexpr float WEIGHT_SHIFT = std::is_same<T, __half>::value ? 10.f : 0.f;
 template <typename T> constexpr float WEIGHT_UNIT = std::is_same<T, __half>::value ? 0x1p-10f : 1.f;
@@ -1103,10 +1104,27 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b) {
   return y;
 }
 
-// e_i = dout_i . out_i - dlse_i of the rows that belong to sequences, and each block's largest finite |dout|.  Bound by memory.
+// What the finite values of sequences' rows reach: squares of the norms of dout's and of v's rows, and |dlse|, the largest of each block.
+struct Largest { float dout, v, dlse; };
+__device__ __forceinline__ Largest most_of(const Largest &x, const Largest &y) { return {fmaxf(x.dout, y.dout), fmaxf(x.v, y.v), fmaxf(x.dlse, y.dlse)}; }
+__device__ __forceinline__ Largest most_of_warp(Largest x) {
+#pragma unroll
+  for (int o = 16; o; o /= 2) x = most_of(x, {__shfl_xor_sync(~0u, x.dout, o), __shfl_xor_sync(~0u, x.v, o), __shfl_xor_sync(~0u, x.dlse, o)});
+  return x;
+}
+// The power of two that ds is held times, as its exponent (at most 100, so that 32 bits hold it and what it multiplies).
+__device__ __forceinline__ int ds_exponent(const Largest &x) {
+  const float bound = fminf(2.f * sqrtf(x.dout) * sqrtf(x.v) + x.dlse, 0x1.fffffep127f);
+  int e = 15;
+  if (bound > 0.f) frexpf(bound, &e);                  // bound < 2^e
+  return min(100, 15 - e);
+}
+
+// e_i = dout_i . out_i - dlse_i of the rows that belong to sequences, and in float16 what bounds ds.  Bound by memory.
 template <typename T, int D>
-__global__ void __launch_bounds__(DELTA_THREADS) k_delta(const Args a, float *largest) {
+__global__ void __launch_bounds__(DELTA_THREADS) k_delta(const Args a, Largest *largest) {
   constexpr int PER = D / 8;                           // lanes of a row
+  constexpr bool HALF = std::is_same<T, __half>::value;
   __shared__ int ends[2];
   dependents_may_start();
   if (threadIdx.x == 0) ends[0] = a.n_tokens, ends[1] = 0;
@@ -1120,11 +1138,11 @@ __global__ void __launch_bounds__(DELTA_THREADS) k_delta(const Args a, float *la
   const bool aligned = (((uintptr_t)a.dout.data >> 1 | (uintptr_t)a.out.data >> 1 | (uintptr_t)a.low.data >> 1 | a.dout.tok | a.dout.head | a.out.tok | a.out.head |
                          a.low.tok | a.low.head) & 7) == 0;
   const int c = threadIdx.x % PER;
-  float most = 0.f;
+  Largest most = {0.f, 0.f, 0.f};
   const int64_t rows = (int64_t)(to - from) * a.q_heads;
   for (int64_t first = (int64_t)blockIdx.x * (DELTA_THREADS / PER); first < rows; first += (int64_t)gridDim.x * (DELTA_THREADS / PER)) {
     const int64_t r = first + threadIdx.x / PER;
-    float sum = 0.f;
+    float sum = 0.f, square = 0.f;
     if (r < rows) {
       const int64_t token = quotient(r, a.q_heads) + from;
       const int head = (int)(r - (token - from) * a.q_heads);
@@ -1139,45 +1157,69 @@ __global__ void __launch_bounds__(DELTA_THREADS) k_delta(const Args a, float *la
       for (int i = 0; i < 8; i++) {
         const float w = widen(e[i]);
         sum += w * (widen(f[i]) + widen(g[i]));
-        if (isfinite(w)) most = fmaxf(most, fabsf(w));
+        if (HALF && isfinite(w)) square += w * w;
       }
     }
 #pragma unroll
-    for (int o = PER / 2; o; o /= 2) sum += __shfl_xor_sync(~0u, sum, o);
+    for (int o = PER / 2; o; o /= 2) {
+      sum += __shfl_xor_sync(~0u, sum, o);
+      if (HALF) square += __shfl_xor_sync(~0u, square, o);
+    }
+    if (HALF) most.dout = fmaxf(most.dout, square);
     if (r < rows && c == 0) {
       const int64_t at = (int64_t)from * a.q_heads + r;
-      a.delta[at] = sum - (a.dlse ? a.dlse[at] : 0.f);
+      const float dl = a.dlse ? a.dlse[at] : 0.f;
+      if (HALF && isfinite(dl)) most.dlse = fmaxf(most.dlse, fabsf(dl));
+      a.delta[at] = sum - dl;
     }
   }
-  if (std::is_same<T, __half>::value) {
-    __shared__ float warps[DELTA_THREADS / 32];
+  if (HALF) {
+    const bool v_aligned = (((uintptr_t)a.v.data >> 1 | a.v.tok | a.v.head) & 7) == 0;
+    const int64_t v_rows = (int64_t)(to - from) * a.kv_heads;
+    for (int64_t first = (int64_t)blockIdx.x * (DELTA_THREADS / PER); first < v_rows; first += (int64_t)gridDim.x * (DELTA_THREADS / PER)) {
+      const int64_t r = first + threadIdx.x / PER;
+      float square = 0.f;
+      if (r < v_rows) {
+        const int64_t token = quotient(r, a.kv_heads);
+        const T *x = row_at<const T>(a.v, token + from, (int)(r - token * a.kv_heads)) + c * 8;
+        const uint4 u = v_aligned ? *(const uint4 *)x : gather16(x);
+        T e[8];
+        memcpy(e, &u, 16);
 #pragma unroll
-    for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+        for (int i = 0; i < 8; i++) {
+          const float w = widen(e[i]);
+          if (isfinite(w)) square += w * w;
+        }
+      }
+#pragma unroll
+      for (int o = PER / 2; o; o /= 2) square += __shfl_xor_sync(~0u, square, o);
+      most.v = fmaxf(most.v, square);
+    }
+    __shared__ Largest warps[DELTA_THREADS / 32];
+    most = most_of_warp(most);
     if (threadIdx.x % 32 == 0) warps[threadIdx.x / 32] = most;
     __syncthreads();
     if (threadIdx.x == 0) {
-      for (int w = 0; w < DELTA_THREADS / 32; w++) most = fmaxf(most, warps[w]);
+      for (int w = 0; w < DELTA_THREADS / 32; w++) most = most_of(most, warps[w]);
       largest[blockIdx.x] = most;
     }
   }
 }
 
-// The power of two that ds is held times: of the largest |dout| all threads of the block look for.
-template <typename T> __device__ __forceinline__ float ds_factor(const float *largest, void *scratch) {
+// The factor of ds, from what bounds it: all threads of the block look.
+template <typename T> __device__ __forceinline__ float ds_factor(const Largest *largest, void *scratch) {
   if (!std::is_same<T, __half>::value) return 1.f;
-  float *const warps = (float *)scratch;
+  static_assert(GRAD_THREADS / 32 * sizeof(Largest) <= SCRATCH, "room for the warps' largest");
+  Largest *const warps = (Largest *)scratch;
   __syncthreads();
-  float most = 0.f;
-  for (int i = threadIdx.x; i < DELTA_BLOCKS; i += GRAD_THREADS) most = fmaxf(most, largest[i]);
-#pragma unroll
-  for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+  Largest most = {0.f, 0.f, 0.f};
+  for (int i = threadIdx.x; i < DELTA_BLOCKS; i += GRAD_THREADS) most = most_of(most, largest[i]);
+  most = most_of_warp(most);
   if (threadIdx.x % 32 == 0) warps[threadIdx.x / 32] = most;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < GRAD_THREADS / 32; w++) most = fmaxf(most, warps[w]);
-  int e = 0;
-  if (most > 0.f) frexpf(most, &e);
-  return ldexpf(1.f, -e);
+  for (int w = 0; w < GRAD_THREADS / 32; w++) most = most_of(most, warps[w]);
+  return ldexpf(1.f, ds_exponent(most));
 }
 
 // Maps of the rows of queries (or of dout): a box is the `group` heads of a key head of `q` tokens; of keys and values.
@@ -1235,7 +1277,7 @@ template <int D> struct GradKv {
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const Items<true> items, const Cut cut, const float *largest, const __grid_constant__ GradMaps maps) {
+__global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const Items<true> items, const Cut cut, const Largest *largest, const __grid_constant__ GradMaps maps) {
   constexpr int BYTES = GradKv<D>::BYTES, STAGES = GradKv<D>::STAGES, STATS = GradKv<D>::STATS, COLUMNS = TILE * 128;
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char *const kv = smem, *const ring = kv + 2 * BYTES;
@@ -1598,7 +1640,7 @@ template <int D> struct GradQ {
 };
 
 template <typename T, int D>
-__global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const Items<false> items, const Cut cut, const float *largest, const __grid_constant__ GradMaps maps) {
+__global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const Items<false> items, const Cut cut, const Largest *largest, const __grid_constant__ GradMaps maps) {
   constexpr int BYTES = GradQ<D>::BYTES, STAGES = GradQ<D>::STAGES, COLUMNS = TILE * 128;
   extern __shared__ __align__(1024) unsigned char smem[];
   unsigned char *const rows = smem, *const ring = rows + 2 * BYTES;
@@ -1886,7 +1928,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_q(const Args a, const 
 
 // Sums of the parts of items that were cut, in their order: a thread for a row and an eighth of its columns.
 template <typename T, int D, bool BY_KEYS>
-__device__ __forceinline__ void join_grad(const Args &a, const Items<BY_KEYS> &items, const Cut &cut, const float *largest, int block) {
+__device__ __forceinline__ void join_grad(const Args &a, const Items<BY_KEYS> &items, const Cut &cut, const Largest *largest, int block) {
   constexpr int ROWS = BY_KEYS ? 2 * TILE : TILE, E = D / 32;   // (keys' gradients after values')
   const int c = block / (ROWS / 32), lane = threadIdx.x % 32, column = threadIdx.x / 32;
   const int4 end = cut.ends[c];
@@ -1897,13 +1939,9 @@ __device__ __forceinline__ void join_grad(const Args &a, const Items<BY_KEYS> &i
   if (BY_KEYS && which == 0) {
     f = WEIGHT_UNIT<T>;
   } else if (std::is_same<T, __half>::value) {
-    float most = 0.f;
-    for (int i = lane; i < DELTA_BLOCKS; i += 32) most = fmaxf(most, largest[i]);
-#pragma unroll
-    for (int o = 16; o; o /= 2) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
-    int e = 0;
-    if (most > 0.f) frexpf(most, &e);
-    f = ldexpf(f, e);
+    Largest most = {0.f, 0.f, 0.f};
+    for (int i = lane; i < DELTA_BLOCKS; i += 32) most = most_of(most, largest[i]);
+    f = ldexpf(f, -ds_exponent(most_of_warp(most)));
   }
   const int in_tile = BY_KEYS ? 0 : r / a.in_group, at = BY_KEYS ? end.z * TILE + r : end.z * items.q + in_tile;
   if (at >= s.n || (!BY_KEYS && in_tile >= items.q)) return;
@@ -1933,7 +1971,7 @@ __device__ __forceinline__ void join_grad(const Args &a, const Items<BY_KEYS> &i
 
 constexpr int JOIN_KV = SMS * (2 * TILE / 32), JOIN_Q = SMS * (TILE / 32);   // its blocks
 template <typename T, int D>
-__global__ void __launch_bounds__(JOIN_THREADS) k_join_grad(const Args a, const Items<true> by_keys, const Items<false> by_rows, const Cut kv, const Cut q, const float *largest) {
+__global__ void __launch_bounds__(JOIN_THREADS) k_join_grad(const Args a, const Items<true> by_keys, const Items<false> by_rows, const Cut kv, const Cut q, const Largest *largest) {
   wait_for_kernels_before();
   if (blockIdx.x < JOIN_KV) join_grad<T, D, true>(a, by_keys, kv, largest, blockIdx.x);
   else join_grad<T, D, false>(a, by_rows, q, largest, blockIdx.x - JOIN_KV);
@@ -2001,10 +2039,11 @@ cudaError_t run_forward(const Args &a, FwdMaps &maps, int32_t dtype, uint32_t di
   return dim == 64 ? forward<__half, 64>(a, maps, most, w, s) : forward<__half, 128>(a, maps, most, w, s);
 }
 
-// The gradients' workspace: e of every row, each block's largest |dout|, partial results, and q, dout, k, v where TMA cannot take
+// The gradients' workspace: e of every row, what bounds ds in float16, partial results, and q, dout, k, v where TMA cannot take
 // them as they lie.
 struct GradPlan {
-  float *delta, *largest;
+  float *delta;
+  Largest *largest;
   Cut kv, q;
   char *copy[4];
   size_t bytes;
@@ -2018,7 +2057,7 @@ GradPlan plan_grad(const gts_prompt_grad_desc &d, const bool (&copied)[4], char 
     return x;
   };
   p.delta = (float *)take((size_t)f.n_tokens * f.q_heads * sizeof(float));
-  p.largest = (float *)take(DELTA_BLOCKS * sizeof(float));
+  p.largest = (Largest *)take(DELTA_BLOCKS * sizeof(Largest));
   p.kv.blocks = p.q.blocks = SMS;
   p.kv.ends = (int4 *)take(SMS * sizeof(int4)), p.q.ends = (int4 *)take(SMS * sizeof(int4));
   p.kv.o = (float4 *)take((size_t)SMS * 2 * 2 * TILE * f.head_dim * sizeof(float));
@@ -2052,7 +2091,7 @@ cudaError_t backward(const Args &a, const GradPlan &p, const GradMaps &maps, cud
   const int queries = TILE / a.group;
   const Items<true> by_keys = {queries, a.causal};
   const Items<false> by_rows = {queries, a.causal};
-  const float *const largest = p.largest;
+  const Largest *const largest = p.largest;
   e = launch_kernel(k_delta<T, D>, DELTA_BLOCKS, DELTA_THREADS, 0, s, false, a, p.largest);
   // each may start while the one before it ends, and waits for all of it before it reads what that, or one before, has written
   if (e == cudaSuccess) e = launch_kernel(k_grad_kv<T, D>, SMS, GRAD_THREADS, GradKv<D>::SMEM, s, true, a, by_keys, p.kv, largest, maps);
