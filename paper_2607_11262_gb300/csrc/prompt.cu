@@ -1447,6 +1447,11 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
 #pragma unroll
             for (int k = 0; k < 4; k++) bad_rows[tiles % STATS * 4 + k] = bad[k];
           }
+          if (which && (bad[0] | bad[1] | bad[2] | bad[3])) {   // their ds is NaN, dv gets what the tile has lost at the item's end
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+              if (bad[k] >> lane & 1) stats[(tiles % STATS * 2 + 1) * TILE + lane + k * 32] = NAN;
+          }
           __syncwarp();
           if (lane == 0) bar_arrive(ready(slot));
         }
@@ -1515,6 +1520,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
     Item i;
     while (next_all(i)) {
       const int key = i.t * TILE + r;
+      bool odd = false;                                         // whether dout's tiles have lost infinite and NaN values
       for (int t = i.tile0; t < i.tile1; t++, tiles++) {
         const int q0 = first_query(i, t);
         const bool masked = hides(i, q0);
@@ -1539,10 +1545,10 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
         }
         need(ready(2 * tiles + 1), tiles / 4);                  // (e)
         if (masked) {
-          // (dout has lost its infinite and NaN values here: weights of rows that had some become NaN)
-          const uint32_t bad = bad_rows[tiles % STATS * 4 + w];
+          const uint32_t *const bad = bad_rows + tiles % STATS * 4;
+          odd |= (bad[0] | bad[1] | bad[2] | bad[3]) != 0;
 #pragma unroll
-          for (int c = 0; c < 32; c++) p[c] = c < first_seen ? 0 : bad >> c & 1 ? 0x7FFFFFFFu : p[c];
+          for (int c = 0; c < 32; c++) p[c] = c < first_seen ? 0 : p[c];
         }
 #pragma unroll
         for (int c = 0; c < 32; c += 2) pk[c / 2] = pack<T>(__uint_as_float(p[c]), __uint_as_float(p[c + 1]));
@@ -1585,6 +1591,34 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) k_grad_kv(const Args a, const
       if (!alive) break;
       done++;
       tc_after();
+      if (w < 2 && __any_sync(~0u, odd)) {
+        // dout's values that are not finite, from tiles that hide rows from some keys: each for the keys that its row sees
+#pragma unroll 1
+        for (int c = 0; c < D / 2; c += 16) {
+          uint32_t o[16];
+          const uint32_t at = dv_at + lanes + w * (D / 2) + c;
+          tc_ld16(o, at);
+          tc_ld_wait();
+#pragma unroll 1
+          for (int t = i.tile0; t < i.tile1 && hides(i, first_query(i, t)); t++) {
+            const int q0 = first_query(i, t), live = min(items.q, i.n - q0) * a.group;
+#pragma unroll 1
+            for (int x = 0; x < live; x++) {
+              const int query = q0 + x / a.in_group, head = i.kh * a.group + x % a.in_group;
+              if (query < key || isfinite(a.delta[((int64_t)i.first + query) * a.q_heads + head])) continue;
+              const T *const from = row_at<const T>(a.dout, (int64_t)i.first + query, head) + w * (D / 2) + c;
+#pragma unroll
+              for (int z = 0; z < 16; z++) {
+                const float v = widen(from[z]);
+                if (!isfinite(v)) o[z] = __float_as_uint(__uint_as_float(o[z]) + v);
+              }
+            }
+          }
+          __syncwarp();
+          tc_st16(at, o);
+          tc_st_wait();
+        }
+      }
       const bool whole = i.tile0 == 0 && i.tile1 == i.tiles;
       float4 *const part = whole ? nullptr : cut.o + ((((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 2 + w / 2) * (D / 4) + w % 2 * (D / 8)) * TILE + r;
       store_row<T, D / 2>((w < 2 ? dv_at : dk_at) + lanes + w % 2 * (D / 2), row_at<T>(to, (int64_t)i.first + key, i.kh) + w % 2 * (D / 2), part, key < i.keys,
