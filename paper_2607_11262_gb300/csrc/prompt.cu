@@ -67,7 +67,6 @@ constexpr int NOTHING = -1;
 
 struct Cut {
   int blocks;
-  int queries;           // of an item of rows (two halves of them); of a tile of rows
   int4 *ends;            // [blocks]: the item that begins in a block and goes on: sequence (or NOTHING), key head, item, further blocks
   float4 *o;             // [blocks][2][D / 4][rows of an item]: parts of the item that began before (0) and of the one that goes on (1)
   float2 *ml;            // [blocks][2][rows]: maximum (of log2 scores) and sum
@@ -2039,14 +2038,14 @@ bool rows_map(CUtensorMap &map, const Heads &h, int heads, int tokens, int dim, 
 }
 
 // The forward pass's workspace.
-size_t plan(Cut &c, int dim, int queries, char *at) {
+size_t plan(Cut &c, int dim, char *at) {
   size_t n = 0;
   auto take = [&](size_t bytes) {
     char *x = at ? at + n : nullptr;
     n += up(bytes);
     return x;
   };
-  c.blocks = SMS, c.queries = queries;
+  c.blocks = SMS;
   c.ends = (int4 *)take(SMS * sizeof(int4));
   c.ml = (float2 *)take((size_t)SMS * 2 * 256 * sizeof(float2));
   c.o = (float4 *)take((size_t)SMS * 2 * 256 * dim * sizeof(float));
@@ -2060,7 +2059,7 @@ cudaError_t forward(const Args &a, const FwdMaps &maps, int64_t most_keys, char 
   if (e != cudaSuccess) return e;
   Cut cut;
   const Items<false> items = {2 * (128 / a.group), a.causal};
-  plan(cut, D, items.q, workspace);
+  plan(cut, D, workspace);
   e = launch_kernel(k_forward<T, D>, cut.blocks, FWD_THREADS, Fwd<D>::SMEM, s, false, a, items, cut, maps);
   if (e != cudaSuccess || most_keys <= TILE) return e;   // (items of one tile are not cut)
   return launch_kernel(k_join<T, D>, cut.blocks * JOIN_BLOCKS, JOIN_THREADS, 0, s, true, a, items, cut);
@@ -2226,9 +2225,9 @@ const char *refuse_shape(const gts_chunk_desc &d) {
 
 }  // namespace
 
-extern "C" size_t gts_prompt_workspace_bytes(const gts_prompt_desc *d) { 
+extern "C" size_t gts_prompt_workspace_bytes(const gts_prompt_desc *d) {
   Cut c;
-  return !d || refuse_shape(*d) ? 0 : plan(c, (int)d->head_dim, 0, nullptr);
+  return !d || refuse_shape(*d) ? 0 : plan(c, (int)d->head_dim, nullptr);
 }
 
 extern "C" gts_status gts_prompt_attention(const gts_prompt_desc *d, void *stream) {
@@ -2276,9 +2275,9 @@ extern "C" gts_status gts_prompt_attention_grad(const gts_prompt_grad_desc *d, v
   return e == cudaSuccess ? GTS_OK : gts::cuda_fail(e, "attention: launch");
 }
 
-extern "C" size_t gts_chunk_workspace_bytes(const gts_chunk_desc *d) { 
+extern "C" size_t gts_chunk_workspace_bytes(const gts_chunk_desc *d) {
   Cut c;
-  return !d || refuse_shape(*d) ? 0 : plan(c, (int)d->cache.head_dim, 0, nullptr);
+  return !d || refuse_shape(*d) ? 0 : plan(c, (int)d->cache.head_dim, nullptr);
 }
 
 extern "C" gts_status gts_chunk_attention(const gts_chunk_desc *d, void *stream) {
