@@ -384,7 +384,8 @@ __device__ __forceinline__ void clean_tile(unsigned char *tile, int lane, int li
 // The halves alternate: while one turns scores into weights, the tensor cores work for the other.  An item's first scores are
 // worked out, and its queries brought, while the rows of the one before store their results.  The maximum that scores are taken against is
 // raised, and what was summed rescaled, only when it has grown by more than 8 (in log 2).  Weights are rounded to the values'
-// type for their product; the sum is of the unrounded ones, all else is in 32 bits.
+// type for their product; the sum is of the unrounded ones, all else is in 32 bits.  In float16 both are held times 2^7, so that weights
+// stay below 2^15 and lose 2^-32 of the largest one at most: many keys of little weight count (65536 of 2^-25.5 are 0.1%).
 //
 // A row's thread reads its scores twice, for the maximum and for the weights: 104 registers to a thread do not hold 64 scores.  The
 // weights of the first 32 keys of both threads are multiplied while those of the others are made (1441 against 1605 us for 16384 tokens,
@@ -399,6 +400,7 @@ __device__ __forceinline__ void clean_tile(unsigned char *tile, int lane, int li
 // (both halves are at their ends at the same time; the stores themselves are 5%).  A head of 64: 8192 tokens of 16 heads, causal, 161 us.
 constexpr int ROW_WARPS = 16, ROW_THREADS = ROW_WARPS * 32, BLOCK_THREADS = ROW_THREADS + 128, FWD_THREADS = BLOCK_THREADS, QUEUE = 4;
 constexpr float RAISE = 8.f;
+template <typename T> constexpr float HELD = std::is_same<T, __half>::value ? 7.f : 0.f;   // weights and their sum: times 2^7
 template <int D> struct Fwd {
   static constexpr bool APART = D == 64;               // sums of their own for either half of a tile's keys
   static constexpr int PIECE = APART ? 16 : 32;        // columns that a row's results are stored by (the other way round: 2% and 4% more)
@@ -838,7 +840,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
           l *= f;
           m = to;
         }
-        const float from = m == -INFINITY ? 0.f : m;
+        const float from = m == -INFINITY ? 0.f : m - HELD<T>;
         if (cleaned) {
           // values that are not finite: each for the rows that see it, before the products are added (the tile is clean: waited for
           // above, before both threads of a row agree to go on)
@@ -920,6 +922,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) k_forward(const Args a, const 
         if (!alive) break;                                 // (both)
         l += l1;
       }
+      m -= HELD<T>;
       tiles += i.tile1 - i.tile0;
       const int64_t part = ((int64_t)blockIdx.x * 2 + (i.tile0 == 0)) * 256 + h * 128 + r;
       const float inv = l == 0.f ? 0.f : 1.f / l;
