@@ -133,7 +133,9 @@ size_t gts_attention_workspace_bytes(const gts_attention_desc *desc);
  *   out = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),   lse = m + log sum_j exp(s_j - m).
  * Query head h uses key head h / (q_heads / kv_heads).  Rows of no sequence (before starts[0], from starts[n_seqs] on) are left as
  * they are, or get out = 0 (zero_rest bit 0) and lse = -infinity (bit 1); what they hold in q, k and v is not looked at.  starts
- * has to rise from 0 or more to n_tokens at most: other values are clamped to that (d_status, see above).
+ * has to rise from 0 or more to n_tokens at most: other values are clamped to that (d_status, see above).  A row whose scores are all
+ * -infinity counts as one that sees no key: out = 0, lse = -infinity; one with a score of +infinity or NaN is NaN.  Results may not
+ * overlap what the call reads.
  * Types: GTS_BF16 or GTS_F16; head_dim 64 or 128; q_heads a multiple of kv_heads, at most 128 times it; scale positive.  Products
  * are summed in 32 bits. */
 typedef struct {
@@ -160,7 +162,8 @@ size_t gts_prompt_workspace_bytes(const gts_prompt_desc *desc);
  *   dv_j = sum_i p_ij dout_i,   dq_i = scale sum_j ds_ij k_j,   dk_j = scale sum_i ds_ij q_i,
  * those of a key head summed over its query heads.  Rows of no sequence are left as they are, or get 0: dq, dk, dv with
  * bits 0, 1, 2 of forward.zero_rest.
- * Every sum has one order: results repeat bit for bit. */
+ * Every sum has one order: results repeat bit for bit.  GTS_F16 holds ds to 2^-39 of 2 max |dout_i| max |v_j| + max |dlse_i| (norms of
+ * rows, over the call).  Results may not overlap what the call reads. */
 typedef struct {
   gts_prompt_desc forward;
   gts_heads dout;
@@ -174,7 +177,7 @@ gts_status gts_prompt_attention_grad(const gts_prompt_grad_desc *desc, void *str
 size_t gts_prompt_grad_workspace_bytes(const gts_prompt_grad_desc *desc);
 
 /* Attention of chunks of new tokens over a paged cache that holds them already.  Sequence b's queries are the rows starts[b] ..
- * starts[b + 1] - 1 of q, its keys the first lens[b] tokens of its pages (page_table row b); the last query sees all of them,
+ * starts[b + 1] - 1 of q, its keys the first lens[b] tokens of its pages (page_table row b; none where lens[b] is negative); the last query sees all of them,
  * and query i those j < lens[b] - (n - 1 - i), n its sequence's queries.  A query that sees no key gets out = 0 and lse =
  * -infinity.  Otherwise as gts_prompt_attention; cache values that no query sees may be anything, NaN included. */
 typedef struct {

@@ -387,17 +387,19 @@ __device__ __forceinline__ void clean_tile(unsigned char *tile, int lane, int li
 // type for their product; the sum is of the unrounded ones, all else is in 32 bits.  In float16 both are held times 2^7, so that weights
 // stay below 2^15 and lose 2^-32 of the largest one at most: many keys of little weight count (65536 of 2^-25.5 are 0.1%).
 //
-// A row's thread reads its scores twice, for the maximum and for the weights: 104 registers to a thread do not hold 64 scores.  The
-// weights of the first 32 keys of both threads are multiplied while those of the others are made (1441 against 1605 us for 16384 tokens,
-// causal, 32 heads on 8 of 128).  At a head of 64 each of the two threads has sums and a maximum of its own, joined at the end
+// A row's thread reads its scores twice, for the maximum and for the weights: 104 registers to a thread do not hold 64 scores (as it is,
+// 240 bytes a thread are reloaded from spills at a head of 128, 308 at 64, over all paths).  The weights of the first 32 keys of both
+// threads are multiplied while those of the others are made (1470 against 1605 us for 16384 tokens, causal, 32 heads on 8 of 128).
+// At a head of 64 each of the two threads has sums and a maximum of its own, joined at the end
 // (APART): no exchange for each tile, and four streams of scores for the tensor cores instead of two.  A thread with 128 keys of
 // its own takes 1510 us there, but loses on short sequences; weights against the last tile's maximum, mended where it has grown,
 // take 10% more at a head of 128.
 //
 // Bound by the chain of a tile from scores to weights to products, and on short sequences by the ends of items.  16384 tokens of 32
 // heads on 8 of 128 without a mask: 2815 us, 1.56 PFLOP/s, 82% of the rate of a large matrix product; 2300 cycles for a tile of both
-// halves against 2048 of products.  24 sequences of 1024: 288 us causal and 376 not, of which an item's begin and end take 6 of 19 us
-// (both halves are at their ends at the same time; the stores themselves are 5%).  A head of 64: 8192 tokens of 16 heads, causal, 161 us.
+// halves against 2048 of products.  24 sequences of 1024: 289 us causal and 376 not, of which an item's begin and end take 6 of 19 us
+// (both halves are at their ends at the same time; the stores themselves are 5%).  The tensor cores are busy for 35% of the causal time, and where
+// items change so often rows wait for instructions as well as for scores.  A head of 64: 8192 tokens of 16 heads, causal, 160 us.
 constexpr int ROW_WARPS = 16, ROW_THREADS = ROW_WARPS * 32, BLOCK_THREADS = ROW_THREADS + 128, FWD_THREADS = BLOCK_THREADS, QUEUE = 4;
 constexpr float RAISE = 8.f;
 template <typename T> constexpr float HELD = std::is_same<T, __half>::value ? 7.f : 0.f;   // weights and their sum: times 2^7
@@ -1086,10 +1088,12 @@ __global__ void __launch_bounds__(JOIN_THREADS) k_join(const Args a, const Items
 // no atomic adds, and nothing of the size of the scores is ever stored.  Weights p and ds are rounded to the inputs' type for
 // their products; all else is in 32 bits.
 //
-// Bound by the rows' threads and the products of 128 weights, which want as much of shared memory as of the tensor cores: a tile of
-// k_grad_kv takes 1.33 us against 1.07 of its four products, one of k_grad_q 1.15 against 0.8 of its three (0.93 of shared memory's time).
-// 32 heads on 8 of 128, causal: one sequence of 16384 tokens 5.45 ms (1.0 PFLOP/s of the five products, 1.4 of the seven that are done),
-// 24 of 1024 780 us, 8 of 512 to 4096 1.31 ms.  The three kernels start while the one before ends (1024 tokens: 67 us).
+// Bound by the rows' threads and the products of 128 weights, which want as much of shared memory as of the tensor cores: over 4096 tokens without
+// a mask a tile of k_grad_kv takes 2960 cycles, ends of items included, against 2048 of its four products, one of k_grad_q 2460 against
+// 1536 of its three.  k_grad_kv reloads 196 to 208 bytes a thread from spills, k_grad_q none in bfloat16 and 20 in float16.
+// 32 heads on 8 of 128, causal: one sequence of 16384 tokens 5.4 ms (1.0 PFLOP/s of the five products, 1.4 of the seven that are done),
+// 24 of 1024 775 us, 8 of 512 to 4096 1.30 ms.  The kernels start while the one before ends, and wait for it before they read what it
+// wrote (1024 tokens: 66 us).
 //
 // float16 is short of numbers: weights are held times 2^10, and ds times the power of two that puts a bound of the call's |ds| between
 // 2^14 and 2^15, below its largest number by a factor of two.  As p <= 1 and out is a mean of values, |ds_ij| = p_ij |dout_i . v_j - dout_i .

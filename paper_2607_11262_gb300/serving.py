@@ -652,11 +652,13 @@ def prompt_attention(q, k, v, starts, causal=True, scale=None, out=None, lse=Non
     are the rows ``starts[b]`` .. ``starts[b + 1] - 1`` (int32 [seqs + 1], rising, on the device).  A query sees its sequence's keys
     up to its own (``causal``) or all of them; ``scale``: of the products, positive (default 1 / sqrt(head_dim)).  lse (float32
     [tokens, heads]) is the logarithm of the sum of exponentials; ``low``, a tensor like out, gets what rounding took from out, for
-    ``prompt_attention_grad``.  Rows of no sequence get zeros and lse = -inf; those
-    of a given ``out`` or ``lse`` are left as they are.  Starts out of range are clamped and store GTS_ERR_INVALID_PARAMS to ``status`` (int32 [1]
+    ``prompt_attention_grad``.  Rows of no sequence get zeros and lse = -inf, and so does a row whose visible scores are all -inf; rows of no
+    sequence of a given ``out`` or ``lse`` are left as they are.  A row that sees a score of +inf or NaN is NaN.  Results may not
+    overlap what the call reads.  Starts out of range are clamped and store GTS_ERR_INVALID_PARAMS to ``status`` (int32 [1]
     on the device), where given.  A kernel whose waits run out (after two seconds) stores GTS_ERR_STEP_LIMIT there, and its rows are NaN.
 
-    With outputs, workspace and stream left to the call, gradients flow from out and lse to q, k and v (once).  A backward pass that is
+    With outputs, workspace and stream left to the call, gradients flow from out and lse to q, k and v (once; torch.func does not go through).
+    The graph holds q, k, v, out, lse and ``low``, which is as large as out.  A backward pass that is
     captured into a graph while another graph of the same leaves lives wants that one made on the capturing stream: torch ties
     a leaf's gradient to the stream of its first use."""
     if _differentiated(q) or _differentiated(k) or _differentiated(v):
@@ -670,7 +672,9 @@ def prompt_attention_grad(dout, q, k, v, out, lse, starts, causal=True, scale=No
                           out_dv=None, workspace=None, status=None, stream=None):
     """The gradients (dq, dk, dv) of ``prompt_attention`` from those of its results (``dlse`` [tokens, heads] float32, default none);
     ``out``, ``lse`` and ``low`` are what it gave (without ``low`` dq and dk are 4 to 10% less exact).  Every sum has one order, so
-    results repeat bit for bit.  Rows of no sequence get zeros; those of a given output are left as they are.  ``workspace``: of gts_prompt_grad_workspace_bytes, by default the call's own."""
+    results repeat bit for bit.  float16: what is summed for dq and dk is held to 2^-39 of 2 max |dout_i| max |v_j| + max |dlse_i| (norms
+    of rows, over the call).  Rows of no sequence get zeros; those of a given output are left as they are.  Results may not overlap
+    what the call reads.  ``workspace``: of gts_prompt_grad_workspace_bytes, by default the call's own."""
     shape, qs, ks, vs, device, starts_at = _prompt_shape(q, k, v, starts)
     handle = _handle(stream, device)
     T, heads = shape[1:3]
@@ -716,10 +720,10 @@ def chunk_attention(q, starts, cache, page_table, lens, scale=None, out=None, ls
 
     q [tokens, heads, head_dim] holds the new tokens of all sequences, packed: those of sequence b are the rows ``starts[b]`` ..
     ``starts[b + 1] - 1`` (int32 [seqs + 1], rising).  Their keys and values are in the cache already, as the newest of the
-    sequence's first ``lens[b]`` tokens (int32) of the pages in ``page_table[b]`` (int32 [seqs, max_pages]; entries past its length
-    are not looked at): each query sees the tokens up to its own.  A query that sees nothing gets zeros and lse = -inf; so do rows
+    sequence's first ``lens[b]`` tokens (int32; a negative length is none) of the pages in ``page_table[b]`` (int32 [seqs, max_pages];
+    entries past its length are not looked at): each query sees the tokens up to its own.  A query that sees nothing gets zeros and lse = -inf; so do rows
     of no sequence, but those of a given ``out`` or ``lse`` are left as they are.  Types, scale, status and heads as in
-    ``prompt_attention``; a page number or length out of range is not followed.  ``prefix_attention`` does the same for a few tokens of each
+    ``prompt_attention``; a page number out of range or a length beyond the table is not followed.  ``prefix_attention`` does the same for a few tokens of each
     sequence, and shares a prefix."""
     cache_values = cache._descriptor()
     dtype, device = cache.dtype, cache.device
